@@ -318,6 +318,98 @@ int weight_grad_prox_update(const csrt_csr *w_in, const float *dy, const float *
 int debias_update(csrt_csr *w, const float *g_nnz, float eta, void *stream);
 
 /* ------------------------------------------------------------------------ */
+/* Dense layers (16-bit, tensor cores). The paper trains its compressed      */
+/* layers against dense ones and has no form for them; these calls are this  */
+/* library's. They keep its orientation: W is M x K, activations are         */
+/* feature-major (X is K x n, Y is M x n).                                   */
+/* ------------------------------------------------------------------------ */
+
+#define CSRT_DT_F32 0
+#define CSRT_DT_BF16 1
+#define CSRT_DT_F16 2
+
+#define CSRT_ACT_NONE 0
+#define CSRT_ACT_RELU 1
+#define CSRT_ACT_GELU 2  /* tanh form: 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
+#define CSRT_ACT_SILU 3  /* z / (1 + exp(-z)) */
+
+/* A row-major device matrix whose rows are ld elements apart (ld >= cols). */
+typedef struct csrt_mat {
+    void *data;
+    int32_t rows, cols;
+    int64_t ld;
+    int32_t dtype;   /* CSRT_DT_* */
+} csrt_mat;
+
+/* Bytes of workspace of the dense-layer calls on a layer of m outputs and k
+ * inputs with at most max_n columns. Initialise with csrt_workspace_init; the
+ * status word works as for the other calls. Host only. */
+int csrt_dense_workspace_bytes(int32_t m, int32_t k, int32_t max_n, size_t *bytes);
+
+/* csrt_dense_fwd -- y = act(W x + bias) + residual, one rounding at the end.
+ * w (M x K) and x (K x n) have one 16-bit type; the sums are float32. bias
+ * (M floats), residual (M x n, y's type) and z may be NULL; z (M x n, w's
+ * type) receives the pre-activation W x + bias. y is M x n, of w's type or
+ * float32. residual may be y itself (same data and ld); w, x, y and z must
+ * not overlap otherwise. Any sizes, n = 1 (one token) and 0 among them; rows
+ * that are 16-byte aligned (data and ld) are read and written in place by
+ * TMA, others are copied once into the workspace or stored piecewise. */
+int csrt_dense_fwd(const csrt_mat *w, const csrt_mat *x, const float *bias, int32_t act, const csrt_mat *residual,
+                   csrt_mat *z, csrt_mat *y, void *ws, size_t ws_bytes, void *stream);
+
+/* csrt_dense_bwd_x -- gradient of a layer's input from dy (M x n), the
+ * gradient of its pre-activation: dx = (W^T dy) * act'(z_below) + residual.
+ * z_below (K x n, w's type, may be NULL: no factor) is the pre-activation of
+ * the layer below, so that dx is that layer's dy; residual (K x n, dx's type,
+ * may be NULL) is the gradient that reaches x by another path. dx is K x n,
+ * of w's type or float32; residual may be dx itself. */
+int csrt_dense_bwd_x(const csrt_mat *w, const csrt_mat *dy, const csrt_mat *z_below, int32_t act,
+                     const csrt_mat *residual, csrt_mat *dx, void *ws, size_t ws_bytes, void *stream);
+
+/* csrt_dense_bwd_w -- gradients of a layer's weights and bias: dw = dy x^T
+ * (M x K) and db[i] = sum_c dy[i, c] (M floats, may be NULL), both added to
+ * what is there when accumulate != 0. No 1/n factor. dw is float32 or of dy's
+ * type; float32 sums are rounded to nearest every 512 columns (the tensor
+ * core's own accumulation truncates). */
+int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, csrt_mat *dw, float *db, void *ws,
+                     size_t ws_bytes, void *stream);
+
+/* dpre = dy * act'(z), element by element (the step from a layer's output to
+ * its pre-activation where no product above carries it); with CSRT_ACT_NONE a
+ * conversion (z may be NULL). Each matrix of any CSRT_DT_* type; dpre may be
+ * dy itself. */
+int csrt_dense_act_bwd(const csrt_mat *dy, const csrt_mat *z, int32_t act, csrt_mat *dpre, void *stream);
+
+/* w <- fl32(fl32(w * fl32(1 - eta*decay)) - fl32(eta*d)) for the float32 w;
+ * w16 (may be NULL) receives the new w rounded to its type. d is of any type.
+ * eta and decay finite and >= 0. */
+int csrt_dense_update(csrt_mat *w, const csrt_mat *d, float eta, float decay, csrt_mat *w16, void *stream);
+
+/* Workspace of csrt_orthogonalize for `batch` matrices of rows x cols. */
+int csrt_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, size_t *bytes);
+
+/* csrt_orthogonalize -- the direction of an orthogonalised update (the Muon
+ * optimiser's), for `batch` matrices of one shape:
+ *   m <- beta*m + g;  u = nesterov ? g + beta*m : m     (momentum NULL: u = g)
+ *   X = u / max(||u||_F, eps);  `steps` times  X <- a X + (b A + c A A) X
+ * with A = X X^T (products on the right, A = X^T X, where rows > cols) and
+ * (a, b, c) = (3.4445, -4.7750, 2.0315), which brings the singular values near
+ * 1;  o = scale * X.
+ * g and o are batch matrices g_stride / o_stride elements apart, float32 or
+ * bfloat16 each; momentum is float32, batch x rows x cols, contiguous, updated
+ * in place. ||u||_F is summed in float64. The products run on float16
+ * operands (11 significant bits; all matrices are scaled so that entries lie
+ * within their bounds, as singular values stay below 1.21), X is carried with
+ * 22 bits and sums are float32, so o is within about 1e-3 of the exact
+ * iteration (2-norm, relative). A matrix holding an infinity or a NaN yields
+ * NaN. o may feed prox_update_compact as the search direction of a layer's
+ * prox step. beta in [0, 1), eps > 0 and finite, 0 <= steps <= 32, batch <=
+ * 65535. o must not overlap g or momentum. */
+int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float *momentum, float beta,
+                       int32_t nesterov, int32_t steps, float eps, float scale, csrt_mat *o, int64_t o_stride,
+                       void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------ */
 /* Network glue (Caffe layers the paper uses but does not describe).         */
 /* Convolution activations are C x (B*H*W) matrices: channel, then sample,   */
 /* then row, then column.                                                    */

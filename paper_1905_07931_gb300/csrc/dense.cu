@@ -1,0 +1,355 @@
+// Dense layers: forward product with bias, activation and residual in its epilogue, the two backward products, the
+// elementwise act' and the weight update (include/csrtrain.h). The products run on gemm16_kernel (gemm16.cuh).
+#include <cmath>
+
+#include "gemm16.cuh"
+#include "gemm16_host.cuh"
+
+namespace csrt {
+
+constexpr int64_t kMaxElems = (int64_t)1 << 40;   // largest matrix extent taken (rows x ld)
+
+static size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+static int check_mat(const csrt_mat *m, const char *name) {
+    CSRT_ARG(m != nullptr, "%s is NULL", name);
+    CSRT_ARG(m->rows >= 0 && m->cols >= 0, "%s: negative size", name);
+    CSRT_ARG(m->ld >= m->cols && (m->rows == 0 || m->ld < kMaxElems / (m->rows + 1)), "%s: bad ld", name);
+    CSRT_ARG(m->dtype == CSRT_DT_F32 || m->dtype == CSRT_DT_BF16 || m->dtype == CSRT_DT_F16, "%s: unknown dtype", name);
+    CSRT_ARG(m->data != nullptr || m->rows == 0 || m->cols == 0, "%s: data is NULL", name);
+    CSRT_ARG(reinterpret_cast<uintptr_t>(m->data) % dt_size(m->dtype) == 0, "%s: data is not aligned to its type", name);
+    return CSRT_OK;
+}
+
+static int check_shape(const csrt_mat *m, const char *name, int32_t rows, int32_t cols) {
+    CSRT_ARG(m->rows == rows && m->cols == cols, "%s is %d x %d, must be %d x %d", name, m->rows, m->cols, rows, cols);
+    return CSRT_OK;
+}
+
+#define CSRT_TRY(call)                  \
+    do {                                \
+        const int rc_ = (call);         \
+        if (rc_ != CSRT_OK) return rc_; \
+    } while (0)
+
+static bool overlap(const csrt_mat *a, const csrt_mat *b) {
+    if (a == nullptr || b == nullptr || a->rows == 0 || b->rows == 0 || a->cols == 0 || b->cols == 0) return false;
+    const char *pa = static_cast<const char *>(a->data), *pb = static_cast<const char *>(b->data);
+    const int64_t la = ((a->rows - 1) * a->ld + a->cols) * dt_size(a->dtype);
+    const int64_t lb = ((b->rows - 1) * b->ld + b->cols) * dt_size(b->dtype);
+    return pa < pb + lb && pb < pa + la;
+}
+static bool same_place(const csrt_mat *a, const csrt_mat *b) {
+    return a->data == b->data && a->ld == b->ld && a->dtype == b->dtype;
+}
+
+// Columns of an interleaved buffer may share its extent without sharing elements: only what an output and an input
+// both name counts, so outputs are checked as whole extents except where rows interleave (equal ld).
+static bool clash(const csrt_mat *out, const csrt_mat *in) {
+    if (!overlap(out, in)) return false;
+    if (out->ld == in->ld && out->dtype == in->dtype) {
+        const int64_t d = (static_cast<const char *>(in->data) - static_cast<const char *>(out->data)) /
+                          (int64_t)dt_size(out->dtype);
+        const int64_t c = ((d % out->ld) + out->ld) % out->ld;   // first column of `in` within out's rows
+        return c < out->cols || c + in->cols > out->ld;
+    }
+    return true;
+}
+
+// ---------------------------------------------------------------------------
+// Copy of an operand whose rows are not 16-byte aligned into padded rows.
+// ---------------------------------------------------------------------------
+__global__ void pack16_kernel(const uint16_t *__restrict__ src, int64_t ld, int32_t rows, int32_t cols,
+                              uint16_t *__restrict__ dst, int64_t dld) {
+    pdl_enter();
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
+        for (int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; c < cols; c += (int64_t)gridDim.x * blockDim.x)
+            dst[r * dld + c] = src[r * ld + c];
+}
+
+// Operand of a product: in place, or packed at *at (advanced).
+static int operand(const csrt_mat *m, char **at, cudaStream_t s, GOperand *o) {
+    o->p = m->data;
+    o->rows = m->rows;
+    o->cols = m->cols;
+    o->ld = m->ld;
+    if (tma_rows_ok(m->data, m->ld, 2)) return CSRT_OK;
+    o->ld = (int64_t)align_up((size_t)m->cols, 8);
+    o->p = *at;
+    *at += align_up((size_t)m->rows * o->ld * 2, 256);
+    const unsigned gx = (unsigned)imin<int64_t>(ceil_div<int64_t>(m->cols, 256), 64);
+    const unsigned gy = (unsigned)imin<int64_t>(m->rows, imax<int64_t>(1, (int64_t)num_sms() * 16 / gx));
+    launch_pdl(pack16_kernel, dim3(gx, gy), dim3(256), 0, s, static_cast<const uint16_t *>(m->data), m->ld, m->rows,
+               m->cols, static_cast<uint16_t *>(o->p), o->ld);
+    count_launch();
+    return check_launch("pack16_kernel");
+}
+
+static GMat epi_mat(const csrt_mat *m) {
+    GMat g = {};
+    if (m == nullptr) return g;
+    g.p = m->data;
+    g.ld = m->ld;
+    g.dtype = m->dtype;
+    g.vec = tma_rows_ok(m->data, m->ld, dt_size(m->dtype));
+    return g;
+}
+
+// D = A B^T with the dense epilogue.
+static int dense_product(const csrt_mat *am, bool a_mn, const csrt_mat *bm, bool b_mn, GArgs a, csrt_mat *out0,
+                         csrt_mat *out1, void *ws, cudaStream_t s) {
+    GProduct p;
+    char *at = ws_scratch(ws) + kPartialBytes;
+    CSRT_TRY(operand(am, &at, s, &p.a));
+    CSRT_TRY(operand(bm, &at, s, &p.b));
+    p.a_mn = a_mn;
+    p.b_mn = b_mn;
+    a.f16 = am->dtype == CSRT_DT_F16;
+    a.m = out0->rows;
+    a.n = out0->cols;
+    a.batch = 1;
+    a.out0 = epi_mat(out0);
+    a.out1 = epi_mat(out1);
+    if (out0->dtype == CSRT_DT_F32) a.out1.vec = 0;   // the staging slot holds one float32 block, or two 16-bit ones
+    a.hdr = static_cast<WsHeader *>(ws);
+    a.counters = ws_counters(ws);
+    a.partial = reinterpret_cast<float *>(ws_scratch(ws));
+    p.reduction = a_mn ? am->rows : am->cols;
+    return out0->dtype == CSRT_DT_F32 ? launch_gemm16<kEpiDense, true>(p, a, s) : launch_gemm16<kEpiDense, false>(p, a, s);
+}
+
+// ---------------------------------------------------------------------------
+// Row sums (db), act' and update
+// ---------------------------------------------------------------------------
+template <bool F16>
+__global__ void row_sums_kernel(const uint16_t *__restrict__ dy, int64_t ld, int32_t rows, int32_t cols, bool vec,
+                                bool accumulate, float *__restrict__ db) {
+    pdl_enter();
+    __shared__ float s_part[8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const uint16_t *p = dy + r * ld;
+        float sum = 0.f;
+        if (vec) {
+            for (int64_t c = threadIdx.x * 8; c < cols; c += blockDim.x * 8) {
+                if (c + 8 <= cols) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(p + c);
+                    const float2 x = unpack16(u.x, F16), y = unpack16(u.y, F16), z = unpack16(u.z, F16),
+                                 w = unpack16(u.w, F16);
+                    sum += ((x.x + x.y) + (y.x + y.y)) + ((z.x + z.y) + (w.x + w.y));
+                } else {
+                    for (int64_t i = c; i < cols; ++i) sum += load1(p, i, F16 ? CSRT_DT_F16 : CSRT_DT_BF16);
+                }
+            }
+        } else {
+            for (int64_t c = threadIdx.x; c < cols; c += blockDim.x) sum += load1(p, c, F16 ? CSRT_DT_F16 : CSRT_DT_BF16);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) s_part[warp] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float t = 0.f;
+            for (int w = 0; w < (int)(blockDim.x >> 5); ++w) t += s_part[w];
+            db[r] = accumulate ? db[r] + t : t;
+        }
+        __syncthreads();
+    }
+}
+
+__global__ void act_bwd_kernel(GMat dy, GMat z, int32_t act, GMat out, int32_t rows, int32_t cols) {
+    pdl_enter();
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
+        for (int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; c < cols; c += (int64_t)gridDim.x * blockDim.x) {
+            float v = load1(dy.p, r * dy.ld + c, dy.dtype);
+            if (act != CSRT_ACT_NONE) v *= act_deriv(load1(z.p, r * z.ld + c, z.dtype), act);
+            store1(out.p, r * out.ld + c, v, out.dtype);
+        }
+}
+
+__global__ void dense_update_kernel(GMat w, GMat d, float eta, float keep, GMat w16, int32_t rows, int32_t cols) {
+    pdl_enter();
+    float *wp = static_cast<float *>(w.p);
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
+        for (int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; c < cols; c += (int64_t)gridDim.x * blockDim.x) {
+            const float v = __fsub_rn(__fmul_rn(wp[r * w.ld + c], keep), __fmul_rn(eta, load1(d.p, r * d.ld + c, d.dtype)));
+            wp[r * w.ld + c] = v;
+            if (w16.p != nullptr) store1(w16.p, r * w16.ld + c, v, w16.dtype);
+        }
+}
+
+static dim3 elementwise_grid(int32_t rows, int32_t cols) {
+    const unsigned gx = (unsigned)imin<int64_t>(ceil_div<int64_t>(cols, 256), 4096);
+    const unsigned gy = (unsigned)imin<int64_t>(rows, imax<int64_t>(1, imin<int64_t>(65535, (int64_t)num_sms() * 64 / gx)));
+    return dim3(gx, gy);
+}
+
+static size_t operand_bytes(int64_t rows, int64_t cols) { return align_up((size_t)(rows * ((cols + 7) / 8 * 8) * 2), 256); }
+
+static size_t dense_bytes(int64_t m, int64_t k, int64_t n) {
+    return kWsReservedBytes + kPartialBytes + operand_bytes(m, k) + operand_bytes(m, n) + operand_bytes(k, n);
+}
+
+static int check_call(const csrt_mat *a, const char *an, const csrt_mat *b, const char *bn, int32_t m, int32_t k,
+                      int32_t n, const void *ws, size_t ws_bytes) {
+    CSRT_ARG(a->dtype != CSRT_DT_F32 && a->dtype == b->dtype, "%s and %s must have one 16-bit type", an, bn);
+    CSRT_ARG(ws != nullptr, "workspace is NULL");
+    CSRT_ARG((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
+    if (ws_bytes < dense_bytes(m, k, n))
+        return fail(CSRT_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, dense_bytes(m, k, n));
+    return CSRT_OK;
+}
+
+static int check_out(const csrt_mat *o, const char *name, int32_t dtype) {
+    CSRT_ARG(o->dtype == CSRT_DT_F32 || o->dtype == dtype, "%s must be float32 or of the operands' type", name);
+    return CSRT_OK;
+}
+
+}  // namespace csrt
+
+using namespace csrt;
+
+extern "C" {
+
+int csrt_dense_workspace_bytes(int32_t m, int32_t k, int32_t max_n, size_t *bytes) {
+    CSRT_ARG(bytes != nullptr, "bytes is NULL");
+    CSRT_ARG(m >= 0 && k >= 0 && max_n >= 0, "negative size");
+    *bytes = dense_bytes(m, k, max_n);
+    return CSRT_OK;
+}
+
+int csrt_dense_fwd(const csrt_mat *w, const csrt_mat *x, const float *bias, int32_t act, const csrt_mat *residual,
+                   csrt_mat *z, csrt_mat *y, void *ws, size_t ws_bytes, void *stream) {
+    CSRT_TRY(check_mat(w, "w"));
+    CSRT_TRY(check_mat(x, "x"));
+    CSRT_TRY(check_mat(y, "y"));
+    const int32_t m = w->rows, k = w->cols, n = x->cols;
+    CSRT_TRY(check_shape(x, "x", k, n));
+    CSRT_TRY(check_shape(y, "y", m, n));
+    CSRT_ARG(act >= CSRT_ACT_NONE && act <= CSRT_ACT_SILU, "unknown activation %d", act);
+    CSRT_TRY(check_call(w, "w", x, "x", m, k, n, ws, ws_bytes));
+    CSRT_TRY(check_out(y, "y", w->dtype));
+    if (residual != nullptr) {
+        CSRT_TRY(check_mat(residual, "residual"));
+        CSRT_TRY(check_shape(residual, "residual", m, n));
+        CSRT_ARG(residual->dtype == y->dtype, "residual must have y's type");
+        CSRT_ARG(same_place(residual, y) || !clash(y, residual), "y overlaps residual");
+    }
+    if (z != nullptr) {
+        CSRT_TRY(check_mat(z, "z"));
+        CSRT_TRY(check_shape(z, "z", m, n));
+        CSRT_ARG(z->dtype == w->dtype, "z must have w's type");
+        CSRT_ARG(!clash(z, y) && !clash(z, x) && !clash(z, w) && (residual == nullptr || !clash(z, residual)),
+                 "z overlaps another matrix");
+    }
+    CSRT_ARG(!clash(y, x) && !clash(y, w), "y overlaps an operand");
+    if (m == 0 || n == 0) return CSRT_OK;
+    GArgs a = {};
+    a.bias = bias;
+    a.act = act;
+    a.c1 = epi_mat(residual);
+    return dense_product(w, false, x, true, a, y, z, ws, as_stream(stream));
+}
+
+int csrt_dense_bwd_x(const csrt_mat *w, const csrt_mat *dy, const csrt_mat *z_below, int32_t act,
+                     const csrt_mat *residual, csrt_mat *dx, void *ws, size_t ws_bytes, void *stream) {
+    CSRT_TRY(check_mat(w, "w"));
+    CSRT_TRY(check_mat(dy, "dy"));
+    CSRT_TRY(check_mat(dx, "dx"));
+    const int32_t m = w->rows, k = w->cols, n = dy->cols;
+    CSRT_TRY(check_shape(dy, "dy", m, n));
+    CSRT_TRY(check_shape(dx, "dx", k, n));
+    CSRT_ARG(act >= CSRT_ACT_NONE && act <= CSRT_ACT_SILU, "unknown activation %d", act);
+    CSRT_TRY(check_call(w, "w", dy, "dy", m, k, n, ws, ws_bytes));
+    CSRT_TRY(check_out(dx, "dx", w->dtype));
+    CSRT_ARG(z_below != nullptr || act == CSRT_ACT_NONE, "an activation needs z_below");
+    if (z_below != nullptr) {
+        CSRT_TRY(check_mat(z_below, "z_below"));
+        CSRT_TRY(check_shape(z_below, "z_below", k, n));
+        CSRT_ARG(z_below->dtype == w->dtype, "z_below must have w's type");
+        CSRT_ARG(!clash(dx, z_below), "dx overlaps z_below");
+    }
+    if (residual != nullptr) {
+        CSRT_TRY(check_mat(residual, "residual"));
+        CSRT_TRY(check_shape(residual, "residual", k, n));
+        CSRT_ARG(residual->dtype == dx->dtype, "residual must have dx's type");
+        CSRT_ARG(same_place(residual, dx) || !clash(dx, residual), "dx overlaps residual");
+    }
+    CSRT_ARG(!clash(dx, dy) && !clash(dx, w), "dx overlaps an operand");
+    if (k == 0 || n == 0) return CSRT_OK;
+    GArgs a = {};
+    a.act = act;
+    a.act_grad = act != CSRT_ACT_NONE;
+    if (a.act_grad) a.c0 = epi_mat(z_below);
+    a.c1 = epi_mat(residual);
+    return dense_product(w, true, dy, true, a, dx, nullptr, ws, as_stream(stream));
+}
+
+int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, csrt_mat *dw, float *db, void *ws,
+                     size_t ws_bytes, void *stream) {
+    CSRT_TRY(check_mat(dy, "dy"));
+    CSRT_TRY(check_mat(x, "x"));
+    CSRT_TRY(check_mat(dw, "dw"));
+    const int32_t m = dy->rows, k = x->rows, n = dy->cols;
+    CSRT_TRY(check_shape(x, "x", k, n));
+    CSRT_TRY(check_shape(dw, "dw", m, k));
+    CSRT_TRY(check_call(dy, "dy", x, "x", m, k, n, ws, ws_bytes));
+    CSRT_TRY(check_out(dw, "dw", dy->dtype));
+    CSRT_ARG(!clash(dw, dy) && !clash(dw, x), "dw overlaps an operand");
+    cudaStream_t s = as_stream(stream);
+    if (db != nullptr && m > 0) {
+        const bool vec = tma_rows_ok(dy->data, dy->ld, 2);
+        const dim3 grid((unsigned)imin<int64_t>(m, (int64_t)num_sms() * 16)), block(n > 1024 ? 256 : 64);
+        const uint16_t *p = static_cast<const uint16_t *>(dy->data);
+        if (dy->dtype == CSRT_DT_F16)
+            launch_pdl(row_sums_kernel<true>, grid, block, 0, s, p, dy->ld, m, n, vec, accumulate != 0, db);
+        else
+            launch_pdl(row_sums_kernel<false>, grid, block, 0, s, p, dy->ld, m, n, vec, accumulate != 0, db);
+        count_launch();
+        CSRT_TRY(check_launch("row_sums_kernel"));
+    }
+    if (m == 0 || k == 0) return CSRT_OK;
+    GArgs a = {};
+    if (accumulate) a.c1 = epi_mat(dw);
+    return dense_product(dy, false, x, false, a, dw, nullptr, ws, s);
+}
+
+int csrt_dense_act_bwd(const csrt_mat *dy, const csrt_mat *z, int32_t act, csrt_mat *dpre, void *stream) {
+    CSRT_TRY(check_mat(dy, "dy"));
+    CSRT_TRY(check_mat(dpre, "dpre"));
+    CSRT_ARG(act >= CSRT_ACT_NONE && act <= CSRT_ACT_SILU, "unknown activation %d", act);
+    CSRT_TRY(check_shape(dpre, "dpre", dy->rows, dy->cols));
+    CSRT_ARG(same_place(dy, dpre) || !clash(dpre, dy), "dpre overlaps dy");
+    if (act != CSRT_ACT_NONE) {
+        CSRT_TRY(check_mat(z, "z"));
+        CSRT_TRY(check_shape(z, "z", dy->rows, dy->cols));
+        CSRT_ARG(!clash(dpre, z), "dpre overlaps z");
+    }
+    if (dy->rows == 0 || dy->cols == 0) return CSRT_OK;
+    launch_pdl(act_bwd_kernel, elementwise_grid(dy->rows, dy->cols), dim3(256), 0, as_stream(stream), epi_mat(dy),
+               act == CSRT_ACT_NONE ? GMat{} : epi_mat(z), act, epi_mat(dpre), dy->rows, dy->cols);
+    count_launch();
+    return check_launch("act_bwd_kernel");
+}
+
+int csrt_dense_update(csrt_mat *w, const csrt_mat *d, float eta, float decay, csrt_mat *w16, void *stream) {
+    CSRT_TRY(check_mat(w, "w"));
+    CSRT_TRY(check_mat(d, "d"));
+    CSRT_ARG(w->dtype == CSRT_DT_F32, "w must be float32");
+    CSRT_TRY(check_shape(d, "d", w->rows, w->cols));
+    CSRT_ARG(std::isfinite(eta) && std::isfinite(decay) && eta >= 0.f && decay >= 0.f, "eta and decay must be finite and >= 0");
+    CSRT_ARG(!clash(w, d), "w overlaps d");
+    if (w16 != nullptr) {
+        CSRT_TRY(check_mat(w16, "w16"));
+        CSRT_TRY(check_shape(w16, "w16", w->rows, w->cols));
+        CSRT_ARG(!clash(w16, d) && !clash(w16, w), "w16 overlaps another matrix");
+    }
+    if (w->rows == 0 || w->cols == 0) return CSRT_OK;
+    const float keep = 1.f - eta * decay;
+    launch_pdl(dense_update_kernel, elementwise_grid(w->rows, w->cols), dim3(256), 0, as_stream(stream), epi_mat(w),
+               epi_mat(d), eta, keep, epi_mat(w16), w->rows, w->cols);
+    count_launch();
+    return check_launch("dense_update_kernel");
+}
+
+}  // extern "C"

@@ -1,0 +1,693 @@
+// Matrix product of 16-bit operands (float16 or bfloat16) on the 5th-generation tensor cores, float32
+// accumulation, with the epilogues of the dense layer and of the orthogonalised update:
+//
+//   D[b][i, j] = epilogue( sum_r A[b][i, r] B[b][j, r] ),   i < m, j < n, b < batch
+//
+// Either operand may be stored with the reduction index r contiguous ("K-major") or with its own row index
+// contiguous ("MN-major"): both are fetched by TMA in 64-element (128-byte) wide boxes with the 128-byte swizzle, and
+// the instruction descriptor's major bits do the rest, so W x, W^T dy, dy x^T, X X^T, X^T X and B X all run without a
+// transposed copy.
+//
+// One unit of work is a tile of D (or, with splits > 1, one slice of its reduction). Roles in a CTA:
+//  * warp 0, one lane: TMA producer over a ring of 64-deep stages (full / empty mbarriers);
+//  * warp 1, one lane: tcgen05.mma issue; the accumulator is double-buffered in tensor memory, so a tile's epilogue
+//    overlaps the next tile's loads and products;
+//  * warps 2..9: epilogue. Warp w reads TMEM lanes 32 (w & 3) .. + 31 and every other group of 32 columns, applies
+//    the epilogue in float32, rounds once, and leaves through 64- or 128-byte swizzled staging and a TMA store
+//    (guarded stores where the output's rows are not 16-byte aligned).
+// CG = 2 pairs two CTAs of a cluster on one tile of 2 x 128 rows: each holds its 128 rows of A and half the columns
+// of B, and the leader issues the pair's MMAs.
+//
+// Long float32 sums: the tensor core adds each 16-deep block of products to the float32 accumulator with truncation,
+// which drifts by about 4e-6 of the result over 4096 terms and 1.4e-5 where all terms have one sign (measured).
+// Float32 outputs therefore take the accumulator out every kPromoteKb stages (512 terms) and add it, rounded to
+// nearest, to float32 sums in the epilogue warps' registers (PROMOTE); 16-bit outputs do not need it.
+//
+// Splits: each slice's warp leaves its float32 partial tile in the workspace and counts in; the last one adds the
+// slices in slice order (one order whatever the timing, so results repeat bit for bit) and runs the epilogue.
+//
+// Every wait is bounded: one that runs out sets the CTA's abort flag, the roles drain and meet, and the kernel ends
+// with CSRT_DEV_TIMEOUT in the status word.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "tc_common.cuh"
+
+namespace csrt {
+
+constexpr int kGBK = 64;                 // reduction depth of a stage (128 bytes)
+constexpr int kGThreads = 320;           // TMA, MMA and eight epilogue warps
+constexpr int kGEpiWarps = 8;
+constexpr int kPromoteKb = 8;            // stages per tensor-memory accumulation of a float32 output
+constexpr int kGStageOut = 8192;         // staging bytes of an epilogue warp (two slots)
+
+enum { kEpiDense = 0, kEpiGram = 1, kEpiPoly = 2, kEpiApply = 3 };
+
+// An epilogue operand or output: row-major m x n, batch matrices `stride` elements apart.
+struct GMat {
+    void *p;
+    int64_t ld, stride;
+    int32_t dtype;     // CSRT_DT_*
+    int32_t vec;       // rows 16-byte aligned: vector access; outputs: TMA store
+};
+
+struct GArgs {
+    int32_t m, n, kb, batch;          // output size, stages of the reduction, matrices
+    int32_t tiles_m, tiles_n;
+    int32_t units;                    // work units per launch (tiles x splits x batch)
+    int32_t splits, kb_split;
+    int32_t a_mn, b_mn;               // operand stored MN-major
+    int32_t f16;                      // operands and 16-bit epilogue tensors are float16 (else bfloat16)
+    // epilogue
+    const float *bias;
+    int32_t act, act_grad;            // activation; act_grad: multiply by act'(c0) instead
+    float alpha, beta, gamma;         // orthogonalisation: alpha acc + beta c0 (+ beta c1)
+    GMat c0, c1;                      // z_below / A / X high; residual / X low
+    GMat out0, out1;                  // y, dx, dW, A, B, X high, O; z, X low
+    float *partial;                   // split slices
+    int32_t *counters;
+    WsHeader *hdr;
+};
+
+struct GMaps {
+    CUtensorMap a, b, out0, out1;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t mapa_u32(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// Bounded wait on an mbarrier phase (about a quarter of a second), given up early once the CTA aborts.
+__device__ __forceinline__ bool gwait(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+    const uint32_t addr = smem_u32(bar);
+    for (unsigned i = 0; i < (1u << 18); ++i) {
+        uint32_t done;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
+            " selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(done)
+            : "r"(addr), "r"(parity), "r"(1000u)
+            : "memory");
+        if (done) return true;
+        if (*abort_flag) return false;
+    }
+    *abort_flag = 1;
+    return false;
+}
+
+template <int CG>
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+            ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+            "[%0], [%1, {%2, %3, %4}], [%5];"
+            ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+}
+
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, int x, int y, int z, const void *src) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(x), "r"(y), "r"(z), "r"(smem_u32(src))
+                 : "memory");
+}
+
+// Shared-memory descriptor with the 128-byte swizzle. K-major: rows of 128 bytes, 8-row groups 1024 bytes apart.
+// MN-major: 64 operand rows to a 128-byte line, a line per reduction index, 8-line groups 1024 bytes apart and the
+// next 64 operand rows kGBK lines (8192 bytes) further on.
+__device__ __forceinline__ uint64_t gdesc(uint32_t addr, bool mn) {
+    uint64_t d = 0;
+    d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(mn ? (kGBK * 128) >> 4 : 1) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+template <int CG>
+__device__ __forceinline__ void mma_16(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
+    if constexpr (CG == 1)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(ad), "l"(bd), "r"(idesc), "r"(acc)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(ad), "l"(bd), "r"(idesc), "r"(acc)
+            : "memory");
+}
+
+// Arrive on a barrier (of both CTAs of a pair) once the MMAs issued so far are done.
+template <int CG>
+__device__ __forceinline__ void commit_to(uint64_t *bar) {
+    if constexpr (CG == 1)
+        mma_commit(bar);
+    else
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                smem_u32(bar)),
+            "h"((uint16_t)3)
+            : "memory");
+}
+
+// The same for a barrier of this CTA alone.
+template <int CG>
+__device__ __forceinline__ void commit_own(uint64_t *bar) {
+    if constexpr (CG == 1)
+        mma_commit(bar);
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+                     : "memory");
+}
+
+// ---------------------------------------------------------------------------
+// Element types and activations
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t pack16(float lo, float hi, bool f16) {
+    if (f16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+__device__ __forceinline__ float2 unpack16(uint32_t u, bool f16) {
+    if (f16) return __half22float2(*reinterpret_cast<const __half2 *>(&u));
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+}
+
+__device__ __forceinline__ float load1(const void *p, int64_t i, int dtype) {
+    if (dtype == CSRT_DT_F32) return static_cast<const float *>(p)[i];
+    if (dtype == CSRT_DT_F16) return __half2float(static_cast<const __half *>(p)[i]);
+    return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+}
+
+__device__ __forceinline__ void store1(void *p, int64_t i, float v, int dtype) {
+    if (dtype == CSRT_DT_F32) static_cast<float *>(p)[i] = v;
+    else if (dtype == CSRT_DT_F16) static_cast<__half *>(p)[i] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
+}
+
+// act(z) and act'(z) in float32. gelu is the tanh form, 0.5 z (1 + tanh u) = z / (1 + exp(-2u)) with
+// u = sqrt(2/pi) (z + 0.044715 z^3); silu is z / (1 + exp(-z)). The fast exponential and quotient are off by a few
+// 2^-22 of the sigmoid, far below the 16-bit rounding of the result.
+constexpr float kGelu2 = 1.5957691216057308f;     // 2 sqrt(2/pi)
+constexpr float kGelu3 = 0.044715f;
+
+__device__ __forceinline__ float act_value(float z, int act) {
+    if (act == CSRT_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
+    if (act == CSRT_ACT_GELU) return __fdividef(z, 1.f + __expf(-kGelu2 * (z + kGelu3 * z * z * z)));
+    if (act == CSRT_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+    return z;
+}
+
+__device__ __forceinline__ float act_deriv(float z, int act) {
+    if (act == CSRT_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if (act == CSRT_ACT_GELU) {
+        const float p = __fdividef(1.f, 1.f + __expf(-kGelu2 * (z + kGelu3 * z * z * z)));
+        return p + z * p * (1.f - p) * kGelu2 * (1.f + 3.f * kGelu3 * z * z);
+    }
+    if (act == CSRT_ACT_SILU) {
+        const float p = __fdividef(1.f, 1.f + __expf(-z));
+        return p * (1.f + z * (1.f - p));
+    }
+    return 1.f;
+}
+
+// 32 consecutive elements of a row of an epilogue operand, as float32 (0 beyond `left`).
+__device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int64_t off, int left) {
+    if (c.vec && left >= 32) {
+        if (c.dtype == CSRT_DT_F32) {
+            const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(c.p) + off);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float4 f = p[i];
+                v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
+            }
+        } else {
+            const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(c.p) + off);
+            const bool h = c.dtype == CSRT_DT_F16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint4 u = p[i];
+                const float2 a = unpack16(u.x, h), b = unpack16(u.y, h), d = unpack16(u.z, h), e = unpack16(u.w, h);
+                v[8 * i] = a.x, v[8 * i + 1] = a.y, v[8 * i + 2] = b.x, v[8 * i + 3] = b.y;
+                v[8 * i + 4] = d.x, v[8 * i + 5] = d.y, v[8 * i + 6] = e.x, v[8 * i + 7] = e.y;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = i < left ? load1(c.p, off + i, c.dtype) : 0.f;
+    }
+}
+
+// Row `row` (of this lane) and columns col .. col + 31 of an output leave the warp: `slot` is its staging area.
+// Rows of 64 bytes (16-bit) take the 64-byte swizzle, rows of 128 bytes (float32) the 128-byte one.
+__device__ __forceinline__ void store32(const float (&v)[32], const GMat &o, const CUtensorMap *map, uint8_t *slot,
+                                        int b, int row, int col, int m, int n) {
+    const int lane = threadIdx.x & 31;
+    if (o.vec) {
+        if (o.dtype == CSRT_DT_F32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                *reinterpret_cast<float4 *>(slot + lane * 128 + ((i ^ (lane & 7)) << 4)) =
+                    make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        } else {
+            const bool h = o.dtype == CSRT_DT_F16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<uint4 *>(slot + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) =
+                    make_uint4(pack16(v[8 * i], v[8 * i + 1], h), pack16(v[8 * i + 2], v[8 * i + 3], h),
+                               pack16(v[8 * i + 4], v[8 * i + 5], h), pack16(v[8 * i + 6], v[8 * i + 7], h));
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0 && row < m && col < n) tma_store_3d(map, col, row, b, slot);   // lane 0's row is the block's first
+    } else if (row < m) {
+        const int64_t off = b * o.stride + (int64_t)row * o.ld + col;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (col + i < n) store1(o.p, off + i, v[i], o.dtype);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Work units
+// ---------------------------------------------------------------------------
+struct GUnit {
+    int b, tm, tn, split, kb0, kb1, tile;
+};
+
+// Unit u: batch matrix, tile and slice. Tiles run down bands of eight tile rows, so that the units in flight share
+// operand tiles in L2. A symmetric product (kEpiGram, kEpiPoly) has the tiles on and above the diagonal only.
+template <bool SYM>
+__device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
+    GUnit r;
+    const int tiles = SYM ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
+    r.split = u % a.splits;
+    const int t = u / a.splits;
+    r.tile = t;
+    r.b = t / tiles;
+    int q = t - r.b * tiles;
+    if (SYM) {
+        int i = 0;
+        while (q >= a.tiles_m - i) q -= a.tiles_m - i++;
+        r.tm = i;
+        r.tn = i + q;
+    } else {
+        constexpr int kBand = 8;
+        const int band = q / (kBand * a.tiles_n), first = band * kBand;
+        const int rows = min(kBand, a.tiles_m - first);
+        q -= first * a.tiles_n;
+        r.tm = first + q % rows;
+        r.tn = q / rows;
+    }
+    r.kb0 = r.split * a.kb_split;
+    r.kb1 = min(a.kb, r.kb0 + a.kb_split);
+    return r;
+}
+
+// The epilogue of 32 columns of a row in float32.
+template <int EPI>
+__device__ __forceinline__ void epilogue32(float (&v)[32], const GArgs &a, const GMaps &maps, uint8_t *slot, int b,
+                                           int row, int col) {
+    const int left = row < a.m ? a.n - col : 0;
+    if constexpr (EPI == kEpiDense) {
+        if (a.bias != nullptr) {
+            const float bi = row < a.m ? __ldg(a.bias + row) : 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] += bi;
+        }
+        if (a.out1.p != nullptr) store32(v, a.out1, &maps.out1, slot + 2048, b, row, col, a.m, a.n);
+        if (a.act_grad) {
+            float z[32];
+            load32(z, a.c0, b * a.c0.stride + (int64_t)row * a.c0.ld + col, left);
+            if (a.act == CSRT_ACT_RELU) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_RELU);
+            } else if (a.act == CSRT_ACT_GELU) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_GELU);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_SILU);
+            }
+        } else if (a.act == CSRT_ACT_RELU) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_RELU);
+        } else if (a.act == CSRT_ACT_GELU) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_GELU);
+        } else if (a.act == CSRT_ACT_SILU) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_SILU);
+        }
+        if (a.c1.p != nullptr) {
+            float r[32];
+            load32(r, a.c1, b * a.c1.stride + (int64_t)row * a.c1.ld + col, left);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] += r[i];
+        }
+        store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
+    } else if constexpr (EPI == kEpiGram || EPI == kEpiPoly) {
+        if constexpr (EPI == kEpiGram) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= a.alpha;
+        } else {
+            float c[32];
+            load32(c, a.c0, b * a.c0.stride + (int64_t)row * a.c0.ld + col, left);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = a.alpha * v[i] + a.beta * c[i];
+        }
+        store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
+    } else {
+        float c[32];
+        const int64_t off = b * a.c0.stride + (int64_t)row * a.c0.ld + col;
+        load32(c, a.c0, off, left);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = a.alpha * v[i] + a.beta * c[i];
+        load32(c, a.c1, off, left);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = (v[i] + a.beta * c[i]) * a.gamma;
+        store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
+        if (a.out1.p != nullptr) {   // what float16 drops of X, kept beside it
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
+            store32(v, a.out1, &maps.out1, slot + 2048, b, row, col, a.m, a.n);
+        }
+    }
+}
+
+// The same 32 values into the mirrored place of a symmetric output (float16): lane-contiguous stores.
+__device__ __forceinline__ void mirror32(const float (&v)[32], const GMat &o, int b, int row, int col, int m, int n) {
+    if (row >= m) return;
+    __half *p = static_cast<__half *>(o.p) + b * o.stride + row;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        if (col + i < n) p[(int64_t)(col + i) * o.ld] = __float2half_rn(v[i]);
+}
+
+template <int CG, int BN>
+constexpr int gstage_bytes() {
+    return 128 * 128 + (BN / CG) * 128;
+}
+template <int CG, int BN>
+constexpr int gstages() {
+    return (227 * 1024 - kGEpiWarps * kGStageOut - 2048) / gstage_bytes<CG, BN>();
+}
+template <int CG, int BN>
+constexpr int gsmem_bytes() {
+    return gstages<CG, BN>() * gstage_bytes<CG, BN>() + kGEpiWarps * kGStageOut + 1024 + 512;
+}
+
+template <int CG, int BN, int EPI, bool PROMOTE>
+__global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
+    gemm16_kernel(const __grid_constant__ GMaps maps, const __grid_constant__ GArgs a) {
+    static_assert(BN % 64 == 0 && BN / CG >= 64 && 2 * BN <= 512, "two accumulators in tensor memory");
+    constexpr bool SYM = EPI == kEpiGram || EPI == kEpiPoly;
+    constexpr int kStages = gstages<CG, BN>();
+    constexpr int kStageBytes = gstage_bytes<CG, BN>();
+    constexpr int kABytes = 128 * 128;
+    constexpr int kBRows = BN / CG;                       // columns of D whose B rows this CTA holds
+    constexpr int kChunks = BN / 32;
+    constexpr uint32_t kCols = 2 * BN;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *epi = smem + kStages * kStageBytes;
+    uint64_t *full = reinterpret_cast<uint64_t *>(epi + kGEpiWarps * kGStageOut);
+    uint64_t *empty = full + kStages;
+    uint64_t *accf = empty + kStages;    // [2] accumulator ready
+    uint64_t *acce = accf + 2;           // [2] accumulator drained
+    uint64_t *fin = acce + 2;            // all MMAs complete
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(fin + 1);
+    __shared__ volatile int s_abort;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const int unit0 = blockIdx.x / CG, ustep = gridDim.x / CG;
+
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(full + s, 1);
+            mbar_init(empty + s, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(accf + i, 1);
+            mbar_init(acce + i, CG * kGEpiWarps);
+        }
+        mbar_init(fin, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.a)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.b)) : "memory");
+    }
+    if (warp == 1) {
+        if constexpr (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                         "r"(kCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                         "r"(kCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync_all();   // the peer's barriers are initialised
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *tmem_slot;
+    pdl_enter();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;
+            for (int u = unit0; u < a.units && !s_abort; u += ustep) {
+                const GUnit w = unit_of<SYM>(a, u);
+                const int m0 = (w.tm * CG + (int)rank) * 128, n0 = w.tn * BN + (int)rank * kBRows;
+                for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
+                    const int s = it % kStages;
+                    if (!gwait(empty + s, ((it / kStages) & 1) ^ 1, &s_abort)) break;
+                    uint8_t *sa = smem + s * kStageBytes, *sb = sa + kABytes;
+                    uint32_t bar = smem_u32(full + s);
+                    if constexpr (CG == 2) bar = mapa_u32(bar, 0);
+                    if (rank == 0) mbar_expect_tx(full + s, CG * kStageBytes);
+                    if (a.a_mn) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            tma_load_3d<CG>(sa + i * 8192, &maps.a, m0 + i * 64, kb * kGBK, w.b, bar);
+                    } else {
+                        tma_load_3d<CG>(sa, &maps.a, kb * kGBK, m0, w.b, bar);
+                    }
+                    if (a.b_mn) {
+#pragma unroll
+                        for (int i = 0; i < kBRows / 64; ++i)
+                            tma_load_3d<CG>(sb + i * 8192, &maps.b, n0 + i * 64, kb * kGBK, w.b, bar);
+                    } else {
+                        tma_load_3d<CG>(sb, &maps.b, kb * kGBK, n0, w.b, bar);
+                    }
+                }
+            }
+            // an aborted CTA's loads in flight must land before it may exit (its own barriers show them on rank 0)
+            if (s_abort && rank == 0)
+                for (int i = imax(0, it - kStages); i < it; ++i) mbar_wait(full + i % kStages, (i / kStages) & 1);
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = (1u << 4) | ((a.f16 ? 0u : 1u) << 7) | ((a.f16 ? 0u : 1u) << 10) |
+                                   ((uint32_t)a.a_mn << 15) | ((uint32_t)a.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
+                                   ((uint32_t)((128 * CG) >> 4) << 24);
+            const uint32_t a_step = a.a_mn ? 2048 : 32, b_step = a.b_mn ? 2048 : 32;
+            int it = 0, j = 0;
+            for (int u = unit0; u < a.units && !s_abort; u += ustep) {
+                const GUnit w = unit_of<SYM>(a, u);
+                int kb = w.kb0;
+                do {   // one accumulation: the whole unit, or kPromoteKb stages of it
+                    const int stop = PROMOTE ? min(w.kb1, kb + kPromoteKb) : w.kb1;
+                    const int acc = j & 1;
+                    if (!gwait(acce + acc, ((j >> 1) & 1) ^ 1, &s_abort)) break;
+                    ++j;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t d = tmem + (uint32_t)(acc * BN);
+                    for (const int first = kb; kb < stop; ++kb, ++it) {
+                        const int s = it % kStages;
+                        if (!gwait(full + s, (it / kStages) & 1, &s_abort)) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t sa = smem_u32(smem + s * kStageBytes), sb = sa + kABytes;
+#pragma unroll
+                        for (int k = 0; k < kGBK / 16; ++k)
+                            mma_16<CG>(d, gdesc(sa + k * a_step, a.a_mn), gdesc(sb + k * b_step, a.b_mn), idesc,
+                                       (kb > first || k > 0) ? 1u : 0u);
+                        commit_to<CG>(empty + s);
+                    }
+                    commit_to<CG>(accf + acc);
+                } while (kb < w.kb1 && !s_abort);
+            }
+            commit_own<CG>(fin);
+            mbar_wait(fin, 0);   // nothing of ours still runs on the tensor cores
+        }
+    } else {
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        uint8_t *stage0 = epi + (warp - 2) * kGStageOut;
+        uint32_t acce_bar[2] = {smem_u32(acce), smem_u32(acce + 1)};
+        if constexpr (CG == 2) {
+            acce_bar[0] = mapa_u32(acce_bar[0], 0);
+            acce_bar[1] = mapa_u32(acce_bar[1], 0);
+        }
+        int j = 0, slot = 0;
+        for (int u = unit0; u < a.units; u += ustep) {
+            const GUnit w = unit_of<SYM>(a, u);
+            const int row = (w.tm * CG + (int)rank) * 128 + q * 32 + lane, n0 = w.tn * BN;
+            const bool empty_sum = w.kb1 <= w.kb0;
+            float sums[PROMOTE ? kChunks / 2 : 1][32];
+            bool ok = true;
+            int kb = w.kb0;
+            uint32_t d = 0;
+            do {
+                const int acc = j & 1;
+                ok = __all_sync(0xffffffffu, gwait(accf + acc, (j >> 1) & 1, &s_abort));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                d = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
+                if constexpr (PROMOTE) {
+#pragma unroll
+                    for (int i = 0; i < kChunks / 2; ++i) {
+                        uint32_t r[32];
+                        tmem_ld_32cols(d + (uint32_t)((2 * i + half) * 32), r);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            sums[i][e] = empty_sum ? 0.f
+                                                   : (kb == w.kb0 ? __uint_as_float(r[e])
+                                                                  : sums[i][e] + __uint_as_float(r[e]));
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0)
+                        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(acce_bar[acc])
+                                     : "memory");
+                    ++j;
+                    kb += kPromoteKb;
+                } else {
+                    kb = w.kb1;
+                }
+            } while (kb < w.kb1);
+            if (!ok) break;
+
+            bool last = true;
+            const int64_t slab = 128 * BN;
+            float *part = nullptr;
+            if (a.splits > 1) part = a.partial + ((int64_t)w.tile * a.splits * CG + rank) * slab + q * 32 + lane;
+#pragma unroll 1
+            for (int pass = 0; pass < 2; ++pass) {
+                // pass 0: this unit's sums (to the epilogue, or to its slab); pass 1: the slices joined
+                if (pass == 1) {
+                    if (a.splits == 1) break;
+                    __threadfence();
+                    __syncwarp();
+                    int n_in = 0;
+                    int32_t *cnt = a.counters + ((int64_t)w.tile * CG + rank) * kGEpiWarps + (warp - 2);
+                    if (lane == 0) n_in = atomicAdd(cnt, 1);
+                    n_in = __shfl_sync(0xffffffffu, n_in, 0);
+                    last = n_in == a.splits - 1;
+                    if (!last) break;
+                    if (lane == 0) *cnt = 0;
+                    __threadfence();
+                }
+#pragma unroll(PROMOTE ? kChunks / 2 : 1)
+                for (int i = 0; i < kChunks / 2; ++i) {
+                    const int ci = 2 * i + half;
+                    float v[32];
+                    if (pass == 0) {
+                        if constexpr (PROMOTE) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = sums[i][e];
+                        } else {
+                            uint32_t r[32];
+                            tmem_ld_32cols(d + (uint32_t)(ci * 32), r);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = empty_sum ? 0.f : __uint_as_float(r[e]);
+                            if (i == kChunks / 2 - 1) {
+                                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                                __syncwarp();
+                                if (lane == 0)
+                                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                                                     acce_bar[j & 1])
+                                                 : "memory");
+                                ++j;
+                            }
+                        }
+                        if (a.splits > 1) {
+                            float *p = part + (int64_t)w.split * CG * slab + (int64_t)ci * 32 * 128;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) p[e * 128] = v[e];
+                            continue;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = 0.f;
+                        for (int sl = 0; sl < a.splits; ++sl) {
+                            const float *p = part + (int64_t)sl * CG * slab + (int64_t)ci * 32 * 128;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] += __ldcg(p + e * 128);
+                        }
+                    }
+                    const int col = n0 + ci * 32;
+                    if (col >= a.n) continue;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    __syncwarp();
+                    epilogue32<EPI>(v, a, maps, stage0 + slot * (kGStageOut / 2), w.b, row, col);
+                    if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    slot ^= 1;
+                    if constexpr (SYM)
+                        if (w.tm != w.tn) mirror32(v, a.out0, w.b, row, col, a.m, a.n);
+                }
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync_all();
+    if (threadIdx.x == 0 && s_abort) {
+        dev_flag(a.hdr, CSRT_DEV_TIMEOUT);
+        a.hdr->timeout_site = 6;
+    }
+    if (warp == 1) {
+        __syncwarp();
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if constexpr (CG == 1)
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
+    }
+}
+
+}  // namespace csrt

@@ -1,0 +1,369 @@
+// Orthogonalised update (csrt_orthogonalize): momentum, normalisation and the Newton-Schulz products
+//
+//   X <- a X + (b A + c A A) X,   A = X X^T  (X^T X and products on the right where X has more rows than columns)
+//
+// as three launches of gemm16_kernel per step: A with its mirrored half, B = b A + c A A likewise, and a X + B X.
+//
+// Number formats. Singular values stay in [0, 1.203] (p(s) = a s + b s^3 + c s^5 maps [0, 1.203] into itself), so
+// every entry of X, A and B is bounded (1.203, 1.45, 2.81) and fits float16 once scaled by a power of two: X and A
+// are stored times 2^15, B times 2^14. float16 keeps 11 significant bits where bfloat16 keeps 8, at the same
+// tensor-core rate: bfloat16 operands alone would put o about 1e-2 off. X is carried as a float16 pair (high part,
+// the operand of the products, and low part, 22 bits together), so that the term a X - all there is for the small
+// singular values - does not gather a rounding per step.
+//
+// The Frobenius norm is summed in float64 over float32 sums of eight squares; a sum out of float32's safe range is
+// taken again in float64, so that neither tiny nor huge gradients lose it.
+#include <cmath>
+
+#include "gemm16_host.cuh"
+
+namespace csrt {
+
+constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
+constexpr float kXScale = 32768.f;
+constexpr int kPrepThreads = 256;
+constexpr int kPrepBlocks = 1024;   // most blocks (norm partials) per matrix
+
+struct PrepArgs {
+    GMat g;                 // gradient
+    float *mom;             // contiguous, or NULL
+    float beta, eps, scale;
+    int32_t nesterov, rows, cols, vec;
+    double *partial;        // [batch][gridDim.x]
+    __half *hi, *lo;        // X, or
+    GMat o;                 // with no steps: the normalised direction itself
+    int64_t ldx;
+    int32_t direct;
+};
+
+// Eight consecutive elements of row r from column c: gradient, old momentum -> u (and the new momentum stored).
+template <bool UPDATE>
+__device__ __forceinline__ void direction8(const PrepArgs &a, int b, int r, int c, int cnt, float (&u)[8]) {
+    const int64_t gi = b * a.g.stride + (int64_t)r * a.g.ld + c;
+    const int64_t mi = ((int64_t)b * a.rows + r) * a.cols + c;
+    float g[8], m[8];
+    if (a.vec) {
+        if (a.g.dtype == CSRT_DT_F32) {
+            const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(a.g.p) + gi);
+            const float4 x = p[0], y = p[1];
+            g[0] = x.x, g[1] = x.y, g[2] = x.z, g[3] = x.w, g[4] = y.x, g[5] = y.y, g[6] = y.z, g[7] = y.w;
+        } else {
+            const uint4 x = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.g.p) + gi);
+            const float2 p = unpack16(x.x, false), q = unpack16(x.y, false), s = unpack16(x.z, false),
+                         t = unpack16(x.w, false);
+            g[0] = p.x, g[1] = p.y, g[2] = q.x, g[3] = q.y, g[4] = s.x, g[5] = s.y, g[6] = t.x, g[7] = t.y;
+        }
+        if (a.mom != nullptr) {
+            const float4 *p = reinterpret_cast<const float4 *>(a.mom + mi);
+            const float4 x = p[0], y = p[1];
+            m[0] = x.x, m[1] = x.y, m[2] = x.z, m[3] = x.w, m[4] = y.x, m[5] = y.y, m[6] = y.z, m[7] = y.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            g[i] = i < cnt ? load1(a.g.p, gi + i, a.g.dtype) : 0.f;
+            m[i] = a.mom != nullptr && i < cnt ? a.mom[mi + i] : 0.f;
+        }
+    }
+    if (a.mom == nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = g[i];
+        return;
+    }
+    if (UPDATE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = __fadd_rn(__fmul_rn(a.beta, m[i]), g[i]);
+        if (a.vec) {
+            float4 *p = reinterpret_cast<float4 *>(a.mom + mi);
+            p[0] = make_float4(m[0], m[1], m[2], m[3]);
+            p[1] = make_float4(m[4], m[5], m[6], m[7]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < cnt) a.mom[mi + i] = m[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = a.nesterov ? __fadd_rn(g[i], __fmul_rn(a.beta, m[i])) : m[i];
+}
+
+__device__ __forceinline__ double block_sum(double v) {
+    __shared__ double s_part[kPrepThreads / 32];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double t = 0.0;
+    for (int w = 0; w < kPrepThreads / 32; ++w) t += s_part[w];
+    __syncthreads();
+    return t;
+}
+
+// First pass over the gradients: momentum, and the squares of u summed per block.
+__global__ void __launch_bounds__(kPrepThreads) ortho_momentum_kernel(PrepArgs a) {
+    pdl_enter();
+    const int b = blockIdx.y;
+    const uint32_t per_row = (uint32_t)(a.cols + 7) / 8, total = per_row * (uint32_t)a.rows;
+    double sum = 0.0;
+    for (uint32_t t = blockIdx.x * kPrepThreads + threadIdx.x; t < total; t += gridDim.x * kPrepThreads) {
+        const uint32_t r = t / per_row, c = (t - r * per_row) * 8;
+        float u[8];
+        direction8<true>(a, b, (int)r, (int)c, min(8, a.cols - (int)c), u);
+        float s = 0.f, big = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            s += u[i] * u[i];
+            big = fmaxf(big, fabsf(u[i]));
+        }
+        if (s > 1e-24f && s < 1e37f) {
+            sum += (double)s;
+        } else if (big > 0.f || s != s) {
+            for (int i = 0; i < 8; ++i) sum += (double)u[i] * (double)u[i];
+        }
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) a.partial[(int64_t)b * gridDim.x + blockIdx.x] = sum;
+}
+
+// Second pass: X = u / max(||u||_F, eps) as the scaled float16 pair.
+__global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
+    pdl_enter();
+    const int b = blockIdx.y;
+    double n2 = 0.0;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kPrepThreads) n2 += a.partial[(int64_t)b * gridDim.x + i];
+    n2 = block_sum(n2);
+    double norm = sqrt(n2);
+    norm = norm < (double)a.eps ? (double)a.eps : norm;   // a NaN stays
+    const float f = (float)((a.direct ? (double)a.scale : (double)kXScale) / norm);
+    const uint32_t per_row = (uint32_t)(a.cols + 7) / 8, total = per_row * (uint32_t)a.rows;
+    for (uint32_t t = blockIdx.x * kPrepThreads + threadIdx.x; t < total; t += gridDim.x * kPrepThreads) {
+        const uint32_t r = t / per_row, c = (t - r * per_row) * 8;
+        const int cnt = min(8, a.cols - (int)c);
+        float u[8];
+        direction8<false>(a, b, (int)r, (int)c, cnt, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] *= f;
+        if (a.direct) {
+            for (int i = 0; i < cnt; ++i)
+                store1(a.o.p, b * a.o.stride + (int64_t)r * a.o.ld + c + i, u[i], a.o.dtype);
+            continue;
+        }
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            h[i] = pack16(u[2 * i], u[2 * i + 1], true);
+            const float2 back = unpack16(h[i], true);
+            l[i] = pack16(u[2 * i] - back.x, u[2 * i + 1] - back.y, true);
+        }
+        // rows are padded to a multiple of eight, so the tail of a row may be written whole
+        const int64_t xi = ((int64_t)b * a.rows + r) * a.ldx + c;
+        *reinterpret_cast<uint4 *>(a.hi + xi) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4 *>(a.lo + xi) = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+}
+
+struct OrthoLayout {
+    int64_t ldx, lds;
+    size_t partial, x0, x1, lo, a, b, total;   // offsets after the reserved part
+};
+
+static OrthoLayout layout(int64_t batch, int64_t rows, int64_t cols) {
+    auto up = [](int64_t v, int64_t q) { return (v + q - 1) / q * q; };
+    OrthoLayout l;
+    const int64_t s = rows < cols ? rows : cols;
+    l.ldx = up(cols, 64);
+    l.lds = up(s, 64);
+    size_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t r = at;
+        at += (size_t)up(bytes, 256);
+        return r;
+    };
+    l.partial = take(batch * kPrepBlocks * (int64_t)sizeof(double));
+    l.x0 = take(batch * rows * l.ldx * 2);
+    l.x1 = take(batch * rows * l.ldx * 2);
+    l.lo = take(batch * rows * l.ldx * 2);
+    l.a = take(batch * s * l.lds * 2);
+    l.b = take(batch * s * l.lds * 2);
+    l.total = at;
+    return l;
+}
+
+static int check_batch(const csrt_mat *m, const char *name, int32_t batch, int64_t stride) {
+    CSRT_ARG(m != nullptr, "%s is NULL", name);
+    CSRT_ARG(m->rows >= 0 && m->cols >= 0 && (int64_t)m->rows * m->cols < (int64_t)1 << 31, "%s: bad size", name);
+    CSRT_ARG(m->ld >= m->cols && m->ld < (int64_t)1 << 31, "%s: bad ld", name);
+    CSRT_ARG(stride >= 0 && stride < (int64_t)1 << 40, "%s: bad batch stride", name);
+    CSRT_ARG(m->dtype == CSRT_DT_F32 || m->dtype == CSRT_DT_BF16, "%s must be float32 or bfloat16", name);
+    CSRT_ARG(m->data != nullptr || batch == 0 || m->rows == 0 || m->cols == 0, "%s: data is NULL", name);
+    CSRT_ARG(reinterpret_cast<uintptr_t>(m->data) % dt_size(m->dtype) == 0, "%s: data is not aligned to its type", name);
+    return CSRT_OK;
+}
+
+static bool extents_meet(const void *a, int64_t abytes, const void *b, int64_t bbytes) {
+    const char *pa = static_cast<const char *>(a), *pb = static_cast<const char *>(b);
+    return pa < pb + bbytes && pb < pa + abytes;
+}
+
+}  // namespace csrt
+
+using namespace csrt;
+
+extern "C" {
+
+int csrt_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, size_t *bytes) {
+    CSRT_ARG(bytes != nullptr, "bytes is NULL");
+    CSRT_ARG(batch >= 0 && rows >= 0 && cols >= 0, "negative size");
+    CSRT_ARG(batch <= 65535 && (int64_t)rows * cols < (int64_t)1 << 31, "rows*cols must be below 2^31, batch at most 65535");
+    *bytes = kWsReservedBytes + layout(batch, rows, cols).total;
+    return CSRT_OK;
+}
+
+int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float *momentum, float beta,
+                       int32_t nesterov, int32_t steps, float eps, float scale, csrt_mat *o, int64_t o_stride,
+                       void *ws, size_t ws_bytes, void *stream) {
+    CSRT_ARG(batch >= 0 && batch <= 65535, "batch must be in [0, 65535]");
+    int rc = check_batch(g, "g", batch, g_stride);
+    if (rc != CSRT_OK) return rc;
+    rc = check_batch(o, "o", batch, o_stride);
+    if (rc != CSRT_OK) return rc;
+    const int32_t rows = g->rows, cols = g->cols;
+    CSRT_ARG(o->rows == rows && o->cols == cols, "o is %d x %d, must be %d x %d", o->rows, o->cols, rows, cols);
+    CSRT_ARG(std::isfinite(beta) && beta >= 0.f && beta < 1.f, "beta must be in [0, 1)");
+    CSRT_ARG(std::isfinite(eps) && eps > 0.f, "eps must be finite and > 0");
+    CSRT_ARG(std::isfinite(scale), "scale must be finite");
+    CSRT_ARG(steps >= 0 && steps <= 32, "steps must be in [0, 32]");
+    if (batch == 0 || rows == 0 || cols == 0) return CSRT_OK;
+    CSRT_ARG(batch == 1 || o_stride >= (int64_t)(rows - 1) * o->ld + cols ||
+                 (o_stride >= cols && o->ld >= (batch - 1) * o_stride + cols),
+             "the matrices of o overlap");
+    const int64_t g_bytes = ((batch - 1) * g_stride + (int64_t)(rows - 1) * g->ld + cols) * dt_size(g->dtype);
+    const int64_t o_bytes = ((batch - 1) * o_stride + (int64_t)(rows - 1) * o->ld + cols) * dt_size(o->dtype);
+    const int64_t m_bytes = (int64_t)batch * rows * cols * 4;
+    CSRT_ARG(!extents_meet(o->data, o_bytes, g->data, g_bytes), "o overlaps g");
+    CSRT_ARG(momentum == nullptr || (!extents_meet(o->data, o_bytes, momentum, m_bytes) &&
+                                     !extents_meet(g->data, g_bytes, momentum, m_bytes)),
+             "momentum overlaps g or o");
+    CSRT_ARG(reinterpret_cast<uintptr_t>(momentum) % 4 == 0, "momentum is not aligned to its type");
+    CSRT_ARG(ws != nullptr && (reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is NULL or not 256-byte aligned");
+    const OrthoLayout l = layout(batch, rows, cols);
+    if (ws_bytes < kWsReservedBytes + l.total)
+        return fail(CSRT_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, kWsReservedBytes + l.total);
+    cudaStream_t s = as_stream(stream);
+    char *base = ws_scratch(ws);
+
+    PrepArgs p = {};
+    p.g.p = g->data;
+    p.g.ld = g->ld;
+    p.g.stride = g_stride;
+    p.g.dtype = g->dtype;
+    p.mom = momentum;
+    p.beta = beta;
+    p.eps = eps;
+    p.scale = scale;
+    p.nesterov = nesterov != 0;
+    p.rows = rows;
+    p.cols = cols;
+    p.vec = cols % 8 == 0 && tma_rows_ok(g->data, g->ld, dt_size(g->dtype)) && (g_stride * dt_size(g->dtype)) % 16 == 0 &&
+            (reinterpret_cast<uintptr_t>(momentum) & 15) == 0;
+    p.partial = reinterpret_cast<double *>(base + l.partial);
+    p.hi = reinterpret_cast<__half *>(base + l.x0);
+    p.lo = reinterpret_cast<__half *>(base + l.lo);
+    p.ldx = l.ldx;
+    p.direct = steps == 0;
+    p.o.p = o->data;
+    p.o.ld = o->ld;
+    p.o.stride = o_stride;
+    p.o.dtype = o->dtype;
+    p.o.vec = tma_rows_ok(o->data, o->ld, dt_size(o->dtype)) && (batch == 1 || o_stride * dt_size(o->dtype) % 16 == 0);
+    const int64_t chunks = (int64_t)rows * ((cols + 7) / 8);
+    int64_t blocks = imin<int64_t>(ceil_div<int64_t>(chunks, kPrepThreads), kPrepBlocks);
+    blocks = imin<int64_t>(blocks, imax<int64_t>(1, (int64_t)num_sms() * 8 / batch));
+    const dim3 grid((unsigned)blocks, (unsigned)batch);
+    launch_pdl(ortho_momentum_kernel, grid, dim3(kPrepThreads), 0, s, p);
+    launch_pdl(ortho_scale_kernel, grid, dim3(kPrepThreads), 0, s, p);
+    count_launch(2);
+    rc = check_launch("ortho_scale_kernel");
+    if (rc != CSRT_OK || steps == 0) return rc;
+
+    const bool tall = rows > cols;
+    const int32_t sh = tall ? cols : rows;
+    auto mat = [&](size_t off, int64_t ld, int64_t n_rows) {
+        GMat m = {};
+        m.p = base + off;
+        m.ld = ld;
+        m.stride = ld * n_rows;
+        m.dtype = CSRT_DT_F16;
+        m.vec = 1;
+        return m;
+    };
+    auto op = [&](size_t off, int64_t r, int64_t c, int64_t ld) {
+        GOperand q;
+        q.p = base + off;
+        q.rows = r;
+        q.cols = c;
+        q.ld = ld;
+        q.stride = r * ld;
+        return q;
+    };
+    GArgs common = {};
+    common.batch = batch;
+    common.f16 = 1;
+    common.hdr = static_cast<WsHeader *>(ws);
+    common.counters = ws_counters(ws);
+    size_t xc = l.x0, xn = l.x1;
+    for (int step = 0; step < steps; ++step) {
+        const bool last = step == steps - 1;
+        GProduct q;
+        GArgs a = common;   // A = X X^T or X^T X, times 2^15
+        q.a = q.b = op(xc, rows, cols, l.ldx);
+        q.a_mn = q.b_mn = tall;
+        q.reduction = tall ? rows : cols;
+        a.m = a.n = sh;
+        a.alpha = 1.f / kXScale;
+        a.out0 = mat(l.a, l.lds, sh);
+        rc = launch_gemm16<kEpiGram, false>(q, a, s);
+        if (rc != CSRT_OK) return rc;
+
+        a = common;         // B = b A + c A A, times 2^14
+        q.a = q.b = op(l.a, sh, sh, l.lds);
+        q.a_mn = q.b_mn = false;
+        q.reduction = sh;
+        a.m = a.n = sh;
+        a.alpha = kNsC * 0.5f / kXScale;
+        a.beta = kNsB * 0.5f;
+        a.c0 = mat(l.a, l.lds, sh);
+        a.out0 = mat(l.b, l.lds, sh);
+        rc = launch_gemm16<kEpiPoly, false>(q, a, s);
+        if (rc != CSRT_OK) return rc;
+
+        a = common;         // X' = a X + B X, times 2^15; the last one is o
+        const GOperand ob = op(l.b, sh, sh, l.lds), ox = op(xc, rows, cols, l.ldx);
+        q.a = tall ? ox : ob;
+        q.b = tall ? ob : ox;
+        q.a_mn = false;
+        q.b_mn = !tall;
+        q.reduction = sh;
+        a.m = rows;
+        a.n = cols;
+        a.alpha = 2.f / kXScale;
+        a.beta = kNsA;
+        a.gamma = last ? scale / kXScale : 1.f;
+        a.c0 = mat(xc, l.ldx, rows);
+        a.c1 = mat(l.lo, l.ldx, rows);
+        if (last) {
+            a.out0 = p.o;
+        } else {
+            a.out0 = mat(xn, l.ldx, rows);
+            a.out1 = mat(l.lo, l.ldx, rows);
+        }
+        rc = launch_gemm16<kEpiApply, false>(q, a, s);
+        if (rc != CSRT_OK) return rc;
+        const size_t t = xc;
+        xc = xn;
+        xn = t;
+    }
+    return CSRT_OK;
+}
+
+}  // extern "C"

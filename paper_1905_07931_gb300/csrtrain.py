@@ -20,6 +20,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_lib", "lib
 CSRT_OK, CSRT_ERR_ARG, CSRT_ERR_CUDA, CSRT_ERR_WORKSPACE = 0, 1, 2, 3
 CSRT_DEV_CAPACITY, CSRT_DEV_TIMEOUT, CSRT_DEV_NONFINITE, CSRT_DEV_INVALID = 1, 2, 4, 8
 CSRT_PREC_FP32, CSRT_PREC_TF32 = 0, 1
+CSRT_DT_F32, CSRT_DT_BF16, CSRT_DT_F16 = 0, 1, 2
+CSRT_ACT_NONE, CSRT_ACT_RELU, CSRT_ACT_GELU, CSRT_ACT_SILU = 0, 1, 2, 3
 
 
 class csrt_csr(ctypes.Structure):
@@ -29,6 +31,10 @@ class csrt_csr(ctypes.Structure):
         ("t_row_ptr", c_void_p), ("t_col_idx", c_void_p), ("t_val", c_void_p),
         ("t_pos", c_void_p),
     ]
+
+
+class csrt_mat(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("rows", c_int32), ("cols", c_int32), ("ld", c_int64), ("dtype", c_int32)]
 
 
 class CsrtError(RuntimeError):
@@ -66,6 +72,18 @@ _SIGS = {
                                  c_float, c_float, c_float, POINTER(csrt_csr), c_void_p, c_size_t, c_void_p],
     "weight_grad_prox_update": [POINTER(csrt_csr), c_void_p, c_void_p, c_int32, c_float, c_float, c_int32, c_void_p,
                                 POINTER(csrt_csr), c_void_p, c_size_t, c_void_p],
+    "csrt_dense_workspace_bytes": [c_int32, c_int32, c_int32, POINTER(c_size_t)],
+    "csrt_dense_fwd": [POINTER(csrt_mat), POINTER(csrt_mat), c_void_p, c_int32, POINTER(csrt_mat), POINTER(csrt_mat),
+                       POINTER(csrt_mat), c_void_p, c_size_t, c_void_p],
+    "csrt_dense_bwd_x": [POINTER(csrt_mat), POINTER(csrt_mat), POINTER(csrt_mat), c_int32, POINTER(csrt_mat),
+                         POINTER(csrt_mat), c_void_p, c_size_t, c_void_p],
+    "csrt_dense_bwd_w": [POINTER(csrt_mat), POINTER(csrt_mat), c_int32, POINTER(csrt_mat), c_void_p, c_void_p, c_size_t,
+                         c_void_p],
+    "csrt_dense_act_bwd": [POINTER(csrt_mat), POINTER(csrt_mat), c_int32, POINTER(csrt_mat), c_void_p],
+    "csrt_dense_update": [POINTER(csrt_mat), POINTER(csrt_mat), c_float, c_float, POINTER(csrt_mat), c_void_p],
+    "csrt_orthogonalize_workspace_bytes": [c_int32, c_int32, c_int32, POINTER(c_size_t)],
+    "csrt_orthogonalize": [POINTER(csrt_mat), c_int64, c_int32, c_void_p, c_float, c_int32, c_int32, c_float, c_float,
+                           POINTER(csrt_mat), c_int64, c_void_p, c_size_t, c_void_p],
     "csrt_bias_act_fwd": [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p],
     "csrt_relu_bwd": [c_void_p, c_void_p, c_int64, c_void_p],
     "csrt_bias_grad_sgd": [c_void_p, c_int32, c_int32, c_void_p, c_float, c_void_p, c_void_p],
@@ -202,7 +220,10 @@ class Workspace:
         nbytes = c_size_t(0)
         _check(lib().csrt_workspace_bytes(int(rows), int(cols), int(max_n), ctypes.byref(nbytes)),
                "csrt_workspace_bytes")
-        self.nbytes = int(nbytes.value)
+        self._init(nbytes.value, device, stream)
+
+    def _init(self, nbytes, device, stream):
+        self.nbytes = int(nbytes)
         self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
         _check(lib().csrt_workspace_init(_ptr(self.buf), self.nbytes, _stream(stream)), "csrt_workspace_init")
 
@@ -351,6 +372,122 @@ def weight_grad_prox_update(w_in: CSR, dy: torch.Tensor, x: torch.Tensor, eta: f
 def debias_update(w: CSR, g: torch.Tensor, eta: float, stream=None):
     _f32(g, "g", 1)
     _check(lib().debias_update(w.struct, _ptr(g), float(eta), _stream(stream)), "debias_update")
+
+
+# ---------------------------------------------------------------------------
+# Dense layers and the orthogonalised update
+# ---------------------------------------------------------------------------
+
+_DTYPES = {torch.float32: CSRT_DT_F32, torch.bfloat16: CSRT_DT_BF16, torch.float16: CSRT_DT_F16}
+_ACTS = {"none": CSRT_ACT_NONE, "relu": CSRT_ACT_RELU, "gelu": CSRT_ACT_GELU, "silu": CSRT_ACT_SILU}
+
+
+class DenseWorkspace(Workspace):
+    """Workspace of the dense-layer calls on a layer of m outputs and k inputs
+    with at most max_n columns."""
+
+    def __init__(self, m: int, k: int, max_n: int, device="cuda", stream=None):
+        nbytes = c_size_t(0)
+        _check(lib().csrt_dense_workspace_bytes(int(m), int(k), int(max_n), ctypes.byref(nbytes)),
+               "csrt_dense_workspace_bytes")
+        self._init(nbytes.value, device, stream)
+
+
+class OrthogonalizeWorkspace(Workspace):
+    """Workspace of orthogonalize for `batch` matrices of rows x cols."""
+
+    def __init__(self, batch: int, rows: int, cols: int, device="cuda", stream=None):
+        nbytes = c_size_t(0)
+        _check(lib().csrt_orthogonalize_workspace_bytes(int(batch), int(rows), int(cols), ctypes.byref(nbytes)),
+               "csrt_orthogonalize_workspace_bytes")
+        self._init(nbytes.value, device, stream)
+
+
+def _mat(t, name):
+    """csrt_mat of a 2-D CUDA tensor whose rows are contiguous (any row stride
+    of at least a row)."""
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D CUDA tensor")
+    rows, cols = t.shape
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if ld < cols:
+        if rows > 1:
+            raise ValueError(f"{name}: rows overlap")
+        ld = cols
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        raise ValueError(f"{name}: {t.dtype} is not supported")
+    return csrt_mat(t.data_ptr(), rows, cols, ld, dtype)
+
+
+def _act(act):
+    if act not in _ACTS:
+        raise ValueError(f"unknown activation {act!r}")
+    return _ACTS[act]
+
+
+def dense_fwd(w, x, y, ws: Workspace, bias=None, act: str = "none", residual=None, z=None, stream=None):
+    """y = act(w x + bias) + residual; z (optional) receives w x + bias."""
+    if bias is not None:
+        _f32(bias, "bias", w.shape[0])
+    _check(lib().csrt_dense_fwd(_mat(w, "w"), _mat(x, "x"), _ptr(bias), _act(act),
+                                None if residual is None else _mat(residual, "residual"),
+                                None if z is None else _mat(z, "z"), _mat(y, "y"), ws.ptr, ws.nbytes,
+                                _stream(stream)), "csrt_dense_fwd")
+
+
+def dense_bwd_x(w, dy, dx, ws: Workspace, z_below=None, act: str = "none", residual=None, stream=None):
+    """dx = (w^T dy) * act'(z_below) + residual."""
+    _check(lib().csrt_dense_bwd_x(_mat(w, "w"), _mat(dy, "dy"), None if z_below is None else _mat(z_below, "z_below"),
+                                  _act(act), None if residual is None else _mat(residual, "residual"), _mat(dx, "dx"),
+                                  ws.ptr, ws.nbytes, _stream(stream)), "csrt_dense_bwd_x")
+
+
+def dense_bwd_w(dy, x, dw, ws: Workspace, db=None, accumulate: bool = False, stream=None):
+    """dw = dy x^T and db = the row sums of dy (both added to what is there with accumulate)."""
+    if db is not None:
+        _f32(db, "db", dy.shape[0])
+    _check(lib().csrt_dense_bwd_w(_mat(dy, "dy"), _mat(x, "x"), 1 if accumulate else 0, _mat(dw, "dw"), _ptr(db),
+                                  ws.ptr, ws.nbytes, _stream(stream)), "csrt_dense_bwd_w")
+
+
+def dense_act_bwd(dy, z, act: str, dpre, stream=None):
+    """dpre = dy * act'(z); a conversion with act "none" (z may then be None)."""
+    _check(lib().csrt_dense_act_bwd(_mat(dy, "dy"), None if z is None else _mat(z, "z"), _act(act), _mat(dpre, "dpre"),
+                                    _stream(stream)), "csrt_dense_act_bwd")
+
+
+def dense_update(w, d, eta: float, decay: float = 0.0, w16=None, stream=None):
+    """w <- w (1 - eta decay) - eta d for the float32 w; w16 (optional) receives its 16-bit copy."""
+    _check(lib().csrt_dense_update(_mat(w, "w"), _mat(d, "d"), float(eta), float(decay),
+                                   None if w16 is None else _mat(w16, "w16"), _stream(stream)), "csrt_dense_update")
+
+
+def orthogonalize(g, o, ws: Workspace, momentum=None, beta: float = 0.95, nesterov: bool = True, steps: int = 5,
+                  eps: float = 1e-7, scale: float = 1.0, stream=None):
+    """o = scale * the Newton-Schulz orthogonalisation of the momentum direction
+    of g. g and o are rows x cols, or batch x rows x cols; momentum (float32,
+    contiguous, g's shape) is updated in place, None orthogonalises g itself."""
+    if g.dim() not in (2, 3) or g.shape != o.shape:
+        raise ValueError("g and o must have one shape, rows x cols or batch x rows x cols")
+    batch = 1
+    g_stride = o_stride = 0
+    g2, o2 = g, o
+    if g.dim() == 3:
+        batch = g.shape[0]
+        if batch == 0:
+            return
+        g_stride, o_stride = g.stride(0), o.stride(0)
+        g2, o2 = g[0], o[0]
+    if momentum is not None:
+        if momentum.shape != g.shape:
+            raise ValueError("momentum must have g's shape")
+        _f32(momentum, "momentum")
+    _check(lib().csrt_orthogonalize(_mat(g2, "g"), g_stride, batch, _ptr(momentum), float(beta), 1 if nesterov else 0,
+                                    int(steps), float(eps), float(scale), _mat(o2, "o"), o_stride, ws.ptr, ws.nbytes,
+                                    _stream(stream)), "csrt_orthogonalize")
 
 
 # ---------------------------------------------------------------------------
