@@ -2,7 +2,7 @@
 // elementwise act' and the weight update (include/csrtrain.h). The products run on gemm16_kernel (gemm16.cuh).
 #include <cmath>
 
-#include "gemm16.cuh"
+#include "dense_tokens.cuh"
 #include "gemm16_host.cuh"
 
 namespace csrt {
@@ -110,7 +110,8 @@ static int dense_product(const csrt_mat *am, bool a_mn, const csrt_mat *bm, bool
     a.batch = 1;
     a.out0 = epi_mat(out0);
     a.out1 = epi_mat(out1);
-    if (out0->dtype == CSRT_DT_F32) a.out1.vec = 0;   // the staging slot holds one float32 block, or two 16-bit ones
+    // a staging slot holds two aligned 16-bit blocks, or one block of any other kind
+    if (out1 != nullptr && (out0->dtype == CSRT_DT_F32 || !a.out0.vec || !a.out1.vec)) a.out0.vec = a.out1.vec = 0;
     a.hdr = static_cast<WsHeader *>(ws);
     a.counters = ws_counters(ws);
     a.partial = reinterpret_cast<float *>(ws_scratch(ws));
@@ -244,6 +245,23 @@ int csrt_dense_fwd(const csrt_mat *w, const csrt_mat *x, const float *bias, int3
     }
     CSRT_ARG(!clash(y, x) && !clash(y, w), "y overlaps an operand");
     if (m == 0 || n == 0) return CSRT_OK;
+    if (n <= kTokensMax) {
+        TokenArgs t = {};
+        t.w = static_cast<const uint16_t *>(w->data);
+        t.x = static_cast<const uint16_t *>(x->data);
+        t.ldw = w->ld;
+        t.ldx = x->ld;
+        t.m = m;
+        t.k = k;
+        t.bias = bias;
+        t.act = act;
+        t.res = epi_mat(residual);
+        t.z = epi_mat(z);
+        t.y = epi_mat(y);
+        const bool vec = k % 8 == 0 && tma_rows_ok(w->data, w->ld, 2) && x->ld == n &&
+                         (reinterpret_cast<uintptr_t>(x->data) & 15) == 0;
+        return dense_tokens(t, n, w->dtype == CSRT_DT_F16, vec, as_stream(stream));
+    }
     GArgs a = {};
     a.bias = bias;
     a.act = act;

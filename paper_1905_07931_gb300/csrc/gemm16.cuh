@@ -12,9 +12,9 @@
 //  * warp 0, one lane: TMA producer over a ring of 64-deep stages (full / empty mbarriers);
 //  * warp 1, one lane: tcgen05.mma issue; the accumulator is double-buffered in tensor memory, so a tile's epilogue
 //    overlaps the next tile's loads and products;
-//  * warps 2..9: epilogue. Warp w reads TMEM lanes 32 (w & 3) .. + 31 and every other group of 32 columns, applies
+//  * warps 4..11: epilogue. Warp w reads TMEM lanes 32 (w & 3) .. + 31 and every other group of 32 columns, applies
 //    the epilogue in float32, rounds once, and leaves through 64- or 128-byte swizzled staging and a TMA store
-//    (guarded stores where the output's rows are not 16-byte aligned).
+//    (where the output's rows are not 16-byte aligned: by rows of 32 elements, a lane each).
 // CG = 2 pairs two CTAs of a cluster on one tile of 2 x 128 rows: each holds its 128 rows of A and half the columns
 // of B, and the leader issues the pair's MMAs.
 //
@@ -38,10 +38,10 @@
 namespace csrt {
 
 constexpr int kGBK = 64;                 // reduction depth of a stage (128 bytes)
-constexpr int kGThreads = 320;           // TMA, MMA and eight epilogue warps
+constexpr int kGThreads = 384;           // a warpgroup for TMA and MMA, two for the epilogue
 constexpr int kGEpiWarps = 8;
 constexpr int kPromoteKb = 8;            // stages per tensor-memory accumulation of a float32 output
-constexpr int kGStageOut = 8192;         // staging bytes of an epilogue warp (two slots)
+constexpr int kGStageOut = 4096;         // staging bytes of an epilogue warp
 
 enum { kEpiDense = 0, kEpiGram = 1, kEpiPoly = 2, kEpiApply = 3 };
 
@@ -59,6 +59,7 @@ struct GArgs {
     int32_t units;                    // work units per launch (tiles x splits x batch)
     int32_t splits, kb_split;
     int32_t a_mn, b_mn;               // operand stored MN-major
+    int32_t slots;                    // 32-column groups that an epilogue warp can have in staging: 1 or 2
     int32_t f16;                      // operands and 16-bit epilogue tensors are float16 (else bfloat16)
     // epilogue
     const float *bias;
@@ -92,22 +93,62 @@ __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
 }
 
-// Bounded wait on an mbarrier phase (about a quarter of a second), given up early once the CTA aborts.
+// Bounded wait on an mbarrier phase: gives up after 4e9 cycles (about two seconds), or once the CTA aborts.
+__device__ __forceinline__ bool gtry(uint32_t addr, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(done)
+        : "r"(addr), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+// One look that does not wait (try_wait may hold the warp for microseconds).
+__device__ __forceinline__ bool glook(uint32_t addr, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(done)
+        : "r"(addr), "r"(parity)
+        : "memory");
+    return done != 0;
+}
 __device__ __forceinline__ bool gwait(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
     const uint32_t addr = smem_u32(bar);
-    for (unsigned i = 0; i < (1u << 18); ++i) {
-        uint32_t done;
-        asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
-            " selp.u32 %0, 1, 0, p;\n}\n"
-            : "=r"(done)
-            : "r"(addr), "r"(parity), "r"(1000u)
-            : "memory");
-        if (done) return true;
-        if (*abort_flag) return false;
+    long long t0 = 0;
+#pragma unroll 1
+    for (unsigned i = 1; i < (1u << 30); ++i) {
+        if (gtry(addr, parity)) return true;
+        if ((i & 255) == 0) {
+            if (*abort_flag) return false;
+            const long long t = clock64();
+            if (t0 == 0) t0 = t;
+            else if (t - t0 > 4000000000ll) break;
+        }
     }
     *abort_flag = 1;
     return false;
+}
+
+// The same by a whole warp, which stays together whatever a lane saw.
+__device__ __forceinline__ bool gwait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+    return __all_sync(0xffffffffu, gwait(bar, parity, abort_flag));
+}
+
+// As gwait_warp, where `seen` is the outcome of an earlier look at the barrier: looking at the next stage's barrier
+// before the work of the present one hides the look's latency (about 100 cycles).
+__device__ __forceinline__ bool gwait_seen(bool seen, uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+    if (__all_sync(0xffffffffu, seen)) return true;
+    return gwait_warp(bar, parity, abort_flag);
+}
+
+// One lane of the (whole) warp, the same one every time.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n selp.u32 %0, 1, 0, e;\n}\n" : "=r"(p));
+    return p != 0;
 }
 
 template <int CG>
@@ -184,6 +225,21 @@ __device__ __forceinline__ void commit_own(uint64_t *bar) {
                      : "memory");
 }
 
+__device__ __forceinline__ void tmem_st_32cols(uint32_t taddr, const float (&f)[32]) {
+    uint32_t r[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(f[i]);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
 // ---------------------------------------------------------------------------
 // Element types and activations
 // ---------------------------------------------------------------------------
@@ -199,6 +255,15 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool f16) {
 __device__ __forceinline__ float2 unpack16(uint32_t u, bool f16) {
     if (f16) return __half22float2(*reinterpret_cast<const __half2 *>(&u));
     return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+}
+
+// 16 bytes that are read once: not kept in L1.
+__device__ __forceinline__ uint4 ld_stream_u4(const void *p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p));
+    return v;
 }
 
 __device__ __forceinline__ float load1(const void *p, int64_t i, int dtype) {
@@ -239,30 +304,57 @@ __device__ __forceinline__ float act_deriv(float z, int act) {
     return 1.f;
 }
 
-// 32 consecutive elements of a row of an epilogue operand, as float32 (0 beyond `left`).
-__device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int64_t off, int left) {
-    if (c.vec && left >= 32) {
-        if (c.dtype == CSRT_DT_F32) {
-            const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(c.p) + off);
+// 32 consecutive elements of a row of an epilogue operand, as float32 (0 beyond the matrix). `row` is this lane's
+// row, `col` the warp's first column. Rows that are not 16-byte aligned are read a row at a time, a lane per column,
+// and turned in the warp's staging area `turn` (32 x 33 floats do not fit it, so 16 rows at a time).
+__device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int b, int row, int col, int m, int n,
+                                       float *turn) {
+    const int lane = threadIdx.x & 31;
+    if (c.vec) {
+        const int64_t off = b * c.stride + (int64_t)row * c.ld + col;
+        if (row < m && col + 32 <= n) {
+            if (c.dtype == CSRT_DT_F32) {
+                const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(c.p) + off);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float4 f = p[i];
-                v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
+                for (int i = 0; i < 8; ++i) {
+                    const float4 f = p[i];
+                    v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
+                }
+            } else {
+                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(c.p) + off);
+                const bool h = c.dtype == CSRT_DT_F16;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 u = p[i];
+                    const float2 a = unpack16(u.x, h), d = unpack16(u.y, h), e = unpack16(u.z, h), f = unpack16(u.w, h);
+                    v[8 * i] = a.x, v[8 * i + 1] = a.y, v[8 * i + 2] = d.x, v[8 * i + 3] = d.y;
+                    v[8 * i + 4] = e.x, v[8 * i + 5] = e.y, v[8 * i + 6] = f.x, v[8 * i + 7] = f.y;
+                }
             }
         } else {
-            const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(c.p) + off);
-            const bool h = c.dtype == CSRT_DT_F16;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 u = p[i];
-                const float2 a = unpack16(u.x, h), b = unpack16(u.y, h), d = unpack16(u.z, h), e = unpack16(u.w, h);
-                v[8 * i] = a.x, v[8 * i + 1] = a.y, v[8 * i + 2] = b.x, v[8 * i + 3] = b.y;
-                v[8 * i + 4] = d.x, v[8 * i + 5] = d.y, v[8 * i + 6] = e.x, v[8 * i + 7] = e.y;
-            }
+            for (int i = 0; i < 32; ++i) v[i] = row < m && col + i < n ? load1(c.p, off + i, c.dtype) : 0.f;
         }
     } else {
+        const int row0 = row - lane;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = i < left ? load1(c.p, off + i, c.dtype) : 0.f;
+        for (int part = 0; part < 2; ++part) {
+            float f[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int rr = row0 + part * 16 + r;
+                f[r] = rr < m && col + lane < n ? load1(c.p, b * c.stride + (int64_t)rr * c.ld + col + lane, c.dtype) : 0.f;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int r = 0; r < 16; ++r) turn[r * 33 + lane] = f[r];
+            __syncwarp();
+            if ((lane >> 4) == part) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = turn[(lane & 15) * 33 + i];
+            }
+            __syncwarp();
+        }
     }
 }
 
@@ -288,11 +380,27 @@ __device__ __forceinline__ void store32(const float (&v)[32], const GMat &o, con
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0 && row < m && col < n) tma_store_3d(map, col, row, b, slot);   // lane 0's row is the block's first
-    } else if (row < m) {
-        const int64_t off = b * o.stride + (int64_t)row * o.ld + col;
+    } else {
+        float *turn = reinterpret_cast<float *>(slot);
+        const int row0 = row - lane;
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (col + i < n) store1(o.p, off + i, v[i], o.dtype);
+        for (int part = 0; part < 2; ++part) {
+            __syncwarp();
+            if ((lane >> 4) == part) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) turn[(lane & 15) * 33 + i] = v[i];
+            }
+            __syncwarp();
+            if (col + lane < n) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int rr = row0 + part * 16 + r;
+                    if (rr < m)
+                        store1(o.p, b * o.stride + (int64_t)rr * o.ld + col + lane, turn[r * 33 + lane], o.dtype);
+                }
+            }
+        }
+        __syncwarp();
     }
 }
 
@@ -332,21 +440,23 @@ __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
     return r;
 }
 
-// The epilogue of 32 columns of a row in float32.
+// The epilogue of 32 columns of a row in float32. `slot` is free staging; unaligned operands turn in it before any
+// output is staged, and unaligned outputs turn in it one after the other.
 template <int EPI>
 __device__ __forceinline__ void epilogue32(float (&v)[32], const GArgs &a, const GMaps &maps, uint8_t *slot, int b,
                                            int row, int col) {
-    const int left = row < a.m ? a.n - col : 0;
+    float *turn = reinterpret_cast<float *>(slot);
     if constexpr (EPI == kEpiDense) {
+        float r[32];
+        if (a.c1.p != nullptr) load32(r, a.c1, b, row, col, a.m, a.n, turn);
         if (a.bias != nullptr) {
             const float bi = row < a.m ? __ldg(a.bias + row) : 0.f;
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += bi;
         }
-        if (a.out1.p != nullptr) store32(v, a.out1, &maps.out1, slot + 2048, b, row, col, a.m, a.n);
         if (a.act_grad) {
             float z[32];
-            load32(z, a.c0, b * a.c0.stride + (int64_t)row * a.c0.ld + col, left);
+            load32(z, a.c0, b, row, col, a.m, a.n, turn);
             if (a.act == CSRT_ACT_RELU) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_RELU);
@@ -357,19 +467,21 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const GArgs &a, const
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_SILU);
             }
-        } else if (a.act == CSRT_ACT_RELU) {
+        } else {
+            // z and y are both aligned or both not (checked on the host): their stagings do not meet
+            if (a.out1.p != nullptr) store32(v, a.out1, &maps.out1, a.out1.vec ? slot + 2048 : slot, b, row, col, a.m, a.n);
+            if (a.act == CSRT_ACT_RELU) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_RELU);
-        } else if (a.act == CSRT_ACT_GELU) {
+                for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_RELU);
+            } else if (a.act == CSRT_ACT_GELU) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_GELU);
-        } else if (a.act == CSRT_ACT_SILU) {
+                for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_GELU);
+            } else if (a.act == CSRT_ACT_SILU) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_SILU);
+                for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_SILU);
+            }
         }
         if (a.c1.p != nullptr) {
-            float r[32];
-            load32(r, a.c1, b * a.c1.stride + (int64_t)row * a.c1.ld + col, left);
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += r[i];
         }
@@ -380,18 +492,17 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const GArgs &a, const
             for (int i = 0; i < 32; ++i) v[i] *= a.alpha;
         } else {
             float c[32];
-            load32(c, a.c0, b * a.c0.stride + (int64_t)row * a.c0.ld + col, left);
+            load32(c, a.c0, b, row, col, a.m, a.n, turn);
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = a.alpha * v[i] + a.beta * c[i];
         }
         store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
     } else {
         float c[32];
-        const int64_t off = b * a.c0.stride + (int64_t)row * a.c0.ld + col;
-        load32(c, a.c0, off, left);
+        load32(c, a.c0, b, row, col, a.m, a.n, turn);
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = a.alpha * v[i] + a.beta * c[i];
-        load32(c, a.c1, off, left);
+        load32(c, a.c1, b, row, col, a.m, a.n, turn);
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = (v[i] + a.beta * c[i]) * a.gamma;
         store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
@@ -486,18 +597,24 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     const uint32_t tmem = *tmem_slot;
     pdl_enter();
 
+    // The sums of PROMOTE take the registers that the first warpgroup does not need:
+    // 128 x 40 + 256 x 232 = 384 x 168, the launch's own total.
     if (warp == 0) {
-        if (lane == 0) {
-            int it = 0;
-            for (int u = unit0; u < a.units && !s_abort; u += ustep) {
-                const GUnit w = unit_of<SYM>(a, u);
-                const int m0 = (w.tm * CG + (int)rank) * 128, n0 = w.tn * BN + (int)rank * kBRows;
-                for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
-                    const int s = it % kStages;
-                    if (!gwait(empty + s, ((it / kStages) & 1) ^ 1, &s_abort)) break;
-                    uint8_t *sa = smem + s * kStageBytes, *sb = sa + kABytes;
-                    uint32_t bar = smem_u32(full + s);
-                    if constexpr (CG == 2) bar = mapa_u32(bar, 0);
+        if constexpr (PROMOTE) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        int s = 0, issued = 0;
+        uint32_t ph = 1;
+        bool seen = true;   // the ring starts empty
+        for (int u = unit0; u < a.units && !s_abort; u += ustep) {
+            const GUnit w = unit_of<SYM>(a, u);
+            const int m0 = (w.tm * CG + (int)rank) * 128, n0 = w.tn * BN + (int)rank * kBRows;
+            for (int kb = w.kb0; kb < w.kb1; ++kb) {
+                if (!gwait_seen(seen, empty + s, ph, &s_abort)) break;
+                const int s1 = s + 1 == kStages ? 0 : s + 1;
+                seen = glook(smem_u32(empty + s1), s1 == 0 ? ph ^ 1 : ph);
+                uint8_t *sa = smem + s * kStageBytes, *sb = sa + kABytes;
+                uint32_t bar = smem_u32(full + s);
+                if constexpr (CG == 2) bar = mapa_u32(bar, 0);
+                if (elect_one()) {
                     if (rank == 0) mbar_expect_tx(full + s, CG * kStageBytes);
                     if (a.a_mn) {
 #pragma unroll
@@ -514,48 +631,72 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         tma_load_3d<CG>(sb, &maps.b, kb * kGBK, n0, w.b, bar);
                     }
                 }
+                issued = imin(issued + 1, kStages);
+                if (++s == kStages) s = 0, ph ^= 1;
             }
-            // an aborted CTA's loads in flight must land before it may exit (its own barriers show them on rank 0)
-            if (s_abort && rank == 0)
-                for (int i = imax(0, it - kStages); i < it; ++i) mbar_wait(full + i % kStages, (i / kStages) & 1);
         }
+        // an aborted CTA's loads in flight must land before it may exit (rank 0's barriers count the pair's bytes)
+        if (s_abort && rank == 0 && lane == 0)
+            for (int i = 0; i < issued; ++i) {
+                if (--s < 0) s = kStages - 1, ph ^= 1;
+                mbar_wait(full + s, ph ^ 1);
+            }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if constexpr (PROMOTE) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (rank == 0) {
+            // The whole warp walks the stages and one lane issues: descriptors and addresses stay uniform, which
+            // keeps the issue of a stage's four MMAs short (a lone lane took about 290 cycles for them, more than a
+            // 128-column tile's MMAs themselves).
             const uint32_t idesc = (1u << 4) | ((a.f16 ? 0u : 1u) << 7) | ((a.f16 ? 0u : 1u) << 10) |
                                    ((uint32_t)a.a_mn << 15) | ((uint32_t)a.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
                                    ((uint32_t)((128 * CG) >> 4) << 24);
-            const uint32_t a_step = a.a_mn ? 2048 : 32, b_step = a.b_mn ? 2048 : 32;
-            int it = 0, j = 0;
+            const uint32_t a_step = (a.a_mn ? 2048 : 32) >> 4, b_step = (a.b_mn ? 2048 : 32) >> 4;
+            const uint64_t a0 = gdesc(smem_u32(smem), a.a_mn), b0 = gdesc(smem_u32(smem) + kABytes, a.b_mn);
+            int s = 0, j = 0;
+            uint32_t ph = 0;
+            bool seen = false;
             for (int u = unit0; u < a.units && !s_abort; u += ustep) {
                 const GUnit w = unit_of<SYM>(a, u);
                 int kb = w.kb0;
                 do {   // one accumulation: the whole unit, or kPromoteKb stages of it
                     const int stop = PROMOTE ? min(w.kb1, kb + kPromoteKb) : w.kb1;
                     const int acc = j & 1;
-                    if (!gwait(acce + acc, ((j >> 1) & 1) ^ 1, &s_abort)) break;
+                    if (!gwait_warp(acce + acc, ((j >> 1) & 1) ^ 1, &s_abort)) break;
                     ++j;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t d = tmem + (uint32_t)(acc * BN);
-                    for (const int first = kb; kb < stop; ++kb, ++it) {
-                        const int s = it % kStages;
-                        if (!gwait(full + s, (it / kStages) & 1, &s_abort)) break;
+                    uint32_t more = 0;   // the first product overwrites the accumulator
+                    for (; kb < stop; ++kb) {
+                        if (!gwait_seen(seen, full + s, ph, &s_abort)) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint32_t sa = smem_u32(smem + s * kStageBytes), sb = sa + kABytes;
+                        const int s1 = s + 1 == kStages ? 0 : s + 1;
+                        seen = glook(smem_u32(full + s1), s1 == 0 ? ph ^ 1 : ph);
+                        const uint64_t ad = a0 + (uint32_t)(s * (kStageBytes >> 4)), bd = b0 + (uint32_t)(s * (kStageBytes >> 4));
+                        if (elect_one()) {
+                            mma_16<CG>(d, ad, bd, idesc, more);
 #pragma unroll
-                        for (int k = 0; k < kGBK / 16; ++k)
-                            mma_16<CG>(d, gdesc(sa + k * a_step, a.a_mn), gdesc(sb + k * b_step, a.b_mn), idesc,
-                                       (kb > first || k > 0) ? 1u : 0u);
-                        commit_to<CG>(empty + s);
+                            for (uint32_t k = 1; k < kGBK / 16; ++k)
+                                mma_16<CG>(d, ad + k * a_step, bd + k * b_step, idesc, 1);
+                            commit_to<CG>(empty + s);
+                        }
+                        more = 1;
+                        if (++s == kStages) s = 0, ph ^= 1;
                     }
-                    commit_to<CG>(accf + acc);
+                    if (elect_one()) commit_to<CG>(accf + acc);
                 } while (kb < w.kb1 && !s_abort);
+                __syncwarp();
             }
-            commit_own<CG>(fin);
+            __syncwarp();
+            if (elect_one()) commit_own<CG>(fin);
             mbar_wait(fin, 0);   // nothing of ours still runs on the tensor cores
+            __syncwarp();
         }
+    } else if (warp < 4) {
+        if constexpr (PROMOTE) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;
-        uint8_t *stage0 = epi + (warp - 2) * kGStageOut;
+        if constexpr (PROMOTE) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        uint8_t *stage0 = epi + (warp - 4) * kGStageOut;
         uint32_t acce_bar[2] = {smem_u32(acce), smem_u32(acce + 1)};
         if constexpr (CG == 2) {
             acce_bar[0] = mapa_u32(acce_bar[0], 0);
@@ -566,10 +707,16 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             const GUnit w = unit_of<SYM>(a, u);
             const int row = (w.tm * CG + (int)rank) * 128 + q * 32 + lane, n0 = w.tn * BN;
             const bool empty_sum = w.kb1 <= w.kb0;
-            float sums[PROMOTE ? kChunks / 2 : 1][32];
             bool ok = true;
-            int kb = w.kb0;
             uint32_t d = 0;
+            float sums[PROMOTE ? kChunks / 2 : 1][32];
+            if constexpr (PROMOTE) {
+#pragma unroll
+                for (int i = 0; i < kChunks / 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sums[i][e] = 0.f;
+            }
+            int kb = w.kb0;
             do {
                 const int acc = j & 1;
                 ok = __all_sync(0xffffffffu, gwait(accf + acc, (j >> 1) & 1, &s_abort));
@@ -577,23 +724,30 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 d = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
                 if constexpr (PROMOTE) {
+                    const bool first = kb == w.kb0;
+                    kb += kPromoteKb;
+                    if (first && kb >= w.kb1) break;   // a short sum stays as it is
 #pragma unroll
                     for (int i = 0; i < kChunks / 2; ++i) {
                         uint32_t r[32];
                         tmem_ld_32cols(d + (uint32_t)((2 * i + half) * 32), r);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            sums[i][e] = empty_sum ? 0.f
-                                                   : (kb == w.kb0 ? __uint_as_float(r[e])
-                                                                  : sums[i][e] + __uint_as_float(r[e]));
+                        for (int e = 0; e < 32; ++e) sums[i][e] += __uint_as_float(r[e]);
                     }
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0)
-                        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(acce_bar[acc])
-                                     : "memory");
-                    ++j;
-                    kb += kPromoteKb;
+                    if (kb < w.kb1) {
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0)
+                            asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                                             acce_bar[acc])
+                                         : "memory");
+                        ++j;
+                    } else {   // the whole sums go back to this accumulator's place
+#pragma unroll
+                        for (int i = 0; i < kChunks / 2; ++i)
+                            tmem_st_32cols(d + (uint32_t)((2 * i + half) * 32), sums[i]);
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    }
                 } else {
                     kb = w.kb1;
                 }
@@ -612,7 +766,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     __threadfence();
                     __syncwarp();
                     int n_in = 0;
-                    int32_t *cnt = a.counters + ((int64_t)w.tile * CG + rank) * kGEpiWarps + (warp - 2);
+                    int32_t *cnt = a.counters + ((int64_t)w.tile * CG + rank) * kGEpiWarps + (warp - 4);
                     if (lane == 0) n_in = atomicAdd(cnt, 1);
                     n_in = __shfl_sync(0xffffffffu, n_in, 0);
                     last = n_in == a.splits - 1;
@@ -620,28 +774,23 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     if (lane == 0) *cnt = 0;
                     __threadfence();
                 }
-#pragma unroll(PROMOTE ? kChunks / 2 : 1)
+#pragma unroll 1
                 for (int i = 0; i < kChunks / 2; ++i) {
                     const int ci = 2 * i + half;
                     float v[32];
                     if (pass == 0) {
-                        if constexpr (PROMOTE) {
+                        uint32_t r[32];
+                        tmem_ld_32cols(d + (uint32_t)(ci * 32), r);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = sums[i][e];
-                        } else {
-                            uint32_t r[32];
-                            tmem_ld_32cols(d + (uint32_t)(ci * 32), r);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = empty_sum ? 0.f : __uint_as_float(r[e]);
-                            if (i == kChunks / 2 - 1) {
-                                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                                __syncwarp();
-                                if (lane == 0)
-                                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
-                                                     acce_bar[j & 1])
-                                                 : "memory");
-                                ++j;
-                            }
+                        for (int e = 0; e < 32; ++e) v[e] = empty_sum ? 0.f : __uint_as_float(r[e]);
+                        if (i == kChunks / 2 - 1) {
+                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0)
+                                asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                                                 acce_bar[j & 1])
+                                             : "memory");
+                            ++j;
                         }
                         if (a.splits > 1) {
                             float *p = part + (int64_t)w.split * CG * slab + (int64_t)ci * 32 * 128;
@@ -660,11 +809,14 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     }
                     const int col = n0 + ci * 32;
                     if (col >= a.n) continue;
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    if (lane == 0) {
+                        if (a.slots == 2) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                        else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    }
                     __syncwarp();
                     epilogue32<EPI>(v, a, maps, stage0 + slot * (kGStageOut / 2), w.b, row, col);
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                    slot ^= 1;
+                    slot = a.slots == 2 ? slot ^ 1 : 0;
                     if constexpr (SYM)
                         if (w.tm != w.tn) mirror32(v, a.out0, w.b, row, col, a.m, a.n);
                 }

@@ -79,6 +79,9 @@ int launch_tile(const GProduct &p, GArgs a, cudaStream_t s) {
         return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused an output");
     if (a.out1.vec && !out_map(&maps.out1, a.out1, a.m, a.n, a.batch))
         return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused an output");
+    // one aligned 16-bit output and no operand to turn: a group needs half the staging
+    const bool turns = !a.out0.vec || (a.c0.p != nullptr && !a.c0.vec) || (a.c1.p != nullptr && !a.c1.vec);
+    a.slots = a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !turns ? 2 : 1;
     auto kernel = gemm16_kernel<CG, BN, EPI, PROMOTE>;
     constexpr int smem = gsmem_bytes<CG, BN>();
     static bool attr_set[64] = {false};
@@ -94,9 +97,50 @@ int launch_tile(const GProduct &p, GArgs a, cudaStream_t s) {
     return check_launch("gemm16_kernel");
 }
 
+// Time of a product in microseconds by a simple model of gemm16_kernel: waves of units, each loading its stages and
+// then running an epilogue that overlaps the next unit's stages but not the last's; joining slices costs their
+// partial tiles' trip through L2.
+struct GTile {
+    int cg, bn;
+    double stage, epi;   // us per stage, us per unit's epilogue
+};
+inline double model_us(const GTile &t, int64_t tiles, int64_t kb, int64_t splits) {
+    const int64_t slots = imax(1, num_sms() / t.cg);
+    const int64_t units = tiles * splits, waves = ceil_div(units, slots);
+    const double unit = (double)ceil_div(imax<int64_t>(kb, 1), splits) * t.stage;
+    double us = 2.0 + waves * (unit > t.epi ? unit : t.epi) + t.epi;
+    if (splits > 1) us += 1.0 + 0.5 * splits;
+    return us;
+}
+
 template <int EPI, bool PROMOTE>
-int launch_gemm16(const GProduct &p, const GArgs &a, cudaStream_t s) {
+int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the dense products need a GPU with tcgen05");
+    const bool sym = EPI == kEpiGram || EPI == kEpiPoly;
+    const GTile cand[3] = {{2, 256, 0.36, 4.0}, {1, 128, 0.26, 2.5}, {1, 64, 0.22, 1.6}};
+    const int64_t kb = ceil_div<int64_t>(p.reduction, kGBK);
+    int best = 0, best_s = 1;
+    double best_us = 1e30;
+    for (int c = 0; c < (sym ? 2 : 3); ++c) {
+        const GTile &t = cand[c];
+        const int64_t tm = ceil_div<int64_t>(a.m, 128 * t.cg), tn = ceil_div<int64_t>(a.n, t.bn);
+        const int64_t tiles = a.batch * (sym ? tm * (tm + 1) / 2 : tm * tn);
+        for (int64_t sp = 1; sp <= 32 && sp * 4 <= imax<int64_t>(kb, 4); ++sp) {
+            if (sp > 1 && ((size_t)(tiles * sp) * t.cg * 128 * t.bn * sizeof(float) > kPartialBytes ||
+                           tiles * t.cg * kGEpiWarps > (int64_t)kWsCounterInts || a.partial == nullptr))
+                break;
+            const double us = model_us(t, tiles, kb, sp);
+            if (us < best_us) {
+                best_us = us;
+                best = c;
+                best_s = (int)sp;
+            }
+        }
+    }
+    a.splits = best_s;
+    if (best == 0) return launch_tile<2, 256, EPI, PROMOTE>(p, a, s);
+    if constexpr (EPI == kEpiDense)
+        if (best == 2) return launch_tile<1, 64, EPI, PROMOTE>(p, a, s);
     return launch_tile<1, 128, EPI, PROMOTE>(p, a, s);
 }
 
