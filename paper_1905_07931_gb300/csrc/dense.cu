@@ -95,7 +95,8 @@ static GMat epi_mat(const csrt_mat *m) {
     return g;
 }
 
-// D = A B^T with the dense epilogue.
+// D = A B^T with the epilogue of the forward (kEpiFwd) or the backward products.
+template <int EPI>
 static int dense_product(const csrt_mat *am, bool a_mn, const csrt_mat *bm, bool b_mn, GArgs a, csrt_mat *out0,
                          csrt_mat *out1, void *ws, cudaStream_t s) {
     GProduct p;
@@ -116,7 +117,7 @@ static int dense_product(const csrt_mat *am, bool a_mn, const csrt_mat *bm, bool
     a.counters = ws_counters(ws);
     a.partial = reinterpret_cast<float *>(ws_scratch(ws));
     p.reduction = a_mn ? am->rows : am->cols;
-    return out0->dtype == CSRT_DT_F32 ? launch_gemm16<kEpiDense, true>(p, a, s) : launch_gemm16<kEpiDense, false>(p, a, s);
+    return out0->dtype == CSRT_DT_F32 ? launch_gemm16<EPI, true>(p, a, s) : launch_gemm16<EPI, false>(p, a, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -266,7 +267,7 @@ int csrt_dense_fwd(const csrt_mat *w, const csrt_mat *x, const float *bias, int3
     a.bias = bias;
     a.act = act;
     a.c1 = epi_mat(residual);
-    return dense_product(w, false, x, true, a, y, z, ws, as_stream(stream));
+    return dense_product<kEpiFwd>(w, false, x, true, a, y, z, ws, as_stream(stream));
 }
 
 int csrt_dense_bwd_x(const csrt_mat *w, const csrt_mat *dy, const csrt_mat *z_below, int32_t act,
@@ -297,10 +298,9 @@ int csrt_dense_bwd_x(const csrt_mat *w, const csrt_mat *dy, const csrt_mat *z_be
     if (k == 0 || n == 0) return CSRT_OK;
     GArgs a = {};
     a.act = act;
-    a.act_grad = act != CSRT_ACT_NONE;
-    if (a.act_grad) a.c0 = epi_mat(z_below);
+    if (act != CSRT_ACT_NONE) a.c0 = epi_mat(z_below);
     a.c1 = epi_mat(residual);
-    return dense_product(w, true, dy, true, a, dx, nullptr, ws, as_stream(stream));
+    return dense_product<kEpiBwd>(w, true, dy, true, a, dx, nullptr, ws, as_stream(stream));
 }
 
 int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, csrt_mat *dw, float *db, void *ws,
@@ -329,7 +329,7 @@ int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, 
     if (m == 0 || k == 0) return CSRT_OK;
     GArgs a = {};
     if (accumulate) a.c1 = epi_mat(dw);
-    return dense_product(dy, false, x, false, a, dw, nullptr, ws, s);
+    return dense_product<kEpiBwd>(dy, false, x, false, a, dw, nullptr, ws, s);
 }
 
 int csrt_dense_act_bwd(const csrt_mat *dy, const csrt_mat *z, int32_t act, csrt_mat *dpre, void *stream) {

@@ -41,9 +41,12 @@ constexpr int kGBK = 64;                 // reduction depth of a stage (128 byte
 constexpr int kGThreads = 384;           // a warpgroup for TMA and MMA, two for the epilogue
 constexpr int kGEpiWarps = 8;
 constexpr int kPromoteKb = 8;            // stages per tensor-memory accumulation of a float32 output
+constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
+constexpr float kXScale = 32768.f, kInvXScale = 1.f / 32768.f;   // scale of X and A in float16; B's is half of it
 constexpr int kGStageOut = 4096;         // staging bytes of an epilogue warp
 
-enum { kEpiDense = 0, kEpiGram = 1, kEpiPoly = 2, kEpiApply = 3 };
+enum { kEpiFwd = 0, kEpiBwd = 1, kEpiNs = 2 };
+enum { kNsGram = 0, kNsPoly = 1, kNsApply = 2 };   // the products of a Newton-Schulz step (GArgs::kind)
 
 // An epilogue operand or output: row-major m x n, batch matrices `stride` elements apart.
 struct GMat {
@@ -63,8 +66,12 @@ struct GArgs {
     int32_t f16;                      // operands and 16-bit epilogue tensors are float16 (else bfloat16)
     // epilogue
     const float *bias;
-    int32_t act, act_grad;            // activation; act_grad: multiply by act'(c0) instead
-    float alpha, beta, gamma;         // orthogonalisation: alpha acc + beta c0 (+ beta c1)
+    int32_t act;                      // activation (kEpiFwd), or act' of c0 as a factor (kEpiBwd)
+    int32_t kind, sym, tall;          // kEpiNs: kNs*, tiles on and above the diagonal only, X has more rows than columns
+    float alpha, gamma;               // kEpiNs: scale of the sum, of the result
+    const float *diag_in;             // kEpiNs: diagonal of A (kNsPoly) or B (kNsApply), s_pad per matrix
+    float *diag_out;                  // kEpiNs: diagonal of A (kNsGram) or B (kNsPoly)
+    int32_t s_pad;
     GMat c0, c1;                      // z_below / A / X high; residual / X low
     GMat out0, out1;                  // y, dx, dW, A, B, X high, O; z, X low
     float *partial;                   // split slices
@@ -75,6 +82,25 @@ struct GArgs {
 struct GMaps {
     CUtensorMap a, b, out0, out1;
 };
+
+// A launch: one product, or the products of all Newton-Schulz steps one after the other (kNsSets different ones,
+// see ns_set), with a barrier of the whole (cooperative) grid between them.
+constexpr int kNsSets = 6;
+template <int EPI>
+struct GLaunch {
+    static constexpr int kSets = EPI == kEpiNs ? kNsSets : 1;
+    GMaps maps[kSets];
+    GArgs args[kSets];
+    int32_t phases;
+    uint32_t *arrived;                // CTAs that have finished a phase, all phases together; zero at the start
+};
+
+// Sets of a Newton-Schulz launch: A of the even and odd steps' X, B, X' of the even and odd steps, the last X'.
+__device__ __forceinline__ int ns_set(int phase, int phases) {
+    if (phases == 1) return 0;   // a launch of one product
+    const int step = phase / 3, k = phase - 3 * step;
+    return k == 0 ? (step & 1) : k == 1 ? 2 : phase == phases - 1 ? 5 : 3 + (step & 1);
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -142,6 +168,27 @@ __device__ __forceinline__ bool gwait_warp(uint64_t *bar, uint32_t parity, volat
 __device__ __forceinline__ bool gwait_seen(bool seen, uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
     if (__all_sync(0xffffffffu, seen)) return true;
     return gwait_warp(bar, parity, abort_flag);
+}
+
+// Wait of a whole warp until `arrived` reaches `target`; bounded like gwait.
+__device__ __forceinline__ bool grid_wait(const uint32_t *arrived, uint32_t target, volatile int *abort_flag) {
+    bool ok = false;
+    if ((threadIdx.x & 31) == 0) {
+        const long long t0 = clock64();
+        for (unsigned i = 1; i < (1u << 30); ++i) {
+            uint32_t v;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
+            if (v >= target) {
+                ok = true;
+                break;
+            }
+            if (*abort_flag || ((i & 255) == 0 && clock64() - t0 > 4000000000ll)) break;
+        }
+        if (!ok) *abort_flag = 1;
+    }
+    ok = __all_sync(0xffffffffu, ok || (threadIdx.x & 31) != 0);
+    __syncwarp();
+    return ok;
 }
 
 // One lane of the (whole) warp, the same one every time.
@@ -412,21 +459,22 @@ struct GUnit {
 };
 
 // Unit u: batch matrix, tile and slice. Tiles run down bands of eight tile rows, so that the units in flight share
-// operand tiles in L2. A symmetric product (kEpiGram, kEpiPoly) has the tiles on and above the diagonal only.
-template <bool SYM>
+// operand tiles in L2. A symmetric product has the tiles that reach above the diagonal only: tile row i starts at
+// tile column R i, R tile columns to a tile row.
+template <int R>
 __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
     GUnit r;
-    const int tiles = SYM ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
+    const int tiles = a.sym ? a.tiles_m * a.tiles_n - R * (a.tiles_m * (a.tiles_m - 1) / 2) : a.tiles_m * a.tiles_n;
     r.split = u % a.splits;
     const int t = u / a.splits;
     r.tile = t;
     r.b = t / tiles;
     int q = t - r.b * tiles;
-    if (SYM) {
+    if (a.sym) {
         int i = 0;
-        while (q >= a.tiles_m - i) q -= a.tiles_m - i++;
+        while (q >= a.tiles_n - R * i) q -= a.tiles_n - R * i++;
         r.tm = i;
-        r.tn = i + q;
+        r.tn = R * i + q;
     } else {
         constexpr int kBand = 8;
         const int band = q / (kBand * a.tiles_n), first = band * kBand;
@@ -440,23 +488,77 @@ __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
     return r;
 }
 
+// An epilogue operand's 32 elements, 16-bit and aligned, fetched ahead of their use (through L2: another SM may have
+// written them earlier in this launch).
+__device__ __forceinline__ bool ahead_ok(const GMat &c, int col, int n) {
+    return c.p != nullptr && c.vec && c.dtype != CSRT_DT_F32 && col + 32 <= n;
+}
+__device__ __forceinline__ void fetch_ahead(uint32_t (&u)[16], const GMat &c, int b, int row, int col, int m, int n) {
+    if (ahead_ok(c, col, n) && row < m) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(c.p) + b * c.stride +
+                                                         (int64_t)row * c.ld + col);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 q = __ldcg(p + i);
+            u[4 * i] = q.x, u[4 * i + 1] = q.y, u[4 * i + 2] = q.z, u[4 * i + 3] = q.w;
+        }
+    }
+}
+// The diagonal at this lane's row (once per unit) and at column col + lane.
+__device__ __forceinline__ float diag_ahead(const GArgs &a, int b, int at, int limit) {
+    return a.diag_in != nullptr && at < limit ? __ldcg(a.diag_in + (int64_t)b * a.s_pad + at) : 0.f;
+}
+__device__ __forceinline__ void take32(float (&v)[32], const uint32_t (&u)[16], const GMat &c, int b, int row, int col,
+                                       int m, int n, float *turn) {
+    if (ahead_ok(c, col, n)) {
+        const bool h = c.dtype == CSRT_DT_F16;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float2 f = unpack16(u[i], h);
+            v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        }
+    } else {
+        load32(v, c, b, row, col, m, n, turn);
+    }
+}
+
 // The epilogue of 32 columns of a row in float32. `slot` is free staging; unaligned operands turn in it before any
-// output is staged, and unaligned outputs turn in it one after the other.
+// output is staged, and unaligned outputs turn in it one after the other. u0, u1: c0 and c1 fetched ahead;
+// di, dj: the diagonal (GArgs::diag_in) at this lane's row and at column col + lane.
 template <int EPI>
-__device__ __forceinline__ void epilogue32(float (&v)[32], const GArgs &a, const GMaps &maps, uint8_t *slot, int b,
-                                           int row, int col) {
+__device__ __forceinline__ void epilogue32(float (&v)[32], const uint32_t (&u0)[16], const uint32_t (&u1)[16],
+                                           float di, float dj, const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col) {
     float *turn = reinterpret_cast<float *>(slot);
-    if constexpr (EPI == kEpiDense) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (EPI == kEpiFwd) {
         float r[32];
-        if (a.c1.p != nullptr) load32(r, a.c1, b, row, col, a.m, a.n, turn);
+        if (a.c1.p != nullptr) take32(r, u1, a.c1, b, row, col, a.m, a.n, turn);
         if (a.bias != nullptr) {
             const float bi = row < a.m ? __ldg(a.bias + row) : 0.f;
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += bi;
         }
-        if (a.act_grad) {
+        // z and y are both aligned or both not (checked on the host): their stagings do not meet
+        if (a.out1.p != nullptr) store32(v, a.out1, &maps.out1, a.out1.vec ? slot + 2048 : slot, b, row, col, a.m, a.n);
+        if (a.act == CSRT_ACT_RELU) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_RELU);
+        } else if (a.act == CSRT_ACT_GELU) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_GELU);
+        } else if (a.act == CSRT_ACT_SILU) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_SILU);
+        }
+        if (a.c1.p != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] += r[i];
+        }
+        store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
+    } else if constexpr (EPI == kEpiBwd) {
+        if (a.c0.p != nullptr) {
             float z[32];
-            load32(z, a.c0, b, row, col, a.m, a.n, turn);
+            take32(z, u0, a.c0, b, row, col, a.m, a.n, turn);
             if (a.act == CSRT_ACT_RELU) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_RELU);
@@ -467,44 +569,58 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const GArgs &a, const
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_SILU);
             }
-        } else {
-            // z and y are both aligned or both not (checked on the host): their stagings do not meet
-            if (a.out1.p != nullptr) store32(v, a.out1, &maps.out1, a.out1.vec ? slot + 2048 : slot, b, row, col, a.m, a.n);
-            if (a.act == CSRT_ACT_RELU) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_RELU);
-            } else if (a.act == CSRT_ACT_GELU) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_GELU);
-            } else if (a.act == CSRT_ACT_SILU) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_SILU);
-            }
         }
         if (a.c1.p != nullptr) {
+            float r[32];
+            take32(r, u1, a.c1, b, row, col, a.m, a.n, turn);
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += r[i];
         }
         store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
-    } else if constexpr (EPI == kEpiGram || EPI == kEpiPoly) {
-        if constexpr (EPI == kEpiGram) {
+    } else if (a.kind != kNsApply) {
+        // A or B: the diagonal goes to its own float32 vector and is left out of the float16 matrix. Warps' rows and
+        // columns start at multiples of 32, so a diagonal element of this group, if any, is element `lane`.
+        const bool on_diag = row - lane == col;
+        float d = 0.f;
+        if (a.kind == kNsGram) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] *= a.alpha;
-        } else {
-            float c[32];
-            load32(c, a.c0, b, row, col, a.m, a.n, turn);
+            if (on_diag) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = a.alpha * v[i] + a.beta * c[i];
+                for (int i = 0; i < 32; ++i)
+                    if (i == lane) d = v[i], v[i] = 0.f;
+                d *= kInvXScale;
+            }
+        } else {
+            // off the diagonal b R + c ((d_i + d_j) R + (R R)_ij), on it b d_i + c (d_i^2 + (R R)_ii)
+            float r[32];
+            take32(r, u0, a.c0, b, row, col, a.m, a.n, turn);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                v[i] = a.alpha * v[i] + 0.5f * (kNsB + kNsC * (di + __shfl_sync(0xffffffffu, dj, i))) * r[i];
+            if (on_diag) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i == lane) d = v[i], v[i] = 0.f;
+                d = kNsB * di + kNsC * di * di + d * (2.f * kInvXScale);
+            }
         }
+        if (on_diag && row < a.m) a.diag_out[(int64_t)b * a.s_pad + row] = d;
         store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
     } else {
-        float c[32];
-        load32(c, a.c0, b, row, col, a.m, a.n, turn);
+        // (a + e) X + B X with the diagonal e of B by row (or by column where X has more rows than columns)
+        float c[32], t[32];
+        take32(c, u0, a.c0, b, row, col, a.m, a.n, turn);
+        take32(t, u1, a.c1, b, row, col, a.m, a.n, turn);
+        if (a.tall) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = a.alpha * v[i] + a.beta * c[i];
-        load32(c, a.c1, b, row, col, a.m, a.n, turn);
+            for (int i = 0; i < 32; ++i)
+                v[i] = (a.alpha * v[i] + (kNsA + __shfl_sync(0xffffffffu, dj, i)) * (c[i] + t[i])) * a.gamma;
+        } else {
+            const float e = kNsA + di;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = (v[i] + a.beta * c[i]) * a.gamma;
+            for (int i = 0; i < 32; ++i) v[i] = (a.alpha * v[i] + e * (c[i] + t[i])) * a.gamma;
+        }
         store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
         if (a.out1.p != nullptr) {   // what float16 drops of X, kept beside it
 #pragma unroll
@@ -538,9 +654,10 @@ constexpr int gsmem_bytes() {
 
 template <int CG, int BN, int EPI, bool PROMOTE>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
-    gemm16_kernel(const __grid_constant__ GMaps maps, const __grid_constant__ GArgs a) {
+    gemm16_kernel(const __grid_constant__ GLaunch<EPI> L) {
     static_assert(BN % 64 == 0 && BN / CG >= 64 && 2 * BN <= 512, "two accumulators in tensor memory");
-    constexpr bool SYM = EPI == kEpiGram || EPI == kEpiPoly;
+    constexpr bool NS = EPI == kEpiNs;
+    constexpr int R = 128 * CG / BN;                      // tile columns to a tile row (symmetric products)
     constexpr int kStages = gstages<CG, BN>();
     constexpr int kStageBytes = gstage_bytes<CG, BN>();
     constexpr int kABytes = 128 * 128;
@@ -555,8 +672,10 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     uint64_t *accf = empty + kStages;    // [2] accumulator ready
     uint64_t *acce = accf + 2;           // [2] accumulator drained
     uint64_t *fin = acce + 2;            // all MMAs complete
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(fin + 1);
+    uint64_t *go = fin + 1;              // the phase's inputs are in place (kEpiNs)
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(go + 1);
     __shared__ volatile int s_abort;
+    __shared__ int s_done;               // epilogue warps through with a phase, all phases together
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
@@ -564,6 +683,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
 
     if (threadIdx.x == 0) {
         s_abort = 0;
+        s_done = 0;
         for (int s = 0; s < kStages; ++s) {
             mbar_init(full + s, 1);
             mbar_init(empty + s, 1);
@@ -573,9 +693,10 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             mbar_init(acce + i, CG * kGEpiWarps);
         }
         mbar_init(fin, 1);
+        mbar_init(go, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.a)) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.b)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&L.maps[0].a)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&L.maps[0].b)) : "memory");
     }
     if (warp == 1) {
         if constexpr (CG == 1) {
@@ -597,15 +718,29 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     const uint32_t tmem = *tmem_slot;
     pdl_enter();
 
-    // The sums of PROMOTE take the registers that the first warpgroup does not need:
-    // 128 x 40 + 256 x 232 = 384 x 168, the launch's own total.
+    // The epilogue (32 columns with two operands, or the sums of PROMOTE) takes the registers that the first warpgroup
+    // does not need: 128 x 56 + 256 x 224 = 384 x 168, the launch's own total.
     if (warp == 0) {
-        if constexpr (PROMOTE) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         int s = 0, issued = 0;
         uint32_t ph = 1;
         bool seen = true;   // the ring starts empty
+        for (int phase = 0; phase < L.phases && !s_abort; ++phase) {
+        const GArgs &a = L.args[NS ? ns_set(phase, L.phases) : 0];
+        const GMaps &maps = L.maps[NS ? ns_set(phase, L.phases) : 0];
+        if constexpr (NS) {
+            if (elect_one()) {   // while the others finish
+                asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.a)) : "memory");
+                asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.b)) : "memory");
+            }
+            if (phase > 0 && !grid_wait(L.arrived, (uint32_t)phase * gridDim.x, &s_abort)) break;
+            if (lane == 0)
+                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(go)) : "memory");
+            // the loads below go through the async proxy and follow what the barrier ordered
+            if (phase > 0) asm volatile("fence.proxy.async;" ::: "memory");
+        }
         for (int u = unit0; u < a.units && !s_abort; u += ustep) {
-            const GUnit w = unit_of<SYM>(a, u);
+            const GUnit w = unit_of<R>(a, u);
             const int m0 = (w.tm * CG + (int)rank) * 128, n0 = w.tn * BN + (int)rank * kBRows;
             for (int kb = w.kb0; kb < w.kb1; ++kb) {
                 if (!gwait_seen(seen, empty + s, ph, &s_abort)) break;
@@ -635,6 +770,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                 if (++s == kStages) s = 0, ph ^= 1;
             }
         }
+        }
         // an aborted CTA's loads in flight must land before it may exit (rank 0's barriers count the pair's bytes)
         if (s_abort && rank == 0 && lane == 0)
             for (int i = 0; i < issued; ++i) {
@@ -642,21 +778,23 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                 mbar_wait(full + s, ph ^ 1);
             }
     } else if (warp == 1) {
-        if constexpr (PROMOTE) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (rank == 0) {
             // The whole warp walks the stages and one lane issues: descriptors and addresses stay uniform, which
             // keeps the issue of a stage's four MMAs short (a lone lane took about 290 cycles for them, more than a
             // 128-column tile's MMAs themselves).
+            int s = 0, j = 0;
+            uint32_t ph = 0;
+            bool seen = false;
+            for (int phase = 0; phase < L.phases && !s_abort; ++phase) {
+            const GArgs &a = L.args[NS ? ns_set(phase, L.phases) : 0];
             const uint32_t idesc = (1u << 4) | ((a.f16 ? 0u : 1u) << 7) | ((a.f16 ? 0u : 1u) << 10) |
                                    ((uint32_t)a.a_mn << 15) | ((uint32_t)a.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
                                    ((uint32_t)((128 * CG) >> 4) << 24);
             const uint32_t a_step = (a.a_mn ? 2048 : 32) >> 4, b_step = (a.b_mn ? 2048 : 32) >> 4;
             const uint64_t a0 = gdesc(smem_u32(smem), a.a_mn), b0 = gdesc(smem_u32(smem) + kABytes, a.b_mn);
-            int s = 0, j = 0;
-            uint32_t ph = 0;
-            bool seen = false;
             for (int u = unit0; u < a.units && !s_abort; u += ustep) {
-                const GUnit w = unit_of<SYM>(a, u);
+                const GUnit w = unit_of<R>(a, u);
                 int kb = w.kb0;
                 do {   // one accumulation: the whole unit, or kPromoteKb stages of it
                     const int stop = PROMOTE ? min(w.kb1, kb + kPromoteKb) : w.kb1;
@@ -686,15 +824,16 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                 } while (kb < w.kb1 && !s_abort);
                 __syncwarp();
             }
+            }
             __syncwarp();
             if (elect_one()) commit_own<CG>(fin);
             mbar_wait(fin, 0);   // nothing of ours still runs on the tensor cores
             __syncwarp();
         }
     } else if (warp < 4) {
-        if constexpr (PROMOTE) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     } else {
-        if constexpr (PROMOTE) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int q = warp & 3, half = (warp - 4) >> 2;
         uint8_t *stage0 = epi + (warp - 4) * kGStageOut;
         uint32_t acce_bar[2] = {smem_u32(acce), smem_u32(acce + 1)};
@@ -702,11 +841,25 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             acce_bar[0] = mapa_u32(acce_bar[0], 0);
             acce_bar[1] = mapa_u32(acce_bar[1], 0);
         }
-        int j = 0, slot = 0;
+        int j = 0;
+        uint32_t u0[16] = {}, u1[16] = {};
+        float di = 0.f, dj = 0.f;
+        for (int phase = 0; phase < L.phases; ++phase) {
+        int slot = 0;   // a phase ends with its staging free; the next one may use it in other portions
+        const GArgs &a = L.args[NS ? ns_set(phase, L.phases) : 0];
+        const GMaps &maps = L.maps[NS ? ns_set(phase, L.phases) : 0];
+        if constexpr (NS)
+            if (!gwait_warp(go, phase & 1, &s_abort)) break;
         for (int u = unit0; u < a.units; u += ustep) {
-            const GUnit w = unit_of<SYM>(a, u);
+            const GUnit w = unit_of<R>(a, u);
             const int row = (w.tm * CG + (int)rank) * 128 + q * 32 + lane, n0 = w.tn * BN;
             const bool empty_sum = w.kb1 <= w.kb0;
+            if (NS) di = diag_ahead(a, w.b, row, imin(a.m, a.s_pad));
+            if (a.splits == 1) {
+                fetch_ahead(u0, a.c0, w.b, row, n0 + half * 32, a.m, a.n);
+                fetch_ahead(u1, a.c1, w.b, row, n0 + half * 32, a.m, a.n);
+                if (NS) dj = diag_ahead(a, w.b, n0 + half * 32 + lane, imin(a.n, a.s_pad));
+            }
             bool ok = true;
             uint32_t d = 0;
             float sums[PROMOTE ? kChunks / 2 : 1][32];
@@ -752,7 +905,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     kb = w.kb1;
                 }
             } while (kb < w.kb1);
-            if (!ok) break;
+            if (!ok) break;   // the abort flag is set
 
             bool last = true;
             const int64_t slab = 128 * BN;
@@ -809,18 +962,41 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     }
                     const int col = n0 + ci * 32;
                     if (col >= a.n) continue;
+                    if (pass == 1) {
+                        fetch_ahead(u0, a.c0, w.b, row, col, a.m, a.n);
+                        fetch_ahead(u1, a.c1, w.b, row, col, a.m, a.n);
+                        if (NS) dj = diag_ahead(a, w.b, col + lane, imin(a.n, a.s_pad));
+                    }
                     if (lane == 0) {
                         if (a.slots == 2) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                         else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     }
                     __syncwarp();
-                    epilogue32<EPI>(v, a, maps, stage0 + slot * (kGStageOut / 2), w.b, row, col);
+                    epilogue32<EPI>(v, u0, u1, di, dj, a, maps, stage0 + slot * (kGStageOut / 2), w.b, row, col);
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     slot = a.slots == 2 ? slot ^ 1 : 0;
-                    if constexpr (SYM)
-                        if (w.tm != w.tn) mirror32(v, a.out0, w.b, row, col, a.m, a.n);
+                    if (pass == 0 && i + 1 < kChunks / 2) {   // the next group's operands, while this one leaves
+                        fetch_ahead(u0, a.c0, w.b, row, col + 64, a.m, a.n);
+                        fetch_ahead(u1, a.c1, w.b, row, col + 64, a.m, a.n);
+                        if (NS) dj = diag_ahead(a, w.b, col + 64 + lane, imin(a.n, a.s_pad));
+                    }
+                    if constexpr (NS)
+                        if (a.sym && w.tn >= R * (w.tm + 1)) mirror32(v, a.out0, w.b, row, col, a.m, a.n);
                 }
             }
+        }
+        if (NS && phase + 1 < L.phases) {
+            // This warp's outputs are in place: its TMA stores are complete, its lanes' own stores are ordered before the
+            // count by the block-scope fences. The CTA's last warp says so to the grid, with one release for all.
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            __threadfence_block();
+            __syncwarp();
+            if (lane == 0 && !s_abort && atomicAdd(&s_done, 1) % kGEpiWarps == kGEpiWarps - 1) {
+                __threadfence_block();
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(L.arrived) : "memory");
+            }
+            __syncwarp();
+        }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
@@ -829,8 +1005,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     __syncthreads();
     if constexpr (CG == 2) cluster_sync_all();
     if (threadIdx.x == 0 && s_abort) {
-        dev_flag(a.hdr, CSRT_DEV_TIMEOUT);
-        a.hdr->timeout_site = 6;
+        dev_flag(L.args[0].hdr, CSRT_DEV_TIMEOUT);
+        L.args[0].hdr->timeout_site = 6;
     }
     if (warp == 1) {
         __syncwarp();

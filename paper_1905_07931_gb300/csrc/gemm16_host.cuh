@@ -45,6 +45,11 @@ inline bool make_map3(CUtensorMap *map, const void *base, int dtype, int64_t row
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles of a product; `sym`: those that reach above the diagonal, `ratio` tile columns to a tile row.
+inline int64_t tile_count(bool sym, int64_t tm, int64_t tn, int64_t ratio) {
+    return sym ? tm * tn - ratio * (tm * (tm - 1) / 2) : tm * tn;
+}
+
 inline bool operand_map(CUtensorMap *map, const GOperand &o, bool mn, int box_rows, int dtype, int batch) {
     return make_map3(map, o.p, dtype, o.rows, o.cols, o.ld, batch, o.stride, 64, mn ? kGBK : box_rows,
                      CU_TENSOR_MAP_SWIZZLE_128B);
@@ -55,17 +60,16 @@ inline bool out_map(CUtensorMap *map, const GMat &o, int m, int n, int batch) {
                      o.dtype == CSRT_DT_F32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
-template <int CG, int BN, int EPI, bool PROMOTE>
-int launch_tile(const GProduct &p, GArgs a, cudaStream_t s) {
+// Dimensions and maps of one product on CG x 128 x BN tiles.
+template <int CG, int BN>
+int fill_set(const GProduct &p, GArgs &a, GMaps &maps) {
     const int dtype = a.f16 ? CSRT_DT_F16 : CSRT_DT_BF16;
-    GMaps maps = {};
     a.a_mn = p.a_mn;
     a.b_mn = p.b_mn;
     a.kb = (int32_t)ceil_div<int64_t>(p.reduction, kGBK);
     a.tiles_m = (int32_t)ceil_div<int64_t>(a.m, 128 * CG);
     a.tiles_n = (int32_t)ceil_div<int64_t>(a.n, BN);
-    const bool sym = EPI == kEpiGram || EPI == kEpiPoly;
-    const int64_t tiles = (int64_t)a.batch * (sym ? (int64_t)a.tiles_m * (a.tiles_m + 1) / 2 : (int64_t)a.tiles_m * a.tiles_n);
+    const int64_t tiles = a.batch * tile_count(a.sym, a.tiles_m, a.tiles_n, 128 * CG / BN);
     if (a.splits < 1) a.splits = 1;
     a.kb_split = ceil_div<int32_t>(imax(a.kb, 1), a.splits);
     a.splits = ceil_div<int32_t>(imax(a.kb, 1), a.kb_split);
@@ -82,19 +86,19 @@ int launch_tile(const GProduct &p, GArgs a, cudaStream_t s) {
     // one aligned 16-bit output and no operand to turn: a group needs half the staging
     const bool turns = !a.out0.vec || (a.c0.p != nullptr && !a.c0.vec) || (a.c1.p != nullptr && !a.c1.vec);
     a.slots = a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !turns ? 2 : 1;
-    auto kernel = gemm16_kernel<CG, BN, EPI, PROMOTE>;
-    constexpr int smem = gsmem_bytes<CG, BN>();
-    static bool attr_set[64] = {false};
+    return CSRT_OK;
+}
+
+template <auto kernel>
+int allow_smem(int smem) {
+    static bool done[64] = {false};
     int dev = 0;
     CSRT_CHECK_CUDA(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+    if (dev < 0 || dev >= 64 || !done[dev]) {
         CSRT_CHECK_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        if (dev >= 0 && dev < 64) attr_set[dev] = true;
+        if (dev >= 0 && dev < 64) done[dev] = true;
     }
-    const int grid = imin(a.units, imax(1, num_sms() / CG)) * CG;
-    launch_pdl(kernel, dim3(grid), dim3(kGThreads), smem, s, maps, a);
-    count_launch();
-    return check_launch("gemm16_kernel");
+    return CSRT_OK;
 }
 
 // Time of a product in microseconds by a simple model of gemm16_kernel: waves of units, each loading its stages and
@@ -104,44 +108,71 @@ struct GTile {
     int cg, bn;
     double stage, epi;   // us per stage, us per unit's epilogue
 };
+constexpr GTile kTiles[3] = {{2, 256, 0.31, 3.6}, {1, 128, 0.21, 2.0}, {1, 64, 0.19, 1.3}};
 inline double model_us(const GTile &t, int64_t tiles, int64_t kb, int64_t splits) {
     const int64_t slots = imax(1, num_sms() / t.cg);
     const int64_t units = tiles * splits, waves = ceil_div(units, slots);
     const double unit = (double)ceil_div(imax<int64_t>(kb, 1), splits) * t.stage;
-    double us = 2.0 + waves * (unit > t.epi ? unit : t.epi) + t.epi;
-    if (splits > 1) us += 1.0 + 0.5 * splits;
+    double us = 3.0 + waves * (unit > t.epi ? unit : t.epi) + t.epi;
+    if (splits > 1) us += 2.0 + 0.5 * splits;
     return us;
+}
+
+// Best number of slices of a product on tiles t, and its time.
+inline int best_splits(const GTile &t, const GArgs &a, int64_t reduction, double *us) {
+    const int64_t kb = ceil_div<int64_t>(reduction, kGBK);
+    const int64_t tiles = a.batch * tile_count(a.sym, ceil_div<int64_t>(a.m, 128 * t.cg), ceil_div<int64_t>(a.n, t.bn),
+                                               128 * t.cg / t.bn);
+    int best = 1;
+    *us = 1e30;
+    for (int64_t sp = 1; sp <= 32 && sp * 2 <= imax<int64_t>(kb, 2); ++sp) {
+        if (sp > 1 && ((size_t)(tiles * sp) * t.cg * 128 * t.bn * sizeof(float) > kPartialBytes ||
+                       tiles * t.cg * kGEpiWarps > (int64_t)kWsCounterInts))
+            break;
+        const double v = model_us(t, tiles, kb, sp);
+        if (v < *us) {
+            *us = v;
+            best = (int)sp;
+        }
+    }
+    return best;
+}
+
+template <int CG, int BN, int EPI, bool PROMOTE>
+int launch_tile(const GProduct &p, const GArgs &a, cudaStream_t s) {
+    GLaunch<EPI> l = {};
+    l.args[0] = a;
+    l.phases = 1;
+    int rc = fill_set<CG, BN>(p, l.args[0], l.maps[0]);
+    if (rc != CSRT_OK) return rc;
+    constexpr auto kernel = gemm16_kernel<CG, BN, EPI, PROMOTE>;
+    constexpr int smem = gsmem_bytes<CG, BN>();
+    rc = allow_smem<kernel>(smem);
+    if (rc != CSRT_OK) return rc;
+    const int grid = imin(l.args[0].units, imax(1, num_sms() / CG)) * CG;
+    launch_pdl(kernel, dim3(grid), dim3(kGThreads), smem, s, l);
+    count_launch();
+    return check_launch("gemm16_kernel");
 }
 
 template <int EPI, bool PROMOTE>
 int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the dense products need a GPU with tcgen05");
-    const bool sym = EPI == kEpiGram || EPI == kEpiPoly;
-    const GTile cand[3] = {{2, 256, 0.36, 4.0}, {1, 128, 0.26, 2.5}, {1, 64, 0.22, 1.6}};
-    const int64_t kb = ceil_div<int64_t>(p.reduction, kGBK);
     int best = 0, best_s = 1;
     double best_us = 1e30;
-    for (int c = 0; c < (sym ? 2 : 3); ++c) {
-        const GTile &t = cand[c];
-        const int64_t tm = ceil_div<int64_t>(a.m, 128 * t.cg), tn = ceil_div<int64_t>(a.n, t.bn);
-        const int64_t tiles = a.batch * (sym ? tm * (tm + 1) / 2 : tm * tn);
-        for (int64_t sp = 1; sp <= 32 && sp * 4 <= imax<int64_t>(kb, 4); ++sp) {
-            if (sp > 1 && ((size_t)(tiles * sp) * t.cg * 128 * t.bn * sizeof(float) > kPartialBytes ||
-                           tiles * t.cg * kGEpiWarps > (int64_t)kWsCounterInts || a.partial == nullptr))
-                break;
-            const double us = model_us(t, tiles, kb, sp);
-            if (us < best_us) {
-                best_us = us;
-                best = c;
-                best_s = (int)sp;
-            }
+    for (int c = 0; c < 3; ++c) {
+        double us;
+        const int sp = best_splits(kTiles[c], a, p.reduction, &us);
+        if (us < best_us) {
+            best_us = us;
+            best = c;
+            best_s = sp;
         }
     }
     a.splits = best_s;
     if (best == 0) return launch_tile<2, 256, EPI, PROMOTE>(p, a, s);
-    if constexpr (EPI == kEpiDense)
-        if (best == 2) return launch_tile<1, 64, EPI, PROMOTE>(p, a, s);
-    return launch_tile<1, 128, EPI, PROMOTE>(p, a, s);
+    if (best == 1) return launch_tile<1, 128, EPI, PROMOTE>(p, a, s);
+    return launch_tile<1, 64, EPI, PROMOTE>(p, a, s);
 }
 
 }  // namespace csrt

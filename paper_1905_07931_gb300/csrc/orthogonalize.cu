@@ -2,7 +2,9 @@
 //
 //   X <- a X + (b A + c A A) X,   A = X X^T  (X^T X and products on the right where X has more rows than columns)
 //
-// as three launches of gemm16_kernel per step: A with its mirrored half, B = b A + c A A likewise, and a X + B X.
+// as three products per step on gemm16_kernel: A with its mirrored half, B = b A + c A A likewise, and a X + B X. For
+// small matrices one launch runs all of them, a cooperative grid of one CTA per SM with a grid-wide barrier between
+// products; for large ones each is a launch on the tiles that suit it.
 //
 // Number formats. Singular values stay in [0, 1.203] (p(s) = a s + b s^3 + c s^5 maps [0, 1.203] into itself), so
 // every entry of X, A and B is bounded (1.203, 1.45, 2.81) and fits float16 once scaled by a power of two: X and A
@@ -19,8 +21,6 @@
 
 namespace csrt {
 
-constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
-constexpr float kXScale = 32768.f;
 constexpr int kPrepThreads = 256;
 constexpr int kPrepBlocks = 1024;   // most blocks (norm partials) per matrix
 
@@ -34,6 +34,7 @@ struct PrepArgs {
     GMat o;                 // with no steps: the normalised direction itself
     int64_t ldx;
     int32_t direct;
+    uint32_t *arrived;      // the products' grid barrier, cleared here
 };
 
 // Eight consecutive elements of row r from column c: gradient, old momentum -> u (and the new momentum stored).
@@ -129,6 +130,7 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_momentum_kernel(PrepArgs a
 __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
     pdl_enter();
     const int b = blockIdx.y;
+    if (threadIdx.x == 0 && blockIdx.x == 0 && b == 0) *a.arrived = 0;
     double n2 = 0.0;
     for (int i = threadIdx.x; i < (int)gridDim.x; i += kPrepThreads) n2 += a.partial[(int64_t)b * gridDim.x + i];
     n2 = block_sum(n2);
@@ -164,7 +166,7 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
 
 struct OrthoLayout {
     int64_t ldx, lds;
-    size_t partial, x0, x1, lo, a, b, total;   // offsets after the reserved part
+    size_t slices, arrived, partial, x0, x1, lo, a, b, diag_a, diag_b, total;   // offsets after the reserved part
 };
 
 static OrthoLayout layout(int64_t batch, int64_t rows, int64_t cols) {
@@ -179,14 +181,187 @@ static OrthoLayout layout(int64_t batch, int64_t rows, int64_t cols) {
         at += (size_t)up(bytes, 256);
         return r;
     };
+    l.slices = take((int64_t)kPartialBytes);
+    l.arrived = take(256);
     l.partial = take(batch * kPrepBlocks * (int64_t)sizeof(double));
     l.x0 = take(batch * rows * l.ldx * 2);
     l.x1 = take(batch * rows * l.ldx * 2);
     l.lo = take(batch * rows * l.ldx * 2);
     l.a = take(batch * s * l.lds * 2);
     l.b = take(batch * s * l.lds * 2);
+    l.diag_a = take(batch * l.lds * 4);
+    l.diag_b = take(batch * l.lds * 4);
     l.total = at;
     return l;
+}
+
+struct NsPlan {
+    int32_t batch, rows, cols, steps;
+    float scale;
+    char *base;
+    OrthoLayout l;
+    GMat o;
+    void *ws;
+};
+
+// Product `set` of the six that make up the steps (ns_set).
+static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
+    const OrthoLayout &l = q.l;
+    const bool tall = q.rows > q.cols;
+    const int32_t sh = tall ? q.cols : q.rows;
+    auto mat = [&](size_t off, int64_t ld, int64_t n_rows) {
+        GMat m = {};
+        m.p = q.base + off;
+        m.ld = ld;
+        m.stride = ld * n_rows;
+        m.dtype = CSRT_DT_F16;
+        m.vec = 1;
+        return m;
+    };
+    auto op = [&](size_t off, int64_t r, int64_t c, int64_t ld) {
+        GOperand o;
+        o.p = q.base + off;
+        o.rows = r;
+        o.cols = c;
+        o.ld = ld;
+        o.stride = r * ld;
+        return o;
+    };
+    a = GArgs{};
+    a.batch = q.batch;
+    a.f16 = 1;
+    a.hdr = static_cast<WsHeader *>(q.ws);
+    a.counters = ws_counters(q.ws);
+    a.partial = reinterpret_cast<float *>(q.base + l.slices);
+    a.s_pad = (int32_t)l.lds;
+    a.tall = tall;
+    float *diag_a = reinterpret_cast<float *>(q.base + l.diag_a), *diag_b = reinterpret_cast<float *>(q.base + l.diag_b);
+    const size_t x = set == 1 || set == 4 || (set == 5 && (q.steps - 1) % 2) ? l.x1 : l.x0;
+    const GOperand ox = op(x, q.rows, q.cols, l.ldx), oa = op(l.a, sh, sh, l.lds), ob = op(l.b, sh, sh, l.lds);
+    if (set <= 1) {          // A = X X^T or X^T X, times 2^15
+        p.a = p.b = ox;
+        p.a_mn = p.b_mn = tall;
+        p.reduction = tall ? q.rows : q.cols;
+        a.kind = kNsGram;
+        a.sym = 1;
+        a.m = a.n = sh;
+        a.alpha = kInvXScale;
+        a.diag_out = diag_a;
+        a.out0 = mat(l.a, l.lds, sh);
+    } else if (set == 2) {   // B = b A + c A A, times 2^14
+        p.a = p.b = oa;
+        p.a_mn = p.b_mn = false;
+        p.reduction = sh;
+        a.kind = kNsPoly;
+        a.sym = 1;
+        a.m = a.n = sh;
+        a.alpha = kNsC * 0.5f * kInvXScale;
+        a.diag_in = diag_a;
+        a.diag_out = diag_b;
+        a.c0 = mat(l.a, l.lds, sh);
+        a.out0 = mat(l.b, l.lds, sh);
+    } else {                 // X' = a X + B X, times 2^15; the last one is o
+        p.a = tall ? ox : ob;
+        p.b = tall ? ob : ox;
+        p.a_mn = false;
+        p.b_mn = !tall;
+        p.reduction = sh;
+        a.kind = kNsApply;
+        a.m = q.rows;
+        a.n = q.cols;
+        a.alpha = 2.f * kInvXScale;
+        a.gamma = set == 5 ? q.scale * kInvXScale : 1.f;
+        a.diag_in = diag_b;
+        a.c0 = mat(x, l.ldx, q.rows);
+        a.c1 = mat(l.lo, l.ldx, q.rows);
+        a.out0 = set == 5 ? q.o : mat(set == 3 ? l.x1 : l.x0, l.ldx, q.rows);
+        if (set != 5) a.out1 = mat(l.lo, l.ldx, q.rows);
+    }
+}
+
+// All steps in one cooperative launch on CG x 128 x BN tiles.
+template <int CG, int BN>
+static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
+    GLaunch<kEpiNs> n = {};
+    int32_t units = 1;
+    for (int set = 0; set < kNsSets; ++set) {
+        GProduct p;
+        GArgs &a = n.args[set];
+        ns_product(q, set, p, a);
+        double us;
+        a.splits = best_splits(tile, a, p.reduction, &us);
+        const int rc = fill_set<CG, BN>(p, a, n.maps[set]);
+        if (rc != CSRT_OK) return rc;
+        units = imax(units, a.units);
+    }
+    n.phases = 3 * q.steps;
+    n.arrived = reinterpret_cast<uint32_t *>(q.base + q.l.arrived);
+
+    constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false>;
+    constexpr int smem = gsmem_bytes<CG, BN>();
+    const int rc = allow_smem<kernel>(smem);
+    if (rc != CSRT_OK) return rc;
+    // CTAs that the GPU can hold at once: all of them have to be there for the barrier
+    static int resident[64] = {0};
+    int dev = 0;
+    CSRT_CHECK_CUDA(cudaGetDevice(&dev));
+    int slots = dev >= 0 && dev < 64 ? resident[dev] : 0;
+    if (slots == 0) {
+        CSRT_CHECK_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&slots, kernel, kGThreads, smem));
+        slots *= num_sms();
+        if (slots < 1) return fail(CSRT_ERR_CUDA, "the orthogonalisation does not fit the GPU");
+        if (dev >= 0 && dev < 64) resident[dev] = slots;
+    }
+    static_assert(CG == 1, "residency is counted in single CTAs");
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)imin(units, imin(slots, num_sms())));
+    cfg.blockDim = dim3(kGThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CSRT_CHECK_CUDA(cudaLaunchKernelEx(&cfg, kernel, n));
+    count_launch();
+    return check_launch("gemm16_kernel (Newton-Schulz)");
+}
+
+// Between products: a grid barrier of the one launch against a launch of its own (us, measured).
+constexpr double kBarrierUs = 1.5, kLaunchUs = 3.0;
+
+static int ns_products(const NsPlan &q, cudaStream_t s) {
+    if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the orthogonalisation needs a GPU with tcgen05");
+    // One launch runs all products on one kind of tile; launches of their own let each have its best. Take what the
+    // model finds faster: small matrices one launch, large ones a launch per product.
+    double one[3] = {0.0, kBarrierUs * 3, kBarrierUs * 3}, each = 0.0;
+    for (int set = 0; set < 4; ++set) {
+        if (set == 1) continue;   // as set 0
+        GProduct p;
+        GArgs a;
+        ns_product(q, set, p, a);
+        double best = 1e30;
+        for (int c = 0; c < 3; ++c) {
+            double us;
+            best_splits(kTiles[c], a, p.reduction, &us);
+            one[c] += us;
+            if (us < best) best = us;
+        }
+        each += best + kLaunchUs;
+    }
+    if (one[1] <= each && one[1] <= one[2]) return launch_ns<1, 128>(q, kTiles[1], s);
+    if (one[2] <= each) return launch_ns<1, 64>(q, kTiles[2], s);
+    for (int phase = 0; phase < 3 * q.steps; ++phase) {
+        const int step = phase / 3, k = phase % 3;
+        const int set = k == 0 ? step & 1 : k == 1 ? 2 : phase == 3 * q.steps - 1 ? 5 : 3 + (step & 1);
+        GProduct p;
+        GArgs a;
+        ns_product(q, set, p, a);
+        const int rc = launch_gemm16<kEpiNs, false>(p, a, s);
+        if (rc != CSRT_OK) return rc;
+    }
+    return CSRT_OK;
 }
 
 static int check_batch(const csrt_mat *m, const char *name, int32_t batch, int64_t stride) {
@@ -270,6 +445,7 @@ int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float
     p.hi = reinterpret_cast<__half *>(base + l.x0);
     p.lo = reinterpret_cast<__half *>(base + l.lo);
     p.ldx = l.ldx;
+    p.arrived = reinterpret_cast<uint32_t *>(base + l.arrived);
     p.direct = steps == 0;
     p.o.p = o->data;
     p.o.ld = o->ld;
@@ -286,84 +462,17 @@ int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float
     rc = check_launch("ortho_scale_kernel");
     if (rc != CSRT_OK || steps == 0) return rc;
 
-    const bool tall = rows > cols;
-    const int32_t sh = tall ? cols : rows;
-    auto mat = [&](size_t off, int64_t ld, int64_t n_rows) {
-        GMat m = {};
-        m.p = base + off;
-        m.ld = ld;
-        m.stride = ld * n_rows;
-        m.dtype = CSRT_DT_F16;
-        m.vec = 1;
-        return m;
-    };
-    auto op = [&](size_t off, int64_t r, int64_t c, int64_t ld) {
-        GOperand q;
-        q.p = base + off;
-        q.rows = r;
-        q.cols = c;
-        q.ld = ld;
-        q.stride = r * ld;
-        return q;
-    };
-    GArgs common = {};
-    common.batch = batch;
-    common.f16 = 1;
-    common.hdr = static_cast<WsHeader *>(ws);
-    common.counters = ws_counters(ws);
-    size_t xc = l.x0, xn = l.x1;
-    for (int step = 0; step < steps; ++step) {
-        const bool last = step == steps - 1;
-        GProduct q;
-        GArgs a = common;   // A = X X^T or X^T X, times 2^15
-        q.a = q.b = op(xc, rows, cols, l.ldx);
-        q.a_mn = q.b_mn = tall;
-        q.reduction = tall ? rows : cols;
-        a.m = a.n = sh;
-        a.alpha = 1.f / kXScale;
-        a.out0 = mat(l.a, l.lds, sh);
-        rc = launch_gemm16<kEpiGram, false>(q, a, s);
-        if (rc != CSRT_OK) return rc;
-
-        a = common;         // B = b A + c A A, times 2^14
-        q.a = q.b = op(l.a, sh, sh, l.lds);
-        q.a_mn = q.b_mn = false;
-        q.reduction = sh;
-        a.m = a.n = sh;
-        a.alpha = kNsC * 0.5f / kXScale;
-        a.beta = kNsB * 0.5f;
-        a.c0 = mat(l.a, l.lds, sh);
-        a.out0 = mat(l.b, l.lds, sh);
-        rc = launch_gemm16<kEpiPoly, false>(q, a, s);
-        if (rc != CSRT_OK) return rc;
-
-        a = common;         // X' = a X + B X, times 2^15; the last one is o
-        const GOperand ob = op(l.b, sh, sh, l.lds), ox = op(xc, rows, cols, l.ldx);
-        q.a = tall ? ox : ob;
-        q.b = tall ? ob : ox;
-        q.a_mn = false;
-        q.b_mn = !tall;
-        q.reduction = sh;
-        a.m = rows;
-        a.n = cols;
-        a.alpha = 2.f / kXScale;
-        a.beta = kNsA;
-        a.gamma = last ? scale / kXScale : 1.f;
-        a.c0 = mat(xc, l.ldx, rows);
-        a.c1 = mat(l.lo, l.ldx, rows);
-        if (last) {
-            a.out0 = p.o;
-        } else {
-            a.out0 = mat(xn, l.ldx, rows);
-            a.out1 = mat(l.lo, l.ldx, rows);
-        }
-        rc = launch_gemm16<kEpiApply, false>(q, a, s);
-        if (rc != CSRT_OK) return rc;
-        const size_t t = xc;
-        xc = xn;
-        xn = t;
-    }
-    return CSRT_OK;
+    NsPlan plan;
+    plan.batch = batch;
+    plan.rows = rows;
+    plan.cols = cols;
+    plan.steps = steps;
+    plan.scale = scale;
+    plan.base = base;
+    plan.l = l;
+    plan.o = p.o;
+    plan.ws = ws;
+    return ns_products(plan, s);
 }
 
 }  // extern "C"
