@@ -54,6 +54,7 @@ struct GMat {
     int64_t ld, stride;
     int32_t dtype;     // CSRT_DT_*
     int32_t vec;       // rows 16-byte aligned: vector access; outputs: TMA store
+    int32_t pad;       // rows may be read up to ld, whatever the matrix's columns
 };
 
 struct GArgs {
@@ -351,36 +352,26 @@ __device__ __forceinline__ float act_deriv(float z, int act) {
     return 1.f;
 }
 
-// 32 consecutive elements of a row of an epilogue operand, as float32 (0 beyond the matrix). `row` is this lane's
-// row, `col` the warp's first column. Rows that are not 16-byte aligned are read a row at a time, a lane per column,
-// and turned in the warp's staging area `turn` (32 x 33 floats do not fit it, so 16 rows at a time).
+// 32 consecutive elements of a row of an epilogue operand that is not fetched ahead, as float32 (0 beyond the
+// matrix). `row` is this lane's row, `col` the warp's first column. Aligned float32 rows are read in place. Rows that
+// are not 16-byte aligned are read a row at a time, a lane per column, and turned in the warp's staging area `turn`
+// (32 x 33 floats do not fit it, so 16 rows at a time).
 __device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int b, int row, int col, int m, int n,
                                        float *turn) {
     const int lane = threadIdx.x & 31;
     if (c.vec) {
-        const int64_t off = b * c.stride + (int64_t)row * c.ld + col;
-        if (row < m && col + 32 <= n) {
-            if (c.dtype == CSRT_DT_F32) {
-                const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(c.p) + off);
+        const float *p = static_cast<const float *>(c.p) + b * c.stride + (int64_t)row * c.ld + col;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float4 f = p[i];
-                    v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
-                }
-            } else {
-                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(c.p) + off);
-                const bool h = c.dtype == CSRT_DT_F16;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint4 u = p[i];
-                    const float2 a = unpack16(u.x, h), d = unpack16(u.y, h), e = unpack16(u.z, h), f = unpack16(u.w, h);
-                    v[8 * i] = a.x, v[8 * i + 1] = a.y, v[8 * i + 2] = d.x, v[8 * i + 3] = d.y;
-                    v[8 * i + 4] = e.x, v[8 * i + 5] = e.y, v[8 * i + 6] = f.x, v[8 * i + 7] = f.y;
-                }
+        for (int i = 0; i < 8; ++i) {
+            float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (row < m && col + 4 * i + 4 <= n) {
+                f = *reinterpret_cast<const float4 *>(p + 4 * i);
+            } else if (row < m) {
+                if (col + 4 * i < n) f.x = p[4 * i];
+                if (col + 4 * i + 1 < n) f.y = p[4 * i + 1];
+                if (col + 4 * i + 2 < n) f.z = p[4 * i + 2];
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = row < m && col + i < n ? load1(c.p, off + i, c.dtype) : 0.f;
+            v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
         }
     } else {
         const int row0 = row - lane;
@@ -488,51 +479,72 @@ __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
     return r;
 }
 
-// An epilogue operand's 32 elements, 16-bit and aligned, fetched ahead of their use (through L2: another SM may have
-// written them earlier in this launch).
-__device__ __forceinline__ bool ahead_ok(const GMat &c, int col, int n) {
-    return c.p != nullptr && c.vec && c.dtype != CSRT_DT_F32 && col + 32 <= n;
+// The warp's 32 x 32 elements of an aligned 16-bit epilogue operand, fetched ahead of their use: a load instruction
+// takes eight whole rows of 64 bytes, four lanes to a row. Through L2 only: another SM may have written them earlier
+// in this launch.
+__device__ __forceinline__ bool ahead_ok(const GMat &c) {
+    return c.p != nullptr && c.vec && c.dtype != CSRT_DT_F32;
 }
-__device__ __forceinline__ void fetch_ahead(uint32_t (&u)[16], const GMat &c, int b, int row, int col, int m, int n) {
-    if (ahead_ok(c, col, n) && row < m) {
-        const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(c.p) + b * c.stride +
-                                                         (int64_t)row * c.ld + col);
+__device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GMat &c, int b, int row0, int col, int m, int n) {
+    if (!ahead_ok(c)) return;
+    const int lane = threadIdx.x & 31, r = lane >> 2, c8 = col + 8 * (lane & 3);
+    const uint16_t *p = static_cast<const uint16_t *>(c.p) + b * c.stride + (int64_t)(row0 + r) * c.ld + c8;
+    if (c.pad ? c8 < c.ld : c8 + 8 <= n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (row0 + r + 8 * i < m) u[i] = __ldcg(reinterpret_cast<const uint4 *>(p + (int64_t)(8 * i) * c.ld));
+    } else if (c8 < n) {   // the last columns of rows that end inside the eight
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint4 q = __ldcg(p + i);
-            u[4 * i] = q.x, u[4 * i + 1] = q.y, u[4 * i + 2] = q.z, u[4 * i + 3] = q.w;
+            uint32_t w[4] = {0, 0, 0, 0};
+            if (row0 + r + 8 * i < m) {
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (c8 + e < n) w[e >> 1] |= (uint32_t)p[(int64_t)(8 * i) * c.ld + e] << (16 * (e & 1));
+            }
+            u[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
+    }
+}
+// This lane's row of it, turned in `slot` (2 KB; left free).
+__device__ __forceinline__ void take32(float (&v)[32], const uint4 (&u)[4], const GMat &c, int b, int row, int col,
+                                       int m, int n, uint8_t *slot) {
+    const int lane = threadIdx.x & 31;
+    if (ahead_ok(c)) {
+        const bool h = c.dtype == CSRT_DT_F16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 8 * i + (lane >> 2);
+            *reinterpret_cast<uint4 *>(slot + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4)) = u[i];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(slot + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4));
+            const float2 f0 = unpack16(q.x, h), f1 = unpack16(q.y, h), f2 = unpack16(q.z, h), f3 = unpack16(q.w, h);
+            v[8 * i] = f0.x, v[8 * i + 1] = f0.y, v[8 * i + 2] = f1.x, v[8 * i + 3] = f1.y;
+            v[8 * i + 4] = f2.x, v[8 * i + 5] = f2.y, v[8 * i + 6] = f3.x, v[8 * i + 7] = f3.y;
+        }
+        __syncwarp();
+    } else {
+        load32(v, c, b, row, col, m, n, reinterpret_cast<float *>(slot));
     }
 }
 // The diagonal at this lane's row (once per unit) and at column col + lane.
 __device__ __forceinline__ float diag_ahead(const GArgs &a, int b, int at, int limit) {
     return a.diag_in != nullptr && at < limit ? __ldcg(a.diag_in + (int64_t)b * a.s_pad + at) : 0.f;
 }
-__device__ __forceinline__ void take32(float (&v)[32], const uint32_t (&u)[16], const GMat &c, int b, int row, int col,
-                                       int m, int n, float *turn) {
-    if (ahead_ok(c, col, n)) {
-        const bool h = c.dtype == CSRT_DT_F16;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float2 f = unpack16(u[i], h);
-            v[2 * i] = f.x, v[2 * i + 1] = f.y;
-        }
-    } else {
-        load32(v, c, b, row, col, m, n, turn);
-    }
-}
 
 // The epilogue of 32 columns of a row in float32. `slot` is free staging; unaligned operands turn in it before any
 // output is staged, and unaligned outputs turn in it one after the other. u0, u1: c0 and c1 fetched ahead;
 // di, dj: the diagonal (GArgs::diag_in) at this lane's row and at column col + lane.
 template <int EPI>
-__device__ __forceinline__ void epilogue32(float (&v)[32], const uint32_t (&u0)[16], const uint32_t (&u1)[16],
+__device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4], const uint4 (&u1)[4],
                                            float di, float dj, const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col) {
-    float *turn = reinterpret_cast<float *>(slot);
     const int lane = threadIdx.x & 31;
     if constexpr (EPI == kEpiFwd) {
         float r[32];
-        if (a.c1.p != nullptr) take32(r, u1, a.c1, b, row, col, a.m, a.n, turn);
+        if (a.c1.p != nullptr) take32(r, u1, a.c1, b, row, col, a.m, a.n, slot);
         if (a.bias != nullptr) {
             const float bi = row < a.m ? __ldg(a.bias + row) : 0.f;
 #pragma unroll
@@ -558,7 +570,7 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint32_t (&u0)[
     } else if constexpr (EPI == kEpiBwd) {
         if (a.c0.p != nullptr) {
             float z[32];
-            take32(z, u0, a.c0, b, row, col, a.m, a.n, turn);
+            take32(z, u0, a.c0, b, row, col, a.m, a.n, slot);
             if (a.act == CSRT_ACT_RELU) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_RELU);
@@ -572,7 +584,7 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint32_t (&u0)[
         }
         if (a.c1.p != nullptr) {
             float r[32];
-            take32(r, u1, a.c1, b, row, col, a.m, a.n, turn);
+            take32(r, u1, a.c1, b, row, col, a.m, a.n, slot);
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += r[i];
         }
@@ -594,7 +606,7 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint32_t (&u0)[
         } else {
             // off the diagonal b R + c ((d_i + d_j) R + (R R)_ij), on it b d_i + c (d_i^2 + (R R)_ii)
             float r[32];
-            take32(r, u0, a.c0, b, row, col, a.m, a.n, turn);
+            take32(r, u0, a.c0, b, row, col, a.m, a.n, slot);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 v[i] = a.alpha * v[i] + 0.5f * (kNsB + kNsC * (di + __shfl_sync(0xffffffffu, dj, i))) * r[i];
@@ -610,8 +622,8 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint32_t (&u0)[
     } else {
         // (a + e) X + B X with the diagonal e of B by row (or by column where X has more rows than columns)
         float c[32], t[32];
-        take32(c, u0, a.c0, b, row, col, a.m, a.n, turn);
-        take32(t, u1, a.c1, b, row, col, a.m, a.n, turn);
+        take32(c, u0, a.c0, b, row, col, a.m, a.n, slot);
+        take32(t, u1, a.c1, b, row, col, a.m, a.n, slot);
         if (a.tall) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -842,7 +854,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             acce_bar[1] = mapa_u32(acce_bar[1], 0);
         }
         int j = 0;
-        uint32_t u0[16] = {}, u1[16] = {};
+        uint4 u0[4] = {}, u1[4] = {};
         float di = 0.f, dj = 0.f;
         for (int phase = 0; phase < L.phases; ++phase) {
         int slot = 0;   // a phase ends with its staging free; the next one may use it in other portions
@@ -856,8 +868,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             const bool empty_sum = w.kb1 <= w.kb0;
             if (NS) di = diag_ahead(a, w.b, row, imin(a.m, a.s_pad));
             if (a.splits == 1) {
-                fetch_ahead(u0, a.c0, w.b, row, n0 + half * 32, a.m, a.n);
-                fetch_ahead(u1, a.c1, w.b, row, n0 + half * 32, a.m, a.n);
+                fetch_ahead(u0, a.c0, w.b, row - lane, n0 + half * 32, a.m, a.n);
+                fetch_ahead(u1, a.c1, w.b, row - lane, n0 + half * 32, a.m, a.n);
                 if (NS) dj = diag_ahead(a, w.b, n0 + half * 32 + lane, imin(a.n, a.s_pad));
             }
             bool ok = true;
@@ -910,7 +922,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             bool last = true;
             const int64_t slab = 128 * BN;
             float *part = nullptr;
-            if (a.splits > 1) part = a.partial + ((int64_t)w.tile * a.splits * CG + rank) * slab + q * 32 + lane;
+            if (a.splits > 1) part = a.partial + ((int64_t)w.tile * a.splits * CG + rank) * slab + (q * 32 + lane) * 4;
 #pragma unroll 1
             for (int pass = 0; pass < 2; ++pass) {
                 // pass 0: this unit's sums (to the epilogue, or to its slab); pass 1: the slices joined
@@ -948,23 +960,38 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         if (a.splits > 1) {
                             float *p = part + (int64_t)w.split * CG * slab + (int64_t)ci * 32 * 128;
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) p[e * 128] = v[e];
+                            for (int e = 0; e < 8; ++e)
+                                *reinterpret_cast<float4 *>(p + e * 512) =
+                                    make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
                             continue;
                         }
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0.f;
-                        for (int sl = 0; sl < a.splits; ++sl) {
+                        for (int sl = 0; sl < a.splits; sl += 2) {   // two slices' loads in flight
                             const float *p = part + (int64_t)sl * CG * slab + (int64_t)ci * 32 * 128;
+                            const bool two = sl + 1 < a.splits;
+                            float4 f[8], g[8];
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] += __ldcg(p + e * 128);
+                            for (int e = 0; e < 8; ++e) {
+                                f[e] = __ldcg(reinterpret_cast<const float4 *>(p + e * 512));
+                                g[e] = two ? __ldcg(reinterpret_cast<const float4 *>(p + CG * slab + e * 512))
+                                           : make_float4(0.f, 0.f, 0.f, 0.f);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                v[4 * e] = (v[4 * e] + f[e].x) + g[e].x;
+                                v[4 * e + 1] = (v[4 * e + 1] + f[e].y) + g[e].y;
+                                v[4 * e + 2] = (v[4 * e + 2] + f[e].z) + g[e].z;
+                                v[4 * e + 3] = (v[4 * e + 3] + f[e].w) + g[e].w;
+                            }
                         }
                     }
                     const int col = n0 + ci * 32;
                     if (col >= a.n) continue;
                     if (pass == 1) {
-                        fetch_ahead(u0, a.c0, w.b, row, col, a.m, a.n);
-                        fetch_ahead(u1, a.c1, w.b, row, col, a.m, a.n);
+                        fetch_ahead(u0, a.c0, w.b, row - lane, col, a.m, a.n);
+                        fetch_ahead(u1, a.c1, w.b, row - lane, col, a.m, a.n);
                         if (NS) dj = diag_ahead(a, w.b, col + lane, imin(a.n, a.s_pad));
                     }
                     if (lane == 0) {
@@ -976,8 +1003,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     slot = a.slots == 2 ? slot ^ 1 : 0;
                     if (pass == 0 && i + 1 < kChunks / 2) {   // the next group's operands, while this one leaves
-                        fetch_ahead(u0, a.c0, w.b, row, col + 64, a.m, a.n);
-                        fetch_ahead(u1, a.c1, w.b, row, col + 64, a.m, a.n);
+                        fetch_ahead(u0, a.c0, w.b, row - lane, col + 64, a.m, a.n);
+                        fetch_ahead(u1, a.c1, w.b, row - lane, col + 64, a.m, a.n);
                         if (NS) dj = diag_ahead(a, w.b, col + 64 + lane, imin(a.n, a.s_pad));
                     }
                     if constexpr (NS)

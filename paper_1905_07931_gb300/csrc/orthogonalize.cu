@@ -215,7 +215,7 @@ static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
         m.ld = ld;
         m.stride = ld * n_rows;
         m.dtype = CSRT_DT_F16;
-        m.vec = 1;
+        m.vec = m.pad = 1;
         return m;
     };
     auto op = [&](size_t off, int64_t r, int64_t c, int64_t ld) {
