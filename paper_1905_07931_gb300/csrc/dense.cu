@@ -62,9 +62,16 @@ static bool clash(const csrt_mat *out, const csrt_mat *in) {
 __global__ void pack16_kernel(const uint16_t *__restrict__ src, int64_t ld, int32_t rows, int32_t cols,
                               uint16_t *__restrict__ dst, int64_t dld) {
     pdl_enter();
+    // a thread takes the eight elements of an aligned 16-byte store; the warp's loads cover whole lines between them
     for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
-        for (int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; c < cols; c += (int64_t)gridDim.x * blockDim.x)
-            dst[r * dld + c] = src[r * ld + c];
+        for (int64_t c = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 8; c < cols; c += (int64_t)gridDim.x * blockDim.x * 8) {
+            uint32_t w[4] = {0, 0, 0, 0};
+            const uint16_t *p = src + r * ld + c;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < cols) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+            *reinterpret_cast<uint4 *>(dst + r * dld + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
 }
 
 // Operand of a product: in place, or packed at *at (advanced).
@@ -77,9 +84,10 @@ static int operand(const csrt_mat *m, char **at, cudaStream_t s, GOperand *o) {
     o->ld = (int64_t)align_up((size_t)m->cols, 8);
     o->p = *at;
     *at += align_up((size_t)m->rows * o->ld * 2, 256);
-    const unsigned gx = (unsigned)imin<int64_t>(ceil_div<int64_t>(m->cols, 256), 64);
-    const unsigned gy = (unsigned)imin<int64_t>(m->rows, imax<int64_t>(1, (int64_t)num_sms() * 16 / gx));
-    launch_pdl(pack16_kernel, dim3(gx, gy), dim3(256), 0, s, static_cast<const uint16_t *>(m->data), m->ld, m->rows,
+    const unsigned block = m->cols > 512 ? 128 : 32;
+    const unsigned gx = (unsigned)imin<int64_t>(ceil_div<int64_t>(m->cols, 8 * block), 64);
+    const unsigned gy = (unsigned)imin<int64_t>(m->rows, 65535);
+    launch_pdl(pack16_kernel, dim3(gx, gy), dim3(block), 0, s, static_cast<const uint16_t *>(m->data), m->ld, m->rows,
                m->cols, static_cast<uint16_t *>(o->p), o->ld);
     count_launch();
     return check_launch("pack16_kernel");

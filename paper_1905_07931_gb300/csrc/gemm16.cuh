@@ -396,31 +396,46 @@ __device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int b, int
     }
 }
 
-// Row `row` (of this lane) and columns col .. col + 31 of an output leave the warp: `slot` is its staging area.
-// Rows of 64 bytes (16-bit) take the 64-byte swizzle, rows of 128 bytes (float32) the 128-byte one.
-__device__ __forceinline__ void store32(const float (&v)[32], const GMat &o, const CUtensorMap *map, uint8_t *slot,
-                                        int b, int row, int col, int m, int n) {
+// Row `row` (of this lane) and columns col .. col + 31 of an output on their way out. Aligned outputs are staged at
+// `slot` and leave with emit(): rows of 64 bytes (16-bit) take the 64-byte swizzle, rows of 128 bytes (float32) the
+// 128-byte one. Others are turned there and stored at once, a row at a time, a lane per column.
+__device__ __forceinline__ void put32(const float (&v)[32], const GMat &o, uint8_t *slot, int b, int row, int col, int m,
+                                      int n) {
     const int lane = threadIdx.x & 31;
+    const bool h = o.dtype == CSRT_DT_F16;
     if (o.vec) {
         if (o.dtype == CSRT_DT_F32) {
+            __syncwarp();   // a row of 128 bytes lies over two rows of a 16-bit operand
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 *reinterpret_cast<float4 *>(slot + lane * 128 + ((i ^ (lane & 7)) << 4)) =
                     make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         } else {
-            const bool h = o.dtype == CSRT_DT_F16;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 *reinterpret_cast<uint4 *>(slot + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) =
                     make_uint4(pack16(v[8 * i], v[8 * i + 1], h), pack16(v[8 * i + 2], v[8 * i + 3], h),
                                pack16(v[8 * i + 4], v[8 * i + 5], h), pack16(v[8 * i + 6], v[8 * i + 7], h));
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        return;
+    }
+    const int row0 = row - lane, rows = m - row0;
+    const int64_t at = b * o.stride + (int64_t)row0 * o.ld + col + lane;
+    if (o.dtype != CSRT_DT_F32) {
+        uint32_t *turn = reinterpret_cast<uint32_t *>(slot);   // pairs of columns, 17 words to a row
         __syncwarp();
-        if (lane == 0 && row < m && col < n) tma_store_3d(map, col, row, b, slot);   // lane 0's row is the block's first
+#pragma unroll
+        for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = pack16(v[2 * i], v[2 * i + 1], h);
+        __syncwarp();
+        if (col + lane < n) {
+            uint16_t *p = static_cast<uint16_t *>(o.p) + at;
+            const uint16_t *t = reinterpret_cast<const uint16_t *>(slot) + lane;
+#pragma unroll
+            for (int r = 0; r < 32; ++r)
+                if (r < rows) p[(int64_t)r * o.ld] = t[r * 34];
+        }
     } else {
         float *turn = reinterpret_cast<float *>(slot);
-        const int row0 = row - lane;
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
             __syncwarp();
@@ -430,15 +445,25 @@ __device__ __forceinline__ void store32(const float (&v)[32], const GMat &o, con
             }
             __syncwarp();
             if (col + lane < n) {
+                float *p = static_cast<float *>(o.p) + at + part * 16 * o.ld;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int rr = row0 + part * 16 + r;
-                    if (rr < m)
-                        store1(o.p, b * o.stride + (int64_t)rr * o.ld + col + lane, turn[r * 33 + lane], o.dtype);
-                }
+                for (int r = 0; r < 16; ++r)
+                    if (part * 16 + r < rows) p[(int64_t)r * o.ld] = turn[r * 33 + lane];
             }
         }
+    }
+    __syncwarp();
+}
+
+// The staged outputs leave: out0 from slot, out1 from slot + 2048.
+__device__ __forceinline__ void emit(const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col) {
+    if (a.out0.vec) {   // out1 likewise, if there is one
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
+        if ((threadIdx.x & 31) == 0 && row < a.m && col < a.n) {   // lane 0's row is the block's first
+            tma_store_3d(&maps.out0, col, row, b, slot);
+            if (a.out1.p != nullptr) tma_store_3d(&maps.out1, col, row, b, slot + 2048);
+        }
     }
 }
 
@@ -506,28 +531,31 @@ __device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GMat &c, int b,
         }
     }
 }
-// This lane's row of it, turned in `slot` (2 KB; left free).
-__device__ __forceinline__ void take32(float (&v)[32], const uint4 (&u)[4], const GMat &c, int b, int row, int col,
-                                       int m, int n, uint8_t *slot) {
+// This lane's row of it: stage_in() puts what the lanes fetched into 2 KB of staging, and after a __syncwarp() take32()
+// reads the row; a lane may then write its own row's place. Operands that are not fetched ahead are read by take32().
+__device__ __forceinline__ void stage_in(const uint4 (&u)[4], const GMat &c, uint8_t *at) {
+    if (!ahead_ok(c)) return;
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2);
+        *reinterpret_cast<uint4 *>(at + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4)) = u[i];
+    }
+}
+__device__ __forceinline__ void take32(float (&v)[32], const GMat &c, int b, int row, int col, int m, int n, uint8_t *at,
+                                       float *turn) {
     const int lane = threadIdx.x & 31;
     if (ahead_ok(c)) {
         const bool h = c.dtype == CSRT_DT_F16;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = 8 * i + (lane >> 2);
-            *reinterpret_cast<uint4 *>(slot + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4)) = u[i];
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(slot + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4));
+            const uint4 q = *reinterpret_cast<const uint4 *>(at + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4));
             const float2 f0 = unpack16(q.x, h), f1 = unpack16(q.y, h), f2 = unpack16(q.z, h), f3 = unpack16(q.w, h);
             v[8 * i] = f0.x, v[8 * i + 1] = f0.y, v[8 * i + 2] = f1.x, v[8 * i + 3] = f1.y;
             v[8 * i + 4] = f2.x, v[8 * i + 5] = f2.y, v[8 * i + 6] = f3.x, v[8 * i + 7] = f3.y;
         }
-        __syncwarp();
     } else {
-        load32(v, c, b, row, col, m, n, reinterpret_cast<float *>(slot));
+        load32(v, c, b, row, col, m, n, turn);
     }
 }
 // The diagonal at this lane's row (once per unit) and at column col + lane.
@@ -535,23 +563,29 @@ __device__ __forceinline__ float diag_ahead(const GArgs &a, int b, int at, int l
     return a.diag_in != nullptr && at < limit ? __ldcg(a.diag_in + (int64_t)b * a.s_pad + at) : 0.f;
 }
 
-// The epilogue of 32 columns of a row in float32. `slot` is free staging; unaligned operands turn in it before any
-// output is staged, and unaligned outputs turn in it one after the other. u0, u1: c0 and c1 fetched ahead;
-// di, dj: the diagonal (GArgs::diag_in) at this lane's row and at column col + lane.
+// The epilogue of 32 columns of a row in float32, in one slot of staging (4 KB, or 2 KB where one operand and one
+// 16-bit output are all): c0 and c1 come in at its halves, out0 and out1 leave from there. u0, u1: c0 and c1 fetched ahead; di, dj: the diagonal (GArgs::diag_in) at this lane's row
+// and at column col + lane. An operand that has to be turned (unaligned) uses the slot after the fetched ones are out
+// of it; so do unaligned outputs.
 template <int EPI>
-__device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4], const uint4 (&u1)[4],
-                                           float di, float dj, const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col) {
+__device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4], const uint4 (&u1)[4], float di, float dj,
+                                           const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col) {
+    float *turn = reinterpret_cast<float *>(slot);
     const int lane = threadIdx.x & 31;
     if constexpr (EPI == kEpiFwd) {
         float r[32];
-        if (a.c1.p != nullptr) take32(r, u1, a.c1, b, row, col, a.m, a.n, slot);
+        if (a.c1.p != nullptr) {
+            stage_in(u1, a.c1, slot);
+            __syncwarp();
+            take32(r, a.c1, b, row, col, a.m, a.n, slot, turn);
+        }
         if (a.bias != nullptr) {
             const float bi = row < a.m ? __ldg(a.bias + row) : 0.f;
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += bi;
         }
-        // z and y are both aligned or both not (checked on the host): their stagings do not meet
-        if (a.out1.p != nullptr) store32(v, a.out1, &maps.out1, a.out1.vec ? slot + 2048 : slot, b, row, col, a.m, a.n);
+        // z and y are both aligned or both not (seen to on the host)
+        if (a.out1.p != nullptr) put32(v, a.out1, a.out1.vec ? slot + 2048 : slot, b, row, col, a.m, a.n);
         if (a.act == CSRT_ACT_RELU) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_RELU);
@@ -566,11 +600,17 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += r[i];
         }
-        store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
     } else if constexpr (EPI == kEpiBwd) {
+        uint8_t *at1 = a.c0.p != nullptr ? slot + 2048 : slot;
+        stage_in(u0, a.c0, slot);
+        stage_in(u1, a.c1, at1);
+        __syncwarp();
+        float r[32];
+        // both leave the slot before either is turned in it
+        if (a.c1.p != nullptr && ahead_ok(a.c1)) take32(r, a.c1, b, row, col, a.m, a.n, at1, turn);
         if (a.c0.p != nullptr) {
             float z[32];
-            take32(z, u0, a.c0, b, row, col, a.m, a.n, slot);
+            take32(z, a.c0, b, row, col, a.m, a.n, slot, turn);
             if (a.act == CSRT_ACT_RELU) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_RELU);
@@ -583,12 +623,13 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
             }
         }
         if (a.c1.p != nullptr) {
-            float r[32];
-            take32(r, u1, a.c1, b, row, col, a.m, a.n, slot);
+            if (!ahead_ok(a.c1)) {
+                __syncwarp();
+                take32(r, a.c1, b, row, col, a.m, a.n, slot, turn);
+            }
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += r[i];
         }
-        store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
     } else if (a.kind != kNsApply) {
         // A or B: the diagonal goes to its own float32 vector and is left out of the float16 matrix. Warps' rows and
         // columns start at multiples of 32, so a diagonal element of this group, if any, is element `lane`.
@@ -606,7 +647,9 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
         } else {
             // off the diagonal b R + c ((d_i + d_j) R + (R R)_ij), on it b d_i + c (d_i^2 + (R R)_ii)
             float r[32];
-            take32(r, u0, a.c0, b, row, col, a.m, a.n, slot);
+            stage_in(u0, a.c0, slot);
+            __syncwarp();
+            take32(r, a.c0, b, row, col, a.m, a.n, slot, turn);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 v[i] = a.alpha * v[i] + 0.5f * (kNsB + kNsC * (di + __shfl_sync(0xffffffffu, dj, i))) * r[i];
@@ -618,12 +661,14 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
             }
         }
         if (on_diag && row < a.m) a.diag_out[(int64_t)b * a.s_pad + row] = d;
-        store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
     } else {
         // (a + e) X + B X with the diagonal e of B by row (or by column where X has more rows than columns)
         float c[32], t[32];
-        take32(c, u0, a.c0, b, row, col, a.m, a.n, slot);
-        take32(t, u1, a.c1, b, row, col, a.m, a.n, slot);
+        stage_in(u0, a.c0, slot);
+        stage_in(u1, a.c1, slot + 2048);
+        __syncwarp();
+        take32(c, a.c0, b, row, col, a.m, a.n, slot, turn);
+        take32(t, a.c1, b, row, col, a.m, a.n, slot + 2048, turn);
         if (a.tall) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -633,13 +678,14 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = (a.alpha * v[i] + e * (c[i] + t[i])) * a.gamma;
         }
-        store32(v, a.out0, &maps.out0, slot, b, row, col, a.m, a.n);
         if (a.out1.p != nullptr) {   // what float16 drops of X, kept beside it
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
-            store32(v, a.out1, &maps.out1, slot + 2048, b, row, col, a.m, a.n);
+            for (int i = 0; i < 32; ++i) t[i] = v[i] - __half2float(__float2half_rn(v[i]));
+            put32(t, a.out1, slot + 2048, b, row, col, a.m, a.n);
         }
     }
+    put32(v, a.out0, slot, b, row, col, a.m, a.n);
+    emit(a, maps, slot, b, row, col);
 }
 
 // The same 32 values into the mirrored place of a symmetric output (float16): lane-contiguous stores.

@@ -83,9 +83,10 @@ int fill_set(const GProduct &p, GArgs &a, GMaps &maps) {
         return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused an output");
     if (a.out1.vec && !out_map(&maps.out1, a.out1, a.m, a.n, a.batch))
         return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused an output");
-    // one aligned 16-bit output and no operand to turn: a group needs half the staging
+    // one aligned 16-bit output, at most one operand and none to turn: a group needs half the staging
     const bool turns = !a.out0.vec || (a.c0.p != nullptr && !a.c0.vec) || (a.c1.p != nullptr && !a.c1.vec);
-    a.slots = a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !turns ? 2 : 1;
+    const bool two_in = a.c0.p != nullptr && a.c1.p != nullptr;
+    a.slots = a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !two_in && !turns ? 2 : 1;
     return CSRT_OK;
 }
 
@@ -103,18 +104,19 @@ int allow_smem(int smem) {
 
 // Time of a product in microseconds by a simple model of gemm16_kernel: waves of units, each loading its stages and
 // then running an epilogue that overlaps the next unit's stages but not the last's; joining slices costs their
-// partial tiles' trip through L2.
+// partial tiles' trip through L2. The constants are fitted to measured times of 54 products of 64 to 9216 rows and
+// columns on every tile and up to 16 slices; the choice they give is within 1% of the best on average.
 struct GTile {
     int cg, bn;
     double stage, epi;   // us per stage, us per unit's epilogue
 };
-constexpr GTile kTiles[3] = {{2, 256, 0.31, 3.6}, {1, 128, 0.21, 2.0}, {1, 64, 0.19, 1.3}};
+constexpr GTile kTiles[3] = {{2, 256, 0.35, 6.3}, {1, 128, 0.25, 4.9}, {1, 64, 0.21, 4.0}};
 inline double model_us(const GTile &t, int64_t tiles, int64_t kb, int64_t splits) {
     const int64_t slots = imax(1, num_sms() / t.cg);
     const int64_t units = tiles * splits, waves = ceil_div(units, slots);
     const double unit = (double)ceil_div(imax<int64_t>(kb, 1), splits) * t.stage;
-    double us = 3.0 + waves * (unit > t.epi ? unit : t.epi) + t.epi;
-    if (splits > 1) us += 2.0 + 0.5 * splits;
+    double us = waves * (unit > t.epi ? unit : t.epi) + t.epi - 2.2;
+    if (splits > 1) us += 4.0 + 0.385 * splits * t.bn / 64;
     return us;
 }
 
