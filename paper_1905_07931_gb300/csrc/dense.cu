@@ -6,6 +6,12 @@
 #include "gemm16_host.cuh"
 
 namespace csrt {
+// The kernels' instances are compiled in dense_gemm_fwd.cu and dense_gemm_bwd.cu.
+int dense_gemm_fwd(const GProduct &p, const GArgs &a, bool wide, cudaStream_t s);
+int dense_gemm_bwd(const GProduct &p, const GArgs &a, bool wide, cudaStream_t s);
+}  // namespace csrt
+
+namespace csrt {
 
 constexpr int64_t kMaxElems = (int64_t)1 << 40;   // largest matrix extent taken (rows x ld)
 
@@ -125,7 +131,8 @@ static int dense_product(const csrt_mat *am, bool a_mn, const csrt_mat *bm, bool
     a.counters = ws_counters(ws);
     a.partial = reinterpret_cast<float *>(ws_scratch(ws));
     p.reduction = a_mn ? am->rows : am->cols;
-    return out0->dtype == CSRT_DT_F32 ? launch_gemm16<EPI, true>(p, a, s) : launch_gemm16<EPI, false>(p, a, s);
+    const bool wide = out0->dtype == CSRT_DT_F32;
+    return EPI == kEpiFwd ? dense_gemm_fwd(p, a, wide, s) : dense_gemm_bwd(p, a, wide, s);
 }
 
 // ---------------------------------------------------------------------------

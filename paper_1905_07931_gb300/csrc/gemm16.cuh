@@ -26,6 +26,9 @@
 // Splits: each slice's warp leaves its float32 partial tile in the workspace and counts in; the last one adds the
 // slices in slice order (one order whatever the timing, so results repeat bit for bit) and runs the epilogue.
 //
+// GEN = false is the kernel for aligned matrices (16-bit outputs, float32 ones with PROMOTE): a third of the code, which
+// matters to short products, whose one pass through the epilogue mostly waits for instructions.
+//
 // Every wait is bounded: one that runs out sets the CTA's abort flag, the roles drain and meet, and the kernel ends
 // with CSRT_DEV_TIMEOUT in the status word.
 #pragma once
@@ -300,6 +303,16 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool f16) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+__device__ __forceinline__ void pack_all(uint32_t (&w)[16], const float (&v)[32], bool f16) {
+    if (f16) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = pack16(v[2 * i], v[2 * i + 1], true);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = pack16(v[2 * i], v[2 * i + 1], false);
+    }
+}
+
 __device__ __forceinline__ float2 unpack16(uint32_t u, bool f16) {
     if (f16) return __half22float2(*reinterpret_cast<const __half2 *>(&u));
     return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
@@ -356,10 +369,11 @@ __device__ __forceinline__ float act_deriv(float z, int act) {
 // matrix). `row` is this lane's row, `col` the warp's first column. Aligned float32 rows are read in place. Rows that
 // are not 16-byte aligned are read a row at a time, a lane per column, and turned in the warp's staging area `turn`
 // (32 x 33 floats do not fit it, so 16 rows at a time).
+template <bool GEN>
 __device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int b, int row, int col, int m, int n,
                                        float *turn) {
     const int lane = threadIdx.x & 31;
-    if (c.vec) {
+    if (!GEN || c.vec) {
         const float *p = static_cast<const float *>(c.p) + b * c.stride + (int64_t)row * c.ld + col;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -399,23 +413,25 @@ __device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int b, int
 // Row `row` (of this lane) and columns col .. col + 31 of an output on their way out. Aligned outputs are staged at
 // `slot` and leave with emit(): rows of 64 bytes (16-bit) take the 64-byte swizzle, rows of 128 bytes (float32) the
 // 128-byte one. Others are turned there and stored at once, a row at a time, a lane per column.
+template <bool GEN, bool WIDE>
 __device__ __forceinline__ void put32(const float (&v)[32], const GMat &o, uint8_t *slot, int b, int row, int col, int m,
                                       int n) {
     const int lane = threadIdx.x & 31;
     const bool h = o.dtype == CSRT_DT_F16;
-    if (o.vec) {
-        if (o.dtype == CSRT_DT_F32) {
+    if (!GEN || o.vec) {
+        if (GEN ? o.dtype == CSRT_DT_F32 : WIDE) {
             __syncwarp();   // a row of 128 bytes lies over two rows of a 16-bit operand
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 *reinterpret_cast<float4 *>(slot + lane * 128 + ((i ^ (lane & 7)) << 4)) =
                     make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         } else {
+            uint32_t w[16];
+            pack_all(w, v, h);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 *reinterpret_cast<uint4 *>(slot + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) =
-                    make_uint4(pack16(v[8 * i], v[8 * i + 1], h), pack16(v[8 * i + 2], v[8 * i + 3], h),
-                               pack16(v[8 * i + 4], v[8 * i + 5], h), pack16(v[8 * i + 6], v[8 * i + 7], h));
+                    make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
         }
         return;
     }
@@ -423,9 +439,11 @@ __device__ __forceinline__ void put32(const float (&v)[32], const GMat &o, uint8
     const int64_t at = b * o.stride + (int64_t)row0 * o.ld + col + lane;
     if (o.dtype != CSRT_DT_F32) {
         uint32_t *turn = reinterpret_cast<uint32_t *>(slot);   // pairs of columns, 17 words to a row
+        uint32_t w[16];
+        pack_all(w, v, h);
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = pack16(v[2 * i], v[2 * i + 1], h);
+        for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = w[i];
         __syncwarp();
         if (col + lane < n) {
             uint16_t *p = static_cast<uint16_t *>(o.p) + at;
@@ -456,8 +474,9 @@ __device__ __forceinline__ void put32(const float (&v)[32], const GMat &o, uint8
 }
 
 // The staged outputs leave: out0 from slot, out1 from slot + 2048.
+template <bool GEN>
 __device__ __forceinline__ void emit(const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col) {
-    if (a.out0.vec) {   // out1 likewise, if there is one
+    if (!GEN || a.out0.vec) {   // out1 likewise, if there is one
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if ((threadIdx.x & 31) == 0 && row < a.m && col < a.n) {   // lane 0's row is the block's first
@@ -481,10 +500,14 @@ template <int R>
 __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
     GUnit r;
     const int tiles = a.sym ? a.tiles_m * a.tiles_n - R * (a.tiles_m * (a.tiles_m - 1) / 2) : a.tiles_m * a.tiles_n;
-    r.split = u % a.splits;
-    const int t = u / a.splits;
+    int t = u;
+    r.split = 0;
+    if (a.splits > 1) {
+        t = u / a.splits;
+        r.split = u - t * a.splits;
+    }
     r.tile = t;
-    r.b = t / tiles;
+    r.b = a.batch > 1 ? t / tiles : 0;
     int q = t - r.b * tiles;
     if (a.sym) {
         int i = 0;
@@ -493,11 +516,11 @@ __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
         r.tn = R * i + q;
     } else {
         constexpr int kBand = 8;
-        const int band = q / (kBand * a.tiles_n), first = band * kBand;
+        const int band = a.tiles_m > kBand ? q / (kBand * a.tiles_n) : 0, first = band * kBand;
         const int rows = min(kBand, a.tiles_m - first);
         q -= first * a.tiles_n;
-        r.tm = first + q % rows;
-        r.tn = q / rows;
+        r.tn = rows == kBand ? q / kBand : q / rows;
+        r.tm = first + q - r.tn * rows;
     }
     r.kb0 = r.split * a.kb_split;
     r.kb1 = min(a.kb, r.kb0 + a.kb_split);
@@ -507,11 +530,13 @@ __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
 // The warp's 32 x 32 elements of an aligned 16-bit epilogue operand, fetched ahead of their use: a load instruction
 // takes eight whole rows of 64 bytes, four lanes to a row. Through L2 only: another SM may have written them earlier
 // in this launch.
+template <bool GEN, bool WIDE>
 __device__ __forceinline__ bool ahead_ok(const GMat &c) {
-    return c.p != nullptr && c.vec && c.dtype != CSRT_DT_F32;
+    return GEN ? c.p != nullptr && c.vec && c.dtype != CSRT_DT_F32 : !WIDE && c.p != nullptr;
 }
+template <bool GEN, bool WIDE>
 __device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GMat &c, int b, int row0, int col, int m, int n) {
-    if (!ahead_ok(c)) return;
+    if (!ahead_ok<GEN, WIDE>(c)) return;
     const int lane = threadIdx.x & 31, r = lane >> 2, c8 = col + 8 * (lane & 3);
     const uint16_t *p = static_cast<const uint16_t *>(c.p) + b * c.stride + (int64_t)(row0 + r) * c.ld + c8;
     if (c.pad ? c8 < c.ld : c8 + 8 <= n) {
@@ -533,8 +558,9 @@ __device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GMat &c, int b,
 }
 // This lane's row of it: stage_in() puts what the lanes fetched into 2 KB of staging, and after a __syncwarp() take32()
 // reads the row; a lane may then write its own row's place. Operands that are not fetched ahead are read by take32().
+template <bool GEN, bool WIDE>
 __device__ __forceinline__ void stage_in(const uint4 (&u)[4], const GMat &c, uint8_t *at) {
-    if (!ahead_ok(c)) return;
+    if (!ahead_ok<GEN, WIDE>(c)) return;
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -542,20 +568,34 @@ __device__ __forceinline__ void stage_in(const uint4 (&u)[4], const GMat &c, uin
         *reinterpret_cast<uint4 *>(at + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4)) = u[i];
     }
 }
+template <bool GEN, bool WIDE>
 __device__ __forceinline__ void take32(float (&v)[32], const GMat &c, int b, int row, int col, int m, int n, uint8_t *at,
                                        float *turn) {
     const int lane = threadIdx.x & 31;
-    if (ahead_ok(c)) {
-        const bool h = c.dtype == CSRT_DT_F16;
+    if (!GEN && WIDE) {
+        load32<false>(v, c, b, row, col, m, n, turn);
+    } else if (!GEN || ahead_ok<GEN, WIDE>(c)) {
+        uint32_t w[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint4 q = *reinterpret_cast<const uint4 *>(at + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4));
-            const float2 f0 = unpack16(q.x, h), f1 = unpack16(q.y, h), f2 = unpack16(q.z, h), f3 = unpack16(q.w, h);
-            v[8 * i] = f0.x, v[8 * i + 1] = f0.y, v[8 * i + 2] = f1.x, v[8 * i + 3] = f1.y;
-            v[8 * i + 4] = f2.x, v[8 * i + 5] = f2.y, v[8 * i + 6] = f3.x, v[8 * i + 7] = f3.y;
+            w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
+        }
+        if (c.dtype == CSRT_DT_F16) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 f = unpack16(w[i], true);
+                v[2 * i] = f.x, v[2 * i + 1] = f.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 f = unpack16(w[i], false);
+                v[2 * i] = f.x, v[2 * i + 1] = f.y;
+            }
         }
     } else {
-        load32(v, c, b, row, col, m, n, turn);
+        load32<true>(v, c, b, row, col, m, n, turn);
     }
 }
 // The diagonal at this lane's row (once per unit) and at column col + lane.
@@ -567,7 +607,7 @@ __device__ __forceinline__ float diag_ahead(const GArgs &a, int b, int at, int l
 // 16-bit output are all): c0 and c1 come in at its halves, out0 and out1 leave from there. u0, u1: c0 and c1 fetched ahead; di, dj: the diagonal (GArgs::diag_in) at this lane's row
 // and at column col + lane. An operand that has to be turned (unaligned) uses the slot after the fetched ones are out
 // of it; so do unaligned outputs.
-template <int EPI>
+template <int EPI, bool GEN, bool WIDE>
 __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4], const uint4 (&u1)[4], float di, float dj,
                                            const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col) {
     float *turn = reinterpret_cast<float *>(slot);
@@ -575,9 +615,9 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
     if constexpr (EPI == kEpiFwd) {
         float r[32];
         if (a.c1.p != nullptr) {
-            stage_in(u1, a.c1, slot);
+            stage_in<GEN, WIDE>(u1, a.c1, slot);
             __syncwarp();
-            take32(r, a.c1, b, row, col, a.m, a.n, slot, turn);
+            take32<GEN, WIDE>(r, a.c1, b, row, col, a.m, a.n, slot, turn);
         }
         if (a.bias != nullptr) {
             const float bi = row < a.m ? __ldg(a.bias + row) : 0.f;
@@ -585,7 +625,7 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
             for (int i = 0; i < 32; ++i) v[i] += bi;
         }
         // z and y are both aligned or both not (seen to on the host)
-        if (a.out1.p != nullptr) put32(v, a.out1, a.out1.vec ? slot + 2048 : slot, b, row, col, a.m, a.n);
+        if (a.out1.p != nullptr) put32<GEN, false>(v, a.out1, !GEN || a.out1.vec ? slot + 2048 : slot, b, row, col, a.m, a.n);
         if (a.act == CSRT_ACT_RELU) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], CSRT_ACT_RELU);
@@ -602,15 +642,15 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
         }
     } else if constexpr (EPI == kEpiBwd) {
         uint8_t *at1 = a.c0.p != nullptr ? slot + 2048 : slot;
-        stage_in(u0, a.c0, slot);
-        stage_in(u1, a.c1, at1);
+        stage_in<GEN, false>(u0, a.c0, slot);
+        stage_in<GEN, WIDE>(u1, a.c1, at1);
         __syncwarp();
         float r[32];
         // both leave the slot before either is turned in it
-        if (a.c1.p != nullptr && ahead_ok(a.c1)) take32(r, a.c1, b, row, col, a.m, a.n, at1, turn);
+        if (a.c1.p != nullptr && ahead_ok<GEN, WIDE>(a.c1)) take32<GEN, WIDE>(r, a.c1, b, row, col, a.m, a.n, at1, turn);
         if (a.c0.p != nullptr) {
             float z[32];
-            take32(z, a.c0, b, row, col, a.m, a.n, slot, turn);
+            take32<GEN, false>(z, a.c0, b, row, col, a.m, a.n, slot, turn);
             if (a.act == CSRT_ACT_RELU) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] *= act_deriv(z[i], CSRT_ACT_RELU);
@@ -623,9 +663,9 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
             }
         }
         if (a.c1.p != nullptr) {
-            if (!ahead_ok(a.c1)) {
+            if (!ahead_ok<GEN, WIDE>(a.c1)) {
                 __syncwarp();
-                take32(r, a.c1, b, row, col, a.m, a.n, slot, turn);
+                take32<GEN, WIDE>(r, a.c1, b, row, col, a.m, a.n, slot, turn);
             }
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += r[i];
@@ -647,9 +687,9 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
         } else {
             // off the diagonal b R + c ((d_i + d_j) R + (R R)_ij), on it b d_i + c (d_i^2 + (R R)_ii)
             float r[32];
-            stage_in(u0, a.c0, slot);
+            stage_in<GEN, false>(u0, a.c0, slot);
             __syncwarp();
-            take32(r, a.c0, b, row, col, a.m, a.n, slot, turn);
+            take32<GEN, false>(r, a.c0, b, row, col, a.m, a.n, slot, turn);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 v[i] = a.alpha * v[i] + 0.5f * (kNsB + kNsC * (di + __shfl_sync(0xffffffffu, dj, i))) * r[i];
@@ -664,11 +704,11 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
     } else {
         // (a + e) X + B X with the diagonal e of B by row (or by column where X has more rows than columns)
         float c[32], t[32];
-        stage_in(u0, a.c0, slot);
-        stage_in(u1, a.c1, slot + 2048);
+        stage_in<GEN, false>(u0, a.c0, slot);
+        stage_in<GEN, WIDE>(u1, a.c1, slot + 2048);
         __syncwarp();
-        take32(c, a.c0, b, row, col, a.m, a.n, slot, turn);
-        take32(t, a.c1, b, row, col, a.m, a.n, slot + 2048, turn);
+        take32<GEN, false>(c, a.c0, b, row, col, a.m, a.n, slot, turn);
+        take32<GEN, WIDE>(t, a.c1, b, row, col, a.m, a.n, slot + 2048, turn);
         if (a.tall) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -681,11 +721,11 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
         if (a.out1.p != nullptr) {   // what float16 drops of X, kept beside it
 #pragma unroll
             for (int i = 0; i < 32; ++i) t[i] = v[i] - __half2float(__float2half_rn(v[i]));
-            put32(t, a.out1, slot + 2048, b, row, col, a.m, a.n);
+            put32<GEN, false>(t, a.out1, slot + 2048, b, row, col, a.m, a.n);
         }
     }
-    put32(v, a.out0, slot, b, row, col, a.m, a.n);
-    emit(a, maps, slot, b, row, col);
+    put32<GEN, WIDE>(v, a.out0, slot, b, row, col, a.m, a.n);
+    emit<GEN>(a, maps, slot, b, row, col);
 }
 
 // The same 32 values into the mirrored place of a symmetric output (float16): lane-contiguous stores.
@@ -710,7 +750,7 @@ constexpr int gsmem_bytes() {
     return gstages<CG, BN>() * gstage_bytes<CG, BN>() + kGEpiWarps * kGStageOut + 1024 + 512;
 }
 
-template <int CG, int BN, int EPI, bool PROMOTE>
+template <int CG, int BN, int EPI, bool PROMOTE, bool GEN>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     gemm16_kernel(const __grid_constant__ GLaunch<EPI> L) {
     static_assert(BN % 64 == 0 && BN / CG >= 64 && 2 * BN <= 512, "two accumulators in tensor memory");
@@ -914,8 +954,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             const bool empty_sum = w.kb1 <= w.kb0;
             if (NS) di = diag_ahead(a, w.b, row, imin(a.m, a.s_pad));
             if (a.splits == 1) {
-                fetch_ahead(u0, a.c0, w.b, row - lane, n0 + half * 32, a.m, a.n);
-                fetch_ahead(u1, a.c1, w.b, row - lane, n0 + half * 32, a.m, a.n);
+                fetch_ahead<GEN, false>(u0, a.c0, w.b, row - lane, n0 + half * 32, a.m, a.n);
+                fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, n0 + half * 32, a.m, a.n);
                 if (NS) dj = diag_ahead(a, w.b, n0 + half * 32 + lane, imin(a.n, a.s_pad));
             }
             bool ok = true;
@@ -1036,8 +1076,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     const int col = n0 + ci * 32;
                     if (col >= a.n) continue;
                     if (pass == 1) {
-                        fetch_ahead(u0, a.c0, w.b, row - lane, col, a.m, a.n);
-                        fetch_ahead(u1, a.c1, w.b, row - lane, col, a.m, a.n);
+                        fetch_ahead<GEN, false>(u0, a.c0, w.b, row - lane, col, a.m, a.n);
+                        fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, col, a.m, a.n);
                         if (NS) dj = diag_ahead(a, w.b, col + lane, imin(a.n, a.s_pad));
                     }
                     if (lane == 0) {
@@ -1045,12 +1085,12 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     }
                     __syncwarp();
-                    epilogue32<EPI>(v, u0, u1, di, dj, a, maps, stage0 + slot * (kGStageOut / 2), w.b, row, col);
+                    epilogue32<EPI, GEN, PROMOTE>(v, u0, u1, di, dj, a, maps, stage0 + slot * (kGStageOut / 2), w.b, row, col);
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     slot = a.slots == 2 ? slot ^ 1 : 0;
                     if (pass == 0 && i + 1 < kChunks / 2) {   // the next group's operands, while this one leaves
-                        fetch_ahead(u0, a.c0, w.b, row - lane, col + 64, a.m, a.n);
-                        fetch_ahead(u1, a.c1, w.b, row - lane, col + 64, a.m, a.n);
+                        fetch_ahead<GEN, false>(u0, a.c0, w.b, row - lane, col + 64, a.m, a.n);
+                        fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, col + 64, a.m, a.n);
                         if (NS) dj = diag_ahead(a, w.b, col + 64 + lane, imin(a.n, a.s_pad));
                     }
                     if constexpr (NS)

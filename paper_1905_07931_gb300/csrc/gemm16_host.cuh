@@ -140,14 +140,20 @@ inline int best_splits(const GTile &t, const GArgs &a, int64_t reduction, double
     return best;
 }
 
-template <int CG, int BN, int EPI, bool PROMOTE>
+// Whether the kernel for aligned matrices serves: every epilogue matrix 16-byte aligned and of the kernel's own types.
+inline bool aligned_set(const GArgs &a, bool wide) {
+    auto fine = [](const GMat &c, bool w) { return c.p == nullptr || (c.vec && (c.dtype == CSRT_DT_F32) == w); };
+    return a.out0.vec && (a.out0.dtype == CSRT_DT_F32) == wide && fine(a.out1, false) && fine(a.c0, false) && fine(a.c1, wide);
+}
+
+template <int CG, int BN, int EPI, bool PROMOTE, bool GEN>
 int launch_tile(const GProduct &p, const GArgs &a, cudaStream_t s) {
     GLaunch<EPI> l = {};
     l.args[0] = a;
     l.phases = 1;
     int rc = fill_set<CG, BN>(p, l.args[0], l.maps[0]);
     if (rc != CSRT_OK) return rc;
-    constexpr auto kernel = gemm16_kernel<CG, BN, EPI, PROMOTE>;
+    constexpr auto kernel = gemm16_kernel<CG, BN, EPI, PROMOTE, GEN>;
     constexpr int smem = gsmem_bytes<CG, BN>();
     rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
@@ -172,9 +178,14 @@ int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
         }
     }
     a.splits = best_s;
-    if (best == 0) return launch_tile<2, 256, EPI, PROMOTE>(p, a, s);
-    if (best == 1) return launch_tile<1, 128, EPI, PROMOTE>(p, a, s);
-    return launch_tile<1, 64, EPI, PROMOTE>(p, a, s);
+    if (aligned_set(a, PROMOTE)) {
+        if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, false>(p, a, s);
+        if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, false>(p, a, s);
+        return launch_tile<1, 64, EPI, PROMOTE, false>(p, a, s);
+    }
+    if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, true>(p, a, s);
+    if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, true>(p, a, s);
+    return launch_tile<1, 64, EPI, PROMOTE, true>(p, a, s);
 }
 
 }  // namespace csrt

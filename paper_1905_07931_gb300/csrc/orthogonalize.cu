@@ -280,7 +280,7 @@ static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
 }
 
 // All steps in one cooperative launch on CG x 128 x BN tiles.
-template <int CG, int BN>
+template <int CG, int BN, bool GEN>
 static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     GLaunch<kEpiNs> n = {};
     int32_t units = 1;
@@ -297,7 +297,7 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     n.phases = 3 * q.steps;
     n.arrived = reinterpret_cast<uint32_t *>(q.base + q.l.arrived);
 
-    constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false>;
+    constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false, GEN>;
     constexpr int smem = gsmem_bytes<CG, BN>();
     const int rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
@@ -350,8 +350,10 @@ static int ns_products(const NsPlan &q, cudaStream_t s) {
         }
         each += best + kLaunchUs;
     }
-    if (one[1] <= each && one[1] <= one[2]) return launch_ns<1, 128>(q, kTiles[1], s);
-    if (one[2] <= each) return launch_ns<1, 64>(q, kTiles[2], s);
+    const bool gen = !q.o.vec || q.o.dtype == CSRT_DT_F32;   // only o can need the general kernel
+    if (one[1] <= each && one[1] <= one[2])
+        return gen ? launch_ns<1, 128, true>(q, kTiles[1], s) : launch_ns<1, 128, false>(q, kTiles[1], s);
+    if (one[2] <= each) return gen ? launch_ns<1, 64, true>(q, kTiles[2], s) : launch_ns<1, 64, false>(q, kTiles[2], s);
     for (int phase = 0; phase < 3 * q.steps; ++phase) {
         const int step = phase / 3, k = phase % 3;
         const int set = k == 0 ? step & 1 : k == 1 ? 2 : phase == 3 * q.steps - 1 ? 5 : 3 + (step & 1);
