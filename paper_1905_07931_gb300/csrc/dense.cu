@@ -138,39 +138,15 @@ static int dense_product(const csrt_mat *am, bool a_mn, const csrt_mat *bm, bool
 // ---------------------------------------------------------------------------
 // Row sums (db), act' and update
 // ---------------------------------------------------------------------------
+// A warp per row.
 template <bool F16>
 __global__ void row_sums_kernel(const uint16_t *__restrict__ dy, int64_t ld, int32_t rows, int32_t cols, bool vec,
                                 bool accumulate, float *__restrict__ db) {
     pdl_enter();
-    __shared__ float s_part[8];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const uint16_t *p = dy + r * ld;
-        float sum = 0.f;
-        if (vec) {
-            for (int64_t c = threadIdx.x * 8; c < cols; c += blockDim.x * 8) {
-                if (c + 8 <= cols) {
-                    const uint4 u = *reinterpret_cast<const uint4 *>(p + c);
-                    const float2 x = unpack16(u.x, F16), y = unpack16(u.y, F16), z = unpack16(u.z, F16),
-                                 w = unpack16(u.w, F16);
-                    sum += ((x.x + x.y) + (y.x + y.y)) + ((z.x + z.y) + (w.x + w.y));
-                } else {
-                    for (int64_t i = c; i < cols; ++i) sum += load1(p, i, F16 ? CSRT_DT_F16 : CSRT_DT_BF16);
-                }
-            }
-        } else {
-            for (int64_t c = threadIdx.x; c < cols; c += blockDim.x) sum += load1(p, c, F16 ? CSRT_DT_F16 : CSRT_DT_BF16);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) s_part[warp] = sum;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            float t = 0.f;
-            for (int w = 0; w < (int)(blockDim.x >> 5); ++w) t += s_part[w];
-            db[r] = accumulate ? db[r] + t : t;
-        }
-        __syncthreads();
+    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    for (int64_t r = (int64_t)blockIdx.x * warps + (threadIdx.x >> 5); r < rows; r += (int64_t)gridDim.x * warps) {
+        const float t = warp_row_sum<F16>(dy + r * ld, cols, vec);
+        if (lane == 0) db[r] = accumulate ? db[r] + t : t;
     }
 }
 
@@ -330,20 +306,44 @@ int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, 
     CSRT_TRY(check_out(dw, "dw", dy->dtype));
     CSRT_ARG(!clash(dw, dy) && !clash(dw, x), "dw overlaps an operand");
     cudaStream_t s = as_stream(stream);
-    if (db != nullptr && m > 0) {
-        const bool vec = tma_rows_ok(dy->data, dy->ld, 2);
-        const dim3 grid((unsigned)imin<int64_t>(m, (int64_t)num_sms() * 16)), block(n > 1024 ? 256 : 64);
-        const uint16_t *p = static_cast<const uint16_t *>(dy->data);
-        if (dy->dtype == CSRT_DT_F16)
-            launch_pdl(row_sums_kernel<true>, grid, block, 0, s, p, dy->ld, m, n, vec, accumulate != 0, db);
-        else
-            launch_pdl(row_sums_kernel<false>, grid, block, 0, s, p, dy->ld, m, n, vec, accumulate != 0, db);
-        count_launch();
-        CSRT_TRY(check_launch("row_sums_kernel"));
-    }
-    if (m == 0 || k == 0) return CSRT_OK;
     GArgs a = {};
     if (accumulate) a.c1 = epi_mat(dw);
+    if (db != nullptr && m > 0) {
+        const bool vec = tma_rows_ok(dy->data, dy->ld, 2);
+        const uint16_t *p = static_cast<const uint16_t *>(dy->data);
+        // The product's idle warps take the row sums along (two warps an SM, about 3 KB/us each, against a kernel of
+        // its own at HBM rate and a launch of 3 us) unless they would outlast it.
+        bool along = false;
+        if (k > 0) {
+            GArgs t = {};
+            t.m = m;
+            t.n = k;
+            t.batch = 1;
+            const GChoice c = choose_tile(t, n);
+            const int64_t units = ceil_div<int64_t>(m, 128 * kTiles[c.tile].cg) * ceil_div<int64_t>(k, kTiles[c.tile].bn) *
+                                  c.splits * kTiles[c.tile].cg;
+            const double us = (double)m * n * 2 / (2.0 * imin<int64_t>(units, num_sms()) * 3000.0);
+            along = us <= imax(c.us, 4.0);
+        }
+        if (along) {
+            a.sum_src = p;
+            a.sum_ld = dy->ld;
+            a.sum_rows = m;
+            a.sum_cols = n;
+            a.sum_vec = vec;
+            a.sum_add = accumulate != 0;
+            a.sum_dst = db;
+        } else {
+            const dim3 grid((unsigned)imin<int64_t>(ceil_div<int64_t>(m, 4), (int64_t)num_sms() * 16)), block(128);
+            if (dy->dtype == CSRT_DT_F16)
+                launch_pdl(row_sums_kernel<true>, grid, block, 0, s, p, dy->ld, m, n, vec, accumulate != 0, db);
+            else
+                launch_pdl(row_sums_kernel<false>, grid, block, 0, s, p, dy->ld, m, n, vec, accumulate != 0, db);
+            count_launch();
+            CSRT_TRY(check_launch("row_sums_kernel"));
+        }
+    }
+    if (m == 0 || k == 0) return CSRT_OK;
     return dense_product<kEpiBwd>(dy, false, x, false, a, dw, nullptr, ws, s);
 }
 

@@ -70,6 +70,10 @@ struct GArgs {
     int32_t f16;                      // operands and 16-bit epilogue tensors are float16 (else bfloat16)
     // epilogue
     const float *bias;
+    const uint16_t *sum_src;          // kEpiBwd: matrix whose row sums the idle warps take (NULL: none)
+    int64_t sum_ld;
+    int32_t sum_rows, sum_cols, sum_vec, sum_add;
+    float *sum_dst;
     int32_t act;                      // activation (kEpiFwd), or act' of c0 as a factor (kEpiBwd)
     int32_t kind, sym, tall;          // kEpiNs: kNs*, tiles on and above the diagonal only, X has more rows than columns
     float alpha, gamma;               // kEpiNs: scale of the sum, of the result
@@ -484,6 +488,28 @@ __device__ __forceinline__ void emit(const GArgs &a, const GMaps &maps, uint8_t 
             if (a.out1.p != nullptr) tma_store_3d(&maps.out1, col, row, b, slot + 2048);
         }
     }
+}
+
+// Sum of a row of 16-bit elements by a warp: four 16-byte loads a lane in flight, float32, lanes joined at the end.
+template <bool F16>
+__device__ __forceinline__ float warp_row_sum(const uint16_t *p, int cols, bool vec) {
+    const int lane = threadIdx.x & 31;
+    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+    int c = vec ? cols & ~7 : 0;
+    if (vec) {
+#pragma unroll 4
+        for (int t = lane * 8; t < c; t += 256) {
+            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p + t));
+            const float2 x = unpack16(u.x, F16), y = unpack16(u.y, F16), z = unpack16(u.z, F16), w = unpack16(u.w, F16);
+            s0 += x.x + x.y, s1 += y.x + y.y, s2 += z.x + z.y, s3 += w.x + w.y;
+        }
+    }
+#pragma unroll 4
+    for (int t = c + lane; t < cols; t += 32) s0 += load1(p, t, F16 ? CSRT_DT_F16 : CSRT_DT_BF16);
+    float s = (s0 + s1) + (s2 + s3);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
 }
 
 // ---------------------------------------------------------------------------
@@ -930,6 +956,16 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
         }
     } else if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if constexpr (EPI == kEpiBwd) {   // the bias gradient beside the product: two rows of dy at a time
+            const GArgs &a = L.args[0];
+            if (a.sum_src != nullptr)
+                for (int r = blockIdx.x * 2 + warp - 2; r < a.sum_rows; r += gridDim.x * 2) {
+                    const uint16_t *p = a.sum_src + (int64_t)r * a.sum_ld;
+                    const float t = a.f16 ? warp_row_sum<true>(p, a.sum_cols, a.sum_vec)
+                                          : warp_row_sum<false>(p, a.sum_cols, a.sum_vec);
+                    if (lane == 0) a.sum_dst[r] = a.sum_add ? a.sum_dst[r] + t : t;
+                }
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int q = warp & 3, half = (warp - 4) >> 2;

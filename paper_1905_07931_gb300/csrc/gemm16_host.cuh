@@ -163,21 +163,27 @@ int launch_tile(const GProduct &p, const GArgs &a, cudaStream_t s) {
     return check_launch("gemm16_kernel");
 }
 
+// The tile and slices of a product by the model.
+struct GChoice {
+    int tile, splits;
+    double us;
+};
+inline GChoice choose_tile(const GArgs &a, int64_t reduction) {
+    GChoice best = {0, 1, 1e30};
+    for (int c = 0; c < 3; ++c) {
+        double us;
+        const int sp = best_splits(kTiles[c], a, reduction, &us);
+        if (us < best.us) best = {c, sp, us};
+    }
+    return best;
+}
+
 template <int EPI, bool PROMOTE>
 int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the dense products need a GPU with tcgen05");
-    int best = 0, best_s = 1;
-    double best_us = 1e30;
-    for (int c = 0; c < 3; ++c) {
-        double us;
-        const int sp = best_splits(kTiles[c], a, p.reduction, &us);
-        if (us < best_us) {
-            best_us = us;
-            best = c;
-            best_s = sp;
-        }
-    }
-    a.splits = best_s;
+    const GChoice choice = choose_tile(a, p.reduction);
+    const int best = choice.tile;
+    a.splits = choice.splits;
     if (aligned_set(a, PROMOTE)) {
         if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, false>(p, a, s);
         if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, false>(p, a, s);
