@@ -477,15 +477,24 @@ __device__ __forceinline__ void put32(const float (&v)[32], const GMat &o, uint8
     __syncwarp();
 }
 
-// The staged outputs leave: out0 from slot, out1 from slot + 2048.
+// The 32 x 32 block turned about the diagonal, in the layout of put32 (float16).
+__device__ __forceinline__ void put32_turned(const float (&v)[32], uint8_t *at) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        *reinterpret_cast<__half *>(at + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2) = __float2half_rn(v[i]);
+}
+
+// The staged outputs leave: out0 from slot, out1 - or the mirrored block of out0 - from slot + 2048.
 template <bool GEN>
-__device__ __forceinline__ void emit(const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col) {
+__device__ __forceinline__ void emit(const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col, bool mirror) {
     if (!GEN || a.out0.vec) {   // out1 likewise, if there is one
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if ((threadIdx.x & 31) == 0 && row < a.m && col < a.n) {   // lane 0's row is the block's first
             tma_store_3d(&maps.out0, col, row, b, slot);
             if (a.out1.p != nullptr) tma_store_3d(&maps.out1, col, row, b, slot + 2048);
+            if (mirror) tma_store_3d(&maps.out0, row, col, b, slot + 2048);
         }
     }
 }
@@ -635,7 +644,8 @@ __device__ __forceinline__ float diag_ahead(const GArgs &a, int b, int at, int l
 // of it; so do unaligned outputs.
 template <int EPI, bool GEN, bool WIDE>
 __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4], const uint4 (&u1)[4], float di, float dj,
-                                           const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col) {
+                                           const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col,
+                                           bool mirror) {
     float *turn = reinterpret_cast<float *>(slot);
     const int lane = threadIdx.x & 31;
     if constexpr (EPI == kEpiFwd) {
@@ -751,16 +761,8 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
         }
     }
     put32<GEN, WIDE>(v, a.out0, slot, b, row, col, a.m, a.n);
-    emit<GEN>(a, maps, slot, b, row, col);
-}
-
-// The same 32 values into the mirrored place of a symmetric output (float16): lane-contiguous stores.
-__device__ __forceinline__ void mirror32(const float (&v)[32], const GMat &o, int b, int row, int col, int m, int n) {
-    if (row >= m) return;
-    __half *p = static_cast<__half *>(o.p) + b * o.stride + row;
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-        if (col + i < n) p[(int64_t)(col + i) * o.ld] = __float2half_rn(v[i]);
+    if (EPI == kEpiNs && mirror) put32_turned(v, slot + 2048);
+    emit<GEN>(a, maps, slot, b, row, col, EPI == kEpiNs && mirror);
 }
 
 template <int CG, int BN>
@@ -861,7 +863,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             if (lane == 0)
                 asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(go)) : "memory");
             // the loads below go through the async proxy and follow what the barrier ordered
-            if (phase > 0) asm volatile("fence.proxy.async;" ::: "memory");
+            if (phase > 0) asm volatile("fence.proxy.async.global;" ::: "memory");
         }
         for (int u = unit0; u < a.units && !s_abort; u += ustep) {
             const GUnit w = unit_of<R>(a, u);
@@ -1121,7 +1123,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     }
                     __syncwarp();
-                    epilogue32<EPI, GEN, PROMOTE>(v, u0, u1, di, dj, a, maps, stage0 + slot * (kGStageOut / 2), w.b, row, col);
+                    epilogue32<EPI, GEN, PROMOTE>(v, u0, u1, di, dj, a, maps, stage0 + slot * (kGStageOut / 2), w.b, row, col,
+                                                  NS && a.sym && w.tn >= R * (w.tm + 1));
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     slot = a.slots == 2 ? slot ^ 1 : 0;
                     if (pass == 0 && i + 1 < kChunks / 2) {   // the next group's operands, while this one leaves
@@ -1129,8 +1132,6 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, col + 64, a.m, a.n);
                         if (NS) dj = diag_ahead(a, w.b, col + 64 + lane, imin(a.n, a.s_pad));
                     }
-                    if constexpr (NS)
-                        if (a.sym && w.tn >= R * (w.tm + 1)) mirror32(v, a.out0, w.b, row, col, a.m, a.n);
                 }
             }
         }

@@ -86,7 +86,7 @@ int fill_set(const GProduct &p, GArgs &a, GMaps &maps) {
     // one aligned 16-bit output, at most one operand and none to turn: a group needs half the staging
     const bool turns = !a.out0.vec || (a.c0.p != nullptr && !a.c0.vec) || (a.c1.p != nullptr && !a.c1.vec);
     const bool two_in = a.c0.p != nullptr && a.c1.p != nullptr;
-    a.slots = a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !two_in && !turns ? 2 : 1;
+    a.slots = a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !a.sym && !two_in && !turns ? 2 : 1;
     return CSRT_OK;
 }
 
