@@ -322,6 +322,15 @@ __device__ __forceinline__ float2 unpack16(uint32_t u, bool f16) {
     return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
 }
 
+// 16 bytes through L2 into u where `yes`, u kept otherwise. One predicated instruction: a conditional assignment makes
+// the compiler merge the two by a move, which waits for the load.
+__device__ __forceinline__ void ld_cg_if(uint4 &u, const void *p, bool yes) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %5, 0;\n @p ld.global.cg.v4.u32 {%0,%1,%2,%3}, [%4];\n}\n"
+        : "+r"(u.x), "+r"(u.y), "+r"(u.z), "+r"(u.w)
+        : "l"(p), "r"((uint32_t)yes));
+}
+
 // 16 bytes that are read once: not kept in L1.
 __device__ __forceinline__ uint4 ld_stream_u4(const void *p) {
     uint4 v;
@@ -569,6 +578,34 @@ template <bool GEN, bool WIDE>
 __device__ __forceinline__ bool ahead_ok(const GMat &c) {
     return GEN ? c.p != nullptr && c.vec && c.dtype != CSRT_DT_F32 : !WIDE && c.p != nullptr;
 }
+// A unit's view of such an operand in the lean kernel, whose columns are a multiple of eight or padded to one.
+struct GAhead {
+    const char *p;     // this lane's place in the unit's first row and column (NULL: no operand)
+    int64_t step;      // bytes to the lane's next row, eight further on
+    int32_t lim;       // columns readable from the unit's first one
+    uint32_t rows;     // bit i: row 8 i + lane / 4 exists
+};
+template <bool WIDE>
+__device__ __forceinline__ GAhead ahead_of(const GMat &c, int b, int row0, int col0, int m, int n) {
+    const int lane = threadIdx.x & 31, r = lane >> 2;
+    GAhead g = {nullptr, 0, 0, 0};
+    if (!ahead_ok<false, WIDE>(c)) return g;
+    g.p = reinterpret_cast<const char *>(static_cast<const uint16_t *>(c.p) + b * c.stride + (int64_t)(row0 + r) * c.ld +
+                                         col0 + 8 * (lane & 3));
+    g.step = 16 * c.ld;
+    g.lim = (c.pad ? (int)c.ld : n) - col0 - 8 * (lane & 3);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) g.rows |= (row0 + r + 8 * i < m ? 1u : 0u) << i;
+    return g;
+}
+__device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GAhead &g, int off) {
+    if (g.p == nullptr) return;
+    const char *p = g.p + 2 * off;
+    const uint32_t rows = off < g.lim ? g.rows : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ld_cg_if(u[i], p + i * g.step, (rows >> i) & 1);
+}
+
 template <bool GEN, bool WIDE>
 __device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GMat &c, int b, int row0, int col, int m, int n) {
     if (!ahead_ok<GEN, WIDE>(c)) return;
@@ -635,7 +672,11 @@ __device__ __forceinline__ void take32(float (&v)[32], const GMat &c, int b, int
 }
 // The diagonal at this lane's row (once per unit) and at column col + lane.
 __device__ __forceinline__ float diag_ahead(const GArgs &a, int b, int at, int limit) {
-    return a.diag_in != nullptr && at < limit ? __ldcg(a.diag_in + (int64_t)b * a.s_pad + at) : 0.f;
+    float v = 0.f;   // one predicated load, see ld_cg_if
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n @p ld.global.cg.f32 %0, [%1];\n}\n"
+                 : "+f"(v)
+                 : "l"(a.diag_in + (int64_t)b * a.s_pad + at), "r"((uint32_t)(a.diag_in != nullptr && at < limit)));
+    return v;
 }
 
 // The epilogue of 32 columns of a row in float32, in one slot of staging (4 KB, or 2 KB where one operand and one
@@ -990,12 +1031,24 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             const GUnit w = unit_of<R>(a, u);
             const int row = (w.tm * CG + (int)rank) * 128 + q * 32 + lane, n0 = w.tn * BN;
             const bool empty_sum = w.kb1 <= w.kb0;
-            if (NS) di = diag_ahead(a, w.b, row, imin(a.m, a.s_pad));
-            if (a.splits == 1) {
-                fetch_ahead<GEN, false>(u0, a.c0, w.b, row - lane, n0 + half * 32, a.m, a.n);
-                fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, n0 + half * 32, a.m, a.n);
-                if (NS) dj = diag_ahead(a, w.b, n0 + half * 32 + lane, imin(a.n, a.s_pad));
+            GAhead g0 = {}, g1 = {};
+            if constexpr (!GEN) {
+                g0 = ahead_of<false>(a.c0, w.b, row - lane, n0, a.m, a.n);
+                g1 = ahead_of<PROMOTE>(a.c1, w.b, row - lane, n0, a.m, a.n);
             }
+            const bool by_col = NS && (a.kind == kNsPoly || a.tall);
+            auto fetch = [&](int ci) {   // the operands of the 32 columns n0 + 32 ci ..
+                if constexpr (GEN) {
+                    fetch_ahead<GEN, false>(u0, a.c0, w.b, row - lane, n0 + ci * 32, a.m, a.n);
+                    fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, n0 + ci * 32, a.m, a.n);
+                } else {
+                    fetch_ahead(u0, g0, ci * 32);
+                    fetch_ahead(u1, g1, ci * 32);
+                }
+                if (by_col) dj = diag_ahead(a, w.b, n0 + ci * 32 + lane, imin(a.n, a.s_pad));
+            };
+            if (NS) di = diag_ahead(a, w.b, row, imin(a.m, a.s_pad));
+            if (a.splits == 1) fetch(half);
             bool ok = true;
             uint32_t d = 0;
             float sums[PROMOTE ? kChunks / 2 : 1][32];
@@ -1113,11 +1166,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     }
                     const int col = n0 + ci * 32;
                     if (col >= a.n) continue;
-                    if (pass == 1) {
-                        fetch_ahead<GEN, false>(u0, a.c0, w.b, row - lane, col, a.m, a.n);
-                        fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, col, a.m, a.n);
-                        if (NS) dj = diag_ahead(a, w.b, col + lane, imin(a.n, a.s_pad));
-                    }
+                    if (pass == 1) fetch(ci);
                     if (lane == 0) {
                         if (a.slots == 2) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                         else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -1127,11 +1176,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                                                   NS && a.sym && w.tn >= R * (w.tm + 1));
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     slot = a.slots == 2 ? slot ^ 1 : 0;
-                    if (pass == 0 && i + 1 < kChunks / 2) {   // the next group's operands, while this one leaves
-                        fetch_ahead<GEN, false>(u0, a.c0, w.b, row - lane, col + 64, a.m, a.n);
-                        fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, col + 64, a.m, a.n);
-                        if (NS) dj = diag_ahead(a, w.b, col + 64 + lane, imin(a.n, a.s_pad));
-                    }
+                    if (pass == 0 && i + 1 < kChunks / 2) fetch(ci + 2);   // the next group's, while this one leaves
                 }
             }
         }

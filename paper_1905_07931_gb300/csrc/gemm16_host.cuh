@@ -140,10 +140,14 @@ inline int best_splits(const GTile &t, const GArgs &a, int64_t reduction, double
     return best;
 }
 
-// Whether the kernel for aligned matrices serves: every epilogue matrix 16-byte aligned and of the kernel's own types.
+// Whether the kernel for aligned matrices serves: every epilogue matrix 16-byte aligned and of the kernel's own types,
+// and the 16-bit operands readable in eights up to the end of a row.
 inline bool aligned_set(const GArgs &a, bool wide) {
-    auto fine = [](const GMat &c, bool w) { return c.p == nullptr || (c.vec && (c.dtype == CSRT_DT_F32) == w); };
-    return a.out0.vec && (a.out0.dtype == CSRT_DT_F32) == wide && fine(a.out1, false) && fine(a.c0, false) && fine(a.c1, wide);
+    auto fine = [&](const GMat &c, bool w) {
+        return c.p == nullptr || (c.vec && (c.dtype == CSRT_DT_F32) == w && (w || c.pad || a.n % 8 == 0));
+    };
+    return a.out0.vec && (a.out0.dtype == CSRT_DT_F32) == wide && (a.out1.p == nullptr || a.out1.vec) && fine(a.c0, false) &&
+           fine(a.c1, wide);
 }
 
 template <int CG, int BN, int EPI, bool PROMOTE, bool GEN>
