@@ -91,16 +91,21 @@ struct GMaps {
     CUtensorMap a, b, out0, out1;
 };
 
-// A launch: one product, or the products of all Newton-Schulz steps one after the other (kNsSets different ones,
-// see ns_set), with a barrier of the whole (cooperative) grid between them.
+// A launch: one product, or the products of all Newton-Schulz steps of all matrices (kNsSets different ones, see
+// ns_set). In the latter the units of all phases form one sequence, phase by phase and matrix by matrix, dealt round to
+// the CTAs of a cooperative grid; a unit waits until its own matrix's units of the phase before have finished, so
+// matrices drift apart and fill each other's gaps. A CTA takes its units in order and all CTAs are resident, so the
+// earliest unfinished unit can always run.
 constexpr int kNsSets = 6;
+constexpr int kGoRing = 16;   // more than the units that a CTA can have between its producer and its epilogue
 template <int EPI>
 struct GLaunch {
     static constexpr int kSets = EPI == kEpiNs ? kNsSets : 1;
     GMaps maps[kSets];
     GArgs args[kSets];
     int32_t phases;
-    uint32_t *arrived;                // CTAs that have finished a phase, all phases together; zero at the start
+    int32_t step_units[3];            // units per matrix of the three products of a step
+    uint32_t *done;                   // per matrix: units finished, all phases together; zero at the start
 };
 
 // Sets of a Newton-Schulz launch: A of the even and odd steps' X, B, X' of the even and odd steps, the last X'.
@@ -178,8 +183,8 @@ __device__ __forceinline__ bool gwait_seen(bool seen, uint64_t *bar, uint32_t pa
     return gwait_warp(bar, parity, abort_flag);
 }
 
-// Wait of a whole warp until `arrived` reaches `target`; bounded like gwait.
-__device__ __forceinline__ bool grid_wait(const uint32_t *arrived, uint32_t target, volatile int *abort_flag) {
+// Wait of a whole warp until a matrix's count reaches `target`; bounded like gwait.
+__device__ __forceinline__ bool units_wait(const uint32_t *arrived, uint32_t target, volatile int *abort_flag) {
     bool ok = false;
     if ((threadIdx.x & 31) == 0) {
         const long long t0 = clock64();
@@ -806,6 +811,18 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
     emit<GEN>(a, maps, slot, b, row, col, EPI == kEpiNs && mirror);
 }
 
+// Units per matrix of the phases before `phase`, and this CTA's first unit of it.
+__device__ __forceinline__ uint32_t units_before(const int32_t (&n)[3], int phase) {
+    const int step = phase / 3, k = phase - 3 * step;
+    return (uint32_t)(step * (n[0] + n[1] + n[2]) + (k > 0 ? n[0] : 0) + (k > 1 ? n[1] : 0));
+}
+template <int EPI>
+__device__ __forceinline__ int first_unit(const GLaunch<EPI> &L, int phase, int batch, int unit0, int ustep) {
+    if (EPI != kEpiNs || phase == 0) return unit0;
+    const int r = (int)((uint64_t)units_before(L.step_units, phase) * (uint32_t)batch % (uint32_t)ustep);
+    return unit0 >= r ? unit0 - r : unit0 - r + ustep;
+}
+
 template <int CG, int BN>
 constexpr int gstage_bytes() {
     return 128 * 128 + (BN / CG) * 128;
@@ -839,10 +856,10 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     uint64_t *accf = empty + kStages;    // [2] accumulator ready
     uint64_t *acce = accf + 2;           // [2] accumulator drained
     uint64_t *fin = acce + 2;            // all MMAs complete
-    uint64_t *go = fin + 1;              // the phase's inputs are in place (kEpiNs)
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(go + 1);
+    uint64_t *go = fin + 1;              // [kGoRing] a unit's inputs are in place (kEpiNs)
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(go + kGoRing);
     __shared__ volatile int s_abort;
-    __shared__ int s_done;               // epilogue warps through with a phase, all phases together
+    __shared__ int s_done[kGoRing];      // epilogue warps through with a unit (kEpiNs)
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
@@ -850,7 +867,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
 
     if (threadIdx.x == 0) {
         s_abort = 0;
-        s_done = 0;
+        for (int i = 0; i < kGoRing; ++i) s_done[i] = 0;
         for (int s = 0; s < kStages; ++s) {
             mbar_init(full + s, 1);
             mbar_init(empty + s, 1);
@@ -860,7 +877,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             mbar_init(acce + i, CG * kGEpiWarps);
         }
         mbar_init(fin, 1);
-        mbar_init(go, 1);
+        for (int i = 0; i < kGoRing; ++i) mbar_init(go + i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&L.maps[0].a)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&L.maps[0].b)) : "memory");
@@ -892,22 +909,29 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
         int s = 0, issued = 0;
         uint32_t ph = 1;
         bool seen = true;   // the ring starts empty
+        int n_go = 0;
         for (int phase = 0; phase < L.phases && !s_abort; ++phase) {
         const GArgs &a = L.args[NS ? ns_set(phase, L.phases) : 0];
         const GMaps &maps = L.maps[NS ? ns_set(phase, L.phases) : 0];
-        if constexpr (NS) {
-            if (elect_one()) {   // while the others finish
+        if constexpr (NS)
+            if (elect_one()) {
                 asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.a)) : "memory");
                 asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.b)) : "memory");
             }
-            if (phase > 0 && !grid_wait(L.arrived, (uint32_t)phase * gridDim.x, &s_abort)) break;
-            if (lane == 0)
-                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(go)) : "memory");
-            // the loads below go through the async proxy and follow what the barrier ordered
-            if (phase > 0) asm volatile("fence.proxy.async.global;" ::: "memory");
-        }
-        for (int u = unit0; u < a.units && !s_abort; u += ustep) {
+        int known = -1;   // matrix whose inputs of this phase are known to be there
+        for (int u = first_unit(L, phase, a.batch, unit0, ustep); u < a.units && !s_abort; u += ustep) {
             const GUnit w = unit_of<R>(a, u);
+            if (NS && L.phases > 1) {
+                if (phase > 0 && w.b != known) {
+                    if (!units_wait(L.done + w.b, units_before(L.step_units, phase), &s_abort)) break;
+                    known = w.b;
+                }
+                if (lane == 0)
+                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(go + n_go % kGoRing)) : "memory");
+                ++n_go;
+                // the loads below go through the async proxy and follow what the wait ordered
+                if (phase > 0) asm volatile("fence.proxy.async.global;" ::: "memory");
+            }
             const int m0 = (w.tm * CG + (int)rank) * 128, n0 = w.tn * BN + (int)rank * kBRows;
             for (int kb = w.kb0; kb < w.kb1; ++kb) {
                 if (!gwait_seen(seen, empty + s, ph, &s_abort)) break;
@@ -960,7 +984,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                                    ((uint32_t)((128 * CG) >> 4) << 24);
             const uint32_t a_step = (a.a_mn ? 2048 : 32) >> 4, b_step = (a.b_mn ? 2048 : 32) >> 4;
             const uint64_t a0 = gdesc(smem_u32(smem), a.a_mn), b0 = gdesc(smem_u32(smem) + kABytes, a.b_mn);
-            for (int u = unit0; u < a.units && !s_abort; u += ustep) {
+            for (int u = first_unit(L, phase, a.batch, unit0, ustep); u < a.units && !s_abort; u += ustep) {
                 const GUnit w = unit_of<R>(a, u);
                 int kb = w.kb0;
                 do {   // one accumulation: the whole unit, or kPromoteKb stages of it
@@ -1019,15 +1043,20 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             acce_bar[1] = mapa_u32(acce_bar[1], 0);
         }
         int j = 0;
+        int n_go = 0;
         uint4 u0[4] = {}, u1[4] = {};
         float di = 0.f, dj = 0.f;
         for (int phase = 0; phase < L.phases; ++phase) {
-        int slot = 0;   // a phase ends with its staging free; the next one may use it in other portions
+        // the next phase may use the staging in other portions
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        int slot = 0;
         const GArgs &a = L.args[NS ? ns_set(phase, L.phases) : 0];
         const GMaps &maps = L.maps[NS ? ns_set(phase, L.phases) : 0];
-        if constexpr (NS)
-            if (!gwait_warp(go, phase & 1, &s_abort)) break;
-        for (int u = unit0; u < a.units; u += ustep) {
+        for (int u = first_unit(L, phase, a.batch, unit0, ustep); u < a.units; u += ustep) {
+            if (NS && L.phases > 1) {
+                if (!gwait_warp(go + n_go % kGoRing, (n_go / kGoRing) & 1, &s_abort)) break;
+                ++n_go;
+            }
             const GUnit w = unit_of<R>(a, u);
             const int row = (w.tm * CG + (int)rank) * 128 + q * 32 + lane, n0 = w.tn * BN;
             const bool empty_sum = w.kb1 <= w.kb0;
@@ -1179,18 +1208,20 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     if (pass == 0 && i + 1 < kChunks / 2) fetch(ci + 2);   // the next group's, while this one leaves
                 }
             }
-        }
-        if (NS && phase + 1 < L.phases) {
-            // This warp's outputs are in place: its TMA stores are complete, its lanes' own stores are ordered before the
-            // count by the block-scope fences. The CTA's last warp says so to the grid, with one release for all.
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-            __threadfence_block();
-            __syncwarp();
-            if (lane == 0 && !s_abort && atomicAdd(&s_done, 1) % kGEpiWarps == kGEpiWarps - 1) {
+            if (NS && L.phases > 1) {
+                // This warp's share of the unit is in place: its TMA stores are complete, its lanes' own stores are
+                // ordered before the count by the block-scope fences. The unit's last warp says so for its matrix.
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
                 __threadfence_block();
-                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(L.arrived) : "memory");
+                __syncwarp();
+                int *count = &s_done[(n_go - 1) % kGoRing];
+                if (lane == 0 && atomicAdd(count, 1) == kGEpiWarps - 1) {
+                    *count = 0;
+                    __threadfence_block();
+                    asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(L.done + w.b) : "memory");
+                }
+                __syncwarp();
             }
-            __syncwarp();
         }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");

@@ -34,7 +34,7 @@ struct PrepArgs {
     GMat o;                 // with no steps: the normalised direction itself
     int64_t ldx;
     int32_t direct;
-    uint32_t *arrived;      // the products' grid barrier, cleared here
+    uint32_t *done;         // the products' counts per matrix, cleared here
 };
 
 // Eight consecutive elements of row r from column c: gradient, old momentum -> u (and the new momentum stored).
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_momentum_kernel(PrepArgs a
 __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
     pdl_enter();
     const int b = blockIdx.y;
-    if (threadIdx.x == 0 && blockIdx.x == 0 && b == 0) *a.arrived = 0;
+    if (threadIdx.x == 0 && blockIdx.x == 0) a.done[b] = 0;
     double n2 = 0.0;
     for (int i = threadIdx.x; i < (int)gridDim.x; i += kPrepThreads) n2 += a.partial[(int64_t)b * gridDim.x + i];
     n2 = block_sum(n2);
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
 
 struct OrthoLayout {
     int64_t ldx, lds;
-    size_t slices, arrived, partial, x0, x1, lo, a, b, diag_a, diag_b, total;   // offsets after the reserved part
+    size_t slices, done, partial, x0, x1, lo, a, b, diag_a, diag_b, total;   // offsets after the reserved part
 };
 
 static OrthoLayout layout(int64_t batch, int64_t rows, int64_t cols) {
@@ -182,7 +182,7 @@ static OrthoLayout layout(int64_t batch, int64_t rows, int64_t cols) {
         return r;
     };
     l.slices = take((int64_t)kPartialBytes);
-    l.arrived = take(256);
+    l.done = take(batch * (int64_t)sizeof(uint32_t));
     l.partial = take(batch * kPrepBlocks * (int64_t)sizeof(double));
     l.x0 = take(batch * rows * l.ldx * 2);
     l.x1 = take(batch * rows * l.ldx * 2);
@@ -289,13 +289,17 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
         GArgs &a = n.args[set];
         ns_product(q, set, p, a);
         double us;
-        a.splits = best_splits(tile, a, p.reduction, &us);
+        // slices of different matrices' phases would share their place in the workspace
+        a.splits = q.batch == 1 ? best_splits(tile, a, p.reduction, &us) : 1;
         const int rc = fill_set<CG, BN>(p, a, n.maps[set]);
         if (rc != CSRT_OK) return rc;
         units = imax(units, a.units);
     }
     n.phases = 3 * q.steps;
-    n.arrived = reinterpret_cast<uint32_t *>(q.base + q.l.arrived);
+    n.done = reinterpret_cast<uint32_t *>(q.base + q.l.done);
+    n.step_units[0] = n.args[0].units / q.batch;
+    n.step_units[1] = n.args[2].units / q.batch;
+    n.step_units[2] = n.args[3].units / q.batch;
 
     constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false, GEN>;
     constexpr int smem = gsmem_bytes<CG, BN>();
@@ -447,7 +451,7 @@ int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float
     p.hi = reinterpret_cast<__half *>(base + l.x0);
     p.lo = reinterpret_cast<__half *>(base + l.lo);
     p.ldx = l.ldx;
-    p.arrived = reinterpret_cast<uint32_t *>(base + l.arrived);
+    p.done = reinterpret_cast<uint32_t *>(base + l.done);
     p.direct = steps == 0;
     p.o.p = o->data;
     p.o.ld = o->ld;
