@@ -105,7 +105,7 @@ struct GLaunch {
     GArgs args[kSets];
     int32_t phases;
     int32_t step_units[3];            // units per matrix of the three products of a step
-    uint32_t *done;                   // per matrix: units finished, all phases together; zero at the start
+    uint32_t *done;                   // per matrix: units finished, all phases together, by each CTA; zero at the start
 };
 
 // Sets of a Newton-Schulz launch: A of the even and odd steps' X, B, X' of the even and odd steps, the last X'.
@@ -923,7 +923,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             const GUnit w = unit_of<R>(a, u);
             if (NS && L.phases > 1) {
                 if (phase > 0 && w.b != known) {
-                    if (!units_wait(L.done + w.b, units_before(L.step_units, phase), &s_abort)) break;
+                    if (!units_wait(L.done + w.b, units_before(L.step_units, phase) * CG, &s_abort)) break;
                     known = w.b;
                 }
                 if (lane == 0)

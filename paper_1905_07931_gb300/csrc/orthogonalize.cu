@@ -2,9 +2,9 @@
 //
 //   X <- a X + (b A + c A A) X,   A = X X^T  (X^T X and products on the right where X has more rows than columns)
 //
-// as three products per step on gemm16_kernel: A with its mirrored half, B = b A + c A A likewise, and a X + B X. For
-// small matrices one launch runs all of them, a cooperative grid of one CTA per SM with a grid-wide barrier between
-// products; for large ones each is a launch on the tiles that suit it.
+// as three products per step on gemm16_kernel: A with its mirrored half, B = b A + c A A likewise, and a X + B X. One
+// cooperative launch runs all of them for all matrices, a unit waiting for its own matrix only (GLaunch); a single
+// large matrix takes a launch per product.
 //
 // Number formats. Singular values stay in [0, 1.203] (p(s) = a s + b s^3 + c s^5 maps [0, 1.203] into itself), so
 // every entry of X, A and B is bounded (1.203, 1.45, 2.81) and fits float16 once scaled by a power of two: X and A
@@ -305,23 +305,36 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     constexpr int smem = gsmem_bytes<CG, BN>();
     const int rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
-    // CTAs that the GPU can hold at once: all of them have to be there for the barrier
+    // CTAs (or pairs) that the GPU can hold at once: all of them have to be there, as units wait for one another
     static int resident[64] = {0};
     int dev = 0;
     CSRT_CHECK_CUDA(cudaGetDevice(&dev));
     int slots = dev >= 0 && dev < 64 ? resident[dev] : 0;
     if (slots == 0) {
-        CSRT_CHECK_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&slots, kernel, kGThreads, smem));
-        slots *= num_sms();
+        if (CG == 1) {
+            CSRT_CHECK_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&slots, kernel, kGThreads, smem));
+            slots *= num_sms();
+        } else {
+            cudaLaunchAttribute dim[1];
+            dim[0].id = cudaLaunchAttributeClusterDimension;
+            dim[0].val.clusterDim.x = CG;
+            dim[0].val.clusterDim.y = dim[0].val.clusterDim.z = 1;
+            cudaLaunchConfig_t probe = {};
+            probe.gridDim = dim3(num_sms() / CG * CG);
+            probe.blockDim = dim3(kGThreads);
+            probe.dynamicSmemBytes = smem;
+            probe.attrs = dim;
+            probe.numAttrs = 1;
+            CSRT_CHECK_CUDA(cudaOccupancyMaxActiveClusters(&slots, kernel, &probe));
+        }
         if (slots < 1) return fail(CSRT_ERR_CUDA, "the orthogonalisation does not fit the GPU");
         if (dev >= 0 && dev < 64) resident[dev] = slots;
     }
-    static_assert(CG == 1, "residency is counted in single CTAs");
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeCooperative;
     attr[0].val.cooperative = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)imin(units, imin(slots, num_sms())));
+    cfg.gridDim = dim3((unsigned)(imin(units, imin(slots, imax(1, num_sms() / CG))) * CG));
     cfg.blockDim = dim3(kGThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -332,32 +345,20 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     return check_launch("gemm16_kernel (Newton-Schulz)");
 }
 
-// Between products: a grid barrier of the one launch against a launch of its own (us, measured).
-constexpr double kBarrierUs = 1.5, kLaunchUs = 3.0;
-
 static int ns_products(const NsPlan &q, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the orthogonalisation needs a GPU with tcgen05");
-    // One launch runs all products on one kind of tile; launches of their own let each have its best. Take what the
-    // model finds faster: small matrices one launch, large ones a launch per product.
-    double one[3] = {0.0, kBarrierUs * 3, kBarrierUs * 3}, each = 0.0;
-    for (int set = 0; set < 4; ++set) {
-        if (set == 1) continue;   // as set 0
-        GProduct p;
-        GArgs a;
-        ns_product(q, set, p, a);
-        double best = 1e30;
-        for (int c = 0; c < 3; ++c) {
-            double us;
-            best_splits(kTiles[c], a, p.reduction, &us);
-            one[c] += us;
-            if (us < best) best = us;
-        }
-        each += best + kLaunchUs;
-    }
+    // By the number of 128 x 128 tiles of X (measured, us for the whole call on 64 / 128 / 256 wide tiles in one launch
+    // and on launches of their own): few tiles take the narrow ones, which share the work among more SMs
+    // (1024 x 1024: 127 / 156 / 230, 140; 3 x 2048 x 512: 160 / 184 / 248, 200); from 200 tiles on 128 x 128
+    // (1000 x 9216: 360 / 341 / 400, 344; 2 x 1500 x 3000: 441 / 344 / 369, 424); from 700 on, where L2 traffic
+    // counts, pairs of SMs, in one launch for several matrices, which fill each other's gaps (3 x 2048 x 2048:
+    // 785 / 510 / 451, 606), and for a single one each product on the tile that suits it best (4096 x 4096:
+    // 1836 / 1320 / 1071, 1010).
+    const int64_t tiles = (int64_t)q.batch * ceil_div<int64_t>(q.rows, 128) * ceil_div<int64_t>(q.cols, 128);
     const bool gen = !q.o.vec || q.o.dtype == CSRT_DT_F32;   // only o can need the general kernel
-    if (one[1] <= each && one[1] <= one[2])
-        return gen ? launch_ns<1, 128, true>(q, kTiles[1], s) : launch_ns<1, 128, false>(q, kTiles[1], s);
-    if (one[2] <= each) return gen ? launch_ns<1, 64, true>(q, kTiles[2], s) : launch_ns<1, 64, false>(q, kTiles[2], s);
+    if (tiles < 200) return gen ? launch_ns<1, 64, true>(q, kTiles[2], s) : launch_ns<1, 64, false>(q, kTiles[2], s);
+    if (tiles < 700) return gen ? launch_ns<1, 128, true>(q, kTiles[1], s) : launch_ns<1, 128, false>(q, kTiles[1], s);
+    if (q.batch > 1) return gen ? launch_ns<2, 256, true>(q, kTiles[0], s) : launch_ns<2, 256, false>(q, kTiles[0], s);
     for (int phase = 0; phase < 3 * q.steps; ++phase) {
         const int step = phase / 3, k = phase % 3;
         const int set = k == 0 ? step & 1 : k == 1 ? 2 : phase == 3 * q.steps - 1 ? 5 : 3 + (step & 1);
