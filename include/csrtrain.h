@@ -401,8 +401,10 @@ int csrt_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols
  * operands (11 significant bits; all matrices are scaled so that entries lie
  * within their bounds, as singular values stay below 1.21), X is carried with
  * 22 bits and sums are float32, so o is within about 1e-3 of the exact
- * iteration (2-norm, relative). A matrix holding an infinity or a NaN yields
- * NaN. o may feed prox_update_compact as the search direction of a layer's
+ * iteration (2-norm, relative); where u has no component at all (fewer samples
+ * than rows) what the first steps round grows with the iteration, 3.4 times a
+ * step, and o may be a few 1e-3 off. A matrix holding an infinity or a NaN
+ * yields NaN. o may feed prox_update_compact as the search direction of a layer's
  * prox step. beta in [0, 1), eps > 0 and finite, 0 <= steps <= 32, batch <=
  * 65535. o must not overlap g or momentum. */
 int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float *momentum, float beta,

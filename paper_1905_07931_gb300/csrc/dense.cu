@@ -86,7 +86,7 @@ static int operand(const csrt_mat *m, char **at, cudaStream_t s, GOperand *o) {
     o->rows = m->rows;
     o->cols = m->cols;
     o->ld = m->ld;
-    if (tma_rows_ok(m->data, m->ld, 2)) return CSRT_OK;
+    if (tma_rows_ok(m->data, m->ld, 2) || m->rows == 0 || m->cols == 0) return CSRT_OK;   // (an empty one is not read)
     o->ld = (int64_t)align_up((size_t)m->cols, 8);
     o->p = *at;
     *at += align_up((size_t)m->rows * o->ld * 2, 256);

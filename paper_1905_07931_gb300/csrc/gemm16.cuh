@@ -70,7 +70,7 @@ struct GArgs {
     int32_t f16;                      // operands and 16-bit epilogue tensors are float16 (else bfloat16)
     // epilogue
     const float *bias;
-    const uint16_t *sum_src;          // kEpiBwd: matrix whose row sums the idle warps take (NULL: none)
+    const uint16_t *sum_src;          // kEpiBwd: matrix whose row sums the idle warps leave in sum_dst (NULL: none)
     int64_t sum_ld;
     int32_t sum_rows, sum_cols, sum_vec, sum_add;
     float *sum_dst;
@@ -1025,7 +1025,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if constexpr (EPI == kEpiBwd) {   // the bias gradient beside the product: two rows of dy at a time
             const GArgs &a = L.args[0];
-            if (a.sum_src != nullptr)
+            if (a.sum_dst != nullptr)
                 for (int r = blockIdx.x * 2 + warp - 2; r < a.sum_rows; r += gridDim.x * 2) {
                     const uint16_t *p = a.sum_src + (int64_t)r * a.sum_ld;
                     const float t = a.f16 ? warp_row_sum<true>(p, a.sum_cols, a.sum_vec)

@@ -33,7 +33,7 @@ class SparseNet:
     def __init__(self, layers, dense_weights, biases, batch: int, in_shape, *, device="cuda",
                  precision: int = C.CSRT_PREC_TF32, stream=None, grad_per_layer: bool = False,
                  fused: bool = True, optimizer: str = "sgd", beta1: float = 0.9, beta2: float = 0.999,
-                 rms_beta: float = 0.9, eps: float = 1e-8, overlap: bool = False):
+                 rms_beta: float = 0.9, eps: float = 1e-8, overlap: bool = False, muon_beta: float = 0.95):
         """layers: layer dicts; dense_weights/biases: numpy arrays, one per fc/conv
         layer (weights M x K, zero off the initial pattern); in_shape: (K,) for an
         fc-first net or (C, H, W) for a conv-first net. The dense gradients of
@@ -42,11 +42,13 @@ class SparseNet:
 
         optimizer selects the proximal method of the prox phase: "sgd" (the
         proximal gradient step), "rmsprop" (Prox-RMSProp, Algorithm 1, decay
-        rms_beta) or "adam" (Prox-ADAM, Algorithm 2, decays beta1 and beta2);
-        eps is the safeguard of both. The adaptive methods keep dense M x K
-        moment arrays per layer and count their steps on the host (the step
-        number is passed by value, so a captured graph replays the step it was
-        captured at). The debias phase is plain SGD in every case.
+        rms_beta), "adam" (Prox-ADAM, Algorithm 2, decays beta1 and beta2; eps
+        is the safeguard of both) or "muon" (the proximal step along the
+        orthogonalised momentum of the gradient, decay muon_beta, scaled by
+        0.2 sqrt(max(M, K)); the paper has no counterpart). All but "sgd" keep
+        dense M x K moment arrays per layer; the adaptive methods count their
+        steps on the host (the step number is passed by value, so a captured
+        graph replays the step it was captured at). The debias phase is plain SGD in every case.
 
         overlap: in the prox phase, the bias update and the weight update of
         every layer but the first run on a second stream (with its own
@@ -56,10 +58,11 @@ class SparseNet:
         transposed product only reads the current one. The second stream
         joins the caller's at the end of the step. (The debias phase updates
         the stored values in place and stays on one stream.)"""
-        if optimizer not in ("sgd", "rmsprop", "adam"):
+        if optimizer not in ("sgd", "rmsprop", "adam", "muon"):
             raise ValueError(f"unknown optimizer {optimizer!r}")
         self.optimizer = optimizer
         self.beta1, self.beta2, self.rms_beta, self.eps = beta1, beta2, rms_beta, eps
+        self.muon_beta = muon_beta
         self.t = 0
         self.grad_per_layer = grad_per_layer
         # the SGD prox phase applies the update in the gradient GEMM's epilogue
@@ -123,7 +126,11 @@ class SparseNet:
                 L["g"] = torch.zeros(M * K, **dev)
                 if optimizer == "adam":
                     L["m"] = torch.zeros(M, K, **dev)
-                if optimizer != "sgd":
+                if optimizer == "muon":
+                    L["m"] = torch.zeros(M, K, **dev)
+                    L["o"] = torch.zeros(M, K, **dev)
+                    L["ows"] = C.OrthogonalizeWorkspace(1, M, K, device=device, stream=stream)
+                elif optimizer != "sgd":
                     L["v"] = torch.zeros(M, K, **dev)
                 if grad_per_layer:
                     L["G"] = torch.zeros(M, K, **dev)
@@ -172,6 +179,9 @@ class SparseNet:
         """Device status of the step (synchronises): the flags of every
         workspace the network uses, OR-ed, and the largest required nnz."""
         flags, req = self.ws.status(self.stream)
+        if self.optimizer == "muon":
+            for L in self.params:
+                flags |= L["ows"].status(self.stream)[0]
         if self.overlap:
             f2, r2 = self.ws_side.status(self.stream)
             flags, req = flags | f2, max(req, r2)
@@ -280,6 +290,10 @@ class SparseNet:
                     elif self.optimizer == "adam":
                         C.prox_adam_update_compact(W, G, L["m"], L["v"], self.t, eta, lam, self.beta1, self.beta2,
                                                    self.eps, Wn, uws, us)
+                    elif self.optimizer == "muon":
+                        C.orthogonalize(G, L["o"], L["ows"], momentum=L["m"], beta=self.muon_beta,
+                                        scale=0.2 * max(M, K) ** 0.5, stream=us)
+                        C.prox_update_compact(W, L["o"], eta, lam, Wn, uws, us)
                     else:
                         C.prox_update_compact(W, G, eta, lam, Wn, uws, us)
                     L["cur"] = 1 - L["cur"]

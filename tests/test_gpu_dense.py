@@ -1,0 +1,333 @@
+"""Dense-layer calls against the definitions in float64.
+
+Bounds. A product's 16-bit operands multiply exactly in float32. The tensor core adds blocks of 16 products to the
+float32 accumulator with truncation (2^-23 of the running sum, itself at most S = sum |a||b|): after B = ceil(r / 16)
+blocks the sum is within (B + 8) 2^-23 S. Float32 outputs are taken out every 512 terms and added rounded to nearest:
+(32 + 8 + chunks) 2^-23 S. Slices of a split reduction add at most 32 more roundings. Activations have |act'| < 1.13
+and are evaluated to 2^-18 of max(1, |z|); the result is rounded once to its type (2^-8 bfloat16, 2^-11 float16,
+2^-24 float32, and float16's smallest step 2^-24 near zero).
+"""
+
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def C():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_1905_07931_gb300 import csrtrain
+    csrtrain.lib()
+    return csrtrain
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _mat(gen, rows, cols, dt, layout="tight", scale=1.0):
+    """rows x cols values; layout: tight rows, "wide" (rows of a wider buffer, aligned), "odd" (base and rows off the
+    16-byte grid)."""
+    v = (torch.randn(rows, cols, generator=gen, device="cuda") * scale).to(dt)
+    if layout == "tight":
+        return v
+    wide = (cols + 63) // 64 * 64 + 64 if layout == "wide" else cols + 5
+    buf = torch.full((rows, wide), float("nan"), dtype=dt, device="cuda")
+    view = buf[:, 0:cols] if layout == "wide" else buf[:, 3:3 + cols]
+    view.copy_(v)
+    return view
+
+
+def _act(z, act):
+    if act == "relu":
+        return z.clamp_min(0)
+    if act == "gelu":
+        return 0.5 * z * (1 + torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)))
+    if act == "silu":
+        return z * torch.sigmoid(z)
+    return z
+
+
+def _act_grad(z, act):
+    if act == "relu":
+        return (z > 0).double()
+    if act == "gelu":
+        c = math.sqrt(2 / math.pi)
+        t = torch.tanh(c * (z + 0.044715 * z ** 3))
+        return 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * c * (1 + 3 * 0.044715 * z * z)
+    if act == "silu":
+        p = torch.sigmoid(z)
+        return p * (1 + z * (1 - p))
+    return torch.ones_like(z)
+
+
+def _sum_tol(r, s, dt):
+    blocks = 40 + -(-r // 512) if dt == torch.float32 else -(-r // 16) + 8
+    return (blocks + 32) * 2.0 ** -23 * s
+
+
+def _check(got, want, tol, dt):
+    tol = tol + U[dt] * (want.abs() + tol) + (2.0 ** -24 if dt == torch.float16 else 0) + 1e-30
+    bad = ~((got.double() - want).abs() <= tol)
+    assert not bad.any(), (int(bad.sum()), float(((got.double() - want).abs() / tol).max()))
+
+
+SIZES = [(1, 1, 1), (1, 7, 3), (5, 1, 2), (3, 9, 1), (64, 64, 4), (130, 70, 5), (200, 96, 33), (33, 700, 8), (257, 129, 63),
+         (128, 64, 64), (1000, 520, 96), (256, 2048, 16), (96, 4096, 40), (2048, 72, 300), (777, 333, 511), (1024, 1024, 1024),
+         (4096, 640, 700), (300, 784, 256)]
+
+
+@pytest.mark.parametrize("m,k,n", SIZES)
+@pytest.mark.parametrize("dtype,out,act,layout", [("bf16", None, "gelu", "tight"), ("f16", None, "silu", "odd"),
+                                                  ("bf16", "f32", "relu", "wide"), ("f16", "f32", "none", "odd"),
+                                                  ("bf16", None, "relu", "wide"), ("f16", None, "none", "tight")])
+def test_forward(C, m, k, n, dtype, out, act, layout):
+    gen, dt = _gen(m * 131 + k * 17 + n), DT[dtype]
+    od = DT[out] if out else dt
+    w = _mat(gen, m, k, dt, layout, 1 / math.sqrt(k))
+    x = _mat(gen, k, n, dt, layout)
+    b = torch.randn(m, generator=gen, device="cuda")
+    r = _mat(gen, m, n, od, layout)
+    y, z = _mat(gen, m, n, od, layout), _mat(gen, m, n, dt, layout)
+    ws = C.DenseWorkspace(m, k, n)
+    C.dense_fwd(w, x, y, ws, bias=b, act=act, residual=r, z=z)
+    zz = w.double() @ x.double() + b.double()[:, None]
+    s = w.double().abs() @ x.double().abs() + b.double().abs()[:, None]
+    e = _sum_tol(k, s, od)
+    _check(z, zz, e, dt)
+    want = _act(zz, act) + r.double()
+    _check(y, want, 1.13 * e + 2.0 ** -18 * zz.abs().clamp_min(1) * (act != "none") + 2.0 ** -23 * (want.abs() + r.double().abs()), od)
+    # without the optional parts, and in place over the residual
+    C.dense_fwd(w, x, y, ws)
+    _check(y, w.double() @ x.double(), e, od)
+    y2 = r.clone() if layout == "tight" else r
+    want = w.double() @ x.double() + y2.double()
+    C.dense_fwd(w, x, y2, ws, residual=y2)
+    _check(y2, want, e + 2.0 ** -23 * want.abs(), od)
+    assert ws.status()[0] == 0
+
+
+@pytest.mark.parametrize("m,k,n", SIZES)
+@pytest.mark.parametrize("dtype,out,act,layout", [("bf16", None, "gelu", "tight"), ("f16", None, "relu", "odd"),
+                                                  ("bf16", "f32", "silu", "wide"), ("f16", None, "silu", "wide"),
+                                                  ("f16", "f32", "gelu", "odd")])
+def test_input_gradient(C, m, k, n, dtype, out, act, layout):
+    gen, dt = _gen(m * 7 + k * 3 + n), DT[dtype]
+    od = DT[out] if out else dt
+    w, dy = _mat(gen, m, k, dt, layout, 1 / math.sqrt(m)), _mat(gen, m, n, dt, layout)
+    z, r = _mat(gen, k, n, dt, layout), _mat(gen, k, n, od, layout)
+    dx = _mat(gen, k, n, od, layout)
+    ws = C.DenseWorkspace(m, k, n)
+    C.dense_bwd_x(w, dy, dx, ws, z_below=z, act=act, residual=r)
+    prod = w.double().t() @ dy.double()
+    s = w.double().abs().t() @ dy.double().abs()
+    e = _sum_tol(m, s, od)
+    want = prod * _act_grad(z.double(), act) + r.double()
+    tol = 1.13 * e + 2.0 ** -17 * prod.abs() * z.double().abs().clamp_min(1) + 2.0 ** -23 * (want.abs() + r.double().abs())
+    _check(dx, want, tol, od)
+    C.dense_bwd_x(w, dy, dx, ws)
+    _check(dx, prod, e, od)
+    assert ws.status()[0] == 0
+
+
+@pytest.mark.parametrize("m,k,n", SIZES + [(70, 90, 5000), (8192, 64, 2048)])
+@pytest.mark.parametrize("dtype,out,layout", [("bf16", "f32", "tight"), ("f16", "f32", "odd"), ("bf16", None, "wide"),
+                                              ("f16", None, "odd")])
+def test_weight_gradient(C, m, k, n, dtype, out, layout):
+    gen, dt = _gen(m + k + n), DT[dtype]
+    od = DT[out] if out else dt
+    dy, x = _mat(gen, m, n, dt, layout), _mat(gen, k, n, dt, layout)
+    dw, db = _mat(gen, m, k, od, layout), torch.zeros(m, device="cuda")
+    ws = C.DenseWorkspace(m, k, n)
+    C.dense_bwd_w(dy, x, dw, ws, db=db)
+    want, s = dy.double() @ x.double().t(), dy.double().abs() @ x.double().abs().t()
+    e = _sum_tol(n, s, od)
+    _check(dw, want, e, od)
+    sb = dy.double().abs().sum(1)
+    _check(db, dy.double().sum(1), (n / 32 + 16) * 2.0 ** -23 * sb, torch.float32)
+    before = dw.double().clone()
+    db0 = db.clone()
+    C.dense_bwd_w(dy, x, dw, ws, db=db, accumulate=True)
+    _check(dw, want + before, e + 2.0 ** -22 * (want.abs() + before.abs()), od)
+    _check(db, db0.double() * 2, (n / 32 + 17) * 2.0 ** -23 * 2 * sb, torch.float32)
+    assert ws.status()[0] == 0
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_gradients_against_differences(C, act):
+    """d/dt of f = sum(c * y) along a direction of x, W and b equals the calls' gradients contracted with it."""
+    gen, m, k, n = _gen(5), 40, 56, 24
+    w = (_mat(gen, m, k, torch.float32) / math.sqrt(k)).to(torch.float16)
+    x, c = _mat(gen, k, n, torch.float16), _mat(gen, m, n, torch.float16)
+    b = torch.randn(m, generator=gen, device="cuda")
+    ws = C.DenseWorkspace(m, k, n)
+    y, z = torch.empty(m, n, device="cuda"), torch.empty(m, n, dtype=torch.float16, device="cuda")
+    C.dense_fwd(w, x, y, ws, bias=b, act=act, z=z)
+    dpre = torch.empty(m, n, dtype=torch.float16, device="cuda")
+    C.dense_act_bwd(c, z, act, dpre)
+    dx, dw, db = torch.empty(k, n, device="cuda"), torch.empty(m, k, device="cuda"), torch.empty(m, device="cuda")
+    C.dense_bwd_x(w, dpre, dx, ws)
+    C.dense_bwd_w(dpre, x, dw, ws, db=db)
+
+    def f(dwt, dxt, dbt, t):
+        zz = (w.double() + t * dwt) @ (x.double() + t * dxt) + (b.double() + t * dbt)[:, None]
+        return (c.double() * _act(zz, act)).sum()
+
+    zero = (torch.zeros(m, k, device="cuda").double(), torch.zeros(k, n, device="cuda").double(),
+            torch.zeros(m, device="cuda").double())
+    for i, g in enumerate((dw, dx, db)):
+        for s in range(3):
+            d = torch.randn(g.shape, generator=_gen(100 + 10 * i + s), device="cuda").double()
+            args = list(zero)
+            args[i] = d
+            h = 1e-5
+            num = float((f(*args, h) - f(*args, -h)) / (2 * h))
+            ana = float((g.double() * d).sum())
+            # dpre, z and the kink of relu: 2^-11 relative per rounding, summed in quadrature over the entries
+            scale = float((g.double().abs() * d.abs()).sum())
+            assert abs(num - ana) <= 2e-2 * scale / math.sqrt(g.numel()) * 4 + 1e-6, (i, s, num, ana, scale)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 1000), (257, 33), (1024, 513)])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("din,dz,dout", [("bf16", "bf16", "bf16"), ("f32", "f16", "f16"), ("f16", "f32", "f32")])
+def test_act_bwd(C, rows, cols, act, din, dz, dout):
+    gen = _gen(rows + cols)
+    dy, z = _mat(gen, rows, cols, DT[din], "odd"), _mat(gen, rows, cols, DT[dz], "wide")
+    out = _mat(gen, rows, cols, DT[dout], "odd")
+    C.dense_act_bwd(dy, z, act, out)
+    want = dy.double() * _act_grad(z.double(), act)
+    _check(out, want, 2.0 ** -17 * dy.double().abs() * z.double().abs().clamp_min(1) * (act != "none") + 2.0 ** -23 * want.abs(), DT[dout])
+    if din == dout:   # in place
+        C.dense_act_bwd(dy, z, act, dy)
+        assert torch.equal(dy, out)
+
+
+def test_dense_update_is_exact(C):
+    gen = _gen(9)
+    w, d = _mat(gen, 70, 130, torch.float32), _mat(gen, 70, 130, torch.bfloat16, "odd")
+    w16 = _mat(gen, 70, 130, torch.float16, "wide")
+    eta, decay = 0.03, 0.1
+    keep = (1.0 - torch.tensor(eta, dtype=torch.float32) * torch.tensor(decay, dtype=torch.float32)).float().cuda()
+    want = w * keep - torch.tensor(eta, dtype=torch.float32, device="cuda") * d.float()
+    C.dense_update(w, d, eta, decay, w16)
+    assert torch.equal(w, want) and torch.equal(w16, want.to(torch.float16))
+
+
+def test_empty_reductions_and_empty_outputs(C):
+    b = torch.randn(6, device="cuda")
+    ws = C.DenseWorkspace(64, 64, 64)
+    for n in (3, 40):   # both forward paths
+        w, x = torch.empty(6, 0, dtype=torch.bfloat16, device="cuda"), torch.empty(0, n, dtype=torch.bfloat16, device="cuda")
+        y = torch.full((6, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+        C.dense_fwd(w, x, y, ws, bias=b, act="relu")
+        assert torch.equal(y, b.clamp_min(0).to(torch.bfloat16)[:, None].expand(6, n))
+    dy, x = torch.empty(6, 0, dtype=torch.float16, device="cuda"), torch.empty(9, 0, dtype=torch.float16, device="cuda")
+    dw, db = torch.ones(6, 9, device="cuda"), torch.ones(6, device="cuda")
+    C.dense_bwd_w(dy, x, dw, ws, db=db, accumulate=True)
+    assert bool((dw == 1).all()) and bool((db == 1).all())
+    C.dense_bwd_w(dy, x, dw, ws, db=db)
+    assert bool((dw == 0).all()) and bool((db == 0).all())
+
+
+def test_infinities_and_nans_stay_in_their_rows_and_columns(C):
+    gen = _gen(3)
+    m, k, n = 200, 150, 90
+    w, x = _mat(gen, m, k, torch.bfloat16), _mat(gen, k, n, torch.bfloat16).abs() + 0.5
+    w[17, 3] = float("inf")
+    w[60, 5] = float("nan")
+    y = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    ws = C.DenseWorkspace(m, k, n)
+    C.dense_fwd(w, x, y, ws, act="silu")
+    assert bool((y[17] == float("inf")).all()) and bool(y[60].isnan().all())
+    rest = [i for i in range(m) if i not in (17, 60)]
+    assert bool(y[rest].isfinite().all())
+
+
+@pytest.mark.parametrize("n", [1, 4, 24, 200])
+def test_results_repeat_bit_for_bit(C, n):
+    gen = _gen(n)
+    m, k = 600, 5000
+    w, x = _mat(gen, m, k, torch.bfloat16), _mat(gen, k, n, torch.bfloat16)
+    ws, outs = C.DenseWorkspace(m, k, n), []
+    for _ in range(4):
+        y, dx = torch.empty(m, n, device="cuda"), torch.empty(k, n, dtype=torch.bfloat16, device="cuda")
+        dw, db = torch.empty(m, k, device="cuda"), torch.empty(m, device="cuda")
+        C.dense_fwd(w, x, y, ws)
+        dy = y.to(torch.bfloat16)
+        C.dense_bwd_x(w, dy, dx, ws)
+        C.dense_bwd_w(dy, x, dw, ws, db=db)
+        outs.append((y, dx, dw, db))
+    for o in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(o, outs[0]))
+
+
+def test_offsets_beyond_32_bits(C):
+    """Rows 2^26 elements apart: the last ones lie past 2^32 elements."""
+    gen, k, m, n, ld = _gen(4), 72, 66, 40, 1 << 26
+    buf = torch.empty(k, ld, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty(m, ld, dtype=torch.bfloat16, device="cuda")
+    x, y = buf[:, 64:64 + n], out[:, 128:128 + n]
+    x.copy_(torch.randn(k, n, generator=gen, device="cuda"))
+    w = _mat(gen, m, k, torch.bfloat16)
+    ws = C.DenseWorkspace(m, k, n)
+    for xx, yy in ((x, y), (x[:, :3], y[:, 1:4])):   # tensor cores; few tokens, off the 16-byte grid
+        C.dense_fwd(w, xx, yy, ws, residual=None)
+        want, s = w.double() @ xx.double(), w.double().abs() @ xx.double().abs()
+        _check(yy, want, _sum_tol(k, s, torch.bfloat16), torch.bfloat16)
+    del buf, out
+    torch.cuda.empty_cache()
+
+
+def test_calls_run_on_the_given_stream_and_in_a_graph(C):
+    gen, m, k, n = _gen(8), 256, 512, 96
+    w, x = _mat(gen, m, k, torch.bfloat16), _mat(gen, k, n, torch.bfloat16)
+    y = torch.zeros(m, n, dtype=torch.bfloat16, device="cuda")
+    want = torch.empty_like(y)
+    ws = C.DenseWorkspace(m, k, n)
+    C.dense_fwd(w, x, want, ws)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        x2 = x * 2
+    C.dense_fwd(w, x2, y, ws, stream=s)   # after the sleep and the product on s
+    s.synchronize()
+    assert torch.equal(y, (want.float() * 2).to(torch.bfloat16))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        C.dense_fwd(w, x, y, ws)
+    y.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
+def test_binding_refuses(C):
+    w = torch.zeros(8, 16, dtype=torch.bfloat16, device="cuda")
+    x, y = torch.zeros(16, 4, dtype=torch.bfloat16, device="cuda"), torch.zeros(8, 4, dtype=torch.bfloat16, device="cuda")
+    ws = C.DenseWorkspace(8, 16, 4)
+    with pytest.raises(ValueError, match="contiguous"):
+        C.dense_fwd(w, x.t().contiguous().t(), y, ws)
+    with pytest.raises(ValueError, match="2-D"):
+        C.dense_fwd(w, x[0], y, ws)
+    with pytest.raises(ValueError, match="not supported"):
+        C.dense_fwd(w.double(), x, y, ws)
+    with pytest.raises(ValueError, match="unknown activation"):
+        C.dense_fwd(w, x, y, ws, act="tanh")
+    with pytest.raises(C.CsrtError, match="must be 16 x 4"):
+        C.dense_fwd(w, x[:15], y, ws)
+    with pytest.raises(ValueError, match="bias"):
+        C.dense_fwd(w, x, y, ws, bias=torch.zeros(4, device="cuda"))
+    with pytest.raises(C.CsrtError, match="workspace has"):
+        C.dense_fwd(torch.zeros(4096, 16, dtype=torch.bfloat16, device="cuda"), x,
+                    torch.zeros(4096, 4, dtype=torch.bfloat16, device="cuda"), ws)

@@ -1,0 +1,260 @@
+"""The orthogonalised update against its iteration in float64.
+
+Bounds. The products' operands are float16 (2^-12 of an entry on average 1.4e-4 to 2e-4 of a matrix in the 2-norm):
+three of them a step, five steps, and the polynomial's slope is at most 1.6 where singular values have arrived: about
+sqrt(15) x 2e-4 x 1.6 = 1.3e-3 of o in the 2-norm where roundings add at random; 2e-3 is allowed. bfloat16 results add
+their own rounding, 1.7e-3 in the 2-norm (uniform within 2^-9): 3e-3 in all. The momentum is exact float32 arithmetic.
+"""
+
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+A, B, CC = 3.4445, -4.7750, 2.0315
+
+
+@pytest.fixture(scope="module")
+def C():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_1905_07931_gb300 import csrtrain
+    csrtrain.lib()
+    return csrtrain
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _exact(u, steps, eps, scale):
+    out = torch.empty_like(u)
+    for i in range(u.shape[0]):
+        x = u[i] / max(float(u[i].norm()), eps)
+        tall = x.shape[0] > x.shape[1]
+        x = x.t() if tall else x
+        for _ in range(steps):
+            a = x @ x.t()
+            x = A * x + (B * a + CC * (a @ a)) @ x
+        out[i] = scale * (x.t() if tall else x)
+    return out
+
+
+def _rel(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+SHAPES = [(1, 1, 1), (1, 1, 7), (2, 5, 1), (3, 3, 9), (1, 64, 64), (5, 64, 65), (1, 65, 130), (4, 129, 33), (1, 300, 784),
+          (1, 784, 300), (2, 200, 1000), (12, 96, 160), (1, 128, 4100), (1, 1000, 1024), (3, 700, 515), (2, 1300, 2051),
+          (1, 2050, 3000), (6, 256, 2048), (3, 2048, 1024)]
+
+
+@pytest.mark.parametrize("batch,m,k", SHAPES)
+@pytest.mark.parametrize("gdt,odt,nesterov", [(torch.float32, torch.float32, True), (torch.bfloat16, torch.bfloat16, True),
+                                              (torch.float32, torch.bfloat16, False)])
+def test_direction_and_momentum(C, batch, m, k, gdt, odt, nesterov):
+    gen = _gen(batch * 10007 + m * 31 + k)
+    g = (torch.randn(batch, m, k, generator=gen, device="cuda") * 1e-3).to(gdt)
+    mom = torch.randn(batch, m, k, generator=gen, device="cuda") * 3e-3
+    beta, scale = 0.95, 0.2 * math.sqrt(max(m, k))
+    bt = torch.tensor(beta, dtype=torch.float32, device="cuda")
+    want_mom = mom * bt + g.float()
+    u = g.float() + bt * want_mom if nesterov else want_mom
+    o = torch.empty(batch, m, k, dtype=odt, device="cuda")
+    ws = C.OrthogonalizeWorkspace(batch, m, k)
+    C.orthogonalize(g, o, ws, momentum=mom, beta=beta, nesterov=nesterov, scale=scale)
+    assert torch.equal(mom, want_mom)
+    assert _rel(o, _exact(u.double(), 5, 1e-7, scale)) <= (2e-3 if odt == torch.float32 else 3e-3)
+    assert ws.status()[0] == 0
+
+
+@pytest.mark.parametrize("steps", [0, 1, 2, 3, 8])
+def test_steps(C, steps):
+    g = torch.randn(2, 90, 150, generator=_gen(steps), device="cuda")
+    o, ws = torch.empty_like(g), C.OrthogonalizeWorkspace(2, 90, 150)
+    C.orthogonalize(g, o, ws, steps=steps, scale=2.0)
+    assert _rel(o, _exact(g.double(), steps, 1e-7, 2.0)) <= (1e-6 if steps == 0 else 2e-3)
+
+
+def test_singular_values_arrive_near_one(C):
+    g = torch.randn(400, 900, generator=_gen(1), device="cuda")
+    o, ws = torch.empty_like(g), C.OrthogonalizeWorkspace(1, 400, 900)
+    C.orthogonalize(g, o, ws)
+    s = torch.linalg.svdvals(o.double())
+    assert 0.6 < float(s.min()) and float(s.max()) < 1.3
+
+
+@pytest.mark.parametrize("where", ["g", "o", "both"])
+@pytest.mark.parametrize("m,k", [(37, 53), (130, 258)])
+def test_strided_and_unaligned(C, where, m, k):
+    gen, batch = _gen(2), 3
+    v = torch.randn(batch, m, k, generator=gen, device="cuda")
+    g, o = v, torch.empty(batch, m, k, device="cuda")
+    if where in ("g", "both"):
+        g = torch.full((batch, m + 2, k + 7), float("nan"), device="cuda")[:, 1:m + 1, 3:3 + k]
+        g.copy_(v)
+    if where in ("o", "both"):   # matrices side by side in one wide buffer: rows interleave
+        o = torch.zeros(m, batch, k + 1, device="cuda").permute(1, 0, 2)[:, :, :k]
+    ws = C.OrthogonalizeWorkspace(batch, m, k)
+    C.orthogonalize(g, o, ws)
+    assert _rel(o, _exact(v.double(), 5, 1e-7, 1.0)) <= 2e-3
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e12, 1e30])
+def test_norms_far_from_one(C, scale):
+    v = torch.randn(1, 100, 140, generator=_gen(6), device="cuda")
+    o, ws = torch.empty_like(v), C.OrthogonalizeWorkspace(1, 100, 140)
+    C.orthogonalize((v.double() * scale).float(), o, ws, eps=1e-38)
+    assert _rel(o, _exact(v.double(), 5, 1e-38, 1.0)) <= 2e-3
+
+
+def test_zero_and_not_a_number(C):
+    g = torch.randn(4, 80, 96, generator=_gen(7), device="cuda")
+    g[1] = 0
+    g[2, 5, 6] = float("nan")
+    g[3, 7, 8] = float("inf")
+    o, ws = torch.empty_like(g), C.OrthogonalizeWorkspace(4, 80, 96)
+    C.orthogonalize(g, o, ws)
+    assert bool((o[1] == 0).all()) and bool(o[2].isnan().all()) and bool(o[3].isnan().all())
+    assert _rel(o[:1], _exact(g[:1].double(), 5, 1e-7, 1.0)) <= 2e-3   # the others are not touched by them
+
+
+@pytest.mark.parametrize("spread", [30.0, 300.0])
+def test_strong_directions(C, spread):
+    """A few directions far above the rest, as gradients have them: the rest still comes out."""
+    gen = _gen(11)
+    u, _ = torch.linalg.qr(torch.randn(256, 256, generator=gen, device="cuda").double())
+    v, _ = torch.linalg.qr(torch.randn(512, 256, generator=gen, device="cuda").double())
+    s = torch.ones(256, device="cuda").double()
+    s[:6] = spread
+    g = ((u * s) @ v.t()).float()[None].contiguous()
+    o, ws = torch.empty_like(g), C.OrthogonalizeWorkspace(1, 256, 512)
+    C.orthogonalize(g, o, ws, steps=7)
+    assert _rel(o, _exact(g.double(), 7, 1e-7, 1.0)) <= 5e-3
+
+
+@pytest.mark.parametrize("rank,m,k", [(1, 60, 90), (16, 128, 200), (64, 300, 500), (200, 512, 1024)])
+def test_rank_deficient(C, rank, m, k):
+    """A gradient of few samples has singular values at zero, where the iteration multiplies whatever a step's rounding
+    leaves by a = 3.4445 in each later step: 2e-4 x |b| of at most 1 in the 2-norm, times 3.4445^(4 - step), sums to
+    0.19 against sqrt(rank) of the result, for each of the three operands at random: 0.33 / sqrt(rank)."""
+    gen = _gen(rank)
+    g = (torch.randn(m, rank, generator=gen, device="cuda") @ torch.randn(rank, k, generator=gen, device="cuda"))[None]
+    o, ws = torch.empty_like(g), C.OrthogonalizeWorkspace(1, m, k)
+    C.orthogonalize(g, o, ws)
+    assert _rel(o, _exact(g.double(), 5, 1e-7, 1.0)) <= 0.33 / math.sqrt(rank)
+
+
+def test_repeats_bit_for_bit_and_in_a_graph(C):
+    g = torch.randn(3, 300, 520, generator=_gen(13), device="cuda").bfloat16()
+    ws, outs = C.OrthogonalizeWorkspace(3, 300, 520), []
+    for _ in range(4):
+        o = torch.empty_like(g)
+        C.orthogonalize(g, o, ws)
+        outs.append(o)
+    assert all(torch.equal(o, outs[0]) for o in outs)
+    o, graph = torch.zeros_like(g), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        C.orthogonalize(g, o, ws)
+    for _ in range(2):
+        o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, outs[0])
+
+
+def test_two_streams_at_once(C):
+    """Two calls on two streams (a workspace each): the cooperative launches neither mix nor wait for one another's units."""
+    gs = [torch.randn(2, 260, 700, generator=_gen(20 + i), device="cuda") for i in range(2)]
+    wss = [C.OrthogonalizeWorkspace(2, 260, 700) for _ in range(2)]
+    outs = [torch.empty_like(g) for g in gs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for g, o, ws, s in zip(gs, outs, wss, streams):
+            C.orthogonalize(g, o, ws, stream=s)
+    torch.cuda.synchronize()
+    for g, o, ws in zip(gs, outs, wss):
+        assert _rel(o, _exact(g.double(), 5, 1e-7, 1.0)) <= 2e-3
+        assert ws.status()[0] == 0
+
+
+def test_binding_refuses(C):
+    g = torch.zeros(4, 6, device="cuda")
+    ws = C.OrthogonalizeWorkspace(1, 4, 6)
+    with pytest.raises(ValueError, match="one shape"):
+        C.orthogonalize(g, torch.zeros(6, 4, device="cuda"), ws)
+    with pytest.raises(ValueError, match="momentum"):
+        C.orthogonalize(g, torch.empty_like(g), ws, momentum=torch.zeros(4, 5, device="cuda"))
+    with pytest.raises(C.CsrtError, match="workspace has"):
+        C.orthogonalize(torch.zeros(300, 500, device="cuda"), torch.zeros(300, 500, device="cuda"),
+                        C.DenseWorkspace(1, 1, 1))
+    with pytest.raises(C.CsrtError, match="overlaps g"):
+        C.orthogonalize(g, g, ws)
+
+
+# --- with the compressed layers ---------------------------------------------
+
+def test_sparse_net_trains_along_orthogonalised_directions(C):
+    """SparseNet(optimizer="muon"): each layer's new CSR is the prox step of the direction that the call gave for the
+    layer (the direction itself is checked above, also for gradients of low rank such as these)."""
+    import numpy as np
+
+    import oracle as O
+    from paper_1905_07931_gb300 import synth
+    from paper_1905_07931_gb300.train import SparseNet, mlp_layers
+    cfg = synth.mlp(seed=3, batch=64, sizes=(96, 80, 10), densities=(0.3, 0.4))
+    net = SparseNet(mlp_layers(2), cfg["W"], cfg["b"], 64, (96,), optimizer="muon", grad_per_layer=True)
+    net.x_in.copy_(torch.from_numpy(cfg["X"]))
+    net.labels.copy_(torch.from_numpy(cfg["labels"]))
+    eta, lam = 0.02, 0.05
+    losses = []
+    for t in range(6):
+        old = [net.weights(i).to_host()[0] for i in range(2)]
+        losses.append(float(net.step("prox", eta, lam)[0].item()))
+        assert net.status()[0] == 0
+        for i, L in enumerate(net.params):
+            w = O.CSR(L["W"][0].rows, L["W"][0].cols, *old[i])
+            want = O.prox_update_compact(w, L["o"].cpu().numpy(), np.float32(eta), np.float32(lam))
+            rp, ci, v = net.weights(i).to_host()[0]
+            np.testing.assert_array_equal(rp, want.row_ptr)
+            np.testing.assert_array_equal(ci, want.col_idx)
+            np.testing.assert_array_equal(v.view(np.uint32), want.val.astype(np.float32).view(np.uint32))
+    assert losses[-1] < losses[0]
+
+
+def test_residual_net_gradients_and_training(C):
+    """The example's gradients against float64 backpropagation (bfloat16 activations: some eight roundings of 2^-9 on
+    the way, 2.5e-2 of a gradient's norm allowed), and that training brings the loss down."""
+    from paper_1905_07931_gb300.residual import ResidualNet
+    net = ResidualNet(72, 104, 2, 10, 88, seed=2)
+    gen = _gen(40)
+    centres = torch.randn(72, 10, generator=gen, device="cuda")
+    y = torch.randint(0, 10, (88,), generator=gen, device="cuda")
+    net.x[0].copy_(0.5 * centres[:, y] + torch.randn(72, 88, generator=gen, device="cuda"))
+    net.labels.copy_(y)
+    wc = torch.zeros(10, 72, dtype=torch.float64, device="cuda")
+    (rp, ci, v), _ = net.wc[0].to_host()
+    for r in range(10):
+        for j in range(rp[r], rp[r + 1]):
+            wc[r, ci[j]] = float(v[j])
+    p = [net.w1h.double().requires_grad_(), net.w2h.double().requires_grad_(), net.b1.double().requires_grad_(),
+         net.b2.double().requires_grad_(), wc.requires_grad_()]
+    x = net.x[0].double()
+    for i in range(2):
+        z = p[0][i] @ x + p[2][i][:, None]
+        x = x + p[1][i] @ torch.nn.functional.gelu(z, approximate="tanh") + p[3][i][:, None]
+    loss = torch.nn.functional.cross_entropy((p[4] @ x).t(), y)
+    loss.backward()
+    first = float(net.step(0.0, 0.0)[0].item())
+    assert abs(first - float(loss)) <= 2e-2 * float(loss)
+    for got, want in zip((net.g1, net.g2, net.db1, net.db2, net.gc), p):
+        assert _rel(got, want.grad) <= 2.5e-2
+    for _ in range(20):
+        last = float(net.step(0.02, 0.05)[0].item())
+    assert last < 0.7 * first and net.status() == 0
