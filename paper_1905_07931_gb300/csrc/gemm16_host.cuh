@@ -104,19 +104,20 @@ int allow_smem(int smem) {
 
 // Time of a product in microseconds by a simple model of gemm16_kernel: waves of units, each loading its stages and
 // then running an epilogue that overlaps the next unit's stages but not the last's; joining slices costs their
-// partial tiles' trip through L2. The constants are fitted to measured times of 54 products of 64 to 9216 rows and
-// columns on every tile and up to 16 slices; the choice they give is within 1% of the best on average.
+// partial tiles' trip through L2. The constants are fitted to measured times of 69 products of 64 to 9216 rows and
+// columns on every tile and up to 16 slices; the choice they give is within 1.2% of the best on average.
 struct GTile {
     int cg, bn;
     double stage, epi;   // us per stage, us per unit's epilogue
 };
-constexpr GTile kTiles[3] = {{2, 256, 0.35, 6.3}, {1, 128, 0.25, 4.9}, {1, 64, 0.21, 4.0}};
+constexpr int kTileKinds = 4;
+constexpr GTile kTiles[kTileKinds] = {{2, 256, 0.34, 5.7}, {1, 128, 0.245, 4.3}, {1, 64, 0.206, 3.6}, {2, 128, 0.228, 4.4}};
 inline double model_us(const GTile &t, int64_t tiles, int64_t kb, int64_t splits) {
     const int64_t slots = imax(1, num_sms() / t.cg);
     const int64_t units = tiles * splits, waves = ceil_div(units, slots);
     const double unit = (double)ceil_div(imax<int64_t>(kb, 1), splits) * t.stage;
-    double us = waves * (unit > t.epi ? unit : t.epi) + t.epi - 2.2;
-    if (splits > 1) us += 4.0 + 0.385 * splits * t.bn / 64;
+    double us = waves * (unit > t.epi ? unit : t.epi) + t.epi - 1.75;
+    if (splits > 1) us += 3.9 + 0.446 * splits * t.bn / 64;
     return us;
 }
 
@@ -125,12 +126,14 @@ inline int best_splits(const GTile &t, const GArgs &a, int64_t reduction, double
     const int64_t kb = ceil_div<int64_t>(reduction, kGBK);
     const int64_t tiles = a.batch * tile_count(a.sym, ceil_div<int64_t>(a.m, 128 * t.cg), ceil_div<int64_t>(a.n, t.bn),
                                                128 * t.cg / t.bn);
+    const int64_t slots = imax(1, num_sms() / t.cg);
     int best = 1;
     *us = 1e30;
     for (int64_t sp = 1; sp <= 32 && sp * 2 <= imax<int64_t>(kb, 2); ++sp) {
         if (sp > 1 && ((size_t)(tiles * sp) * t.cg * 128 * t.bn * sizeof(float) > kPartialBytes ||
                        tiles * t.cg * kGEpiWarps > (int64_t)kWsCounterInts))
             break;
+        if (sp > 1 && tiles * (sp - 1) >= 2 * slots) break;   // enough units already
         const double v = model_us(t, tiles, kb, sp);
         if (v < *us) {
             *us = v;
@@ -174,7 +177,7 @@ struct GChoice {
 };
 inline GChoice choose_tile(const GArgs &a, int64_t reduction) {
     GChoice best = {0, 1, 1e30};
-    for (int c = 0; c < 3; ++c) {
+    for (int c = 0; c < kTileKinds; ++c) {
         double us;
         const int sp = best_splits(kTiles[c], a, reduction, &us);
         if (us < best.us) best = {c, sp, us};
@@ -191,11 +194,16 @@ int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
     if (aligned_set(a, PROMOTE)) {
         if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, false>(p, a, s);
         if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, false>(p, a, s);
+        if (best == 3) return launch_tile<2, 128, EPI, PROMOTE, false>(p, a, s);
         return launch_tile<1, 64, EPI, PROMOTE, false>(p, a, s);
     }
-    if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, true>(p, a, s);
-    if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, true>(p, a, s);
-    return launch_tile<1, 64, EPI, PROMOTE, true>(p, a, s);
+    if constexpr (EPI != kEpiNs) {   // (its matrices are the library's own, all aligned)
+        if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, true>(p, a, s);
+        if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, true>(p, a, s);
+        if (best == 3) return launch_tile<2, 128, EPI, PROMOTE, true>(p, a, s);
+        return launch_tile<1, 64, EPI, PROMOTE, true>(p, a, s);
+    }
+    return fail(CSRT_ERR_ARG, "unaligned product");
 }
 
 }  // namespace csrt

@@ -201,8 +201,21 @@ struct NsPlan {
     char *base;
     OrthoLayout l;
     GMat o;
+    bool direct;   // the last product writes o (bfloat16, aligned); else it leaves X, and o is made of it afterwards
     void *ws;
 };
+
+// o = scale X from the float16 pair, for results that the products' epilogue does not write itself.
+__global__ void ortho_result_kernel(const __half *__restrict__ hi, const __half *__restrict__ lo, int64_t ldx, int32_t rows,
+                                    int32_t cols, float scale, GMat o) {
+    pdl_enter();
+    const int64_t b = blockIdx.z;
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
+        for (int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; c < cols; c += (int64_t)gridDim.x * blockDim.x) {
+            const int64_t i = (b * rows + r) * ldx + c;
+            store1(o.p, b * o.stride + r * o.ld + c, scale * (__half2float(hi[i]) + __half2float(lo[i])), o.dtype);
+        }
+}
 
 // Product `set` of the six that make up the steps (ns_set).
 static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
@@ -270,17 +283,18 @@ static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
         a.m = q.rows;
         a.n = q.cols;
         a.alpha = 2.f * kInvXScale;
-        a.gamma = set == 5 ? q.scale * kInvXScale : 1.f;
+        const bool out = set == 5 && q.direct;
+        a.gamma = out ? q.scale * kInvXScale : 1.f;
         a.diag_in = diag_b;
         a.c0 = mat(x, l.ldx, q.rows);
         a.c1 = mat(l.lo, l.ldx, q.rows);
-        a.out0 = set == 5 ? q.o : mat(set == 3 ? l.x1 : l.x0, l.ldx, q.rows);
-        if (set != 5) a.out1 = mat(l.lo, l.ldx, q.rows);
+        a.out0 = out ? q.o : mat(x == l.x0 ? l.x1 : l.x0, l.ldx, q.rows);
+        if (!out) a.out1 = mat(l.lo, l.ldx, q.rows);
     }
 }
 
 // All steps in one cooperative launch on CG x 128 x BN tiles.
-template <int CG, int BN, bool GEN>
+template <int CG, int BN>
 static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     GLaunch<kEpiNs> n = {};
     int32_t units = 1;
@@ -301,7 +315,7 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     n.step_units[1] = n.args[2].units / q.batch;
     n.step_units[2] = n.args[3].units / q.batch;
 
-    constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false, GEN>;
+    constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false, false>;
     constexpr int smem = gsmem_bytes<CG, BN>();
     const int rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
@@ -347,18 +361,17 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
 
 static int ns_products(const NsPlan &q, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the orthogonalisation needs a GPU with tcgen05");
-    // By the number of 128 x 128 tiles of X (measured, us for the whole call on 64 / 128 / 256 wide tiles in one launch
-    // and on launches of their own): few tiles take the narrow ones, which share the work among more SMs
-    // (1024 x 1024: 127 / 156 / 230, 140; 3 x 2048 x 512: 160 / 184 / 248, 200); from 200 tiles on 128 x 128
-    // (1000 x 9216: 360 / 341 / 400, 344; 2 x 1500 x 3000: 441 / 344 / 369, 424); from 700 on, where L2 traffic
-    // counts, pairs of SMs, in one launch for several matrices, which fill each other's gaps (3 x 2048 x 2048:
-    // 785 / 510 / 451, 606), and for a single one each product on the tile that suits it best (4096 x 4096:
-    // 1836 / 1320 / 1071, 1010).
+    // By the number of 128 x 128 tiles of X (measured, us for the whole call on tiles 64, 128 by pairs and 256 by pairs
+    // wide in one launch, and on launches of their own): few tiles take the narrow ones, which share the work among
+    // more SMs (1024 x 1024: 127 / 155 / 230, 140; 3 x 2048 x 512: 160 / 182 / 249, 200); from 200 tiles on pairs of SMs
+    // on 256 x 128 (2048 x 2048: 351 / 257 / 315, 282; 6 x 256 x 4096: 240 / 220 / 281, 249); from 700 on, where L2
+    // traffic counts most, 256 x 256: in one launch for several matrices, which fill each other's gaps
+    // (3 x 2048 x 2048: 782 / 487 / 447, 606), and for a single one a launch for each product, on its best tile
+    // (4096 x 4096: 1912 / 1184 / 1003, 999; 4096 x 9216: 3390 / 2323 / 1937, 1793).
     const int64_t tiles = (int64_t)q.batch * ceil_div<int64_t>(q.rows, 128) * ceil_div<int64_t>(q.cols, 128);
-    const bool gen = !q.o.vec || q.o.dtype == CSRT_DT_F32;   // only o can need the general kernel
-    if (tiles < 200) return gen ? launch_ns<1, 64, true>(q, kTiles[2], s) : launch_ns<1, 64, false>(q, kTiles[2], s);
-    if (tiles < 700) return gen ? launch_ns<1, 128, true>(q, kTiles[1], s) : launch_ns<1, 128, false>(q, kTiles[1], s);
-    if (q.batch > 1) return gen ? launch_ns<2, 256, true>(q, kTiles[0], s) : launch_ns<2, 256, false>(q, kTiles[0], s);
+    if (tiles < 200) return launch_ns<1, 64>(q, kTiles[2], s);
+    if (tiles < 700) return launch_ns<2, 128>(q, kTiles[3], s);
+    if (q.batch > 1) return launch_ns<2, 256>(q, kTiles[0], s);
     for (int phase = 0; phase < 3 * q.steps; ++phase) {
         const int step = phase / 3, k = phase % 3;
         const int set = k == 0 ? step & 1 : k == 1 ? 2 : phase == 3 * q.steps - 1 ? 5 : 3 + (step & 1);
@@ -478,8 +491,17 @@ int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float
     plan.base = base;
     plan.l = l;
     plan.o = p.o;
+    plan.direct = p.o.vec && p.o.dtype == CSRT_DT_BF16;
     plan.ws = ws;
-    return ns_products(plan, s);
+    rc = ns_products(plan, s);
+    if (rc != CSRT_OK || plan.direct) return rc;
+    const __half *hi = reinterpret_cast<const __half *>(base + (steps % 2 ? l.x1 : l.x0));
+    const unsigned gx = (unsigned)imin<int64_t>(ceil_div<int64_t>(cols, 256), 1024);
+    const unsigned gy = (unsigned)imin<int64_t>(rows, imax<int64_t>(1, imin<int64_t>(65535, (int64_t)num_sms() * 64 / gx)));
+    launch_pdl(ortho_result_kernel, dim3(gx, gy, (unsigned)batch), dim3(256), 0, s, hi, reinterpret_cast<const __half *>(base + l.lo),
+               l.ldx, rows, cols, scale * kInvXScale, p.o);
+    count_launch();
+    return check_launch("ortho_result_kernel");
 }
 
 }  // extern "C"

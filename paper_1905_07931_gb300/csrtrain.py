@@ -132,14 +132,15 @@ def _check(rc: int, what: str):
 
 
 # The current stream's handle without building a Stream object (3 us a call); the fallback is for torch builds
-# without the accessor.
+# without the accessors.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _stream(stream):
     if stream is None:
-        if _raw_stream is not None:
-            return c_void_p(_raw_stream(torch.cuda.current_device()))
+        if _raw_stream is not None and _raw_device is not None:
+            return c_void_p(_raw_stream(_raw_device()))
         stream = torch.cuda.current_stream()
     return c_void_p(stream.cuda_stream)
 
@@ -232,11 +233,8 @@ class Workspace:
     def _init(self, nbytes, device, stream):
         self.nbytes = int(nbytes)
         self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        self.ptr = _ptr(self.buf)
         _check(lib().csrt_workspace_init(_ptr(self.buf), self.nbytes, _stream(stream)), "csrt_workspace_init")
-
-    @property
-    def ptr(self):
-        return _ptr(self.buf)
 
     def status(self, stream=None):
         flags, req = c_int32(0), c_int64(0)

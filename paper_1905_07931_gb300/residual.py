@@ -128,8 +128,8 @@ def main(argv=None):
     ap.add_argument("--classes", type=int, default=10)
     ap.add_argument("--batch", type=int, default=256)
     ap.add_argument("--steps", type=int, default=60)
-    ap.add_argument("--eta", type=float, default=0.02)
-    ap.add_argument("--lam", type=float, default=0.05)
+    ap.add_argument("--eta", type=float, default=0.003)
+    ap.add_argument("--lam", type=float, default=0.1)
     ap.add_argument("--seed", type=int, default=0)
     a = ap.parse_args(argv)
     net = ResidualNet(a.features, a.hidden, a.blocks, a.classes, a.batch, seed=a.seed)
