@@ -4,8 +4,10 @@
 // A warp takes two rows of W (or, where there are few rows, a share of two rows' K: the block's warps then join in
 // shared memory). Per step each lane loads 16 bytes of either row and the 8 n values of x that belong to them - x is
 // K x n with the tokens contiguous, so they are consecutive too, and all warps of an SM find them in L1 - and runs
-// 16 n float32 FMAs. Bound by HBM: 4096 x 4096 at n = 1 reads 33.6 MB. Two rows per warp halve the x traffic in L1
-// and double the loads in flight.
+// 16 n float32 FMAs. Bound by the stream: 4096 x 4096 at n = 1 reads 33.6 MB in 7.4 us (4.5 TB/s with the launch; 5.0 us
+// at the measured copy rate), 4096 x 9216 75.5 MB in 13.8 us. Two rows per warp halve the x traffic in L1 and double the
+// loads in flight: one row takes 8.0 and 15.3 us, four rows 7.3 and 13.7 but 3.7 instead of 2.8 us on 300 x 784. Above
+// four tokens the float32 FMAs (n per weight) no longer fit beside the stream and the tensor cores take over.
 #include "gemm16.cuh"
 #include "dense_tokens.cuh"
 
@@ -33,7 +35,7 @@ __global__ void __launch_bounds__(kTokWarps * 32) dense_tokens_kernel(const __gr
         for (int r = 0; r < kTokRows; ++r) w[r] = a.w + (int64_t)min(row0 + r, a.m - 1) * a.ldw;
         if constexpr (VEC) {
             const int steps = a.k / 8;   // k % 8 == 0 here
-#pragma unroll 4
+#pragma unroll 8
             for (int t = part * 32 + lane; t < steps; t += a.wpr * 32) {
                 uint4 u[kTokRows];
 #pragma unroll
@@ -67,7 +69,7 @@ __global__ void __launch_bounds__(kTokWarps * 32) dense_tokens_kernel(const __gr
                 }
             }
         } else {
-#pragma unroll 4
+#pragma unroll 8
             for (int t = part * 32 + lane; t < a.k; t += a.wpr * 32) {
                 float xf[N];
 #pragma unroll
@@ -117,10 +119,11 @@ static void launch_tokens(const TokenArgs &a, bool f16, unsigned grid, cudaStrea
 }
 
 int dense_tokens(TokenArgs a, int n, bool f16, bool vec, cudaStream_t s) {
-    // enough warps to fill the SMs: up to eight share two rows, as long as each keeps a few steps of K
+    // 48 warps an SM where the rows do not give them (24 leave 8.3 us for 4096 x 4096): up to eight warps share two
+    // rows, as long as each keeps a few steps of K
     const int64_t pairs = ceil_div<int64_t>(a.m, kTokRows);
     a.wpr = 1;
-    while (a.wpr < kTokWarps && pairs * a.wpr < (int64_t)num_sms() * 24 && a.k / (a.wpr * 2) >= 512) a.wpr *= 2;
+    while (a.wpr < kTokWarps && pairs * a.wpr < (int64_t)num_sms() * 48 && a.k / (a.wpr * 2) >= 512) a.wpr *= 2;
     const unsigned grid = (unsigned)ceil_div<int64_t>(pairs, kTokWarps / a.wpr);
     switch (n) {
         case 1: vec ? launch_tokens<1, true>(a, f16, grid, s) : launch_tokens<1, false>(a, f16, grid, s); break;
