@@ -321,9 +321,9 @@ int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, 
             t.batch = 1;
             const GChoice c = choose_tile(t, n);
             const int64_t units = ceil_div<int64_t>(m, 128 * kTiles[c.tile].cg) * ceil_div<int64_t>(k, kTiles[c.tile].bn) *
-                                  c.splits * kTiles[c.tile].cg;
+                                  c.split.splits * kTiles[c.tile].cg;
             const double us = (double)m * n * 2 / (2.0 * imin<int64_t>(units, num_sms()) * 3000.0);
-            along = us <= imax(c.us, 4.0);
+            along = us <= imax(c.split.us, 4.0);
         }
         if (along) {
             a.sum_src = p;

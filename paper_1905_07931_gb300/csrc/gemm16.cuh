@@ -23,7 +23,8 @@
 // Float32 outputs therefore take the accumulator out every kPromoteKb stages (512 terms) and add it, rounded to
 // nearest, to float32 sums in the epilogue warps' registers (PROMOTE); 16-bit outputs do not need it.
 //
-// Splits: each slice's warp leaves its float32 partial tile in the workspace and counts in; the last one adds the
+// Splits: where tiles are few, or where the tiles left over after whole waves are (GArgs::whole), a tile's reduction is
+// shared. Each slice's warp leaves its float32 partial tile in the workspace and counts in; the last one adds the
 // slices in slice order (one order whatever the timing, so results repeat bit for bit) and runs the epilogue.
 //
 // GEN = false is the kernel for aligned matrices (16-bit outputs, float32 ones with PROMOTE), without the code that
@@ -71,8 +72,8 @@ struct GMat {
 struct GArgs {
     int32_t m, n, kb, batch;          // output size, stages of the reduction, matrices
     int32_t tiles_m, tiles_n;
-    int32_t units;                    // work units per launch (tiles x splits x batch)
-    int32_t splits, kb_split;
+    int32_t units;                    // work units per launch: `whole` tiles, then the others in `splits` slices each
+    int32_t whole, splits, kb_split;  // (splits == 1: whole is not used)
     int32_t a_mn, b_mn;               // operand stored MN-major
     int32_t slots;                    // 32-column groups that an epilogue warp can have in staging: 1 or 2
     int32_t f16;                      // operands and 16-bit epilogue tensors are float16 (else bfloat16)
@@ -547,7 +548,8 @@ __device__ __forceinline__ float warp_row_sum(const uint16_t *p, int cols, bool 
 // Work units
 // ---------------------------------------------------------------------------
 struct GUnit {
-    int b, tm, tn, split, kb0, kb1, tile;
+    int b, tm, tn, kb0, kb1;
+    int splits, split, tile;   // slices of its tile, its own one, and the tile's number among the split ones
 };
 
 // Unit u: batch matrix, tile and slice. Tiles run down bands of eight tile rows, so that the units in flight share
@@ -558,12 +560,14 @@ __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
     GUnit r;
     const int tiles = a.sym ? a.tiles_m * a.tiles_n - R * (a.tiles_m * (a.tiles_m - 1) / 2) : a.tiles_m * a.tiles_n;
     int t = u;
-    r.split = 0;
-    if (a.splits > 1) {
-        t = u / a.splits;
-        r.split = u - t * a.splits;
+    r.splits = 1;
+    r.split = r.tile = 0;
+    if (a.splits > 1 && u >= a.whole) {
+        r.splits = a.splits;
+        r.tile = (u - a.whole) / a.splits;
+        r.split = u - a.whole - r.tile * a.splits;
+        t = a.whole + r.tile;
     }
-    r.tile = t;
     r.b = a.batch > 1 ? t / tiles : 0;
     int q = t - r.b * tiles;
     if (a.sym) {
@@ -579,8 +583,8 @@ __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
         r.tn = rows == kBand ? q / kBand : q / rows;
         r.tm = first + q - r.tn * rows;
     }
-    r.kb0 = r.split * a.kb_split;
-    r.kb1 = min(a.kb, r.kb0 + a.kb_split);
+    r.kb0 = r.splits > 1 ? r.split * a.kb_split : 0;
+    r.kb1 = r.splits > 1 ? min(a.kb, r.kb0 + a.kb_split) : a.kb;
     return r;
 }
 
@@ -1085,7 +1089,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                 if (by_col) dj = diag_ahead(a, w.b, n0 + ci * 32 + lane, imin(a.n, a.s_pad));
             };
             if (NS) di = diag_ahead(a, w.b, row, imin(a.m, a.s_pad));
-            if (a.splits == 1) fetch(half);
+            if (w.splits == 1) fetch(half);
             bool ok = true;
             uint32_t d = 0;
             float sums[PROMOTE ? kChunks / 2 : 1][32];
@@ -1136,19 +1140,19 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             bool last = true;
             const int64_t slab = 128 * BN;
             float *part = nullptr;
-            if (a.splits > 1) part = a.partial + ((int64_t)w.tile * a.splits * CG + rank) * slab + (q * 32 + lane) * 4;
+            if (w.splits > 1) part = a.partial + ((int64_t)w.tile * w.splits * CG + rank) * slab + (q * 32 + lane) * 4;
 #pragma unroll 1
             for (int pass = 0; pass < 2; ++pass) {
                 // pass 0: this unit's sums (to the epilogue, or to its slab); pass 1: the slices joined
                 if (pass == 1) {
-                    if (a.splits == 1) break;
+                    if (w.splits == 1) break;
                     __threadfence();
                     __syncwarp();
                     int n_in = 0;
                     int32_t *cnt = a.counters + ((int64_t)w.tile * CG + rank) * kGEpiWarps + (warp - 4);
                     if (lane == 0) n_in = atomicAdd(cnt, 1);
                     n_in = __shfl_sync(0xffffffffu, n_in, 0);
-                    last = n_in == a.splits - 1;
+                    last = n_in == w.splits - 1;
                     if (!last) break;
                     if (lane == 0) *cnt = 0;
                     __threadfence();
@@ -1171,7 +1175,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                                              : "memory");
                             ++j;
                         }
-                        if (a.splits > 1) {
+                        if (w.splits > 1) {
                             float *p = part + (int64_t)w.split * CG * slab + (int64_t)ci * 32 * 128;
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
@@ -1182,9 +1186,9 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0.f;
-                        for (int sl = 0; sl < a.splits; sl += 2) {   // two slices' loads in flight
+                        for (int sl = 0; sl < w.splits; sl += 2) {   // two slices' loads in flight
                             const float *p = part + (int64_t)sl * CG * slab + (int64_t)ci * 32 * 128;
-                            const bool two = sl + 1 < a.splits;
+                            const bool two = sl + 1 < w.splits;
                             float4 f[8], g[8];
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {

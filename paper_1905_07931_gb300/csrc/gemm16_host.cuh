@@ -74,7 +74,7 @@ int fill_set(const GProduct &p, GArgs &a, GMaps &maps) {
     a.kb_split = ceil_div<int32_t>(imax(a.kb, 1), a.splits);
     a.splits = ceil_div<int32_t>(imax(a.kb, 1), a.kb_split);
     CSRT_ARG(tiles * a.splits < ((int64_t)1 << 31), "product too large");
-    a.units = (int32_t)(tiles * a.splits);
+    a.units = (int32_t)(a.splits == 1 ? tiles : a.whole + (tiles - a.whole) * a.splits);
     // an empty reduction loads nothing; its maps still have to be valid, so they are left out
     if (a.kb > 0 && (!operand_map(&maps.a, p.a, p.a_mn, 128, dtype, a.batch) ||
                      !operand_map(&maps.b, p.b, p.b_mn, BN / CG, dtype, a.batch)))
@@ -112,32 +112,39 @@ struct GTile {
 };
 constexpr int kTileKinds = 4;
 constexpr GTile kTiles[kTileKinds] = {{2, 256, 0.34, 5.7}, {1, 128, 0.245, 4.3}, {1, 64, 0.206, 3.6}, {2, 128, 0.228, 4.4}};
-inline double model_us(const GTile &t, int64_t tiles, int64_t kb, int64_t splits) {
+inline double model_us(const GTile &t, int64_t tiles, int64_t kb, int64_t whole, int64_t splits) {
     const int64_t slots = imax(1, num_sms() / t.cg);
-    const int64_t units = tiles * splits, waves = ceil_div(units, slots);
-    const double unit = (double)ceil_div(imax<int64_t>(kb, 1), splits) * t.stage;
-    double us = waves * (unit > t.epi ? unit : t.epi) + t.epi - 1.75;
+    const double tile = (double)imax<int64_t>(kb, 1) * t.stage;
+    double us = t.epi - 1.75;
+    if (whole > 0) us += ceil_div(whole, slots) * (tile > t.epi ? tile : t.epi);
+    if (tiles > whole) {
+        const double unit = (double)ceil_div(imax<int64_t>(kb, 1), splits) * t.stage;
+        us += ceil_div((tiles - whole) * splits, slots) * (unit > t.epi ? unit : t.epi);
+    }
     if (splits > 1) us += 3.9 + 0.446 * splits * t.bn / 64;
     return us;
 }
 
-// Best number of slices of a product on tiles t, and its time.
-inline int best_splits(const GTile &t, const GArgs &a, int64_t reduction, double *us) {
-    const int64_t kb = ceil_div<int64_t>(reduction, kGBK);
+// Best sharing of a product's reductions on tiles t, and its time: all tiles in one number of slices, or (tail) those
+// that are left over after whole waves.
+struct GSplit {
+    int whole, splits;
+    double us;
+};
+inline GSplit best_splits(const GTile &t, const GArgs &a, int64_t reduction, bool tail) {
+    const int64_t kb = ceil_div<int64_t>(reduction, kGBK), slots = imax(1, num_sms() / t.cg);
     const int64_t tiles = a.batch * tile_count(a.sym, ceil_div<int64_t>(a.m, 128 * t.cg), ceil_div<int64_t>(a.n, t.bn),
                                                128 * t.cg / t.bn);
-    const int64_t slots = imax(1, num_sms() / t.cg);
-    int best = 1;
-    *us = 1e30;
-    for (int64_t sp = 1; sp <= 32 && sp * 2 <= imax<int64_t>(kb, 2); ++sp) {
-        if (sp > 1 && ((size_t)(tiles * sp) * t.cg * 128 * t.bn * sizeof(float) > kPartialBytes ||
-                       tiles * t.cg * kGEpiWarps > (int64_t)kWsCounterInts))
-            break;
-        if (sp > 1 && tiles * (sp - 1) >= 2 * slots) break;   // enough units already
-        const double v = model_us(t, tiles, kb, sp);
-        if (v < *us) {
-            *us = v;
-            best = (int)sp;
+    GSplit best = {0, 1, model_us(t, tiles, kb, 0, 1)};
+    const int64_t waves = tail && tiles < ((int64_t)1 << 30) ? tiles / slots : 0;
+    for (int64_t whole = 0; whole <= waves * slots; whole += imax<int64_t>(1, waves * slots)) {
+        const int64_t rest = tiles - whole;
+        for (int64_t sp = 2; sp <= 32 && sp * 2 <= kb && rest > 0 && rest * (sp - 1) < 2 * slots; ++sp) {
+            if ((size_t)(rest * sp) * t.cg * 128 * t.bn * sizeof(float) > kPartialBytes ||
+                rest * t.cg * kGEpiWarps > (int64_t)kWsCounterInts)
+                break;
+            const double us = model_us(t, tiles, kb, whole, sp);
+            if (us < best.us) best = {(int)whole, (int)sp, us};
         }
     }
     return best;
@@ -172,15 +179,14 @@ int launch_tile(const GProduct &p, const GArgs &a, cudaStream_t s) {
 
 // The tile and slices of a product by the model.
 struct GChoice {
-    int tile, splits;
-    double us;
+    int tile;
+    GSplit split;
 };
 inline GChoice choose_tile(const GArgs &a, int64_t reduction) {
-    GChoice best = {0, 1, 1e30};
+    GChoice best = {0, {0, 1, 1e30}};
     for (int c = 0; c < kTileKinds; ++c) {
-        double us;
-        const int sp = best_splits(kTiles[c], a, reduction, &us);
-        if (us < best.us) best = {c, sp, us};
+        const GSplit s = best_splits(kTiles[c], a, reduction, true);
+        if (s.us < best.split.us) best = {c, s};
     }
     return best;
 }
@@ -190,7 +196,8 @@ int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the dense products need a GPU with tcgen05");
     const GChoice choice = choose_tile(a, p.reduction);
     const int best = choice.tile;
-    a.splits = choice.splits;
+    a.whole = choice.split.whole;
+    a.splits = choice.split.splits;
     if (aligned_set(a, PROMOTE)) {
         if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, false>(p, a, s);
         if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, false>(p, a, s);

@@ -302,9 +302,8 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
         GProduct p;
         GArgs &a = n.args[set];
         ns_product(q, set, p, a);
-        double us;
         // slices of different matrices' phases would share their place in the workspace
-        a.splits = q.batch == 1 ? best_splits(tile, a, p.reduction, &us) : 1;
+        a.splits = q.batch == 1 ? best_splits(tile, a, p.reduction, false).splits : 1;
         const int rc = fill_set<CG, BN>(p, a, n.maps[set]);
         if (rc != CSRT_OK) return rc;
         units = imax(units, a.units);
