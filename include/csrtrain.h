@@ -399,8 +399,8 @@ int csrt_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols
  * bfloat16 each; momentum is float32, batch x rows x cols, contiguous, updated
  * in place. ||u||_F is summed in float64. The products run on float16
  * operands (11 significant bits; all matrices are scaled so that entries lie
- * within their bounds, as singular values stay below 1.21), X is carried with
- * 22 bits and sums are float32, so o is within about 1e-3 of the exact
+ * within their bounds, as singular values stay below 1.21), X and all sums are
+ * float32, so o is within about 1e-3 of the exact
  * iteration (2-norm, relative); where u has no component at all (fewer samples
  * than rows) what the first steps round grows with the iteration, 3.4 times a
  * step, and o may be a few 1e-3 off. A matrix holding an infinity or a NaN

@@ -55,10 +55,15 @@ constexpr int kGEpiWarps = 8;
 constexpr int kPromoteKb = 8;            // stages per tensor-memory accumulation of a float32 output
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kXScale = 32768.f, kInvXScale = 1.f / 32768.f;   // scale of X and A in float16; B's is half of it
-constexpr int kGStageOut = 4096;         // staging bytes of an epilogue warp
-
 enum { kEpiFwd = 0, kEpiBwd = 1, kEpiNs = 2 };
 enum { kNsGram = 0, kNsPoly = 1, kNsApply = 2 };   // the products of a Newton-Schulz step (GArgs::kind)
+
+// Staging bytes of an epilogue warp; kEpiNs has a float32 block and a float16 one in it.
+template <int EPI>
+constexpr int stage_out() {
+    return EPI == kEpiNs ? 6144 : 4096;
+}
+
 
 // An epilogue operand or output: row-major m x n, batch matrices `stride` elements apart.
 struct GMat {
@@ -75,7 +80,7 @@ struct GArgs {
     int32_t units;                    // work units per launch: `whole` tiles, then the others in `splits` slices each
     int32_t whole, splits, kb_split;  // (splits == 1: whole is not used)
     int32_t a_mn, b_mn;               // operand stored MN-major
-    int32_t slots;                    // 32-column groups that an epilogue warp can have in staging: 1 or 2
+    int32_t slots;                    // 32-column groups that an epilogue warp can have in staging: 1 or (dense) 2
     int32_t f16;                      // operands and 16-bit epilogue tensors are float16 (else bfloat16)
     // epilogue
     const float *bias;
@@ -89,8 +94,8 @@ struct GArgs {
     const float *diag_in;             // kEpiNs: diagonal of A (kNsPoly) or B (kNsApply), s_pad per matrix
     float *diag_out;                  // kEpiNs: diagonal of A (kNsGram) or B (kNsPoly)
     int32_t s_pad;
-    GMat c0, c1;                      // z_below / A / X high; residual / X low
-    GMat out0, out1;                  // y, dx, dW, A, B, X high, O; z, X low
+    GMat c0, c1;                      // z_below / A / X (float32); residual
+    GMat out0, out1;                  // y, dx, dW, A, B, X (float16), o; z, X (float32)
     float *partial;                   // split slices
     int32_t *counters;
     WsHeader *hdr;
@@ -508,16 +513,17 @@ __device__ __forceinline__ void put32_turned(const float (&v)[32], uint8_t *at) 
         *reinterpret_cast<__half *>(at + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2) = __float2half_rn(v[i]);
 }
 
-// The staged outputs leave: out0 from slot, out1 - or the mirrored block of out0 - from slot + 2048.
+// The staged outputs leave: out0 from at0, out1 - or the mirrored block of out0 - from at1.
 template <bool GEN>
-__device__ __forceinline__ void emit(const GArgs &a, const GMaps &maps, uint8_t *slot, int b, int row, int col, bool mirror) {
+__device__ __forceinline__ void emit(const GArgs &a, const GMaps &maps, const uint8_t *at0, const uint8_t *at1, int b, int row,
+                                     int col, bool mirror) {
     if (!GEN || a.out0.vec) {   // out1 likewise, if there is one
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if ((threadIdx.x & 31) == 0 && row < a.m && col < a.n) {   // lane 0's row is the block's first
-            tma_store_3d(&maps.out0, col, row, b, slot);
-            if (a.out1.p != nullptr) tma_store_3d(&maps.out1, col, row, b, slot + 2048);
-            if (mirror) tma_store_3d(&maps.out0, row, col, b, slot + 2048);
+            tma_store_3d(&maps.out0, col, row, b, at0);
+            if (a.out1.p != nullptr) tma_store_3d(&maps.out1, col, row, b, at1);
+            if (mirror) tma_store_3d(&maps.out0, row, col, b, at1);
         }
     }
 }
@@ -614,6 +620,27 @@ __device__ __forceinline__ GAhead ahead_of(const GMat &c, int b, int row0, int c
 #pragma unroll
     for (int i = 0; i < 4; ++i) g.rows |= (row0 + r + 8 * i < m ? 1u : 0u) << i;
     return g;
+}
+// The same for a padded float32 operand (kNsApply): eight lanes to a row of 128 bytes, four rows to an instruction.
+__device__ __forceinline__ GAhead ahead_of_f32(const GMat &c, int b, int row0, int col0, int m) {
+    const int lane = threadIdx.x & 31, r = lane >> 3;
+    GAhead g;
+    g.p = reinterpret_cast<const char *>(static_cast<const float *>(c.p) + b * c.stride + (int64_t)(row0 + r) * c.ld + col0 +
+                                         4 * (lane & 7));
+    g.step = 16 * c.ld;
+    g.lim = (int)c.ld - col0 - 4 * (lane & 7);
+    g.rows = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g.rows |= (row0 + r + 4 * i < m ? 1u : 0u) << i;
+    return g;
+}
+__device__ __forceinline__ void fetch_ahead_f32(uint4 (&u0)[4], uint4 (&u1)[4], const GAhead &g, int off) {
+    const char *p = g.p + 4 * off;
+    const uint32_t rows = off < g.lim ? g.rows : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ld_cg_if(u0[i], p + i * g.step, (rows >> i) & 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ld_cg_if(u1[i], p + (i + 4) * g.step, (rows >> (i + 4)) & 1);
 }
 __device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GAhead &g, int off) {
     if (g.p == nullptr) return;
@@ -796,31 +823,38 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
         }
         if (on_diag && row < a.m) a.diag_out[(int64_t)b * a.s_pad + row] = d;
     } else {
-        // (a + e) X + B X with the diagonal e of B by row (or by column where X has more rows than columns)
-        float c[32], t[32];
-        stage_in<GEN, false>(u0, a.c0, slot);
-        stage_in<GEN, WIDE>(u1, a.c1, slot + 2048);
+        // (a + e) X + B X with the diagonal e of B by row (or by column where X has more rows than columns). X is
+        // float32: it comes in at the slot's first 4 KB and leaves from there, the float16 operand of the next products
+        // (or o) from the 2 KB behind.
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3);
+            *reinterpret_cast<uint4 *>(slot + r * 128 + (((lane & 7) ^ (r & 7)) << 4)) = i < 4 ? u0[i & 3] : u1[i & 3];
+        }
         __syncwarp();
-        take32<GEN, false>(c, a.c0, b, row, col, a.m, a.n, slot, turn);
-        take32<GEN, WIDE>(t, a.c1, b, row, col, a.m, a.n, slot + 2048, turn);
+        float c[32];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 f = *reinterpret_cast<const float4 *>(slot + lane * 128 + ((i ^ (lane & 7)) << 4));
+            c[4 * i] = f.x, c[4 * i + 1] = f.y, c[4 * i + 2] = f.z, c[4 * i + 3] = f.w;
+        }
         if (a.tall) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-                v[i] = (a.alpha * v[i] + (kNsA + __shfl_sync(0xffffffffu, dj, i)) * (c[i] + t[i])) * a.gamma;
+                v[i] = (a.alpha * v[i] + (kNsA + __shfl_sync(0xffffffffu, dj, i)) * c[i]) * a.gamma;
         } else {
             const float e = kNsA + di;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = (a.alpha * v[i] + e * (c[i] + t[i])) * a.gamma;
+            for (int i = 0; i < 32; ++i) v[i] = (a.alpha * v[i] + e * c[i]) * a.gamma;
         }
-        if (a.out1.p != nullptr) {   // what float16 drops of X, kept beside it
-#pragma unroll
-            for (int i = 0; i < 32; ++i) t[i] = v[i] - __half2float(__float2half_rn(v[i]));
-            put32<GEN, false>(t, a.out1, slot + 2048, b, row, col, a.m, a.n);
-        }
+        if (a.out1.p != nullptr) put32<false, true>(v, a.out1, slot, b, row, col, a.m, a.n);
+        put32<false, false>(v, a.out0, slot + 4096, b, row, col, a.m, a.n);
+        emit<false>(a, maps, slot + 4096, slot, b, row, col, false);
+        return;
     }
     put32<GEN, WIDE>(v, a.out0, slot, b, row, col, a.m, a.n);
     if (EPI == kEpiNs && mirror) put32_turned(v, slot + 2048);
-    emit<GEN>(a, maps, slot, b, row, col, EPI == kEpiNs && mirror);
+    emit<GEN>(a, maps, slot, slot + 2048, b, row, col, EPI == kEpiNs && mirror);
 }
 
 // Units per matrix of the phases before `phase`, and this CTA's first unit of it.
@@ -839,13 +873,13 @@ template <int CG, int BN>
 constexpr int gstage_bytes() {
     return 128 * 128 + (BN / CG) * 128;
 }
-template <int CG, int BN>
+template <int CG, int BN, int EPI>
 constexpr int gstages() {
-    return (227 * 1024 - kGEpiWarps * kGStageOut - 2048) / gstage_bytes<CG, BN>();
+    return (227 * 1024 - kGEpiWarps * stage_out<EPI>() - 2048) / gstage_bytes<CG, BN>();
 }
-template <int CG, int BN>
+template <int CG, int BN, int EPI>
 constexpr int gsmem_bytes() {
-    return gstages<CG, BN>() * gstage_bytes<CG, BN>() + kGEpiWarps * kGStageOut + 1024 + 512;
+    return gstages<CG, BN, EPI>() * gstage_bytes<CG, BN>() + kGEpiWarps * stage_out<EPI>() + 1024 + 512;
 }
 
 template <int CG, int BN, int EPI, bool PROMOTE, bool GEN>
@@ -854,7 +888,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     static_assert(BN % 64 == 0 && BN / CG >= 64 && 2 * BN <= 512, "two accumulators in tensor memory");
     constexpr bool NS = EPI == kEpiNs;
     constexpr int R = 128 * CG / BN;                      // tile columns to a tile row (symmetric products)
-    constexpr int kStages = gstages<CG, BN>();
+    constexpr int kStages = gstages<CG, BN, EPI>();
     constexpr int kStageBytes = gstage_bytes<CG, BN>();
     constexpr int kABytes = 128 * 128;
     constexpr int kBRows = BN / CG;                       // columns of D whose B rows this CTA holds
@@ -863,7 +897,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *epi = smem + kStages * kStageBytes;
-    uint64_t *full = reinterpret_cast<uint64_t *>(epi + kGEpiWarps * kGStageOut);
+    uint64_t *full = reinterpret_cast<uint64_t *>(epi + kGEpiWarps * stage_out<EPI>());
     uint64_t *empty = full + kStages;
     uint64_t *accf = empty + kStages;    // [2] accumulator ready
     uint64_t *acce = accf + 2;           // [2] accumulator drained
@@ -1048,7 +1082,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int q = warp & 3, half = (warp - 4) >> 2;
-        uint8_t *stage0 = epi + (warp - 4) * kGStageOut;
+        uint8_t *stage0 = epi + (warp - 4) * stage_out<EPI>();
         uint32_t acce_bar[2] = {smem_u32(acce), smem_u32(acce + 1)};
         if constexpr (CG == 2) {
             acce_bar[0] = mapa_u32(acce_bar[0], 0);
@@ -1074,17 +1108,23 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             const bool empty_sum = w.kb1 <= w.kb0;
             GAhead g0 = {}, g1 = {};
             if constexpr (!GEN) {
-                g0 = ahead_of<false>(a.c0, w.b, row - lane, n0, a.m, a.n);
-                g1 = ahead_of<PROMOTE>(a.c1, w.b, row - lane, n0, a.m, a.n);
+                if (NS && a.kind == kNsApply) {
+                    g0 = ahead_of_f32(a.c0, w.b, row - lane, n0, a.m);
+                } else {
+                    g0 = ahead_of<false>(a.c0, w.b, row - lane, n0, a.m, a.n);
+                    g1 = ahead_of<PROMOTE>(a.c1, w.b, row - lane, n0, a.m, a.n);
+                }
             }
             const bool by_col = NS && (a.kind == kNsPoly || a.tall);
             auto fetch = [&](int ci) {   // the operands of the 32 columns n0 + 32 ci ..
                 if constexpr (GEN) {
                     fetch_ahead<GEN, false>(u0, a.c0, w.b, row - lane, n0 + ci * 32, a.m, a.n);
                     fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, n0 + ci * 32, a.m, a.n);
+                } else if (NS && a.kind == kNsApply) {
+                    fetch_ahead_f32(u0, u1, g0, ci * 32);
                 } else {
                     fetch_ahead(u0, g0, ci * 32);
-                    fetch_ahead(u1, g1, ci * 32);
+                    if (!NS) fetch_ahead(u1, g1, ci * 32);
                 }
                 if (by_col) dj = diag_ahead(a, w.b, n0 + ci * 32 + lane, imin(a.n, a.s_pad));
             };
@@ -1213,7 +1253,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     }
                     __syncwarp();
-                    epilogue32<EPI, GEN, PROMOTE>(v, u0, u1, di, dj, a, maps, stage0 + slot * (kGStageOut / 2), w.b, row, col,
+                    epilogue32<EPI, GEN, PROMOTE>(v, u0, u1, di, dj, a, maps, stage0 + slot * (stage_out<EPI>() / 2), w.b, row, col,
                                                   NS && a.sym && w.tn >= R * (w.tm + 1));
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     slot = a.slots == 2 ? slot ^ 1 : 0;

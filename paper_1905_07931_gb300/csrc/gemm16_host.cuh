@@ -61,7 +61,7 @@ inline bool out_map(CUtensorMap *map, const GMat &o, int m, int n, int batch) {
 }
 
 // Dimensions and maps of one product on CG x 128 x BN tiles.
-template <int CG, int BN>
+template <int CG, int BN, int EPI>
 int fill_set(const GProduct &p, GArgs &a, GMaps &maps) {
     const int dtype = a.f16 ? CSRT_DT_F16 : CSRT_DT_BF16;
     a.a_mn = p.a_mn;
@@ -86,7 +86,7 @@ int fill_set(const GProduct &p, GArgs &a, GMaps &maps) {
     // one aligned 16-bit output, at most one operand and none to turn: a group needs half the staging
     const bool turns = !a.out0.vec || (a.c0.p != nullptr && !a.c0.vec) || (a.c1.p != nullptr && !a.c1.vec);
     const bool two_in = a.c0.p != nullptr && a.c1.p != nullptr;
-    a.slots = a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !a.sym && !two_in && !turns ? 2 : 1;
+    a.slots = EPI != kEpiNs && a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !two_in && !turns ? 2 : 1;
     return CSRT_OK;
 }
 
@@ -165,10 +165,10 @@ int launch_tile(const GProduct &p, const GArgs &a, cudaStream_t s) {
     GLaunch<EPI> l = {};
     l.args[0] = a;
     l.phases = 1;
-    int rc = fill_set<CG, BN>(p, l.args[0], l.maps[0]);
+    int rc = fill_set<CG, BN, EPI>(p, l.args[0], l.maps[0]);
     if (rc != CSRT_OK) return rc;
     constexpr auto kernel = gemm16_kernel<CG, BN, EPI, PROMOTE, GEN>;
-    constexpr int smem = gsmem_bytes<CG, BN>();
+    constexpr int smem = gsmem_bytes<CG, BN, EPI>();
     rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
     const int grid = imin(l.args[0].units, imax(1, num_sms() / CG)) * CG;
@@ -198,13 +198,13 @@ int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
     const int best = choice.tile;
     a.whole = choice.split.whole;
     a.splits = choice.split.splits;
-    if (aligned_set(a, PROMOTE)) {
+    if (EPI == kEpiNs || aligned_set(a, PROMOTE)) {
         if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, false>(p, a, s);
         if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, false>(p, a, s);
         if (best == 3) return launch_tile<2, 128, EPI, PROMOTE, false>(p, a, s);
         return launch_tile<1, 64, EPI, PROMOTE, false>(p, a, s);
     }
-    if constexpr (EPI != kEpiNs) {   // (its matrices are the library's own, all aligned)
+    if constexpr (EPI != kEpiNs) {   // (whose matrices are the library's own, all aligned)
         if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, true>(p, a, s);
         if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, true>(p, a, s);
         if (best == 3) return launch_tile<2, 128, EPI, PROMOTE, true>(p, a, s);

@@ -9,9 +9,16 @@
 // Number formats. Singular values stay in [0, 1.203] (p(s) = a s + b s^3 + c s^5 maps [0, 1.203] into itself), so
 // every entry of X, A and B is bounded (1.203, 1.45, 2.81) and fits float16 once scaled by a power of two: X and A
 // are stored times 2^15, B times 2^14. float16 keeps 11 significant bits where bfloat16 keeps 8, at the same
-// tensor-core rate: bfloat16 operands alone would put o about 1e-2 off. X is carried as a float16 pair (high part,
-// the operand of the products, and low part, 22 bits together), so that the term a X - all there is for the small
-// singular values - does not gather a rounding per step.
+// tensor-core rate: bfloat16 operands alone would put o about 1e-2 off. X itself is carried in float32 (times 2^15) beside
+// its float16 copy, so that the term a X - all there is for the small singular values - does not gather a rounding per
+// step. The diagonals of A and B are kept apart, in float32: near convergence they hold nearly all of A and B, whose
+// rounding would otherwise be the largest error of o (a bfloat16 o was 2.2e-3 to 2.8e-3 off with them inside, and is
+// 1.7e-3 off now, its own rounding).
+//
+// What bounds it (measured, whole calls): 4096 x 9216 takes 2.0 ms for 2.66 TFLOP of necessary work (1.4 ms at the library's
+// rate): its products run at 1.5 to 1.65 PFLOP/s with waves 90% full, the two passes over gradient and momentum take
+// 0.14 ms at HBM rate. Smaller ones are bound by latency: a product costs at least 4 us - operands from L2, the epilogue's
+// own, the release to the other SMs - so fifteen of them 60 to 75 us, whatever the size (a 64 x 64 matrix: 60 us).
 //
 // The Frobenius norm is summed in float64 over float32 sums of eight squares; a sum out of float32's safe range is
 // taken again in float64, so that neither tiny nor huge gradients lose it.
@@ -30,7 +37,8 @@ struct PrepArgs {
     float beta, eps, scale;
     int32_t nesterov, rows, cols, vec;
     double *partial;        // [batch][gridDim.x]
-    __half *hi, *lo;        // X, or
+    __half *hi;             // X, its float16 copy
+    float *x;               // and itself, or
     GMat o;                 // with no steps: the normalised direction itself
     int64_t ldx;
     int32_t direct;
@@ -126,7 +134,7 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_momentum_kernel(PrepArgs a
     if (threadIdx.x == 0) a.partial[(int64_t)b * gridDim.x + blockIdx.x] = sum;
 }
 
-// Second pass: X = u / max(||u||_F, eps) as the scaled float16 pair.
+// Second pass: X = u / max(||u||_F, eps), scaled, in float32 and float16.
 __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
     pdl_enter();
     const int b = blockIdx.y;
@@ -150,23 +158,21 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
                 store1(a.o.p, b * a.o.stride + (int64_t)r * a.o.ld + c + i, u[i], a.o.dtype);
             continue;
         }
-        uint32_t h[4], l[4];
+        uint32_t h[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[i] = pack16(u[2 * i], u[2 * i + 1], true);
-            const float2 back = unpack16(h[i], true);
-            l[i] = pack16(u[2 * i] - back.x, u[2 * i + 1] - back.y, true);
-        }
+        for (int i = 0; i < 4; ++i) h[i] = pack16(u[2 * i], u[2 * i + 1], true);
         // rows are padded to a multiple of eight, so the tail of a row may be written whole
         const int64_t xi = ((int64_t)b * a.rows + r) * a.ldx + c;
         *reinterpret_cast<uint4 *>(a.hi + xi) = make_uint4(h[0], h[1], h[2], h[3]);
-        *reinterpret_cast<uint4 *>(a.lo + xi) = make_uint4(l[0], l[1], l[2], l[3]);
+        float4 *x = reinterpret_cast<float4 *>(a.x + xi);
+        x[0] = make_float4(u[0], u[1], u[2], u[3]);
+        x[1] = make_float4(u[4], u[5], u[6], u[7]);
     }
 }
 
 struct OrthoLayout {
     int64_t ldx, lds;
-    size_t slices, done, partial, x0, x1, lo, a, b, diag_a, diag_b, total;   // offsets after the reserved part
+    size_t slices, done, partial, x0, x1, xf, a, b, diag_a, diag_b, total;   // offsets after the reserved part
 };
 
 static OrthoLayout layout(int64_t batch, int64_t rows, int64_t cols) {
@@ -186,7 +192,7 @@ static OrthoLayout layout(int64_t batch, int64_t rows, int64_t cols) {
     l.partial = take(batch * kPrepBlocks * (int64_t)sizeof(double));
     l.x0 = take(batch * rows * l.ldx * 2);
     l.x1 = take(batch * rows * l.ldx * 2);
-    l.lo = take(batch * rows * l.ldx * 2);
+    l.xf = take(batch * rows * l.ldx * 4);
     l.a = take(batch * s * l.lds * 2);
     l.b = take(batch * s * l.lds * 2);
     l.diag_a = take(batch * l.lds * 4);
@@ -205,15 +211,14 @@ struct NsPlan {
     void *ws;
 };
 
-// o = scale X from the float16 pair, for results that the products' epilogue does not write itself.
-__global__ void ortho_result_kernel(const __half *__restrict__ hi, const __half *__restrict__ lo, int64_t ldx, int32_t rows,
-                                    int32_t cols, float scale, GMat o) {
+// o = scale X, for results that the products' epilogue does not write itself.
+__global__ void ortho_result_kernel(const float *__restrict__ x, int64_t ldx, int32_t rows, int32_t cols, float scale, GMat o) {
     pdl_enter();
     const int64_t b = blockIdx.z;
     for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
         for (int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; c < cols; c += (int64_t)gridDim.x * blockDim.x) {
             const int64_t i = (b * rows + r) * ldx + c;
-            store1(o.p, b * o.stride + r * o.ld + c, scale * (__half2float(hi[i]) + __half2float(lo[i])), o.dtype);
+            store1(o.p, b * o.stride + r * o.ld + c, scale * x[i], o.dtype);
         }
 }
 
@@ -286,10 +291,10 @@ static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
         const bool out = set == 5 && q.direct;
         a.gamma = out ? q.scale * kInvXScale : 1.f;
         a.diag_in = diag_b;
-        a.c0 = mat(x, l.ldx, q.rows);
-        a.c1 = mat(l.lo, l.ldx, q.rows);
+        a.c0 = mat(l.xf, l.ldx, q.rows);
+        a.c0.dtype = CSRT_DT_F32;
         a.out0 = out ? q.o : mat(x == l.x0 ? l.x1 : l.x0, l.ldx, q.rows);
-        if (!out) a.out1 = mat(l.lo, l.ldx, q.rows);
+        if (!out) a.out1 = a.c0;
     }
 }
 
@@ -304,7 +309,7 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
         ns_product(q, set, p, a);
         // slices of different matrices' phases would share their place in the workspace
         a.splits = q.batch == 1 ? best_splits(tile, a, p.reduction, false).splits : 1;
-        const int rc = fill_set<CG, BN>(p, a, n.maps[set]);
+        const int rc = fill_set<CG, BN, kEpiNs>(p, a, n.maps[set]);
         if (rc != CSRT_OK) return rc;
         units = imax(units, a.units);
     }
@@ -315,7 +320,7 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     n.step_units[2] = n.args[3].units / q.batch;
 
     constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false, false>;
-    constexpr int smem = gsmem_bytes<CG, BN>();
+    constexpr int smem = gsmem_bytes<CG, BN, kEpiNs>();
     const int rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
     // CTAs (or pairs) that the GPU can hold at once: all of them have to be there, as units wait for one another
@@ -362,11 +367,11 @@ static int ns_products(const NsPlan &q, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the orthogonalisation needs a GPU with tcgen05");
     // By the number of 128 x 128 tiles of X (measured, us for the whole call on tiles 64, 128 by pairs and 256 by pairs
     // wide in one launch, and on launches of their own): few tiles take the narrow ones, which share the work among
-    // more SMs (1024 x 1024: 127 / 155 / 230, 140; 3 x 2048 x 512: 160 / 182 / 249, 200); from 200 tiles on pairs of SMs
-    // on 256 x 128 (2048 x 2048: 351 / 257 / 315, 282; 6 x 256 x 4096: 240 / 220 / 281, 249); from 700 on, where L2
+    // more SMs (1024 x 1024: 124 / 148 / 220, 140; 3 x 2048 x 512: 154 / 175 / 241, 200); from 200 tiles on pairs of SMs
+    // on 256 x 128 (2048 x 2048: 334 / 249 / 307, 282; 6 x 256 x 4096: 228 / 206 / 271, 249); from 700 on, where L2
     // traffic counts most, 256 x 256: in one launch for several matrices, which fill each other's gaps
-    // (3 x 2048 x 2048: 782 / 487 / 447, 606), and for a single one a launch for each product, on its best tile
-    // (4096 x 4096: 1912 / 1184 / 1003, 999; 4096 x 9216: 3390 / 2323 / 1937, 1793).
+    // (3 x 2048 x 2048: 758 / 484 / 444, 606), and for a single one a launch for each product, on its best tile
+    // (4096 x 4096: 1857 / 1216 / 1065, 1034; 4096 x 9216: 3398 / 2346 / 1982, 1890).
     const int64_t tiles = (int64_t)q.batch * ceil_div<int64_t>(q.rows, 128) * ceil_div<int64_t>(q.cols, 128);
     if (tiles < 200) return launch_ns<1, 64>(q, kTiles[2], s);
     if (tiles < 700) return launch_ns<2, 128>(q, kTiles[3], s);
@@ -462,7 +467,7 @@ int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float
             (reinterpret_cast<uintptr_t>(momentum) & 15) == 0;
     p.partial = reinterpret_cast<double *>(base + l.partial);
     p.hi = reinterpret_cast<__half *>(base + l.x0);
-    p.lo = reinterpret_cast<__half *>(base + l.lo);
+    p.x = reinterpret_cast<float *>(base + l.xf);
     p.ldx = l.ldx;
     p.done = reinterpret_cast<uint32_t *>(base + l.done);
     p.direct = steps == 0;
@@ -494,11 +499,10 @@ int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float
     plan.ws = ws;
     rc = ns_products(plan, s);
     if (rc != CSRT_OK || plan.direct) return rc;
-    const __half *hi = reinterpret_cast<const __half *>(base + (steps % 2 ? l.x1 : l.x0));
     const unsigned gx = (unsigned)imin<int64_t>(ceil_div<int64_t>(cols, 256), 1024);
     const unsigned gy = (unsigned)imin<int64_t>(rows, imax<int64_t>(1, imin<int64_t>(65535, (int64_t)num_sms() * 64 / gx)));
-    launch_pdl(ortho_result_kernel, dim3(gx, gy, (unsigned)batch), dim3(256), 0, s, hi, reinterpret_cast<const __half *>(base + l.lo),
-               l.ldx, rows, cols, scale * kInvXScale, p.o);
+    launch_pdl(ortho_result_kernel, dim3(gx, gy, (unsigned)batch), dim3(256), 0, s,
+               reinterpret_cast<const float *>(base + l.xf), l.ldx, rows, cols, scale * kInvXScale, p.o);
     count_launch();
     return check_launch("ortho_result_kernel");
 }
