@@ -343,7 +343,8 @@ typedef struct csrt_mat {
 
 /* Bytes of workspace of the dense-layer calls on a layer of m outputs and k
  * inputs with at most max_n columns. Initialise with csrt_workspace_init; the
- * status word works as for the other calls. Host only. */
+ * status word works as for the other calls, and a workspace that reported
+ * CSRT_DEV_TIMEOUT is initialised again before its next use. Host only. */
 int csrt_dense_workspace_bytes(int32_t m, int32_t k, int32_t max_n, size_t *bytes);
 
 /* csrt_dense_fwd -- y = act(W x + bias) + residual, one rounding at the end.

@@ -1279,6 +1279,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
     }
+    if (s_abort)   // copies that nothing waits for any more land before the shared memory goes
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if constexpr (CG == 2) cluster_sync_all();

@@ -331,3 +331,44 @@ def test_binding_refuses(C):
     with pytest.raises(C.CsrtError, match="workspace has"):
         C.dense_fwd(torch.zeros(4096, 16, dtype=torch.bfloat16, device="cuda"), x,
                     torch.zeros(4096, 4, dtype=torch.bfloat16, device="cuda"), ws)
+
+
+@pytest.mark.parametrize("m,k,n", [(96, 72, 40), (70, 40, 3), (130, 33, 1), (200, 160, 136)])
+@pytest.mark.parametrize("odd", [0, 3])
+def test_rows_far_apart(C, m, k, n, odd):
+    """Matrices whose last row lies past 2^31 elements give the bits of the same rows close together."""
+    gen = _gen(m + k + n + odd)
+    bufs = []
+
+    def pair(rows, cols, dt):
+        close = (cols + 63) // 64 * 64 + odd
+        far = (2 ** 31 // (rows - 1) // 64 + 1) * 64 + odd
+        out = []
+        v = torch.randn(rows, cols, generator=gen, device="cuda").to(dt)
+        for ld in (close, far):
+            buf = torch.empty(odd + (rows - 1) * ld + cols, dtype=dt, device="cuda")
+            bufs.append(buf)
+            out.append(buf.as_strided((rows, cols), (ld, 1), odd))
+            out[-1].copy_(v)
+        return out
+
+    ws = C.DenseWorkspace(m, k, n)
+    bias = torch.randn(m, generator=gen, device="cuda")
+    bf, f32 = torch.bfloat16, torch.float32
+    w, x, r, z, y = pair(m, k, bf), pair(k, n, bf), pair(m, n, bf), pair(m, n, bf), pair(m, n, bf)
+    for i in range(2):
+        C.dense_fwd(w[i], x[i], y[i], ws, bias=bias, act="gelu", residual=r[i], z=z[i])
+    assert torch.equal(y[0], y[1]) and torch.equal(z[0], z[1])
+    del r
+    bufs.clear()
+    dx, dw, zb = pair(k, n, bf), pair(m, k, f32), pair(k, n, bf)
+    db = torch.zeros(2, m, device="cuda")
+    for i in range(2):
+        C.dense_bwd_x(w[i], z[i], dx[i], ws, z_below=zb[i], act="silu")
+        C.dense_bwd_w(z[i], x[i], dw[i], ws, db=db[i], accumulate=True)
+    assert torch.equal(dx[0], dx[1]) and torch.equal(dw[0], dw[1]) and torch.equal(db[0], db[1])
+    w16 = pair(m, k, bf)
+    for i in range(2):
+        C.dense_update(dw[i], w[i], 0.1, 0.01, w16[i])
+        C.dense_act_bwd(z[i], x[i] if m == k else z[i], "gelu", y[i])
+    assert torch.equal(dw[0], dw[1]) and torch.equal(w16[0], w16[1]) and torch.equal(y[0], y[1])

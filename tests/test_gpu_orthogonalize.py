@@ -258,3 +258,22 @@ def test_residual_net_gradients_and_training(C):
     for _ in range(20):
         last = float(net.step(0.02, 0.05)[0].item())
     assert last < 0.7 * first and net.status() == 0
+
+
+@pytest.mark.parametrize("m,k", [(96, 160), (65, 33)])
+@pytest.mark.parametrize("odt", [torch.float32, torch.bfloat16])
+def test_matrices_far_apart(C, m, k, odt):
+    """A batch whose second matrix lies past 2^31 elements gives the bits of the same matrices close together."""
+    gen = _gen(m + k)
+    far = 2 ** 31 + 64
+    g = torch.randn(2, m, k, generator=gen, device="cuda")
+    bg = torch.empty(far + m * k, device="cuda")
+    bo = torch.empty(far + m * k, dtype=odt, device="cuda")
+    gf, of = bg.as_strided((2, m, k), (far, k, 1)), bo.as_strided((2, m, k), (far, k, 1))
+    gf.copy_(g)
+    o = torch.empty(2, m, k, dtype=odt, device="cuda")
+    ws = C.OrthogonalizeWorkspace(2, m, k)
+    ma, mb = torch.zeros(2, m, k, device="cuda"), torch.zeros(2, m, k, device="cuda")
+    C.orthogonalize(g, o, ws, momentum=ma)
+    C.orthogonalize(gf, of, ws, momentum=mb)
+    assert torch.equal(o, of) and torch.equal(ma, mb)
