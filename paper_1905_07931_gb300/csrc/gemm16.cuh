@@ -36,7 +36,8 @@
 // instead of 160 us for the promoted sums. 256 x 256 tiles by pairs of SMs halve the operand traffic through L2 of 128 x
 // 128 tiles, which bounds those at about 1.3 PFLOP/s; products too small for a wave of them take 256 x 128, 128 x 128 or
 // 128 x 64 tiles and slices (gemm16_host.cuh). Short reductions are bound by the epilogue: a 128 x 256 share of a tile
-// takes 5 us in it (4096 x 9216 from 256 columns, 151 MB of float32: 44 us, 22 at the measured copy rate).
+// takes 5 us in it (4096 x 9216 from 256 columns, 151 MB of float32: 41 us, 22 at the measured copy rate; added to
+// what is there 83, 45).
 //
 // Every wait is bounded: one that runs out sets the CTA's abort flag, the roles drain and meet, and the kernel ends
 // with CSRT_DEV_TIMEOUT in the status word.
@@ -58,10 +59,11 @@ constexpr float kXScale = 32768.f, kInvXScale = 1.f / 32768.f;   // scale of X a
 enum { kEpiFwd = 0, kEpiBwd = 1, kEpiNs = 2 };
 enum { kNsGram = 0, kNsPoly = 1, kNsApply = 2 };   // the products of a Newton-Schulz step (GArgs::kind)
 
-// Staging bytes of an epilogue warp; kEpiNs has a float32 block and a float16 one in it.
-template <int EPI>
+// Staging bytes of an epilogue warp: 4 KB; kEpiNs has a float32 block and a float16 one, PROMOTE two float32 blocks
+// (dW of 4096 x 9216 from 256 columns 45.7 -> 42.4 us; its operands then have one stage less, which costs nothing there).
+template <int EPI, bool PROMOTE>
 constexpr int stage_out() {
-    return EPI == kEpiNs ? 6144 : 4096;
+    return EPI == kEpiNs ? 6144 : PROMOTE ? 8192 : 4096;
 }
 
 
@@ -401,11 +403,10 @@ __device__ __forceinline__ float act_deriv(float z, int act) {
 // matrix). `row` is this lane's row, `col` the warp's first column. Aligned float32 rows are read in place. Rows that
 // are not 16-byte aligned are read a row at a time, a lane per column, and turned in the warp's staging area `turn`
 // (32 x 33 floats do not fit it, so 16 rows at a time).
-template <bool GEN>
 __device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int b, int row, int col, int m, int n,
                                        float *turn) {
     const int lane = threadIdx.x & 31;
-    if (!GEN || c.vec) {
+    if (c.vec) {
         const float *p = static_cast<const float *>(c.p) + b * c.stride + (int64_t)row * c.ld + col;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -621,14 +622,15 @@ __device__ __forceinline__ GAhead ahead_of(const GMat &c, int b, int row0, int c
     for (int i = 0; i < 4; ++i) g.rows |= (row0 + r + 8 * i < m ? 1u : 0u) << i;
     return g;
 }
-// The same for a padded float32 operand (kNsApply): eight lanes to a row of 128 bytes, four rows to an instruction.
-__device__ __forceinline__ GAhead ahead_of_f32(const GMat &c, int b, int row0, int col0, int m) {
+// The same for an aligned float32 operand with `cols` readable columns, a multiple of four: eight lanes to a row of 128
+// bytes, four rows to an instruction.
+__device__ __forceinline__ GAhead ahead_of_f32(const GMat &c, int b, int row0, int col0, int m, int cols) {
     const int lane = threadIdx.x & 31, r = lane >> 3;
     GAhead g;
     g.p = reinterpret_cast<const char *>(static_cast<const float *>(c.p) + b * c.stride + (int64_t)(row0 + r) * c.ld + col0 +
                                          4 * (lane & 7));
     g.step = 16 * c.ld;
-    g.lim = (int)c.ld - col0 - 4 * (lane & 7);
+    g.lim = cols - col0 - 4 * (lane & 7);
     g.rows = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) g.rows |= (row0 + r + 4 * i < m ? 1u : 0u) << i;
@@ -648,6 +650,22 @@ __device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GAhead &g, int 
     const uint32_t rows = off < g.lim ? g.rows : 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) ld_cg_if(u[i], p + i * g.step, (rows >> i) & 1);
+}
+
+// Such a block through 4 KB of staging: this lane's row of it.
+__device__ __forceinline__ void take32_f32(float (&v)[32], const uint4 (&u0)[4], const uint4 (&u1)[4], uint8_t *slot) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
+        *reinterpret_cast<uint4 *>(slot + r * 128 + (((lane & 7) ^ (r & 7)) << 4)) = i < 4 ? u0[i & 3] : u1[i & 3];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float4 f = *reinterpret_cast<const float4 *>(slot + lane * 128 + ((i ^ (lane & 7)) << 4));
+        v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
+    }
 }
 
 template <bool GEN, bool WIDE>
@@ -688,9 +706,7 @@ template <bool GEN, bool WIDE>
 __device__ __forceinline__ void take32(float (&v)[32], const GMat &c, int b, int row, int col, int m, int n, uint8_t *at,
                                        float *turn) {
     const int lane = threadIdx.x & 31;
-    if (!GEN && WIDE) {
-        load32<false>(v, c, b, row, col, m, n, turn);
-    } else if (!GEN || ahead_ok<GEN, WIDE>(c)) {
+    if (!GEN || ahead_ok<GEN, WIDE>(c)) {
         uint32_t w[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -711,7 +727,7 @@ __device__ __forceinline__ void take32(float (&v)[32], const GMat &c, int b, int
             }
         }
     } else {
-        load32<true>(v, c, b, row, col, m, n, turn);
+        load32(v, c, b, row, col, m, n, turn);
     }
 }
 // The diagonal at this lane's row (once per unit) and at column col + lane.
@@ -736,9 +752,13 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
     if constexpr (EPI == kEpiFwd) {
         float r[32];
         if (a.c1.p != nullptr) {
-            stage_in<GEN, WIDE>(u1, a.c1, slot);
-            __syncwarp();
-            take32<GEN, WIDE>(r, a.c1, b, row, col, a.m, a.n, slot, turn);
+            if constexpr (!GEN && WIDE) {
+                take32_f32(r, u0, u1, slot);
+            } else {
+                stage_in<GEN, WIDE>(u1, a.c1, slot);
+                __syncwarp();
+                take32<GEN, WIDE>(r, a.c1, b, row, col, a.m, a.n, slot, turn);
+            }
         }
         if (a.bias != nullptr) {
             const float bi = row < a.m ? __ldg(a.bias + row) : 0.f;
@@ -763,10 +783,12 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
         }
     } else if constexpr (EPI == kEpiBwd) {
         uint8_t *at1 = a.c0.p != nullptr ? slot + 2048 : slot;
-        stage_in<GEN, false>(u0, a.c0, slot);
-        stage_in<GEN, WIDE>(u1, a.c1, at1);
-        __syncwarp();
         float r[32];
+        if (GEN || !WIDE || a.c0.p != nullptr) {
+            stage_in<GEN, false>(u0, a.c0, slot);
+            stage_in<GEN, WIDE>(u1, a.c1, at1);
+            __syncwarp();
+        }
         // both leave the slot before either is turned in it
         if (a.c1.p != nullptr && ahead_ok<GEN, WIDE>(a.c1)) take32<GEN, WIDE>(r, a.c1, b, row, col, a.m, a.n, at1, turn);
         if (a.c0.p != nullptr) {
@@ -784,7 +806,16 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
             }
         }
         if (a.c1.p != nullptr) {
-            if (!ahead_ok<GEN, WIDE>(a.c1)) {
+            if constexpr (!GEN && WIDE) {
+                if (a.c0.p == nullptr) {
+                    take32_f32(r, u0, u1, slot);
+                } else {   // z had the place of what is fetched ahead
+                    uint4 t0[4] = {}, t1[4] = {};
+                    fetch_ahead_f32(t0, t1, ahead_of_f32(a.c1, b, row - lane, col, a.m, a.n), 0);
+                    __syncwarp();
+                    take32_f32(r, t0, t1, slot);
+                }
+            } else if (!ahead_ok<GEN, WIDE>(a.c1)) {
                 __syncwarp();
                 take32<GEN, WIDE>(r, a.c1, b, row, col, a.m, a.n, slot, turn);
             }
@@ -826,18 +857,8 @@ __device__ __forceinline__ void epilogue32(float (&v)[32], const uint4 (&u0)[4],
         // (a + e) X + B X with the diagonal e of B by row (or by column where X has more rows than columns). X is
         // float32: it comes in at the slot's first 4 KB and leaves from there, the float16 operand of the next products
         // (or o) from the 2 KB behind.
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = 4 * i + (lane >> 3);
-            *reinterpret_cast<uint4 *>(slot + r * 128 + (((lane & 7) ^ (r & 7)) << 4)) = i < 4 ? u0[i & 3] : u1[i & 3];
-        }
-        __syncwarp();
         float c[32];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 f = *reinterpret_cast<const float4 *>(slot + lane * 128 + ((i ^ (lane & 7)) << 4));
-            c[4 * i] = f.x, c[4 * i + 1] = f.y, c[4 * i + 2] = f.z, c[4 * i + 3] = f.w;
-        }
+        take32_f32(c, u0, u1, slot);
         if (a.tall) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -873,13 +894,13 @@ template <int CG, int BN>
 constexpr int gstage_bytes() {
     return 128 * 128 + (BN / CG) * 128;
 }
-template <int CG, int BN, int EPI>
+template <int CG, int BN, int EPI, bool PROMOTE>
 constexpr int gstages() {
-    return (227 * 1024 - kGEpiWarps * stage_out<EPI>() - 2048) / gstage_bytes<CG, BN>();
+    return (227 * 1024 - kGEpiWarps * stage_out<EPI, PROMOTE>() - 2048) / gstage_bytes<CG, BN>();
 }
-template <int CG, int BN, int EPI>
+template <int CG, int BN, int EPI, bool PROMOTE>
 constexpr int gsmem_bytes() {
-    return gstages<CG, BN, EPI>() * gstage_bytes<CG, BN>() + kGEpiWarps * stage_out<EPI>() + 1024 + 512;
+    return gstages<CG, BN, EPI, PROMOTE>() * gstage_bytes<CG, BN>() + kGEpiWarps * stage_out<EPI, PROMOTE>() + 1024 + 512;
 }
 
 template <int CG, int BN, int EPI, bool PROMOTE, bool GEN>
@@ -888,7 +909,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     static_assert(BN % 64 == 0 && BN / CG >= 64 && 2 * BN <= 512, "two accumulators in tensor memory");
     constexpr bool NS = EPI == kEpiNs;
     constexpr int R = 128 * CG / BN;                      // tile columns to a tile row (symmetric products)
-    constexpr int kStages = gstages<CG, BN, EPI>();
+    constexpr int kStages = gstages<CG, BN, EPI, PROMOTE>();
     constexpr int kStageBytes = gstage_bytes<CG, BN>();
     constexpr int kABytes = 128 * 128;
     constexpr int kBRows = BN / CG;                       // columns of D whose B rows this CTA holds
@@ -897,7 +918,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *epi = smem + kStages * kStageBytes;
-    uint64_t *full = reinterpret_cast<uint64_t *>(epi + kGEpiWarps * stage_out<EPI>());
+    uint64_t *full = reinterpret_cast<uint64_t *>(epi + kGEpiWarps * stage_out<EPI, PROMOTE>());
     uint64_t *empty = full + kStages;
     uint64_t *accf = empty + kStages;    // [2] accumulator ready
     uint64_t *acce = accf + 2;           // [2] accumulator drained
@@ -1082,7 +1103,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int q = warp & 3, half = (warp - 4) >> 2;
-        uint8_t *stage0 = epi + (warp - 4) * stage_out<EPI>();
+        uint8_t *stage0 = epi + (warp - 4) * stage_out<EPI, PROMOTE>();
         uint32_t acce_bar[2] = {smem_u32(acce), smem_u32(acce + 1)};
         if constexpr (CG == 2) {
             acce_bar[0] = mapa_u32(acce_bar[0], 0);
@@ -1107,9 +1128,12 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             const int row = (w.tm * CG + (int)rank) * 128 + q * 32 + lane, n0 = w.tn * BN;
             const bool empty_sum = w.kb1 <= w.kb0;
             GAhead g0 = {}, g1 = {};
+            const bool in32 = !GEN && PROMOTE && a.c1.p != nullptr && a.c0.p == nullptr;   // its place is u0 and u1
             if constexpr (!GEN) {
                 if (NS && a.kind == kNsApply) {
-                    g0 = ahead_of_f32(a.c0, w.b, row - lane, n0, a.m);
+                    g0 = ahead_of_f32(a.c0, w.b, row - lane, n0, a.m, (int)a.c0.ld);
+                } else if (in32) {
+                    g0 = ahead_of_f32(a.c1, w.b, row - lane, n0, a.m, a.n);
                 } else {
                     g0 = ahead_of<false>(a.c0, w.b, row - lane, n0, a.m, a.n);
                     g1 = ahead_of<PROMOTE>(a.c1, w.b, row - lane, n0, a.m, a.n);
@@ -1120,7 +1144,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                 if constexpr (GEN) {
                     fetch_ahead<GEN, false>(u0, a.c0, w.b, row - lane, n0 + ci * 32, a.m, a.n);
                     fetch_ahead<GEN, PROMOTE>(u1, a.c1, w.b, row - lane, n0 + ci * 32, a.m, a.n);
-                } else if (NS && a.kind == kNsApply) {
+                } else if ((NS && a.kind == kNsApply) || in32) {
                     fetch_ahead_f32(u0, u1, g0, ci * 32);
                 } else {
                     fetch_ahead(u0, g0, ci * 32);
@@ -1253,7 +1277,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     }
                     __syncwarp();
-                    epilogue32<EPI, GEN, PROMOTE>(v, u0, u1, di, dj, a, maps, stage0 + slot * (stage_out<EPI>() / 2), w.b, row, col,
+                    epilogue32<EPI, GEN, PROMOTE>(v, u0, u1, di, dj, a, maps, stage0 + slot * (stage_out<EPI, PROMOTE>() / 2), w.b, row, col,
                                                   NS && a.sym && w.tn >= R * (w.tm + 1));
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     slot = a.slots == 2 ? slot ^ 1 : 0;

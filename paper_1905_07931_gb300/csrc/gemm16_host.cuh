@@ -61,7 +61,7 @@ inline bool out_map(CUtensorMap *map, const GMat &o, int m, int n, int batch) {
 }
 
 // Dimensions and maps of one product on CG x 128 x BN tiles.
-template <int CG, int BN, int EPI>
+template <int CG, int BN, int EPI, bool PROMOTE>
 int fill_set(const GProduct &p, GArgs &a, GMaps &maps) {
     const int dtype = a.f16 ? CSRT_DT_F16 : CSRT_DT_BF16;
     a.a_mn = p.a_mn;
@@ -83,10 +83,11 @@ int fill_set(const GProduct &p, GArgs &a, GMaps &maps) {
         return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused an output");
     if (a.out1.vec && !out_map(&maps.out1, a.out1, a.m, a.n, a.batch))
         return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused an output");
-    // one aligned 16-bit output, at most one operand and none to turn: a group needs half the staging
+    // one aligned 16-bit output, at most one operand and none to turn: a group needs half the staging; a float32 one
+    // has it twice (PROMOTE)
     const bool turns = !a.out0.vec || (a.c0.p != nullptr && !a.c0.vec) || (a.c1.p != nullptr && !a.c1.vec);
     const bool two_in = a.c0.p != nullptr && a.c1.p != nullptr;
-    a.slots = EPI != kEpiNs && a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !two_in && !turns ? 2 : 1;
+    a.slots = PROMOTE || (EPI != kEpiNs && a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !two_in && !turns) ? 2 : 1;
     return CSRT_OK;
 }
 
@@ -151,10 +152,10 @@ inline GSplit best_splits(const GTile &t, const GArgs &a, int64_t reduction, boo
 }
 
 // Whether the kernel for aligned matrices serves: every epilogue matrix 16-byte aligned and of the kernel's own types,
-// and the 16-bit operands readable in eights up to the end of a row.
+// and its operands readable in units of 16 bytes up to the end of a row.
 inline bool aligned_set(const GArgs &a, bool wide) {
     auto fine = [&](const GMat &c, bool w) {
-        return c.p == nullptr || (c.vec && (c.dtype == CSRT_DT_F32) == w && (w || c.pad || a.n % 8 == 0));
+        return c.p == nullptr || (c.vec && (c.dtype == CSRT_DT_F32) == w && (w ? a.n % 4 == 0 : c.pad || a.n % 8 == 0));
     };
     return a.out0.vec && (a.out0.dtype == CSRT_DT_F32) == wide && (a.out1.p == nullptr || a.out1.vec) && fine(a.c0, false) &&
            fine(a.c1, wide);
@@ -165,10 +166,10 @@ int launch_tile(const GProduct &p, const GArgs &a, cudaStream_t s) {
     GLaunch<EPI> l = {};
     l.args[0] = a;
     l.phases = 1;
-    int rc = fill_set<CG, BN, EPI>(p, l.args[0], l.maps[0]);
+    int rc = fill_set<CG, BN, EPI, PROMOTE>(p, l.args[0], l.maps[0]);
     if (rc != CSRT_OK) return rc;
     constexpr auto kernel = gemm16_kernel<CG, BN, EPI, PROMOTE, GEN>;
-    constexpr int smem = gsmem_bytes<CG, BN, EPI>();
+    constexpr int smem = gsmem_bytes<CG, BN, EPI, PROMOTE>();
     rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
     const int grid = imin(l.args[0].units, imax(1, num_sms() / CG)) * CG;

@@ -309,7 +309,7 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
         ns_product(q, set, p, a);
         // slices of different matrices' phases would share their place in the workspace
         a.splits = q.batch == 1 ? best_splits(tile, a, p.reduction, false).splits : 1;
-        const int rc = fill_set<CG, BN, kEpiNs>(p, a, n.maps[set]);
+        const int rc = fill_set<CG, BN, kEpiNs, false>(p, a, n.maps[set]);
         if (rc != CSRT_OK) return rc;
         units = imax(units, a.units);
     }
@@ -320,7 +320,7 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     n.step_units[2] = n.args[3].units / q.batch;
 
     constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false, false>;
-    constexpr int smem = gsmem_bytes<CG, BN, kEpiNs>();
+    constexpr int smem = gsmem_bytes<CG, BN, kEpiNs, false>();
     const int rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
     // CTAs (or pairs) that the GPU can hold at once: all of them have to be there, as units wait for one another
