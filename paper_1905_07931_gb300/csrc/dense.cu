@@ -63,20 +63,30 @@ static bool clash(const csrt_mat *out, const csrt_mat *in) {
 }
 
 // ---------------------------------------------------------------------------
-// Copy of an operand whose rows are not 16-byte aligned into padded rows.
+// Copy of an operand whose rows are not 16-byte aligned into padded rows. A thread takes the eight elements of an
+// aligned 16-byte store out of the one or two aligned 16-byte words that hold them (as long as those lie within the
+// matrix); short rows share a block. 4096 x 1777 adds 6.8 us to a product, 9216 x 5 2.
 // ---------------------------------------------------------------------------
 __global__ void pack16_kernel(const uint16_t *__restrict__ src, int64_t ld, int32_t rows, int32_t cols,
                               uint16_t *__restrict__ dst, int64_t dld) {
     pdl_enter();
-    // a thread takes the eight elements of an aligned 16-byte store; the warp's loads cover whole lines between them
-    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
+    const uintptr_t first = reinterpret_cast<uintptr_t>(src);
+    const uintptr_t end = reinterpret_cast<uintptr_t>(src + (int64_t)(rows - 1) * ld + cols);
+    for (int64_t r = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; r < rows; r += (int64_t)gridDim.y * blockDim.y)
         for (int64_t c = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 8; c < cols; c += (int64_t)gridDim.x * blockDim.x * 8) {
-            uint32_t w[4] = {0, 0, 0, 0};
             const uint16_t *p = src + r * ld + c;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c + e < cols) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
-            *reinterpret_cast<uint4 *>(dst + r * dld + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            const int count = (int)imin<int64_t>(cols - c, 8);
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p), word = at & ~(uintptr_t)15;
+            const bool two = (at & 15) + 2 * count > 16;
+            uint4 u;
+            if (word >= first && word + (two ? 32 : 16) <= end) {
+                const uint4 lo = __ldg(reinterpret_cast<const uint4 *>(word));
+                const uint4 hi = two ? __ldg(reinterpret_cast<const uint4 *>(word) + 1) : make_uint4(0, 0, 0, 0);
+                u = eight_at(lo, hi, (uint32_t)(at & 15));
+            } else {
+                u = eight_singly(p, count);
+            }
+            *reinterpret_cast<uint4 *>(dst + r * dld + c) = u;
         }
 }
 
@@ -90,10 +100,11 @@ static int operand(const csrt_mat *m, char **at, cudaStream_t s, GOperand *o) {
     o->ld = (int64_t)align_up((size_t)m->cols, 8);
     o->p = *at;
     *at += align_up((size_t)m->rows * o->ld * 2, 256);
-    const unsigned block = m->cols > 512 ? 128 : 32;
-    const unsigned gx = (unsigned)imin<int64_t>(ceil_div<int64_t>(m->cols, 8 * block), 64);
-    const unsigned gy = (unsigned)imin<int64_t>(m->rows, 65535);
-    launch_pdl(pack16_kernel, dim3(gx, gy), dim3(block), 0, s, static_cast<const uint16_t *>(m->data), m->ld, m->rows,
+    unsigned bx = 1;   // threads along a row: a block of 256 takes several short rows
+    while (bx < 256 && (int64_t)bx * 8 < m->cols) bx *= 2;
+    const unsigned gx = (unsigned)imin<int64_t>(ceil_div<int64_t>(m->cols, 8 * bx), 64);
+    const unsigned gy = (unsigned)imin<int64_t>(ceil_div<int64_t>(m->rows, 256 / bx), 65535);
+    launch_pdl(pack16_kernel, dim3(gx, gy), dim3(bx, 256 / bx), 0, s, static_cast<const uint16_t *>(m->data), m->ld, m->rows,
                m->cols, static_cast<uint16_t *>(o->p), o->ld);
     count_launch();
     return check_launch("pack16_kernel");

@@ -399,7 +399,7 @@ __device__ __forceinline__ float act_deriv(float z, int act) {
     return 1.f;
 }
 
-// 32 consecutive elements of a row of an epilogue operand that is not fetched ahead, as float32 (0 beyond the
+// 32 consecutive elements of a row of a float32 epilogue operand in the general kernel (0 beyond the
 // matrix). `row` is this lane's row, `col` the warp's first column. Aligned float32 rows are read in place. Rows that
 // are not 16-byte aligned are read a row at a time, a lane per column, and turned in the warp's staging area `turn`
 // (32 x 33 floats do not fit it, so 16 rows at a time).
@@ -422,13 +422,14 @@ __device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int b, int
         }
     } else {
         const int row0 = row - lane;
+        const float *p = static_cast<const float *>(c.p) + b * c.stride;
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
             float f[16];
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int rr = row0 + part * 16 + r;
-                f[r] = rr < m && col + lane < n ? load1(c.p, b * c.stride + (int64_t)rr * c.ld + col + lane, c.dtype) : 0.f;
+                f[r] = rr < m && col + lane < n ? p[(int64_t)rr * c.ld + col + lane] : 0.f;
             }
             __syncwarp();
 #pragma unroll
@@ -595,12 +596,12 @@ __device__ __forceinline__ GUnit unit_of(const GArgs &a, int u) {
     return r;
 }
 
-// The warp's 32 x 32 elements of an aligned 16-bit epilogue operand, fetched ahead of their use: a load instruction
+// The warp's 32 x 32 elements of a 16-bit epilogue operand, fetched ahead of their use: a load instruction
 // takes eight whole rows of 64 bytes, four lanes to a row. Through L2 only: another SM may have written them earlier
 // in this launch.
 template <bool GEN, bool WIDE>
 __device__ __forceinline__ bool ahead_ok(const GMat &c) {
-    return GEN ? c.p != nullptr && c.vec && c.dtype != CSRT_DT_F32 : !WIDE && c.p != nullptr;
+    return c.p != nullptr && (GEN ? c.dtype != CSRT_DT_F32 : !WIDE);
 }
 // A unit's view of such an operand in the lean kernel, whose columns are a multiple of eight or padded to one.
 struct GAhead {
@@ -668,26 +669,59 @@ __device__ __forceinline__ void take32_f32(float (&v)[32], const uint4 (&u0)[4],
     }
 }
 
+// The eight 16-bit elements that start `off` bytes into the 32 of lo and hi.
+__device__ __forceinline__ uint4 eight_at(const uint4 &lo, const uint4 &hi, uint32_t off) {
+    uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = off & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = off & 4 ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (off & 2) * 8);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Up to eight elements from p on, one at a time.
+__device__ __forceinline__ uint4 eight_singly(const uint16_t *p, int count) {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < count) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The general kernel's fetch, rows at any alignment: the one or two aligned 16-byte words that hold a lane's eight
+// elements, as long as they lie within the matrix (between its first and its last element; only its two ends may not),
+// and the eight cut out of them. Reading them a row at a time, a lane per column, took
+// dx of 4096 x 1777 from 1000 rows 68 us with z at odd rows, 43 this way.
 template <bool GEN, bool WIDE>
 __device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GMat &c, int b, int row0, int col, int m, int n) {
     if (!ahead_ok<GEN, WIDE>(c)) return;
-    const int lane = threadIdx.x & 31, r = lane >> 2, c8 = col + 8 * (lane & 3);
-    const uint16_t *p = static_cast<const uint16_t *>(c.p) + b * c.stride + (int64_t)(row0 + r) * c.ld + c8;
-    if (c.pad ? c8 < c.ld : c8 + 8 <= n) {
+    const int lane = threadIdx.x & 31, r = row0 + (lane >> 2), c8 = col + 8 * (lane & 3), count = n - c8;
+    const uint16_t *base = static_cast<const uint16_t *>(c.p) + b * c.stride;
+    const uint16_t *p = base + (int64_t)r * c.ld + c8;
+    if (c.vec && count >= 8) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (row0 + r + 8 * i < m) u[i] = __ldcg(reinterpret_cast<const uint4 *>(p + (int64_t)(8 * i) * c.ld));
-    } else if (c8 < n) {   // the last columns of rows that end inside the eight
+            if (r + 8 * i < m) u[i] = __ldcg(reinterpret_cast<const uint4 *>(p + (int64_t)(8 * i) * c.ld));
+        return;
+    }
+    const uintptr_t first = reinterpret_cast<uintptr_t>(base);
+    const uintptr_t end = reinterpret_cast<uintptr_t>(base + (int64_t)(m - 1) * c.ld + n);
+    uint4 lo[4] = {}, hi[4] = {};
+    uint32_t singly = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t w[4] = {0, 0, 0, 0};
-            if (row0 + r + 8 * i < m) {
+    for (int i = 0; i < 4; ++i) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p + (int64_t)(8 * i) * c.ld), word = at & ~(uintptr_t)15;
+        const bool there = r + 8 * i < m && count > 0, two = (at & 15) + 2 * imin(count, 8) > 16;
+        const bool inside = word >= first && word + (two ? 32 : 16) <= end;
+        ld_cg_if(lo[i], reinterpret_cast<const void *>(word), there && inside);
+        ld_cg_if(hi[i], reinterpret_cast<const void *>(word + 16), there && inside && two);
+        singly |= (there && !inside ? 1u : 0u) << i;
+    }
 #pragma unroll
-                for (int e = 0; e < 7; ++e)
-                    if (c8 + e < n) w[e >> 1] |= (uint32_t)p[(int64_t)(8 * i) * c.ld + e] << (16 * (e & 1));
-            }
-            u[i] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+    for (int i = 0; i < 4; ++i) {
+        u[i] = eight_at(lo[i], hi[i], (uint32_t)(reinterpret_cast<uintptr_t>(p + (int64_t)(8 * i) * c.ld) & 15));
+        if (singly >> i & 1) u[i] = eight_singly(p + (int64_t)(8 * i) * c.ld, count);
     }
 }
 // This lane's row of it: stage_in() puts what the lanes fetched into 2 KB of staging, and after a __syncwarp() take32()

@@ -83,11 +83,10 @@ int fill_set(const GProduct &p, GArgs &a, GMaps &maps) {
         return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused an output");
     if (a.out1.vec && !out_map(&maps.out1, a.out1, a.m, a.n, a.batch))
         return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused an output");
-    // one aligned 16-bit output, at most one operand and none to turn: a group needs half the staging; a float32 one
-    // has it twice (PROMOTE)
-    const bool turns = !a.out0.vec || (a.c0.p != nullptr && !a.c0.vec) || (a.c1.p != nullptr && !a.c1.vec);
+    // one aligned 16-bit output, at most one operand: a group needs half the staging; a float32 output has it
+    // twice (PROMOTE)
     const bool two_in = a.c0.p != nullptr && a.c1.p != nullptr;
-    a.slots = PROMOTE || (EPI != kEpiNs && a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !two_in && !turns) ? 2 : 1;
+    a.slots = PROMOTE || (EPI != kEpiNs && a.out0.dtype != CSRT_DT_F32 && a.out1.p == nullptr && !two_in && a.out0.vec) ? 2 : 1;
     return CSRT_OK;
 }
 
