@@ -1273,6 +1273,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                                              : "memory");
                             ++j;
                         }
+                        if (n0 + ci * 32 >= a.n) continue;
                         if (w.splits > 1) {
                             float *p = part + (int64_t)w.split * CG * slab + (int64_t)ci * 32 * 128;
 #pragma unroll
@@ -1282,6 +1283,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                             continue;
                         }
                     } else {
+                        if (n0 + ci * 32 >= a.n) continue;
+                        fetch(ci);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0.f;
                         for (int sl = 0; sl < w.splits; sl += 2) {   // two slices' loads in flight
@@ -1304,8 +1307,6 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         }
                     }
                     const int col = n0 + ci * 32;
-                    if (col >= a.n) continue;
-                    if (pass == 1) fetch(ci);
                     if (lane == 0) {
                         if (a.slots == 2) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                         else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
