@@ -16,8 +16,16 @@ namespace csrt {
 constexpr int kTokWarps = 8;
 constexpr int kTokRows = 2;
 
+// Blocks an SM holds, by the registers n tokens take. Two tokens are held to fewer than the 40 they would take (17.7 ->
+// 15.7 us on 4096 x 9216), more tokens spill in their loop then; one token takes 32 by itself, and a bound makes the
+// compiler order its loads worse (4096 x 4096: 7.6 us without one, 15 with the weakest).
+__host__ __device__ constexpr int tok_blocks(int n) {
+    return n == 1 ? 8 : n == 2 ? 7 : n == 3 ? 5 : 4;
+}
+
+
 template <int N, bool VEC, bool F16>
-__global__ void __launch_bounds__(kTokWarps * 32) dense_tokens_kernel(const __grid_constant__ TokenArgs a) {
+__global__ void __launch_bounds__(kTokWarps * 32, N == 1 ? 0 : tok_blocks(N)) dense_tokens_kernel(const __grid_constant__ TokenArgs a) {
     pdl_enter();
     __shared__ float s_part[kTokWarps][kTokRows * N];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -119,11 +127,12 @@ static void launch_tokens(const TokenArgs &a, bool f16, unsigned grid, cudaStrea
 }
 
 int dense_tokens(TokenArgs a, int n, bool f16, bool vec, cudaStream_t s) {
-    // 48 warps an SM where the rows do not give them (24 leave 8.3 us for 4096 x 4096): up to eight warps share two
-    // rows, as long as each keeps a few steps of K
-    const int64_t pairs = ceil_div<int64_t>(a.m, kTokRows);
+    // As many warps as the GPU holds at once where the rows do not give them: up to eight share two rows, as long as
+    // each keeps a few steps of K (one token of 4096 x 4096: 7.6 us at 54 warps an SM, 8.3 at 27). A second wave costs
+    // more than its warps bring (three tokens: 10.3 against 9.2 us).
+    const int64_t pairs = ceil_div<int64_t>(a.m, kTokRows), held = (int64_t)num_sms() * tok_blocks(n) * kTokWarps;
     a.wpr = 1;
-    while (a.wpr < kTokWarps && pairs * a.wpr < (int64_t)num_sms() * 48 && a.k / (a.wpr * 2) >= 512) a.wpr *= 2;
+    while (a.wpr < kTokWarps && pairs * a.wpr * 2 <= held && a.k / (a.wpr * 2) >= 512) a.wpr *= 2;
     const unsigned grid = (unsigned)ceil_div<int64_t>(pairs, kTokWarps / a.wpr);
     switch (n) {
         case 1: vec ? launch_tokens<1, true>(a, f16, grid, s) : launch_tokens<1, false>(a, f16, grid, s); break;
