@@ -36,8 +36,8 @@
 // instead of 160 us for the promoted sums. 256 x 256 tiles by pairs of SMs halve the operand traffic through L2 of 128 x
 // 128 tiles, which bounds those at about 1.3 PFLOP/s; products too small for a wave of them take 256 x 128, 128 x 128 or
 // 128 x 64 tiles and slices (gemm16_host.cuh). Short reductions are bound by the epilogue: a 128 x 256 share of a tile
-// takes 5 us in it (4096 x 9216 from 256 columns, 151 MB of float32: 41 us, 22 at the measured copy rate; added to
-// what is there 83, 45).
+// takes 5 us in it (4096 x 9216 from 256 columns, 151 MB of float32: 39 us, 22 at the measured copy rate; added to
+// what is there 79, 45).
 //
 // Every wait is bounded: one that runs out sets the CTA's abort flag, the roles drain and meet, and the kernel ends
 // with CSRT_DEV_TIMEOUT in the status word.
@@ -1145,6 +1145,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
         }
         int j = 0;
         int n_go = 0;
+        GUnit ahead = {};
         uint4 u0[4] = {}, u1[4] = {};
         float di = 0.f, dj = 0.f;
         for (int phase = 0; phase < L.phases; ++phase) {
@@ -1158,7 +1159,9 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                 if (!gwait_warp(go + n_go % kGoRing, (n_go / kGoRing) & 1, &s_abort)) break;
                 ++n_go;
             }
-            const GUnit w = unit_of<R>(a, u);
+            // float32 results, whose units are bound by this warp: decoded while the unit before was on its way out (the
+            // divisions take 500 cycles)
+            const GUnit w = !PROMOTE || u == unit0 ? unit_of<R>(a, u) : ahead;
             const int row = (w.tm * CG + (int)rank) * 128 + q * 32 + lane, n0 = w.tn * BN;
             const bool empty_sum = w.kb1 <= w.kb0;
             GAhead g0 = {}, g1 = {};
@@ -1190,26 +1193,28 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             if (w.splits == 1) fetch(half);
             bool ok = true;
             uint32_t d = 0;
-            float sums[PROMOTE ? kChunks / 2 : 1][32];
-            if constexpr (PROMOTE) {
-#pragma unroll
-                for (int i = 0; i < kChunks / 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) sums[i][e] = 0.f;
-            }
-            int kb = w.kb0;
-            do {
-                const int acc = j & 1;
-                ok = __all_sync(0xffffffffu, gwait(accf + acc, (j >> 1) & 1, &s_abort));
+            if (!PROMOTE || w.kb1 - w.kb0 <= kPromoteKb) {
+                ok = gwait_warp(accf + (j & 1), (j >> 1) & 1, &s_abort);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                d = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
-                if constexpr (PROMOTE) {
-                    const bool first = kb == w.kb0;
-                    kb += kPromoteKb;
-                    if (first && kb >= w.kb1) break;   // a short sum stays as it is
+                d = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)((j & 1) * BN);
+            } else {
+                // a long float32 sum: taken out every kPromoteKb stages, the whole sums put back for the epilogue
+                float sums[PROMOTE ? kChunks / 2 : 1][32];
 #pragma unroll
-                    for (int i = 0; i < kChunks / 2; ++i) {
+                for (int i = 0; i < (PROMOTE ? kChunks / 2 : 1); ++i)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sums[i][e] = 0.f;
+                int kb = w.kb0;
+                do {
+                    const int acc = j & 1;
+                    ok = gwait_warp(accf + acc, (j >> 1) & 1, &s_abort);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    d = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
+                    kb += kPromoteKb;
+#pragma unroll
+                    for (int i = 0; i < (PROMOTE ? kChunks / 2 : 1); ++i) {
                         uint32_t r[32];
                         tmem_ld_32cols(d + (uint32_t)((2 * i + half) * 32), r);
 #pragma unroll
@@ -1219,22 +1224,20 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
                         if (lane == 0)
-                            asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
-                                             acce_bar[acc])
+                            asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(acce_bar[acc])
                                          : "memory");
                         ++j;
-                    } else {   // the whole sums go back to this accumulator's place
+                    } else {
 #pragma unroll
-                        for (int i = 0; i < kChunks / 2; ++i)
+                        for (int i = 0; i < (PROMOTE ? kChunks / 2 : 1); ++i)
                             tmem_st_32cols(d + (uint32_t)((2 * i + half) * 32), sums[i]);
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                     }
-                } else {
-                    kb = w.kb1;
-                }
-            } while (kb < w.kb1);
+                } while (kb < w.kb1);
+            }
             if (!ok) break;   // the abort flag is set
 
+            if (PROMOTE && u + ustep < a.units) ahead = unit_of<R>(a, u + ustep);
             bool last = true;
             const int64_t slab = 128 * BN;
             float *part = nullptr;
