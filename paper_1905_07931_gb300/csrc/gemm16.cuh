@@ -126,7 +126,6 @@ struct GLaunch {
 
 // Sets of a Newton-Schulz launch: A of the even and odd steps' X, B, X' of the even and odd steps, the last X'.
 __device__ __forceinline__ int ns_set(int phase, int phases) {
-    if (phases == 1) return 0;   // a launch of one product
     const int step = phase / 3, k = phase - 3 * step;
     return k == 0 ? (step & 1) : k == 1 ? 2 : phase == phases - 1 ? 5 : 3 + (step & 1);
 }
@@ -1022,7 +1021,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
         int known = -1;   // matrix whose inputs of this phase are known to be there
         for (int u = first_unit(L, phase, a.batch, unit0, ustep); u < a.units && !s_abort; u += ustep) {
             const GUnit w = unit_of<R>(a, u);
-            if (NS && L.phases > 1) {
+            if (NS) {
                 if (phase > 0 && w.b != known) {
                     if (!units_wait(L.done + w.b, units_before(L.step_units, phase) * CG, &s_abort)) break;
                     known = w.b;
@@ -1155,7 +1154,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
         const GArgs &a = L.args[NS ? ns_set(phase, L.phases) : 0];
         const GMaps &maps = L.maps[NS ? ns_set(phase, L.phases) : 0];
         for (int u = first_unit(L, phase, a.batch, unit0, ustep); u < a.units; u += ustep) {
-            if (NS && L.phases > 1) {
+            if (NS) {
                 if (!gwait_warp(go + n_go % kGoRing, (n_go / kGoRing) & 1, &s_abort)) break;
                 ++n_go;
             }
@@ -1322,7 +1321,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                     if (pass == 0 && i + 1 < kChunks / 2) fetch(ci + 2);   // the next group's, while this one leaves
                 }
             }
-            if (NS && L.phases > 1) {
+            if (NS) {
                 // This warp's share of the unit is in place: its TMA stores are complete, its lanes' own stores are
                 // ordered before the count by the block-scope fences. The unit's last warp says so for its matrix.
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");

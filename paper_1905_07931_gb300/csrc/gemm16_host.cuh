@@ -198,19 +198,16 @@ int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
     const int best = choice.tile;
     a.whole = choice.split.whole;
     a.splits = choice.split.splits;
-    if (EPI == kEpiNs || aligned_set(a, PROMOTE)) {
+    if (aligned_set(a, PROMOTE)) {
         if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, false>(p, a, s);
         if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, false>(p, a, s);
         if (best == 3) return launch_tile<2, 128, EPI, PROMOTE, false>(p, a, s);
         return launch_tile<1, 64, EPI, PROMOTE, false>(p, a, s);
     }
-    if constexpr (EPI != kEpiNs) {   // (whose matrices are the library's own, all aligned)
-        if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, true>(p, a, s);
-        if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, true>(p, a, s);
-        if (best == 3) return launch_tile<2, 128, EPI, PROMOTE, true>(p, a, s);
-        return launch_tile<1, 64, EPI, PROMOTE, true>(p, a, s);
-    }
-    return fail(CSRT_ERR_ARG, "unaligned product");
+    if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, true>(p, a, s);
+    if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, true>(p, a, s);
+    if (best == 3) return launch_tile<2, 128, EPI, PROMOTE, true>(p, a, s);
+    return launch_tile<1, 64, EPI, PROMOTE, true>(p, a, s);
 }
 
 }  // namespace csrt

@@ -3,8 +3,8 @@
 //   X <- a X + (b A + c A A) X,   A = X X^T  (X^T X and products on the right where X has more rows than columns)
 //
 // as three products per step on gemm16_kernel: A with its mirrored half, B = b A + c A A likewise, and a X + B X. One
-// cooperative launch runs all of them for all matrices, a unit waiting for its own matrix only (GLaunch); a single
-// large matrix takes a launch per product.
+// cooperative launch runs all of them for all matrices, a unit waiting for its own matrix only (GLaunch). A launch per
+// product was slower throughout (64 x 64: 74 against 64 us; 3 x 2048 x 2048: 595, 442; 4096 x 9216: 1947, 1858).
 //
 // Number formats. Singular values stay in [0, 1.203] (p(s) = a s + b s^3 + c s^5 maps [0, 1.203] into itself), so
 // every entry of X, A and B is bounded (1.203, 1.45, 2.81) and fits float16 once scaled by a power of two: X and A
@@ -308,7 +308,9 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
         GArgs &a = n.args[set];
         ns_product(q, set, p, a);
         // slices of different matrices' phases would share their place in the workspace
-        a.splits = q.batch == 1 ? best_splits(tile, a, p.reduction, false).splits : 1;
+        const GSplit split = q.batch == 1 ? best_splits(tile, a, p.reduction, true) : GSplit{0, 1, 0.};
+        a.whole = split.whole;
+        a.splits = split.splits;
         const int rc = fill_set<CG, BN, kEpiNs, false>(p, a, n.maps[set]);
         if (rc != CSRT_OK) return rc;
         units = imax(units, a.units);
@@ -366,26 +368,14 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
 static int ns_products(const NsPlan &q, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the orthogonalisation needs a GPU with tcgen05");
     // By the number of 128 x 128 tiles of X (measured, us for the whole call on tiles 64, 128 by pairs and 256 by pairs
-    // wide in one launch, and on launches of their own): few tiles take the narrow ones, which share the work among
-    // more SMs (1024 x 1024: 124 / 148 / 220, 140; 3 x 2048 x 512: 154 / 175 / 241, 200); from 200 tiles on pairs of SMs
-    // on 256 x 128 (2048 x 2048: 334 / 249 / 307, 282; 6 x 256 x 4096: 228 / 206 / 271, 249); from 700 on, where L2
-    // traffic counts most, 256 x 256: in one launch for several matrices, which fill each other's gaps
-    // (3 x 2048 x 2048: 758 / 484 / 444, 606), and for a single one a launch for each product, on its best tile
-    // (4096 x 4096: 1857 / 1216 / 1065, 1034; 4096 x 9216: 3398 / 2346 / 1982, 1890).
+    // wide): few tiles take the narrow ones, which share the work among more SMs (1024 x 1024: 123 / 147 / 217;
+    // 3 x 2048 x 512: 154 / 174 / 239); from 200 tiles on pairs of SMs on 256 x 128 (2048 x 2048: 334 / 247 / 306;
+    // 6 x 256 x 4096: 226 / 203 / 267; 4096 x 1000: 246 / 237 / 290); from 700 on, where L2 traffic counts most,
+    // 256 x 256 (3 x 2048 x 2048: 738 / 487 / 442; 4096 x 4096: 1826 / 1188 / 1027; 4096 x 9216: 3747 / 2204 / 1858).
     const int64_t tiles = (int64_t)q.batch * ceil_div<int64_t>(q.rows, 128) * ceil_div<int64_t>(q.cols, 128);
     if (tiles < 200) return launch_ns<1, 64>(q, kTiles[2], s);
     if (tiles < 700) return launch_ns<2, 128>(q, kTiles[3], s);
-    if (q.batch > 1) return launch_ns<2, 256>(q, kTiles[0], s);
-    for (int phase = 0; phase < 3 * q.steps; ++phase) {
-        const int step = phase / 3, k = phase % 3;
-        const int set = k == 0 ? step & 1 : k == 1 ? 2 : phase == 3 * q.steps - 1 ? 5 : 3 + (step & 1);
-        GProduct p;
-        GArgs a;
-        ns_product(q, set, p, a);
-        const int rc = launch_gemm16<kEpiNs, false>(p, a, s);
-        if (rc != CSRT_OK) return rc;
-    }
-    return CSRT_OK;
+    return launch_ns<2, 256>(q, kTiles[0], s);
 }
 
 static int check_batch(const csrt_mat *m, const char *name, int32_t batch, int64_t stride) {
