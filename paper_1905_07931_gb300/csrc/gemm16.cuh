@@ -32,8 +32,8 @@
 // too (512 x 512 x 512: 5.4 against 6.6 us).
 //
 // Bounds and rates (GB300, measured): 4096 x 4096 x 8192 bfloat16 143 us, 1.91 PFLOP/s, which is the tensor cores' rate
-// under load (the library's product takes 137 us); 8192 x 8192 x 4096 285 us, 1.93 PFLOP/s. dW in float32 takes 169
-// instead of 160 us for the promoted sums. 256 x 256 tiles by pairs of SMs halve the operand traffic through L2 of 128 x
+// under load (the library's product takes 137 us); 8192 x 8192 x 4096 280 us, 1.96 PFLOP/s. dW in float32 takes 159
+// instead of 149 us for the promoted sums. 256 x 256 tiles by pairs of SMs halve the operand traffic through L2 of 128 x
 // 128 tiles, which bounds those at about 1.3 PFLOP/s; products too small for a wave of them take 256 x 128, 128 x 128 or
 // 128 x 64 tiles and slices (gemm16_host.cuh). Short reductions are bound by the epilogue: a 128 x 256 share of a tile
 // takes 5 us in it (4096 x 9216 from 256 columns, 151 MB of float32: 39 us, 22 at the measured copy rate; added to

@@ -15,10 +15,11 @@
 // rounding would otherwise be the largest error of o (a bfloat16 o was 2.2e-3 to 2.8e-3 off with them inside, and is
 // 1.7e-3 off now, its own rounding).
 //
-// What bounds it (measured, whole calls): 4096 x 9216 takes 2.0 ms for 2.66 TFLOP of necessary work (1.4 ms at the library's
-// rate): its products run at 1.5 to 1.65 PFLOP/s with waves 90% full, the two passes over gradient and momentum take
-// 0.14 ms at HBM rate. Smaller ones are bound by latency: a product costs at least 4 us - operands from L2, the epilogue's
-// own, the release to the other SMs - so fifteen of them 60 to 75 us, whatever the size (a 64 x 64 matrix: 60 us).
+// What bounds it (measured, whole calls): 4096 x 9216 takes 1.86 ms for 2.66 TFLOP of necessary work (1.4 ms at the
+// library's rate; 2.0 ms when calls follow one another for long and the power limit sets the clock): products at 1.5 to
+// 1.65 PFLOP/s, waves 90% full, and 0.14 ms for the two passes over gradient and momentum, at HBM rate. Smaller ones are
+// bound by latency: a product costs at least 4 us - operands from L2, the epilogue's own, the release to the other SMs -
+// so fifteen of them 64 us and more, whatever the size (a 64 x 64 matrix: 64 us).
 //
 // The Frobenius norm is summed in float64 over float32 sums of eight squares; a sum out of float32's safe range is
 // taken again in float64, so that neither tiny nor huge gradients lose it.

@@ -277,3 +277,17 @@ def test_matrices_far_apart(C, m, k, odt):
     C.orthogonalize(g, o, ws, momentum=ma)
     C.orthogonalize(gf, of, ws, momentum=mb)
     assert torch.equal(o, of) and torch.equal(ma, mb)
+
+
+@pytest.mark.parametrize("batch,m,k", [(1, 3000, 4000), (1, 4001, 2900), (4, 1500, 2000)])
+@pytest.mark.parametrize("odt", [torch.float32, torch.bfloat16])
+def test_large_matrices(C, batch, m, k, odt):
+    """Sizes from which on the largest tiles serve, their left-over tiles in slices where there is one matrix."""
+    gen = _gen(batch + m + k)
+    g = torch.randn(batch, m, k, generator=gen, device="cuda")
+    o, o2 = torch.empty(batch, m, k, dtype=odt, device="cuda"), torch.empty(batch, m, k, dtype=odt, device="cuda")
+    ws = C.OrthogonalizeWorkspace(batch, m, k)
+    C.orthogonalize(g, o, ws, scale=0.5)
+    C.orthogonalize(g, o2, ws, scale=0.5)
+    assert torch.equal(o, o2)
+    assert _rel(o, _exact(g.double(), 5, 1e-7, 0.5)) <= (2e-3 if odt == torch.float32 else 3e-3)
