@@ -333,7 +333,8 @@ int debias_update(csrt_csr *w, const float *g_nnz, float eta, void *stream);
 #define CSRT_ACT_GELU 2  /* tanh form: 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
 #define CSRT_ACT_SILU 3  /* z / (1 + exp(-z)) */
 
-/* A row-major device matrix whose rows are ld elements apart (ld >= cols). */
+/* A row-major device matrix whose rows are ld elements apart (ld >= cols).
+ * What lies between two rows is never written; it may be read, and is ignored. */
 typedef struct csrt_mat {
     void *data;
     int32_t rows, cols;
