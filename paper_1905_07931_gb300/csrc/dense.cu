@@ -330,7 +330,9 @@ int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, 
             t.m = m;
             t.n = k;
             t.batch = 1;
-            const GChoice c = choose_tile(t, n);
+            t.out0 = epi_mat(dw);
+            t.c1 = a.c1;
+            const GChoice c = choose_tile(t, n, aligned_set(t, dw->dtype == CSRT_DT_F32));
             const int64_t units = ceil_div<int64_t>(m, 128 * kTiles[c.tile].cg) * ceil_div<int64_t>(k, kTiles[c.tile].bn) *
                                   c.split.splits * kTiles[c.tile].cg;
             const double us = (double)m * n * 2 / (2.0 * imin<int64_t>(units, num_sms()) * 3000.0);

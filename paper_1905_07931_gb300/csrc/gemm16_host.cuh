@@ -105,13 +105,17 @@ int allow_smem(int smem) {
 // Time of a product in microseconds by a simple model of gemm16_kernel: waves of units, each loading its stages and
 // then running an epilogue that overlaps the next unit's stages but not the last's; joining slices costs their
 // partial tiles' trip through L2. The constants are fitted to measured times of 69 products of 64 to 9216 rows and
-// columns on every tile and up to 16 slices; the choice they give is within 1.2% of the best on average.
+// columns on every tile and up to 16 slices; the choice they give is within 1.2% of the best on average (the general
+// kernel's epilogues on 24 products of odd sizes: dx of 4096 x 1777 from 1000 rows takes 21.9 us on 128 x 128 tiles,
+// 24.9 on the 256 x 256 that the aligned kernel's times would choose).
 struct GTile {
     int cg, bn;
     double stage, epi;   // us per stage, us per unit's epilogue
+    double epi_gen;      // the same in the general kernel, whose unaligned rows are read and stored piecewise
 };
 constexpr int kTileKinds = 4;
-constexpr GTile kTiles[kTileKinds] = {{2, 256, 0.34, 5.7}, {1, 128, 0.245, 4.3}, {1, 64, 0.206, 3.6}, {2, 128, 0.228, 4.4}};
+constexpr GTile kTiles[kTileKinds] = {
+    {2, 256, 0.34, 5.7, 8.8}, {1, 128, 0.245, 4.3, 5.9}, {1, 64, 0.206, 3.6, 4.0}, {2, 128, 0.228, 4.4, 6.6}};
 inline double model_us(const GTile &t, int64_t tiles, int64_t kb, int64_t whole, int64_t splits) {
     const int64_t slots = imax(1, num_sms() / t.cg);
     const double tile = (double)imax<int64_t>(kb, 1) * t.stage;
@@ -182,10 +186,12 @@ struct GChoice {
     int tile;
     GSplit split;
 };
-inline GChoice choose_tile(const GArgs &a, int64_t reduction) {
+inline GChoice choose_tile(const GArgs &a, int64_t reduction, bool aligned) {
     GChoice best = {0, {0, 1, 1e30}};
     for (int c = 0; c < kTileKinds; ++c) {
-        const GSplit s = best_splits(kTiles[c], a, reduction, true);
+        GTile t = kTiles[c];
+        if (!aligned) t.epi = t.epi_gen;
+        const GSplit s = best_splits(t, a, reduction, true);
         if (s.us < best.split.us) best = {c, s};
     }
     return best;
@@ -194,11 +200,12 @@ inline GChoice choose_tile(const GArgs &a, int64_t reduction) {
 template <int EPI, bool PROMOTE>
 int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the dense products need a GPU with tcgen05");
-    const GChoice choice = choose_tile(a, p.reduction);
+    const bool aligned = aligned_set(a, PROMOTE);
+    const GChoice choice = choose_tile(a, p.reduction, aligned);
     const int best = choice.tile;
     a.whole = choice.split.whole;
     a.splits = choice.split.splits;
-    if (aligned_set(a, PROMOTE)) {
+    if (aligned) {
         if (best == 0) return launch_tile<2, 256, EPI, PROMOTE, false>(p, a, s);
         if (best == 1) return launch_tile<1, 128, EPI, PROMOTE, false>(p, a, s);
         if (best == 3) return launch_tile<2, 128, EPI, PROMOTE, false>(p, a, s);
