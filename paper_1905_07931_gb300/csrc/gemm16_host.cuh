@@ -105,13 +105,13 @@ int allow_smem(int smem) {
 // Time of a product in microseconds by a simple model of gemm16_kernel: waves of units, each loading its stages and
 // then running an epilogue that overlaps the next unit's stages but not the last's; joining slices costs their
 // partial tiles' trip through L2. The constants are fitted to measured times of 69 products of 64 to 9216 rows and
-// columns on every tile and up to 16 slices; the choice they give is within 1.2% of the best on average (the general
-// kernel's epilogues on 24 products of odd sizes: dx of 4096 x 1777 from 1000 rows takes 21.9 us on 128 x 128 tiles,
-// 24.9 on the 256 x 256 that the aligned kernel's times would choose).
+// columns on every tile and up to 16 slices; the choice they give is within 1.2% of the best on average. The longer
+// epilogues are fitted to 24 products of odd sizes: dx of 4096 x 1777 from 1000 rows takes 21.9 us on 128 x 128 tiles
+// and 24.9 on the 256 x 256 that the short one would choose, aligned with z and a residual 22.8 and 27.2.
 struct GTile {
     int cg, bn;
     double stage, epi;   // us per stage, us per unit's epilogue
-    double epi_gen;      // the same in the general kernel, whose unaligned rows are read and stored piecewise
+    double epi_more;     // the same in the general kernel, or with z or two more matrices to read and write
 };
 constexpr int kTileKinds = 4;
 constexpr GTile kTiles[kTileKinds] = {
@@ -187,10 +187,11 @@ struct GChoice {
     GSplit split;
 };
 inline GChoice choose_tile(const GArgs &a, int64_t reduction, bool aligned) {
+    const bool more = !aligned || a.c0.p != nullptr || (a.c1.p != nullptr && a.out1.p != nullptr);
     GChoice best = {0, {0, 1, 1e30}};
     for (int c = 0; c < kTileKinds; ++c) {
         GTile t = kTiles[c];
-        if (!aligned) t.epi = t.epi_gen;
+        if (more) t.epi = t.epi_more;
         const GSplit s = best_splits(t, a, reduction, true);
         if (s.us < best.split.us) best = {c, s};
     }
