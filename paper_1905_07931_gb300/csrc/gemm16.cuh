@@ -691,7 +691,8 @@ __device__ __forceinline__ uint4 eight_singly(const uint16_t *p, int count) {
 // The general kernel's fetch, rows at any alignment: the one or two aligned 16-byte words that hold a lane's eight
 // elements, as long as they lie within the matrix (between its first and its last element; only its two ends may not),
 // and the eight cut out of them. Reading them a row at a time, a lane per column, took
-// dx of 4096 x 1777 from 1000 rows 68 us with z at odd rows, 43 this way.
+// dx of 4096 x 1777 from 1000 rows 68 us with z at odd rows, 43 this way
+// on the same tiles (37 on those that it takes now).
 template <bool GEN, bool WIDE>
 __device__ __forceinline__ void fetch_ahead(uint4 (&u)[4], const GMat &c, int b, int row0, int col, int m, int n) {
     if (!ahead_ok<GEN, WIDE>(c)) return;
