@@ -145,7 +145,10 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
     n2 = block_sum(n2);
     double norm = sqrt(n2);
     norm = norm < (double)a.eps ? (double)a.eps : norm;   // a NaN stays
-    const float f = (float)((a.direct ? (double)a.scale : (double)kXScale) / norm);
+    // Factors that float32 does not hold (norms below 1e-34, or scale / norm out of its range) are applied in float64.
+    const double fd = (a.direct ? (double)a.scale : (double)kXScale) / norm;
+    const bool in_range = fabs(fd) >= 0x1p-126 && fabs(fd) < 0x1p127;
+    const float f = (float)fd;
     const uint32_t per_row = (uint32_t)(a.cols + 7) / 8, total = per_row * (uint32_t)a.rows;
     for (uint32_t t = blockIdx.x * kPrepThreads + threadIdx.x; t < total; t += gridDim.x * kPrepThreads) {
         const uint32_t r = t / per_row, c = (t - r * per_row) * 8;
@@ -153,7 +156,7 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
         float u[8];
         direction8<false>(a, b, (int)r, (int)c, cnt, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] *= f;
+        for (int i = 0; i < 8; ++i) u[i] = in_range ? u[i] * f : (float)((double)u[i] * fd);
         if (a.direct) {
             for (int i = 0; i < cnt; ++i)
                 store1(a.o.p, b * a.o.stride + (int64_t)r * a.o.ld + c + i, u[i], a.o.dtype);

@@ -291,3 +291,30 @@ def test_large_matrices(C, batch, m, k, odt):
     C.orthogonalize(g, o2, ws, scale=0.5)
     assert torch.equal(o, o2)
     assert _rel(o, _exact(g.double(), 5, 1e-7, 0.5)) <= (2e-3 if odt == torch.float32 else 3e-3)
+
+
+@pytest.mark.parametrize("m,k", [(40, 60), (33, 7)])
+@pytest.mark.parametrize("steps", [0, 5])
+def test_factors_out_of_float32_range(C, m, k, steps):
+    """eps and norms so small (or, with no steps, a result so far from the norm) that the factor between u and o is no
+    float32: a zero matrix stays zero, others come out as from the definition."""
+    # entries that float32 holds exactly: 2^-120 times a float16
+    v = torch.randn(1, m, k, generator=_gen(m + steps), device="cuda").half().double()
+    cases = [(0.0, 1e-38, 1.0), (0.0, 1e-45, 8.0), (2.0 ** -120, 1e-38, 1.0), (2.0 ** -120, 1e-45, 8.0)]
+    if steps == 0:
+        cases += [(2.0 ** -120, 1e-45, 3e38), (2.0 ** 110, 1e-7, 2e-5), (2.0 ** 110, 1e-7, 1e-6)]
+    ws = C.OrthogonalizeWorkspace(1, m, k)
+    for factor, eps, scale in cases:
+        g = (v * factor).float()
+        assert torch.equal(g.double(), v * factor)
+        o = torch.full_like(g, float("nan"))
+        C.orthogonalize(g, o, ws, eps=eps, steps=steps, scale=scale)
+        if factor == 0.0:
+            assert bool((o == 0).all())
+        else:   # without steps: the float32 factor's and the product's roundings, and float32's smallest step
+            want = _exact(g.double(), steps, 0.0, scale)
+            assert bool(o.isfinite().all())
+            if steps == 0:
+                assert bool(((o.double() - want).abs() <= 2.0 ** -22 * want.abs() + 2.0 ** -149).all())
+            else:
+                assert _rel(o, want) <= 2e-3
