@@ -385,8 +385,12 @@ __device__ __forceinline__ float act_value(float z, int act) {
     return z;
 }
 
+// gelu' and silu' are 0 or 1 to float32 from |z| = 104 on (exp(-104) is below its smallest step). z is held to 128, so that
+// neither z^2 nor z (1 - p) overflows against a zero factor: a float16 z beyond 65504 is kept as an infinity and still has
+// a derivative. A NaN stays.
 __device__ __forceinline__ float act_deriv(float z, int act) {
     if (act == CSRT_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if (fabsf(z) > 128.f) z = copysignf(128.f, z);
     if (act == CSRT_ACT_GELU) {
         const float p = __fdividef(1.f, 1.f + __expf(-kGelu2 * (z + kGelu3 * z * z * z)));
         return p + z * p * (1.f - p) * kGelu2 * (1.f + 3.f * kGelu3 * z * z);

@@ -372,3 +372,31 @@ def test_rows_far_apart(C, m, k, n, odd):
         C.dense_update(dw[i], w[i], 0.1, 0.01, w16[i])
         C.dense_act_bwd(z[i], x[i] if m == k else z[i], "gelu", y[i])
     assert torch.equal(dw[0], dw[1]) and torch.equal(w16[0], w16[1]) and torch.equal(y[0], y[1])
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("dtype,n", [("bf16", 16), ("bf16", 13), ("f16", 16), ("f16", 13)])
+def test_derivatives_far_from_zero(C, act, dtype, n):
+    """act' is 1 (z > 0) or 0 (z < 0) within float32 where |z| is large, up to infinities: those that float16 keeps of a
+    pre-activation beyond 65504, and bfloat16's whole range."""
+    dt, inf = DT[dtype], float("inf")
+    big = [120.0, 6e4, inf] + ([1e13, 1e19, 1e25, 3e38] if dtype == "bf16" else [200.0])
+    z = torch.tensor(big + [-v for v in big], device="cuda").to(dt)
+    k, m = z.numel(), 40
+    one = (z > 0).to(dt)
+    zz = z[:, None].repeat(1, n).contiguous()
+    dy = _mat(_gen(n), k, n, dt)
+    out = torch.empty_like(dy)
+    C.dense_act_bwd(dy, zz, act, out)
+    assert torch.equal(out, dy * one[:, None])
+    # the same in the epilogue of the input gradient: the plain product where z > 0, nothing elsewhere
+    w, g = _mat(_gen(1), m, k, dt), _mat(_gen(2), m, n, dt)
+    dx, plain = torch.empty(k, n, dtype=dt, device="cuda"), torch.empty(k, n, dtype=dt, device="cuda")
+    ws = C.DenseWorkspace(m, k, n)
+    C.dense_bwd_x(w, g, plain, ws)
+    C.dense_bwd_x(w, g, dx, ws, z_below=zz, act=act)
+    assert torch.equal(dx, plain * one[:, None])
+    # a NaN is not taken for a large number
+    zz[0] = float("nan")
+    C.dense_act_bwd(dy, zz, act, out)
+    assert bool(out[0].isnan().all()) and not bool(out[1:].isnan().any())
