@@ -155,8 +155,13 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
         const int cnt = min(8, a.cols - (int)c);
         float u[8];
         direction8<false>(a, b, (int)r, (int)c, cnt, u);
+        if (in_range) {   // a branch of its own: with float64 products beside it 12 x 512 x 2048 took 390 us, 320 so
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = in_range ? u[i] * f : (float)((double)u[i] * fd);
+            for (int i = 0; i < 8; ++i) u[i] *= f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = (float)((double)u[i] * fd);
+        }
         if (a.direct) {
             for (int i = 0; i < cnt; ++i)
                 store1(a.o.p, b * a.o.stride + (int64_t)r * a.o.ld + c + i, u[i], a.o.dtype);
