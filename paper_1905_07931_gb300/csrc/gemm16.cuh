@@ -19,9 +19,13 @@
 // of B, and the leader issues the pair's MMAs.
 //
 // Long float32 sums: the tensor core adds each 16-deep block of products to the float32 accumulator with truncation,
-// which drifts by about 4e-6 of the result over 4096 terms and 1.4e-5 where all terms have one sign (measured).
-// Float32 outputs therefore take the accumulator out every kPromoteKb stages (512 terms) and add it, rounded to
-// nearest, to float32 sums in the epilogue warps' registers (PROMOTE); 16-bit outputs do not need it.
+// which drifts by about 4e-6 of the result over 4096 terms and 2.8e-5 where all terms have one sign (7e-9 a term,
+// measured). Float32 outputs therefore take the accumulator out every kPromoteKb stages (512 terms) and add it, rounded
+// to nearest, to float32 sums in the epilogue warps' registers (PROMOTE). 16-bit outputs take the PROMOTE kernel only where
+// the drift of one accumulation would near their own rounding (kLongF16, kLongBf16; 300000 terms of one sign were 2e-3
+// off in float16, half a step of which is 4.9e-4). The Newton-Schulz products, whose Gram matrix of 2 x 64 x 8000000 put
+// the update 4% off, have instances of their own (LONG) that add every kLongKb stages to float32 sums in the workspace;
+// the same code in the instances for ordinary lengths costs those 1%.
 //
 // Splits: where tiles are few, or where the tiles left over after whole waves are (GArgs::whole), a tile's reduction is
 // shared. Each slice's warp leaves its float32 partial tile in the workspace and counts in; the last one adds the
@@ -54,6 +58,9 @@ constexpr int kGBK = 64;                 // reduction depth of a stage (128 byte
 constexpr int kGThreads = 384;           // a warpgroup for TMA and MMA, two for the epilogue
 constexpr int kGEpiWarps = 8;
 constexpr int kPromoteKb = 8;            // stages per tensor-memory accumulation of a float32 output
+constexpr int kLongF16 = 512;            // the most of a 16-bit one: 2.3e-4 after 32768 terms of one sign, half of half a step
+constexpr int kLongBf16 = 2048;          // 9e-4 after 131072 terms, a quarter of half a step
+constexpr int kLongKb = 256;             // and of a Newton-Schulz product: 1.2e-4 after 16384 terms
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kXScale = 32768.f, kInvXScale = 1.f / 32768.f;   // scale of X and A in float16; B's is half of it
 enum { kEpiFwd = 0, kEpiBwd = 1, kEpiNs = 2 };
@@ -98,7 +105,7 @@ struct GArgs {
     int32_t s_pad;
     GMat c0, c1;                      // z_below / A / X (float32); residual
     GMat out0, out1;                  // y, dx, dW, A, B, X (float16), o; z, X (float32)
-    float *partial;                   // split slices
+    float *partial;                   // split slices; long sums (LONG): by slice, or by CTA where no tile is split
     int32_t *counters;
     WsHeader *hdr;
 };
@@ -390,7 +397,8 @@ __device__ __forceinline__ float act_value(float z, int act) {
 // a derivative. A NaN stays.
 __device__ __forceinline__ float act_deriv(float z, int act) {
     if (act == CSRT_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-    if (fabsf(z) > 128.f) z = copysignf(128.f, z);
+    // min(|z|, 128) with z's sign: one instruction
+    asm("min.NaN.xorsign.abs.f32 %0, %0, 0f43000000;" : "+f"(z));
     if (act == CSRT_ACT_GELU) {
         const float p = __fdividef(1.f, 1.f + __expf(-kGelu2 * (z + kGelu3 * z * z * z)));
         return p + z * p * (1.f - p) * kGelu2 * (1.f + 3.f * kGelu3 * z * z);
@@ -941,7 +949,7 @@ constexpr int gsmem_bytes() {
     return gstages<CG, BN, EPI, PROMOTE>() * gstage_bytes<CG, BN>() + kGEpiWarps * stage_out<EPI, PROMOTE>() + 1024 + 512;
 }
 
-template <int CG, int BN, int EPI, bool PROMOTE, bool GEN>
+template <int CG, int BN, int EPI, bool PROMOTE, bool GEN, bool LONG>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     gemm16_kernel(const __grid_constant__ GLaunch<EPI> L) {
     static_assert(BN % 64 == 0 && BN / CG >= 64 && 2 * BN <= 512, "two accumulators in tensor memory");
@@ -953,6 +961,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
     constexpr int kBRows = BN / CG;                       // columns of D whose B rows this CTA holds
     constexpr int kChunks = BN / 32;
     constexpr uint32_t kCols = 2 * BN;
+    constexpr int kAccKb = PROMOTE ? kPromoteKb : kLongKb;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *epi = smem + kStages * kStageBytes;
@@ -1092,8 +1101,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             for (int u = first_unit(L, phase, a.batch, unit0, ustep); u < a.units && !s_abort; u += ustep) {
                 const GUnit w = unit_of<R>(a, u);
                 int kb = w.kb0;
-                do {   // one accumulation: the whole unit, or kPromoteKb stages of it
-                    const int stop = PROMOTE ? min(w.kb1, kb + kPromoteKb) : w.kb1;
+                do {   // one accumulation: the whole unit, or kAccKb stages of it
+                    const int stop = PROMOTE || LONG ? min(w.kb1, kb + kAccKb) : w.kb1;
                     const int acc = j & 1;
                     if (!gwait_warp(acce + acc, ((j >> 1) & 1) ^ 1, &s_abort)) break;
                     ++j;
@@ -1197,6 +1206,42 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             if (w.splits == 1) fetch(half);
             bool ok = true;
             uint32_t d = 0;
+            const int64_t slab = 128 * BN;
+            [[maybe_unused]] float *sums_at = nullptr;
+            if constexpr (LONG) {
+                // a long sum: all but its last part go to the workspace, a lane's own elements each
+                if (w.kb1 - w.kb0 > kLongKb) {
+                    const int64_t own = w.splits > 1 ? ((int64_t)w.tile * w.splits + w.split) * CG + rank : blockIdx.x;
+                    sums_at = a.partial + own * slab + (q * 32 + lane) * 4;
+                    for (int kb = w.kb0; kb + kLongKb < w.kb1; kb += kLongKb) {
+                        const int acc = j & 1;
+                        ok = gwait_warp(accf + acc, (j >> 1) & 1, &s_abort);
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        d = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
+#pragma unroll 1
+                        for (int ci = half; ci < kChunks; ci += 2) {
+                            uint32_t r[32];
+                            tmem_ld_32cols(d + (uint32_t)(ci * 32), r);
+                            float4 *p = reinterpret_cast<float4 *>(sums_at + (int64_t)ci * 32 * 128);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                float4 f = kb == w.kb0 ? make_float4(0.f, 0.f, 0.f, 0.f) : p[e * 128];
+                                f.x += __uint_as_float(r[4 * e]), f.y += __uint_as_float(r[4 * e + 1]);
+                                f.z += __uint_as_float(r[4 * e + 2]), f.w += __uint_as_float(r[4 * e + 3]);
+                                p[e * 128] = f;
+                            }
+                        }
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0)
+                            asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(acce_bar[acc])
+                                         : "memory");
+                        ++j;
+                    }
+                    if (!ok) break;   // the abort flag is set
+                }
+            }
             if (!PROMOTE || w.kb1 - w.kb0 <= kPromoteKb) {
                 ok = gwait_warp(accf + (j & 1), (j >> 1) & 1, &s_abort);
                 if (!ok) break;
@@ -1243,7 +1288,6 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
 
             if (PROMOTE && u + ustep < a.units) ahead = unit_of<R>(a, u + ustep);
             bool last = true;
-            const int64_t slab = 128 * BN;
             float *part = nullptr;
             if (w.splits > 1) part = a.partial + ((int64_t)w.tile * w.splits * CG + rank) * slab + (q * 32 + lane) * 4;
 #pragma unroll 1
@@ -1271,6 +1315,15 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
                         tmem_ld_32cols(d + (uint32_t)(ci * 32), r);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = empty_sum ? 0.f : __uint_as_float(r[e]);
+                        if constexpr (LONG)
+                            if (sums_at != nullptr) {
+                                const float4 *p = reinterpret_cast<const float4 *>(sums_at + (int64_t)ci * 32 * 128);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const float4 f = p[e * 128];
+                                    v[4 * e] += f.x, v[4 * e + 1] += f.y, v[4 * e + 2] += f.z, v[4 * e + 3] += f.w;
+                                }
+                            }
                         if (i == kChunks / 2 - 1) {
                             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                             __syncwarp();

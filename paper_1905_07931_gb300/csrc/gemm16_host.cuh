@@ -171,7 +171,7 @@ int launch_tile(const GProduct &p, const GArgs &a, cudaStream_t s) {
     l.phases = 1;
     int rc = fill_set<CG, BN, EPI, PROMOTE>(p, l.args[0], l.maps[0]);
     if (rc != CSRT_OK) return rc;
-    constexpr auto kernel = gemm16_kernel<CG, BN, EPI, PROMOTE, GEN>;
+    constexpr auto kernel = gemm16_kernel<CG, BN, EPI, PROMOTE, GEN, false>;
     constexpr int smem = gsmem_bytes<CG, BN, EPI, PROMOTE>();
     rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
@@ -198,11 +198,20 @@ inline GChoice choose_tile(const GArgs &a, int64_t reduction, bool aligned) {
     return best;
 }
 
+// Stages of the longest accumulation that sharing `s` leaves of a reduction.
+inline int64_t longest(const GSplit &s, int64_t reduction) {
+    const int64_t kb = ceil_div<int64_t>(reduction, kGBK);
+    return s.splits == 1 || s.whole > 0 ? kb : ceil_div<int64_t>(kb, s.splits);
+}
+
+// A 16-bit result of sums too long for one accumulation is the promoting kernel's, in its general form.
 template <int EPI, bool PROMOTE>
 int launch_gemm16(const GProduct &p, GArgs a, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the dense products need a GPU with tcgen05");
     const bool aligned = aligned_set(a, PROMOTE);
     const GChoice choice = choose_tile(a, p.reduction, aligned);
+    if constexpr (!PROMOTE)
+        if (longest(choice.split, p.reduction) > (a.f16 ? kLongF16 : kLongBf16)) return launch_gemm16<EPI, true>(p, a, s);
     const int best = choice.tile;
     a.whole = choice.split.whole;
     a.splits = choice.split.splits;

@@ -311,8 +311,9 @@ static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
     }
 }
 
-// All steps in one cooperative launch on CG x 128 x BN tiles.
-template <int CG, int BN>
+// All steps in one cooperative launch on CG x 128 x BN tiles. LONG: a product has a long sum; the slabs of the slices are
+// then those of long sums too, so that either all tiles of a product are split or, with a slab for each CTA, none.
+template <int CG, int BN, bool LONG>
 static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     GLaunch<kEpiNs> n = {};
     int32_t units = 1;
@@ -321,7 +322,7 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
         GArgs &a = n.args[set];
         ns_product(q, set, p, a);
         // slices of different matrices' phases would share their place in the workspace
-        const GSplit split = q.batch == 1 ? best_splits(tile, a, p.reduction, true) : GSplit{0, 1, 0.};
+        const GSplit split = q.batch == 1 ? best_splits(tile, a, p.reduction, !LONG) : GSplit{0, 1, 0.};
         a.whole = split.whole;
         a.splits = split.splits;
         const int rc = fill_set<CG, BN, kEpiNs, false>(p, a, n.maps[set]);
@@ -334,7 +335,7 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     n.step_units[1] = n.args[2].units / q.batch;
     n.step_units[2] = n.args[3].units / q.batch;
 
-    constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false, false>;
+    constexpr auto kernel = gemm16_kernel<CG, BN, kEpiNs, false, false, LONG>;
     constexpr int smem = gsmem_bytes<CG, BN, kEpiNs, false>();
     const int rc = allow_smem<kernel>(smem);
     if (rc != CSRT_OK) return rc;
@@ -367,7 +368,9 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     attr[0].id = cudaLaunchAttributeCooperative;
     attr[0].val.cooperative = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(imin(units, imin(slots, imax(1, num_sms() / CG))) * CG));
+    slots = imin(slots, imax(1, num_sms() / CG));
+    if (LONG) slots = imin(slots, (int)(kPartialBytes / (CG * 128 * BN * sizeof(float))));
+    cfg.gridDim = dim3((unsigned)(imin(units, slots) * CG));
     cfg.blockDim = dim3(kGThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -378,6 +381,19 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
     return check_launch("gemm16_kernel (Newton-Schulz)");
 }
 
+// Whether a product would accumulate more than kLongKb stages at once on tiles t.
+static bool has_long_sum(const NsPlan &q, const GTile &t) {
+    if (imax(q.rows, q.cols) <= kLongKb * kGBK) return false;
+    for (int set : {0, 2, 3}) {
+        GProduct p;
+        GArgs a;
+        ns_product(q, set, p, a);
+        const GSplit split = q.batch == 1 ? best_splits(t, a, p.reduction, true) : GSplit{0, 1, 0.};
+        if (longest(split, p.reduction) > kLongKb) return true;
+    }
+    return false;
+}
+
 static int ns_products(const NsPlan &q, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the orthogonalisation needs a GPU with tcgen05");
     // By the number of 128 x 128 tiles of X (measured, us for the whole call on tiles 64, 128 by pairs and 256 by pairs
@@ -386,9 +402,11 @@ static int ns_products(const NsPlan &q, cudaStream_t s) {
     // 6 x 256 x 4096: 226 / 203 / 267; 4096 x 1000: 246 / 237 / 290); from 700 on, where L2 traffic counts most,
     // 256 x 256 (3 x 2048 x 2048: 738 / 487 / 442; 4096 x 4096: 1826 / 1188 / 1027; 4096 x 9216: 3747 / 2204 / 1858).
     const int64_t tiles = (int64_t)q.batch * ceil_div<int64_t>(q.rows, 128) * ceil_div<int64_t>(q.cols, 128);
-    if (tiles < 200) return launch_ns<1, 64>(q, kTiles[2], s);
-    if (tiles < 700) return launch_ns<2, 128>(q, kTiles[3], s);
-    return launch_ns<2, 256>(q, kTiles[0], s);
+    if (has_long_sum(q, kTiles[tiles < 200 ? 2 : tiles < 700 ? 3 : 0]))
+        return tiles < 700 ? launch_ns<2, 128, true>(q, kTiles[3], s) : launch_ns<2, 256, true>(q, kTiles[0], s);
+    if (tiles < 200) return launch_ns<1, 64, false>(q, kTiles[2], s);
+    if (tiles < 700) return launch_ns<2, 128, false>(q, kTiles[3], s);
+    return launch_ns<2, 256, false>(q, kTiles[0], s);
 }
 
 static int check_batch(const csrt_mat *m, const char *name, int32_t batch, int64_t stride) {

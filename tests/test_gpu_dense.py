@@ -400,3 +400,81 @@ def test_derivatives_far_from_zero(C, act, dtype, n):
     zz[0] = float("nan")
     C.dense_act_bwd(dy, zz, act, out)
     assert bool(out[0].isnan().all()) and not bool(out[1:].isnan().any())
+
+
+@pytest.mark.parametrize("kind,m,k,n,dtype,odd", [
+    ("dw", 2048, 2048, 300000, "f16", 0),     # whole sums
+    ("dw", 2000, 2001, 300000, "f16", 1),     # the same at odd rows
+    ("dw", 2048, 2048, 40000, "f16", 0),      # just above what float16 takes in one go
+    ("dw", 1000, 1000, 400000, "f16", 0),     # long slices
+    ("dw", 64, 60, 2000000, "f16", 0),        # one tile in as many slices as there are
+    ("dw", 2048, 2048, 1200000, "bf16", 0),
+    ("fwd", 2048, 300000, 2048, "f16", 0),
+    ("fwd", 2040, 300000, 2049, "f16", 1),
+    ("dx", 300000, 2048, 2048, "f16", 0),
+    ("dx", 300000, 2001, 2000, "f16", 1)])
+def test_long_sums_of_one_sign_are_rounded_once(C, kind, m, k, n, dtype, odd):
+    """16-bit results of long reductions. Up to 32768 (float16) or 131072 (bfloat16) terms lose at most 2^-23 of the
+    running sum with each block of 16; longer ones are float32 sums of 512 terms each, rounded to nearest (32 + chunks).
+    Then up to 32 slices, and the result's own rounding."""
+    gen, dt = _gen(m + k + n), DT[dtype]
+    lay = "odd" if odd else "tight"
+
+    def positive(rows, cols, f):
+        v = torch.rand(rows, cols, generator=gen, device="cuda", dtype=torch.float32).mul_(0.1 * f).add_(0.05 * f).to(dt)
+        if not odd:
+            return v
+        buf = torch.zeros(rows, cols + 5, dtype=dt, device="cuda")
+        buf[:, 3:3 + cols].copy_(v)
+        return buf[:, 3:3 + cols]
+
+    r = {"dw": n, "fwd": k, "dx": m}[kind]
+    f = min(1.0, math.sqrt(2e5 / r))       # within float16's range
+    ws = C.DenseWorkspace(m, k, n)
+    if kind == "dw":
+        a, b, out = positive(m, n, f), positive(k, n, f), _mat(gen, m, k, dt, lay)
+        C.dense_bwd_w(a, b, out, ws)
+        want = a[:64].double() @ b[:64].double().t()
+        far = a[-32:].double() @ b[-32:].double().t()
+    elif kind == "fwd":
+        a, b, out = positive(m, k, f), positive(k, n, f), _mat(gen, m, n, dt, lay)
+        C.dense_fwd(a, b, out, ws)
+        want, far = a[:64].double() @ b[:, :64].double(), a[-32:].double() @ b[:, -32:].double()
+    else:
+        a, b, out = positive(m, k, f), positive(m, n, f), _mat(gen, k, n, dt, lay)
+        C.dense_bwd_x(a, b, out, ws)
+        want, far = a[:, :64].double().t() @ b[:, :64].double(), a[:, -32:].double().t() @ b[:, -32:].double()
+    limit = 32768 if dtype == "f16" else 131072
+    tol = (max(min(r, limit) // 16, 32 + r // 512) + 32) * 2.0 ** -23
+    for got, exact in ((out[:64, :64], want), (out[-32:, -32:], far)):
+        exact = exact[:got.shape[0], :got.shape[1]]
+        assert float(exact.max()) < 6e4
+        _check(got, exact, tol * exact, dt)
+    assert ws.status()[0] == 0
+
+
+@pytest.mark.parametrize("kind,m,k,n", [("fwd", 200, 20000, 130), ("fwd", 2030, 70000, 2050), ("dx", 70000, 2000, 2001)])
+@pytest.mark.parametrize("layout", ["tight", "odd"])
+def test_long_sums_with_every_epilogue(C, kind, m, k, n, layout):
+    gen, dt = _gen(m + n), torch.float16
+    ws = C.DenseWorkspace(m, k, n)
+    w = _mat(gen, m, k, dt, layout, 1 / math.sqrt(k if kind == "fwd" else m))
+    if kind == "fwd":
+        x, b, r = _mat(gen, k, n, dt, layout), torch.randn(m, generator=gen, device="cuda"), _mat(gen, m, n, dt, layout)
+        y, z = _mat(gen, m, n, dt, layout), _mat(gen, m, n, dt, layout)
+        C.dense_fwd(w, x, y, ws, bias=b, act="silu", residual=r, z=z)
+        zz, s = w.double() @ x.double() + b.double()[:, None], w.double().abs() @ x.double().abs()
+        e = _sum_tol(min(k, 32768), s, dt)
+        _check(z, zz, e, dt)
+        want = _act(zz, "silu") + r.double()
+        _check(y, want, 1.13 * e + 2.0 ** -18 * zz.abs().clamp_min(1) + 2.0 ** -23 * (want.abs() + r.double().abs()), dt)
+    else:
+        dy, z, r = _mat(gen, m, n, dt, layout), _mat(gen, k, n, dt, layout), _mat(gen, k, n, dt, layout)
+        dx = _mat(gen, k, n, dt, layout)
+        C.dense_bwd_x(w, dy, dx, ws, z_below=z, act="gelu", residual=r)
+        prod, s = w.double().t() @ dy.double(), w.double().abs().t() @ dy.double().abs()
+        e = _sum_tol(min(m, 32768), s, dt)
+        want = prod * _act_grad(z.double(), "gelu") + r.double()
+        _check(dx, want, 1.13 * e + 2.0 ** -17 * prod.abs() * z.double().abs().clamp_min(1) +
+               2.0 ** -23 * (want.abs() + r.double().abs()), dt)
+    assert ws.status()[0] == 0

@@ -318,3 +318,35 @@ def test_factors_out_of_float32_range(C, m, k, steps):
                 assert bool(((o.double() - want).abs() <= 2.0 ** -22 * want.abs() + 2.0 ** -149).all())
             else:
                 assert _rel(o, want) <= 2e-3
+
+
+@pytest.mark.parametrize("batch,m,k", [(2, 64, 20000), (2, 130, 40000), (2, 64, 1200000), (2, 1200000, 40), (1, 33, 4000000),
+                                       (3, 300, 300000)])
+def test_very_long_matrices(C, batch, m, k):
+    """The Gram matrix's sums of squares, all of one sign, over a long side: 1.2e-4 of A at most (the tensor core's own
+    sums stop after 16384 terms), within what the bounds above allow."""
+    g = torch.randn(batch, m, k, generator=_gen(batch + m + k), device="cuda")
+    o, ws = torch.empty_like(g), C.OrthogonalizeWorkspace(batch, m, k)
+    C.orthogonalize(g, o, ws)
+    assert ws.status()[0] == 0
+    for i in range(batch):
+        assert _rel(o[i:i + 1], _exact(g[i:i + 1].double(), 5, 1e-7, 1.0)) <= 2e-3
+
+
+def test_short_side_of_many_thousands(C):
+    """All three products have long sums. u = Q1 diag(s) Q2^T, so that the iteration acts on s alone. Where u is zero the
+    roundings grow as csrtrain.h says: a few 1e-3."""
+    n, r = 16640, 512
+    gen = _gen(77)
+    q1, _ = torch.linalg.qr(torch.randn(n, r, generator=gen, device="cuda").double())
+    q2, _ = torch.linalg.qr(torch.randn(n, r, generator=gen, device="cuda").double())
+    s = 1.0 + torch.rand(r, generator=gen, device="cuda").double()
+    g = ((q1 * s) @ q2.t()).float()[None].contiguous()
+    o, ws = torch.empty_like(g), C.OrthogonalizeWorkspace(1, n, n)
+    C.orthogonalize(g, o, ws)
+    p = s / s.norm()
+    for _ in range(5):
+        p = A * p + B * p ** 3 + CC * p ** 5
+    want = (q1 * p) @ q2.t()
+    assert ws.status()[0] == 0
+    assert _rel(o[0], want) <= 4e-3
