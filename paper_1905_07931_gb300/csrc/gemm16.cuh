@@ -546,17 +546,17 @@ template <bool F16>
 __device__ __forceinline__ float warp_row_sum(const uint16_t *p, int cols, bool vec) {
     const int lane = threadIdx.x & 31;
     float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-    int c = vec ? cols & ~7 : 0;
+    const uint32_t n = (uint32_t)cols, c = vec ? n & ~7u : 0;   // unsigned: t may pass 2^31 on its last step
     if (vec) {
 #pragma unroll 4
-        for (int t = lane * 8; t < c; t += 256) {
+        for (uint32_t t = lane * 8; t < c; t += 256) {
             const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p + t));
             const float2 x = unpack16(u.x, F16), y = unpack16(u.y, F16), z = unpack16(u.z, F16), w = unpack16(u.w, F16);
             s0 += x.x + x.y, s1 += y.x + y.y, s2 += z.x + z.y, s3 += w.x + w.y;
         }
     }
 #pragma unroll 4
-    for (int t = c + lane; t < cols; t += 32) s0 += load1(p, t, F16 ? CSRT_DT_F16 : CSRT_DT_BF16);
+    for (uint32_t t = c + lane; t < n; t += 32) s0 += load1(p, t, F16 ? CSRT_DT_F16 : CSRT_DT_BF16);
     float s = (s0 + s1) + (s2 + s3);
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -1140,7 +1140,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
         if constexpr (EPI == kEpiBwd) {   // the bias gradient beside the product: two rows of dy at a time
             const GArgs &a = L.args[0];
             if (a.sum_dst != nullptr)
-                for (int r = blockIdx.x * 2 + warp - 2; r < a.sum_rows; r += gridDim.x * 2) {
+                for (uint32_t r = blockIdx.x * 2 + warp - 2; r < (uint32_t)a.sum_rows; r += gridDim.x * 2) {
                     const uint16_t *p = a.sum_src + (int64_t)r * a.sum_ld;
                     const float t = a.f16 ? warp_row_sum<true>(p, a.sum_cols, a.sum_vec)
                                           : warp_row_sum<false>(p, a.sum_cols, a.sum_vec);

@@ -478,3 +478,39 @@ def test_long_sums_with_every_epilogue(C, kind, m, k, n, layout):
         _check(dx, want, 1.13 * e + 2.0 ** -17 * prod.abs() * z.double().abs().clamp_min(1) +
                2.0 ** -23 * (want.abs() + r.double().abs()), dt)
     assert ws.status()[0] == 0
+
+
+def _marked(rows, cols, at):
+    """bfloat16 zeros with powers of two at the given places, so that every order of a sum is exact."""
+    t = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    for i, (r, c) in enumerate(at):
+        t[r, c] = 2.0 ** (i % 8)
+    return t
+
+
+@pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31 - 8])
+@pytest.mark.parametrize("k", [0, 1])
+def test_bias_gradient_of_rows_near_2_31_columns(C, n, k):
+    """The last steps of a row's sum pass 2^31; with the product's idle warps (k = 1) and by itself."""
+    at = [(0, 0), (0, 2 ** 30), (0, 2 ** 31 - 300), (0, 2 ** 31 - 40), (0, n - 9), (0, n - 1)]
+    dy, x = _marked(1, n, at), torch.ones(k, n, dtype=torch.bfloat16, device="cuda")
+    dw, db, ws = torch.zeros(1, k, device="cuda"), torch.zeros(1, device="cuda"), C.DenseWorkspace(1, k, n)
+    C.dense_bwd_w(dy, x, dw, ws, db=db)
+    assert float(db) == 63.0 and bool((dw == 63.0).all())
+    assert ws.status()[0] == 0
+    del dy, x, ws
+    torch.cuda.empty_cache()
+
+
+def test_bias_gradient_near_2_31_rows(C):
+    m = 2 ** 31 - 100
+    rows = [0, 2 ** 30 + 1, m - 305, m - 204, m - 1]
+    dy, x = _marked(m, 1, [(r, 0) for r in rows]), torch.ones(1, 1, dtype=torch.bfloat16, device="cuda")
+    dw, db, ws = torch.empty(m, 1, device="cuda"), torch.empty(m, device="cuda"), C.DenseWorkspace(m, 1, 1)
+    C.dense_bwd_w(dy, x, dw, ws, db=db)
+    for got in (dw.view(-1), db):
+        assert [float(got[r]) for r in rows] == [1.0, 2.0, 4.0, 8.0, 16.0]
+        assert int(torch.count_nonzero(got)) == 5 and float(got.sum()) == 31.0
+    assert ws.status()[0] == 0
+    del dy, dw, db, ws, got
+    torch.cuda.empty_cache()
