@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kTokWarps * 32, N == 1 ? 0 : tok_blocks(N)) de
             }
         } else {
 #pragma unroll 8
-            for (int t = part * 32 + lane; t < a.k; t += a.wpr * 32) {
+            for (uint32_t t = part * 32 + lane; t < (uint32_t)a.k; t += a.wpr * 32) {   // t may pass 2^31 on its last step
                 float xf[N];
 #pragma unroll
                 for (int c = 0; c < N; ++c) xf[c] = load1(a.x, (int64_t)t * a.ldx + c, dtype);

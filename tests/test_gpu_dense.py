@@ -514,3 +514,15 @@ def test_bias_gradient_near_2_31_rows(C):
     assert ws.status()[0] == 0
     del dy, dw, db, ws, got
     torch.cuda.empty_cache()
+
+
+def test_one_token_of_nearly_2_31_inputs(C):
+    k = 2 ** 31 - 9      # no multiple of eight: a lane's last steps pass 2^31
+    w = _marked(2, k, [(0, 0), (1, 1), (0, 2 ** 31 - 300), (1, 2 ** 31 - 40), (0, k - 2), (1, k - 1)])
+    x, y = torch.ones(k, 1, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 1, device="cuda")
+    ws = C.DenseWorkspace(2, k, 1)
+    C.dense_fwd(w, x, y, ws)
+    assert y.view(-1).tolist() == [1.0 + 4 + 16, 2.0 + 8 + 32]
+    assert ws.status()[0] == 0
+    del w, x, ws
+    torch.cuda.empty_cache()
