@@ -20,7 +20,7 @@ static size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static int check_mat(const csrt_mat *m, const char *name) {
     CSRT_ARG(m != nullptr, "%s is NULL", name);
     CSRT_ARG(m->rows >= 0 && m->cols >= 0, "%s: negative size", name);
-    CSRT_ARG(m->ld >= m->cols && (m->rows == 0 || m->ld < kMaxElems / (m->rows + 1)), "%s: bad ld", name);
+    CSRT_ARG(m->ld >= m->cols && (m->rows == 0 || m->ld < kMaxElems / ((int64_t)m->rows + 1)), "%s: bad ld", name);
     CSRT_ARG(m->dtype == CSRT_DT_F32 || m->dtype == CSRT_DT_BF16 || m->dtype == CSRT_DT_F16, "%s: unknown dtype", name);
     CSRT_ARG(m->data != nullptr || m->rows == 0 || m->cols == 0, "%s: data is NULL", name);
     CSRT_ARG(reinterpret_cast<uintptr_t>(m->data) % dt_size(m->dtype) == 0, "%s: data is not aligned to its type", name);

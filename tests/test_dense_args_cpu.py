@@ -122,3 +122,11 @@ def test_orthogonalize_refuses(C):
     assert L.csrt_orthogonalize_workspace_bytes(3, 300, 784, ctypes.byref(n)) == 0 and n.value > 3 * 300 * 784 * 6
     _expect(C, L.csrt_orthogonalize_workspace_bytes(1, 1 << 16, 1 << 16, ctypes.byref(n)), "2^31")
     _expect(C, L.csrt_dense_workspace_bytes(-1, 3, 3, ctypes.byref(n)), "negative")
+
+
+def test_the_largest_number_of_rows_is_taken(C):
+    """2^31 - 1 rows pass the check of the leading dimension (the call then fails on the output's shape)."""
+    L, m = C.lib(), 2 ** 31 - 1
+    w, x = _m(C, 1, m, 1), _m(C, 2, 1, 4)
+    _expect(C, L.csrt_dense_fwd(w, x, None, 0, None, None, _m(C, 3, 8, 4), WS, BIG, None), f"y is 8 x 4, must be {m} x 4")
+    _expect(C, L.csrt_dense_fwd(_m(C, 1, m, 1, ld=1 << 10), x, None, 0, None, None, _m(C, 3, 8, 4), WS, BIG, None), "w: bad ld")
