@@ -1181,7 +1181,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             const bool in32 = !GEN && PROMOTE && a.c1.p != nullptr && a.c0.p == nullptr;   // its place is u0 and u1
             if constexpr (!GEN) {
                 if (NS && a.kind == kNsApply) {
-                    g0 = ahead_of_f32(a.c0, w.b, row - lane, n0, a.m, (int)a.c0.ld);
+                    g0 = ahead_of_f32(a.c0, w.b, row - lane, n0, a.m, (int)imin<int64_t>(a.c0.ld, INT32_MAX));
                 } else if (in32) {
                     g0 = ahead_of_f32(a.c1, w.b, row - lane, n0, a.m, a.n);
                 } else {

@@ -113,7 +113,7 @@ __device__ __forceinline__ double block_sum(double v) {
 __global__ void __launch_bounds__(kPrepThreads) ortho_momentum_kernel(PrepArgs a) {
     pdl_enter();
     const int b = blockIdx.y;
-    const uint32_t per_row = (uint32_t)(a.cols + 7) / 8, total = per_row * (uint32_t)a.rows;
+    const uint32_t per_row = ((uint32_t)a.cols + 7) / 8, total = per_row * (uint32_t)a.rows;
     double sum = 0.0;
     for (uint32_t t = blockIdx.x * kPrepThreads + threadIdx.x; t < total; t += gridDim.x * kPrepThreads) {
         const uint32_t r = t / per_row, c = (t - r * per_row) * 8;
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kPrepThreads) ortho_scale_kernel(PrepArgs a) {
         if (fabs(rest) < 0x1p-126) f1 = 0x1p-90f, rest *= 0x1p90;
     }
     const float f = (float)rest;
-    const uint32_t per_row = (uint32_t)(a.cols + 7) / 8, total = per_row * (uint32_t)a.rows;
+    const uint32_t per_row = ((uint32_t)a.cols + 7) / 8, total = per_row * (uint32_t)a.rows;
     for (uint32_t t = blockIdx.x * kPrepThreads + threadIdx.x; t < total; t += gridDim.x * kPrepThreads) {
         const uint32_t r = t / per_row, c = (t - r * per_row) * 8;
         const int cnt = min(8, a.cols - (int)c);
@@ -497,7 +497,7 @@ int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float
     p.o.stride = o_stride;
     p.o.dtype = o->dtype;
     p.o.vec = tma_rows_ok(o->data, o->ld, dt_size(o->dtype)) && (batch == 1 || o_stride * dt_size(o->dtype) % 16 == 0);
-    const int64_t chunks = (int64_t)rows * ((cols + 7) / 8);
+    const int64_t chunks = rows * (((int64_t)cols + 7) / 8);
     int64_t blocks = imin<int64_t>(ceil_div<int64_t>(chunks, kPrepThreads), kPrepBlocks);
     blocks = imin<int64_t>(blocks, imax<int64_t>(1, (int64_t)num_sms() * 8 / batch));
     const dim3 grid((unsigned)blocks, (unsigned)batch);

@@ -350,3 +350,25 @@ def test_short_side_of_many_thousands(C):
     want = (q1 * p) @ q2.t()
     assert ws.status()[0] == 0
     assert _rel(o[0], want) <= 4e-3
+
+
+def test_a_row_of_nearly_2_31_elements(C):
+    """A vector has one singular value: o is the iteration's scalar times the unit vector."""
+    n = 2 ** 31 - 1
+    m, k = 1, n
+    g = torch.zeros(m, k, device="cuda")
+    o = torch.full((m, k), float("nan"), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 5, 2 ** 30, n - 300, n - 9, n - 1], device="cuda")
+    g.view(-1)[at] = torch.tensor([3.0, -1.0, 2.0, -4.0, 0.5, 1.5], device="cuda")
+    ws = C.OrthogonalizeWorkspace(1, m, k)
+    C.orthogonalize(g, o, ws, steps=2)
+    v = g.view(-1)[at].double()
+    p = 1.0
+    for _ in range(2):
+        p = A * p + B * p ** 3 + CC * p ** 5
+    assert ws.status()[0] == 0
+    # X's float16 copies, the Gram sum and o's own rounding
+    assert _rel(o.view(-1)[at], p * v / v.norm()) <= 3e-3
+    assert int(torch.count_nonzero(o)) == 6
+    del g, o, ws
+    torch.cuda.empty_cache()
