@@ -31,6 +31,7 @@ namespace csrt {
 
 constexpr int kPrepThreads = 256;
 constexpr int kPrepBlocks = 1024;   // most blocks (norm partials) per matrix
+constexpr int kOneByOne = 1 << 26;  // longest side that the matrices of a batch may have in one launch
 
 struct PrepArgs {
     GMat g;                 // gradient
@@ -215,7 +216,7 @@ static OrthoLayout layout(int64_t batch, int64_t rows, int64_t cols) {
 }
 
 struct NsPlan {
-    int32_t batch, rows, cols, steps;
+    int32_t first, batch, rows, cols, steps;   // matrices first .. first + batch - 1
     float scale;
     char *base;
     OrthoLayout l;
@@ -242,20 +243,20 @@ static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
     const int32_t sh = tall ? q.cols : q.rows;
     auto mat = [&](size_t off, int64_t ld, int64_t n_rows) {
         GMat m = {};
-        m.p = q.base + off;
         m.ld = ld;
         m.stride = ld * n_rows;
-        m.dtype = CSRT_DT_F16;
+        m.dtype = off == l.xf ? CSRT_DT_F32 : CSRT_DT_F16;
+        m.p = q.base + off + q.first * m.stride * dt_size(m.dtype);
         m.vec = m.pad = 1;
         return m;
     };
     auto op = [&](size_t off, int64_t r, int64_t c, int64_t ld) {
         GOperand o;
-        o.p = q.base + off;
         o.rows = r;
         o.cols = c;
         o.ld = ld;
         o.stride = r * ld;
+        o.p = q.base + off + q.first * o.stride * 2;
         return o;
     };
     a = GArgs{};
@@ -266,7 +267,8 @@ static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
     a.partial = reinterpret_cast<float *>(q.base + l.slices);
     a.s_pad = (int32_t)l.lds;
     a.tall = tall;
-    float *diag_a = reinterpret_cast<float *>(q.base + l.diag_a), *diag_b = reinterpret_cast<float *>(q.base + l.diag_b);
+    float *diag_a = reinterpret_cast<float *>(q.base + l.diag_a) + q.first * l.lds;
+    float *diag_b = reinterpret_cast<float *>(q.base + l.diag_b) + q.first * l.lds;
     const size_t x = set == 1 || set == 4 || (set == 5 && (q.steps - 1) % 2) ? l.x1 : l.x0;
     const GOperand ox = op(x, q.rows, q.cols, l.ldx), oa = op(l.a, sh, sh, l.lds), ob = op(l.b, sh, sh, l.lds);
     if (set <= 1) {          // A = X X^T or X^T X, times 2^15
@@ -305,7 +307,6 @@ static void ns_product(const NsPlan &q, int set, GProduct &p, GArgs &a) {
         a.gamma = out ? q.scale * kInvXScale : 1.f;
         a.diag_in = diag_b;
         a.c0 = mat(l.xf, l.ldx, q.rows);
-        a.c0.dtype = CSRT_DT_F32;
         a.out0 = out ? q.o : mat(x == l.x0 ? l.x1 : l.x0, l.ldx, q.rows);
         if (!out) a.out1 = a.c0;
     }
@@ -330,7 +331,7 @@ static int launch_ns(const NsPlan &q, const GTile &tile, cudaStream_t s) {
         units = imax(units, a.units);
     }
     n.phases = 3 * q.steps;
-    n.done = reinterpret_cast<uint32_t *>(q.base + q.l.done);
+    n.done = reinterpret_cast<uint32_t *>(q.base + q.l.done) + q.first;
     n.step_units[0] = n.args[0].units / q.batch;
     n.step_units[1] = n.args[2].units / q.batch;
     n.step_units[2] = n.args[3].units / q.batch;
@@ -396,6 +397,19 @@ static bool has_long_sum(const NsPlan &q, const GTile &t) {
 
 static int ns_products(const NsPlan &q, cudaStream_t s) {
     if (!device_is_sm10x()) return fail(CSRT_ERR_CUDA, "the orthogonalisation needs a GPU with tcgen05");
+    // The units of a batch are not sliced: one that walks a side of hundreds of millions would outlast the others' bounded
+    // wait for it (two seconds), so that such matrices, 0.3 s to a slice at most, go one by one.
+    if (q.batch > 1 && imax(q.rows, q.cols) > kOneByOne) {
+        for (int32_t b = 0; b < q.batch; ++b) {
+            NsPlan one = q;
+            one.first = b;
+            one.batch = 1;
+            one.o.p = static_cast<char *>(q.o.p) + b * q.o.stride * dt_size(q.o.dtype);
+            const int rc = ns_products(one, s);
+            if (rc != CSRT_OK) return rc;
+        }
+        return CSRT_OK;
+    }
     // By the number of 128 x 128 tiles of X (measured, us for the whole call on tiles 64, 128 by pairs and 256 by pairs
     // wide): few tiles take the narrow ones, which share the work among more SMs (1024 x 1024: 123 / 147 / 217;
     // 3 x 2048 x 512: 154 / 174 / 239); from 200 tiles on pairs of SMs on 256 x 128 (2048 x 2048: 334 / 247 / 306;
@@ -508,6 +522,7 @@ int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float
     if (rc != CSRT_OK || steps == 0) return rc;
 
     NsPlan plan;
+    plan.first = 0;
     plan.batch = batch;
     plan.rows = rows;
     plan.cols = cols;

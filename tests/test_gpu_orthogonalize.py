@@ -372,3 +372,40 @@ def test_a_row_of_nearly_2_31_elements(C):
     assert int(torch.count_nonzero(o)) == 6
     del g, o, ws
     torch.cuda.empty_cache()
+
+
+def test_a_batch_of_the_longest_rows(C):
+    """Two rows of nearly 2^31 elements in one call: their sums are shared among the SMs, so that no unit waits for seconds."""
+    n, batch = 2 ** 31 - 1, 2
+    g = torch.zeros(batch, 1, n, device="cuda")
+    o = torch.full((batch, 1, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 2 ** 30, n - 9, n - 1], device="cuda")
+    vals = torch.tensor([[3.0, -1.0, 2.0, 0.5], [1.0, 4.0, -2.0, 8.0]], device="cuda")
+    for i in range(batch):
+        g[i, 0, at] = vals[i]
+    ws = C.OrthogonalizeWorkspace(batch, 1, n)
+    C.orthogonalize(g, o, ws, steps=1)
+    assert ws.status()[0] == 0
+    for i in range(batch):
+        v = vals[i].double() / vals[i].double().norm()
+        assert _rel(o[i, 0, at], (A + B + CC) * v) <= 3e-3
+    assert int(torch.count_nonzero(o)) == 8
+    del g, o, ws
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("odt", [torch.float32, torch.bfloat16])
+def test_long_batches_one_by_one(C, odt):
+    """Matrices that a call takes one after the other give what each gives by itself, bit for bit."""
+    batch, k = 2, 2 ** 26 + 64
+    g = torch.randn(batch, 2, k, generator=_gen(91), device="cuda")
+    o, ws = torch.empty(batch, 2, k, dtype=odt, device="cuda"), C.OrthogonalizeWorkspace(batch, 2, k)
+    C.orthogonalize(g, o, ws, steps=2)
+    one, wso = torch.empty(2, k, dtype=odt, device="cuda"), C.OrthogonalizeWorkspace(1, 2, k)
+    for i in range(batch):
+        C.orthogonalize(g[i], one, wso, steps=2)
+        assert torch.equal(one, o[i])
+    assert ws.status()[0] == 0
+    assert _rel(o, _exact(g.double(), 2, 1e-7, 1.0)) <= (2e-3 if odt == torch.float32 else 3e-3)
+    del g, o, ws, one, wso
+    torch.cuda.empty_cache()
