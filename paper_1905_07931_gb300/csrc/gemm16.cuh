@@ -422,7 +422,7 @@ __device__ __forceinline__ void load32(float (&v)[32], const GMat &c, int b, int
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (row < m && col + 4 * i + 4 <= n) {
+            if (row < m && 4 * i + 4 <= n - col) {
                 f = *reinterpret_cast<const float4 *>(p + 4 * i);
             } else if (row < m) {
                 if (col + 4 * i < n) f.x = p[4 * i];

@@ -526,3 +526,27 @@ def test_one_token_of_nearly_2_31_inputs(C):
     assert ws.status()[0] == 0
     del w, x, ws
     torch.cuda.empty_cache()
+
+
+def test_nearly_2_31_columns(C):
+    """One row of 2^31 - 1 columns through the epilogues: a float32 residual of aligned rows, z and bias at odd ones."""
+    n = 2 ** 31 - 1
+    at = torch.tensor([0, 1, 2 ** 30, n - 32, n - 4, n - 1], device="cuda")
+    vals = torch.tensor([1.0, -2.0, 3.0, -4.0, 5.0, 6.0], device="cuda")
+    x = torch.zeros(1, n, dtype=torch.bfloat16, device="cuda")
+    x[0, at] = vals.bfloat16()
+    r = torch.empty(1, n + 1, device="cuda")[:, :n]
+    r.fill_(0.5)
+    w, b = torch.full((1, 1), 2.0, dtype=torch.bfloat16, device="cuda"), torch.ones(1, device="cuda")
+    y, ws = torch.empty(1, n, device="cuda"), C.DenseWorkspace(1, 1, n)
+    C.dense_fwd(w, x, y, ws, bias=b, residual=r.as_strided((1, n), (n + 1, 1)))
+    assert torch.equal(y[0, at], 2 * vals + 1.5) and int((y == 1.5).sum()) == n - 6
+    z = torch.ones(1, n, dtype=torch.bfloat16, device="cuda")
+    z[0, at[1]] = -1.0
+    C.dense_bwd_x(w, x, y, ws, z_below=z, act="relu", residual=r.as_strided((1, n), (n + 1, 1)))
+    want = 2 * vals + 0.5
+    want[1] = 0.5
+    assert torch.equal(y[0, at], want) and int((y == 0.5).sum()) == n - 5
+    assert ws.status()[0] == 0
+    del x, r, y, z, ws
+    torch.cuda.empty_cache()
