@@ -353,7 +353,7 @@ int csrt_dense_workspace_bytes(int32_t m, int32_t k, int32_t max_n, size_t *byte
  * (M floats), residual (M x n, y's type) and z may be NULL; z (M x n, w's
  * type) receives the pre-activation W x + bias. y is M x n, of w's type or
  * float32. residual may be y itself (same data and ld); w, x, y and z must
- * not overlap otherwise. Any sizes, n = 1 (one token) and 0 among them; rows
+ * not overlap otherwise, nor bias and y or z. Any sizes, n = 1 (one token) and 0 among them; rows
  * that are 16-byte aligned (data and ld) are read and written in place by
  * TMA, others are copied once into the workspace or stored piecewise. */
 int csrt_dense_fwd(const csrt_mat *w, const csrt_mat *x, const float *bias, int32_t act, const csrt_mat *residual,
@@ -369,8 +369,8 @@ int csrt_dense_bwd_x(const csrt_mat *w, const csrt_mat *dy, const csrt_mat *z_be
                      const csrt_mat *residual, csrt_mat *dx, void *ws, size_t ws_bytes, void *stream);
 
 /* csrt_dense_bwd_w -- gradients of a layer's weights and bias: dw = dy x^T
- * (M x K) and db[i] = sum_c dy[i, c] (M floats, may be NULL), both added to
- * what is there when accumulate != 0. No 1/n factor. dw is float32 or of dy's
+ * (M x K) and db[i] = sum_c dy[i, c] (M floats, may be NULL; no part of the
+ * matrices), both added to what is there when accumulate != 0. No 1/n factor. dw is float32 or of dy's
  * type; float32 sums are rounded to nearest every 512 columns (the tensor
  * core's own accumulation truncates). */
 int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, csrt_mat *dw, float *db, void *ws,

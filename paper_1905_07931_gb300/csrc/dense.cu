@@ -62,6 +62,24 @@ static bool clash(const csrt_mat *out, const csrt_mat *in) {
     return true;
 }
 
+// Whether a float32 vector of n elements (may be NULL) shares bytes with a matrix's elements: it may lie between two rows.
+static bool vector_meets(const float *v, int64_t n, const csrt_mat *m) {
+    csrt_mat flat = {};
+    flat.data = const_cast<float *>(v);
+    flat.rows = 1;
+    flat.cols = (int32_t)n;
+    flat.ld = n;
+    flat.dtype = CSRT_DT_F32;
+    if (v == nullptr || !overlap(m, &flat)) return false;
+    const int64_t row = m->ld * dt_size(m->dtype), used = m->cols * (int64_t)dt_size(m->dtype);
+    const int64_t d = reinterpret_cast<const char *>(v) - static_cast<const char *>(m->data);
+    return d < 0 || d % row < used || d % row + n * 4 > row;
+}
+static int check_vector(const float *v, const char *name) {
+    CSRT_ARG(reinterpret_cast<uintptr_t>(v) % 4 == 0, "%s is not aligned to its type", name);
+    return CSRT_OK;
+}
+
 // ---------------------------------------------------------------------------
 // Copy of an operand whose rows are not 16-byte aligned into padded rows. A thread takes the eight elements of an
 // aligned 16-byte store out of the one or two aligned 16-byte words that hold them (as long as those lie within the
@@ -246,6 +264,9 @@ int csrt_dense_fwd(const csrt_mat *w, const csrt_mat *x, const float *bias, int3
         CSRT_ARG(!clash(z, y) && !clash(z, x) && !clash(z, w) && (residual == nullptr || !clash(z, residual)),
                  "z overlaps another matrix");
     }
+    CSRT_TRY(check_vector(bias, "bias"));
+    CSRT_ARG(!vector_meets(bias, m, y), "bias overlaps y");
+    CSRT_ARG(z == nullptr || !vector_meets(bias, m, z), "bias overlaps z");
     CSRT_ARG(!clash(y, x) && !clash(y, w), "y overlaps an operand");
     if (m == 0 || n == 0) return CSRT_OK;
     if (n <= kTokensMax) {
@@ -316,6 +337,10 @@ int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, 
     CSRT_TRY(check_call(dy, "dy", x, "x", m, k, n, ws, ws_bytes));
     CSRT_TRY(check_out(dw, "dw", dy->dtype));
     CSRT_ARG(!clash(dw, dy) && !clash(dw, x), "dw overlaps an operand");
+    CSRT_TRY(check_vector(db, "db"));
+    CSRT_ARG(!vector_meets(db, m, dw), "db overlaps dw");
+    CSRT_ARG(!vector_meets(db, m, dy), "db overlaps dy");
+    CSRT_ARG(!vector_meets(db, m, x), "db overlaps x");
     cudaStream_t s = as_stream(stream);
     GArgs a = {};
     if (accumulate) a.c1 = epi_mat(dw);

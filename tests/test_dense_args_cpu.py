@@ -130,3 +130,29 @@ def test_the_largest_number_of_rows_is_taken(C):
     w, x = _m(C, 1, m, 1), _m(C, 2, 1, 4)
     _expect(C, L.csrt_dense_fwd(w, x, None, 0, None, None, _m(C, 3, 8, 4), WS, BIG, None), f"y is 8 x 4, must be {m} x 4")
     _expect(C, L.csrt_dense_fwd(_m(C, 1, m, 1, ld=1 << 10), x, None, 0, None, None, _m(C, 3, 8, 4), WS, BIG, None), "w: bad ld")
+
+
+def test_bias_and_its_gradient_are_checked(C):
+    """float32 vectors off their alignment, or over a matrix that the call writes (db also over one that it reads)."""
+    L, vp = C.lib(), ctypes.c_void_p
+    w, x, y, z = _m(C, 1, 8, 16), _m(C, 2, 16, 4), _m(C, 3, 8, 4), _m(C, 4, 8, 4)
+
+    def fwd(bias, y=y):
+        return L.csrt_dense_fwd(w, x, vp(bias), 0, None, z, y, WS, BIG, None)
+
+    _expect(C, fwd(A * 9 + 2), "bias is not aligned")
+    _expect(C, fwd(A * 3 + 32), "bias overlaps y")
+    _expect(C, fwd(A * 4 - 16), "bias overlaps z")
+    _expect(C, fwd(A * 3 + 64 * 7 + 4, y=_m(C, 3, 8, 4, ld=32)), "bias overlaps y")
+    # beside y's rows, or after its last one, it is no overlap: the call goes on to the next check, which this y fails
+    for at in (A + 8, A + 32, A + 64 * 7 + 8):
+        _expect(C, fwd(at, y=_m(C, 1, 8, 4, ld=32)), "y overlaps an operand")
+    dy, xx, dw = _m(C, 1, 8, 4), _m(C, 2, 16, 4), _m(C, 5, 8, 16, dtype=0)
+
+    def bwd(db):
+        return L.csrt_dense_bwd_w(dy, xx, 0, dw, vp(db), WS, BIG, None)
+
+    _expect(C, bwd(A * 9 + 1), "db is not aligned")
+    _expect(C, bwd(A * 5 + 128), "db overlaps dw")
+    _expect(C, bwd(A * 1 + 32), "db overlaps dy")
+    _expect(C, bwd(A * 2 - 4), "db overlaps x")
