@@ -95,7 +95,7 @@ struct GArgs {
     const float *bias;
     const uint16_t *sum_src;          // kEpiBwd: matrix whose row sums the idle warps leave in sum_dst (NULL: none)
     int64_t sum_ld;
-    int32_t sum_rows, sum_cols, sum_vec, sum_add;
+    int32_t sum_rows, sum_cols, sum_add;
     float *sum_dst;
     int32_t act;                      // activation (kEpiFwd), or act' of c0 as a factor (kEpiBwd)
     int32_t kind, sym, tall;          // kEpiNs: kNs*, tiles on and above the diagonal only, X has more rows than columns
@@ -541,22 +541,19 @@ __device__ __forceinline__ void emit(const GArgs &a, const GMaps &maps, const ui
     }
 }
 
-// Sum of a row of 16-bit elements by a warp: four 16-byte loads a lane in flight, float32, lanes joined at the end.
+// Sum of a 16-byte aligned row of 16-bit elements by a warp: four 16-byte loads a lane in flight, float32, lanes joined at the end.
 template <bool F16>
-__device__ __forceinline__ float warp_row_sum(const uint16_t *p, int cols, bool vec) {
+__device__ __forceinline__ float warp_row_sum(const uint16_t *p, int cols) {
     const int lane = threadIdx.x & 31;
     float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-    const uint32_t n = (uint32_t)cols, c = vec ? n & ~7u : 0;   // unsigned: t may pass 2^31 on its last step
-    if (vec) {
+    const uint32_t n = (uint32_t)cols, c = n & ~7u;   // unsigned: t may pass 2^31 on its last step
 #pragma unroll 4
-        for (uint32_t t = lane * 8; t < c; t += 256) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p + t));
-            const float2 x = unpack16(u.x, F16), y = unpack16(u.y, F16), z = unpack16(u.z, F16), w = unpack16(u.w, F16);
-            s0 += x.x + x.y, s1 += y.x + y.y, s2 += z.x + z.y, s3 += w.x + w.y;
-        }
+    for (uint32_t t = lane * 8; t < c; t += 256) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p + t));
+        const float2 x = unpack16(u.x, F16), y = unpack16(u.y, F16), z = unpack16(u.z, F16), w = unpack16(u.w, F16);
+        s0 += x.x + x.y, s1 += y.x + y.y, s2 += z.x + z.y, s3 += w.x + w.y;
     }
-#pragma unroll 4
-    for (uint32_t t = c + lane; t < n; t += 32) s0 += load1(p, t, F16 ? CSRT_DT_F16 : CSRT_DT_BF16);
+    if (c + lane < n) s0 += load1(p, c + lane, F16 ? CSRT_DT_F16 : CSRT_DT_BF16);
     float s = (s0 + s1) + (s2 + s3);
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -1142,8 +1139,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kGThreads, 1)
             if (a.sum_dst != nullptr)
                 for (uint32_t r = blockIdx.x * 2 + warp - 2; r < (uint32_t)a.sum_rows; r += gridDim.x * 2) {
                     const uint16_t *p = a.sum_src + (int64_t)r * a.sum_ld;
-                    const float t = a.f16 ? warp_row_sum<true>(p, a.sum_cols, a.sum_vec)
-                                          : warp_row_sum<false>(p, a.sum_cols, a.sum_vec);
+                    const float t = a.f16 ? warp_row_sum<true>(p, a.sum_cols) : warp_row_sum<false>(p, a.sum_cols);
                     if (lane == 0) a.sum_dst[r] = a.sum_add ? a.sum_dst[r] + t : t;
                 }
         }

@@ -550,3 +550,21 @@ def test_nearly_2_31_columns(C):
     assert ws.status()[0] == 0
     del x, r, y, z, ws
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("m,k,n", [(512, 640, 777), (1000, 520, 1777), (4096, 1024, 1025)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_bias_gradient_of_unaligned_rows_is_the_aligned_ones(C, m, k, n, accumulate):
+    """The row sums that go along with a product are taken of aligned rows in either case, in one order."""
+    gen, ws, res = _gen(m + n), C.DenseWorkspace(m, k, n), []
+    v, x = _mat(gen, m, n, torch.bfloat16), _mat(gen, k, n, torch.bfloat16)
+    for off, wide in ((0, (n + 63) // 64 * 64), (3, n + 6)):
+        buf = torch.full((m, wide), float("nan"), dtype=torch.bfloat16, device="cuda")
+        dy = buf[:, off:off + n]
+        dy.copy_(v)
+        dw, db = torch.ones(m, k, device="cuda"), torch.ones(m, device="cuda")
+        C.dense_bwd_w(dy, x, dw, ws, db=db, accumulate=accumulate)
+        res.append((dw, db))
+    assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
+    want = v.double().sum(1) + accumulate
+    _check(res[1][1], want, (n / 32 + 17) * 2.0 ** -23 * (v.double().abs().sum(1) + 1), torch.float32)
