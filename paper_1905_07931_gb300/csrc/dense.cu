@@ -138,6 +138,12 @@ static GMat epi_mat(const csrt_mat *m) {
     return g;
 }
 
+static GMat out_mat(const csrt_mat *m) {
+    GMat g = epi_mat(m);
+    g.vec = m != nullptr && tma_store_ok(m->data, m->ld, m->cols, dt_size(m->dtype));
+    return g;
+}
+
 static char *operand_space(void *ws) { return ws_scratch(ws) + kPartialBytes; }
 
 // D = A B^T with the epilogue of the forward (kEpiFwd) or the backward products; `at`: the workspace's space for operands.
@@ -153,8 +159,8 @@ static int dense_product(const csrt_mat *am, bool a_mn, const csrt_mat *bm, bool
     a.m = out0->rows;
     a.n = out0->cols;
     a.batch = 1;
-    a.out0 = epi_mat(out0);
-    a.out1 = epi_mat(out1);
+    a.out0 = out_mat(out0);
+    a.out1 = out_mat(out1);
     // a staging slot holds two aligned 16-bit blocks, or one block of any other kind
     if (out1 != nullptr && (out0->dtype == CSRT_DT_F32 || !a.out0.vec || !a.out1.vec)) a.out0.vec = a.out1.vec = 0;
     a.hdr = static_cast<WsHeader *>(ws);
@@ -363,7 +369,7 @@ int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, 
             t.m = m;
             t.n = k;
             t.batch = 1;
-            t.out0 = epi_mat(dw);
+            t.out0 = out_mat(dw);
             t.c1 = a.c1;
             const GChoice c = choose_tile(t, n, aligned_set(t, dw->dtype == CSRT_DT_F32));
             const int64_t units = ceil_div<int64_t>(m, 128 * kTiles[c.tile].cg) * ceil_div<int64_t>(k, kTiles[c.tile].bn) *

@@ -15,6 +15,12 @@ inline bool tma_rows_ok(const void *p, int64_t ld, int size) {
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * size % 16 == 0;
 }
 
+// Rows that TMA may store: it writes whole units of 16 bytes, so one that ends inside a unit would write into the gap
+// before the next (a load stops at the element).
+inline bool tma_store_ok(const void *p, int64_t ld, int64_t cols, int size) {
+    return tma_rows_ok(p, ld, size) && cols * size % 16 == 0;
+}
+
 struct GOperand {
     void *p;
     int64_t rows, cols, ld;   // as stored, row-major

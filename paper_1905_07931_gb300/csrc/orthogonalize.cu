@@ -510,7 +510,7 @@ int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float
     p.o.ld = o->ld;
     p.o.stride = o_stride;
     p.o.dtype = o->dtype;
-    p.o.vec = tma_rows_ok(o->data, o->ld, dt_size(o->dtype)) && (batch == 1 || o_stride * dt_size(o->dtype) % 16 == 0);
+    p.o.vec = tma_store_ok(o->data, o->ld, cols, dt_size(o->dtype)) && (batch == 1 || o_stride * dt_size(o->dtype) % 16 == 0);
     const int64_t chunks = rows * (((int64_t)cols + 7) / 8);
     int64_t blocks = imin<int64_t>(ceil_div<int64_t>(chunks, kPrepThreads), kPrepBlocks);
     blocks = imin<int64_t>(blocks, imax<int64_t>(1, (int64_t)num_sms() * 8 / batch));

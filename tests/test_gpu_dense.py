@@ -568,3 +568,48 @@ def test_bias_gradient_of_unaligned_rows_is_the_aligned_ones(C, m, k, n, accumul
     assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
     want = v.double().sum(1) + accumulate
     _check(res[1][1], want, (n / 32 + 17) * 2.0 ** -23 * (v.double().abs().sum(1) + 1), torch.float32)
+
+
+@pytest.mark.parametrize("n", [1, 3, 4, 5, 7, 8, 9, 12, 30, 33, 100, 130, 257, 516])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("wide", [False, True])
+def test_nothing_is_written_between_rows(C, n, dtype, wide):
+    """Outputs that are the first columns of aligned wider rows: the other columns, and what follows, stay as they are."""
+    gen, dt, m, k = _gen(n), DT[dtype], 150, 72
+    od, ld = torch.float32 if wide else dt, (n + 63) // 64 * 64 + 64
+
+    def out(rows, cols, t, skip=0):
+        buf = torch.full((rows + 1, ld), 7.0, dtype=t, device="cuda")
+        return buf, buf[:rows, skip:skip + cols]
+
+    def untouched(buf, view, skip=0):
+        rest = torch.ones_like(buf, dtype=torch.bool)
+        rest[:view.shape[0], skip:skip + view.shape[1]] = False
+        assert bool((buf[rest] == 7.0).all())
+
+    w, x, dy = _mat(gen, m, k, dt, "tight", 0.1), _mat(gen, k, n, dt), _mat(gen, m, n, dt, "tight", 0.1)
+    ws = C.DenseWorkspace(m, k, n)
+    for skip in (0, 16):
+        (yb, y), (zb, z) = out(m, n, od, skip), out(m, n, dt, skip)
+        C.dense_fwd(w, x, y, ws, act="gelu", z=z)
+        untouched(yb, y, skip), untouched(zb, z, skip)
+        zz = w.double() @ x.double()
+        e = _sum_tol(k, w.double().abs() @ x.double().abs(), od)
+        _check(z, zz, e, dt)
+        yb, y = out(m, n, od, skip)
+        C.dense_fwd(w, x, y, ws)
+        untouched(yb, y, skip)
+        _check(y, zz, e, od)
+        xb, dx = out(k, n, od, skip)
+        C.dense_bwd_x(w, dy, dx, ws)
+        untouched(xb, dx, skip)
+        _check(dx, w.double().t() @ dy.double(), _sum_tol(m, w.double().abs().t() @ dy.double().abs(), od), od)
+        a, b = _mat(gen, m, k, dt), _mat(gen, n, k, dt)
+        wb, dw = out(m, n, od, skip)
+        C.dense_bwd_w(a, b, dw, C.DenseWorkspace(m, n, k))
+        untouched(wb, dw, skip)
+        _check(dw, a.double() @ b.double().t(), _sum_tol(k, a.double().abs() @ b.double().abs().t(), od), od)
+        pb, pre = out(m, n, od, skip)
+        C.dense_act_bwd(dy, dy, "silu", pre)
+        untouched(pb, pre, skip)
+    assert ws.status()[0] == 0

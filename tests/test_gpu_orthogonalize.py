@@ -409,3 +409,16 @@ def test_long_batches_one_by_one(C, odt):
     assert _rel(o, _exact(g.double(), 2, 1e-7, 1.0)) <= (2e-3 if odt == torch.float32 else 3e-3)
     del g, o, ws, one, wso
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("m,k", [(33, 5), (64, 65), (300, 130), (1000, 1001), (2000, 3003)])
+@pytest.mark.parametrize("odt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("batch", [1, 2])
+def test_nothing_is_written_between_rows(C, m, k, odt, batch):
+    """o as the first columns of aligned wider rows, with a row between the matrices: all else stays as it is."""
+    g = torch.randn(batch, m, k, generator=_gen(m + k), device="cuda")
+    buf = torch.full((batch, m + 1, (k + 63) // 64 * 64 + 64), 7.0, dtype=odt, device="cuda")
+    o, ws = buf[:, :m, :k], C.OrthogonalizeWorkspace(batch, m, k)
+    C.orthogonalize(g, o, ws)
+    assert _rel(o, _exact(g.double(), 5, 1e-7, 1.0)) <= (2e-3 if odt == torch.float32 else 3e-3)
+    assert bool((buf[:, m] == 7).all()) and bool((buf[:, :, k:] == 7).all())
