@@ -276,7 +276,16 @@ int csrt_dense_fwd(const csrt_mat *w, const csrt_mat *x, const float *bias, int3
     CSRT_ARG(z == nullptr || !vector_meets(bias, m, z), "bias overlaps z");
     CSRT_ARG(!clash(y, x) && !clash(y, w), "y overlaps an operand");
     if (m == 0 || n == 0) return CSRT_OK;
-    if (n <= kTokensMax) {
+    // One to four tokens stream W past x, unless x has gaps between its rows (columns of a wider buffer): W is then read two
+    // bytes a lane and x by a cache line for each element, which the tensor cores overtake once the product is large enough
+    // to pay for their fixed cost and for the copy of an x that TMA cannot take (us, stream / tensor cores: x in rows of 64,
+    // 1000 x 1024 one token 5.1 / 7.6, 4096 x 1024 one 10.7 / 7.8, 4096 x 4096 one 32 / 12, four 132 / 12; in rows of 61,
+    // 1000 x 4096 four 13.4 / 11.7, 4096 x 2048 two 11.9 / 12.6, 4096 x 4096 two 22 / 14). With W to be copied too the
+    // stream stays (4096 x 4097, one token: 16 to 32 / 26 to 29).
+    const int64_t terms = (int64_t)m * k * n;
+    const bool gaps = x->ld != n && tma_rows_ok(w->data, w->ld, 2) &&
+                      terms >= (int64_t)1 << (tma_rows_ok(x->data, x->ld, 2) ? 22 : 25);
+    if (n <= kTokensMax && !gaps) {
         TokenArgs t = {};
         t.w = static_cast<const uint16_t *>(w->data);
         t.x = static_cast<const uint16_t *>(x->data);

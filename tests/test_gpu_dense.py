@@ -613,3 +613,26 @@ def test_nothing_is_written_between_rows(C, n, dtype, wide):
         C.dense_act_bwd(dy, dy, "silu", pre)
         untouched(pb, pre, skip)
     assert ws.status()[0] == 0
+
+
+@pytest.mark.parametrize("m,k", [(300, 784), (1000, 2048), (4096, 4096), (4096, 4097), (2050, 5000)])
+@pytest.mark.parametrize("n", [1, 2, 3, 4])
+@pytest.mark.parametrize("ld,off", [(64, 0), (64, 5), (61, 2), (8, 1)])
+def test_tokens_that_are_columns_of_a_wider_buffer(C, m, k, n, ld, off):
+    """A few columns of x, z and y between others, which stay as they are: small products and large ones."""
+    gen, dt = _gen(m + k + n + ld), torch.bfloat16
+    w, b = _mat(gen, m, k, dt, "tight", 1 / math.sqrt(k)), torch.randn(m, generator=gen, device="cuda")
+    xb = torch.randn(k, ld, generator=gen, device="cuda").to(dt)
+    yb = torch.full((m, ld), 7.0, dtype=dt, device="cuda")
+    zb = yb.clone()
+    x, y, z = xb[:, off:off + n], yb[:, off:off + n], zb[:, off:off + n]
+    ws = C.DenseWorkspace(m, k, n)
+    C.dense_fwd(w, x, y, ws, bias=b, act="gelu", z=z)
+    zz = w.double() @ x.double() + b.double()[:, None]
+    s = w.double().abs() @ x.double().abs() + b.double().abs()[:, None]
+    e = _sum_tol(k, s, dt)
+    _check(z, zz, e, dt)
+    _check(y, _act(zz, "gelu"), 1.13 * e + 2.0 ** -18 * zz.abs().clamp_min(1), dt)
+    for buf in (yb, zb):
+        assert bool((buf[:, :off] == 7).all()) and bool((buf[:, off + n:] == 7).all())
+    assert ws.status()[0] == 0
