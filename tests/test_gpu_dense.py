@@ -636,3 +636,67 @@ def test_tokens_that_are_columns_of_a_wider_buffer(C, m, k, n, ld, off):
     for buf in (yb, zb):
         assert bool((buf[:, :off] == 7).all()) and bool((buf[:, off + n:] == 7).all())
     assert ws.status()[0] == 0
+
+
+# Rows, columns and reduction of products that the launcher puts on each of its tiles (256 x 256 and 256 x 128 by pairs of
+# SMs, 128 x 128, 128 x 64) with whole reductions, with all tiles in slices and with the left-over ones in slices.
+ON_EVERY_TILE = [(647, 3256, 72), (682, 5064, 64), (180, 4944, 6560), (5936, 216, 8464), (3170, 1584, 3016), (1193, 4048, 4200),
+                 (157, 5056, 64), (148, 4880, 64), (64, 5216, 4016), (136, 2560, 4872), (522, 4384, 8064), (70, 96, 64),
+                 (70, 64, 3176), (154, 4880, 1320), (154, 5072, 2976), (141, 1824, 5496), (5097, 72, 8632), (677, 3224, 6984),
+                 (395, 5632, 6952)]
+ON_EVERY_TILE_ODD = [(1034, 3315, 64), (202, 5233, 8496), (2737, 1859, 4040), (133, 4971, 104), (73, 5105, 4880),
+                     (522, 4383, 8064), (153, 5523, 2648), (5779, 65, 8296), (2792, 841, 6784), (80, 77, 3200), (70, 65, 64)]
+
+
+@pytest.mark.parametrize("rows,cols,r", ON_EVERY_TILE + ON_EVERY_TILE_ODD)
+@pytest.mark.parametrize("op", ["fwd", "dx", "dw"])
+@pytest.mark.parametrize("dtype,out", [("f16", None), ("bf16", "f32")])
+def test_every_tile_with_every_epilogue(C, rows, cols, r, op, dtype, out):
+    gen, dt = _gen(rows + cols + r), DT[dtype]
+    od = DT[out] if out else dt
+    base = _mat(gen, rows, cols, od)       # residual, or what is there
+    there = base.double()
+    ws = C.DenseWorkspace(*{"fwd": (rows, r, cols), "dx": (r, rows, cols), "dw": (rows, cols, r)}[op])
+    o1, o2 = torch.empty(rows, cols, dtype=od, device="cuda"), torch.empty(rows, cols, dtype=od, device="cuda")
+    s = 1 / math.sqrt(r)
+    if op == "fwd":
+        a, b = _mat(gen, rows, r, dt, scale=s), _mat(gen, r, cols, dt)
+        prod, mag = a.double() @ b.double(), a.double().abs() @ b.double().abs()
+        bias, z = torch.randn(rows, generator=gen, device="cuda"), torch.empty(rows, cols, dtype=dt, device="cuda")
+        C.dense_fwd(a, b, o1, ws)
+        C.dense_fwd(a, b, o2, ws, bias=bias, act="silu", residual=base, z=z)
+        e = _sum_tol(r, mag, od)
+        zz = prod + bias.double()[:, None]
+        _check(z, zz, e + 2.0 ** -23 * zz.abs(), dt)
+        want = _act(zz, "silu") + there
+        tol = 1.13 * e + 2.0 ** -18 * zz.abs().clamp_min(1) + 2.0 ** -23 * (want.abs() + there.abs())
+        _check(o2, want, tol, od)
+        C.dense_fwd(a, b, base, ws, residual=base)     # in place
+        _check(base, prod + there, e + 2.0 ** -23 * (prod + there).abs(), od)
+    elif op == "dx":
+        a, b = _mat(gen, r, rows, dt, scale=s), _mat(gen, r, cols, dt)
+        prod, mag = a.double().t() @ b.double(), a.double().abs().t() @ b.double().abs()
+        z = _mat(gen, rows, cols, dt)
+        C.dense_bwd_x(a, b, o1, ws)
+        C.dense_bwd_x(a, b, o2, ws, z_below=z, act="gelu", residual=base)
+        e = _sum_tol(r, mag, od)
+        want = prod * _act_grad(z.double(), "gelu") + there
+        tol = 1.13 * e + 2.0 ** -17 * prod.abs() * z.double().abs().clamp_min(1)
+        _check(o2, want, tol + 2.0 ** -23 * (want.abs() + there.abs()), od)
+        C.dense_bwd_x(a, b, base, ws, z_below=z, act="relu")     # z alone
+        _check(base, prod * (z > 0), e, od)
+    else:
+        a, b = _mat(gen, rows, r, dt, scale=s), _mat(gen, cols, r, dt)
+        prod, mag = a.double() @ b.double().t(), a.double().abs() @ b.double().abs().t()
+        db, db2 = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+        o2.copy_(base)
+        C.dense_bwd_w(a, b, o1, ws, db=db)
+        C.dense_bwd_w(a, b, o2, ws, db=db2, accumulate=True)
+        e = _sum_tol(r, mag, od)
+        want = prod + there
+        _check(o2, want, e + 2.0 ** -23 * (want.abs() + there.abs()), od)
+        sb, t = a.double().abs().sum(1), (r / 32 + 17) * 2.0 ** -23
+        _check(db, a.double().sum(1), t * sb, torch.float32)
+        _check(db2, a.double().sum(1) + 1, t * (sb + 1), torch.float32)
+    _check(o1, prod, e, od)
+    assert ws.status()[0] == 0
