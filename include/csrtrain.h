@@ -405,7 +405,8 @@ int csrt_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols
  * float32, so o is within about 1e-3 of the exact
  * iteration (2-norm, relative); where u has no component at all (fewer samples
  * than rows) what the first steps round grows with the iteration, 3.4 times a
- * step, and o may be a few 1e-3 off. A matrix holding an infinity or a NaN
+ * step, and o may be 2e-3 to 3e-3 off, small matrices of few dimensions more:
+ * up to 0.14 / (rank sqrt(short side)), 3e-2 for 10 x 72 of rank one. A matrix holding an infinity or a NaN
  * yields NaN. o may feed prox_update_compact as the search direction of a layer's
  * prox step. beta in [0, 1), eps > 0 and finite, 0 <= steps <= 32, batch <=
  * 65535. o must not overlap g or momentum. */

@@ -422,3 +422,22 @@ def test_nothing_is_written_between_rows(C, m, k, odt, batch):
     C.orthogonalize(g, o, ws)
     assert _rel(o, _exact(g.double(), 5, 1e-7, 1.0)) <= (2e-3 if odt == torch.float32 else 3e-3)
     assert bool((buf[:, m] == 7).all()) and bool((buf[:, :, k:] == 7).all())
+
+
+@pytest.mark.parametrize("rank,m,k", [(1, 60, 90), (16, 128, 200), (64, 300, 500), (200, 512, 1024), (1, 10, 72), (4, 10, 72),
+                                      (8, 784, 300), (32, 1500, 2000)])
+def test_rank_deficient_within_what_the_header_says(C, rank, m, k):
+    """In the row and column space of u the bound is the one for full rank. Outside, a step's rounding of A and B (1.4e-4
+    of an entry, rms) times X has 2.4e-4 |A| sqrt(rank / s) |X| left, s the short side and A, X of norm 1 / sqrt(rank) and
+    1 / sqrt(rank) a direction at the first step; times |b| for either, times 3.4445^4 and what later steps add (146), over
+    the result's sqrt(rank): 0.14 / (rank sqrt(s)). Beside that the header's 3e-3, 4e-3 with a margin."""
+    gen = _gen(rank + m)
+    g = (torch.randn(m, rank, generator=gen, device="cuda") @ torch.randn(rank, k, generator=gen, device="cuda"))[None]
+    o, ws = torch.empty_like(g), C.OrthogonalizeWorkspace(1, m, k)
+    C.orthogonalize(g, o, ws)
+    want = _exact(g.double(), 5, 1e-7, 1.0)
+    assert _rel(o, want) <= 4e-3 + 0.14 / (rank * math.sqrt(min(m, k)))
+    u, _, vt = torch.linalg.svd(g[0].double(), full_matrices=False)
+    u, vt = u[:, :rank], vt[:rank]
+    err = u @ (u.t() @ (o[0].double() - want[0]) @ vt.t()) @ vt
+    assert float(err.norm() / want.norm()) <= 2e-3
