@@ -354,8 +354,9 @@ int csrt_dense_workspace_bytes(int32_t m, int32_t k, int32_t max_n, size_t *byte
  * type) receives the pre-activation W x + bias. y is M x n, of w's type or
  * float32. residual may be y itself (same data and ld); w, x, y and z must
  * not overlap otherwise, nor bias and y or z. Any sizes, n = 1 (one token) and 0 among them; rows
- * that are 16-byte aligned (data and ld) are read and written in place by
- * TMA, others are copied once into the workspace or stored piecewise. */
+ * that are 16-byte aligned (data and ld) are read in place by TMA, others are
+ * copied once into the workspace; outputs with such rows whose columns fill
+ * whole units of 16 bytes are written by TMA, others piecewise. */
 int csrt_dense_fwd(const csrt_mat *w, const csrt_mat *x, const float *bias, int32_t act, const csrt_mat *residual,
                    csrt_mat *z, csrt_mat *y, void *ws, size_t ws_bytes, void *stream);
 
@@ -372,7 +373,9 @@ int csrt_dense_bwd_x(const csrt_mat *w, const csrt_mat *dy, const csrt_mat *z_be
  * (M x K) and db[i] = sum_c dy[i, c] (M floats, may be NULL; no part of the
  * matrices), both added to what is there when accumulate != 0. No 1/n factor. dw is float32 or of dy's
  * type; float32 sums are rounded to nearest every 512 columns (the tensor
- * core's own accumulation truncates). */
+ * core's own accumulation truncates), 16-bit results of this and the other
+ * products likewise where more than 32768 (float16) or 131072 (bfloat16) terms
+ * would be accumulated in one go. */
 int csrt_dense_bwd_w(const csrt_mat *dy, const csrt_mat *x, int32_t accumulate, csrt_mat *dw, float *db, void *ws,
                      size_t ws_bytes, void *stream);
 

@@ -186,6 +186,8 @@ __global__ void row_sums_kernel(const uint16_t *__restrict__ dy, int64_t ld, int
     }
 }
 
+// An element at a time, 2 or 4 bytes an access: 4096 x 256 takes 9.0 us with gelu' on bfloat16 and 6.6 to convert, 4096 x
+// 9216 297 and 160 (33 at the measured copy rate for the former).
 __global__ void act_bwd_kernel(GMat dy, GMat z, int32_t act, GMat out, int32_t rows, int32_t cols) {
     pdl_enter();
     for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
@@ -196,6 +198,8 @@ __global__ void act_bwd_kernel(GMat dy, GMat z, int32_t act, GMat out, int32_t r
         }
 }
 
+// As act_bwd_kernel: 4096 x 9216 with a float32 direction and a bfloat16 copy takes 139 us (528 MB, 78 at the measured copy
+// rate), 4096 x 256 6.8.
 __global__ void dense_update_kernel(GMat w, GMat d, float eta, float keep, GMat w16, int32_t rows, int32_t cols) {
     pdl_enter();
     float *wp = static_cast<float *>(w.p);

@@ -1,5 +1,6 @@
 // Forward product of one to four tokens (csrt_dense_fwd with n <= kTokensMax): every weight is used n times only, so
-// the call is a stream over W and the tensor cores have nothing to gain.
+// the call is a stream over W and the tensor cores have nothing to gain. (Large products whose tokens are columns of a
+// wider buffer are theirs: the rule in csrt_dense_fwd.)
 //
 // A warp takes two rows of W (or, where there are few rows, a share of two rows' K: the block's warps then join in
 // shared memory). Per step each lane loads 16 bytes of either row and the 8 n values of x that belong to them - x is
@@ -8,6 +9,10 @@
 // at the measured copy rate), 4096 x 9216 75.5 MB in 13.8 us. Two rows per warp halve the x traffic in L1 and double the
 // loads in flight: one row takes 8.0 and 15.3 us, four rows 7.3 and 13.7 but 3.7 instead of 2.8 us on 300 x 784. Above
 // four tokens the float32 FMAs (n per weight) no longer fit beside the stream and the tensor cores take over.
+//
+// That is the vector form. Where K is no multiple of eight, W's rows are not 16-byte aligned or x has gaps, a lane reads
+// two bytes at a time: 4096 x 4097 takes 11.7 us for one token, 17.8 for four (tight x), 300 x 784 with x in rows of 64
+// 6.8 and 15.1.
 #include "gemm16.cuh"
 #include "dense_tokens.cuh"
 

@@ -14,7 +14,11 @@
 //    overlaps the next tile's loads and products;
 //  * warps 4..11: epilogue. Warp w reads TMEM lanes 32 (w & 3) .. + 31 and every other group of 32 columns, applies
 //    the epilogue in float32, rounds once, and leaves through 64- or 128-byte swizzled staging and a TMA store
-//    (where the output's rows are not 16-byte aligned: by rows of 32 elements, a lane each).
+//    (where the output's rows are not 16-byte aligned, or its columns do not fill units of 16 bytes, which is what a TMA
+//    store writes: by rows of 32 elements, a lane each). The accumulator goes back to the MMA warp by a relaxed arrival:
+//    only tensor memory is handed over, whose reads are complete (tcgen05.wait::ld) and ordered before the arrival by
+//    tcgen05.fence::before_thread_sync, as the next MMAs are after the wait by after_thread_sync; no write to shared or
+//    global memory has to become visible with it.
 // CG = 2 pairs two CTAs of a cluster on one tile of 2 x 128 rows: each holds its 128 rows of A and half the columns
 // of B, and the leader issues the pair's MMAs.
 //
@@ -42,6 +46,10 @@
 // 128 x 64 tiles and slices (gemm16_host.cuh). Short reductions are bound by the epilogue: a 128 x 256 share of a tile
 // takes 5 us in it (4096 x 9216 from 256 columns, 151 MB of float32: 39 us, 22 at the measured copy rate; added to
 // what is there 79, 45).
+//
+// An epilogue thread has 224 registers. Two of the 256-wide instances with promoted sums do not keep to them: the general
+// backward one spills 1.7 KB a thread, the lean forward one 0.3 KB (4096 x 4096 x 8192 takes 168 us with a float32 y, 154
+// with a bfloat16 one); all others less than 0.3 KB.
 //
 // Every wait is bounded: one that runs out sets the CTA's abort flag, the roles drain and meet, and the kernel ends
 // with CSRT_DEV_TIMEOUT in the status word.
@@ -79,7 +87,7 @@ struct GMat {
     void *p;
     int64_t ld, stride;
     int32_t dtype;     // CSRT_DT_*
-    int32_t vec;       // rows 16-byte aligned: vector access; outputs: TMA store
+    int32_t vec;       // rows 16-byte aligned: vector access; outputs: TMA store (columns fill units of 16 bytes too)
     int32_t pad;       // rows may be read up to ld, whatever the matrix's columns
 };
 

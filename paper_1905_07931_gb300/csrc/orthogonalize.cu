@@ -415,6 +415,9 @@ static int ns_products(const NsPlan &q, cudaStream_t s) {
     // 3 x 2048 x 512: 154 / 174 / 239); from 200 tiles on pairs of SMs on 256 x 128 (2048 x 2048: 334 / 247 / 306;
     // 6 x 256 x 4096: 226 / 203 / 267; 4096 x 1000: 246 / 237 / 290); from 700 on, where L2 traffic counts most,
     // 256 x 256 (3 x 2048 x 2048: 738 / 487 / 442; 4096 x 4096: 1826 / 1188 / 1027; 4096 x 9216: 3747 / 2204 / 1858).
+    // Those shapes have short sides of 256 and more. Below, tiles of 256 rows are mostly empty and a batch has one to three
+    // units of A a matrix: 6 x 128 x 8192 takes 313 us and 12 x 64 x 9216 455 where one such matrix, with slices, takes 118
+    // and 105.
     const int64_t tiles = (int64_t)q.batch * ceil_div<int64_t>(q.rows, 128) * ceil_div<int64_t>(q.cols, 128);
     if (has_long_sum(q, kTiles[tiles < 200 ? 2 : tiles < 700 ? 3 : 0]))
         return tiles < 700 ? launch_ns<2, 128, true>(q, kTiles[3], s) : launch_ns<2, 256, true>(q, kTiles[0], s);
