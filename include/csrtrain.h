@@ -406,7 +406,8 @@ int csrt_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols
  * operands (11 significant bits; all matrices are scaled so that entries lie
  * within their bounds, as singular values stay below 1.21), X and all sums are
  * float32, so o is within about 1e-3 of the exact
- * iteration (2-norm, relative); where u has no component at all (fewer samples
+ * iteration (2-norm, relative; 5e-3 with short sides of eight and less, where
+ * roundings do not average); where u has no component at all (fewer samples
  * than rows) what the first steps round grows with the iteration, 3.4 times a
  * step, and o may be 2e-3 to 3e-3 off, small matrices of few dimensions more:
  * up to 0.14 / (rank sqrt(short side)), 3e-2 for 10 x 72 of rank one. A matrix holding an infinity or a NaN

@@ -441,3 +441,38 @@ def test_rank_deficient_within_what_the_header_says(C, rank, m, k):
     u, vt = u[:, :rank], vt[:rank]
     err = u @ (u.t() @ (o[0].double() - want[0]) @ vt.t()) @ vt
     assert float(err.norm() / want.norm()) <= 2e-3
+
+
+@pytest.mark.parametrize("workload", ["mlp", "lenet"])
+def test_sparse_net_updates_on_a_second_stream(C, workload):
+    """SparseNet(optimizer="muon") with each layer's update beside the backward pass gives the bits of one stream, on fc
+    and on conv layers."""
+    import numpy as np
+
+    from paper_1905_07931_gb300 import synth
+    from paper_1905_07931_gb300.train import SparseNet, lenet_layers, mlp_layers
+    if workload == "mlp":
+        cfg = synth.mlp(seed=5, batch=64, sizes=(200, 120, 84, 10), densities=(0.3, 0.3, 0.5))
+        layers, shape, count = mlp_layers(3), (200,), 3
+    else:
+        cfg = synth.lenet(seed=5, batch=16)
+        layers, shape, count = lenet_layers(), (1, 28, 28), len(cfg["W"])
+    batch = cfg["labels"].shape[0]
+    nets = []
+    for ov in (False, True):
+        net = SparseNet(layers, cfg["W"], cfg["b"], batch, shape, optimizer="muon", overlap=ov)
+        net.x_in.copy_(torch.from_numpy(np.ascontiguousarray(cfg["X"])).view_as(net.x_in))
+        net.labels.copy_(torch.from_numpy(cfg["labels"]))
+        nets.append(net)
+    losses = []
+    for _ in range(4):
+        pair = [float(net.step("prox", 0.01, 0.05)[0].item()) for net in nets]
+        torch.cuda.synchronize()
+        assert pair[0] == pair[1] and math.isfinite(pair[0])
+        losses.append(pair[0])
+        assert all(net.status()[0] == 0 for net in nets)
+        for i in range(count):
+            for a, b in zip(nets[0].weights(i).to_host()[0], nets[1].weights(i).to_host()[0]):
+                np.testing.assert_array_equal(a.view(np.uint32), b.view(np.uint32))
+            assert torch.equal(nets[0].params[i]["m"], nets[1].params[i]["m"])
+    assert losses[-1] < losses[0]
