@@ -87,7 +87,7 @@ def draw(rng):
             if c["d"] * c["n"] * (1 if c["stream"] != "f32" else 1.6) <= MOST:
                 return c
         elif kind == "clip":
-            c = dict(kind=kind, form="mixed", count=_log(rng, 1, 200), smallest=_log(rng, 1, 1000),
+            c = dict(kind=kind, form="mixed", count=_log(rng, 1, 60), smallest=_log(rng, 1, 1000),
                      largest=_log(rng, 1000, 4096 * 4096), sizes=rng.randrange(1 << 20), active=rng.random() < 0.8,
                      dtype=rng.choice(("f32", "bf16")), out=rng.choice(("f32", "f32", "bf16")))
             if sum(r * k for r, k in _shapes(c)) <= 4096 * (9216 + 4096):
