@@ -64,8 +64,10 @@ extern "C" {
                                  the count that was needed. */
 #define CSRT_DEV_TIMEOUT 2    /* a bounded wait (on another block, or on a bulk copy
                                  into shared memory) gave up; results invalid */
-#define CSRT_DEV_NONFINITE 4  /* the prox step met a NaN in w - eta*G (dropped) */
-#define CSRT_DEV_INVALID 8    /* csrt_validate_csr found a broken invariant */
+#define CSRT_DEV_NONFINITE 4  /* the prox step met a NaN in w - eta*G (dropped); csrt_grad_norm or
+                                 csrt_grad_clip met an infinity or a NaN */
+#define CSRT_DEV_INVALID 8    /* csrt_validate_csr found a broken invariant; a token beyond the
+                                 table of csrt_embed_* (it was taken as padding) */
 
 /* weight_grad_dense precision. */
 #define CSRT_PREC_FP32 0      /* float32 FMA on the CUDA cores */
@@ -417,6 +419,103 @@ int csrt_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols
 int csrt_orthogonalize(const csrt_mat *g, int64_t g_stride, int32_t batch, float *momentum, float beta,
                        int32_t nesterov, int32_t steps, float eps, float scale, csrt_mat *o, int64_t o_stride,
                        void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Around the dense layers of a residual network: the norms before and after */
+/* a block, tokens in, gradients clipped. Types and layout as above.         */
+/* ------------------------------------------------------------------------ */
+
+#define CSRT_NORM_SCALE 0   /* x * weight + bias, no statistics */
+#define CSRT_NORM_RMS 1     /* x / sqrt(mean(x^2) + eps) * weight + bias */
+#define CSRT_NORM_LAYER 2   /* (x - mean(x)) / sqrt(var(x) + eps) * weight + bias; var is the mean square deviation */
+
+#define CSRT_GATE_NONE 0    /* the gate itself */
+#define CSRT_GATE_SIGMOID 1 /* 1 / (1 + exp(-g)) */
+#define CSRT_GATE_SILU 2    /* g / (1 + exp(-g)) */
+
+/* A norm over the d features of each token (column). All arrays are float32 on
+ * the device. */
+typedef struct csrt_norm {
+    int32_t kind;           /* CSRT_NORM_* */
+    float eps;              /* finite, > 0 (not read by CSRT_NORM_SCALE) */
+    const float *weight;    /* [d] or NULL: ones */
+    const float *bias;      /* [d] or NULL: zeros */
+    float *mean;            /* [n]: CSRT_NORM_LAYER's means. Forward: written, may be NULL. Backward: read */
+    float *rstd;            /* [n]: 1 / sqrt(... + eps) of CSRT_NORM_RMS and CSRT_NORM_LAYER, as mean */
+    float *dweight, *dbias; /* [d] or NULL: gradients, written by the backward call */
+} csrt_norm;
+
+/* csrt_block_norm_fwd -- what lies between two blocks of a residual network:
+ *   t = post(y),  h = r_scale * r + a(gate) * t,  v = pre(h)
+ * all d x n: the norm after a block (post), its gate, the scaled residual and
+ * the norm before the next block (pre). y, gate and v have one type, r and h
+ * that type or float32. NULL leaves a part out: post (t = y), gate (factor 1),
+ * r (no residual), y (h = r_scale * r; post and gate are then NULL), pre and v
+ * together, h (not written). At least one of y and r, and of h and v, is given.
+ * Everything is computed in float32 and rounded once: v is the norm of the h
+ * that is not yet rounded. Squares are summed in float32, so entries beyond
+ * 1e18 of a normed matrix overflow its statistics. A token that holds an
+ * infinity or a NaN does not reach the others. h may be r itself; apart from
+ * that no output overlaps anything else. Any d and n, 0 and 1 among them. */
+int csrt_block_norm_fwd(const csrt_mat *y, const csrt_norm *post, const csrt_mat *gate, int32_t gate_act,
+                        const csrt_mat *r, float r_scale, const csrt_norm *pre, csrt_mat *h, csrt_mat *v, void *stream);
+
+/* Workspace of csrt_block_norm_bwd for d features and at most max_n tokens. */
+int csrt_block_norm_workspace_bytes(int32_t d, int32_t max_n, size_t *bytes);
+
+/* csrt_block_norm_bwd -- the backward pass: from dv and dh (the gradient that
+ * reaches h by other paths; either may be NULL, dv with pre) to
+ *   dr = r_scale * dh',  dgate = dh' * t * a'(gate),  dy = post'(a(gate) * dh')
+ * where dh' = dh + pre'(dv), and to the norms' dweight and dbias, sums over all
+ * tokens (added to what is there when accumulate != 0), in a fixed order. h
+ * and y are the forward call's (h as it was stored), the norms hold its
+ * statistics. h may be NULL without pre, y with a post of NULL and no dgate.
+ * dr, dy and dgate may be NULL; dy's presence says whether there is a y. dr may
+ * be dh itself; apart from that no output overlaps anything else. dv, gate, y,
+ * dy and dgate have one type; dh, h and dr that type or float32. */
+int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *h, const csrt_norm *pre,
+                        const csrt_mat *y, const csrt_norm *post, const csrt_mat *gate, int32_t gate_act, float r_scale,
+                        int32_t accumulate, csrt_mat *dr, csrt_mat *dy, csrt_mat *dgate, void *ws, size_t ws_bytes,
+                        void *stream);
+
+/* Workspace of the embedding calls. */
+int csrt_embed_workspace_bytes(int32_t vocab, int32_t d, int32_t max_n, size_t *bytes);
+
+/* csrt_embed_fwd -- x[:, c] = scale * table[tokens[c], :]. table is vocab x d
+ * (a token is a row), x is d x n, of any type each; tokens holds n int32. A
+ * negative token is padding: a column of zeros. A token of vocab or more is
+ * taken as padding too and sets CSRT_DEV_INVALID. scale is finite. */
+int csrt_embed_fwd(const csrt_mat *table, const int32_t *tokens, float scale, csrt_mat *x, void *ws, size_t ws_bytes,
+                   void *stream);
+
+/* csrt_embed_bwd -- the table's gradient: dtable[v, :] = scale * the sum of
+ * dx[:, c] over the tokens c that are v, in ascending c (float32, rounded
+ * once). accumulate == 0 writes every row (zeros where no token is v);
+ * accumulate != 0 adds to the rows that have tokens and touches no other.
+ * Results repeat bit for bit. */
+int csrt_embed_bwd(const csrt_mat *dx, const int32_t *tokens, float scale, int32_t accumulate, csrt_mat *dtable,
+                   void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace of csrt_grad_norm and csrt_grad_clip. */
+int csrt_grad_workspace_bytes(size_t *bytes);
+
+/* csrt_grad_norm -- norm[0] = the square root of the sum of the squares of all
+ * entries of `count` matrices (a host array of csrt_mat, each of any type),
+ * norm[1] = 1 (two floats on the device). Squares are summed in float32 over
+ * short runs, then in float64; runs whose squares float32 does not hold are
+ * scaled first, so every norm that float32 holds is found. An infinity or a
+ * NaN gives an infinite or NaN norm and sets CSRT_DEV_NONFINITE. */
+int csrt_grad_norm(const csrt_mat *g, int32_t count, float *norm, void *ws, size_t ws_bytes, void *stream);
+
+/* csrt_grad_clip -- csrt_grad_norm, then out[i] = g[i] * norm[1] with
+ * norm[1] = norm[0] > max_norm ? max_norm / norm[0] : 1. out is a host array
+ * of `count` matrices of g's shapes and any types, each overlapping nothing
+ * but, where it is g[i] itself, g[i]; NULL: g itself. Where the factor is 1
+ * matrices in place are left as they are. A norm that is infinite or NaN
+ * leaves the factor at 1. max_norm > 0 and finite. No matrix of out may
+ * overlap another. */
+int csrt_grad_clip(const csrt_mat *g, int32_t count, float max_norm, const csrt_mat *out, float *norm, void *ws,
+                   size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------ */
 /* Network glue (Caffe layers the paper uses but does not describe).         */

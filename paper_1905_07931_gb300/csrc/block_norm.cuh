@@ -1,0 +1,76 @@
+// The norms around a block of a residual network (include/csrtrain.h, csrt_block_norm_*): arguments of the kernels.
+#pragma once
+
+#include "gemm16.cuh"
+
+namespace csrt {
+
+struct NormSide {
+    int32_t kind;                 // CSRT_NORM_*, -1: no such norm
+    float eps;
+    const float *w, *b;
+    float *mean, *rstd;
+    float *dw, *db;
+};
+
+// p == nullptr: the matrix is not given.
+struct NormMat {
+    char *p;
+    int64_t ld;
+};
+
+struct NormArgs {
+    int32_t d, n;
+    int32_t gate_act;
+    int32_t accumulate;
+    float r_scale;
+    NormSide post, pre;
+    NormMat y, g, r, h, v;         // r is dh in the backward pass
+    NormMat dv, dr, dy, dg;
+    float *partial;                // backward: row sums of a group of tokens, [group][4][d] (post dw, db; pre dw, db)
+    int32_t groups;                // blocks (or clusters) along the tokens, each with row sums of its own
+};
+
+constexpr int kNormGroups = 304;   // two for each SM of a GB300
+enum { kSumPostW = 0, kSumPostB = 1, kSumPreW = 2, kSumPreB = 3 };
+
+template <typename T>
+__device__ __forceinline__ float to_f(T v);
+template <>
+__device__ __forceinline__ float to_f(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+template <>
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T from_f(float v);
+template <>
+__device__ __forceinline__ float from_f(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_f(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
+
+// a(g) and a'(g). FAST takes the fast exponential and quotient: the sigmoid is off by (4 + 1.2 |g|) 2^-23 of itself, 2^-18 where
+// it is above 2^-24, far below a 16-bit rounding. float32 matrices take the others.
+template <bool FAST>
+__device__ __forceinline__ float sigmoid_of(float g) {
+    return FAST ? __fdividef(1.f, 1.f + __expf(-g)) : 1.f / (1.f + expf(-g));
+}
+template <bool FAST>
+__device__ __forceinline__ float gate_value(float g, int act) {
+    if (act == CSRT_GATE_NONE) return g;
+    const float p = sigmoid_of<FAST>(g);
+    return act == CSRT_GATE_SIGMOID ? p : g * p;
+}
+template <bool FAST>
+__device__ __forceinline__ void gate_both(float g, int act, float &value, float &slope) {
+    value = g;
+    slope = 1.f;
+    if (act == CSRT_GATE_NONE) return;
+    const float p = sigmoid_of<FAST>(g);
+    value = act == CSRT_GATE_SIGMOID ? p : g * p;
+    slope = act == CSRT_GATE_SIGMOID ? p * (1.f - p) : p * (1.f + g * (1.f - p));
+}
+
+}  // namespace csrt

@@ -2,18 +2,12 @@
 #pragma once
 
 #include "gemm16.cuh"
+#include "mat.cuh"
 
 namespace csrt {
 
 // Scratch of the split products: slabs of 128 x BN floats. A product takes splits only while they all fit.
 constexpr size_t kPartialBytes = (size_t)24 << 20;
-
-inline int dt_size(int dtype) { return dtype == CSRT_DT_F32 ? 4 : 2; }
-
-// Rows that TMA (and 16-byte vector access) can take in place.
-inline bool tma_rows_ok(const void *p, int64_t ld, int size) {
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * size % 16 == 0;
-}
 
 // Rows that TMA may store: it writes whole units of 16 bytes, so one that ends inside a unit would write into the gap
 // before the next (a load stops at the element).

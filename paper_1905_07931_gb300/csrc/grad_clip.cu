@@ -1,0 +1,276 @@
+// The global norm of the gradients of a network and their clipping (csrt_grad_norm, csrt_grad_clip):
+//   norm = sqrt(sum over all matrices of x^2),   out = x min(1, max_norm / norm)
+// Bound by HBM traffic. A launch carries its matrices as arguments, so nothing is copied to the device first and a captured
+// graph holds all it needs.
+#include <cmath>
+
+#include "block_norm.cuh"
+#include "mat.cuh"
+
+namespace csrt {
+
+constexpr int kGradUnit = 16384;    // elements that a block takes at a time
+constexpr int kGradBlocks = 608;    // four blocks of 256 threads an SM
+constexpr int kGradThreads = 256;
+
+struct GradEntry {
+    const char *p;
+    char *o;
+    int64_t ld, ldo;
+    int64_t unit0;          // first unit of this matrix within the launch
+    int64_t count;          // elements
+    int32_t cols;
+    uint8_t dt, dto;
+    uint8_t flat, flat_o;   // rows follow one another without a gap: 1, and the first is 16-byte aligned: 2
+};
+
+template <int N>
+struct GradArgs {
+    GradEntry e[N];
+    int32_t entries;
+    int64_t units;
+    int32_t first, last;    // of the launches of one call
+    float max_norm;         // 0: only the norm
+    float *norm;
+    double *partial;        // kGradBlocks
+    int32_t *ticket;
+    WsHeader *hdr;
+};
+
+template <int N>
+__device__ __forceinline__ const GradEntry &grad_entry(const GradArgs<N> &a, int64_t unit) {
+    int lo = 0, hi = a.entries - 1;   // last entry with unit0 <= unit
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.e[mid].unit0 <= unit) lo = mid;
+        else hi = mid - 1;
+    }
+    return a.e[lo];
+}
+
+template <typename T>
+__device__ __forceinline__ float grad_at(const char *p, int64_t ld, int32_t cols, bool flat, int64_t i) {
+    const T *q = reinterpret_cast<const T *>(p);
+    return to_f<T>(flat ? q[i] : q[i / cols * ld + i % cols]);
+}
+
+// The squares of a thread's elements of a unit: float32 sums unless they overflow, or underflow without being zero.
+template <typename T>
+__device__ __forceinline__ double unit_squares(const GradEntry &e, int64_t base) {
+    const int64_t end = imin<int64_t>(e.count, base + kGradUnit);
+    float s = 0.f;
+    bool some = false;
+    for (int64_t i = base + threadIdx.x; i < end; i += kGradThreads) {
+        const float v = grad_at<T>(e.p, e.ld, e.cols, e.flat != 0, i);
+        s = fmaf(v, v, s);
+        some |= v != 0.f;
+    }
+    // below 2^-80 squares that float32 does not hold (under 2^-126) could matter
+    if ((s >= 8.271806e-25f && s <= 3.4028235e38f) || !some) return s;
+    double t = 0.;
+    for (int64_t i = base + threadIdx.x; i < end; i += kGradThreads) {
+        const double v = grad_at<T>(e.p, e.ld, e.cols, e.flat != 0, i);
+        t += v * v;
+    }
+    return t;
+}
+
+// Sum over the block in a fixed order; the first thread gets it.
+__device__ __forceinline__ double block_sum(double v, double (&part)[kGradThreads / 32]) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < kGradThreads / 32; ++w) v += part[w];
+    __syncthreads();
+    return v;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kGradThreads) grad_norm_kernel(const __grid_constant__ GradArgs<N> a) {
+    pdl_enter();
+    __shared__ double part[kGradThreads / 32];
+    __shared__ bool last;
+    double s = 0.;
+    for (int64_t u = blockIdx.x; u < a.units; u += gridDim.x) {
+        const GradEntry &e = grad_entry(a, u);
+        const int64_t base = (u - e.unit0) * kGradUnit;
+        s += e.dt == CSRT_DT_F32    ? unit_squares<float>(e, base)
+             : e.dt == CSRT_DT_BF16 ? unit_squares<__nv_bfloat16>(e, base)
+                                    : unit_squares<__half>(e, base);
+    }
+    s = block_sum(s, part);
+    if (threadIdx.x == 0) {
+        a.partial[blockIdx.x] = a.first ? s : a.partial[blockIdx.x] + s;
+        last = false;
+        if (a.last) {
+            __threadfence();
+            last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
+        }
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    s = 0.;
+    for (int b = threadIdx.x; b < gridDim.x; b += kGradThreads) s += __ldcg(a.partial + b);
+    s = block_sum(s, part);
+    if (threadIdx.x == 0) {
+        const double norm = sqrt(s);
+        const bool finite = norm <= 1.7976931348623157e308;
+        if (!finite) dev_flag(a.hdr, CSRT_DEV_NONFINITE);
+        a.norm[0] = (float)norm;
+        a.norm[1] = a.max_norm > 0.f && finite && norm > a.max_norm ? (float)(a.max_norm / norm) : 1.f;
+        *a.ticket = 0;
+    }
+}
+
+template <typename T, typename TO>
+__device__ __forceinline__ void unit_scale(const GradEntry &e, int64_t base, float factor) {
+    const int64_t end = imin<int64_t>(e.count, base + kGradUnit);
+    TO *o = reinterpret_cast<TO *>(e.o);
+    for (int64_t i = base + threadIdx.x; i < end; i += kGradThreads)
+        o[e.flat_o ? i : i / e.cols * e.ldo + i % e.cols] =
+            from_f<TO>(grad_at<T>(e.p, e.ld, e.cols, e.flat != 0, i) * factor);
+}
+template <typename T>
+__device__ __forceinline__ void unit_scale_to(const GradEntry &e, int64_t base, float factor) {
+    if (e.dto == CSRT_DT_F32) unit_scale<T, float>(e, base, factor);
+    else if (e.dto == CSRT_DT_BF16) unit_scale<T, __nv_bfloat16>(e, base, factor);
+    else unit_scale<T, __half>(e, base, factor);
+}
+
+template <int N>
+__global__ void __launch_bounds__(kGradThreads) grad_scale_kernel(const __grid_constant__ GradArgs<N> a) {
+    pdl_enter();
+    const float factor = __ldcg(a.norm + 1);
+    for (int64_t u = blockIdx.x; u < a.units; u += gridDim.x) {
+        const GradEntry &e = grad_entry(a, u);
+        if (factor == 1.f && e.o == e.p && e.dt == e.dto) continue;
+        const int64_t base = (u - e.unit0) * kGradUnit;
+        if (e.dt == CSRT_DT_F32) unit_scale_to<float>(e, base, factor);
+        else if (e.dt == CSRT_DT_BF16) unit_scale_to<__nv_bfloat16>(e, base, factor);
+        else unit_scale_to<__half>(e, base, factor);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+static size_t grad_bytes() { return kWsReservedBytes + align_up(kGradBlocks * sizeof(double), 256); }
+
+static int check_grads(const csrt_mat *g, int32_t count, const csrt_mat *out, float *norm, void *ws, size_t ws_bytes) {
+    CSRT_ARG(count >= 0, "count is negative");
+    CSRT_ARG(count == 0 || g != nullptr, "g is NULL");
+    CSRT_ARG(norm != nullptr, "norm is NULL");
+    CSRT_TRY(check_vector(norm, "norm"));
+    for (int32_t k = 0; k < count; ++k) {
+        CSRT_TRY(check_mat(g + k, "g"));
+        CSRT_ARG(!vector_meets(norm, 2, g + k), "norm overlaps g[%d]", k);
+        if (out == nullptr) continue;
+        CSRT_TRY(check_mat(out + k, "out"));
+        CSRT_TRY(check_shape(out + k, "out", g[k].rows, g[k].cols));
+        CSRT_ARG(same_place(out + k, g + k) || !clash(out + k, g + k), "out[%d] overlaps g[%d]", k, k);
+        CSRT_ARG(!vector_meets(norm, 2, out + k), "norm overlaps out[%d]", k);
+    }
+    CSRT_ARG(ws != nullptr, "workspace is NULL");
+    CSRT_ARG((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
+    if (ws_bytes < grad_bytes()) return fail(CSRT_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, grad_bytes());
+    return CSRT_OK;
+}
+
+static uint8_t flatness(const csrt_mat &m) {
+    if (m.rows > 1 && m.ld != m.cols) return 0;
+    return (reinterpret_cast<uintptr_t>(m.data) & 15) == 0 ? 2 : 1;
+}
+
+template <int N>
+static int grad_launch(const csrt_mat *g, int32_t count, float max_norm, const csrt_mat *out, float *norm, void *ws,
+                       cudaStream_t s) {
+    // matrices that hold something, N a launch; the norm's launches come first
+    int32_t full = 0;
+    int64_t all = 0;
+    for (int32_t k = 0; k < count; ++k) {
+        const int64_t c = (int64_t)g[k].rows * g[k].cols;
+        full += c > 0;
+        all += ceil_div<int64_t>(c, kGradUnit);
+    }
+    const unsigned blocks = (unsigned)imax<int64_t>(1, imin<int64_t>(all, kGradBlocks));
+    for (int pass = 0; pass < (max_norm > 0.f ? 2 : 1); ++pass) {
+        int32_t done = 0, k = 0;
+        do {
+            GradArgs<N> a;
+            a.entries = 0;
+            a.units = 0;
+            for (; k < count && a.entries < N; ++k) {
+                const csrt_mat &m = g[k], &o = out != nullptr ? out[k] : g[k];
+                const int64_t c = (int64_t)m.rows * m.cols;
+                if (c == 0) continue;
+                GradEntry &e = a.e[a.entries++];
+                e.p = static_cast<const char *>(m.data);
+                e.o = static_cast<char *>(o.data);
+                e.ld = m.ld;
+                e.ldo = o.ld;
+                e.unit0 = a.units;
+                e.count = c;
+                e.cols = m.cols;
+                e.dt = (uint8_t)m.dtype;
+                e.dto = (uint8_t)o.dtype;
+                e.flat = flatness(m);
+                e.flat_o = flatness(o);
+                a.units += ceil_div<int64_t>(c, kGradUnit);
+                ++done;
+            }
+            a.first = done == a.entries;
+            a.last = done == full;
+            a.max_norm = max_norm;
+            a.norm = norm;
+            a.partial = reinterpret_cast<double *>(ws_scratch(ws));
+            a.ticket = ws_counters(ws);
+            a.hdr = static_cast<WsHeader *>(ws);
+            if (pass == 0) {
+                launch_pdl(grad_norm_kernel<N>, dim3(blocks), dim3(kGradThreads), 0, s, a);
+                count_launch();
+                CSRT_TRY(check_launch("grad_norm_kernel"));
+            } else if (a.units > 0) {
+                launch_pdl(grad_scale_kernel<N>, dim3((unsigned)imin<int64_t>(a.units, kGradBlocks)), dim3(kGradThreads), 0, s, a);
+                count_launch();
+                CSRT_TRY(check_launch("grad_scale_kernel"));
+            }
+        } while (done < full);
+    }
+    return CSRT_OK;
+}
+
+static int grad_call(const csrt_mat *g, int32_t count, float max_norm, const csrt_mat *out, float *norm, void *ws,
+                     void *stream) {
+    if (count <= 16) return grad_launch<16>(g, count, max_norm, out, norm, ws, as_stream(stream));
+    return grad_launch<256>(g, count, max_norm, out, norm, ws, as_stream(stream));
+}
+
+}  // namespace csrt
+
+using namespace csrt;
+
+extern "C" {
+
+int csrt_grad_workspace_bytes(size_t *bytes) {
+    CSRT_ARG(bytes != nullptr, "bytes is NULL");
+    *bytes = grad_bytes();
+    return CSRT_OK;
+}
+
+int csrt_grad_norm(const csrt_mat *g, int32_t count, float *norm, void *ws, size_t ws_bytes, void *stream) {
+    CSRT_TRY(check_grads(g, count, nullptr, norm, ws, ws_bytes));
+    return grad_call(g, count, 0.f, nullptr, norm, ws, stream);
+}
+
+int csrt_grad_clip(const csrt_mat *g, int32_t count, float max_norm, const csrt_mat *out, float *norm, void *ws,
+                   size_t ws_bytes, void *stream) {
+    CSRT_TRY(check_grads(g, count, out, norm, ws, ws_bytes));
+    CSRT_ARG(std::isfinite(max_norm) && max_norm > 0.f, "max_norm must be finite and > 0");
+    return grad_call(g, count, max_norm, out, norm, ws, stream);
+}
+
+}  // extern "C"

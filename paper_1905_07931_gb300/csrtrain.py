@@ -22,6 +22,8 @@ CSRT_DEV_CAPACITY, CSRT_DEV_TIMEOUT, CSRT_DEV_NONFINITE, CSRT_DEV_INVALID = 1, 2
 CSRT_PREC_FP32, CSRT_PREC_TF32 = 0, 1
 CSRT_DT_F32, CSRT_DT_BF16, CSRT_DT_F16 = 0, 1, 2
 CSRT_ACT_NONE, CSRT_ACT_RELU, CSRT_ACT_GELU, CSRT_ACT_SILU = 0, 1, 2, 3
+CSRT_NORM_SCALE, CSRT_NORM_RMS, CSRT_NORM_LAYER = 0, 1, 2
+CSRT_GATE_NONE, CSRT_GATE_SIGMOID, CSRT_GATE_SILU = 0, 1, 2
 
 
 class csrt_csr(ctypes.Structure):
@@ -35,6 +37,11 @@ class csrt_csr(ctypes.Structure):
 
 class csrt_mat(ctypes.Structure):
     _fields_ = [("data", c_void_p), ("rows", c_int32), ("cols", c_int32), ("ld", c_int64), ("dtype", c_int32)]
+
+
+class csrt_norm(ctypes.Structure):
+    _fields_ = [("kind", c_int32), ("eps", c_float), ("weight", c_void_p), ("bias", c_void_p), ("mean", c_void_p),
+                ("rstd", c_void_p), ("dweight", c_void_p), ("dbias", c_void_p)]
 
 
 class CsrtError(RuntimeError):
@@ -84,6 +91,18 @@ _SIGS = {
     "csrt_orthogonalize_workspace_bytes": [c_int32, c_int32, c_int32, POINTER(c_size_t)],
     "csrt_orthogonalize": [POINTER(csrt_mat), c_int64, c_int32, c_void_p, c_float, c_int32, c_int32, c_float, c_float,
                            POINTER(csrt_mat), c_int64, c_void_p, c_size_t, c_void_p],
+    "csrt_block_norm_fwd": [POINTER(csrt_mat), POINTER(csrt_norm), POINTER(csrt_mat), c_int32, POINTER(csrt_mat), c_float,
+                            POINTER(csrt_norm), POINTER(csrt_mat), POINTER(csrt_mat), c_void_p],
+    "csrt_block_norm_workspace_bytes": [c_int32, c_int32, POINTER(c_size_t)],
+    "csrt_block_norm_bwd": [POINTER(csrt_mat), POINTER(csrt_mat), POINTER(csrt_mat), POINTER(csrt_norm),
+                            POINTER(csrt_mat), POINTER(csrt_norm), POINTER(csrt_mat), c_int32, c_float, c_int32,
+                            POINTER(csrt_mat), POINTER(csrt_mat), POINTER(csrt_mat), c_void_p, c_size_t, c_void_p],
+    "csrt_embed_workspace_bytes": [c_int32, c_int32, c_int32, POINTER(c_size_t)],
+    "csrt_embed_fwd": [POINTER(csrt_mat), c_void_p, c_float, POINTER(csrt_mat), c_void_p, c_size_t, c_void_p],
+    "csrt_embed_bwd": [POINTER(csrt_mat), c_void_p, c_float, c_int32, POINTER(csrt_mat), c_void_p, c_size_t, c_void_p],
+    "csrt_grad_workspace_bytes": [POINTER(c_size_t)],
+    "csrt_grad_norm": [POINTER(csrt_mat), c_int32, c_void_p, c_void_p, c_size_t, c_void_p],
+    "csrt_grad_clip": [POINTER(csrt_mat), c_int32, c_float, POINTER(csrt_mat), c_void_p, c_void_p, c_size_t, c_void_p],
     "csrt_bias_act_fwd": [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p],
     "csrt_relu_bwd": [c_void_p, c_void_p, c_int64, c_void_p],
     "csrt_bias_grad_sgd": [c_void_p, c_int32, c_int32, c_void_p, c_float, c_void_p, c_void_p],
@@ -493,6 +512,174 @@ def orthogonalize(g, o, ws: Workspace, momentum=None, beta: float = 0.95, nester
     _check(lib().csrt_orthogonalize(_mat(g2, "g"), g_stride, batch, _ptr(momentum), float(beta), 1 if nesterov else 0,
                                     int(steps), float(eps), float(scale), _mat(o2, "o"), o_stride, ws.ptr, ws.nbytes,
                                     _stream(stream)), "csrt_orthogonalize")
+
+
+# ---------------------------------------------------------------------------
+# Norms around a block, token embedding, gradient clipping
+# ---------------------------------------------------------------------------
+
+_NORMS = {"scale": CSRT_NORM_SCALE, "rms": CSRT_NORM_RMS, "layer": CSRT_NORM_LAYER}
+_GATES = {"none": CSRT_GATE_NONE, "sigmoid": CSRT_GATE_SIGMOID, "silu": CSRT_GATE_SILU}
+
+
+class BlockNormWorkspace(Workspace):
+    """Workspace of block_norm_bwd for d features and at most max_n tokens."""
+
+    def __init__(self, d: int, max_n: int, device="cuda", stream=None):
+        nbytes = c_size_t(0)
+        _check(lib().csrt_block_norm_workspace_bytes(int(d), int(max_n), ctypes.byref(nbytes)),
+               "csrt_block_norm_workspace_bytes")
+        self._init(nbytes.value, device, stream)
+
+
+class EmbedWorkspace(Workspace):
+    """Workspace of the embedding calls for a table of vocab rows of d features and at most max_n tokens."""
+
+    def __init__(self, vocab: int, d: int, max_n: int, device="cuda", stream=None):
+        nbytes = c_size_t(0)
+        _check(lib().csrt_embed_workspace_bytes(int(vocab), int(d), int(max_n), ctypes.byref(nbytes)),
+               "csrt_embed_workspace_bytes")
+        self._init(nbytes.value, device, stream)
+
+
+class GradWorkspace(Workspace):
+    """Workspace of grad_norm and grad_clip (any number of tensors)."""
+
+    def __init__(self, device="cuda", stream=None):
+        nbytes = c_size_t(0)
+        _check(lib().csrt_grad_workspace_bytes(ctypes.byref(nbytes)), "csrt_grad_workspace_bytes")
+        self._init(nbytes.value, device, stream)
+
+
+class Norm:
+    """A norm over the d features of n tokens (csrt_norm): kind "rms", "layer"
+    or "scale"; weight and bias (d floats, or None: ones, zeros); mean and rstd
+    (n floats: statistics that the forward call writes, if given, and the
+    backward call reads); dweight and dbias (d floats: gradients that the
+    backward call writes, if given). The tensors are kept."""
+
+    def __init__(self, kind: str, weight=None, bias=None, eps: float = 1e-5, mean=None, rstd=None, dweight=None,
+                 dbias=None):
+        if kind not in _NORMS:
+            raise ValueError(f"unknown norm {kind!r}")
+        self.kind, self.eps = kind, float(eps)
+        self._features = [(k, _f32(t, k)) for k, t in (("weight", weight), ("bias", bias), ("dweight", dweight),
+                                                       ("dbias", dbias)) if t is not None]
+        self._tokens = [(k, _f32(t, k)) for k, t in (("mean", mean), ("rstd", rstd)) if t is not None]
+        self.weight, self.bias, self.mean, self.rstd, self.dweight, self.dbias = weight, bias, mean, rstd, dweight, dbias
+        self._s = csrt_norm(_NORMS[kind], self.eps, _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), _ptr(dweight),
+                            _ptr(dbias))
+
+    def struct(self, d: int, n: int):
+        for names, need in ((self._features, d), (self._tokens, n)):
+            for name, t in names:
+                if t.numel() < need:
+                    raise ValueError(f"{name} has {t.numel()} elements, needs {need}")
+        return self._s
+
+
+def _gate(act):
+    if act not in _GATES:
+        raise ValueError(f"unknown gate activation {act!r}")
+    return _GATES[act]
+
+
+def _opt(t, name):
+    return None if t is None else _mat(t, name)
+
+
+def _int32(t, name):
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 1:
+        raise ValueError(f"{name} must be a contiguous 1-D int32 CUDA tensor")
+    return t
+
+
+def block_norm_fwd(y, r, h, v, post: Norm | None = None, pre: Norm | None = None, gate=None, gate_act: str = "none",
+                   r_scale: float = 1.0, stream=None):
+    """t = post(y), h = r_scale r + a(gate) t, v = pre(h): what lies between two
+    blocks of a residual network. None leaves out any of y, r, h, post, gate,
+    and pre with v."""
+    shape = next((t.shape for t in (y, r) if t is not None), (0, 0))
+    _check(lib().csrt_block_norm_fwd(_opt(y, "y"), None if post is None else post.struct(*shape), _opt(gate, "gate"),
+                                     _gate(gate_act), _opt(r, "r"), float(r_scale),
+                                     None if pre is None else pre.struct(*shape), _opt(h, "h"), _opt(v, "v"),
+                                     _stream(stream)), "csrt_block_norm_fwd")
+
+
+def block_norm_bwd(dv, dh, h, y, dr, dy, ws: Workspace, post: Norm | None = None, pre: Norm | None = None, gate=None,
+                   gate_act: str = "none", dgate=None, r_scale: float = 1.0, accumulate: bool = False, stream=None):
+    """The gradients dr, dy and dgate (None: not wanted) from dv and dh (either
+    may be None), and the norms' dweight and dbias (added to with accumulate)."""
+    shape = next((t.shape for t in (dv, dh) if t is not None), (0, 0))
+    _check(lib().csrt_block_norm_bwd(_opt(dv, "dv"), _opt(dh, "dh"), _opt(h, "h"),
+                                     None if pre is None else pre.struct(*shape), _opt(y, "y"),
+                                     None if post is None else post.struct(*shape), _opt(gate, "gate"), _gate(gate_act),
+                                     float(r_scale), 1 if accumulate else 0, _opt(dr, "dr"), _opt(dy, "dy"),
+                                     _opt(dgate, "dgate"), ws.ptr, ws.nbytes, _stream(stream)), "csrt_block_norm_bwd")
+
+
+def embed_fwd(table, tokens, x, ws: Workspace, scale: float = 1.0, stream=None):
+    """x[:, c] = scale * table[tokens[c]]; a negative token gives a column of zeros."""
+    if _int32(tokens, "tokens").numel() < x.shape[-1]:
+        raise ValueError(f"tokens has {tokens.numel()} elements, needs {x.shape[-1]}")
+    _check(lib().csrt_embed_fwd(_mat(table, "table"), _ptr(tokens), float(scale), _mat(x, "x"), ws.ptr, ws.nbytes,
+                                _stream(stream)), "csrt_embed_fwd")
+
+
+def embed_bwd(dx, tokens, dtable, ws: Workspace, scale: float = 1.0, accumulate: bool = False, stream=None):
+    """dtable[v] = scale * the sum of dx[:, c] over the tokens c that are v (with
+    accumulate: added to it, rows without tokens left as they are)."""
+    if _int32(tokens, "tokens").numel() < dx.shape[-1]:
+        raise ValueError(f"tokens has {tokens.numel()} elements, needs {dx.shape[-1]}")
+    _check(lib().csrt_embed_bwd(_mat(dx, "dx"), _ptr(tokens), float(scale), 1 if accumulate else 0,
+                                _mat(dtable, "dtable"), ws.ptr, ws.nbytes, _stream(stream)), "csrt_embed_bwd")
+
+
+class TensorList:
+    """Tensors that grad_norm and grad_clip take together, described once: 2-D
+    ones with contiguous rows, or contiguous ones of any shape. The tensors are
+    kept; their storage must stay where it is."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self._s = (csrt_mat * max(1, len(self.tensors)))()
+        for k, t in enumerate(self.tensors):
+            name = f"tensor {k}"
+            if t.dim() != 2:
+                if not t.is_contiguous():
+                    raise ValueError(f"{name} must be contiguous (or 2-D with contiguous rows)")
+                if t.numel() >= 2 ** 31:
+                    t = t.flatten(0, -2) if t.dim() > 2 else t
+                else:
+                    t = t.reshape(1, -1)
+            if t.dim() != 2 or max(t.shape) >= 2 ** 31:
+                raise ValueError(f"{name} has a side of 2^31 or more")
+            self._s[k] = _mat(t, name)
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _tensor_list(x):
+    return x if isinstance(x, TensorList) else TensorList(x)
+
+
+def grad_norm(grads, norm, ws: Workspace, stream=None):
+    """norm[0] = the square root of the sum of squares over all tensors (a TensorList, or a list of tensors)."""
+    grads = _tensor_list(grads)
+    _f32(norm, "norm", 2)
+    _check(lib().csrt_grad_norm(grads._s, len(grads), _ptr(norm), ws.ptr, ws.nbytes, _stream(stream)), "csrt_grad_norm")
+
+
+def grad_clip(grads, max_norm: float, norm, ws: Workspace, out=None, stream=None):
+    """grad_norm, norm[1] = min(1, max_norm / norm[0]) and out = grads * norm[1] (out None: in place)."""
+    grads = _tensor_list(grads)
+    out = None if out is None else _tensor_list(out)
+    if out is not None and len(out) != len(grads):
+        raise ValueError("out must have one tensor for each of grads")
+    _f32(norm, "norm", 2)
+    _check(lib().csrt_grad_clip(grads._s, len(grads), float(max_norm), None if out is None else out._s, _ptr(norm),
+                                ws.ptr, ws.nbytes, _stream(stream)), "csrt_grad_clip")
 
 
 # ---------------------------------------------------------------------------
