@@ -4,6 +4,7 @@
 // Activations are d x n with the token index contiguous, so a norm reduces down the columns. All of it is bound by HBM
 // traffic: a few tens of operations for 8 to 20 bytes.
 #include <cmath>
+#include <initializer_list>
 
 #include "block_norm.cuh"
 #include "mat.cuh"
@@ -284,6 +285,23 @@ static int check_types(int32_t *tb, int32_t *ts) {
     return CSRT_OK;
 }
 
+// Rows of every matrix that is given in whole 16-byte words.
+static bool norm_vector(std::initializer_list<const csrt_mat *> all) {
+    for (const csrt_mat *m : all)
+        if (m != nullptr && !tma_rows_ok(m->data, m->ld, dt_size(m->dtype))) return false;
+    return true;
+}
+
+static NormTile norm_fwd_choice(const NormArgs &a, bool vec) {
+    const int64_t d = a.d, tiles = ceil_div<int64_t>(a.n, 32);
+    if (a.n <= 2) return d > 65536 ? kTileColumns : d <= 1024 ? kTile1x1x4 : kTile1x1x16;
+    if (!vec) return d <= 4096 ? kTile32x1x32 : d <= 8192 ? kTile16x1x32 : d <= 16384 ? kTile8x1x32 : kTileColumns;
+    if (d > 8192) return d <= 16384 ? kTile16x8x8 : kTileColumns;
+    if (d <= 2048 && tiles * ceil_div<int64_t>(d, 128) <= 2 * num_sms()) return kTile32x8x2;
+    if (d <= 4096 && tiles * ceil_div<int64_t>(d, 256) <= 2 * num_sms()) return kTile32x8x4;
+    return kTile32x8x8;
+}
+
 template <typename TB, typename TS>
 static int launch_fwd(const NormArgs &a, cudaStream_t s) {
     const int64_t tiles = ceil_div<int64_t>(a.n, 32);
@@ -382,7 +400,12 @@ int csrt_block_norm_fwd(const csrt_mat *y, const csrt_norm *post, const csrt_mat
     a.r = norm_mat(r);
     a.h = norm_mat(h);
     a.v = norm_mat(v);
-    return CSRT_NORM_DISPATCH(launch_fwd, tb, ts, a, as_stream(stream));
+    const NormTile t = norm_fwd_choice(a, tb != CSRT_DT_F32 && norm_vector({y, gate, r, h, v}));
+    if (t == kTileColumns) return CSRT_NORM_DISPATCH(launch_fwd, tb, ts, a, as_stream(stream));
+    const bool wide = ts == CSRT_DT_F32;
+    return tb == CSRT_DT_F32    ? norm_fwd_f32(a, t, as_stream(stream))
+           : tb == CSRT_DT_BF16 ? norm_fwd_bf16(a, wide, t, as_stream(stream))
+                                : norm_fwd_f16(a, wide, t, as_stream(stream));
 }
 
 int csrt_block_norm_workspace_bytes(int32_t d, int32_t max_n, size_t *bytes) {

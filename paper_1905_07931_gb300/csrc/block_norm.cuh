@@ -28,6 +28,7 @@ struct NormArgs {
     NormMat y, g, r, h, v;         // r is dh in the backward pass
     NormMat dv, dr, dy, dg;
     float *partial;                // backward: row sums of a group of tokens, [group][4][d] (post dw, db; pre dw, db)
+    int32_t cluster;               // blocks that share the features of a tile
     int32_t groups;                // blocks (or clusters) along the tokens, each with row sums of its own
 };
 
@@ -72,5 +73,14 @@ __device__ __forceinline__ void gate_both(float g, int act, float &value, float 
     value = act == CSRT_GATE_SIGMOID ? p : g * p;
     slope = act == CSRT_GATE_SIGMOID ? p * (1.f - p) : p * (1.f + g * (1.f - p));
 }
+
+// Tiles of the kernels that read every matrix once: tokens wide, tokens a thread (8: rows of 16-byte words), features a thread.
+enum NormTile {
+    kTile32x8x8, kTile32x8x4, kTile32x8x2, kTile16x8x8, kTile32x1x32, kTile32x1x16, kTile16x1x32, kTile8x1x32, kTile1x1x16,
+    kTile1x1x4, kTileColumns
+};
+int norm_fwd_bf16(const NormArgs &a, bool wide, NormTile t, cudaStream_t s);   // wide: the residual stream is float32
+int norm_fwd_f16(const NormArgs &a, bool wide, NormTile t, cudaStream_t s);
+int norm_fwd_f32(const NormArgs &a, NormTile t, cudaStream_t s);
 
 }  // namespace csrt

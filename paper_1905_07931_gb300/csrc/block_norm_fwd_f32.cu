@@ -1,0 +1,8 @@
+// Forward norms around a block of float32 matrices.
+#include "block_norm_fwd.cuh"
+
+namespace csrt {
+
+int norm_fwd_f32(const NormArgs &a, NormTile t, cudaStream_t s) { return norm_fwd_tiles<float, float>(a, t, s); }
+
+}  // namespace csrt

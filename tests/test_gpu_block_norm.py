@@ -178,10 +178,14 @@ def test_forward(C, d, n, form):
     # in place over r, without statistics
     r2 = s["r"]
     P, Q = C.Norm(post, s["wpost"], s["bpost"], EPS), C.Norm(pre, s["wpre"], s["bpre"], EPS)
-    v2 = torch.full_like(v, float("nan"))
+    v2, h2 = torch.full((d, n), float("nan"), dtype=v.dtype, device="cuda"), torch.empty((d, n), dtype=h.dtype, device="cuda")
+    C.block_norm_fwd(s["y"], r2, h2, v2, post=P, pre=Q, gate=s["g"], gate_act=act or "none", r_scale=rs)
+    _check(h2, hh, eh, "h into tight rows")
+    _check(v2, vv, ev, "v into tight rows")
+    v2 = _mat(gen, d, n, DT[tb], layout)
     C.block_norm_fwd(s["y"], r2, r2, v2, post=P, pre=Q, gate=s["g"], gate_act=act or "none", r_scale=rs)
     assert torch.equal(r2, h)
-    _check(v2, vv, ev, "v in place")
+    assert torch.equal(v2, v)
 
 
 def _backward(s, post, pre, act, r_scale, st):
