@@ -10,6 +10,7 @@
 // Rows that are not 16-byte aligned take V = 1: an element's aligned 4-byte word is fetched, and its half picked.
 #pragma once
 
+#include <cmath>
 #include <mutex>
 #include <type_traits>
 
@@ -99,30 +100,36 @@ struct Place {
 // A thread's own copies of one matrix: F x V elements of type T in shared memory.
 template <typename T, int TT, int V, int F>
 struct Held {
-    static constexpr int kBytes = V == 8 ? (int)sizeof(T) * 8 : 4;   // a thread and feature
-    static constexpr int kTotal = kBytes * F * kNormThreads;
-    // `src` is the matrix's first element of this thread's column and first feature; nv of its V tokens exist.
-    static __device__ __forceinline__ void fetch(char *base, const char *src, int64_t ld, int rows, int row0, int nv) {
-        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(base);
-        const int64_t step = ld * (int64_t)sizeof(T) * Place<TT, V>::kStep;
+    static constexpr int kWords = V == 8 ? (int)sizeof(T) / 2 : 1;       // of 16 bytes (V = 8) or 4, for one feature
+    static constexpr int kTotal = kWords * (V == 8 ? 16 : 4) * F * kNormThreads;
+    // `src` is the matrix's first element of this thread's column and first feature. Where not all of the tile exists
+    // (!full), nv tokens and the features below `rows` are fetched and the rest is zeros.
+    static __device__ __forceinline__ void fetch(char *base, const char *src, int64_t ld, bool full, int rows, int row0, int nv) {
+        uint32_t dst = (uint32_t)__cvta_generic_to_shared(base) + threadIdx.x * (V == 8 ? 16 : 4);
+        const int64_t step = ld * (int64_t)(sizeof(T) * Place<TT, V>::kStep);
+        // V = 1: the high half of a word lies behind bytes before it, the low half is fetched alone: nothing past the element
+        const bool high = V == 1 && sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(src) & 2) != 0;
+        const int bytes = sizeof(T) == 4 || high ? 4 : 2;
+        if (high) src -= 2;
         const char *none = reinterpret_cast<const char *>(reinterpret_cast<uintptr_t>(src) & ~(uintptr_t)15);
 #pragma unroll
         for (int f = 0; f < F; ++f, src += step) {
-            const int have = row0 + f * Place<TT, V>::kStep < rows ? nv : 0;
             if constexpr (V == 8) {
+                if (full) {
 #pragma unroll
-                for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+                    for (int k = 0; k < kWords; ++k) cp_async16(dst + (f * kWords + k) * kNormThreads * 16, src + 16 * k, 16);
+                } else {
                     constexpr int each = 16 / (int)sizeof(T);
-                    const int here = imin(imax(have - k * each, 0), each);
-                    cp_async16(dst + ((f * ((int)sizeof(T) / 2) + k) * kNormThreads + threadIdx.x) * 16,
-                               here > 0 ? src + 16 * k : none, here * (int)sizeof(T));
+                    const int have = row0 + f * Place<TT, V>::kStep < rows ? nv : 0;
+#pragma unroll
+                    for (int k = 0; k < kWords; ++k) {
+                        const int here = imin(imax(have - k * each, 0), each);
+                        cp_async16(dst + (f * kWords + k) * kNormThreads * 16, here > 0 ? src + 16 * k : none, here * (int)sizeof(T));
+                    }
                 }
             } else {
-                // the high half of a word lies behind bytes before it, the low half is fetched alone: nothing past the element
-                const uintptr_t at = reinterpret_cast<uintptr_t>(src);
-                const int bytes = sizeof(T) == 4 || (at & 2) ? 4 : 2;
-                cp_async4(dst + (f * kNormThreads + threadIdx.x) * 4,
-                          have > 0 ? reinterpret_cast<const char *>(at & ~(uintptr_t)3) : none, have > 0 ? bytes : 0);
+                const bool have = full || (nv > 0 && row0 + f * Place<TT, V>::kStep < rows);
+                cp_async4(dst + f * kNormThreads * 4, have ? src : none, have ? bytes : 0);
             }
         }
     }
@@ -194,127 +201,156 @@ __device__ __forceinline__ void put_tokens(char *dst, const typename Tok<V>::P (
 
 // ---------------------------------------------------------------------------
 // Sums over all features of a token: over a thread's features, the lanes that hold the same tokens, the warps, the
-// cluster's blocks. A pair of values a token, either two sums, or mean and sum of square deviations (MOM), which are merged
-// by the formula of Chan, Golub and LeVeque: no cancellation, and one exchange instead of two.
+// cluster's blocks. One or two sums a token, or its mean and sum of square deviations, which are merged by the formula of
+// Chan, Golub and LeVeque: no cancellation, and one exchange instead of two.
+//
+// Blocks write their totals into each other's shared memory by st.async, which counts on the receiver's mbarrier: a cluster
+// barrier in its place waits for the stores of results in flight too (a fifth of the forward kernel's stalls).
 // ---------------------------------------------------------------------------
-struct Moments {
-    float mean, m2;
-};
-template <bool MOM>
+enum { kOneSum, kTwoSums, kMoments };
+
+template <int MODE>
 __device__ __forceinline__ void merge(float &a, float &b, float na, float a2, float b2, float nb) {
-    if (!MOM) {
+    if (MODE != kMoments) {
         a += a2;
-        b += b2;
+        if (MODE == kTwoSums) b += b2;
         return;
     }
     const float n = na + nb;
-    const float share = n > 0.f ? nb / n : 0.f, delta = a2 - a;
+    const float share = n > 0.f ? __fdividef(nb, n) : 0.f, delta = a2 - a;
     a = fmaf(delta, share, a);
     b = b + b2 + delta * delta * (na * share);
 }
 
 template <int TT>
 struct Exchange {
-    float2 *part;    // [2][warps][TT]
-    float *part_n;   // [2][warps]
-    float2 *slots;   // [2][cluster][TT], written by the other blocks
-    float2 *final;   // [warps][TT]
-    int turn;        // which half: a block may be one exchange ahead of another
+    float2 *slots;    // [2][cluster][TT], written by the cluster's blocks
+    float2 *part;     // [2][warps][TT]; a warp's row of the half that is not in use takes its results to its threads
+    float *part_n;    // [2][warps]
+    uint64_t *bar;    // [2]
+    int turn;         // exchanges so far: halves alternate, as a block may be one exchange ahead of another
     int size, rank, chunk, d;
+    float inv_d;
 
     static constexpr int bytes(int size) {
-        return (int)sizeof(float2) * TT * (2 * kNormWarps + 2 * size + kNormWarps) + 2 * kNormWarps * (int)sizeof(float);
+        return (int)sizeof(float2) * TT * (2 * kNormWarps + 2 * size) + 2 * kNormWarps * (int)sizeof(float) + 2 * (int)sizeof(uint64_t);
     }
     __device__ __forceinline__ Exchange(char *base, int size_, int rank_, int chunk_, int d_)
-        : turn(0), size(size_), rank(rank_), chunk(chunk_), d(d_) {
+        : turn(0), size(size_), rank(rank_), chunk(chunk_), d(d_), inv_d(1.f / (float)d_) {
         slots = reinterpret_cast<float2 *>(base);
         part = slots + 2 * size * TT;
-        final = part + 2 * kNormWarps * TT;
-        part_n = reinterpret_cast<float *>(final + kNormWarps * TT);
+        bar = reinterpret_cast<uint64_t *>(part + 2 * kNormWarps * TT);
+        part_n = reinterpret_cast<float *>(bar + 2);
+        if (size > 1) {
+            if (threadIdx.x == 0) {
+                for (int k = 0; k < 2; ++k)
+                    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(bar + k)) : "memory");
+                asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            }
+            __syncthreads();
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        }
+    }
+    // Every block has started and its barriers are set; before the first exchange.
+    __device__ __forceinline__ void started() const {
+        if (size > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    // No block leaves while another may still write to it.
+    __device__ __forceinline__ void leave() const {
+        if (size > 1) {
+            asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+        }
     }
 };
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 // a, b: this thread's values for its V tokens, over n of its features. Returns the totals for token (lane % TT).
-template <bool MOM, int TT, int V>
+template <int MODE, int TT, int V>
 __device__ __forceinline__ float2 cluster_total(Exchange<TT> &x, float (&a)[V], float (&b)[V], float n) {
     constexpr int kLanes = Place<TT, V>::kLanes;
+    static_assert(V == 1 || Place<TT, V>::kRowsWarp >= V, "a lane ends with one token");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const unsigned full = 0xffffffffu;
-    int token = (lane % kLanes) * V, first = 0;   // of the values still held; lanes with `first` set hold copies
+    int token = (lane % kLanes) * V, copy = 0;   // the first token still held; lanes with `copy` hold another's
     int held = V;
 #pragma unroll
     for (int o = 16; o >= kLanes; o >>= 1) {
-        const float nb = MOM ? __shfl_xor_sync(full, n, o) : 0.f;
+        const float nb = MODE == kMoments ? __shfl_xor_sync(full, n, o) : 0.f;
         if (held > 1) {   // each of the two lanes goes on with half of the tokens
             const bool up = (lane & o) != 0;
             held >>= 1;
 #pragma unroll
             for (int j = 0; j < V / 2; ++j) {
                 if (j >= held) break;
-                float a2 = up ? a[j] : a[j + held], b2 = up ? b[j] : b[j + held];
-                if (up) {
-                    a[j] = a[j + held];
-                    b[j] = b[j + held];
-                }
+                float a2 = up ? a[j] : a[j + held], b2 = 0.f;
+                a[j] = up ? a[j + held] : a[j];
                 a2 = __shfl_xor_sync(full, a2, o);
-                b2 = __shfl_xor_sync(full, b2, o);
-                merge<MOM>(a[j], b[j], n, a2, b2, nb);
+                if (MODE != kOneSum) {
+                    b2 = up ? b[j] : b[j + held];
+                    b[j] = up ? b[j + held] : b[j];
+                    b2 = __shfl_xor_sync(full, b2, o);
+                }
+                merge<MODE>(a[j], b[j], n, a2, b2, nb);
             }
             if (up) token += held;
         } else {
-            const float a2 = __shfl_xor_sync(full, a[0], o), b2 = __shfl_xor_sync(full, b[0], o);
-            merge<MOM>(a[0], b[0], n, a2, b2, nb);
-            first |= lane & o;
+            const float a2 = __shfl_xor_sync(full, a[0], o), b2 = MODE != kOneSum ? __shfl_xor_sync(full, b[0], o) : 0.f;
+            merge<MODE>(a[0], b[0], n, a2, b2, nb);
+            copy |= lane & o;
         }
         n += nb;
     }
     const int half = x.turn & 1;
-    x.turn ^= 1;
     float2 *part = x.part + half * kNormWarps * TT;
-    static_assert(V == 1 || Place<TT, V>::kRowsWarp >= V, "a lane ends with one token");
-    if (first == 0) part[warp * TT + token] = make_float2(a[0], b[0]);
-    if (MOM && lane == 0) x.part_n[half * kNormWarps + warp] = n;
+    if (copy == 0) part[warp * TT + token] = make_float2(a[0], MODE != kOneSum ? b[0] : 0.f);
+    if (MODE == kMoments && lane == 0) x.part_n[half * kNormWarps + warp] = n;
+    const uint32_t bar = (uint32_t)__cvta_generic_to_shared(x.bar + half);
+    if (x.size > 1 && threadIdx.x == 0)
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(x.size * TT * 8) : "memory");
     __syncthreads();
     const int t = lane % TT;
     float2 s = part[t];
-    float sn = MOM ? x.part_n[half * kNormWarps] : 0.f;
+    float sn = MODE == kMoments ? x.part_n[half * kNormWarps] : 0.f;
 #pragma unroll
     for (int w = 1; w < kNormWarps; ++w) {
         const float2 v = part[w * TT + t];
-        const float nb = MOM ? x.part_n[half * kNormWarps + w] : 0.f;
-        merge<MOM>(s.x, s.y, sn, v.x, v.y, nb);
+        const float nb = MODE == kMoments ? x.part_n[half * kNormWarps + w] : 0.f;
+        merge<MODE>(s.x, s.y, sn, v.x, v.y, nb);
         sn += nb;
     }
+    const int parity = (x.turn >> 1) & 1;
+    ++x.turn;
     if (x.size == 1) return s;
     float2 *slots = x.slots + half * x.size * TT;
+    const uint32_t own = (uint32_t)__cvta_generic_to_shared(slots + x.rank * TT + t);
     for (int r = warp; r < x.size; r += kNormWarps)
         if (lane < TT) {
-            const uint32_t own = (uint32_t)__cvta_generic_to_shared(slots + x.rank * TT + t);
-            uint32_t at;
+            uint32_t at, there;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(own), "r"(r));
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(s.x), "f"(s.y) : "memory");
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(bar), "r"(r));
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(at),
+                         "l"(pack2(s.x, s.y)), "r"(there)
+                         : "memory");
         }
-    cluster_arrive();
-    cluster_wait();
+    // never runs out while the cluster lives; the results of a wait that did are NaN
+    if (!mbar_wait_bounded(x.bar + half, parity)) return make_float2(NAN, NAN);
     s = slots[t];
     sn = (float)imin(x.chunk, x.d);
     for (int r = 1; r < x.size; ++r) {
         const float2 v = slots[r * TT + t];
         const float nb = (float)imax(0, imin(x.chunk, x.d - r * x.chunk));
-        merge<MOM>(s.x, s.y, sn, v.x, v.y, nb);
+        merge<MODE>(s.x, s.y, sn, v.x, v.y, nb);
         sn += nb;
     }
     return s;
 }
 
-// Two values for each token (a lane's, for token lane % TT) to the threads that hold it.
+// Two values for each token (a lane's, for token lane % TT) to the threads that hold it, after cluster_total. The row of
+// `part` is this warp's own: others read it only before the barrier of the last exchange and after that of the next.
 template <int TT, int V>
 __device__ __forceinline__ void to_tokens(Exchange<TT> &x, float2 own, int q, float (&a)[V], float (&b)[V]) {
     const int lane = threadIdx.x & 31;
-    float2 *mine = x.final + (threadIdx.x >> 5) * TT;
+    float2 *mine = x.part + ((x.turn & 1) * kNormWarps + (threadIdx.x >> 5)) * TT;
     __syncwarp();
     if (lane < TT) mine[lane] = own;
     __syncwarp();
@@ -324,6 +360,13 @@ __device__ __forceinline__ void to_tokens(Exchange<TT> &x, float2 own, int q, fl
         a[k] = v.x;
         b[k] = v.y;
     }
+    __syncwarp();
+}
+
+// 1 / sqrt(v): the approximation and a Newton step
+__device__ __forceinline__ float rsqrt_near(float v) {
+    const float r = rsqrtf(v);
+    return v <= 3.4028235e38f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
 }
 
 // exp and quotient of the fast sigmoid: 2^-22 and 2^-23 of the result, 2^-24 |g| from the rounded argument
