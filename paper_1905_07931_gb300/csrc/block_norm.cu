@@ -184,16 +184,25 @@ __global__ void __launch_bounds__(kColWarps * 32) norm_bwd_columns_kernel(NormAr
     }
 }
 
-// dweight and dbias: the groups' row sums, added in order.
-__global__ void norm_sums_kernel(NormArgs a) {
+// dweight and dbias: the groups' row sums, added in order. A block takes 32 features, its warps every eighth group.
+__global__ void __launch_bounds__(256) norm_sums_kernel(NormArgs a) {
     pdl_enter();
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= a.d) return;
+    __shared__ float part[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t i = (int64_t)blockIdx.x * 32 + lane;
     float *out[4] = {a.post.dw, a.post.db, a.pre.dw, a.pre.db};
     float *dst = out[blockIdx.y];
     if (dst == nullptr) return;
     float s = 0.f;
-    for (int g = 0; g < a.groups; ++g) s += a.partial[((int64_t)g * 4 + blockIdx.y) * a.d + i];
+    if (i < a.d)
+#pragma unroll 8
+        for (int g = warp; g < a.groups; g += 8) s += __ldcg(a.partial + ((int64_t)g * 4 + blockIdx.y) * a.d + i);
+    part[warp][lane] = s;
+    __syncthreads();
+    if (warp != 0 || i >= a.d) return;
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += part[w][lane];
     dst[i] = a.accumulate ? dst[i] + s : s;
 }
 
@@ -292,14 +301,16 @@ static bool norm_vector(std::initializer_list<const csrt_mat *> all) {
     return true;
 }
 
-static NormTile norm_fwd_choice(const NormArgs &a, bool vec) {
+static NormTile norm_fwd_choice(const NormArgs &a, bool in) {
     const int64_t d = a.d, tiles = ceil_div<int64_t>(a.n, 32);
-    if (a.n <= 2) return d > 65536 ? kTileColumns : d <= 1024 ? kTile1x1x4 : kTile1x1x16;
-    if (!vec) return d <= 4096 ? kTile32x1x32 : d <= 8192 ? kTile16x1x32 : d <= 16384 ? kTile8x1x32 : kTileColumns;
-    if (d > 8192) return d <= 16384 ? kTile16x8x8 : kTileColumns;
-    if (d <= 2048 && tiles * ceil_div<int64_t>(d, 128) <= 2 * num_sms()) return kTile32x8x2;
-    if (d <= 4096 && tiles * ceil_div<int64_t>(d, 256) <= 2 * num_sms()) return kTile32x8x4;
-    return kTile32x8x8;
+    if (a.n <= 2) return d > 65536 ? kTileColumns : d <= 16384 ? kTile1x4 : kTile1x16;
+    if (d > 16384) return kTileColumns;
+    if (in ? d > 10240 : d > 8192) return kTile8x4;
+    if (in && d > 8192) return kTile16x5;
+    if (d <= 2048 && tiles * ceil_div<int64_t>(d, 128) <= 2 * num_sms()) return kTile32x2;
+    if (!in) return d <= 4096 ? kTile32x4 : kTile16x4;
+    if (d <= 4096 && tiles * ceil_div<int64_t>(d, 256) <= 2 * num_sms()) return kTile32x4;
+    return kTile32x8;
 }
 
 template <typename TB, typename TS>
@@ -310,22 +321,29 @@ static int launch_fwd(const NormArgs &a, cudaStream_t s) {
     return check_launch("norm_fwd_columns_kernel");
 }
 
-static int32_t norm_groups(int32_t n) { return (int32_t)imax<int64_t>(1, imin<int64_t>(ceil_div<int64_t>(n, 32), kNormGroups)); }
+static int32_t norm_groups(int32_t n) { return (int32_t)imax<int64_t>(1, imin<int64_t>(n, kNormGroups)); }
 
 static size_t norm_bytes(int64_t d, int32_t max_n) {
     return kWsReservedBytes + align_up((size_t)norm_groups(max_n) * 4 * d * sizeof(float), 256);
 }
 
 template <typename TB, typename TS>
-static int launch_bwd(NormArgs a, cudaStream_t s) {
-    a.groups = norm_groups(a.n);
+static int launch_bwd(NormArgs &a, cudaStream_t s) {
+    a.groups = (int32_t)imin<int64_t>(ceil_div<int64_t>(a.n, 32), kNormGroups);
     launch_pdl(norm_bwd_columns_kernel<TB, TS>, dim3((unsigned)a.groups), dim3(kColWarps * 32), 0, s, a);
     count_launch();
-    CSRT_TRY(check_launch("norm_bwd_columns_kernel"));
-    if (a.post.dw == nullptr && a.post.db == nullptr && a.pre.dw == nullptr && a.pre.db == nullptr) return CSRT_OK;
-    launch_pdl(norm_sums_kernel, dim3((unsigned)ceil_div<int64_t>(a.d, 128), 4), dim3(128), 0, s, a);
-    count_launch();
-    return check_launch("norm_sums_kernel");
+    return check_launch("norm_bwd_columns_kernel");
+}
+
+// wide: the block's matrices are float32 too.
+static NormTile norm_bwd_choice(const NormArgs &a, bool in, bool wide) {
+    const int64_t d = a.d, tiles = ceil_div<int64_t>(a.n, 32);
+    // five float32 matrices of 1024 features a block do not fit into shared memory
+    if (d > (wide ? 8192 : 16384)) return kTileColumns;
+    if (a.n <= 2) return kTile1x4;
+    if (d <= 2048 && (!in || tiles * ceil_div<int64_t>(d, 128) <= 2 * num_sms())) return kTile32x2;
+    if (!in) return d <= 4096 ? kTile16x2 : d <= 8192 ? kTile8x2 : kTile8x4;
+    return d <= 2048 ? kTile32x4 : d <= 8192 ? kTile16x4 : kTile8x4;
 }
 
 // dweight and dbias of no tokens: zeros, unless they are added to.
@@ -400,12 +418,13 @@ int csrt_block_norm_fwd(const csrt_mat *y, const csrt_norm *post, const csrt_mat
     a.r = norm_mat(r);
     a.h = norm_mat(h);
     a.v = norm_mat(v);
-    const NormTile t = norm_fwd_choice(a, tb != CSRT_DT_F32 && norm_vector({y, gate, r, h, v}));
+    const bool in = tb != CSRT_DT_F32 && norm_vector({y, gate, r}), out = norm_vector({h, v});
+    const NormTile t = norm_fwd_choice(a, in);
     if (t == kTileColumns) return CSRT_NORM_DISPATCH(launch_fwd, tb, ts, a, as_stream(stream));
     const bool wide = ts == CSRT_DT_F32;
     return tb == CSRT_DT_F32    ? norm_fwd_f32(a, t, as_stream(stream))
-           : tb == CSRT_DT_BF16 ? norm_fwd_bf16(a, wide, t, as_stream(stream))
-                                : norm_fwd_f16(a, wide, t, as_stream(stream));
+           : tb == CSRT_DT_BF16 ? norm_fwd_bf16(a, wide, t, in, out, as_stream(stream))
+                                : norm_fwd_f16(a, wide, t, in, out, as_stream(stream));
 }
 
 int csrt_block_norm_workspace_bytes(int32_t d, int32_t max_n, size_t *bytes) {
@@ -498,7 +517,17 @@ int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *
         count_launch();
         return check_launch("norm_zero_kernel");
     }
-    return CSRT_NORM_DISPATCH(launch_bwd, tb, ts, a, s);
+    const bool in = tb != CSRT_DT_F32 && norm_vector({dv, dh, h, y, gate}), out = norm_vector({dr, dy, dgate});
+    const NormTile t = norm_bwd_choice(a, in, tb == CSRT_DT_F32);
+    const bool wide = ts == CSRT_DT_F32;
+    CSRT_TRY(t == kTileColumns    ? CSRT_NORM_DISPATCH(launch_bwd, tb, ts, a, s)
+             : tb == CSRT_DT_F32  ? norm_bwd_f32(a, t, s)
+             : tb == CSRT_DT_BF16 ? norm_bwd_bf16(a, wide, t, in, out, s)
+                                  : norm_bwd_f16(a, wide, t, in, out, s));
+    if (po->dweight == nullptr && po->dbias == nullptr && pr->dweight == nullptr && pr->dbias == nullptr) return CSRT_OK;
+    launch_pdl(norm_sums_kernel, dim3((unsigned)ceil_div<int64_t>(d, 32), 4), dim3(256), 0, s, a);
+    count_launch();
+    return check_launch("norm_sums_kernel");
 }
 
 }  // extern "C"

@@ -74,13 +74,14 @@ __device__ __forceinline__ void gate_both(float g, int act, float &value, float 
     slope = act == CSRT_GATE_SIGMOID ? p * (1.f - p) : p * (1.f + g * (1.f - p));
 }
 
-// Tiles of the kernels that read every matrix once: tokens wide, tokens a thread (8: rows of 16-byte words), features a thread.
-enum NormTile {
-    kTile32x8x8, kTile32x8x4, kTile32x8x2, kTile16x8x8, kTile32x1x32, kTile32x1x16, kTile16x1x32, kTile8x1x32, kTile1x1x16,
-    kTile1x1x4, kTileColumns
-};
-int norm_fwd_bf16(const NormArgs &a, bool wide, NormTile t, cudaStream_t s);   // wide: the residual stream is float32
-int norm_fwd_f16(const NormArgs &a, bool wide, NormTile t, cudaStream_t s);
+// Tiles of the kernels that read every matrix once: tokens wide, features a thread.
+enum NormTile { kTileColumns, kTile1x4, kTile1x16, kTile32x8, kTile32x4, kTile32x2, kTile16x5, kTile16x4, kTile16x2, kTile8x4, kTile8x2 };
+// wide: the residual stream is float32; in, out: the rows of all inputs, or results, are 16-byte aligned
+int norm_fwd_bf16(const NormArgs &a, bool wide, NormTile t, bool in, bool out, cudaStream_t s);
+int norm_fwd_f16(const NormArgs &a, bool wide, NormTile t, bool in, bool out, cudaStream_t s);
 int norm_fwd_f32(const NormArgs &a, NormTile t, cudaStream_t s);
+int norm_bwd_bf16(NormArgs &a, bool wide, NormTile t, bool in, bool out, cudaStream_t s);   // sets a.groups
+int norm_bwd_f16(NormArgs &a, bool wide, NormTile t, bool in, bool out, cudaStream_t s);
+int norm_bwd_f32(NormArgs &a, NormTile t, cudaStream_t s);
 
 }  // namespace csrt

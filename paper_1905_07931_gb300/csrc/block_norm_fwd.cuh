@@ -13,7 +13,16 @@ __device__ __forceinline__ void tile_stats(Exchange<TT> &ex, const NormSide &s, 
                                            typename Tok<V>::P (&m)[Tok<V>::N], typename Tok<V>::P (&r)[Tok<V>::N]) {
     typedef Tok<V> T;
     float a[V], b[V];
-    float2 own;
+    auto finish = [&](int t, float2 own) {
+        own.y = rsqrt_near(fmaf(own.y, ex.inv_d, s.eps));
+        const int64_t c = c0 + t;
+        if (ex.rank == 0 && c < n) {   // the lanes that hold copies write the same
+            if (s.mean != nullptr && s.kind == CSRT_NORM_LAYER) s.mean[c] = own.x;
+            if (s.rstd != nullptr) s.rstd[c] = own.y;
+        }
+        own.x = -own.x;
+        return own;
+    };
     typename T::P sq[T::N];
 #pragma unroll
     for (int k = 0; k < T::N; ++k) sq[k] = T::all(0.f);
@@ -44,7 +53,7 @@ __device__ __forceinline__ void tile_stats(Exchange<TT> &ex, const NormSide &s, 
             T::put(a, k, mul2(sum[k], T::all(-1.f)));
             T::put(b, k, sq[k]);
         }
-        own = cluster_total<kMoments>(ex, a, b, cnt);
+        exchange<kMoments>(ex, a, b, cnt, at.q, finish, m, r);
     } else {
 #pragma unroll
         for (int f = 0; f < F; ++f)
@@ -52,30 +61,19 @@ __device__ __forceinline__ void tile_stats(Exchange<TT> &ex, const NormSide &s, 
             for (int k = 0; k < T::N; ++k) sq[k] = fma2(x[f][k], x[f][k], sq[k]);
 #pragma unroll
         for (int k = 0; k < T::N; ++k) T::put(a, k, sq[k]);
-        own = make_float2(0.f, cluster_total<kOneSum>(ex, a, b, 0.f).x);
-    }
-    own.y = rsqrt_near(fmaf(own.y, ex.inv_d, s.eps));
-    const int64_t c = c0 + (threadIdx.x & 31);
-    if (ex.rank == 0 && threadIdx.x < TT && c < n) {
-        if (s.mean != nullptr && s.kind == CSRT_NORM_LAYER) s.mean[c] = own.x;
-        if (s.rstd != nullptr) s.rstd[c] = own.y;
-    }
-    own.x = -own.x;
-    to_tokens(ex, own, at.q, a, b);
-#pragma unroll
-    for (int k = 0; k < T::N; ++k) {
-        m[k] = T::get(a, k);
-        r[k] = T::get(b, k);
+        exchange<kOneSum>(ex, a, b, 0.f, at.q, [&](int t, float2 own) { return finish(t, make_float2(0.f, own.x)); }, m, r);
     }
 }
 
-template <typename TB, typename TS, int TT, int V, int F>
+template <typename TB, typename TS, int TT, int V, int F, bool UIN, bool UOUT>
 __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __grid_constant__ NormArgs a) {
     pdl_enter();
     extern __shared__ __align__(16) char held[];
     typedef Tok<V> T;
-    typedef Held<TB, TT, V, F> HB;
-    typedef Held<TS, TT, V, F> HS;
+    typedef Held<TB, TT, V, F, UIN> HB;
+    typedef Held<TS, TT, V, F, UIN> HS;
+    typedef Result<TB, TT, V, UOUT> RB;
+    typedef Result<TS, TT, V, UOUT> RS;
     typedef typename T::P P;
     constexpr bool kFast = sizeof(TB) == 2;
     constexpr int kFeatures = Place<TT, V>::kStep * F;
@@ -87,7 +85,9 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
     const int64_t i0 = (int64_t)rank * chunk + (at.row0 < rows ? at.row0 : 0);
     char *sy = held, *sg = sy + (a.y.p ? HB::kTotal : 0), *sr = sg + (a.g.p ? HB::kTotal : 0);
     float2 *wpost = reinterpret_cast<float2 *>(sr + (a.r.p ? HS::kTotal : 0)), *wpre = wpost + kFeatures;   // weight, bias
-    Exchange<TT> ex(reinterpret_cast<char *>(wpre + kFeatures), size, rank, chunk, a.d);
+    char *stage = reinterpret_cast<char *>(wpre + kFeatures) + (threadIdx.x >> 5) * RS::kStageBytes;   // this warp's
+    Exchange<TT> ex(reinterpret_cast<char *>(wpre + kFeatures) + kNormWarps * RS::kStageBytes, size, rank, chunk, a.d);
+    const int64_t first = (int64_t)rank * chunk + (threadIdx.x >> 5) * at.kRowsWarp;   // the warp's first feature
     const int64_t tiles = ((int64_t)a.n + TT - 1) / TT;
     int64_t tile = blockIdx.x / size;
 
@@ -101,10 +101,8 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
         if (a.g.p) HB::fetch(sg, a.g.p + (i0 * a.g.ld + c) * sizeof(TB), a.g.ld, full, rows, at.row0, nv);
         if (a.r.p) HS::fetch(sr, a.r.p + (i0 * a.r.ld + c) * sizeof(TS), a.r.ld, full, rows, at.row0, nv);
     };
-    // bit 1 of the address of a 2-byte element: the same for all of a thread's features and tiles (kStep and TT are even,
-    // or TT is 1)
-    auto odd = [&](const NormMat &m, int64_t c) {
-        return V == 1 && (((reinterpret_cast<uintptr_t>(m.p) >> 1) + (uint32_t)(i0 * m.ld + c)) & 1) != 0;
+    auto offset = [&](auto held_type, const NormMat &m, int64_t c) {
+        return decltype(held_type)::offset(m.p + (i0 * m.ld + c) * decltype(held_type)::kSize);
     };
     fetch(tile);
     // weights; zeros beyond `rows`, so that what is computed there is zero
@@ -124,23 +122,18 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
     ex.started();
 
     for (; tile < tiles; tile += a.groups) {
-        const int nv = exist(tile);
         const int64_t c = column(tile);
         P x[F][T::N], m[T::N], r[T::N];
-        char *ph = a.h.p + (i0 * a.h.ld + c) * sizeof(TS);
-        const int64_t step_h = a.h.ld * (int64_t)(sizeof(TS) * at.kStep);
+        RS out_h(a.h, first, tile * TT, a.n);
         auto put_h = [&](int f) {
-            if (a.h.p) {
-                if (at.row0 + f * at.kStep < rows) put_tokens<TS, V>(ph, x[f], nv);
-                ph += step_h;
-            }
+            if (a.h.p) out_h.put(stage, f, at.row0, rows, x[f]);
         };
         cp_async_wait();
-        const bool odd_r = odd(a.r, c);
+        const int off_r = offset(HS(), a.r, c);
         if (a.y.p) {
-            const bool odd_y = odd(a.y, c), odd_g = odd(a.g, c);
+            const int off_y = offset(HB(), a.y, c), off_g = offset(HB(), a.g, c);
 #pragma unroll
-            for (int f = 0; f < F; ++f) HB::read(sy, f, odd_y, x[f]);
+            for (int f = 0; f < F; ++f) HB::read(sy, f, off_y, x[f]);
 #pragma unroll
             for (int k = 0; k < T::N; ++k) {
                 m[k] = T::all(0.f);
@@ -155,7 +148,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
                     x[f][k] = fma2(add2(x[f][k], m[k]), mul2(r[k], T::all(w.x)), T::all(w.y));
                 if (a.g.p) {
                     P g[T::N], v[T::N];
-                    HB::read(sg, f, odd_g, g);
+                    HB::read(sg, f, off_g, g);
                     if (a.gate_act != CSRT_GATE_NONE) {
 #pragma unroll
                         for (int k = 0; k < T::N; ++k) v[k] = sigmoid2<kFast>(g[k]);
@@ -171,7 +164,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
                 }
                 if (a.r.p) {
                     P r0[T::N];
-                    HS::read(sr, f, odd_r, r0);
+                    HS::read(sr, f, off_r, r0);
 #pragma unroll
                     for (int k = 0; k < T::N; ++k) x[f][k] = fma2(r0[k], T::all(a.r_scale), x[f][k]);
                 }
@@ -180,7 +173,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
         } else {
 #pragma unroll
             for (int f = 0; f < F; ++f) {
-                HS::read(sr, f, odd_r, x[f]);
+                HS::read(sr, f, off_r, x[f]);
 #pragma unroll
                 for (int k = 0; k < T::N; ++k) x[f][k] = mul2(x[f][k], T::all(a.r_scale));
                 put_h(f);
@@ -194,47 +187,55 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
             r[k] = T::all(1.f);
         }
         if (a.pre.kind > CSRT_NORM_SCALE) tile_stats<TT, V, F>(ex, a.pre, at, rows, tile * TT, a.n, x, m, r);
-        char *pv = a.v.p + (i0 * a.v.ld + c) * sizeof(TB);
-        const int64_t step_v = a.v.ld * (int64_t)(sizeof(TB) * at.kStep);
+        RB out_v(a.v, first, tile * TT, a.n);
 #pragma unroll
-        for (int f = 0; f < F; ++f, pv += step_v) {
+        for (int f = 0; f < F; ++f) {
             const float2 w = wpre[at.row0 + f * at.kStep];
             P v[T::N];
 #pragma unroll
             for (int k = 0; k < T::N; ++k) v[k] = fma2(add2(x[f][k], m[k]), mul2(r[k], T::all(w.x)), T::all(w.y));
-            if (at.row0 + f * at.kStep < rows) put_tokens<TB, V>(pv, v, nv);
+            out_v.put(stage, f, at.row0, rows, v);
         }
     }
     ex.leave();
 }
 
-template <typename TB, typename TS, int TT, int V, int F>
-int norm_fwd_tile(const NormArgs &a, cudaStream_t s) {
+template <typename TB, typename TS, int TT, int V, int F, bool UIN, bool UOUT>
+int norm_fwd_tile(NormArgs a, cudaStream_t s) {
     const int size = TileShape<TT, V, F>::cluster(a.d);
-    const int smem = (a.y.p ? Held<TB, TT, V, F>::kTotal : 0) + (a.g.p ? Held<TB, TT, V, F>::kTotal : 0) +
-                     (a.r.p ? Held<TS, TT, V, F>::kTotal : 0) + TileShape<TT, V, F>::kFeatures * 16 +
-                     Exchange<TT>::bytes(size);
-    return launch_clusters<norm_fwd_tile_kernel<TB, TS, TT, V, F>>(a, size, ceil_div<int64_t>(a.n, TT), smem, s);
+    constexpr int b = Held<TB, TT, V, F, UIN>::kTotal, w = Held<TS, TT, V, F, UIN>::kTotal;
+    const int smem = (a.y.p ? b : 0) + (a.g.p ? b : 0) + (a.r.p ? w : 0) + TileShape<TT, V, F>::kFeatures * 16 +
+                     kNormWarps * Result<TS, TT, V, UOUT>::kStageBytes + Exchange<TT>::bytes(size);
+    return launch_clusters<norm_fwd_tile_kernel<TB, TS, TT, V, F, UIN, UOUT>>(a, size, ceil_div<int64_t>(a.n, TT), smem, s);
 }
 
+template <typename TB, typename TS, int TT, int F>
+int norm_fwd_aligned(const NormArgs &a, bool out, cudaStream_t s) {
+    return out ? norm_fwd_tile<TB, TS, TT, 8, F, false, false>(a, s) : norm_fwd_tile<TB, TS, TT, 8, F, false, true>(a, s);
+}
+
+// in, out: all rows of the inputs, or of the results, are 16-byte aligned.
 template <typename TB, typename TS>
-int norm_fwd_tiles(const NormArgs &a, NormTile t, cudaStream_t s) {
+int norm_fwd_tiles(const NormArgs &a, NormTile t, bool in, bool out, cudaStream_t s) {
+    switch (t) {
+        case kTile1x4: return norm_fwd_tile<TB, TS, 1, 1, 4, true, true>(a, s);
+        case kTile1x16: return norm_fwd_tile<TB, TS, 1, 1, 16, true, true>(a, s);
+        default: break;
+    }
     if constexpr (sizeof(TB) == 2) {
-        switch (t) {
-            case kTile32x8x8: return norm_fwd_tile<TB, TS, 32, 8, 8>(a, s);
-            case kTile32x8x4: return norm_fwd_tile<TB, TS, 32, 8, 4>(a, s);
-            case kTile32x8x2: return norm_fwd_tile<TB, TS, 32, 8, 2>(a, s);
-            case kTile16x8x8: return norm_fwd_tile<TB, TS, 16, 8, 8>(a, s);
-            default: break;
-        }
+        if (in) switch (t) {
+                case kTile32x8: return norm_fwd_aligned<TB, TS, 32, 8>(a, out, s);
+                case kTile32x4: return norm_fwd_aligned<TB, TS, 32, 4>(a, out, s);
+                case kTile32x2: return norm_fwd_aligned<TB, TS, 32, 2>(a, out, s);
+                case kTile16x5: return norm_fwd_aligned<TB, TS, 16, 5>(a, out, s);
+                default: break;
+            }
     }
     switch (t) {
-        case kTile32x1x32: return norm_fwd_tile<TB, TS, 32, 1, 32>(a, s);
-        case kTile32x1x16: return norm_fwd_tile<TB, TS, 32, 1, 16>(a, s);
-        case kTile16x1x32: return norm_fwd_tile<TB, TS, 16, 1, 32>(a, s);
-        case kTile8x1x32: return norm_fwd_tile<TB, TS, 8, 1, 32>(a, s);
-        case kTile1x1x16: return norm_fwd_tile<TB, TS, 1, 1, 16>(a, s);
-        case kTile1x1x4: return norm_fwd_tile<TB, TS, 1, 1, 4>(a, s);
+        case kTile32x4: return norm_fwd_tile<TB, TS, 32, 8, 4, true, true>(a, s);
+        case kTile32x2: return norm_fwd_tile<TB, TS, 32, 8, 2, true, true>(a, s);
+        case kTile16x4: return norm_fwd_tile<TB, TS, 16, 8, 4, true, true>(a, s);
+        case kTile8x4: return norm_fwd_tile<TB, TS, 8, 8, 4, true, true>(a, s);
         default: return fail(CSRT_ERR_ARG, "unknown tile %d", (int)t);
     }
 }

@@ -3,6 +3,6 @@
 
 namespace csrt {
 
-int norm_fwd_f32(const NormArgs &a, NormTile t, cudaStream_t s) { return norm_fwd_tiles<float, float>(a, t, s); }
+int norm_fwd_f32(const NormArgs &a, NormTile t, cudaStream_t s) { return norm_fwd_tiles<float, float>(a, t, false, false, s); }
 
 }  // namespace csrt

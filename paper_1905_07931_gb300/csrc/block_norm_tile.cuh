@@ -2,12 +2,14 @@
 //
 // A norm reduces down the columns of a feature-major matrix, so a tile is TT tokens wide and as high as the matrix: d
 // features are split over the blocks of a cluster, which exchange their sums through distributed shared memory. Each thread
-// holds V tokens (a vector of 16 bytes, or one) of F features, the same from the first load to the last store; what it
-// loads goes by cp.async into shared memory that no other thread reads. A cluster walks over the tiles of tokens, and the
-// next tile's loads are issued as soon as the present one's are in registers: they run while sums are exchanged and results
-// stored.
+// holds V tokens (eight, or one where there are one or two in all) of F features, the same from the first load to the last
+// store; what it loads goes by cp.async into shared memory that no other thread reads. A cluster walks over the tiles of
+// tokens, and the next tile's loads are issued as soon as the present one's are in registers: they run while sums are
+// exchanged and results stored.
 //
-// Rows that are not 16-byte aligned take V = 1: an element's aligned 4-byte word is fetched, and its half picked.
+// Rows that are not 16-byte aligned (UIN: of an input, UOUT: of an output): a thread fetches the aligned words that its eight
+// tokens touch and shifts them into place by its row's offset, which is the same for all of its features and tiles; results
+// pass through shared memory of the warp's and leave by single elements, 32 tokens of a row (or fewer of several) a store.
 #pragma once
 
 #include <cmath>
@@ -75,6 +77,21 @@ struct Tok<1> {
     static __device__ __forceinline__ float sum(P p) { return p; }
 };
 
+// V values that lie side by side, on a 16-byte boundary where V is eight.
+template <int V>
+__device__ __forceinline__ void load_tokens(const float *p, typename Tok<V>::P (&x)[Tok<V>::N]) {
+    if constexpr (V == 1) {
+        x[0] = *p;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const ulonglong2 v = reinterpret_cast<const ulonglong2 *>(p)[k];
+            x[2 * k] = v.x;
+            x[2 * k + 1] = v.y;
+        }
+    }
+}
+
 __device__ __forceinline__ void cp_async16(uint32_t dst, const char *src, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
@@ -97,62 +114,82 @@ struct Place {
     }
 };
 
-// A thread's own copies of one matrix: F x V elements of type T in shared memory.
-template <typename T, int TT, int V, int F>
+// A thread's own copies of one matrix: F x V elements of type T in shared memory, 16-byte words of it (V = 8, one more
+// where rows are unaligned) or 4-byte ones (V = 1).
+template <typename T, int TT, int V, int F, bool U>
 struct Held {
-    static constexpr int kWords = V == 8 ? (int)sizeof(T) / 2 : 1;       // of 16 bytes (V = 8) or 4, for one feature
-    static constexpr int kTotal = kWords * (V == 8 ? 16 : 4) * F * kNormThreads;
+    static constexpr int kSize = (int)sizeof(T);
+    static constexpr int kWord = V == 8 ? 16 : 4;
+    static constexpr int kWords = V == 8 ? kSize / 2 + (U ? 1 : 0) : 1;   // for one feature
+    static constexpr int kTotal = kWords * kWord * F * kNormThreads;
+    // How far a row's first token of this thread lies behind an aligned word, in elements.
+    static __device__ __forceinline__ int offset(const char *src) {
+        return U || V == 1 ? (int)(reinterpret_cast<uintptr_t>(src) & (kWord - 1)) / kSize : 0;
+    }
     // `src` is the matrix's first element of this thread's column and first feature. Where not all of the tile exists
-    // (!full), nv tokens and the features below `rows` are fetched and the rest is zeros.
+    // (!full), nv tokens and the features below `rows` are fetched and the rest is zeros. What shares an aligned word with
+    // an element in front of it is read too, nothing behind a row's last element.
     static __device__ __forceinline__ void fetch(char *base, const char *src, int64_t ld, bool full, int rows, int row0, int nv) {
-        uint32_t dst = (uint32_t)__cvta_generic_to_shared(base) + threadIdx.x * (V == 8 ? 16 : 4);
-        const int64_t step = ld * (int64_t)(sizeof(T) * Place<TT, V>::kStep);
-        // V = 1: the high half of a word lies behind bytes before it, the low half is fetched alone: nothing past the element
-        const bool high = V == 1 && sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(src) & 2) != 0;
-        const int bytes = sizeof(T) == 4 || high ? 4 : 2;
-        if (high) src -= 2;
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(base) + threadIdx.x * kWord;
+        const int64_t step = ld * (int64_t)(kSize * Place<TT, V>::kStep);
+        const int before = offset(src) * kSize;
+        src -= before;
+        const int bytes = before + nv * kSize;
         const char *none = reinterpret_cast<const char *>(reinterpret_cast<uintptr_t>(src) & ~(uintptr_t)15);
 #pragma unroll
         for (int f = 0; f < F; ++f, src += step) {
-            if constexpr (V == 8) {
-                if (full) {
+            if (V == 8 && !U && full) {
 #pragma unroll
-                    for (int k = 0; k < kWords; ++k) cp_async16(dst + (f * kWords + k) * kNormThreads * 16, src + 16 * k, 16);
-                } else {
-                    constexpr int each = 16 / (int)sizeof(T);
-                    const int have = row0 + f * Place<TT, V>::kStep < rows ? nv : 0;
-#pragma unroll
-                    for (int k = 0; k < kWords; ++k) {
-                        const int here = imin(imax(have - k * each, 0), each);
-                        cp_async16(dst + (f * kWords + k) * kNormThreads * 16, here > 0 ? src + 16 * k : none, here * (int)sizeof(T));
-                    }
-                }
+                for (int k = 0; k < kWords; ++k) cp_async16(dst + (f * kWords + k) * kNormThreads * 16, src + 16 * k, 16);
             } else {
-                const bool have = full || (nv > 0 && row0 + f * Place<TT, V>::kStep < rows);
-                cp_async4(dst + f * kNormThreads * 4, have ? src : none, have ? bytes : 0);
+                const bool have = full || row0 + f * Place<TT, V>::kStep < rows;
+#pragma unroll
+                for (int k = 0; k < kWords; ++k) {
+                    const int here = have && nv > 0 ? imin(imax(bytes - k * kWord, 0), kWord) : 0;
+                    const char *at = here > 0 ? src + kWord * k : none;
+                    if (V == 8) cp_async16(dst + (f * kWords + k) * kNormThreads * 16, at, here);
+                    else cp_async4(dst + f * kNormThreads * 4, at, here);
+                }
             }
         }
     }
-    // `odd`: V = 1 and 2-byte elements: bit 1 of this element's address
-    static __device__ __forceinline__ void read(const char *base, int f, bool odd, typename Tok<V>::P (&x)[Tok<V>::N]) {
+    // off: offset() of the thread's elements
+    static __device__ __forceinline__ void read(const char *base, int f, int off, typename Tok<V>::P (&x)[Tok<V>::N]) {
         if constexpr (V == 1) {
             const uint32_t w = reinterpret_cast<const uint32_t *>(base)[f * kNormThreads + threadIdx.x];
-            if constexpr (sizeof(T) == 4) x[0] = __uint_as_float(w);
-            else if constexpr (std::is_same<T, __nv_bfloat16>::value) x[0] = __uint_as_float(odd ? w & 0xffff0000u : w << 16);
-            else x[0] = __half2float(__ushort_as_half((unsigned short)(odd ? w >> 16 : w & 0xffffu)));
-        } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float4 w = reinterpret_cast<const float4 *>(base)[(f * 2 + k) * kNormThreads + threadIdx.x];
-                x[2 * k] = pack2(w.x, w.y);
-                x[2 * k + 1] = pack2(w.z, w.w);
-            }
+            if constexpr (kSize == 4) x[0] = __uint_as_float(w);
+            else if constexpr (std::is_same<T, __nv_bfloat16>::value) x[0] = __uint_as_float(off ? w & 0xffff0000u : w << 16);
+            else x[0] = __half2float(__ushort_as_half((unsigned short)(off ? w >> 16 : w & 0xffffu)));
         } else {
-            const uint4 w = reinterpret_cast<const uint4 *>(base)[f * kNormThreads + threadIdx.x];
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            constexpr int kOut = kSize * 2;      // 32-bit words of eight elements
+            uint32_t u[kWords * 4];
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) {
+                const uint4 w = reinterpret_cast<const uint4 *>(base)[(f * kWords + k) * kNormThreads + threadIdx.x];
+                u[4 * k] = w.x;
+                u[4 * k + 1] = w.y;
+                u[4 * k + 2] = w.z;
+                u[4 * k + 3] = w.w;
+            }
+            if constexpr (U) {
+                const int words = kSize == 4 ? off : off >> 1;
+                if (words & 2)
+#pragma unroll
+                    for (int k = 0; k < kOut + 2; ++k) u[k] = u[k + 2];
+                if (words & 1)
+#pragma unroll
+                    for (int k = 0; k < kOut + 1; ++k) u[k] = u[k + 1];
+                if constexpr (kSize == 2) {
+                    const int bits = (off & 1) * 16;
+#pragma unroll
+                    for (int k = 0; k < kOut; ++k) u[k] = __funnelshift_r(u[k], u[k + 1], bits);
+                }
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                if constexpr (kSize == 4) {
+                    x[k] = pack2(__uint_as_float(u[2 * k]), __uint_as_float(u[2 * k + 1]));
+                } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
                     x[k] = pack2(__uint_as_float(u[k] << 16), __uint_as_float(u[k] & 0xffff0000u));
                 } else {
                     const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&u[k]));
@@ -163,41 +200,83 @@ struct Held {
     }
 };
 
-// V values to a row's place; nv of them exist.
-template <typename T, int V>
-__device__ __forceinline__ void put_tokens(char *dst, const typename Tok<V>::P (&x)[Tok<V>::N], int nv) {
-    T *o = reinterpret_cast<T *>(dst);
-    if constexpr (V == 1) {
-        if (nv > 0) *o = from_f<T>(x[0]);
-    } else {
-        float v[8];
+// One result matrix: where a thread's elements of a tile go.
+template <typename T, int TT, int V, bool U>
+struct Result {
+    static constexpr int kSize = (int)sizeof(T);
+    static constexpr int kStageBytes = U && V == 8 ? 32 * 8 * kSize : 0;   // of a warp
+    static constexpr int kRowsStore = V == 8 && U ? 32 / TT : 1;           // features that one store of the warp spans
+    char *p;        // this lane's first element
+    int64_t row;    // bytes from a feature to the next
+    int tokens;     // this lane's that exist
+    // first: the warp's first feature in the matrix; c0: the tile's first token
+    __device__ __forceinline__ Result(const NormMat &m, int64_t first, int64_t c0, int32_t n) {
+        const int lane = threadIdx.x & 31;
+        constexpr int each = U ? 1 : V, lanes = TT / each;
+        const int64_t c = c0 + (lane % lanes) * each;
+        row = m.ld * kSize;
+        p = m.p + (first + lane / lanes) * row + c * kSize;
+        tokens = (int)imax<int64_t>(0, imin<int64_t>(each, n - c));
+    }
+    // Feature f of the thread (row0 its first within the block, of `rows`); `stage` is the warp's.
+    __device__ __forceinline__ void put(char *stage, int f, int row0, int rows, const typename Tok<V>::P (&x)[Tok<V>::N]) {
+        char *dst = p + f * Place<TT, V>::kStep * row;
+        if constexpr (V == 1) {
+            if (tokens > 0 && row0 + f * Place<TT, V>::kStep < rows) *reinterpret_cast<T *>(dst) = from_f<T>(x[0]);
+        } else {
+            uint4 w[kSize / 2];
+            if constexpr (kSize == 4) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) unpack2(x[k], v[2 * k], v[2 * k + 1]);
-        if (nv == 8) {
-            if constexpr (sizeof(T) == 4) {
-                reinterpret_cast<float4 *>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
-                reinterpret_cast<float4 *>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                for (int k = 0; k < 2; ++k) {
+                    float a, b, c, d;
+                    unpack2(x[2 * k], a, b);
+                    unpack2(x[2 * k + 1], c, d);
+                    w[k] = make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+                }
             } else {
                 uint32_t u[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
+                    float a, b;
+                    unpack2(x[k], a, b);
                     if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
                         u[k] = *reinterpret_cast<const uint32_t *>(&h);
                     } else {
-                        const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+                        const __half2 h = __floats2half2_rn(a, b);
                         u[k] = *reinterpret_cast<const uint32_t *>(&h);
                     }
                 }
-                *reinterpret_cast<uint4 *>(dst) = make_uint4(u[0], u[1], u[2], u[3]);
+                w[0] = make_uint4(u[0], u[1], u[2], u[3]);
             }
-        } else {
+            if constexpr (U) {
+                const int lane = threadIdx.x & 31;
+                const int own = (threadIdx.x >> 5) * Place<TT, V>::kRowsWarp + f * Place<TT, V>::kStep + lane / TT;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k < nv) o[k] = from_f<T>(v[k]);
+                for (int k = 0; k < kSize / 2; ++k) reinterpret_cast<uint4 *>(stage)[lane * (kSize / 2) + k] = w[k];
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j, dst += kRowsStore * row) {
+                    const T v = reinterpret_cast<const T *>(stage)[lane + 32 * j];
+                    if (tokens > 0 && own + j * kRowsStore < rows) *reinterpret_cast<T *>(dst) = v;
+                }
+                __syncwarp();
+            } else if (row0 + f * Place<TT, V>::kStep < rows) {
+                if (tokens == 8) {
+#pragma unroll
+                    for (int k = 0; k < kSize / 2; ++k) reinterpret_cast<uint4 *>(dst)[k] = w[k];
+                } else {
+                    float v[8];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) unpack2(x[k], v[2 * k], v[2 * k + 1]);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k < tokens) reinterpret_cast<T *>(dst)[k] = from_f<T>(v[k]);
+                }
+            }
         }
     }
-}
+};
 
 // ---------------------------------------------------------------------------
 // Sums over all features of a token: over a thread's features, the lanes that hold the same tokens, the warps, the
@@ -224,22 +303,25 @@ __device__ __forceinline__ void merge(float &a, float &b, float na, float a2, fl
 
 template <int TT>
 struct Exchange {
+    static constexpr int kTokensWarp = TT >= kNormWarps ? TT / kNormWarps : 1;   // tokens that a warp sums up
     float2 *slots;    // [2][cluster][TT], written by the cluster's blocks
-    float2 *part;     // [2][warps][TT]; a warp's row of the half that is not in use takes its results to its threads
-    float *part_n;    // [2][warps]
+    float2 *part;     // [warps][TT]
+    float *last;      // [2][2][TT]: two results a token
     uint64_t *bar;    // [2]
+    float *part_n;    // [warps]
     int turn;         // exchanges so far: halves alternate, as a block may be one exchange ahead of another
     int size, rank, chunk, d;
     float inv_d;
 
     static constexpr int bytes(int size) {
-        return (int)sizeof(float2) * TT * (2 * kNormWarps + 2 * size) + 2 * kNormWarps * (int)sizeof(float) + 2 * (int)sizeof(uint64_t);
+        return (int)sizeof(float2) * TT * (kNormWarps + 2 * size + 2) + kNormWarps * (int)sizeof(float) + 2 * (int)sizeof(uint64_t);
     }
     __device__ __forceinline__ Exchange(char *base, int size_, int rank_, int chunk_, int d_)
         : turn(0), size(size_), rank(rank_), chunk(chunk_), d(d_), inv_d(1.f / (float)d_) {
         slots = reinterpret_cast<float2 *>(base);
         part = slots + 2 * size * TT;
-        bar = reinterpret_cast<uint64_t *>(part + 2 * kNormWarps * TT);
+        last = reinterpret_cast<float *>(part + kNormWarps * TT);
+        bar = reinterpret_cast<uint64_t *>(last + 4 * TT);
         part_n = reinterpret_cast<float *>(bar + 2);
         if (size > 1) {
             if (threadIdx.x == 0) {
@@ -264,11 +346,31 @@ struct Exchange {
     }
 };
 
-// a, b: this thread's values for its V tokens, over n of its features. Returns the totals for token (lane % TT).
-template <int MODE, int TT, int V>
-__device__ __forceinline__ float2 cluster_total(Exchange<TT> &x, float (&a)[V], float (&b)[V], float n) {
+// Joins the values of the eight lanes that differ in the lowest three bits; all get one result.
+template <int MODE>
+__device__ __forceinline__ void join_lanes(float &a, float &b, float &n) {
+    const unsigned full = 0xffffffffu;
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+        const float nb = MODE == kMoments ? __shfl_xor_sync(full, n, o) : 0.f;
+        const float a2 = __shfl_xor_sync(full, a, o), b2 = MODE != kOneSum ? __shfl_xor_sync(full, b, o) : 0.f;
+        merge<MODE>(a, b, n, a2, b2, nb);
+        n += nb;
+    }
+    if (MODE == kMoments) {   // the merge is not symmetric to the last bit
+        const int first = threadIdx.x & 24;
+        a = __shfl_sync(full, a, first);
+        b = __shfl_sync(full, b, first);
+    }
+}
+
+// a, b: this thread's values for its V tokens, over n of its features. finish(token, total) turns a token's totals into two
+// results, which every thread gets for its tokens (x, y).
+template <int MODE, int TT, int V, typename FIN>
+__device__ __forceinline__ void exchange(Exchange<TT> &e, float (&a)[V], float (&b)[V], float n, int q, FIN finish,
+                                         typename Tok<V>::P (&x)[Tok<V>::N], typename Tok<V>::P (&y)[Tok<V>::N]) {
     constexpr int kLanes = Place<TT, V>::kLanes;
-    static_assert(V == 1 || Place<TT, V>::kRowsWarp >= V, "a lane ends with one token");
+    static_assert(V == 1 || Place<TT, V>::kRowsWarp >= V || kLanes * Place<TT, V>::kRowsWarp == 32, "lanes");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const unsigned full = 0xffffffffu;
     int token = (lane % kLanes) * V, copy = 0;   // the first token still held; lanes with `copy` hold another's
@@ -300,67 +402,57 @@ __device__ __forceinline__ float2 cluster_total(Exchange<TT> &x, float (&a)[V], 
         }
         n += nb;
     }
-    const int half = x.turn & 1;
-    float2 *part = x.part + half * kNormWarps * TT;
-    if (copy == 0) part[warp * TT + token] = make_float2(a[0], MODE != kOneSum ? b[0] : 0.f);
-    if (MODE == kMoments && lane == 0) x.part_n[half * kNormWarps + warp] = n;
-    const uint32_t bar = (uint32_t)__cvta_generic_to_shared(x.bar + half);
-    if (x.size > 1 && threadIdx.x == 0)
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(x.size * TT * 8) : "memory");
+    const int half = e.turn & 1, parity = (e.turn >> 1) & 1;
+    ++e.turn;
+    if (copy == 0) e.part[warp * TT + token] = make_float2(a[0], MODE != kOneSum ? b[0] : 0.f);
+    if (MODE == kMoments && lane == 0) e.part_n[warp] = n;
+    const uint32_t bar = (uint32_t)__cvta_generic_to_shared(e.bar + half);
+    if (e.size > 1 && threadIdx.x == 0)
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(e.size * TT * 8) : "memory");
     __syncthreads();
-    const int t = lane % TT;
-    float2 s = part[t];
-    float sn = MODE == kMoments ? x.part_n[half * kNormWarps] : 0.f;
-#pragma unroll
-    for (int w = 1; w < kNormWarps; ++w) {
-        const float2 v = part[w * TT + t];
-        const float nb = MODE == kMoments ? x.part_n[half * kNormWarps + w] : 0.f;
-        merge<MODE>(s.x, s.y, sn, v.x, v.y, nb);
-        sn += nb;
-    }
-    const int parity = (x.turn >> 1) & 1;
-    ++x.turn;
-    if (x.size == 1) return s;
-    float2 *slots = x.slots + half * x.size * TT;
-    const uint32_t own = (uint32_t)__cvta_generic_to_shared(slots + x.rank * TT + t);
-    for (int r = warp; r < x.size; r += kNormWarps)
-        if (lane < TT) {
-            uint32_t at, there;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(own), "r"(r));
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(bar), "r"(r));
-            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(at),
-                         "l"(pack2(s.x, s.y)), "r"(there)
-                         : "memory");
+    // a warp joins its tokens' eight parts, a lane each
+    constexpr int kMine = Exchange<TT>::kTokensWarp;
+    const int j = lane & 7, t = (TT >= kNormWarps ? warp * kMine : 0) + (lane >> 3) % kMine;
+    const bool mine = lane < 8 * kMine && (TT >= kNormWarps || warp == 0);   // the others hold copies
+    float2 s = e.part[j * TT + t];
+    float sn = MODE == kMoments ? e.part_n[j] : 0.f;
+    join_lanes<MODE>(s.x, s.y, sn);
+    if (e.size > 1) {
+        float2 *slots = e.slots + half * e.size * TT;
+        if (mine) {
+            const uint32_t own = (uint32_t)__cvta_generic_to_shared(slots + e.rank * TT + t);
+            for (int r = j; r < e.size; r += 8) {
+                uint32_t at, there;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(own), "r"(r));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(bar), "r"(r));
+                asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(at),
+                             "l"(pack2(s.x, s.y)), "r"(there)
+                             : "memory");
+            }
         }
-    // never runs out while the cluster lives; the results of a wait that did are NaN
-    if (!mbar_wait_bounded(x.bar + half, parity)) return make_float2(NAN, NAN);
-    s = slots[t];
-    sn = (float)imin(x.chunk, x.d);
-    for (int r = 1; r < x.size; ++r) {
-        const float2 v = slots[r * TT + t];
-        const float nb = (float)imax(0, imin(x.chunk, x.d - r * x.chunk));
-        merge<MODE>(s.x, s.y, sn, v.x, v.y, nb);
-        sn += nb;
+        // never runs out while the cluster lives; the results of a wait that did are NaN
+        const bool ok = mbar_wait_bounded(e.bar + half, parity);
+        s = make_float2(0.f, 0.f);
+        sn = 0.f;
+        for (int r = j; r < e.size; r += 8) {
+            const float2 v = slots[r * TT + t];
+            const float nb = (float)imax(0, imin(e.chunk, e.d - r * e.chunk));
+            merge<MODE>(s.x, s.y, sn, v.x, v.y, nb);
+            sn += nb;
+        }
+        __syncwarp();
+        join_lanes<MODE>(s.x, s.y, sn);
+        if (!ok) s = make_float2(NAN, NAN);
     }
-    return s;
-}
-
-// Two values for each token (a lane's, for token lane % TT) to the threads that hold it, after cluster_total. The row of
-// `part` is this warp's own: others read it only before the barrier of the last exchange and after that of the next.
-template <int TT, int V>
-__device__ __forceinline__ void to_tokens(Exchange<TT> &x, float2 own, int q, float (&a)[V], float (&b)[V]) {
-    const int lane = threadIdx.x & 31;
-    float2 *mine = x.part + ((x.turn & 1) * kNormWarps + (threadIdx.x >> 5)) * TT;
-    __syncwarp();
-    if (lane < TT) mine[lane] = own;
-    __syncwarp();
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-        const float2 v = mine[q + k];
-        a[k] = v.x;
-        b[k] = v.y;
+    s = finish(t, s);
+    float *out = e.last + half * 2 * TT;
+    if (mine && j == 0) {
+        out[t] = s.x;
+        out[TT + t] = s.y;
     }
-    __syncwarp();
+    __syncthreads();
+    load_tokens<V>(out + q, x);
+    load_tokens<V>(out + TT + q, y);
 }
 
 // 1 / sqrt(v): the approximation and a Newton step
@@ -403,16 +495,17 @@ struct TileShape {
     static constexpr int kFeatures = Place<TT, V>::kStep * F;   // of a block
     static int cluster(int32_t d) {
         const int64_t c = ceil_div<int64_t>(d, kFeatures);
-        return c <= 8 ? (int)c : c <= kNormClusterMax ? kNormClusterMax : 0;
+        return c <= kNormClusterMax ? (int)c : 0;
     }
 };
 
-// Launches `kernel` on clusters of `size` blocks, as many as fit or as there are tiles.
+// Launches `kernel` on clusters of `size` blocks, as many as fit or as there are tiles (a.groups).
 template <auto kernel>
-int launch_clusters(NormArgs a, int size, int64_t tiles, int smem, cudaStream_t s) {
+int launch_clusters(NormArgs &a, int size, int64_t tiles, int smem, cudaStream_t s) {
     static std::mutex lock;
     static int fit[64][kNormClusterMax + 1] = {{0}};
     int dev = 0;
+    CSRT_ARG(size > 0, "a cluster cannot hold %d features", a.d);
     CSRT_CHECK_CUDA(cudaGetDevice(&dev));
     CSRT_ARG(dev >= 0 && dev < 64, "device %d is out of range", dev);
     cudaLaunchAttribute attr[2];
