@@ -294,10 +294,10 @@ static int check_types(int32_t *tb, int32_t *ts) {
     return CSRT_OK;
 }
 
-// Rows of every matrix that is given in whole 16-byte words.
+// Rows of every matrix that is given in whole 16-byte words, and no further apart than a tensor map can say.
 static bool norm_vector(std::initializer_list<const csrt_mat *> all) {
     for (const csrt_mat *m : all)
-        if (m != nullptr && !tma_rows_ok(m->data, m->ld, dt_size(m->dtype))) return false;
+        if (m != nullptr && (!tma_rows_ok(m->data, m->ld, dt_size(m->dtype)) || m->ld * dt_size(m->dtype) >= (int64_t)1 << 40)) return false;
     return true;
 }
 
@@ -502,13 +502,15 @@ int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *
     a.pre = norm_side(pre);
     a.dv = norm_mat(dv);
     a.r = norm_mat(dh);
-    a.h = norm_mat(h);
-    a.y = norm_mat(y);
+    // what no result asks for is not read
+    a.h = norm_mat(dv != nullptr ? h : nullptr);
+    a.y = norm_mat(post != nullptr || dgate != nullptr ? y : nullptr);
     a.g = norm_mat(gate);
     a.dr = norm_mat(dr);
     a.dy = norm_mat(dy);
     a.dg = norm_mat(dgate);
     a.partial = reinterpret_cast<float *>(ws_scratch(ws));
+    a.hdr = static_cast<WsHeader *>(ws);
     cudaStream_t s = as_stream(stream);
     if (n == 0) {
         if (accumulate || (po->dweight == nullptr && po->dbias == nullptr && pr->dweight == nullptr && pr->dbias == nullptr))

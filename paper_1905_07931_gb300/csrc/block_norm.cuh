@@ -29,6 +29,8 @@ struct NormArgs {
     NormMat dv, dr, dy, dg;
     float *partial;                // backward: row sums of a group of tokens, [group][4][d] (post dw, db; pre dw, db)
     int32_t cluster;               // blocks that share the features of a tile
+    int32_t chunk, box, boxes;     // features of a block, and the loads that bring them
+    WsHeader *hdr;               // takes the flag of a wait that ran out, may be nullptr
     int32_t groups;                // blocks (or clusters) along the tokens, each with row sums of its own
 };
 

@@ -36,13 +36,14 @@ struct TokenSums {
     }
 };
 
-template <typename TB, typename TS, int TT, int V, int F, bool UIN, bool UOUT, int BLOCKS>
-__global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(const __grid_constant__ NormArgs a) {
+template <typename TB, typename TS, int TT, int V, int F, bool TMA, bool UOUT, int BLOCKS>
+__global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(const __grid_constant__ NormArgs a,
+                                                                                  const __grid_constant__ NormMaps maps) {
     pdl_enter();
-    extern __shared__ __align__(16) char held[];
+    extern __shared__ __align__(128) char held[];
     typedef Tok<V> T;
-    typedef Held<TB, TT, V, F, UIN> HB;
-    typedef Held<TS, TT, V, F, UIN> HS;
+    typedef typename InputOf<TMA, TB, TT, V, F>::type HB;
+    typedef typename InputOf<TMA, TS, TT, V, F>::type HS;
     typedef Result<TB, TT, V, UOUT> RB;
     typedef Result<TS, TT, V, UOUT> RS;
     typedef typename T::P P;
@@ -52,7 +53,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
     const int lane = threadIdx.x & 31;
     const int size = a.cluster;
     const int rank = size > 1 ? (int)(blockIdx.x % size) : 0;
-    const int chunk = (a.d + size - 1) / size;
+    const int chunk = a.chunk;
     const int rows = imax(0, imin(chunk, a.d - rank * chunk));
     const int64_t i0 = (int64_t)rank * chunk + (at.row0 < rows ? at.row0 : 0);
     char *p = held;
@@ -68,25 +69,43 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
     float *mine = reinterpret_cast<float *>(weights + kFeatures) + (threadIdx.x >> 5) * 4 * TT;
     char *stage = reinterpret_cast<char *>(weights + kFeatures + kNormWarps * TT) + (threadIdx.x >> 5) * RS::kStageBytes;
     Exchange<TT> ex(reinterpret_cast<char *>(weights + kFeatures + kNormWarps * TT) + kNormWarps * RS::kStageBytes, size, rank,
-                    chunk, a.d);
+                    chunk, a.d, a.hdr);
     const int64_t first = (int64_t)rank * chunk + (threadIdx.x >> 5) * at.kRowsWarp;   // the warp's first feature
     const int64_t tiles = ((int64_t)a.n + TT - 1) / TT;
     int64_t tile = blockIdx.x / size;
 
     auto column = [&](int64_t t) { return t * TT + at.q; };
     auto exist = [&](int64_t t) { return (int)imax<int64_t>(0, imin<int64_t>(V, a.n - column(t))); };
-    auto fetch = [&](auto held_type, const NormMat &m, char *dst, int bytes, int64_t t) {
+    // TMA: by the first thread, once it has announced the bytes
+    auto fetch = [&](auto held_type, const NormMat &m, int k, char *dst, int64_t t) {
         if (!m.p) return;
-        const int nv = exist(t);
-        const int64_t c = nv > 0 ? column(t) : 0;
-        const bool full = rows == kFeatures && (t + 1) * TT <= a.n;
-        decltype(held_type)::fetch(dst, m.p + (i0 * m.ld + c) * bytes, m.ld, full, rows, at.row0, nv);
+        if constexpr (TMA) {
+            load_tile(dst, maps.m + k, a, rank, t * TT, decltype(held_type)::kRow, ex.bar + (k == 3 ? 3 : 2));
+        } else {
+            const int nv = exist(t);
+            const int64_t c = nv > 0 ? column(t) : 0;
+            decltype(held_type)::fetch(dst, m.p + (i0 * m.ld + c) * decltype(held_type)::kSize, m.ld, rows, at.row0, nv);
+        }
     };
+    const int tokens = TMA ? a.box * a.boxes * TT : 0;
     auto fetch_all = [&](int64_t t) {
-        fetch(HB(), a.dv, sv, sizeof(TB), t);
-        fetch(HS(), a.h, sh, sizeof(TS), t);
-        fetch(HS(), a.r, su, sizeof(TS), t);
-        fetch(HB(), a.g, sg, sizeof(TB), t);
+        if (TMA) {
+            if (threadIdx.x != 0) return;
+            mbar_expect_tx(ex.bar + 2, tokens * ((a.dv.p ? HB::kSize : 0) + (a.h.p ? HS::kSize : 0) + (a.r.p ? HS::kSize : 0) +
+                                                 (a.g.p ? HB::kSize : 0)));
+        }
+        fetch(HB(), a.dv, 0, sv, t);
+        fetch(HS(), a.h, 1, sh, t);
+        fetch(HS(), a.r, 2, su, t);
+        fetch(HB(), a.g, 4, sg, t);
+    };
+    auto fetch_y = [&](int64_t t) {
+        if (!a.y.p) return;
+        if (TMA) {
+            if (threadIdx.x != 0) return;
+            mbar_expect_tx(ex.bar + 3, tokens * HB::kSize);
+        }
+        fetch(HB(), a.y, 3, sy, t);
     };
     auto offset = [&](auto held_type, const NormMat &m, int64_t c) {
         return decltype(held_type)::offset(m.p + (i0 * m.ld + c) * decltype(held_type)::kSize);
@@ -104,7 +123,14 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
         return s;
     };
     fetch_all(tile);
-    fetch(HB(), a.y, sy, sizeof(TB), tile);
+    fetch_y(tile);
+    if constexpr (TMA) {
+        if (a.dv.p) clear_rows<HB>(sv, chunk);
+        if (a.h.p) clear_rows<HS>(sh, chunk);
+        if (a.r.p) clear_rows<HS>(su, chunk);
+        if (a.y.p) clear_rows<HB>(sy, chunk);
+        if (a.g.p) clear_rows<HB>(sg, chunk);
+    }
     float4 stat = statistics(tile);
     for (int i = threadIdx.x; i < kFeatures; i += kNormThreads) {
         const int64_t j = (int64_t)rank * chunk + i;
@@ -121,11 +147,13 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
     const bool sums_post = a.post.dw != nullptr || a.post.db != nullptr, sums_pre = a.pre.dw != nullptr || a.pre.db != nullptr;
     TokenSums<TT, V, F> sums;
 
-    for (; tile < tiles; tile += a.groups) {
+    for (int turn = 0; tile < tiles; tile += a.groups, ++turn) {
         const int64_t c = column(tile);
         const int off_v = offset(HB(), a.dv, c), off_u = offset(HS(), a.r, c), off_h = offset(HS(), a.h, c),
                   off_y = offset(HB(), a.y, c), off_g = offset(HB(), a.g, c);
-        cp_async_wait();
+        bool ok = true;
+        if constexpr (TMA) ok = norm_wait(ex.bar + 2, turn & 1, ex.hdr);
+        else cp_async_wait();
         __syncwarp();
         if (lane < TT) {
             mine[lane] = stat.x;
@@ -144,15 +172,15 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
             load_tokens<V>(mine + (2 * post + 1) * TT + at.q, r);
         };
         // the means of s xh and of s, negated, from this thread's sums
-        auto means = [&](const P (&sa)[T::N], const P (&sb)[T::N], bool layer) {
+        auto means = [&](const P (&sa)[T::N], const P (&sb)[T::N], bool layer, auto freed) {
 #pragma unroll
             for (int k = 0; k < T::N; ++k) {
                 T::put(va, k, sa[k]);
                 T::put(vb, k, sb[k]);
             }
             auto finish = [&](int, float2 own) { return make_float2(own.x * -ex.inv_d, layer ? own.y * -ex.inv_d : 0.f); };
-            if (layer) exchange<kTwoSums>(ex, va, vb, 0.f, at.q, finish, al, on);
-            else exchange<kOneSum>(ex, va, vb, 0.f, at.q, finish, al, on);
+            if (layer) exchange<kTwoSums>(ex, va, vb, 0.f, at.q, finish, freed, al, on);
+            else exchange<kOneSum>(ex, va, vb, 0.f, at.q, finish, freed, al, on);
         };
         own_stats(0);
         if (a.pre.kind > CSRT_NORM_SCALE) {
@@ -172,7 +200,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
                     sa[k] = fma2(mul2(add2(h[k], m[k]), r[k]), s, sa[k]);
                 }
             }
-            means(sa, sb, a.pre.kind == CSRT_NORM_LAYER);
+            means(sa, sb, a.pre.kind == CSRT_NORM_LAYER, [] {});
             own_stats(0);
         }
         P x[F][T::N], sa[T::N], sb[T::N];
@@ -211,7 +239,21 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
             }
         }
         const bool more = tile + a.groups < tiles;
+        const bool stats = a.dy.p && a.post.kind > CSRT_NORM_SCALE;
+        auto next = [&] {   // all inputs but y are in registers
+            if (more) {
+                fetch_all(tile + a.groups);
+                stat = statistics(tile + a.groups);
+            }
+        };
+        if (!ok)
+#pragma unroll
+            for (int f = 0; f < F; ++f)
+#pragma unroll
+                for (int k = 0; k < T::N; ++k) x[f][k] = T::all(NAN);
         if (a.dy.p) {
+            if constexpr (TMA)
+                if (a.y.p) ok = norm_wait(ex.bar + 3, turn & 1, ex.hdr) && ok;
             own_stats(1);
 #pragma unroll
             for (int k = 0; k < T::N; ++k) sa[k] = sb[k] = T::all(0.f);
@@ -278,13 +320,16 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
                     sums.add(kSumPostB, f, T::sum(tb));
                 }
             }
-            if (more) {
-                fetch_all(tile + a.groups);
-                stat = statistics(tile + a.groups);
+            if (!TMA || !stats) {
+                if (TMA) __syncthreads();   // of all threads
+                next();
             }
-            if (a.post.kind > CSRT_NORM_SCALE) {
-                means(sa, sb, a.post.kind == CSRT_NORM_LAYER);
+            if (stats) {
+                means(sa, sb, a.post.kind == CSRT_NORM_LAYER, [&] { if (TMA) next(); });
                 own_stats(1);
+                if (!ok)
+#pragma unroll
+                    for (int k = 0; k < T::N; ++k) r[k] = T::all(NAN);
             } else {
 #pragma unroll
                 for (int k = 0; k < T::N; ++k) al[k] = on[k] = T::all(0.f);
@@ -306,10 +351,11 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
                 }
                 out_dy.put(stage, f, at.row0, rows, o);
             }
-            if (more) fetch(HB(), a.y, sy, sizeof(TB), tile + a.groups);
-        } else if (more) {
-            fetch_all(tile + a.groups);
-            stat = statistics(tile + a.groups);
+            if (TMA) __syncthreads();   // all threads have read y
+            if (more) fetch_y(tile + a.groups);
+        } else {
+            if (TMA) __syncthreads();
+            next();
         }
     }
     if (sums_post || sums_pre)
@@ -317,25 +363,38 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
     ex.leave();
 }
 
-template <typename TB, typename TS, int TT, int V, int F, bool UIN, bool UOUT, int BLOCKS>
+template <typename TB, typename TS, int TT, int V, int F, bool TMA, bool UOUT, int BLOCKS>
 int norm_bwd_tile(NormArgs &a, cudaStream_t s) {
+    typedef typename InputOf<TMA, TB, TT, V, F>::type HB;
+    typedef typename InputOf<TMA, TS, TT, V, F>::type HS;
     const int size = TileShape<TT, V, F>::cluster(a.d);
-    constexpr int b = Held<TB, TT, V, F, UIN>::kTotal, w = Held<TS, TT, V, F, UIN>::kTotal;
+    CSRT_ARG(size > 0, "a cluster cannot hold %d features", a.d);
+    const Share share = norm_share(a.d, size, TileShape<TT, V, F>::kFeatures, TMA);
+    a.chunk = share.chunk;
+    a.box = share.box;
+    a.boxes = share.boxes;
+    NormMaps maps;
+    if (TMA && (!norm_map(maps.m, a.dv, dtype_of<TB>(), a, TT) || !norm_map(maps.m + 1, a.h, dtype_of<TS>(), a, TT) ||
+                !norm_map(maps.m + 2, a.r, dtype_of<TS>(), a, TT) || !norm_map(maps.m + 3, a.y, dtype_of<TB>(), a, TT) ||
+                !norm_map(maps.m + 4, a.g, dtype_of<TB>(), a, TT)))
+        return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused a matrix");
+    constexpr int b = HB::kTotal, w = HS::kTotal;
     const int smem = (a.dv.p ? b : 0) + (a.r.p ? w : 0) + (a.h.p ? w : 0) + (a.y.p ? b : 0) + (a.g.p ? b : 0) +
                      (TileShape<TT, V, F>::kFeatures + kNormWarps * TT) * (int)sizeof(float4) +
                      kNormWarps * Result<TS, TT, V, UOUT>::kStageBytes + Exchange<TT>::bytes(size);
-    return launch_clusters<norm_bwd_tile_kernel<TB, TS, TT, V, F, UIN, UOUT, BLOCKS>>(a, size, ceil_div<int64_t>(a.n, TT), smem, s);
+    return launch_clusters<norm_bwd_tile_kernel<TB, TS, TT, V, F, TMA, UOUT, BLOCKS>>(a, maps, size, ceil_div<int64_t>(a.n, TT),
+                                                                                      smem, s);
 }
 
 template <typename TB, typename TS, int TT, int F>
 int norm_bwd_aligned(NormArgs &a, bool out, cudaStream_t s) {
-    return out ? norm_bwd_tile<TB, TS, TT, 8, F, false, false, 2>(a, s) : norm_bwd_tile<TB, TS, TT, 8, F, false, true, 2>(a, s);
+    return out ? norm_bwd_tile<TB, TS, TT, 8, F, true, false, 2>(a, s) : norm_bwd_tile<TB, TS, TT, 8, F, true, true, 2>(a, s);
 }
 
 // in, out: all rows of the inputs, or of the results, are 16-byte aligned.
 template <typename TB, typename TS>
 int norm_bwd_tiles(NormArgs &a, NormTile t, bool in, bool out, cudaStream_t s) {
-    if (t == kTile1x4) return norm_bwd_tile<TB, TS, 1, 1, 4, true, true, 2>(a, s);
+    if (t == kTile1x4) return norm_bwd_tile<TB, TS, 1, 1, 4, false, true, 2>(a, s);
     if constexpr (sizeof(TB) == 2) {
         if (in) switch (t) {
                 case kTile32x4: return norm_bwd_aligned<TB, TS, 32, 4>(a, out, s);
@@ -346,10 +405,10 @@ int norm_bwd_tiles(NormArgs &a, NormTile t, bool in, bool out, cudaStream_t s) {
             }
     }
     switch (t) {
-        case kTile32x2: return norm_bwd_tile<TB, TS, 32, 8, 2, true, true, 2>(a, s);
-        case kTile16x2: return norm_bwd_tile<TB, TS, 16, 8, 2, true, true, 2>(a, s);
-        case kTile8x2: return norm_bwd_tile<TB, TS, 8, 8, 2, true, true, 2>(a, s);
-        case kTile8x4: return norm_bwd_tile<TB, TS, 8, 8, 4, true, true, 1>(a, s);
+        case kTile32x2: return norm_bwd_tile<TB, TS, 32, 8, 2, false, true, 2>(a, s);
+        case kTile16x2: return norm_bwd_tile<TB, TS, 16, 8, 2, false, true, 2>(a, s);
+        case kTile8x2: return norm_bwd_tile<TB, TS, 8, 8, 2, false, true, 2>(a, s);
+        case kTile8x4: return norm_bwd_tile<TB, TS, 8, 8, 4, false, true, 1>(a, s);
         default: return fail(CSRT_ERR_ARG, "unknown tile %d", (int)t);
     }
 }

@@ -7,9 +7,9 @@ namespace csrt {
 
 // Mean (negated) and reciprocal deviation of this thread's V tokens, over all features; `rows` of the block's features
 // exist, x is zero beyond them. Written out by the cluster's first block.
-template <int TT, int V, int F>
+template <int TT, int V, int F, typename FREED>
 __device__ __forceinline__ void tile_stats(Exchange<TT> &ex, const NormSide &s, const Place<TT, V> &at, int rows, int64_t c0,
-                                           int32_t n, const typename Tok<V>::P (&x)[F][Tok<V>::N],
+                                           int32_t n, FREED freed, const typename Tok<V>::P (&x)[F][Tok<V>::N],
                                            typename Tok<V>::P (&m)[Tok<V>::N], typename Tok<V>::P (&r)[Tok<V>::N]) {
     typedef Tok<V> T;
     float a[V], b[V];
@@ -53,7 +53,7 @@ __device__ __forceinline__ void tile_stats(Exchange<TT> &ex, const NormSide &s, 
             T::put(a, k, mul2(sum[k], T::all(-1.f)));
             T::put(b, k, sq[k]);
         }
-        exchange<kMoments>(ex, a, b, cnt, at.q, finish, m, r);
+        exchange<kMoments>(ex, a, b, cnt, at.q, finish, freed, m, r);
     } else {
 #pragma unroll
         for (int f = 0; f < F; ++f)
@@ -61,17 +61,18 @@ __device__ __forceinline__ void tile_stats(Exchange<TT> &ex, const NormSide &s, 
             for (int k = 0; k < T::N; ++k) sq[k] = fma2(x[f][k], x[f][k], sq[k]);
 #pragma unroll
         for (int k = 0; k < T::N; ++k) T::put(a, k, sq[k]);
-        exchange<kOneSum>(ex, a, b, 0.f, at.q, [&](int t, float2 own) { return finish(t, make_float2(0.f, own.x)); }, m, r);
+        exchange<kOneSum>(ex, a, b, 0.f, at.q, [&](int t, float2 own) { return finish(t, make_float2(0.f, own.x)); }, freed, m, r);
     }
 }
 
-template <typename TB, typename TS, int TT, int V, int F, bool UIN, bool UOUT>
-__global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __grid_constant__ NormArgs a) {
+template <typename TB, typename TS, int TT, int V, int F, bool TMA, bool UOUT>
+__global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __grid_constant__ NormArgs a,
+                                                                             const __grid_constant__ NormMaps maps) {
     pdl_enter();
-    extern __shared__ __align__(16) char held[];
+    extern __shared__ __align__(128) char held[];
     typedef Tok<V> T;
-    typedef Held<TB, TT, V, F, UIN> HB;
-    typedef Held<TS, TT, V, F, UIN> HS;
+    typedef typename InputOf<TMA, TB, TT, V, F>::type HB;
+    typedef typename InputOf<TMA, TS, TT, V, F>::type HS;
     typedef Result<TB, TT, V, UOUT> RB;
     typedef Result<TS, TT, V, UOUT> RS;
     typedef typename T::P P;
@@ -80,13 +81,13 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
     const Place<TT, V> at;
     const int size = a.cluster;
     const int rank = size > 1 ? (int)(blockIdx.x % size) : 0;
-    const int chunk = (a.d + size - 1) / size;
+    const int chunk = a.chunk;
     const int rows = imax(0, imin(chunk, a.d - rank * chunk));
     const int64_t i0 = (int64_t)rank * chunk + (at.row0 < rows ? at.row0 : 0);
     char *sy = held, *sg = sy + (a.y.p ? HB::kTotal : 0), *sr = sg + (a.g.p ? HB::kTotal : 0);
     float2 *wpost = reinterpret_cast<float2 *>(sr + (a.r.p ? HS::kTotal : 0)), *wpre = wpost + kFeatures;   // weight, bias
     char *stage = reinterpret_cast<char *>(wpre + kFeatures) + (threadIdx.x >> 5) * RS::kStageBytes;   // this warp's
-    Exchange<TT> ex(reinterpret_cast<char *>(wpre + kFeatures) + kNormWarps * RS::kStageBytes, size, rank, chunk, a.d);
+    Exchange<TT> ex(reinterpret_cast<char *>(wpre + kFeatures) + kNormWarps * RS::kStageBytes, size, rank, chunk, a.d, a.hdr);
     const int64_t first = (int64_t)rank * chunk + (threadIdx.x >> 5) * at.kRowsWarp;   // the warp's first feature
     const int64_t tiles = ((int64_t)a.n + TT - 1) / TT;
     int64_t tile = blockIdx.x / size;
@@ -94,17 +95,31 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
     auto column = [&](int64_t t) { return t * TT + at.q; };
     auto exist = [&](int64_t t) { return (int)imax<int64_t>(0, imin<int64_t>(V, a.n - column(t))); };
     auto fetch = [&](int64_t t) {
-        const int nv = exist(t);
-        const int64_t c = nv > 0 ? column(t) : 0;
-        const bool full = rows == kFeatures && (t + 1) * TT <= a.n;
-        if (a.y.p) HB::fetch(sy, a.y.p + (i0 * a.y.ld + c) * sizeof(TB), a.y.ld, full, rows, at.row0, nv);
-        if (a.g.p) HB::fetch(sg, a.g.p + (i0 * a.g.ld + c) * sizeof(TB), a.g.ld, full, rows, at.row0, nv);
-        if (a.r.p) HS::fetch(sr, a.r.p + (i0 * a.r.ld + c) * sizeof(TS), a.r.ld, full, rows, at.row0, nv);
+        if constexpr (TMA) {
+            if (threadIdx.x != 0) return;
+            uint64_t *bar = ex.bar + 2;
+            const int tokens = a.box * a.boxes * TT;
+            mbar_expect_tx(bar, tokens * ((a.y.p ? HB::kSize : 0) + (a.g.p ? HB::kSize : 0) + (a.r.p ? HS::kSize : 0)));
+            if (a.y.p) load_tile(sy, maps.m, a, rank, t * TT, HB::kRow, bar);
+            if (a.g.p) load_tile(sg, maps.m + 1, a, rank, t * TT, HB::kRow, bar);
+            if (a.r.p) load_tile(sr, maps.m + 2, a, rank, t * TT, HS::kRow, bar);
+        } else {
+            const int nv = exist(t);
+            const int64_t c = nv > 0 ? column(t) : 0;
+            if (a.y.p) HB::fetch(sy, a.y.p + (i0 * a.y.ld + c) * sizeof(TB), a.y.ld, rows, at.row0, nv);
+            if (a.g.p) HB::fetch(sg, a.g.p + (i0 * a.g.ld + c) * sizeof(TB), a.g.ld, rows, at.row0, nv);
+            if (a.r.p) HS::fetch(sr, a.r.p + (i0 * a.r.ld + c) * sizeof(TS), a.r.ld, rows, at.row0, nv);
+        }
     };
     auto offset = [&](auto held_type, const NormMat &m, int64_t c) {
         return decltype(held_type)::offset(m.p + (i0 * m.ld + c) * decltype(held_type)::kSize);
     };
     fetch(tile);
+    if constexpr (TMA) {
+        if (a.y.p) clear_rows<HB>(sy, chunk);
+        if (a.g.p) clear_rows<HB>(sg, chunk);
+        if (a.r.p) clear_rows<HS>(sr, chunk);
+    }
     // weights; zeros beyond `rows`, so that what is computed there is zero
     for (int i = threadIdx.x; i < kFeatures; i += kNormThreads) {
         const int64_t j = (int64_t)rank * chunk + i;
@@ -121,14 +136,16 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
     __syncthreads();
     ex.started();
 
-    for (; tile < tiles; tile += a.groups) {
+    for (int turn = 0; tile < tiles; tile += a.groups, ++turn) {
         const int64_t c = column(tile);
         P x[F][T::N], m[T::N], r[T::N];
         RS out_h(a.h, first, tile * TT, a.n);
         auto put_h = [&](int f) {
             if (a.h.p) out_h.put(stage, f, at.row0, rows, x[f]);
         };
-        cp_async_wait();
+        bool ok = true;
+        if constexpr (TMA) ok = norm_wait(ex.bar + 2, turn & 1, ex.hdr);
+        else cp_async_wait();
         const int off_r = offset(HS(), a.r, c);
         if (a.y.p) {
             const int off_y = offset(HB(), a.y, c), off_g = offset(HB(), a.g, c);
@@ -139,7 +156,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
                 m[k] = T::all(0.f);
                 r[k] = T::all(1.f);
             }
-            if (a.post.kind > CSRT_NORM_SCALE) tile_stats<TT, V, F>(ex, a.post, at, rows, tile * TT, a.n, x, m, r);
+            if (a.post.kind > CSRT_NORM_SCALE) tile_stats<TT, V, F>(ex, a.post, at, rows, tile * TT, a.n, [] {}, x, m, r);
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 const float2 w = wpost[at.row0 + f * at.kStep];
@@ -179,14 +196,25 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
                 put_h(f);
             }
         }
-        if (tile + a.groups < tiles) fetch(tile + a.groups);
+        auto next = [&] {   // the inputs are in registers
+            if (tile + a.groups < tiles) fetch(tile + a.groups);
+        };
+        const bool stats = a.pre.kind > CSRT_NORM_SCALE;
+        if (!TMA || !stats) {
+            if (TMA) __syncthreads();   // of all threads
+            next();
+        }
         if (!a.v.p) continue;
 #pragma unroll
         for (int k = 0; k < T::N; ++k) {
             m[k] = T::all(0.f);
             r[k] = T::all(1.f);
         }
-        if (a.pre.kind > CSRT_NORM_SCALE) tile_stats<TT, V, F>(ex, a.pre, at, rows, tile * TT, a.n, x, m, r);
+        if (stats)
+            tile_stats<TT, V, F>(ex, a.pre, at, rows, tile * TT, a.n, [&] { if (TMA) next(); }, x, m, r);
+        if (!ok)
+#pragma unroll
+            for (int k = 0; k < T::N; ++k) r[k] = T::all(NAN);
         RB out_v(a.v, first, tile * TT, a.n);
 #pragma unroll
         for (int f = 0; f < F; ++f) {
@@ -200,26 +228,36 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
     ex.leave();
 }
 
-template <typename TB, typename TS, int TT, int V, int F, bool UIN, bool UOUT>
+template <typename TB, typename TS, int TT, int V, int F, bool TMA, bool UOUT>
 int norm_fwd_tile(NormArgs a, cudaStream_t s) {
+    typedef typename InputOf<TMA, TB, TT, V, F>::type HB;
+    typedef typename InputOf<TMA, TS, TT, V, F>::type HS;
     const int size = TileShape<TT, V, F>::cluster(a.d);
-    constexpr int b = Held<TB, TT, V, F, UIN>::kTotal, w = Held<TS, TT, V, F, UIN>::kTotal;
-    const int smem = (a.y.p ? b : 0) + (a.g.p ? b : 0) + (a.r.p ? w : 0) + TileShape<TT, V, F>::kFeatures * 16 +
-                     kNormWarps * Result<TS, TT, V, UOUT>::kStageBytes + Exchange<TT>::bytes(size);
-    return launch_clusters<norm_fwd_tile_kernel<TB, TS, TT, V, F, UIN, UOUT>>(a, size, ceil_div<int64_t>(a.n, TT), smem, s);
+    CSRT_ARG(size > 0, "a cluster cannot hold %d features", a.d);
+    const Share share = norm_share(a.d, size, TileShape<TT, V, F>::kFeatures, TMA);
+    a.chunk = share.chunk;
+    a.box = share.box;
+    a.boxes = share.boxes;
+    NormMaps maps;
+    if (TMA && (!norm_map(maps.m, a.y, dtype_of<TB>(), a, TT) || !norm_map(maps.m + 1, a.g, dtype_of<TB>(), a, TT) ||
+                !norm_map(maps.m + 2, a.r, dtype_of<TS>(), a, TT)))
+        return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused a matrix");
+    const int smem = (a.y.p ? HB::kTotal : 0) + (a.g.p ? HB::kTotal : 0) + (a.r.p ? HS::kTotal : 0) +
+                     TileShape<TT, V, F>::kFeatures * 16 + kNormWarps * Result<TS, TT, V, UOUT>::kStageBytes + Exchange<TT>::bytes(size);
+    return launch_clusters<norm_fwd_tile_kernel<TB, TS, TT, V, F, TMA, UOUT>>(a, maps, size, ceil_div<int64_t>(a.n, TT), smem, s);
 }
 
 template <typename TB, typename TS, int TT, int F>
 int norm_fwd_aligned(const NormArgs &a, bool out, cudaStream_t s) {
-    return out ? norm_fwd_tile<TB, TS, TT, 8, F, false, false>(a, s) : norm_fwd_tile<TB, TS, TT, 8, F, false, true>(a, s);
+    return out ? norm_fwd_tile<TB, TS, TT, 8, F, true, false>(a, s) : norm_fwd_tile<TB, TS, TT, 8, F, true, true>(a, s);
 }
 
 // in, out: all rows of the inputs, or of the results, are 16-byte aligned.
 template <typename TB, typename TS>
 int norm_fwd_tiles(const NormArgs &a, NormTile t, bool in, bool out, cudaStream_t s) {
     switch (t) {
-        case kTile1x4: return norm_fwd_tile<TB, TS, 1, 1, 4, true, true>(a, s);
-        case kTile1x16: return norm_fwd_tile<TB, TS, 1, 1, 16, true, true>(a, s);
+        case kTile1x4: return norm_fwd_tile<TB, TS, 1, 1, 4, false, true>(a, s);
+        case kTile1x16: return norm_fwd_tile<TB, TS, 1, 1, 16, false, true>(a, s);
         default: break;
     }
     if constexpr (sizeof(TB) == 2) {
@@ -232,10 +270,10 @@ int norm_fwd_tiles(const NormArgs &a, NormTile t, bool in, bool out, cudaStream_
             }
     }
     switch (t) {
-        case kTile32x4: return norm_fwd_tile<TB, TS, 32, 8, 4, true, true>(a, s);
-        case kTile32x2: return norm_fwd_tile<TB, TS, 32, 8, 2, true, true>(a, s);
-        case kTile16x4: return norm_fwd_tile<TB, TS, 16, 8, 4, true, true>(a, s);
-        case kTile8x4: return norm_fwd_tile<TB, TS, 8, 8, 4, true, true>(a, s);
+        case kTile32x4: return norm_fwd_tile<TB, TS, 32, 8, 4, false, true>(a, s);
+        case kTile32x2: return norm_fwd_tile<TB, TS, 32, 8, 2, false, true>(a, s);
+        case kTile16x4: return norm_fwd_tile<TB, TS, 16, 8, 4, false, true>(a, s);
+        case kTile8x4: return norm_fwd_tile<TB, TS, 8, 8, 4, false, true>(a, s);
         default: return fail(CSRT_ERR_ARG, "unknown tile %d", (int)t);
     }
 }

@@ -3,13 +3,15 @@
 // A norm reduces down the columns of a feature-major matrix, so a tile is TT tokens wide and as high as the matrix: d
 // features are split over the blocks of a cluster, which exchange their sums through distributed shared memory. Each thread
 // holds V tokens (eight, or one where there are one or two in all) of F features, the same from the first load to the last
-// store; what it loads goes by cp.async into shared memory that no other thread reads. A cluster walks over the tiles of
-// tokens, and the next tile's loads are issued as soon as the present one's are in registers: they run while sums are
-// exchanged and results stored.
+// store. A cluster walks over the tiles of tokens, and the next tile's loads are issued as soon as the present one's are in
+// registers: they run while sums are exchanged and results stored.
 //
-// Rows that are not 16-byte aligned (UIN: of an input, UOUT: of an output): a thread fetches the aligned words that its eight
-// tokens touch and shifts them into place by its row's offset, which is the same for all of its features and tiles; results
-// pass through shared memory of the warp's and leave by single elements, 32 tokens of a row (or fewer of several) a store.
+// Aligned inputs (16-byte rows) come by TMA. Fetched by cp.async, with the same overlap, the threads stood at the issue of
+// their loads for 15% to 35% of the time, as the memory pipe takes only so many.
+// Other rows (U): a thread fetches the aligned words that its eight tokens touch by cp.async, into shared memory that no
+// other thread reads, and shifts them into place by its row's offset, which is the same for all of its features and tiles.
+// Results whose rows are unaligned (UOUT) pass through shared memory of the warp's and leave by single elements, 32 tokens of
+// a row (or fewer of several) a store.
 #pragma once
 
 #include <cmath>
@@ -17,7 +19,7 @@
 #include <type_traits>
 
 #include "block_norm.cuh"
-#include "mat.cuh"
+#include "gemm16_host.cuh"
 
 namespace csrt {
 
@@ -114,42 +116,81 @@ struct Place {
     }
 };
 
-// A thread's own copies of one matrix: F x V elements of type T in shared memory, 16-byte words of it (V = 8, one more
-// where rows are unaligned) or 4-byte ones (V = 1).
-template <typename T, int TT, int V, int F, bool U>
+// Eight elements, from the 32-bit words that hold them.
+template <typename T>
+__device__ __forceinline__ void unpack_words(const uint32_t *u, f32x2 (&x)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(T) == 4) {
+            x[k] = pack2(__uint_as_float(u[2 * k]), __uint_as_float(u[2 * k + 1]));
+        } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+            x[k] = pack2(__uint_as_float(u[k] << 16), __uint_as_float(u[k] & 0xffff0000u));
+        } else {
+            const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(u + k));
+            x[k] = pack2(v.x, v.y);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void unpack_words(const uint4 *w, f32x2 (&x)[4]) {
+    uint32_t u[8];
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+        const uint4 v = w[k];
+        u[4 * k] = v.x;
+        u[4 * k + 1] = v.y;
+        u[4 * k + 2] = v.z;
+        u[4 * k + 3] = v.w;
+    }
+    unpack_words<T>(u, x);
+}
+
+// Inputs by TMA: the block's features x TT tokens of one matrix, a row after the other.
+template <typename T, int TT, int F>
+struct Tiled {
+    static constexpr int kSize = (int)sizeof(T);
+    static constexpr int kRow = TT * kSize;
+    static constexpr int kTotal = Place<TT, 8>::kStep * F * kRow;
+    static __device__ __forceinline__ int offset(const char *) { return 0; }
+    static __device__ __forceinline__ void read(const char *base, int f, int, f32x2 (&x)[4]) {
+        const Place<TT, 8> at;
+        unpack_words<T>(reinterpret_cast<const uint4 *>(base + (at.row0 + f * at.kStep) * kRow + at.q * kSize), x);
+    }
+};
+
+// A thread's own copies of one matrix: F x V elements of type T in shared memory, 16-byte words of it (V = 8, one more than
+// they fill) or 4-byte ones (V = 1).
+template <typename T, int TT, int V, int F>
 struct Held {
     static constexpr int kSize = (int)sizeof(T);
     static constexpr int kWord = V == 8 ? 16 : 4;
-    static constexpr int kWords = V == 8 ? kSize / 2 + (U ? 1 : 0) : 1;   // for one feature
+    static constexpr int kWords = V == 8 ? kSize / 2 + 1 : 1;   // for one feature
     static constexpr int kTotal = kWords * kWord * F * kNormThreads;
     // How far a row's first token of this thread lies behind an aligned word, in elements.
     static __device__ __forceinline__ int offset(const char *src) {
-        return U || V == 1 ? (int)(reinterpret_cast<uintptr_t>(src) & (kWord - 1)) / kSize : 0;
+        return (int)(reinterpret_cast<uintptr_t>(src) & (kWord - 1)) / kSize;
     }
-    // `src` is the matrix's first element of this thread's column and first feature. Where not all of the tile exists
-    // (!full), nv tokens and the features below `rows` are fetched and the rest is zeros. What shares an aligned word with
-    // an element in front of it is read too, nothing behind a row's last element.
-    static __device__ __forceinline__ void fetch(char *base, const char *src, int64_t ld, bool full, int rows, int row0, int nv) {
+    // `src` is the matrix's first element of this thread's column and first feature. nv tokens and the features below `rows`
+    // are fetched and the rest is zeros. What shares an aligned word with an element in front of it is read too, nothing
+    // behind a row's last element.
+    static __device__ __forceinline__ void fetch(char *base, const char *src, int64_t ld, int rows, int row0, int nv) {
         const uint32_t dst = (uint32_t)__cvta_generic_to_shared(base) + threadIdx.x * kWord;
         const int64_t step = ld * (int64_t)(kSize * Place<TT, V>::kStep);
         const int before = offset(src) * kSize;
         src -= before;
-        const int bytes = before + nv * kSize;
         const char *none = reinterpret_cast<const char *>(reinterpret_cast<uintptr_t>(src) & ~(uintptr_t)15);
+        int bytes[kWords];
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) bytes[k] = nv > 0 ? imin(imax(before + nv * kSize - k * kWord, 0), kWord) : 0;
 #pragma unroll
         for (int f = 0; f < F; ++f, src += step) {
-            if (V == 8 && !U && full) {
+            const bool have = row0 + f * Place<TT, V>::kStep < rows;
 #pragma unroll
-                for (int k = 0; k < kWords; ++k) cp_async16(dst + (f * kWords + k) * kNormThreads * 16, src + 16 * k, 16);
-            } else {
-                const bool have = full || row0 + f * Place<TT, V>::kStep < rows;
-#pragma unroll
-                for (int k = 0; k < kWords; ++k) {
-                    const int here = have && nv > 0 ? imin(imax(bytes - k * kWord, 0), kWord) : 0;
-                    const char *at = here > 0 ? src + kWord * k : none;
-                    if (V == 8) cp_async16(dst + (f * kWords + k) * kNormThreads * 16, at, here);
-                    else cp_async4(dst + f * kNormThreads * 4, at, here);
-                }
+            for (int k = 0; k < kWords; ++k) {
+                const int here = have ? bytes[k] : 0;
+                const char *at = here > 0 ? src + kWord * k : none;
+                if (V == 8) cp_async16(dst + (f * kWords + k) * kNormThreads * 16, at, here);
+                else cp_async4(dst + f * kNormThreads * 4, at, here);
             }
         }
     }
@@ -171,33 +212,30 @@ struct Held {
                 u[4 * k + 2] = w.z;
                 u[4 * k + 3] = w.w;
             }
-            if constexpr (U) {
-                const int words = kSize == 4 ? off : off >> 1;
-                if (words & 2)
+            const int words = kSize == 4 ? off : off >> 1;
+            if (words & 2)
 #pragma unroll
-                    for (int k = 0; k < kOut + 2; ++k) u[k] = u[k + 2];
-                if (words & 1)
+                for (int k = 0; k < kOut + 2; ++k) u[k] = u[k + 2];
+            if (words & 1)
 #pragma unroll
-                    for (int k = 0; k < kOut + 1; ++k) u[k] = u[k + 1];
-                if constexpr (kSize == 2) {
-                    const int bits = (off & 1) * 16;
+                for (int k = 0; k < kOut + 1; ++k) u[k] = u[k + 1];
+            if constexpr (kSize == 2) {
+                const int bits = (off & 1) * 16;
 #pragma unroll
-                    for (int k = 0; k < kOut; ++k) u[k] = __funnelshift_r(u[k], u[k + 1], bits);
-                }
+                for (int k = 0; k < kOut; ++k) u[k] = __funnelshift_r(u[k], u[k + 1], bits);
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if constexpr (kSize == 4) {
-                    x[k] = pack2(__uint_as_float(u[2 * k]), __uint_as_float(u[2 * k + 1]));
-                } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-                    x[k] = pack2(__uint_as_float(u[k] << 16), __uint_as_float(u[k] & 0xffff0000u));
-                } else {
-                    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&u[k]));
-                    x[k] = pack2(v.x, v.y);
-                }
-            }
+            unpack_words<T>(u, x);
         }
     }
+};
+
+template <bool TMA, typename T, int TT, int V, int F>
+struct InputOf {
+    typedef Held<T, TT, V, F> type;
+};
+template <typename T, int TT, int F>
+struct InputOf<true, T, TT, 8, F> {
+    typedef Tiled<T, TT, F> type;
 };
 
 // One result matrix: where a thread's elements of a tile go.
@@ -301,37 +339,55 @@ __device__ __forceinline__ void merge(float &a, float &b, float na, float a2, fl
     b = b + b2 + delta * delta * (na * share);
 }
 
+// Bounded wait for a phase of an mbarrier (try_wait suspends the thread for a while at a time). It never runs out while the
+// cluster lives: results of a wait that did are NaN.
+__device__ __forceinline__ bool norm_wait(uint64_t *bar, uint32_t parity, WsHeader *hdr) {
+    const uint32_t addr = smem_u32(bar);
+    for (unsigned i = 0; i < kSpinLimit; ++i) {
+        uint32_t done;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+            " selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(done)
+            : "r"(addr), "r"(parity)
+            : "memory");
+        if (done) return true;
+        if (i > 64) __nanosleep(32);
+    }
+    if (hdr != nullptr) dev_flag(hdr, CSRT_DEV_TIMEOUT);
+    return false;
+}
+
 template <int TT>
 struct Exchange {
     static constexpr int kTokensWarp = TT >= kNormWarps ? TT / kNormWarps : 1;   // tokens that a warp sums up
     float2 *slots;    // [2][cluster][TT], written by the cluster's blocks
     float2 *part;     // [warps][TT]
     float *last;      // [2][2][TT]: two results a token
-    uint64_t *bar;    // [2]
+    uint64_t *bar;    // [2]; behind them two for loads
     float *part_n;    // [warps]
+    WsHeader *hdr;    // takes a flag if a wait runs out, may be NULL
     int turn;         // exchanges so far: halves alternate, as a block may be one exchange ahead of another
     int size, rank, chunk, d;
     float inv_d;
 
     static constexpr int bytes(int size) {
-        return (int)sizeof(float2) * TT * (kNormWarps + 2 * size + 2) + kNormWarps * (int)sizeof(float) + 2 * (int)sizeof(uint64_t);
+        return (int)sizeof(float2) * TT * (kNormWarps + 2 * size + 2) + kNormWarps * (int)sizeof(float) + 4 * (int)sizeof(uint64_t);
     }
-    __device__ __forceinline__ Exchange(char *base, int size_, int rank_, int chunk_, int d_)
-        : turn(0), size(size_), rank(rank_), chunk(chunk_), d(d_), inv_d(1.f / (float)d_) {
+    __device__ __forceinline__ Exchange(char *base, int size_, int rank_, int chunk_, int d_, WsHeader *hdr_)
+        : hdr(hdr_), turn(0), size(size_), rank(rank_), chunk(chunk_), d(d_), inv_d(1.f / (float)d_) {
         slots = reinterpret_cast<float2 *>(base);
         part = slots + 2 * size * TT;
         last = reinterpret_cast<float *>(part + kNormWarps * TT);
         bar = reinterpret_cast<uint64_t *>(last + 4 * TT);
-        part_n = reinterpret_cast<float *>(bar + 2);
-        if (size > 1) {
-            if (threadIdx.x == 0) {
-                for (int k = 0; k < 2; ++k)
-                    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(bar + k)) : "memory");
-                asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-            }
-            __syncthreads();
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        part_n = reinterpret_cast<float *>(bar + 4);
+        if (threadIdx.x == 0) {
+            for (int k = 0; k < 4; ++k) mbar_init(bar + k, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
+        __syncthreads();
+        if (size > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
     // Every block has started and its barriers are set; before the first exchange.
     __device__ __forceinline__ void started() const {
@@ -365,9 +421,9 @@ __device__ __forceinline__ void join_lanes(float &a, float &b, float &n) {
 }
 
 // a, b: this thread's values for its V tokens, over n of its features. finish(token, total) turns a token's totals into two
-// results, which every thread gets for its tokens (x, y).
-template <int MODE, int TT, int V, typename FIN>
-__device__ __forceinline__ void exchange(Exchange<TT> &e, float (&a)[V], float (&b)[V], float n, int q, FIN finish,
+// results, which every thread gets for its tokens (x, y). freed() runs once all threads of the block have come here.
+template <int MODE, int TT, int V, typename FIN, typename FREED>
+__device__ __forceinline__ void exchange(Exchange<TT> &e, float (&a)[V], float (&b)[V], float n, int q, FIN finish, FREED freed,
                                          typename Tok<V>::P (&x)[Tok<V>::N], typename Tok<V>::P (&y)[Tok<V>::N]) {
     constexpr int kLanes = Place<TT, V>::kLanes;
     static_assert(V == 1 || Place<TT, V>::kRowsWarp >= V || kLanes * Place<TT, V>::kRowsWarp == 32, "lanes");
@@ -410,6 +466,7 @@ __device__ __forceinline__ void exchange(Exchange<TT> &e, float (&a)[V], float (
     if (e.size > 1 && threadIdx.x == 0)
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(e.size * TT * 8) : "memory");
     __syncthreads();
+    freed();
     // a warp joins its tokens' eight parts, a lane each
     constexpr int kMine = Exchange<TT>::kTokensWarp;
     const int j = lane & 7, t = (TT >= kNormWarps ? warp * kMine : 0) + (lane >> 3) % kMine;
@@ -430,8 +487,7 @@ __device__ __forceinline__ void exchange(Exchange<TT> &e, float (&a)[V], float (
                              : "memory");
             }
         }
-        // never runs out while the cluster lives; the results of a wait that did are NaN
-        const bool ok = mbar_wait_bounded(e.bar + half, parity);
+        const bool ok = norm_wait(e.bar + half, parity, e.hdr);
         s = make_float2(0.f, 0.f);
         sn = 0.f;
         for (int r = j; r < e.size; r += 8) {
@@ -499,9 +555,51 @@ struct TileShape {
     }
 };
 
+// A block's share of the features: `box` of them a TMA load, `boxes` loads.
+struct Share {
+    int chunk, box, boxes;
+};
+inline Share norm_share(int32_t d, int size, int most, bool tma) {
+    Share s = {(int)ceil_div<int64_t>(d, size), 0, 0};
+    if (!tma) return s;
+    for (s.boxes = ceil_div(s.chunk, 256);; ++s.boxes) {   // a box is at most 256 rows, of whole 128 bytes of shared memory
+        s.box = ceil_div(ceil_div(s.chunk, s.boxes), 8) * 8;
+        if (s.box * s.boxes <= most) break;
+    }
+    s.chunk = s.box * s.boxes;
+    return s;
+}
+
+struct NormMaps {
+    CUtensorMap m[5];
+};
+inline bool norm_map(CUtensorMap *map, const NormMat &m, int dtype, const NormArgs &a, int width) {
+    return m.p == nullptr || make_map3(map, m.p, dtype, a.d, a.n, m.ld, 1, 0, width, a.box, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+template <typename T>
+constexpr int dtype_of() {
+    return sizeof(T) == 4 ? CSRT_DT_F32 : std::is_same<T, __half>::value ? CSRT_DT_F16 : CSRT_DT_BF16;
+}
+// All boxes of one matrix's tile, by one thread.
+__device__ __forceinline__ void load_tile(char *dst, const CUtensorMap *map, const NormArgs &a, int rank, int64_t token, int row_bytes,
+                                          uint64_t *bar) {
+    for (int k = 0; k < a.boxes; ++k)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                smem_u32(dst + k * a.box * row_bytes)),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"((int)token), "r"(rank * a.chunk + k * a.box), "r"(0), "r"(smem_u32(bar))
+            : "memory");
+}
+
+// Zeros in the features of a tile that no box brings.
+template <typename H>
+__device__ __forceinline__ void clear_rows(char *tile, int chunk) {
+    for (int i = chunk * H::kRow + (int)threadIdx.x * 4; i < H::kTotal; i += kNormThreads * 4) *reinterpret_cast<uint32_t *>(tile + i) = 0;
+}
+
 // Launches `kernel` on clusters of `size` blocks, as many as fit or as there are tiles (a.groups).
 template <auto kernel>
-int launch_clusters(NormArgs &a, int size, int64_t tiles, int smem, cudaStream_t s) {
+int launch_clusters(NormArgs &a, const NormMaps &maps, int size, int64_t tiles, int smem, cudaStream_t s) {
     static std::mutex lock;
     static int fit[64][kNormClusterMax + 1] = {{0}};
     int dev = 0;
@@ -537,7 +635,7 @@ int launch_clusters(NormArgs &a, int size, int64_t tiles, int smem, cudaStream_t
     a.groups = (int32_t)imin<int64_t>(imin<int64_t>(tiles, resident), kNormGroups);
     cfg.gridDim = dim3((unsigned)(a.groups * size));
     cfg.numAttrs = 2;
-    CSRT_CHECK_CUDA(cudaLaunchKernelEx(&cfg, kernel, a));
+    CSRT_CHECK_CUDA(cudaLaunchKernelEx(&cfg, kernel, a, maps));
     count_launch();
     return CSRT_OK;
 }
