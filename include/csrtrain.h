@@ -489,8 +489,8 @@ int csrt_embed_fwd(const csrt_mat *table, const int32_t *tokens, float scale, cs
                    void *stream);
 
 /* csrt_embed_bwd -- the table's gradient: dtable[v, :] = scale * the sum of
- * dx[:, c] over the tokens c that are v, in ascending c (float32, rounded
- * once). accumulate == 0 writes every row (zeros where no token is v);
+ * dx[:, c] over the tokens c that are v (float32, in one order whatever the
+ * timing, rounded once). accumulate == 0 writes every row (zeros where no token is v);
  * accumulate != 0 adds to the rows that have tokens and touches no other.
  * Results repeat bit for bit. */
 int csrt_embed_bwd(const csrt_mat *dx, const int32_t *tokens, float scale, int32_t accumulate, csrt_mat *dtable,

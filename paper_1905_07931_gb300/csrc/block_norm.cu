@@ -301,7 +301,8 @@ static bool norm_vector(std::initializer_list<const csrt_mat *> all) {
     return true;
 }
 
-static NormTile norm_fwd_choice(const NormArgs &a, bool in) {
+// wide: the stream is wider than the block's matrices.
+static NormTile norm_fwd_choice(const NormArgs &a, bool in, bool wide) {
     const int64_t d = a.d, tiles = ceil_div<int64_t>(a.n, 32);
     if (a.n <= 2) return d > 65536 ? kTileColumns : d <= 16384 ? kTile1x4 : kTile1x16;
     if (d > 16384) return kTileColumns;
@@ -310,7 +311,8 @@ static NormTile norm_fwd_choice(const NormArgs &a, bool in) {
     if (d <= 2048 && tiles * ceil_div<int64_t>(d, 128) <= 2 * num_sms()) return kTile32x2;
     if (!in) return d <= 4096 ? kTile32x4 : kTile16x4;
     if (d <= 4096 && tiles * ceil_div<int64_t>(d, 256) <= 2 * num_sms()) return kTile32x4;
-    return kTile32x8;
+    // 32 tokens of 512 features of a float32 stream leave one block an SM (4096 x 8192: 129 us, half the tile 111)
+    return wide && d > 2048 ? kTile16x4 : kTile32x8;
 }
 
 template <typename TB, typename TS>
@@ -418,8 +420,8 @@ int csrt_block_norm_fwd(const csrt_mat *y, const csrt_norm *post, const csrt_mat
     a.r = norm_mat(r);
     a.h = norm_mat(h);
     a.v = norm_mat(v);
-    const bool in = tb != CSRT_DT_F32 && norm_vector({y, gate, r}), out = norm_vector({h, v});
-    const NormTile t = norm_fwd_choice(a, in);
+    const bool in = tb != CSRT_DT_F32 && norm_vector({y, gate, r}), out = norm_vector({h, v}) && n % 8 == 0;
+    const NormTile t = norm_fwd_choice(a, in, ts != tb);
     if (t == kTileColumns) return CSRT_NORM_DISPATCH(launch_fwd, tb, ts, a, as_stream(stream));
     const bool wide = ts == CSRT_DT_F32;
     return tb == CSRT_DT_F32    ? norm_fwd_f32(a, t, as_stream(stream))
@@ -519,7 +521,7 @@ int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *
         count_launch();
         return check_launch("norm_zero_kernel");
     }
-    const bool in = tb != CSRT_DT_F32 && norm_vector({dv, dh, h, y, gate}), out = norm_vector({dr, dy, dgate});
+    const bool in = tb != CSRT_DT_F32 && norm_vector({dv, dh, h, y, gate}), out = norm_vector({dr, dy, dgate}) && n % 8 == 0;
     const NormTile t = norm_bwd_choice(a, in, tb == CSRT_DT_F32);
     const bool wide = ts == CSRT_DT_F32;
     CSRT_TRY(t == kTileColumns    ? CSRT_NORM_DISPATCH(launch_bwd, tb, ts, a, s)

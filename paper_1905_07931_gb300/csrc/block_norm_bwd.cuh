@@ -64,6 +64,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
     };
     char *sv = take(a.dv, HB::kTotal), *su = take(a.r, HS::kTotal), *sh = take(a.h, HS::kTotal), *sy = take(a.y, HB::kTotal),
          *sg = take(a.g, HB::kTotal);
+    if (!a.y.p) sy = a.dv.p ? sv : su;   // read, and no result depends on it
     float4 *weights = reinterpret_cast<float4 *>(p);   // post weight, post bias, pre weight
     // this warp's: statistics of the tile's tokens (pre mean, negated, and rstd, post likewise), and the stage of results
     float *mine = reinterpret_cast<float *>(weights + kFeatures) + (threadIdx.x >> 5) * 4 * TT;
@@ -90,7 +91,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
     const int tokens = TMA ? a.box * a.boxes * TT : 0;
     auto fetch_all = [&](int64_t t) {
         if (TMA) {
-            if (threadIdx.x != 0) return;
+            if (threadIdx.x != kLoader) return;
             mbar_expect_tx(ex.bar + 2, tokens * ((a.dv.p ? HB::kSize : 0) + (a.h.p ? HS::kSize : 0) + (a.r.p ? HS::kSize : 0) +
                                                  (a.g.p ? HB::kSize : 0)));
         }
@@ -102,7 +103,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
     auto fetch_y = [&](int64_t t) {
         if (!a.y.p) return;
         if (TMA) {
-            if (threadIdx.x != 0) return;
+            if (threadIdx.x != kLoader) return;
             mbar_expect_tx(ex.bar + 3, tokens * HB::kSize);
         }
         fetch(HB(), a.y, 3, sy, t);
@@ -205,14 +206,18 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
         }
         P x[F][T::N], sa[T::N], sb[T::N];
         // dh' and with it dr
-        RS out_dr(a.dr, first, tile * TT, a.n);
+        if (a.r.p) {
 #pragma unroll
-        for (int f = 0; f < F; ++f) {
-            if (a.r.p) HS::read(su, f, off_u, x[f]);
-            else
+            for (int f = 0; f < F; ++f) HS::read(su, f, off_u, x[f]);
+        } else {
+#pragma unroll
+            for (int f = 0; f < F; ++f)
 #pragma unroll
                 for (int k = 0; k < T::N; ++k) x[f][k] = T::all(0.f);
-            if (a.dv.p) {
+        }
+        if (a.dv.p)
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
                 const float w = weights[at.row0 + f * at.kStep].z;
                 P v[T::N], h[T::N];
                 HB::read(sv, f, off_v, v);
@@ -226,12 +231,13 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
                     tw = fma2(v[k], hat, tw);
                     tb = add2(tb, v[k]);
                 }
-                if (sums_pre) {
-                    sums.add(kSumPreW, f, T::sum(tw));
-                    sums.add(kSumPreB, f, T::sum(tb));
-                }
+                sums.add(kSumPreW, f, T::sum(tw));
+                sums.add(kSumPreB, f, T::sum(tb));
             }
-            if (a.dr.p) {
+        if (a.dr.p) {
+            RS out_dr(a.dr, first, tile * TT, a.n);
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
                 P o[T::N];
 #pragma unroll
                 for (int k = 0; k < T::N; ++k) o[k] = mul2(x[f][k], T::all(a.r_scale));
@@ -258,68 +264,44 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
 #pragma unroll
             for (int k = 0; k < T::N; ++k) sa[k] = sb[k] = T::all(0.f);
             RB out_dg(a.dg, first, tile * TT, a.n);
+            const int rows_dg = a.dg.p ? rows : 0;
+            // GATE: CSRT_GATE_*, or -1 for no gate
+            auto pass = [&](auto gate) {
+                constexpr int kGate = decltype(gate)::value;
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                const float4 w = weights[at.row0 + f * at.kStep];
-                P hat[T::N];
-                if (a.y.p) {
+                for (int f = 0; f < F; ++f) {
+                    const float4 w = weights[at.row0 + f * at.kStep];
+                    P hat[T::N];
                     HB::read(sy, f, off_y, hat);
 #pragma unroll
                     for (int k = 0; k < T::N; ++k) hat[k] = mul2(add2(hat[k], m[k]), r[k]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < T::N; ++k) hat[k] = T::all(0.f);
-                }
-                if (a.g.p) {
-                    P g[T::N], value[T::N], slope[T::N];
-                    HB::read(sg, f, off_g, g);
-                    if (a.gate_act == CSRT_GATE_NONE) {
+                    if constexpr (kGate >= 0) {
+                        P g[T::N], o[T::N];
+                        HB::read(sg, f, off_g, g);
 #pragma unroll
                         for (int k = 0; k < T::N; ++k) {
-                            value[k] = g[k];
-                            slope[k] = T::all(1.f);
+                            P value, slope;
+                            gate_of<kGate, kFast>(g[k], T::all(1.f), T::all(-1.f), value, slope);
+                            o[k] = mul2(mul2(x[f][k], fma2(hat[k], T::all(w.x), T::all(w.y))), slope);
+                            x[f][k] = mul2(x[f][k], value);
                         }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < T::N; ++k) {
-                            value[k] = sigmoid2<kFast>(g[k]);
-                            slope[k] = fma2(value[k], T::all(-1.f), T::all(1.f));   // 1 - p
-                        }
-                        if (a.gate_act == CSRT_GATE_SILU) {
-#pragma unroll
-                            for (int k = 0; k < T::N; ++k) {
-                                slope[k] = mul2(value[k], fma2(g[k], slope[k], T::all(1.f)));
-                                value[k] = mul2(value[k], g[k]);
-                            }
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < T::N; ++k) slope[k] = mul2(value[k], slope[k]);
-                        }
+                        out_dg.put(stage, f, at.row0, rows_dg, o);
                     }
-                    if (a.dg.p) {
-                        P o[T::N];
+                    P tw = T::all(0.f), tb = tw;
 #pragma unroll
-                        for (int k = 0; k < T::N; ++k)
-                            o[k] = mul2(mul2(x[f][k], fma2(hat[k], T::all(w.x), T::all(w.y))), slope[k]);
-                        out_dg.put(stage, f, at.row0, rows, o);
+                    for (int k = 0; k < T::N; ++k) {
+                        tw = fma2(x[f][k], hat[k], tw);
+                        tb = add2(tb, x[f][k]);
+                        x[f][k] = mul2(x[f][k], T::all(w.x));
+                        sa[k] = fma2(x[f][k], hat[k], sa[k]);
+                        sb[k] = add2(sb[k], x[f][k]);
                     }
-#pragma unroll
-                    for (int k = 0; k < T::N; ++k) x[f][k] = mul2(x[f][k], value[k]);
-                }
-                P tw = T::all(0.f), tb = tw;
-#pragma unroll
-                for (int k = 0; k < T::N; ++k) {
-                    tw = fma2(x[f][k], hat[k], tw);
-                    tb = add2(tb, x[f][k]);
-                    x[f][k] = mul2(x[f][k], T::all(w.x));
-                    sa[k] = fma2(x[f][k], hat[k], sa[k]);
-                    sb[k] = add2(sb[k], x[f][k]);
-                }
-                if (sums_post) {
                     sums.add(kSumPostW, f, T::sum(tw));
                     sums.add(kSumPostB, f, T::sum(tb));
                 }
-            }
+            };
+            if (a.g.p) with_gate(a.gate_act, pass);
+            else pass(std::integral_constant<int, -1>());
             if (!TMA || !stats) {
                 if (TMA) __syncthreads();   // of all threads
                 next();
@@ -335,22 +317,17 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
                 for (int k = 0; k < T::N; ++k) al[k] = on[k] = T::all(0.f);
             }
             RB out_dy(a.dy, first, tile * TT, a.n);
+            if (stats)
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                P o[T::N];
-                if (a.post.kind > CSRT_NORM_SCALE) {
-                    HB::read(sy, f, off_y, o);
+                for (int f = 0; f < F; ++f) {
+                    P y[T::N];
+                    HB::read(sy, f, off_y, y);
 #pragma unroll
-                    for (int k = 0; k < T::N; ++k) {
-                        const P hat = mul2(add2(o[k], m[k]), r[k]);
-                        o[k] = mul2(fma2(hat, al[k], add2(x[f][k], on[k])), r[k]);
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < T::N; ++k) o[k] = x[f][k];
+                    for (int k = 0; k < T::N; ++k)
+                        x[f][k] = mul2(fma2(mul2(add2(y[k], m[k]), r[k]), al[k], add2(x[f][k], on[k])), r[k]);
                 }
-                out_dy.put(stage, f, at.row0, rows, o);
-            }
+#pragma unroll
+            for (int f = 0; f < F; ++f) out_dy.put(stage, f, at.row0, rows, x[f]);
             if (TMA) __syncthreads();   // all threads have read y
             if (more) fetch_y(tile + a.groups);
         } else {

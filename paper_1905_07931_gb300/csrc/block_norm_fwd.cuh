@@ -65,8 +65,8 @@ __device__ __forceinline__ void tile_stats(Exchange<TT> &ex, const NormSide &s, 
     }
 }
 
-template <typename TB, typename TS, int TT, int V, int F, bool TMA, bool UOUT>
-__global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __grid_constant__ NormArgs a,
+template <typename TB, typename TS, int TT, int V, int F, bool TMA, bool UOUT, int BLOCKS>
+__global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(const __grid_constant__ NormArgs a,
                                                                              const __grid_constant__ NormMaps maps) {
     pdl_enter();
     extern __shared__ __align__(128) char held[];
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
     auto exist = [&](int64_t t) { return (int)imax<int64_t>(0, imin<int64_t>(V, a.n - column(t))); };
     auto fetch = [&](int64_t t) {
         if constexpr (TMA) {
-            if (threadIdx.x != 0) return;
+            if (threadIdx.x != kLoader) return;
             uint64_t *bar = ex.bar + 2;
             const int tokens = a.box * a.boxes * TT;
             mbar_expect_tx(bar, tokens * ((a.y.p ? HB::kSize : 0) + (a.g.p ? HB::kSize : 0) + (a.r.p ? HS::kSize : 0)));
@@ -140,9 +140,6 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
         const int64_t c = column(tile);
         P x[F][T::N], m[T::N], r[T::N];
         RS out_h(a.h, first, tile * TT, a.n);
-        auto put_h = [&](int f) {
-            if (a.h.p) out_h.put(stage, f, at.row0, rows, x[f]);
-        };
         bool ok = true;
         if constexpr (TMA) ok = norm_wait(ex.bar + 2, turn & 1, ex.hdr);
         else cp_async_wait();
@@ -157,43 +154,44 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
                 r[k] = T::all(1.f);
             }
             if (a.post.kind > CSRT_NORM_SCALE) tile_stats<TT, V, F>(ex, a.post, at, rows, tile * TT, a.n, [] {}, x, m, r);
+            // GATE: CSRT_GATE_*, or -1 for no gate. Stores are spread over the features: in a loop of their own they held up
+            // the loads behind them (float32 stream 127 -> 150 us).
+            auto pass = [&](auto gate) {
+                constexpr int kGate = decltype(gate)::value;
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                const float2 w = wpost[at.row0 + f * at.kStep];
+                for (int f = 0; f < F; ++f) {
+                    const float2 w = wpost[at.row0 + f * at.kStep];
 #pragma unroll
-                for (int k = 0; k < T::N; ++k)
-                    x[f][k] = fma2(add2(x[f][k], m[k]), mul2(r[k], T::all(w.x)), T::all(w.y));
-                if (a.g.p) {
-                    P g[T::N], v[T::N];
-                    HB::read(sg, f, off_g, g);
-                    if (a.gate_act != CSRT_GATE_NONE) {
+                    for (int k = 0; k < T::N; ++k)
+                        x[f][k] = fma2(add2(x[f][k], m[k]), mul2(r[k], T::all(w.x)), T::all(w.y));
+                    if constexpr (kGate >= 0) {
+                        P g[T::N];
+                        HB::read(sg, f, off_g, g);
 #pragma unroll
-                        for (int k = 0; k < T::N; ++k) v[k] = sigmoid2<kFast>(g[k]);
-                        if (a.gate_act == CSRT_GATE_SILU)
-#pragma unroll
-                            for (int k = 0; k < T::N; ++k) v[k] = mul2(v[k], g[k]);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < T::N; ++k) v[k] = g[k];
+                        for (int k = 0; k < T::N; ++k) {
+                            P value, slope;
+                            gate_of<kGate, kFast>(g[k], T::all(1.f), T::all(-1.f), value, slope);
+                            x[f][k] = mul2(x[f][k], value);
+                        }
                     }
+                    if (a.r.p) {
+                        P r0[T::N];
+                        HS::read(sr, f, off_r, r0);
 #pragma unroll
-                    for (int k = 0; k < T::N; ++k) x[f][k] = mul2(x[f][k], v[k]);
+                        for (int k = 0; k < T::N; ++k) x[f][k] = fma2(r0[k], T::all(a.r_scale), x[f][k]);
+                    }
+                    if (a.h.p) out_h.put(stage, f, at.row0, rows, x[f]);
                 }
-                if (a.r.p) {
-                    P r0[T::N];
-                    HS::read(sr, f, off_r, r0);
-#pragma unroll
-                    for (int k = 0; k < T::N; ++k) x[f][k] = fma2(r0[k], T::all(a.r_scale), x[f][k]);
-                }
-                put_h(f);
-            }
+            };
+            if (a.g.p) with_gate(a.gate_act, pass);
+            else pass(std::integral_constant<int, -1>());
         } else {
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 HS::read(sr, f, off_r, x[f]);
 #pragma unroll
                 for (int k = 0; k < T::N; ++k) x[f][k] = mul2(x[f][k], T::all(a.r_scale));
-                put_h(f);
+                if (a.h.p) out_h.put(stage, f, at.row0, rows, x[f]);
             }
         }
         auto next = [&] {   // the inputs are in registers
@@ -228,7 +226,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_fwd_tile_kernel(const __
     ex.leave();
 }
 
-template <typename TB, typename TS, int TT, int V, int F, bool TMA, bool UOUT>
+template <typename TB, typename TS, int TT, int V, int F, bool TMA, bool UOUT, int BLOCKS = 2>
 int norm_fwd_tile(NormArgs a, cudaStream_t s) {
     typedef typename InputOf<TMA, TB, TT, V, F>::type HB;
     typedef typename InputOf<TMA, TS, TT, V, F>::type HS;
@@ -244,12 +242,12 @@ int norm_fwd_tile(NormArgs a, cudaStream_t s) {
         return fail(CSRT_ERR_CUDA, "cuTensorMapEncodeTiled refused a matrix");
     const int smem = (a.y.p ? HB::kTotal : 0) + (a.g.p ? HB::kTotal : 0) + (a.r.p ? HS::kTotal : 0) +
                      TileShape<TT, V, F>::kFeatures * 16 + kNormWarps * Result<TS, TT, V, UOUT>::kStageBytes + Exchange<TT>::bytes(size);
-    return launch_clusters<norm_fwd_tile_kernel<TB, TS, TT, V, F, TMA, UOUT>>(a, maps, size, ceil_div<int64_t>(a.n, TT), smem, s);
+    return launch_clusters<norm_fwd_tile_kernel<TB, TS, TT, V, F, TMA, UOUT, BLOCKS>>(a, maps, size, ceil_div<int64_t>(a.n, TT), smem, s);
 }
 
-template <typename TB, typename TS, int TT, int F>
+template <typename TB, typename TS, int TT, int F, int BLOCKS = 2>
 int norm_fwd_aligned(const NormArgs &a, bool out, cudaStream_t s) {
-    return out ? norm_fwd_tile<TB, TS, TT, 8, F, true, false>(a, s) : norm_fwd_tile<TB, TS, TT, 8, F, true, true>(a, s);
+    return out ? norm_fwd_tile<TB, TS, TT, 8, F, true, false, BLOCKS>(a, s) : norm_fwd_tile<TB, TS, TT, 8, F, true, true, BLOCKS>(a, s);
 }
 
 // in, out: all rows of the inputs, or of the results, are 16-byte aligned.
@@ -266,6 +264,7 @@ int norm_fwd_tiles(const NormArgs &a, NormTile t, bool in, bool out, cudaStream_
                 case kTile32x4: return norm_fwd_aligned<TB, TS, 32, 4>(a, out, s);
                 case kTile32x2: return norm_fwd_aligned<TB, TS, 32, 2>(a, out, s);
                 case kTile16x5: return norm_fwd_aligned<TB, TS, 16, 5>(a, out, s);
+                case kTile16x4: return norm_fwd_aligned<TB, TS, 16, 4, 3>(a, out, s);
                 default: break;
             }
     }

@@ -10,7 +10,7 @@
 // their loads for 15% to 35% of the time, as the memory pipe takes only so many.
 // Other rows (U): a thread fetches the aligned words that its eight tokens touch by cp.async, into shared memory that no
 // other thread reads, and shifts them into place by its row's offset, which is the same for all of its features and tiles.
-// Results whose rows are unaligned (UOUT) pass through shared memory of the warp's and leave by single elements, 32 tokens of
+// Results whose rows are unaligned, or end inside a vector (UOUT), pass through shared memory of the warp's and leave by single elements, 32 tokens of
 // a row (or fewer of several) a store.
 #pragma once
 
@@ -26,6 +26,7 @@ namespace csrt {
 constexpr int kNormWarps = 8;
 constexpr int kNormThreads = kNormWarps * 32;
 constexpr int kNormClusterMax = 16;
+constexpr int kLoader = kNormThreads - 32;   // the thread that issues TMA loads
 
 // V tokens as packed pairs (two float32 operations an instruction), or one.
 typedef unsigned long long f32x2;
@@ -256,7 +257,7 @@ struct Result {
         p = m.p + (first + lane / lanes) * row + c * kSize;
         tokens = (int)imax<int64_t>(0, imin<int64_t>(each, n - c));
     }
-    // Feature f of the thread (row0 its first within the block, of `rows`); `stage` is the warp's.
+    // Feature f of the thread (row0 its first within the block, of `rows`; none of 0); `stage` is the warp's.
     __device__ __forceinline__ void put(char *stage, int f, int row0, int rows, const typename Tok<V>::P (&x)[Tok<V>::N]) {
         char *dst = p + f * Place<TT, V>::kStep * row;
         if constexpr (V == 1) {
@@ -299,18 +300,9 @@ struct Result {
                     if (tokens > 0 && own + j * kRowsStore < rows) *reinterpret_cast<T *>(dst) = v;
                 }
                 __syncwarp();
-            } else if (row0 + f * Place<TT, V>::kStep < rows) {
-                if (tokens == 8) {
+            } else if (tokens > 0 && row0 + f * Place<TT, V>::kStep < rows) {   // eight exist, or none
 #pragma unroll
-                    for (int k = 0; k < kSize / 2; ++k) reinterpret_cast<uint4 *>(dst)[k] = w[k];
-                } else {
-                    float v[8];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) unpack2(x[k], v[2 * k], v[2 * k + 1]);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (k < tokens) reinterpret_cast<T *>(dst)[k] = from_f<T>(v[k]);
-                }
+                for (int k = 0; k < kSize / 2; ++k) reinterpret_cast<uint4 *>(dst)[k] = w[k];
             }
         }
     }
@@ -541,6 +533,25 @@ __device__ __forceinline__ f32x2 sigmoid2(f32x2 g) {
 template <bool FAST>
 __device__ __forceinline__ float sigmoid2(float g) {
     return FAST ? rcp_fast(1.f + exp2_fast(g * -1.44269504f)) : sigmoid_of<false>(g);
+}
+
+// a(g) and a'(g) of V tokens. GATE: CSRT_GATE_*, known to the compiler, so that the features of a thread's loop are not
+// separated by branches and their latencies overlap.
+template <int GATE, bool FAST, typename P>
+__device__ __forceinline__ void gate_of(P g, P one, P minus_one, P &value, P &slope) {
+    value = g;
+    slope = one;
+    if (GATE == CSRT_GATE_NONE) return;
+    const P p = sigmoid2<FAST>(g);
+    const P left = fma2(p, minus_one, one);   // 1 - p
+    value = GATE == CSRT_GATE_SILU ? mul2(p, g) : p;
+    slope = GATE == CSRT_GATE_SILU ? mul2(p, fma2(g, left, one)) : mul2(p, left);
+}
+template <typename F>
+__device__ __forceinline__ void with_gate(int act, F body) {
+    if (act == CSRT_GATE_SIGMOID) body(std::integral_constant<int, CSRT_GATE_SIGMOID>());
+    else if (act == CSRT_GATE_SILU) body(std::integral_constant<int, CSRT_GATE_SILU>());
+    else body(std::integral_constant<int, CSRT_GATE_NONE>());
 }
 
 // ---------------------------------------------------------------------------
