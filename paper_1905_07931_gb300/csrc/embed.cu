@@ -17,7 +17,7 @@ struct EmbedArgs {
     int32_t vocab, d, n;
     float scale;
     int32_t accumulate;
-    int32_t in_vec, out_vec;   // rows of the input, the output allow vectors (as each kernel says)
+    int32_t in_vec, out_vec;   // rows of the input, the output allow vectors
     WsHeader *hdr;
     // backward
     int32_t *key[2], *idx[2];  // sorted tokens (vocab: none) and their columns; the second pair is scratch
@@ -31,32 +31,24 @@ struct EmbedArgs {
 };
 
 // ---------------------------------------------------------------------------
-// Lookup: a tile of 64 tokens x 64 features passes through shared memory, read along the table's rows and written along
-// x's. Blocks that follow one another share their tokens, so that a row's pieces are fetched together; the rows of repeated
-// tokens come from L2. in_vec: pairs of features, out_vec: pairs of tokens.
+// Lookup: a tile of 64 tokens x 64 features passes through shared memory. A thread reads one feature of eight tokens along
+// the table's rows and leaves them as one vector in the feature's row; x is written in vectors of eight tokens where its rows
+// allow it (out_vec), else by single elements, 32 tokens a store. Blocks that follow one another share their tokens, so that
+// a row's pieces are fetched together; the rows of repeated tokens come from L2.
 // ---------------------------------------------------------------------------
-template <typename T>
-struct alignas(2 * sizeof(T)) Pair {
-    T a, b;
-};
-template <typename T>
-__device__ __forceinline__ void put_pair(T *p, T a, T b) {
-    if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float2 *>(p) = make_float2(a, b);
-    } else {
-        const Pair<T> w = {a, b};
-        *reinterpret_cast<uint32_t *>(p) = *reinterpret_cast<const uint32_t *>(&w);
-    }
-}
+constexpr int kTile = 64;
+
 template <typename TT, typename TX>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
     pdl_enter();
-    __shared__ float tile[64][65];
-    __shared__ int32_t tok[64];
+    constexpr int kWords = sizeof(TX) / 2;                 // 16-byte words of eight elements
+    constexpr int kPitch = kTile * sizeof(TX) + 16;        // bytes: rows of odd 16-byte words, without bank conflicts
+    __shared__ __align__(16) char tile[kTile * kPitch];
+    __shared__ int32_t tok[kTile];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t across = ceil_div<int64_t>(a.d, 64);
-    const int64_t c0 = blockIdx.x / across * 64, i0 = blockIdx.x % across * 64;
-    if (threadIdx.x < 64) {
+    const int64_t across = ceil_div<int64_t>(a.d, kTile);
+    const int64_t c0 = blockIdx.x / across * kTile, i0 = blockIdx.x % across * kTile;
+    if (threadIdx.x < kTile) {
         const int64_t c = c0 + threadIdx.x;
         int32_t t = c < a.n ? a.tokens[c] : -1;
         if (t >= a.vocab) {
@@ -67,45 +59,44 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
     }
     __syncthreads();
     const TT *table = reinterpret_cast<const TT *>(a.table);
-    Pair<TT> v[8];
+    TT v[2][8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int32_t t = tok[warp + 8 * k];
-        const int64_t i = i0 + 2 * lane;
-        const TT *p = table + (int64_t)t * a.ld + i;
-        v[k].a = v[k].b = from_f<TT>(0.f);
-        if (t >= 0 && i + 1 < a.d && a.in_vec) {
-            if constexpr (sizeof(TT) == 4) {
-                const float2 w = __ldg(reinterpret_cast<const float2 *>(p));
-                v[k] = {w.x, w.y};
-            } else {
-                const uint32_t w = __ldg(reinterpret_cast<const unsigned int *>(p));
-                v[k] = *reinterpret_cast<const Pair<TT> *>(&w);
-            }
-        } else if (t >= 0) {
-            if (i < a.d) v[k].a = p[0];
-            if (i + 1 < a.d) v[k].b = p[1];
+        const int32_t t = tok[warp * 8 + k];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t i = i0 + lane + 32 * u;
+            v[u][k] = t >= 0 && i < a.d ? table[(int64_t)t * a.ld + i] : from_f<TT>(0.f);
         }
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        tile[2 * lane][warp + 8 * k] = a.scale * to_f<TT>(v[k].a);
-        tile[2 * lane + 1][warp + 8 * k] = a.scale * to_f<TT>(v[k].b);
+    for (int u = 0; u < 2; ++u) {
+        alignas(16) TX w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = from_f<TX>(a.scale * to_f<TT>(v[u][k]));
+        uint4 *row = reinterpret_cast<uint4 *>(tile + (lane + 32 * u) * kPitch + warp * 8 * sizeof(TX));
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) row[k] = reinterpret_cast<const uint4 *>(w)[k];
     }
     __syncthreads();
     TX *x = reinterpret_cast<TX *>(a.out);
-    const int64_t c = c0 + 2 * lane;
+    if (a.out_vec && c0 + kTile <= a.n) {
+        constexpr int kLanes = 8 * kWords, kRows = 32 / kLanes;   // lanes along a row of the tile
+#pragma unroll
+        for (int k = 0; k < kTile / 8 / kRows; ++k) {
+            const int r = (k * 8 + warp) * kRows + lane / kLanes, w = lane % kLanes;
+            if (i0 + r < a.d)
+                reinterpret_cast<uint4 *>(x + (i0 + r) * a.ldo + c0)[w] = reinterpret_cast<const uint4 *>(tile + r * kPitch)[w];
+        }
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int64_t i = i0 + warp + 8 * k;
-        if (i >= a.d) break;
-        const Pair<TX> w = {from_f<TX>(tile[warp + 8 * k][2 * lane]), from_f<TX>(tile[warp + 8 * k][2 * lane + 1])};
-        TX *p = x + i * a.ldo + c;
-        if (a.out_vec && c + 1 < a.n) {
-            put_pair(p, w.a, w.b);
-        } else {
-            if (c < a.n) p[0] = w.a;
-            if (c + 1 < a.n) p[1] = w.b;
+        const int r = warp + 8 * k;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t c = c0 + lane + 32 * u;
+            if (i0 + r < a.d && c < a.n) x[(i0 + r) * a.ldo + c] = reinterpret_cast<const TX *>(tile + r * kPitch)[lane + 32 * u];
         }
     }
 }
@@ -248,8 +239,14 @@ __device__ __forceinline__ void embed_turn(const EmbedArgs &a, int64_t unit, TX 
     for (int k = 0; k < kTurnTokens / kSortWarps; ++k) {
         const int t = warp + k * kSortWarps;
         const int64_t c = c0 + t, i = i0 + 2 * lane;
-        if (c < a.n && i < a.pitch)
-            put_pair(out + c * a.pitch + i, tile[2 * lane * kPitch + t], tile[(2 * lane + 1) * kPitch + t]);
+        if (c >= a.n || i >= a.pitch) continue;
+        const TX p = tile[2 * lane * kPitch + t], q = tile[(2 * lane + 1) * kPitch + t];
+        if constexpr (sizeof(TX) == 4) {
+            *reinterpret_cast<float2 *>(out + c * a.pitch + i) = make_float2(p, q);
+        } else {
+            const unsigned lo = *reinterpret_cast<const unsigned short *>(&p), hi = *reinterpret_cast<const unsigned short *>(&q);
+            *reinterpret_cast<uint32_t *>(out + c * a.pitch + i) = lo | hi << 16;
+        }
     }
 }
 
@@ -266,87 +263,113 @@ __global__ void __launch_bounds__(kTurnThreads) embed_turn_kernel(EmbedArgs a) {
 // Second launch: sums over the sorted tokens, kChunk of them by `lanes` threads with eight features each, so that a token
 // that comes often is shared among many. A token's run that lies within a chunk is finished there; the parts of one that does
 // not are kept, and added in order by the third launch. Other blocks write zeros into the rows that no token is.
+// VEC: a thread's features lie side by side and are stored by 16-byte words; else (rows of the table that are not aligned)
+// they lie `lanes` apart, so that the threads' stores do.
 // ---------------------------------------------------------------------------
-constexpr int kChunk = 64, kSumThreads = 128, kZeroRows = 32;
+constexpr int kChunk = 32, kSumThreads = 128, kZeroRows = 32;
 
-template <typename T>
-__device__ __forceinline__ void load8(const char *p, float (&v)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        const float4 x = __ldg(reinterpret_cast<const float4 *>(p)), y = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-        v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-    } else {
-        const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p));
-        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+template <typename T, bool VEC>
+struct Row8 {
+    static constexpr int kWords = VEC ? (int)sizeof(T) * 2 : 8;
+    uint32_t w[kWords];
+    // non-VEC: the first `count` of eight elements that lie `step` apart
+    __device__ __forceinline__ void load(const T *p, int step, int count) {
+        if constexpr (VEC) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const unsigned short lo = (unsigned short)u[k], hi = (unsigned short)(u[k] >> 16);
-            v[2 * k] = to_f<T>(*reinterpret_cast<const T *>(&lo));
-            v[2 * k + 1] = to_f<T>(*reinterpret_cast<const T *>(&hi));
-        }
-    }
-}
-
-// Eight features of a table row from i on: scale * s, or that added to them. out_vec: rows of whole 16-byte words.
-template <typename T>
-__device__ __forceinline__ void put_row(const EmbedArgs &a, int64_t v, int64_t i, const float (&s)[8]) {
-    T *o = reinterpret_cast<T *>(a.out) + v * a.ldo + i;
-    if (a.out_vec && i + 8 <= a.d) {
-        float w[8];
-        if (a.accumulate) {
-            load8<T>(reinterpret_cast<const char *>(o), w);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] += s[k] * a.scale;
+            for (int k = 0; k < kWords / 4; ++k) {
+                const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p) + k);
+                w[4 * k] = x.x;
+                w[4 * k + 1] = x.y;
+                w[4 * k + 2] = x.z;
+                w[4 * k + 3] = x.w;
+            }
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] = s[k] * a.scale;
+            for (int k = 0; k < 8; ++k) w[k] = k < count ? __float_as_uint(to_f<T>(p[k * step])) : 0u;
+        }
+    }
+    __device__ __forceinline__ float get(int k) const {
+        if constexpr (!VEC || sizeof(T) == 4) return __uint_as_float(w[k]);
+        else {
+            const unsigned short h = (unsigned short)(w[k >> 1] >> (16 * (k & 1)));
+            return to_f<T>(*reinterpret_cast<const T *>(&h));
+        }
+    }
+};
+
+// A thread's eight features: i + k * step; the first `count` lie within a row's pitch.
+struct Features {
+    int64_t i;
+    int step, count;
+};
+template <bool VEC>
+__device__ __forceinline__ Features embed_features(const EmbedArgs &a, int64_t group) {
+    const int t = threadIdx.x % a.lanes;
+    if (VEC) return Features{(group * a.lanes + t) * 8, 1, 8};
+    const int64_t i = group * a.lanes * 8 + t;
+    return Features{i, a.lanes, (int)imin<int64_t>(8, (a.pitch - i + a.lanes - 1) / a.lanes)};
+}
+
+// scale * s into a row of the table, or added to it.
+template <typename T, bool VEC>
+__device__ __forceinline__ void put_row(const EmbedArgs &a, int64_t v, Features f, const float (&s)[8]) {
+    T *o = reinterpret_cast<T *>(a.out) + v * a.ldo + f.i;
+    if (VEC && f.i + 8 <= a.d) {
+        float w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = s[k] * a.scale;
+        if (a.accumulate) {
+            Row8<T, true> old;
+            old.load(o, 1, 8);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = fmaf(s[k], a.scale, old.get(k));
         }
         if constexpr (sizeof(T) == 4) {
             reinterpret_cast<float4 *>(o)[0] = make_float4(w[0], w[1], w[2], w[3]);
             reinterpret_cast<float4 *>(o)[1] = make_float4(w[4], w[5], w[6], w[7]);
         } else {
-            uint32_t u[4];
+            alignas(16) T h[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const Pair<T> h = {from_f<T>(w[2 * k]), from_f<T>(w[2 * k + 1])};
-                u[k] = *reinterpret_cast<const uint32_t *>(&h);
-            }
-            *reinterpret_cast<uint4 *>(o) = make_uint4(u[0], u[1], u[2], u[3]);
+            for (int k = 0; k < 8; ++k) h[k] = from_f<T>(w[k]);
+            *reinterpret_cast<uint4 *>(o) = *reinterpret_cast<const uint4 *>(h);
         }
         return;
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        if (i + k < a.d) o[k] = from_f<T>(a.accumulate ? to_f<T>(o[k]) + s[k] * a.scale : s[k] * a.scale);
+        if (f.i + k * f.step < a.d)
+            o[k * f.step] = from_f<T>(a.accumulate ? fmaf(s[k], a.scale, to_f<T>(o[k * f.step])) : s[k] * a.scale);
 }
 
-template <typename TX, typename TT>
-__device__ __forceinline__ void embed_chunk(const EmbedArgs &a, int64_t chunk, int64_t i) {
-    constexpr int kAhead = 4;
+template <typename TX, typename TT, bool VEC>
+__device__ __forceinline__ void embed_chunk(const EmbedArgs &a, int64_t chunk, Features f) {
+    constexpr int kAhead = 8;
     const int32_t *key = a.key[0], *idx = a.idx[0];
+    const TX *rows = reinterpret_cast<const TX *>(a.rows) + f.i;
     const int64_t k0 = chunk * kChunk, k1 = imin<int64_t>(a.n, k0 + kChunk);
     int32_t v = __ldg(key + k0);
     bool head = k0 > 0 && __ldg(key + k0 - 1) == v;   // the run began before this chunk
     const int32_t after = k1 < a.n ? __ldg(key + k1) : -1;
     float s[8] = {0.f};
     auto keep = [&](int slot) {
-        float *o = a.partial + (chunk * 2 + slot) * a.pitch + i;
-        reinterpret_cast<float4 *>(o)[0] = make_float4(s[0], s[1], s[2], s[3]);
-        reinterpret_cast<float4 *>(o)[1] = make_float4(s[4], s[5], s[6], s[7]);
+        float *o = a.partial + (chunk * 2 + slot) * a.pitch + f.i;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < f.count) o[k * f.step] = s[k];
     };
     for (int64_t k = k0; k < k1; k += kAhead) {
         int32_t token[kAhead];
-        float x[kAhead][8];
+        Row8<TX, VEC> x[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             token[u] = k + u < k1 ? __ldg(key + k + u) : a.vocab;
-            if (token[u] < a.vocab) load8<TX>(a.rows + ((int64_t)__ldg(idx + k + u) * a.pitch + i) * sizeof(TX), x[u]);
+            if (token[u] < a.vocab) x[u].load(rows + (int64_t)__ldg(idx + k + u) * a.pitch, f.step, f.count);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (token[u] != v) {   // the run of v is over (none of padding, which sorts last)
                 if (head) keep(0);
-                else if (v < a.vocab) put_row<TT>(a, v, i, s);
+                else if (v < a.vocab) put_row<TT, VEC>(a, v, f, s);
                 head = false;
                 v = token[u];
 #pragma unroll
@@ -354,23 +377,31 @@ __device__ __forceinline__ void embed_chunk(const EmbedArgs &a, int64_t chunk, i
             }
             if (v < a.vocab)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] += x[u][j];
+                for (int j = 0; j < 8; ++j) s[j] += x[u].get(j);
         }
     }
     if (v >= a.vocab) return;
-    if (head) keep(0);   // all of the chunk, or its end as well as its beginning
+    if (head) keep(0);   // all of the chunk
     else if (after == v) keep(1);
-    else put_row<TT>(a, v, i, s);
+    else put_row<TT, VEC>(a, v, f, s);
 }
 
-template <typename TX, typename TT>
+// The group of features and the chunk that a thread of the second and third launch works on.
+template <bool VEC>
+__device__ __forceinline__ bool embed_place(const EmbedArgs &a, Features &f, int64_t &chunk) {
+    const int64_t across = ceil_div<int64_t>(a.pitch, (int64_t)a.lanes * 8);
+    f = embed_features<VEC>(a, (int64_t)blockIdx.x % across);
+    chunk = (int64_t)blockIdx.x / across * (kSumThreads / a.lanes) + threadIdx.x / a.lanes;
+    return f.i < a.pitch && chunk < a.chunks;
+}
+
+template <typename TX, typename TT, bool VEC>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a) {
     pdl_enter();
     if (blockIdx.x < a.sum_blocks) {
-        const int64_t across = ceil_div<int64_t>(a.pitch, (int64_t)a.lanes * 8);
-        const int64_t i = ((int64_t)blockIdx.x % across * a.lanes + threadIdx.x % a.lanes) * 8;
-        const int64_t chunk = (int64_t)blockIdx.x / across * (kSumThreads / a.lanes) + threadIdx.x / a.lanes;
-        if (i < a.pitch && chunk < a.chunks) embed_chunk<TX, TT>(a, chunk, i);
+        Features f;
+        int64_t chunk;
+        if (embed_place<VEC>(a, f, chunk)) embed_chunk<TX, TT, VEC>(a, chunk, f);
         return;
     }
     __shared__ int32_t used[kZeroRows];
@@ -386,33 +417,56 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a) {
         for (int64_t k = from + threadIdx.x; k < to; k += 32) used[__ldg(key + k) - v0] = 1;
     }
     __syncthreads();
-    const float zero[8] = {0.f};
-    for (int r = 0; r < rows; ++r)
-        if (!used[r])
-            for (int64_t i = threadIdx.x * 8; i < a.d; i += kSumThreads * 8) put_row<TT>(a, v0 + r, i, zero);
+    TT *out = reinterpret_cast<TT *>(a.out) + v0 * a.ldo;
+    for (int r = 0; r < rows; ++r, out += a.ldo) {
+        if (used[r]) continue;
+        int64_t i = 0;
+        if (VEC) {
+            constexpr int each = 16 / (int)sizeof(TT);
+            i = a.d / each * each;
+            for (int64_t j = threadIdx.x; j < a.d / each; j += kSumThreads) reinterpret_cast<uint4 *>(out)[j] = make_uint4(0, 0, 0, 0);
+        }
+        for (i += threadIdx.x; i < a.d; i += kSumThreads) out[i] = from_f<TT>(0.f);
+    }
 }
 
 // Third launch: the runs that begin in a chunk and go on after it.
-template <typename TT>
+template <typename TT, bool VEC>
 __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(EmbedArgs a) {
     pdl_enter();
-    const int64_t across = ceil_div<int64_t>(a.pitch, (int64_t)a.lanes * 8);
-    const int64_t i = ((int64_t)blockIdx.x % across * a.lanes + threadIdx.x % a.lanes) * 8;
-    const int64_t chunk = (int64_t)blockIdx.x / across * (kSumThreads / a.lanes) + threadIdx.x / a.lanes;
-    if (i >= a.pitch || chunk + 1 >= a.chunks) return;
+    Features f;
+    int64_t chunk;
+    if (!embed_place<VEC>(a, f, chunk) || chunk + 1 >= a.chunks) return;
     const int32_t *key = a.key[0];
     const int64_t k0 = chunk * kChunk, next = k0 + kChunk;
     const int32_t v = __ldg(key + next - 1);
     if (v >= a.vocab || __ldg(key + next) != v || (__ldg(key + k0) == v && k0 > 0 && __ldg(key + k0 - 1) == v)) return;
-    float s[8], x[8];
-    load8<float>(reinterpret_cast<const char *>(a.partial + (chunk * 2 + 1) * a.pitch + i), s);
-#pragma unroll 4
-    for (int64_t c = chunk + 1; c < a.chunks && __ldg(key + c * kChunk) == v; ++c) {
-        load8<float>(reinterpret_cast<const char *>(a.partial + c * 2 * a.pitch + i), x);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s[k] += x[k];
+    // the chunks that v fills or ends in
+    int64_t end = chunk + 1;
+    for (int64_t step = 1; step > 0;) {   // strides of growing and, once one went too far, halved length
+        if (end - 1 + step < a.chunks && __ldg(key + (end - 1 + step) * kChunk) == v) {
+            end += step;
+            step *= 2;
+        } else {
+            step /= 2;
+        }
     }
-    put_row<TT>(a, v, i, s);
+    float s[8];
+    Row8<float, VEC> x[4];
+    x[0].load(a.partial + (chunk * 2 + 1) * a.pitch + f.i, f.step, f.count);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[k] = x[0].get(k);
+    for (int64_t c = chunk + 1; c < end; c += 4) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (c + u < end) x[u].load(a.partial + (c + u) * 2 * a.pitch + f.i, f.step, f.count);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (c + u < end)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s[k] += x[u].get(k);
+    }
+    put_row<TT, VEC>(a, v, f, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -480,26 +534,31 @@ static int launch_embed_fwd(const EmbedArgs &a, cudaStream_t s) {
     return check_launch("embed_fwd_kernel");
 }
 
-template <typename TX, typename TT>
-static int launch_embed_bwd(EmbedArgs a, cudaStream_t s) {
-    a.tiles = ceil_div<int64_t>(a.n, kTurnTokens) * ceil_div<int64_t>(a.d, kTurnFeatures);
-    for (a.lanes = 1; a.lanes < kSumThreads && a.lanes * 8 < a.pitch;) a.lanes *= 2;
-    const int64_t across = ceil_div<int64_t>(a.pitch, (int64_t)a.lanes * 8);
-    a.sum_blocks = across * ceil_div<int64_t>(a.chunks, kSumThreads / a.lanes);
+template <typename TX, typename TT, bool VEC>
+static int launch_embed_sums(const EmbedArgs &a, cudaStream_t s) {
     const int64_t zero_blocks = a.accumulate ? 0 : ceil_div<int64_t>(a.vocab, kZeroRows);
-    CSRT_ARG(a.tiles < INT32_MAX && a.sum_blocks + zero_blocks < INT32_MAX, "dx is too large");
-    launch_pdl(embed_turn_kernel<TX>, dim3((unsigned)(1 + a.tiles)), dim3(kTurnThreads), 0, s, a);
-    count_launch();
-    CSRT_TRY(check_launch("embed_turn_kernel"));
+    CSRT_ARG(a.sum_blocks + zero_blocks < INT32_MAX, "dx is too large");
     if (a.sum_blocks + zero_blocks > 0) {
-        launch_pdl(embed_sum_kernel<TX, TT>, dim3((unsigned)(a.sum_blocks + zero_blocks)), dim3(kSumThreads), 0, s, a);
+        launch_pdl(embed_sum_kernel<TX, TT, VEC>, dim3((unsigned)(a.sum_blocks + zero_blocks)), dim3(kSumThreads), 0, s, a);
         count_launch();
         CSRT_TRY(check_launch("embed_sum_kernel"));
     }
     if (a.chunks < 2) return CSRT_OK;
-    launch_pdl(embed_join_kernel<TT>, dim3((unsigned)a.sum_blocks), dim3(kSumThreads), 0, s, a);
+    launch_pdl(embed_join_kernel<TT, VEC>, dim3((unsigned)a.sum_blocks), dim3(kSumThreads), 0, s, a);
     count_launch();
     return check_launch("embed_join_kernel");
+}
+
+template <typename TX, typename TT>
+static int launch_embed_bwd(EmbedArgs a, cudaStream_t s) {
+    a.tiles = ceil_div<int64_t>(a.n, kTurnTokens) * ceil_div<int64_t>(a.d, kTurnFeatures);
+    for (a.lanes = 1; a.lanes < kSumThreads && a.lanes * 8 < a.pitch;) a.lanes *= 2;
+    a.sum_blocks = ceil_div<int64_t>(a.pitch, (int64_t)a.lanes * 8) * ceil_div<int64_t>(a.chunks, kSumThreads / a.lanes);
+    CSRT_ARG(a.tiles < INT32_MAX, "dx is too large");
+    launch_pdl(embed_turn_kernel<TX>, dim3((unsigned)(1 + a.tiles)), dim3(kTurnThreads), 0, s, a);
+    count_launch();
+    CSRT_TRY(check_launch("embed_turn_kernel"));
+    return a.out_vec ? launch_embed_sums<TX, TT, true>(a, s) : launch_embed_sums<TX, TT, false>(a, s);
 }
 
 #define CSRT_EMBED_DISPATCH(fn, from, to, ...)                                                                          \
@@ -535,8 +594,7 @@ int csrt_embed_fwd(const csrt_mat *table, const int32_t *tokens, float scale, cs
     CSRT_TRY(check_embed(tokens, scale, vocab, d, n, x, "x", ws, ws_bytes));
     if (d == 0 || n == 0) return CSRT_OK;
     EmbedArgs a = embed_args(table, x, tokens, vocab, d, n, scale, ws);
-    a.in_vec = rows_of(table, 2);
-    a.out_vec = rows_of(x, 2);
+    a.out_vec = tma_rows_ok(x->data, x->ld, dt_size(x->dtype));
     return CSRT_EMBED_DISPATCH(launch_embed_fwd, table->dtype, x->dtype, a, as_stream(stream));
 }
 
