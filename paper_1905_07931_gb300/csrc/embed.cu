@@ -24,7 +24,7 @@ struct EmbedArgs {
     char *rows;                // dx with a token in a row of `pitch` elements
     int64_t pitch;
     float *partial;            // [chunk][2][pitch]: sums of tokens that go on from the chunk before, into the chunk after
-    int32_t chunks;
+    int32_t chunk, chunks;     // tokens of a chunk
     int64_t tiles;             // blocks that transpose
     int32_t lanes;             // threads along a row
     int64_t sum_blocks;
@@ -110,7 +110,9 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
 // thousands of elements a token on.
 // ---------------------------------------------------------------------------
 constexpr int kSortWarps = 16;
+constexpr int kSortPitch = 257;   // of a warp's counts: no bank conflicts when the scan reads across warps
 constexpr int kTurnThreads = kSortWarps * 32;
+static_assert(kTurnThreads == 512, "two threads scan a digit");
 constexpr int kTurnTokens = 128, kTurnFeatures = 64;   // a tile of the others
 
 __device__ __forceinline__ int embed_passes(int32_t vocab) {   // digits of the values 0 .. vocab
@@ -119,8 +121,22 @@ __device__ __forceinline__ int embed_passes(int32_t vocab) {   // digits of the 
     return p;
 }
 
-__device__ void embed_sort(const EmbedArgs &a, int32_t (*count)[kSortWarps]) {
-    constexpr int kAhead = 4;   // rounds whose tokens are fetched together
+// The lanes of this warp with the same digit (eight ballots are far shorter than a match of 32 different values:
+// 17 us a pass over 8192 tokens with it).
+__device__ __forceinline__ unsigned same_digit(int digit, bool in) {
+    unsigned m = __ballot_sync(0xffffffffu, in);
+    if (!in) m = ~m;
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const bool set = (digit >> b) & 1;
+        const unsigned v = __ballot_sync(0xffffffffu, set);
+        m &= set ? v : ~v;
+    }
+    return m;
+}
+
+__device__ void embed_sort(const EmbedArgs &a, int32_t (*count)[kSortPitch]) {
+    constexpr int kAhead = 8;   // rounds whose tokens are fetched together
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const unsigned full = 0xffffffffu;
     const int64_t per = ceil_div<int64_t>(ceil_div<int64_t>(a.n, 32), kSortWarps) * 32;
@@ -132,33 +148,35 @@ __device__ void embed_sort(const EmbedArgs &a, int32_t (*count)[kSortWarps]) {
         const int to = (passes - 1 - p) & 1;
         const int32_t *kin = a.key[to ^ 1], *iin = a.idx[to ^ 1];
         int32_t *kout = a.key[to], *iout = a.idx[to];
-        auto fetch = [&](int64_t k) -> int32_t {
-            if (p > 0) return kin[k];
-            const int32_t t = a.tokens[k];
-            if (t >= a.vocab) dev_flag(a.hdr, CSRT_DEV_INVALID);
-            return t < 0 || t >= a.vocab ? a.vocab : t;
-        };
-        for (int j = lane; j < 256; j += 32) count[j][warp] = 0;
-        __syncwarp();
-        for (int64_t k = k0; k < k1; k += 32 * kAhead) {
-            int32_t key[kAhead];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) key[u] = k + 32 * u + lane < k1 ? fetch(k + 32 * u + lane) : -1;
+        int32_t key[kAhead];
+        auto fetch = [&](int64_t k) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int digit = key[u] >= 0 ? (key[u] >> (8 * p)) & 255 : 256;
-                const unsigned same = __match_any_sync(full, digit);
-                if (digit < 256 && (same & ((1u << lane) - 1)) == 0) count[digit][warp] += __popc(same);
-                __syncwarp();
+                const int64_t at = k + 32 * u + lane;
+                key[u] = at < k1 ? (p > 0 ? kin[at] : a.tokens[at]) : -1;
+                if (p == 0 && at < k1 && (key[u] < 0 || key[u] >= a.vocab)) {
+                    if (key[u] >= 0) dev_flag(a.hdr, CSRT_DEV_INVALID);
+                    key[u] = a.vocab;
+                }
             }
+        };
+        for (int j = lane; j < 256; j += 32) count[warp][j] = 0;
+        __syncwarp();
+        for (int64_t k = k0; k < k1; k += 32 * kAhead) {
+            fetch(k);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (key[u] >= 0) atomicAdd(&count[warp][(key[u] >> (8 * p)) & 255], 1);
         }
         __syncthreads();
-        // exclusive scan of the counts in digit-major order, eight a thread
-        int32_t own[8], sum = 0;
-        int32_t *flat = &count[0][0];
-        for (int j = 0; j < 8; ++j) {
+        // exclusive scan of the counts in digit-major order: half a digit's warps a thread
+        constexpr int kHalf = kSortWarps / 2;
+        const int digit = threadIdx.x >> 1, w0 = (threadIdx.x & 1) * kHalf;
+        int32_t own[kHalf], sum = 0;
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j) {
             own[j] = sum;
-            sum += flat[threadIdx.x * 8 + j];
+            sum += count[w0 + j][digit];
         }
         int32_t incl = sum;
         for (int o = 1; o < 32; o <<= 1) {
@@ -169,27 +187,30 @@ __device__ void embed_sort(const EmbedArgs &a, int32_t (*count)[kSortWarps]) {
         __syncthreads();
         int32_t base = incl - sum;
         for (int w = 0; w < warp; ++w) base += warp_total[w];
-        for (int j = 0; j < 8; ++j) flat[threadIdx.x * 8 + j] = base + own[j];
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j) count[w0 + j][digit] = base + own[j];
         __syncthreads();
         for (int64_t k = k0; k < k1; k += 32 * kAhead) {
-            int32_t key[kAhead], col[kAhead];
+            int32_t col[kAhead];
+            if (k1 - k0 > 32 * kAhead) fetch(k);   // else they are still there
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int64_t at = k + 32 * u + lane;
-                key[u] = at < k1 ? fetch(at) : -1;
                 col[u] = p > 0 && at < k1 ? iin[at] : (int32_t)at;
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int digit = key[u] >= 0 ? (key[u] >> (8 * p)) & 255 : 256;
-                const unsigned same = __match_any_sync(full, digit);
+                if (k + 32 * u >= k1) break;
+                const bool in = key[u] >= 0;
+                const int d = (key[u] >> (8 * p)) & 255;
+                const unsigned same = same_digit(d, in);
                 const int before = __popc(same & ((1u << lane) - 1));
-                const int32_t at = digit < 256 ? count[digit][warp] : 0;
+                const int32_t at = count[warp][d];
                 __syncwarp();
-                if (digit < 256) {
+                if (in) {
                     kout[at + before] = key[u];
                     iout[at + before] = col[u];
-                    if (before == 0) count[digit][warp] = at + __popc(same);
+                    if (before == 0) count[warp][d] = at + __popc(same);
                 }
                 __syncwarp();
             }
@@ -251,11 +272,11 @@ __device__ __forceinline__ void embed_turn(const EmbedArgs &a, int64_t unit, TX 
 }
 
 template <typename TX>
-__global__ void __launch_bounds__(kTurnThreads) embed_turn_kernel(EmbedArgs a) {
+__global__ void __launch_bounds__(kTurnThreads, 4) embed_turn_kernel(EmbedArgs a) {
     pdl_enter();
-    constexpr size_t kTile = kTurnFeatures * (kTurnTokens + 2) * sizeof(TX), kCounts = 256 * kSortWarps * sizeof(int32_t);
+    constexpr size_t kTile = kTurnFeatures * (kTurnTokens + 2) * sizeof(TX), kCounts = kSortPitch * kSortWarps * sizeof(int32_t);
     __shared__ __align__(16) char space[kTile > kCounts ? kTile : kCounts];
-    if (blockIdx.x == 0) embed_sort(a, reinterpret_cast<int32_t(*)[kSortWarps]>(space));
+    if (blockIdx.x == 0) embed_sort(a, reinterpret_cast<int32_t(*)[kSortPitch]>(space));
     else embed_turn<TX>(a, (int64_t)blockIdx.x - 1, reinterpret_cast<TX *>(space));
 }
 
@@ -266,7 +287,9 @@ __global__ void __launch_bounds__(kTurnThreads) embed_turn_kernel(EmbedArgs a) {
 // VEC: a thread's features lie side by side and are stored by 16-byte words; else (rows of the table that are not aligned)
 // they lie `lanes` apart, so that the threads' stores do.
 // ---------------------------------------------------------------------------
-constexpr int kChunk = 32, kSumThreads = 128, kZeroRows = 32;
+constexpr int kSumThreads = 128, kZeroRows = 32;
+constexpr int kFewTokens = 4096;   // up to which chunks are short: few tokens leave threads idle
+constexpr int kShortChunk = 8, kLongChunk = 32;
 
 template <typename T, bool VEC>
 struct Row8 {
@@ -286,6 +309,17 @@ struct Row8 {
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) w[k] = k < count ? __float_as_uint(to_f<T>(p[k * step])) : 0u;
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) {
+            if constexpr (!VEC || sizeof(T) == 4) {
+                w[k] = __float_as_uint(v[k]);
+            } else {
+                const T lo = from_f<T>(v[2 * k]), hi = from_f<T>(v[2 * k + 1]);
+                w[k] = *reinterpret_cast<const unsigned short *>(&lo) | (uint32_t)*reinterpret_cast<const unsigned short *>(&hi) << 16;
+            }
         }
     }
     __device__ __forceinline__ float get(int k) const {
@@ -310,20 +344,14 @@ __device__ __forceinline__ Features embed_features(const EmbedArgs &a, int64_t g
     return Features{i, a.lanes, (int)imin<int64_t>(8, (a.pitch - i + a.lanes - 1) / a.lanes)};
 }
 
-// scale * s into a row of the table, or added to it.
-template <typename T, bool VEC>
-__device__ __forceinline__ void put_row(const EmbedArgs &a, int64_t v, Features f, const float (&s)[8]) {
+// scale * s into a row of the table, or added to `old`, what is there.
+template <typename T, bool VEC, bool ADD>
+__device__ __forceinline__ void put_row(const EmbedArgs &a, int64_t v, Features f, const float (&s)[8], const Row8<T, VEC> &old) {
     T *o = reinterpret_cast<T *>(a.out) + v * a.ldo + f.i;
+    float w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = ADD ? fmaf(s[k], a.scale, old.get(k)) : s[k] * a.scale;
     if (VEC && f.i + 8 <= a.d) {
-        float w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = s[k] * a.scale;
-        if (a.accumulate) {
-            Row8<T, true> old;
-            old.load(o, 1, 8);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] = fmaf(s[k], a.scale, old.get(k));
-        }
         if constexpr (sizeof(T) == 4) {
             reinterpret_cast<float4 *>(o)[0] = make_float4(w[0], w[1], w[2], w[3]);
             reinterpret_cast<float4 *>(o)[1] = make_float4(w[4], w[5], w[6], w[7]);
@@ -337,19 +365,31 @@ __device__ __forceinline__ void put_row(const EmbedArgs &a, int64_t v, Features 
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        if (f.i + k * f.step < a.d)
-            o[k * f.step] = from_f<T>(a.accumulate ? fmaf(s[k], a.scale, to_f<T>(o[k * f.step])) : s[k] * a.scale);
+        if (f.i + k * f.step < a.d) o[k * f.step] = from_f<T>(w[k]);
+}
+// What is there: the elements of row v that lie within the table.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_row(const EmbedArgs &a, int64_t v, Features f, Row8<T, VEC> &old) {
+    const T *o = reinterpret_cast<const T *>(a.out) + v * a.ldo + f.i;
+    if (VEC && f.i + 8 > a.d) {   // the row's end: by elements
+        float w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = f.i + k < a.d ? to_f<T>(o[k]) : 0.f;
+        old.set(w);
+    } else {
+        old.load(o, f.step, VEC ? 8 : (int)imin<int64_t>(f.count, (a.d - f.i + f.step - 1) / f.step));
+    }
 }
 
-template <typename TX, typename TT, bool VEC>
+// ADD: the rows that the sums are added to are fetched with dx's.
+template <typename TX, typename TT, bool VEC, bool ADD>
 __device__ __forceinline__ void embed_chunk(const EmbedArgs &a, int64_t chunk, Features f) {
-    constexpr int kAhead = 8;
+    constexpr int kAhead = ADD || sizeof(TX) == 4 ? 4 : 8;
     const int32_t *key = a.key[0], *idx = a.idx[0];
     const TX *rows = reinterpret_cast<const TX *>(a.rows) + f.i;
-    const int64_t k0 = chunk * kChunk, k1 = imin<int64_t>(a.n, k0 + kChunk);
+    const int64_t k0 = chunk * a.chunk, k1 = imin<int64_t>(a.n, k0 + a.chunk);
     int32_t v = __ldg(key + k0);
     bool head = k0 > 0 && __ldg(key + k0 - 1) == v;   // the run began before this chunk
-    const int32_t after = k1 < a.n ? __ldg(key + k1) : -1;
     float s[8] = {0.f};
     auto keep = [&](int slot) {
         float *o = a.partial + (chunk * 2 + slot) * a.pitch + f.i;
@@ -358,32 +398,33 @@ __device__ __forceinline__ void embed_chunk(const EmbedArgs &a, int64_t chunk, F
             if (k < f.count) o[k * f.step] = s[k];
     };
     for (int64_t k = k0; k < k1; k += kAhead) {
-        int32_t token[kAhead];
+        int32_t token[kAhead + 1];   // and the one behind them
         Row8<TX, VEC> x[kAhead];
+        Row8<TT, VEC> old[ADD ? kAhead : 1];
+#pragma unroll
+        for (int u = 0; u <= kAhead; ++u) token[u] = k + u < a.n ? __ldg(key + k + u) : a.vocab;
+        // without conditions, so that all are on their way together: a row beyond the chunk's end is fetched for nothing
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            token[u] = k + u < k1 ? __ldg(key + k + u) : a.vocab;
-            if (token[u] < a.vocab) x[u].load(rows + (int64_t)__ldg(idx + k + u) * a.pitch, f.step, f.count);
+            x[u].load(rows + (int64_t)__ldg(idx + imin<int64_t>(k + u, k1 - 1)) * a.pitch, f.step, f.count);
+            if (ADD) load_row<TT, VEC>(a, imin(token[u], a.vocab - 1), f, old[ADD ? u : 0]);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (token[u] != v) {   // the run of v is over (none of padding, which sorts last)
+            if (k + u >= k1 || token[u] >= a.vocab) break;   // padding sorts last
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] += x[u].get(j);
+            if (token[u] != token[u + 1]) {   // the run is over
                 if (head) keep(0);
-                else if (v < a.vocab) put_row<TT, VEC>(a, v, f, s);
+                else put_row<TT, VEC, ADD>(a, token[u], f, s, old[ADD ? u : 0]);
                 head = false;
-                v = token[u];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[j] = 0.f;
+            } else if (k + u + 1 == k1) {
+                keep(head ? 0 : 1);
             }
-            if (v < a.vocab)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] += x[u].get(j);
         }
     }
-    if (v >= a.vocab) return;
-    if (head) keep(0);   // all of the chunk
-    else if (after == v) keep(1);
-    else put_row<TT, VEC>(a, v, f, s);
 }
 
 // The group of features and the chunk that a thread of the second and third launch works on.
@@ -395,13 +436,13 @@ __device__ __forceinline__ bool embed_place(const EmbedArgs &a, Features &f, int
     return f.i < a.pitch && chunk < a.chunks;
 }
 
-template <typename TX, typename TT, bool VEC>
+template <typename TX, typename TT, bool VEC, bool ADD>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a) {
     pdl_enter();
     if (blockIdx.x < a.sum_blocks) {
         Features f;
         int64_t chunk;
-        if (embed_place<VEC>(a, f, chunk)) embed_chunk<TX, TT, VEC>(a, chunk, f);
+        if (embed_place<VEC>(a, f, chunk)) embed_chunk<TX, TT, VEC, ADD>(a, chunk, f);
         return;
     }
     __shared__ int32_t used[kZeroRows];
@@ -420,13 +461,13 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a) {
     TT *out = reinterpret_cast<TT *>(a.out) + v0 * a.ldo;
     for (int r = 0; r < rows; ++r, out += a.ldo) {
         if (used[r]) continue;
-        int64_t i = 0;
-        if (VEC) {
-            constexpr int each = 16 / (int)sizeof(TT);
-            i = a.d / each * each;
-            for (int64_t j = threadIdx.x; j < a.d / each; j += kSumThreads) reinterpret_cast<uint4 *>(out)[j] = make_uint4(0, 0, 0, 0);
-        }
-        for (i += threadIdx.x; i < a.d; i += kSumThreads) out[i] = from_f<TT>(0.f);
+        // 16-byte words, and the elements in front of the first and behind the last
+        constexpr int each = 16 / (int)sizeof(TT);
+        const int64_t front = imin<int64_t>(a.d, (int64_t)(-reinterpret_cast<uintptr_t>(out) & 15) / (int64_t)sizeof(TT));
+        const int64_t words = (a.d - front) / each, back = front + words * each;
+        for (int64_t j = threadIdx.x; j < words; j += kSumThreads) reinterpret_cast<uint4 *>(out + front)[j] = make_uint4(0, 0, 0, 0);
+        if (threadIdx.x < front) out[threadIdx.x] = from_f<TT>(0.f);
+        if (threadIdx.x < a.d - back) out[back + threadIdx.x] = from_f<TT>(0.f);
     }
 }
 
@@ -438,35 +479,36 @@ __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(EmbedArgs a) {
     int64_t chunk;
     if (!embed_place<VEC>(a, f, chunk) || chunk + 1 >= a.chunks) return;
     const int32_t *key = a.key[0];
-    const int64_t k0 = chunk * kChunk, next = k0 + kChunk;
+    const int64_t k0 = chunk * a.chunk, next = k0 + a.chunk;
     const int32_t v = __ldg(key + next - 1);
     if (v >= a.vocab || __ldg(key + next) != v || (__ldg(key + k0) == v && k0 > 0 && __ldg(key + k0 - 1) == v)) return;
-    // the chunks that v fills or ends in
-    int64_t end = chunk + 1;
-    for (int64_t step = 1; step > 0;) {   // strides of growing and, once one went too far, halved length
-        if (end - 1 + step < a.chunks && __ldg(key + (end - 1 + step) * kChunk) == v) {
-            end += step;
-            step *= 2;
-        } else {
-            step /= 2;
-        }
-    }
+    constexpr int kAhead = 8;   // chunks whose part is fetched before it is known whether v reaches them
     float s[8];
-    Row8<float, VEC> x[4];
+    Row8<float, VEC> x[kAhead];
+    Row8<TT, VEC> old;
+    if (a.accumulate) load_row<TT, VEC>(a, v, f, old);
     x[0].load(a.partial + (chunk * 2 + 1) * a.pitch + f.i, f.step, f.count);
 #pragma unroll
     for (int k = 0; k < 8; ++k) s[k] = x[0].get(k);
-    for (int64_t c = chunk + 1; c < end; c += 4) {
+    bool more = true;
+    for (int64_t c = chunk + 1; more && c < a.chunks; c += kAhead) {
+        int32_t token[kAhead];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (c + u < end) x[u].load(a.partial + (c + u) * 2 * a.pitch + f.i, f.step, f.count);
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t at = imin<int64_t>(c + u, a.chunks - 1);
+            token[u] = __ldg(key + at * a.chunk);
+            x[u].load(a.partial + at * 2 * a.pitch + f.i, f.step, f.count);
+        }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (c + u < end)
+        for (int u = 0; u < kAhead; ++u) {
+            more = more && c + u < a.chunks && token[u] == v;
+            if (!more) break;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) s[k] += x[u].get(k);
+            for (int k = 0; k < 8; ++k) s[k] += x[u].get(k);
+        }
     }
-    put_row<TT, VEC>(a, v, f, s);
+    if (a.accumulate) put_row<TT, VEC, true>(a, v, f, s, old);
+    else put_row<TT, VEC, false>(a, v, f, s, old);
 }
 
 // ---------------------------------------------------------------------------
@@ -477,7 +519,8 @@ static int64_t embed_pitch(int64_t d) { return ceil_div<int64_t>(d, 8) * 8; }
 // the sorted tokens, dx in rows (float32 at most), the parts of runs
 static size_t embed_bytes(int64_t d, int64_t n) {
     const size_t row = (size_t)embed_pitch(d) * sizeof(float);
-    return kWsReservedBytes + 4 * embed_list_bytes(n) + align_up((size_t)n * row, 256) + align_up(ceil_div<int64_t>(n, kChunk) * 2 * row, 256);
+    const int64_t chunks = imax(ceil_div<int64_t>(imin<int64_t>(n, kFewTokens), kShortChunk), ceil_div<int64_t>(n, kLongChunk));
+    return kWsReservedBytes + 4 * embed_list_bytes(n) + align_up((size_t)n * row, 256) + align_up(chunks * 2 * row, 256);
 }
 
 static int check_embed(const int32_t *tokens, float scale, int32_t vocab, int32_t d, int32_t n, const csrt_mat *out,
@@ -521,7 +564,8 @@ static EmbedArgs embed_args(const csrt_mat *in, const csrt_mat *out, const int32
     a.pitch = embed_pitch(d);
     a.rows = at;
     a.partial = reinterpret_cast<float *>(at + align_up((size_t)n * a.pitch * sizeof(float), 256));
-    a.chunks = (int32_t)ceil_div<int64_t>(n, kChunk);
+    a.chunk = n <= kFewTokens ? kShortChunk : kLongChunk;
+    a.chunks = (int32_t)ceil_div<int64_t>(n, a.chunk);
     return a;
 }
 
@@ -539,7 +583,7 @@ static int launch_embed_sums(const EmbedArgs &a, cudaStream_t s) {
     const int64_t zero_blocks = a.accumulate ? 0 : ceil_div<int64_t>(a.vocab, kZeroRows);
     CSRT_ARG(a.sum_blocks + zero_blocks < INT32_MAX, "dx is too large");
     if (a.sum_blocks + zero_blocks > 0) {
-        launch_pdl(embed_sum_kernel<TX, TT, VEC>, dim3((unsigned)(a.sum_blocks + zero_blocks)), dim3(kSumThreads), 0, s, a);
+        launch_pdl(a.accumulate ? embed_sum_kernel<TX, TT, VEC, true> : embed_sum_kernel<TX, TT, VEC, false>, dim3((unsigned)(a.sum_blocks + zero_blocks)), dim3(kSumThreads), 0, s, a);
         count_launch();
         CSRT_TRY(check_launch("embed_sum_kernel"));
     }

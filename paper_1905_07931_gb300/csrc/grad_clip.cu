@@ -9,9 +9,10 @@
 
 namespace csrt {
 
-constexpr int kGradUnit = 16384;    // elements that a block takes at a time
+constexpr int kGradUnit = 8192;     // elements that a block takes at a time
 constexpr int kGradBlocks = 608;    // four blocks of 256 threads an SM
 constexpr int kGradThreads = 256;
+constexpr int kGradKeep = 2560;     // units of float32: 84 MB
 
 struct GradEntry {
     const char *p;
@@ -29,6 +30,7 @@ struct GradArgs {
     GradEntry e[N];
     int32_t entries;
     int64_t units;
+    int64_t keep;           // the norm's pass leaves the units from this one on in the second-level cache
     int32_t first, last;    // of the launches of one call
     float max_norm;         // 0: only the norm
     float *norm;
@@ -48,31 +50,103 @@ __device__ __forceinline__ const GradEntry &grad_entry(const GradArgs<N> &a, int
     return a.e[lo];
 }
 
+// Element i of a matrix whose rows lie apart. Not inlined: the division takes registers from the loops that never need it.
+__device__ __noinline__ int64_t strided(int64_t i, int32_t cols, int64_t ld) { return i / cols * ld + i % cols; }
 template <typename T>
-__device__ __forceinline__ float grad_at(const char *p, int64_t ld, int32_t cols, bool flat, int64_t i) {
-    const T *q = reinterpret_cast<const T *>(p);
-    return to_f<T>(flat ? q[i] : q[i / cols * ld + i % cols]);
+__device__ __forceinline__ float grad_at(const GradEntry &e, int64_t i) {
+    const T *q = reinterpret_cast<const T *>(e.p);
+    return to_f<T>(e.flat ? q[i] : q[strided(i, e.cols, e.ld)]);
 }
 
-// The squares of a thread's elements of a unit: float32 sums unless they overflow, or underflow without being zero.
+// Vectors of N elements, past the first-level cache. Lines that the second pass will not find any more, and those that it
+// reads or writes for the last time, are the first to leave the second-level cache (`first`).
+__device__ __forceinline__ uint64_t evict_first() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+template <int BYTES>
+__device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[BYTES / 4], bool first, uint64_t policy) {
+    if constexpr (BYTES == 16) {
+        if (first)
+            asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.b32 {%0, %1, %2, %3}, [%4], %5;"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                         : "l"(p), "l"(policy));
+        else
+            asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                         : "l"(p));
+    } else {
+        if (first)
+            asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v2.b32 {%0, %1}, [%2], %3;"
+                         : "=r"(w[0]), "=r"(w[1])
+                         : "l"(p), "l"(policy));
+        else
+            asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    }
+}
+template <int BYTES>
+__device__ __forceinline__ void store_words(void *p, const uint32_t (&w)[BYTES / 4], uint64_t policy) {
+    if constexpr (BYTES == 16)
+        asm volatile("st.global.L2::cache_hint.v4.b32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                     "r"(w[3]), "l"(policy)
+                     : "memory");
+    else
+        asm volatile("st.global.L2::cache_hint.v2.b32 [%0], {%1, %2}, %3;" ::"l"(p), "r"(w[0]), "r"(w[1]), "l"(policy) : "memory");
+}
 template <typename T>
-__device__ __forceinline__ double unit_squares(const GradEntry &e, int64_t base) {
-    const int64_t end = imin<int64_t>(e.count, base + kGradUnit);
-    float s = 0.f;
-    bool some = false;
-    for (int64_t i = base + threadIdx.x; i < end; i += kGradThreads) {
-        const float v = grad_at<T>(e.p, e.ld, e.cols, e.flat != 0, i);
+__device__ __forceinline__ float word_at(const uint32_t *w, int k) {
+    if constexpr (sizeof(T) == 4) {
+        return __uint_as_float(w[k]);
+    } else {
+        const unsigned short h = (unsigned short)(w[k >> 1] >> (16 * (k & 1)));
+        return to_f<T>(*reinterpret_cast<const T *>(&h));
+    }
+}
+
+// The squares of a thread's 32 elements of a unit: float32 sums unless they overflow, or underflow without being zero.
+// By vectors, all fetched together, then what is left of the last one; by elements where vectors are not aligned.
+template <typename T>
+__device__ __forceinline__ double unit_squares(const GradEntry &e, int64_t base, bool first, uint64_t policy) {
+    constexpr int N = 16 / (int)sizeof(T), kEach = kGradUnit / (kGradThreads * N);
+    const int count = (int)imin<int64_t>(e.count - base, kGradUnit);
+    const int vectors = e.flat == 2 ? count / N : 0;
+    float t[4] = {0.f};
+    uint32_t some = 0;
+    uint32_t w[kEach][4];
+    const char *p = e.p + (base + threadIdx.x * N) * (int64_t)sizeof(T);
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        if (u * kGradThreads + (int)threadIdx.x < vectors) load_words<16>(p + u * kGradThreads * 16, w[u], first, policy);
+        else w[u][0] = w[u][1] = w[u][2] = w[u][3] = 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) some |= w[u][k] & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float v = word_at<T>(w[u], k);
+            t[k & 3] = fmaf(v, v, t[k & 3]);
+        }
+    }
+    float s = (t[0] + t[1]) + (t[2] + t[3]);
+    for (int i = vectors * N + threadIdx.x; i < count; i += kGradThreads) {
+        const float v = grad_at<T>(e, base + i);
         s = fmaf(v, v, s);
         some |= v != 0.f;
     }
     // below 2^-80 squares that float32 does not hold (under 2^-126) could matter
-    if ((s >= 8.271806e-25f && s <= 3.4028235e38f) || !some) return s;
-    double t = 0.;
-    for (int64_t i = base + threadIdx.x; i < end; i += kGradThreads) {
-        const double v = grad_at<T>(e.p, e.ld, e.cols, e.flat != 0, i);
-        t += v * v;
-    }
-    return t;
+    if ((s >= 8.271806e-25f && s <= 3.4028235e38f) || some == 0) return s;
+    double d = 0.;
+    auto add = [&](int i) {
+        const double v = grad_at<T>(e, base + i);
+        d += v * v;
+    };
+    for (int u = threadIdx.x; u < vectors; u += kGradThreads)   // the same elements
+        for (int k = 0; k < N; ++k) add(u * N + k);
+    for (int i = vectors * N + threadIdx.x; i < count; i += kGradThreads) add(i);
+    return d;
 }
 
 // Sum over the block in a fixed order; the first thread gets it.
@@ -89,17 +163,19 @@ __device__ __forceinline__ double block_sum(double v, double (&part)[kGradThread
 }
 
 template <int N>
-__global__ void __launch_bounds__(kGradThreads) grad_norm_kernel(const __grid_constant__ GradArgs<N> a) {
+__global__ void __launch_bounds__(kGradThreads, 4) grad_norm_kernel(const __grid_constant__ GradArgs<N> a) {
     pdl_enter();
     __shared__ double part[kGradThreads / 32];
     __shared__ bool last;
     double s = 0.;
+    const uint64_t policy = evict_first();
     for (int64_t u = blockIdx.x; u < a.units; u += gridDim.x) {
         const GradEntry &e = grad_entry(a, u);
         const int64_t base = (u - e.unit0) * kGradUnit;
-        s += e.dt == CSRT_DT_F32    ? unit_squares<float>(e, base)
-             : e.dt == CSRT_DT_BF16 ? unit_squares<__nv_bfloat16>(e, base)
-                                    : unit_squares<__half>(e, base);
+        const bool first = u < a.keep;
+        s += e.dt == CSRT_DT_F32    ? unit_squares<float>(e, base, first, policy)
+             : e.dt == CSRT_DT_BF16 ? unit_squares<__nv_bfloat16>(e, base, first, policy)
+                                    : unit_squares<__half>(e, base, first, policy);
     }
     s = block_sum(s, part);
     if (threadIdx.x == 0) {
@@ -126,32 +202,69 @@ __global__ void __launch_bounds__(kGradThreads) grad_norm_kernel(const __grid_co
     }
 }
 
+template <typename T, typename TO, int N>
+__device__ __forceinline__ void scale_vector(char *o, const uint32_t *w, float factor, uint64_t policy) {
+    uint32_t x[N * sizeof(TO) / 4];
+#pragma unroll
+    for (int k = 0; k < N; k += 4 / (int)sizeof(TO)) {
+        if constexpr (sizeof(TO) == 4) {
+            x[k] = __float_as_uint(word_at<T>(w, k) * factor);
+        } else {
+            const TO lo = from_f<TO>(word_at<T>(w, k) * factor), hi = from_f<TO>(word_at<T>(w, k + 1) * factor);
+            x[k / 2] = *reinterpret_cast<const unsigned short *>(&lo) | (uint32_t)*reinterpret_cast<const unsigned short *>(&hi) << 16;
+        }
+    }
+    store_words<N * sizeof(TO)>(o, x, policy);
+}
 template <typename T, typename TO>
-__device__ __forceinline__ void unit_scale(const GradEntry &e, int64_t base, float factor) {
-    const int64_t end = imin<int64_t>(e.count, base + kGradUnit);
-    TO *o = reinterpret_cast<TO *>(e.o);
-    for (int64_t i = base + threadIdx.x; i < end; i += kGradThreads)
-        o[e.flat_o ? i : i / e.cols * e.ldo + i % e.cols] =
-            from_f<TO>(grad_at<T>(e.p, e.ld, e.cols, e.flat != 0, i) * factor);
+__device__ __forceinline__ void unit_scale(const GradEntry &e, int64_t base, float factor, uint64_t policy) {
+    constexpr int N = sizeof(T) == 2 && sizeof(TO) == 2 ? 8 : 4, kEach = kGradUnit / (kGradThreads * N);
+    constexpr int kIn = N * (int)sizeof(T), kOut = N * (int)sizeof(TO);
+    const int count = (int)imin<int64_t>(e.count - base, kGradUnit);
+    const int vectors = e.flat == 2 && e.flat_o == 2 ? count / N : 0;
+    const char *p = e.p + (base + threadIdx.x * N) * (int64_t)sizeof(T);
+    char *o = e.o + (base + threadIdx.x * N) * (int64_t)sizeof(TO);
+    if (vectors == kGradUnit / N) {
+        uint32_t w[kEach][kIn / 4];
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) load_words<kIn>(p + u * kGradThreads * kIn, w[u], true, policy);
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) scale_vector<T, TO, N>(o + u * kGradThreads * kOut, w[u], factor, policy);
+        return;
+    }
+#pragma unroll 2
+    for (int u = 0; u < kEach; ++u) {
+        if (u * kGradThreads + (int)threadIdx.x >= vectors) break;
+        uint32_t w[kIn / 4];
+        load_words<kIn>(p + u * kGradThreads * kIn, w, true, policy);
+        scale_vector<T, TO, N>(o + u * kGradThreads * kOut, w, factor, policy);
+    }
+    TO *out = reinterpret_cast<TO *>(e.o);
+    for (int i = vectors * N + threadIdx.x; i < count; i += kGradThreads) {
+        const int64_t at = base + i;
+        out[e.flat_o ? at : strided(at, e.cols, e.ldo)] = from_f<TO>(grad_at<T>(e, at) * factor);
+    }
 }
 template <typename T>
-__device__ __forceinline__ void unit_scale_to(const GradEntry &e, int64_t base, float factor) {
-    if (e.dto == CSRT_DT_F32) unit_scale<T, float>(e, base, factor);
-    else if (e.dto == CSRT_DT_BF16) unit_scale<T, __nv_bfloat16>(e, base, factor);
-    else unit_scale<T, __half>(e, base, factor);
+__device__ __forceinline__ void unit_scale_to(const GradEntry &e, int64_t base, float factor, uint64_t policy) {
+    if (e.dto == CSRT_DT_F32) unit_scale<T, float>(e, base, factor, policy);
+    else if (e.dto == CSRT_DT_BF16) unit_scale<T, __nv_bfloat16>(e, base, factor, policy);
+    else unit_scale<T, __half>(e, base, factor, policy);
 }
 
+// From the last unit to the first: the norm's pass has left the last ones in the second-level cache.
 template <int N>
-__global__ void __launch_bounds__(kGradThreads) grad_scale_kernel(const __grid_constant__ GradArgs<N> a) {
+__global__ void __launch_bounds__(kGradThreads, 4) grad_scale_kernel(const __grid_constant__ GradArgs<N> a) {
     pdl_enter();
     const float factor = __ldcg(a.norm + 1);
-    for (int64_t u = blockIdx.x; u < a.units; u += gridDim.x) {
+    const uint64_t policy = evict_first();
+    for (int64_t u = a.units - 1 - blockIdx.x; u >= 0; u -= gridDim.x) {
         const GradEntry &e = grad_entry(a, u);
         if (factor == 1.f && e.o == e.p && e.dt == e.dto) continue;
         const int64_t base = (u - e.unit0) * kGradUnit;
-        if (e.dt == CSRT_DT_F32) unit_scale_to<float>(e, base, factor);
-        else if (e.dt == CSRT_DT_BF16) unit_scale_to<__nv_bfloat16>(e, base, factor);
-        else unit_scale_to<__half>(e, base, factor);
+        if (e.dt == CSRT_DT_F32) unit_scale_to<float>(e, base, factor, policy);
+        else if (e.dt == CSRT_DT_BF16) unit_scale_to<__nv_bfloat16>(e, base, factor, policy);
+        else unit_scale_to<__half>(e, base, factor, policy);
     }
 }
 
@@ -222,6 +335,8 @@ static int grad_launch(const csrt_mat *g, int32_t count, float max_norm, const c
                 a.units += ceil_div<int64_t>(c, kGradUnit);
                 ++done;
             }
+            // a unit is 32 KB in float32: as much as stays beside the results that the second pass writes
+            a.keep = max_norm > 0.f ? a.units - kGradKeep : a.units;
             a.first = done == a.entries;
             a.last = done == full;
             a.max_norm = max_norm;
