@@ -25,7 +25,7 @@ struct EmbedArgs {
     int64_t pitch;
     float *partial;            // [chunk][2][pitch]: sums of tokens that go on from the chunk before, into the chunk after
     int32_t chunk, chunks;     // tokens of a chunk
-    int64_t tiles;             // blocks that transpose
+    int32_t sort_blocks;       // of the first launch, in front of those that turn
     int32_t lanes;             // threads along a row
     int64_t sum_blocks;
 };
@@ -102,13 +102,17 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Gradient, first launch: the first block sorts the tokens, the others turn dx into rows, a token each (read from its columns
-// the gradient would fetch 32 bytes for every two).
+// Gradient, first launch: some blocks sort the tokens, the others turn dx into rows, a token each (read from its columns the
+// gradient would fetch 32 bytes for every two).
 //
-// The sort is a stable radix sort, 8 bits a pass. Each warp owns a contiguous run of tokens; counts are kept per digit and
-// warp, so that a scan of them in that order gives every warp its places. It is done before the others are from some tens of
-// thousands of elements a token on.
+// Up to kRankTokens tokens are sorted by counting: a token's place is the number of tokens that come before it. That is n^2
+// comparisons, 4 us of the GPU's time for 8192 tokens, spread over all of it, while the radix sort below takes 25 us of one
+// block's; from there on the turn of dx hides the radix sort (features by hundreds) or is the smaller part.
+//
+// The radix sort is stable, 8 bits a pass, by one block. Each warp owns a contiguous run of tokens; counts are kept per digit
+// and warp, so that a scan of them in that order gives every warp its places.
 // ---------------------------------------------------------------------------
+constexpr int kRankTokens = 16384;
 constexpr int kSortWarps = 16;
 constexpr int kSortPitch = 257;   // of a warp's counts: no bank conflicts when the scan reads across warps
 constexpr int kTurnThreads = kSortWarps * 32;
@@ -148,17 +152,23 @@ __device__ void embed_sort(const EmbedArgs &a, int32_t (*count)[kSortPitch]) {
         const int to = (passes - 1 - p) & 1;
         const int32_t *kin = a.key[to ^ 1], *iin = a.idx[to ^ 1];
         int32_t *kout = a.key[to], *iout = a.idx[to];
+        const int32_t *source = p > 0 ? kin : a.tokens;
         int32_t key[kAhead];
         auto fetch = [&](int64_t k) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int64_t at = k + 32 * u + lane;
-                key[u] = at < k1 ? (p > 0 ? kin[at] : a.tokens[at]) : -1;
-                if (p == 0 && at < k1 && (key[u] < 0 || key[u] >= a.vocab)) {
-                    if (key[u] >= 0) dev_flag(a.hdr, CSRT_DEV_INVALID);
-                    key[u] = a.vocab;
-                }
+                key[u] = at < k1 ? source[at] : -1;
             }
+            if (p > 0) return;
+            bool beyond = false;   // once for all: a branch at each token would keep them from being fetched together
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                beyond |= key[u] >= a.vocab;
+                const bool pad = key[u] < 0 || key[u] >= a.vocab;
+                key[u] = k + 32 * u + lane >= k1 ? -1 : pad ? a.vocab : key[u];
+            }
+            if (beyond) dev_flag(a.hdr, CSRT_DEV_INVALID);
         };
         for (int j = lane; j < 256; j += 32) count[warp][j] = 0;
         __syncwarp();
@@ -198,19 +208,21 @@ __device__ void embed_sort(const EmbedArgs &a, int32_t (*count)[kSortPitch]) {
                 const int64_t at = k + 32 * u + lane;
                 col[u] = p > 0 && at < k1 ? iin[at] : (int32_t)at;
             }
+            // apart from the places, which depend on the rounds before, so that the ballots of all rounds overlap
+            unsigned same[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) same[u] = same_digit((key[u] >> (8 * p)) & 255, key[u] >= 0);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (k + 32 * u >= k1) break;
-                const bool in = key[u] >= 0;
                 const int d = (key[u] >> (8 * p)) & 255;
-                const unsigned same = same_digit(d, in);
-                const int before = __popc(same & ((1u << lane) - 1));
+                const int before = __popc(same[u] & ((1u << lane) - 1));
                 const int32_t at = count[warp][d];
                 __syncwarp();
-                if (in) {
+                if (key[u] >= 0) {
                     kout[at + before] = key[u];
                     iout[at + before] = col[u];
-                    if (before == 0) count[warp][d] = at + __popc(same);
+                    if (before == 0) count[warp][d] = at + __popc(same[u]);
                 }
                 __syncwarp();
             }
@@ -219,65 +231,142 @@ __device__ void embed_sort(const EmbedArgs &a, int32_t (*count)[kSortPitch]) {
     }
 }
 
-// A tile of dx into rows: in_vec says that four tokens make an aligned vector.
-template <typename TX>
-__device__ __forceinline__ void embed_turn(const EmbedArgs &a, int64_t unit, TX *tile) {
-    constexpr int kPitch = kTurnTokens + (sizeof(TX) == 4 ? 1 : 2);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t along = ceil_div<int64_t>(a.n, kTurnTokens);
-    const int64_t c0 = unit % along * kTurnTokens, i0 = unit / along * kTurnFeatures;
-    const TX *dx = reinterpret_cast<const TX *>(a.table);
-    const bool vec = a.in_vec && c0 + kTurnTokens <= a.n;
-    TX v[kTurnFeatures / kSortWarps][4];
+// The places of 64 tokens: eight slices of the threads compare them with an eighth of all tokens each.
+constexpr int kRankColumns = 64, kRankKeys = 4096;
+
+__device__ __forceinline__ void embed_rank(const EmbedArgs &a, int32_t block, int32_t *keys) {
+    __shared__ int32_t part[kTurnThreads / kRankColumns][kRankColumns];
+    constexpr int kSlice = kRankKeys / (kTurnThreads / kRankColumns);
+    const int slice = threadIdx.x / kRankColumns, column = threadIdx.x % kRankColumns;
+    const int32_t c0 = block * kRankColumns, c = c0 + column;
+    auto token = [&](int32_t k) {
+        const int32_t t = a.tokens[k];
+        return t < 0 || t >= a.vocab ? a.vocab : t;
+    };
+    const int32_t mine = c < a.n ? token(c) : 0;
+    if (slice == 0 && c < a.n && a.tokens[c] >= a.vocab) dev_flag(a.hdr, CSRT_DEV_INVALID);
+    int32_t before = 0;
+    for (int32_t base = 0; base < a.n; base += kRankKeys) {
+        __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kTurnFeatures / kSortWarps; ++k) {
-        const int64_t i = i0 + warp + k * kSortWarps;
-        const TX *p = dx + i * a.ld + c0;
-        if (i < a.d && vec) {
-            if constexpr (sizeof(TX) == 4) {
-                *reinterpret_cast<float4 *>(v[k]) = __ldg(reinterpret_cast<const float4 *>(p) + lane);
-            } else {
-                const uint2 w = __ldg(reinterpret_cast<const uint2 *>(p) + lane);
-                const uint32_t u[2] = {w.x, w.y};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const unsigned short h = (unsigned short)(u[j >> 1] >> (16 * (j & 1)));
-                    v[k][j] = *reinterpret_cast<const TX *>(&h);
-                }
+        for (int k = 0; k < kRankKeys / kTurnThreads; ++k) {
+            const int32_t at = base + k * kTurnThreads + threadIdx.x;
+            keys[k * kTurnThreads + threadIdx.x] = at < a.n ? token(at) : INT32_MAX;
+        }
+        __syncthreads();
+        const int32_t first = base + slice * kSlice;
+        const int4 *p = reinterpret_cast<const int4 *>(keys + slice * kSlice);
+        if (first + kSlice <= c0 || first >= c0 + kRankColumns) {
+            // equal tokens count where they lie in front
+            const int32_t below = first < c0 ? mine + 1 : mine;
+            const int some = imin(kSlice, imax(0, a.n - first));
+#pragma unroll 8
+            for (int k = 0; k < (some + 3) / 4; ++k) {
+                const int4 v = p[k];
+                before += (v.x < below) + (v.y < below) + (v.z < below) + (v.w < below);
             }
         } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[k][j] = i < a.d && c0 + lane + 32 * j < a.n ? p[lane + 32 * j] : from_f<TX>(0.f);
+            for (int k = 0; k < imin(kSlice, a.n - first); ++k) before += keys[slice * kSlice + k] < mine + (first + k < c);
         }
     }
-#pragma unroll
-    for (int k = 0; k < kTurnFeatures / kSortWarps; ++k)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) tile[(warp + k * kSortWarps) * kPitch + (vec ? 4 * lane + j : lane + 32 * j)] = v[k][j];
+    part[slice][column] = before;
     __syncthreads();
-    TX *out = reinterpret_cast<TX *>(a.rows);
+    if (slice != 0 || c >= a.n) return;
+    int32_t place = 0;
 #pragma unroll
-    for (int k = 0; k < kTurnTokens / kSortWarps; ++k) {
-        const int t = warp + k * kSortWarps;
-        const int64_t c = c0 + t, i = i0 + 2 * lane;
-        if (c >= a.n || i >= a.pitch) continue;
-        const TX p = tile[2 * lane * kPitch + t], q = tile[(2 * lane + 1) * kPitch + t];
-        if constexpr (sizeof(TX) == 4) {
-            *reinterpret_cast<float2 *>(out + c * a.pitch + i) = make_float2(p, q);
+    for (int s = 0; s < kTurnThreads / kRankColumns; ++s) place += part[s][column];
+    a.key[0][place] = mine;
+    a.idx[0][place] = c;
+}
+
+// A tile of 64 features x 128 tokens of dx into rows. 16-bit elements: eight tokens of a feature go into shared memory as a
+// word of 16 bytes, words of eight features being permuted so that a warp reads eight features of eight tokens without bank
+// conflicts; a thread takes two tokens of eight features from there and writes 16 bytes of each token's row (the same with
+// 2-byte accesses throughout: 43 us for 4096 x 8192). in_vec: rows of whole 16-byte words; else they are read by elements.
+template <typename TX>
+__device__ __forceinline__ void embed_turn(const EmbedArgs &a, int64_t unit, char *space) {
+    const int64_t along = ceil_div<int64_t>(a.n, kTurnTokens);
+    const int64_t c0 = unit % along * kTurnTokens, i0 = unit / along * kTurnFeatures;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const TX *dx = reinterpret_cast<const TX *>(a.table);
+    TX *out = reinterpret_cast<TX *>(a.rows);
+    if constexpr (sizeof(TX) == 2) {
+        constexpr int kWords = kTurnTokens / 8;   // of a feature
+        uint4 *tile = reinterpret_cast<uint4 *>(space);
+        if (a.in_vec && c0 + kTurnTokens <= a.n) {
+            uint4 v[kTurnFeatures * kWords / kTurnThreads];
+#pragma unroll
+            for (int k = 0; k < kTurnFeatures * kWords / kTurnThreads; ++k) {
+                const int u = k * kTurnThreads + threadIdx.x, f = u / kWords, w = u % kWords;
+                v[k] = make_uint4(0, 0, 0, 0);
+                if (i0 + f < a.d) v[k] = __ldg(reinterpret_cast<const uint4 *>(dx + (i0 + f) * a.ld + c0) + w);
+            }
+#pragma unroll
+            for (int k = 0; k < kTurnFeatures * kWords / kTurnThreads; ++k) {
+                const int u = k * kTurnThreads + threadIdx.x, f = u / kWords, w = u % kWords;
+                tile[f * kWords + (w ^ (f >> 3))] = v[k];
+            }
         } else {
-            const unsigned lo = *reinterpret_cast<const unsigned short *>(&p), hi = *reinterpret_cast<const unsigned short *>(&q);
-            *reinterpret_cast<uint32_t *>(out + c * a.pitch + i) = lo | hi << 16;
+            TX v[kTurnFeatures * kTurnTokens / kTurnThreads];
+#pragma unroll
+            for (int k = 0; k < kTurnFeatures * kTurnTokens / kTurnThreads; ++k) {
+                const int u = k * kTurnThreads + threadIdx.x, f = u / kTurnTokens, t = u % kTurnTokens;
+                v[k] = i0 + f < a.d && c0 + t < a.n ? dx[(i0 + f) * a.ld + c0 + t] : from_f<TX>(0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < kTurnFeatures * kTurnTokens / kTurnThreads; ++k) {
+                const int u = k * kTurnThreads + threadIdx.x, f = u / kTurnTokens, t = u % kTurnTokens;
+                reinterpret_cast<TX *>(space)[f * kTurnTokens + (((t >> 3) ^ (f >> 3)) << 3) + (t & 7)] = v[k];
+            }
+        }
+        __syncthreads();
+        const int g = lane & 7, t = warp * 8 + (lane >> 3) * 2;   // eight features, two tokens
+        const uint32_t *word = reinterpret_cast<const uint32_t *>(space) + g * 8 * (kTurnTokens / 2) + (((t >> 3) ^ g) << 2) + ((t & 7) >> 1);
+        uint32_t x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = word[j * (kTurnTokens / 2)];
+        uint4 lo, hi;
+        lo.x = __byte_perm(x[0], x[1], 0x5410); hi.x = __byte_perm(x[0], x[1], 0x7632);
+        lo.y = __byte_perm(x[2], x[3], 0x5410); hi.y = __byte_perm(x[2], x[3], 0x7632);
+        lo.z = __byte_perm(x[4], x[5], 0x5410); hi.z = __byte_perm(x[4], x[5], 0x7632);
+        lo.w = __byte_perm(x[6], x[7], 0x5410); hi.w = __byte_perm(x[6], x[7], 0x7632);
+        const int64_t c = c0 + t, i = i0 + g * 8;
+        if (i >= a.pitch) return;
+        if (c < a.n) *reinterpret_cast<uint4 *>(out + c * a.pitch + i) = lo;
+        if (c + 1 < a.n) *reinterpret_cast<uint4 *>(out + (c + 1) * a.pitch + i) = hi;
+    } else {
+        constexpr int kPitch = kTurnTokens + 1;
+        TX *tile = reinterpret_cast<TX *>(space);
+#pragma unroll
+        for (int k = 0; k < kTurnFeatures / kSortWarps; ++k) {
+            const int f = warp + k * kSortWarps;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                tile[f * kPitch + lane + 32 * j] =
+                    i0 + f < a.d && c0 + lane + 32 * j < a.n ? dx[(i0 + f) * a.ld + c0 + lane + 32 * j] : 0.f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kTurnTokens / kSortWarps; ++k) {
+            const int t = warp + k * kSortWarps;
+            const int64_t c = c0 + t, i = i0 + 2 * lane;
+            if (c < a.n && i < a.pitch)
+                *reinterpret_cast<float2 *>(out + c * a.pitch + i) =
+                    make_float2(tile[2 * lane * kPitch + t], tile[(2 * lane + 1) * kPitch + t]);
         }
     }
 }
 
-template <typename TX>
-__global__ void __launch_bounds__(kTurnThreads, 4) embed_turn_kernel(EmbedArgs a) {
+template <typename TX, bool RANK>
+__global__ void __launch_bounds__(kTurnThreads, RANK ? 4 : 2) embed_turn_kernel(EmbedArgs a) {
     pdl_enter();
-    constexpr size_t kTile = kTurnFeatures * (kTurnTokens + 2) * sizeof(TX), kCounts = kSortPitch * kSortWarps * sizeof(int32_t);
-    __shared__ __align__(16) char space[kTile > kCounts ? kTile : kCounts];
-    if (blockIdx.x == 0) embed_sort(a, reinterpret_cast<int32_t(*)[kSortPitch]>(space));
-    else embed_turn<TX>(a, (int64_t)blockIdx.x - 1, reinterpret_cast<TX *>(space));
+    constexpr size_t kTile = kTurnFeatures * (kTurnTokens + 2) * sizeof(TX);
+    constexpr size_t kSort = (RANK ? kRankKeys : kSortPitch * kSortWarps) * sizeof(int32_t);
+    __shared__ __align__(16) char space[kTile > kSort ? kTile : kSort];
+    const int64_t unit = (int64_t)blockIdx.x - a.sort_blocks;
+    if (unit >= 0) embed_turn<TX>(a, unit, space);
+    else if (RANK) embed_rank(a, (int32_t)blockIdx.x, reinterpret_cast<int32_t *>(space));
+    else embed_sort(a, reinterpret_cast<int32_t(*)[kSortPitch]>(space));
 }
 
 // ---------------------------------------------------------------------------
@@ -480,9 +569,9 @@ __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(EmbedArgs a) {
     if (!embed_place<VEC>(a, f, chunk) || chunk + 1 >= a.chunks) return;
     const int32_t *key = a.key[0];
     const int64_t k0 = chunk * a.chunk, next = k0 + a.chunk;
-    const int32_t v = __ldg(key + next - 1);
-    if (v >= a.vocab || __ldg(key + next) != v || (__ldg(key + k0) == v && k0 > 0 && __ldg(key + k0 - 1) == v)) return;
-    constexpr int kAhead = 8;   // chunks whose part is fetched before it is known whether v reaches them
+    const int32_t v = __ldg(key + next - 1), after = __ldg(key + next), before = k0 > 0 ? __ldg(key + k0 - 1) : -1;
+    if (v >= a.vocab || after != v || before == v) return;   // sorted: if the token before is v, all of the chunk is
+    constexpr int kAhead = 4;   // chunks whose part is fetched before it is known whether v reaches them
     float s[8];
     Row8<float, VEC> x[kAhead];
     Row8<TT, VEC> old;
@@ -535,11 +624,6 @@ static int check_embed(const int32_t *tokens, float scale, int32_t vocab, int32_
     if (ws_bytes < embed_bytes(d, n))
         return fail(CSRT_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, embed_bytes(d, n));
     return CSRT_OK;
-}
-
-// Rows whose elements 0, k, 2k .. begin on a multiple of k elements.
-static bool rows_of(const csrt_mat *m, int k) {
-    return reinterpret_cast<uintptr_t>(m->data) % (k * dt_size(m->dtype)) == 0 && (m->ld % k == 0 || m->rows <= 1);
 }
 
 static EmbedArgs embed_args(const csrt_mat *in, const csrt_mat *out, const int32_t *tokens, int32_t vocab, int32_t d,
@@ -595,11 +679,14 @@ static int launch_embed_sums(const EmbedArgs &a, cudaStream_t s) {
 
 template <typename TX, typename TT>
 static int launch_embed_bwd(EmbedArgs a, cudaStream_t s) {
-    a.tiles = ceil_div<int64_t>(a.n, kTurnTokens) * ceil_div<int64_t>(a.d, kTurnFeatures);
+    const bool rank = a.n <= kRankTokens;
+    const int64_t tiles = ceil_div<int64_t>(a.n, kTurnTokens) * ceil_div<int64_t>(a.d, kTurnFeatures);
+    a.sort_blocks = rank ? imax(1, ceil_div(a.n, kRankColumns)) : 1;
     for (a.lanes = 1; a.lanes < kSumThreads && a.lanes * 8 < a.pitch;) a.lanes *= 2;
     a.sum_blocks = ceil_div<int64_t>(a.pitch, (int64_t)a.lanes * 8) * ceil_div<int64_t>(a.chunks, kSumThreads / a.lanes);
-    CSRT_ARG(a.tiles < INT32_MAX, "dx is too large");
-    launch_pdl(embed_turn_kernel<TX>, dim3((unsigned)(1 + a.tiles)), dim3(kTurnThreads), 0, s, a);
+    CSRT_ARG(a.sort_blocks + tiles < INT32_MAX, "dx is too large");
+    launch_pdl(rank ? embed_turn_kernel<TX, true> : embed_turn_kernel<TX, false>, dim3((unsigned)(a.sort_blocks + tiles)),
+               dim3(kTurnThreads), 0, s, a);
     count_launch();
     CSRT_TRY(check_launch("embed_turn_kernel"));
     return a.out_vec ? launch_embed_sums<TX, TT, true>(a, s) : launch_embed_sums<TX, TT, false>(a, s);
@@ -653,7 +740,7 @@ int csrt_embed_bwd(const csrt_mat *dx, const int32_t *tokens, float scale, int32
     if (d == 0 || vocab == 0) return CSRT_OK;
     EmbedArgs a = embed_args(dx, dtable, tokens, vocab, d, n, scale, ws);
     a.accumulate = accumulate != 0;
-    a.in_vec = rows_of(dx, 4);
+    a.in_vec = tma_rows_ok(dx->data, dx->ld, dt_size(dx->dtype));
     a.out_vec = tma_rows_ok(dtable->data, dtable->ld, dt_size(dtable->dtype));
     return CSRT_EMBED_DISPATCH(launch_embed_bwd, dx->dtype, dtable->dtype, a, as_stream(stream));
 }
