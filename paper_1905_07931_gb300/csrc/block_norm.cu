@@ -249,17 +249,27 @@ static bool meet(const Operand &a, const Operand &b) {
     return a.v < b.v + b.len && b.v < a.v + a.len;
 }
 
-// Outputs meet nothing, but for one that may be one input itself.
+// Outputs meet nothing, but for one that may be one input itself. Extents are compared first: nearly all pairs end there.
 static int check_apart(const Operand *o, int count, const csrt_mat *alias_out, const csrt_mat *alias_in) {
-    for (int i = 0; i < count; ++i)
+    struct Extent {
+        const char *from, *to;
+    } e[24];
+    for (int i = 0; i < count; ++i) {
+        const csrt_mat *m = o[i].m;
+        e[i].from = m != nullptr ? static_cast<const char *>(m->data) : reinterpret_cast<const char *>(o[i].v);
+        const int64_t bytes = m != nullptr ? ((m->rows - 1) * m->ld + m->cols) * dt_size(m->dtype) : o[i].len * 4;
+        e[i].to = e[i].from != nullptr ? e[i].from + bytes : nullptr;
+    }
+    for (int i = 0; i < count; ++i) {
+        if (!o[i].out) continue;
         for (int j = 0; j < count; ++j) {
-            if (i == j || !o[i].out || (o[j].out && j < i)) continue;
-            if ((o[i].m == nullptr && o[i].v == nullptr) || (o[j].m == nullptr && o[j].v == nullptr)) continue;
+            if (i == j || (o[j].out && j < i) || e[i].from >= e[j].to || e[j].from >= e[i].to) continue;
             if (o[i].m != nullptr && o[i].m == alias_out && o[j].m != nullptr && o[j].m == alias_in &&
                 same_place(alias_out, alias_in))
                 continue;
             CSRT_ARG(!meet(o[i], o[j]), "%s overlaps %s", o[i].name, o[j].name);
         }
+    }
     return CSRT_OK;
 }
 
@@ -301,17 +311,23 @@ static bool norm_vector(std::initializer_list<const csrt_mat *> all) {
     return true;
 }
 
-// wide: the stream is wider than the block's matrices.
-static NormTile norm_fwd_choice(const NormArgs &a, bool in, bool wide) {
+// Tiles by measured times on a GB300 (us, with gate; F x T: features a thread, tokens). Clusters of sixteen blocks leave SMs
+// idle, as a GPC takes only whole ones: 4096 x 8192 takes 101 on 4 x 32 and 68 on 8 x 32. wide: the stream is wider than the
+// block's matrices; in, out: aligned rows.
+static NormTile norm_fwd_choice(const NormArgs &a, bool in, bool out, bool wide) {
     const int64_t d = a.d, tiles = ceil_div<int64_t>(a.n, 32);
+    // one or two tokens: a token a block (one of 4096: 4.5, on 4 x 32 6.6)
     if (a.n <= 2) return d > 65536 ? kTileColumns : d <= 16384 ? kTile1x4 : kTile1x16;
     if (d > 16384) return kTileColumns;
     if (in ? d > 10240 : d > 8192) return kTile8x4;
-    if (in && d > 8192) return kTile16x5;
+    if (in && d > 8192) return kTile16x5;   // 9216 x 2048: 57, on 8 x 16 69
+    // few blocks: small ones (784 x 256: 4.7, on 8 x 32 6.7)
     if (d <= 2048 && tiles * ceil_div<int64_t>(d, 128) <= 2 * num_sms()) return kTile32x2;
-    if (!in) return d <= 4096 ? kTile32x4 : kTile16x4;
-    if (d <= 4096 && tiles * ceil_div<int64_t>(d, 256) <= 2 * num_sms()) return kTile32x4;
-    // 32 tokens of 512 features of a float32 stream leave one block an SM (4096 x 8192: 129 us, half the tile 111)
+    // unaligned inputs take twice the shared memory (4096 x 8191: 152, on 4 x 32 211; 1000 x 7777: 37 and 31)
+    if (!in) return d <= 2048 ? kTile32x4 : kTile16x4;
+    // unaligned results stage through more of it (4096 x 8191: 111, on 8 x 32 142)
+    if (d <= 4096 && (!out || tiles * ceil_div<int64_t>(d, 256) <= 2 * num_sms())) return kTile32x4;
+    // 32 tokens of 512 features of a float32 stream leave one block an SM (4096 x 8192: 129, on 4 x 16 111)
     return wide && d > 2048 ? kTile16x4 : kTile32x8;
 }
 
@@ -337,15 +353,16 @@ static int launch_bwd(NormArgs &a, cudaStream_t s) {
     return check_launch("norm_bwd_columns_kernel");
 }
 
-// wide: the block's matrices are float32 too.
-static NormTile norm_bwd_choice(const NormArgs &a, bool in, bool wide) {
+// As above; wide: the block's matrices are float32 too, f32_stream: the stream is.
+static NormTile norm_bwd_choice(const NormArgs &a, bool in, bool wide, bool f32_stream) {
     const int64_t d = a.d, tiles = ceil_div<int64_t>(a.n, 32);
     // five float32 matrices of 1024 features a block do not fit into shared memory
     if (d > (wide ? 8192 : 16384)) return kTileColumns;
     if (a.n <= 2) return kTile1x4;
     if (d <= 2048 && (!in || tiles * ceil_div<int64_t>(d, 128) <= 2 * num_sms())) return kTile32x2;
     if (!in) return d <= 4096 ? kTile16x2 : d <= 8192 ? kTile8x2 : kTile8x4;
-    return d <= 2048 ? kTile32x4 : d <= 8192 ? kTile16x4 : kTile8x4;
+    // 2048 x 8192: 67 on 4 x 32, 70 on 4 x 16; 4096 x 8192: 148 and 132, with a float32 stream 238 and 253
+    return d <= 2048 || (f32_stream && d <= 4096) ? kTile32x4 : d <= 8192 ? kTile16x4 : kTile8x4;
 }
 
 // dweight and dbias of no tokens: zeros, unless they are added to.
@@ -421,7 +438,7 @@ int csrt_block_norm_fwd(const csrt_mat *y, const csrt_norm *post, const csrt_mat
     a.h = norm_mat(h);
     a.v = norm_mat(v);
     const bool in = tb != CSRT_DT_F32 && norm_vector({y, gate, r}), out = norm_vector({h, v}) && n % 8 == 0;
-    const NormTile t = norm_fwd_choice(a, in, ts != tb);
+    const NormTile t = norm_fwd_choice(a, in, out, ts != tb);
     if (t == kTileColumns) return CSRT_NORM_DISPATCH(launch_fwd, tb, ts, a, as_stream(stream));
     const bool wide = ts == CSRT_DT_F32;
     return tb == CSRT_DT_F32    ? norm_fwd_f32(a, t, as_stream(stream))
@@ -522,7 +539,7 @@ int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *
         return check_launch("norm_zero_kernel");
     }
     const bool in = tb != CSRT_DT_F32 && norm_vector({dv, dh, h, y, gate}), out = norm_vector({dr, dy, dgate}) && n % 8 == 0;
-    const NormTile t = norm_bwd_choice(a, in, tb == CSRT_DT_F32);
+    const NormTile t = norm_bwd_choice(a, in, tb == CSRT_DT_F32, ts == CSRT_DT_F32);
     const bool wide = ts == CSRT_DT_F32;
     CSRT_TRY(t == kTileColumns    ? CSRT_NORM_DISPATCH(launch_bwd, tb, ts, a, s)
              : tb == CSRT_DT_F32  ? norm_bwd_f32(a, t, s)

@@ -563,18 +563,22 @@ class Norm:
         if kind not in _NORMS:
             raise ValueError(f"unknown norm {kind!r}")
         self.kind, self.eps = kind, float(eps)
-        self._features = [(k, _f32(t, k)) for k, t in (("weight", weight), ("bias", bias), ("dweight", dweight),
-                                                       ("dbias", dbias)) if t is not None]
-        self._tokens = [(k, _f32(t, k)) for k, t in (("mean", mean), ("rstd", rstd)) if t is not None]
+        for name, t in (("weight", weight), ("bias", bias), ("mean", mean), ("rstd", rstd), ("dweight", dweight),
+                        ("dbias", dbias)):
+            if t is not None:
+                _f32(t, name)
+        # the fewest elements of what is per feature, and per token
+        self._features = min((t.numel() for t in (weight, bias, dweight, dbias) if t is not None), default=2 ** 31)
+        self._tokens = min((t.numel() for t in (mean, rstd) if t is not None), default=2 ** 31)
         self.weight, self.bias, self.mean, self.rstd, self.dweight, self.dbias = weight, bias, mean, rstd, dweight, dbias
         self._s = csrt_norm(_NORMS[kind], self.eps, _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), _ptr(dweight),
                             _ptr(dbias))
 
     def struct(self, d: int, n: int):
-        for names, need in ((self._features, d), (self._tokens, n)):
-            for name, t in names:
-                if t.numel() < need:
-                    raise ValueError(f"{name} has {t.numel()} elements, needs {need}")
+        if self._features < d:
+            raise ValueError(f"the norm has {self._features} features, needs {d}")
+        if self._tokens < n:
+            raise ValueError(f"the norm has statistics of {self._tokens} tokens, needs {n}")
         return self._s
 
 
