@@ -65,7 +65,7 @@ def build(verbose: bool = False, extra_flags=None) -> str:
             print(r.stdout + r.stderr, file=sys.stderr)
         return obj, True
 
-    with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
+    with ThreadPoolExecutor(max_workers=min(16, os.cpu_count() or 4)) as ex:
         results = list(ex.map(compile_one, srcs))
     objs = [o for o, _ in results]
     rebuilt = any(r for _, r in results)

@@ -379,6 +379,11 @@ __global__ void norm_zero_kernel(NormArgs a) {
          ? (ts == CSRT_DT_F32 ? fn<__nv_bfloat16, float>(__VA_ARGS__) : fn<__nv_bfloat16, __nv_bfloat16>(__VA_ARGS__)) \
          : (ts == CSRT_DT_F32 ? fn<__half, float>(__VA_ARGS__) : fn<__half, __half>(__VA_ARGS__)))
 
+#define CSRT_NORM_TILES(fn, tb, ts)                                          \
+    (tb == CSRT_DT_F32    ? fn##_f32                                         \
+     : tb == CSRT_DT_BF16 ? (ts == CSRT_DT_F32 ? fn##_bf16_f32 : fn##_bf16) \
+                          : (ts == CSRT_DT_F32 ? fn##_f16_f32 : fn##_f16))
+
 }  // namespace csrt
 
 using namespace csrt;
@@ -440,10 +445,7 @@ int csrt_block_norm_fwd(const csrt_mat *y, const csrt_norm *post, const csrt_mat
     const bool in = tb != CSRT_DT_F32 && norm_vector({y, gate, r}), out = norm_vector({h, v}) && n % 8 == 0;
     const NormTile t = norm_fwd_choice(a, in, out, ts != tb);
     if (t == kTileColumns) return CSRT_NORM_DISPATCH(launch_fwd, tb, ts, a, as_stream(stream));
-    const bool wide = ts == CSRT_DT_F32;
-    return tb == CSRT_DT_F32    ? norm_fwd_f32(a, t, as_stream(stream))
-           : tb == CSRT_DT_BF16 ? norm_fwd_bf16(a, wide, t, in, out, as_stream(stream))
-                                : norm_fwd_f16(a, wide, t, in, out, as_stream(stream));
+    return CSRT_NORM_TILES(norm_fwd, tb, ts)(a, t, in, out, as_stream(stream));
 }
 
 int csrt_block_norm_workspace_bytes(int32_t d, int32_t max_n, size_t *bytes) {
@@ -540,11 +542,7 @@ int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *
     }
     const bool in = tb != CSRT_DT_F32 && norm_vector({dv, dh, h, y, gate}), out = norm_vector({dr, dy, dgate}) && n % 8 == 0;
     const NormTile t = norm_bwd_choice(a, in, tb == CSRT_DT_F32, ts == CSRT_DT_F32);
-    const bool wide = ts == CSRT_DT_F32;
-    CSRT_TRY(t == kTileColumns    ? CSRT_NORM_DISPATCH(launch_bwd, tb, ts, a, s)
-             : tb == CSRT_DT_F32  ? norm_bwd_f32(a, t, s)
-             : tb == CSRT_DT_BF16 ? norm_bwd_bf16(a, wide, t, in, out, s)
-                                  : norm_bwd_f16(a, wide, t, in, out, s));
+    CSRT_TRY(t == kTileColumns ? CSRT_NORM_DISPATCH(launch_bwd, tb, ts, a, s) : CSRT_NORM_TILES(norm_bwd, tb, ts)(a, t, in, out, s));
     if (po->dweight == nullptr && po->dbias == nullptr && pr->dweight == nullptr && pr->dbias == nullptr) return CSRT_OK;
     launch_pdl(norm_sums_kernel, dim3((unsigned)ceil_div<int64_t>(d, 32), 4), dim3(256), 0, s, a);
     count_launch();

@@ -78,12 +78,11 @@ __device__ __forceinline__ void gate_both(float g, int act, float &value, float 
 
 // Tiles of the kernels that read every matrix once: tokens wide, features a thread.
 enum NormTile { kTileColumns, kTile1x4, kTile1x16, kTile32x8, kTile32x4, kTile32x2, kTile16x5, kTile16x4, kTile16x2, kTile8x4, kTile8x2 };
-// wide: the residual stream is float32; in, out: the rows of all inputs, or results, are 16-byte aligned
-int norm_fwd_bf16(const NormArgs &a, bool wide, NormTile t, bool in, bool out, cudaStream_t s);
-int norm_fwd_f16(const NormArgs &a, bool wide, NormTile t, bool in, bool out, cudaStream_t s);
-int norm_fwd_f32(const NormArgs &a, NormTile t, cudaStream_t s);
-int norm_bwd_bf16(NormArgs &a, bool wide, NormTile t, bool in, bool out, cudaStream_t s);   // sets a.groups
-int norm_bwd_f16(NormArgs &a, bool wide, NormTile t, bool in, bool out, cudaStream_t s);
-int norm_bwd_f32(NormArgs &a, NormTile t, cudaStream_t s);
+// By the type of the block's matrices and, where it is another, of the stream. in, out: the rows of all inputs, or results,
+// are 16-byte aligned.
+typedef int NormFwd(const NormArgs &a, NormTile t, bool in, bool out, cudaStream_t s);
+typedef int NormBwd(NormArgs &a, NormTile t, bool in, bool out, cudaStream_t s);   // sets a.groups
+NormFwd norm_fwd_bf16, norm_fwd_bf16_f32, norm_fwd_f16, norm_fwd_f16_f32, norm_fwd_f32;
+NormBwd norm_bwd_bf16, norm_bwd_bf16_f32, norm_bwd_f16, norm_bwd_f16_f32, norm_bwd_f32;
 
 }  // namespace csrt

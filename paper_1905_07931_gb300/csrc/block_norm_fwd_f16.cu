@@ -1,10 +1,10 @@
-// Forward norms around a block of float16 matrices.
+// Forward norms around a block of float16 matrices, in a stream of the same.
 #include "block_norm_fwd.cuh"
 
 namespace csrt {
 
-int norm_fwd_f16(const NormArgs &a, bool wide, NormTile t, bool in, bool out, cudaStream_t s) {
-    return wide ? norm_fwd_tiles<__half, float>(a, t, in, out, s) : norm_fwd_tiles<__half, __half>(a, t, in, out, s);
+int norm_fwd_f16(const NormArgs &a, NormTile t, bool in, bool out, cudaStream_t s) {
+    return norm_fwd_tiles<__half, __half>(a, t, in, out, s);
 }
 
 }  // namespace csrt

@@ -3,6 +3,8 @@
 
 namespace csrt {
 
-int norm_fwd_f32(const NormArgs &a, NormTile t, cudaStream_t s) { return norm_fwd_tiles<float, float>(a, t, false, false, s); }
+int norm_fwd_f32(const NormArgs &a, NormTile t, bool in, bool out, cudaStream_t s) {
+    return norm_fwd_tiles<float, float>(a, t, in, out, s);
+}
 
 }  // namespace csrt

@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "block_norm.cuh"
+#include "gemm16_host.cuh"
 #include "mat.cuh"
 
 namespace csrt {
@@ -12,7 +13,6 @@ namespace csrt {
 constexpr int kGradUnit = 8192;     // elements that a block takes at a time
 constexpr int kGradBlocks = 608;    // four blocks of 256 threads an SM
 constexpr int kGradThreads = 256;
-constexpr int kGradKeep = 2560;     // units of float32: 84 MB
 
 struct GradEntry {
     const char *p;
@@ -30,7 +30,6 @@ struct GradArgs {
     GradEntry e[N];
     int32_t entries;
     int64_t units;
-    int64_t keep;           // the norm's pass leaves the units from this one on in the second-level cache
     int32_t first, last;    // of the launches of one call
     float max_norm;         // 0: only the norm
     float *norm;
@@ -58,41 +57,20 @@ __device__ __forceinline__ float grad_at(const GradEntry &e, int64_t i) {
     return to_f<T>(e.flat ? q[i] : q[strided(i, e.cols, e.ld)]);
 }
 
-// Vectors of N elements, past the first-level cache. Lines that the second pass will not find any more, and those that it
-// reads or writes for the last time, are the first to leave the second-level cache (`first`).
-__device__ __forceinline__ uint64_t evict_first() {
-    uint64_t p;
-    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
-    return p;
-}
+// Vectors, past the first-level cache.
 template <int BYTES>
-__device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[BYTES / 4], bool first, uint64_t policy) {
-    if constexpr (BYTES == 16) {
-        if (first)
-            asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.b32 {%0, %1, %2, %3}, [%4], %5;"
-                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                         : "l"(p), "l"(policy));
-        else
-            asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                         : "l"(p));
-    } else {
-        if (first)
-            asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v2.b32 {%0, %1}, [%2], %3;"
-                         : "=r"(w[0]), "=r"(w[1])
-                         : "l"(p), "l"(policy));
-        else
-            asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-    }
-}
-template <int BYTES>
-__device__ __forceinline__ void store_words(void *p, const uint32_t (&w)[BYTES / 4], uint64_t policy) {
+__device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[BYTES / 4]) {
     if constexpr (BYTES == 16)
-        asm volatile("st.global.L2::cache_hint.v4.b32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                     "r"(w[3]), "l"(policy)
-                     : "memory");
+        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                     : "l"(p));
     else
-        asm volatile("st.global.L2::cache_hint.v2.b32 [%0], {%1, %2}, %3;" ::"l"(p), "r"(w[0]), "r"(w[1]), "l"(policy) : "memory");
+        asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+}
+template <int BYTES>
+__device__ __forceinline__ void store_words(void *p, const uint32_t (&w)[BYTES / 4]) {
+    if constexpr (BYTES == 16) *static_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *static_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
 }
 template <typename T>
 __device__ __forceinline__ float word_at(const uint32_t *w, int k) {
@@ -106,8 +84,9 @@ __device__ __forceinline__ float word_at(const uint32_t *w, int k) {
 
 // The squares of a thread's 32 elements of a unit: float32 sums unless they overflow, or underflow without being zero.
 // By vectors, all fetched together, then what is left of the last one; by elements where vectors are not aligned.
+// hold: shared memory that keeps the vectors, or NULL.
 template <typename T>
-__device__ __forceinline__ double unit_squares(const GradEntry &e, int64_t base, bool first, uint64_t policy) {
+__device__ __forceinline__ double unit_squares(const GradEntry &e, int64_t base, uint4 *hold) {
     constexpr int N = 16 / (int)sizeof(T), kEach = kGradUnit / (kGradThreads * N);
     const int count = (int)imin<int64_t>(e.count - base, kGradUnit);
     const int vectors = e.flat == 2 ? count / N : 0;
@@ -117,9 +96,12 @@ __device__ __forceinline__ double unit_squares(const GradEntry &e, int64_t base,
     const char *p = e.p + (base + threadIdx.x * N) * (int64_t)sizeof(T);
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
-        if (u * kGradThreads + (int)threadIdx.x < vectors) load_words<16>(p + u * kGradThreads * 16, w[u], first, policy);
+        if (u * kGradThreads + (int)threadIdx.x < vectors) load_words<16>(p + u * kGradThreads * 16, w[u]);
         else w[u][0] = w[u][1] = w[u][2] = w[u][3] = 0;
     }
+    if (hold != nullptr)
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) hold[u * kGradThreads + threadIdx.x] = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
 #pragma unroll
@@ -149,6 +131,12 @@ __device__ __forceinline__ double unit_squares(const GradEntry &e, int64_t base,
     return d;
 }
 
+__device__ __forceinline__ double squares_of(const GradEntry &e, int64_t base, uint4 *hold) {
+    return e.dt == CSRT_DT_F32    ? unit_squares<float>(e, base, hold)
+           : e.dt == CSRT_DT_BF16 ? unit_squares<__nv_bfloat16>(e, base, hold)
+                                  : unit_squares<__half>(e, base, hold);
+}
+
 // Sum over the block in a fixed order; the first thread gets it.
 __device__ __forceinline__ double block_sum(double v, double (&part)[kGradThreads / 32]) {
 #pragma unroll
@@ -162,20 +150,28 @@ __device__ __forceinline__ double block_sum(double v, double (&part)[kGradThread
     return v;
 }
 
+// The factor for a sum of squares; with `norm` both are written and what is not finite is flagged.
+__device__ __forceinline__ float clip_factor(float max_norm, double squares, float *norm, WsHeader *hdr) {
+    const double root = sqrt(squares);
+    const bool finite = root <= 1.7976931348623157e308;
+    const float factor = max_norm > 0.f && finite && root > max_norm ? (float)(max_norm / root) : 1.f;
+    if (norm != nullptr) {
+        if (!finite) dev_flag(hdr, CSRT_DEV_NONFINITE);
+        norm[0] = (float)root;
+        norm[1] = factor;
+    }
+    return factor;
+}
+
 template <int N>
 __global__ void __launch_bounds__(kGradThreads, 4) grad_norm_kernel(const __grid_constant__ GradArgs<N> a) {
     pdl_enter();
     __shared__ double part[kGradThreads / 32];
     __shared__ bool last;
     double s = 0.;
-    const uint64_t policy = evict_first();
     for (int64_t u = blockIdx.x; u < a.units; u += gridDim.x) {
         const GradEntry &e = grad_entry(a, u);
-        const int64_t base = (u - e.unit0) * kGradUnit;
-        const bool first = u < a.keep;
-        s += e.dt == CSRT_DT_F32    ? unit_squares<float>(e, base, first, policy)
-             : e.dt == CSRT_DT_BF16 ? unit_squares<__nv_bfloat16>(e, base, first, policy)
-                                    : unit_squares<__half>(e, base, first, policy);
+        s += squares_of(e, (u - e.unit0) * kGradUnit, nullptr);
     }
     s = block_sum(s, part);
     if (threadIdx.x == 0) {
@@ -193,17 +189,13 @@ __global__ void __launch_bounds__(kGradThreads, 4) grad_norm_kernel(const __grid
     for (int b = threadIdx.x; b < gridDim.x; b += kGradThreads) s += __ldcg(a.partial + b);
     s = block_sum(s, part);
     if (threadIdx.x == 0) {
-        const double norm = sqrt(s);
-        const bool finite = norm <= 1.7976931348623157e308;
-        if (!finite) dev_flag(a.hdr, CSRT_DEV_NONFINITE);
-        a.norm[0] = (float)norm;
-        a.norm[1] = a.max_norm > 0.f && finite && norm > a.max_norm ? (float)(a.max_norm / norm) : 1.f;
+        clip_factor(a.max_norm, s, a.norm, a.hdr);
         *a.ticket = 0;
     }
 }
 
 template <typename T, typename TO, int N>
-__device__ __forceinline__ void scale_vector(char *o, const uint32_t *w, float factor, uint64_t policy) {
+__device__ __forceinline__ void scale_vector(char *o, const uint32_t *w, float factor) {
     uint32_t x[N * sizeof(TO) / 4];
 #pragma unroll
     for (int k = 0; k < N; k += 4 / (int)sizeof(TO)) {
@@ -214,30 +206,46 @@ __device__ __forceinline__ void scale_vector(char *o, const uint32_t *w, float f
             x[k / 2] = *reinterpret_cast<const unsigned short *>(&lo) | (uint32_t)*reinterpret_cast<const unsigned short *>(&hi) << 16;
         }
     }
-    store_words<N * sizeof(TO)>(o, x, policy);
+    store_words<N * sizeof(TO)>(o, x);
 }
+// hold: the unit's vectors as unit_squares kept them, or NULL.
 template <typename T, typename TO>
-__device__ __forceinline__ void unit_scale(const GradEntry &e, int64_t base, float factor, uint64_t policy) {
+__device__ __forceinline__ void unit_scale(const GradEntry &e, int64_t base, float factor, const char *hold) {
     constexpr int N = sizeof(T) == 2 && sizeof(TO) == 2 ? 8 : 4, kEach = kGradUnit / (kGradThreads * N);
     constexpr int kIn = N * (int)sizeof(T), kOut = N * (int)sizeof(TO);
     const int count = (int)imin<int64_t>(e.count - base, kGradUnit);
     const int vectors = e.flat == 2 && e.flat_o == 2 ? count / N : 0;
     const char *p = e.p + (base + threadIdx.x * N) * (int64_t)sizeof(T);
     char *o = e.o + (base + threadIdx.x * N) * (int64_t)sizeof(TO);
-    if (vectors == kGradUnit / N) {
+    if (hold != nullptr) {
+        const int held = imin(vectors, count / (16 / (int)sizeof(T)) * (16 / (int)sizeof(T)) / N);
+#pragma unroll 4
+        for (int u = threadIdx.x; u < held; u += kGradThreads) {
+            uint32_t w[kIn / 4];
+#pragma unroll
+            for (int k = 0; k < kIn / 4; ++k) w[k] = reinterpret_cast<const uint32_t *>(hold + u * kIn)[k];
+            scale_vector<T, TO, N>(e.o + (base + u * N) * (int64_t)sizeof(TO), w, factor);
+        }
+        for (int u = held + threadIdx.x; u < vectors; u += kGradThreads) {   // beyond the last whole 16 bytes
+            uint32_t w[kIn / 4];
+            load_words<kIn>(e.p + (base + u * N) * (int64_t)sizeof(T), w);
+            scale_vector<T, TO, N>(e.o + (base + u * N) * (int64_t)sizeof(TO), w, factor);
+        }
+    } else if (vectors == kGradUnit / N) {
         uint32_t w[kEach][kIn / 4];
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) load_words<kIn>(p + u * kGradThreads * kIn, w[u], true, policy);
+        for (int u = 0; u < kEach; ++u) load_words<kIn>(p + u * kGradThreads * kIn, w[u]);
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) scale_vector<T, TO, N>(o + u * kGradThreads * kOut, w[u], factor, policy);
+        for (int u = 0; u < kEach; ++u) scale_vector<T, TO, N>(o + u * kGradThreads * kOut, w[u], factor);
         return;
-    }
+    } else {
 #pragma unroll 2
-    for (int u = 0; u < kEach; ++u) {
-        if (u * kGradThreads + (int)threadIdx.x >= vectors) break;
-        uint32_t w[kIn / 4];
-        load_words<kIn>(p + u * kGradThreads * kIn, w, true, policy);
-        scale_vector<T, TO, N>(o + u * kGradThreads * kOut, w, factor, policy);
+        for (int u = 0; u < kEach; ++u) {
+            if (u * kGradThreads + (int)threadIdx.x >= vectors) break;
+            uint32_t w[kIn / 4];
+            load_words<kIn>(p + u * kGradThreads * kIn, w);
+            scale_vector<T, TO, N>(o + u * kGradThreads * kOut, w, factor);
+        }
     }
     TO *out = reinterpret_cast<TO *>(e.o);
     for (int i = vectors * N + threadIdx.x; i < count; i += kGradThreads) {
@@ -246,26 +254,74 @@ __device__ __forceinline__ void unit_scale(const GradEntry &e, int64_t base, flo
     }
 }
 template <typename T>
-__device__ __forceinline__ void unit_scale_to(const GradEntry &e, int64_t base, float factor, uint64_t policy) {
-    if (e.dto == CSRT_DT_F32) unit_scale<T, float>(e, base, factor, policy);
-    else if (e.dto == CSRT_DT_BF16) unit_scale<T, __nv_bfloat16>(e, base, factor, policy);
-    else unit_scale<T, __half>(e, base, factor, policy);
+__device__ __forceinline__ void unit_scale_to(const GradEntry &e, int64_t base, float factor, const char *hold) {
+    if (e.dto == CSRT_DT_F32) unit_scale<T, float>(e, base, factor, hold);
+    else if (e.dto == CSRT_DT_BF16) unit_scale<T, __nv_bfloat16>(e, base, factor, hold);
+    else unit_scale<T, __half>(e, base, factor, hold);
+}
+__device__ __forceinline__ void scale_of(const GradEntry &e, int64_t base, float factor, const char *hold) {
+    if (factor == 1.f && e.o == e.p && e.dt == e.dto) return;
+    if (e.dt == CSRT_DT_F32) unit_scale_to<float>(e, base, factor, hold);
+    else if (e.dt == CSRT_DT_BF16) unit_scale_to<__nv_bfloat16>(e, base, factor, hold);
+    else unit_scale_to<__half>(e, base, factor, hold);
 }
 
-// From the last unit to the first: the norm's pass has left the last ones in the second-level cache.
+// From the last unit to the first: the norm's pass has left some of the last ones in the second-level cache (25 of 235 MB).
+// Loads marked to leave it last brought 4% (58.7M float32 gradients 113 -> 108 us) and would have stayed in other calls' way.
 template <int N>
 __global__ void __launch_bounds__(kGradThreads, 4) grad_scale_kernel(const __grid_constant__ GradArgs<N> a) {
     pdl_enter();
     const float factor = __ldcg(a.norm + 1);
-    const uint64_t policy = evict_first();
     for (int64_t u = a.units - 1 - blockIdx.x; u >= 0; u -= gridDim.x) {
         const GradEntry &e = grad_entry(a, u);
-        if (factor == 1.f && e.o == e.p && e.dt == e.dto) continue;
-        const int64_t base = (u - e.unit0) * kGradUnit;
-        if (e.dt == CSRT_DT_F32) unit_scale_to<float>(e, base, factor, policy);
-        else if (e.dt == CSRT_DT_BF16) unit_scale_to<__nv_bfloat16>(e, base, factor, policy);
-        else unit_scale_to<__half>(e, base, factor, policy);
+        scale_of(e, (u - e.unit0) * kGradUnit, factor, nullptr);
     }
+}
+
+// Norm and scaling in one launch, for no more units than four blocks an SM: each block keeps its unit in shared memory, waits
+// for the others' sums (cooperative launch: all run at the same time), adds them all by itself in one order and scales.
+// 4.8M float32 gradients in 18 tensors: 15.3 us in two launches. With more units a block the second launch's full occupancy
+// reads and writes at the copy rate, and this did not (58.7M: 111 us, two launches 110).
+constexpr int kHoldBytes = kGradUnit * (int)sizeof(float);
+
+template <int N>
+__global__ void __launch_bounds__(kGradThreads, 4) grad_clip_kernel(const __grid_constant__ GradArgs<N> a) {
+    pdl_enter();
+    extern __shared__ __align__(16) char hold[];
+    __shared__ double part[kGradThreads / 32];
+    __shared__ float scale;
+    const GradEntry &e = grad_entry(a, blockIdx.x);
+    const int64_t base = (blockIdx.x - e.unit0) * kGradUnit;
+    double s = squares_of(e, base, reinterpret_cast<uint4 *>(hold));
+    s = block_sum(s, part);
+    if (threadIdx.x == 0) {
+        a.partial[blockIdx.x] = s;
+        __threadfence();
+        atomicAdd(a.ticket, 1);
+        int seen = 0;
+        for (unsigned spin = 0; spin < kSpinLimit; ++spin) {
+            asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(a.ticket) : "memory");
+            if (seen == (int)gridDim.x) break;
+            if (spin > 16) __nanosleep(20);
+        }
+        if (seen != (int)gridDim.x) dev_flag(a.hdr, CSRT_DEV_TIMEOUT);
+        scale = seen == (int)gridDim.x ? 1.f : -1.f;
+    }
+    __syncthreads();
+    if (scale < 0.f) return;   // the others' sums never came: nothing is written
+    s = 0.;
+    for (int b = threadIdx.x; b < gridDim.x; b += kGradThreads) s += __ldcg(a.partial + b);
+    s = block_sum(s, part);
+    if (threadIdx.x == 0) {
+        scale = clip_factor(a.max_norm, s, blockIdx.x == 0 ? a.norm : nullptr, a.hdr);
+        // the last block to have seen all of the sums leaves the counters as they were
+        if (atomicAdd(a.ticket + 1, 1) == (int)gridDim.x - 1) {
+            a.ticket[1] = 0;
+            a.ticket[0] = 0;
+        }
+    }
+    __syncthreads();
+    scale_of(e, base, scale, hold);
 }
 
 // ---------------------------------------------------------------------------
@@ -299,6 +355,24 @@ static uint8_t flatness(const csrt_mat &m) {
 }
 
 template <int N>
+static int grad_once(const GradArgs<N> &a, cudaStream_t s) {
+    CSRT_TRY(allow_smem<grad_clip_kernel<N>>(kHoldBytes));
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.units);
+    cfg.blockDim = dim3(kGradThreads);
+    cfg.dynamicSmemBytes = kHoldBytes;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CSRT_CHECK_CUDA(cudaLaunchKernelEx(&cfg, grad_clip_kernel<N>, a));
+    count_launch();
+    return CSRT_OK;
+}
+
+template <int N>
 static int grad_launch(const csrt_mat *g, int32_t count, float max_norm, const csrt_mat *out, float *norm, void *ws,
                        cudaStream_t s) {
     // matrices that hold something, N a launch; the norm's launches come first
@@ -310,6 +384,7 @@ static int grad_launch(const csrt_mat *g, int32_t count, float max_norm, const c
         all += ceil_div<int64_t>(c, kGradUnit);
     }
     const unsigned blocks = (unsigned)imax<int64_t>(1, imin<int64_t>(all, kGradBlocks));
+    const bool once = max_norm > 0.f && full <= N && full > 0 && all <= imin<int64_t>(4 * num_sms(), kGradBlocks);
     for (int pass = 0; pass < (max_norm > 0.f ? 2 : 1); ++pass) {
         int32_t done = 0, k = 0;
         do {
@@ -335,8 +410,6 @@ static int grad_launch(const csrt_mat *g, int32_t count, float max_norm, const c
                 a.units += ceil_div<int64_t>(c, kGradUnit);
                 ++done;
             }
-            // a unit is 32 KB in float32: as much as stays beside the results that the second pass writes
-            a.keep = max_norm > 0.f ? a.units - kGradKeep : a.units;
             a.first = done == a.entries;
             a.last = done == full;
             a.max_norm = max_norm;
@@ -344,6 +417,7 @@ static int grad_launch(const csrt_mat *g, int32_t count, float max_norm, const c
             a.partial = reinterpret_cast<double *>(ws_scratch(ws));
             a.ticket = ws_counters(ws);
             a.hdr = static_cast<WsHeader *>(ws);
+            if (once) return grad_once(a, s);
             if (pass == 0) {
                 launch_pdl(grad_norm_kernel<N>, dim3(blocks), dim3(kGradThreads), 0, s, a);
                 count_launch();
