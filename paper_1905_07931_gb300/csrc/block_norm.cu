@@ -361,8 +361,10 @@ static NormTile norm_bwd_choice(const NormArgs &a, bool in, bool wide, bool f32_
     if (a.n <= 2) return kTile1x4;
     if (d <= 2048 && (!in || tiles * ceil_div<int64_t>(d, 128) <= 2 * num_sms())) return kTile32x2;
     if (!in) return d <= 4096 ? kTile16x2 : d <= 8192 ? kTile8x2 : kTile8x4;
-    // 2048 x 8192: 67 on 4 x 32, 70 on 4 x 16; 4096 x 8192: 148 and 132, with a float32 stream 238 and 253
-    return d <= 2048 || (f32_stream && d <= 4096) ? kTile32x4 : d <= 8192 ? kTile16x4 : kTile8x4;
+    // 4096 x 8192 with a float32 stream: 224, on 4 x 32, which leaves one block an SM, 238; 2048 x 8192: 96 and 122
+    if (f32_stream && d <= 4096) return kTile16x2;
+    // 2048 x 8192: 67 on 4 x 32, 70 on 4 x 16; 4096 x 8192: 148 and 130
+    return d <= 2048 ? kTile32x4 : d <= 8192 ? kTile16x4 : kTile8x4;
 }
 
 // dweight and dbias of no tokens: zeros, unless they are added to.

@@ -378,6 +378,7 @@ int norm_bwd_tiles(NormArgs &a, NormTile t, bool in, bool out, cudaStream_t s) {
                 case kTile32x2: return norm_bwd_aligned<TB, TS, 32, 2>(a, out, s);
                 case kTile16x4: return norm_bwd_aligned<TB, TS, 16, 4>(a, out, s);
                 case kTile8x4: return norm_bwd_aligned<TB, TS, 8, 4>(a, out, s);
+                case kTile16x2: return norm_bwd_aligned<TB, TS, 16, 2>(a, out, s);
                 default: break;
             }
     }
