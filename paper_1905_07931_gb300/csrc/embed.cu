@@ -2,6 +2,7 @@
 //   x[:, c] = scale table[token c, :],   dtable[v, :] (+)= scale sum_{c: token c = v} dx[:, c]
 // The table holds a token in a row, activations hold it in a column: both directions transpose on the way.
 #include <cmath>
+#include <type_traits>
 
 #include "block_norm.cuh"
 #include "mat.cuh"
@@ -17,6 +18,7 @@ struct EmbedArgs {
     int32_t vocab, d, n;
     float scale;
     int32_t accumulate;
+    int32_t steps;             // lookup: tiles of a block
     int32_t in_vec, out_vec;   // rows of the input, the output allow vectors
     WsHeader *hdr;
     // backward
@@ -36,18 +38,32 @@ struct EmbedArgs {
 // allow it (out_vec), else by single elements, 32 tokens a store. Blocks that follow one another share their tokens, so that
 // a row's pieces are fetched together; the rows of repeated tokens come from L2.
 // ---------------------------------------------------------------------------
-constexpr int kTile = 64;
+constexpr int kTile = 64, kSteps = 4;
 
+// Two 16-bit values in a word.
+template <typename T>
+__device__ __forceinline__ uint32_t two_of(float lo, float hi) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    } else {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+}
+
+// A block takes a.steps tiles of the same tokens: the next one's rows are on their way while one is stored.
 template <typename TT, typename TX>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
     pdl_enter();
     constexpr int kWords = sizeof(TX) / 2;                 // 16-byte words of eight elements
     constexpr int kPitch = kTile * sizeof(TX) + 16;        // bytes: rows of odd 16-byte words, without bank conflicts
-    __shared__ __align__(16) char tile[kTile * kPitch];
+    __shared__ __align__(16) char tiles[2][kTile * kPitch];
     __shared__ int32_t tok[kTile];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t across = ceil_div<int64_t>(a.d, kTile);
-    const int64_t c0 = blockIdx.x / across * kTile, i0 = blockIdx.x % across * kTile;
+    const int64_t across = ceil_div<int64_t>(a.d, kTile * a.steps);
+    const int64_t c0 = blockIdx.x / across * kTile;
+    int64_t i0 = blockIdx.x % across * kTile * a.steps;
     if (threadIdx.x < kTile) {
         const int64_t c = c0 + threadIdx.x;
         int32_t t = c < a.n ? a.tokens[c] : -1;
@@ -58,45 +74,60 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
         tok[threadIdx.x] = t;
     }
     __syncthreads();
-    const TT *table = reinterpret_cast<const TT *>(a.table);
     TT v[2][8];
+    auto fetch = [&](int64_t at) {
+        const TT *table = reinterpret_cast<const TT *>(a.table) + at + lane;
+        const bool in[2] = {at + lane < a.d, at + lane + 32 < a.d};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int32_t t = tok[warp * 8 + k];
+        for (int k = 0; k < 8; ++k) {
+            const int32_t t = tok[warp * 8 + k];
+            const TT *p = table + (int64_t)t * a.ld;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int64_t i = i0 + lane + 32 * u;
-            v[u][k] = t >= 0 && i < a.d ? table[(int64_t)t * a.ld + i] : from_f<TT>(0.f);
+            for (int u = 0; u < 2; ++u) v[u][k] = t >= 0 && in[u] ? __ldg(p + 32 * u) : from_f<TT>(0.f);
         }
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        alignas(16) TX w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = from_f<TX>(a.scale * to_f<TT>(v[u][k]));
-        uint4 *row = reinterpret_cast<uint4 *>(tile + (lane + 32 * u) * kPitch + warp * 8 * sizeof(TX));
-#pragma unroll
-        for (int k = 0; k < kWords; ++k) row[k] = reinterpret_cast<const uint4 *>(w)[k];
-    }
-    __syncthreads();
+    };
+    fetch(i0);
     TX *x = reinterpret_cast<TX *>(a.out);
-    if (a.out_vec && c0 + kTile <= a.n) {
-        constexpr int kLanes = 8 * kWords, kRows = 32 / kLanes;   // lanes along a row of the tile
-#pragma unroll
-        for (int k = 0; k < kTile / 8 / kRows; ++k) {
-            const int r = (k * 8 + warp) * kRows + lane / kLanes, w = lane % kLanes;
-            if (i0 + r < a.d)
-                reinterpret_cast<uint4 *>(x + (i0 + r) * a.ldo + c0)[w] = reinterpret_cast<const uint4 *>(tile + r * kPitch)[w];
-        }
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int r = warp + 8 * k;
+    const bool whole = a.out_vec && c0 + kTile <= a.n;
+    for (int s = 0; s < a.steps && i0 < a.d; ++s, i0 += kTile) {
+        char *tile = tiles[s & 1];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int64_t c = c0 + lane + 32 * u;
-            if (i0 + r < a.d && c < a.n) x[(i0 + r) * a.ldo + c] = reinterpret_cast<const TX *>(tile + r * kPitch)[lane + 32 * u];
+            uint32_t w[4 * kWords];
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const float lo = a.scale * to_f<TT>(v[u][k]), hi = a.scale * to_f<TT>(v[u][k + 1]);
+                if constexpr (sizeof(TX) == 4) {
+                    w[k] = __float_as_uint(lo);
+                    w[k + 1] = __float_as_uint(hi);
+                } else {
+                    w[k / 2] = two_of<TX>(lo, hi);
+                }
+            }
+            uint4 *row = reinterpret_cast<uint4 *>(tile + (lane + 32 * u) * kPitch + warp * 8 * sizeof(TX));
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) row[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        }
+        __syncthreads();   // the other tile has been read before the last one of these
+        if (s + 1 < a.steps && i0 + kTile < a.d) fetch(i0 + kTile);
+        if (whole) {
+            constexpr int kLanes = 8 * kWords, kRows = 32 / kLanes;   // lanes along a row of the tile
+#pragma unroll
+            for (int k = 0; k < kTile / 8 / kRows; ++k) {
+                const int r = (k * 8 + warp) * kRows + lane / kLanes, w = lane % kLanes;
+                if (i0 + r < a.d)
+                    reinterpret_cast<uint4 *>(x + (i0 + r) * a.ldo + c0)[w] = reinterpret_cast<const uint4 *>(tile + r * kPitch)[w];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int r = warp + 8 * k;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int64_t c = c0 + lane + 32 * u;
+                    if (i0 + r < a.d && c < a.n) x[(i0 + r) * a.ldo + c] = reinterpret_cast<const TX *>(tile + r * kPitch)[lane + 32 * u];
+                }
+            }
         }
     }
 }
@@ -654,8 +685,10 @@ static EmbedArgs embed_args(const csrt_mat *in, const csrt_mat *out, const int32
 }
 
 template <typename TT, typename TX>
-static int launch_embed_fwd(const EmbedArgs &a, cudaStream_t s) {
-    const int64_t blocks = ceil_div<int64_t>(a.n, 64) * ceil_div<int64_t>(a.d, 64);
+static int launch_embed_fwd(EmbedArgs a, cudaStream_t s) {
+    const int64_t tiles = ceil_div<int64_t>(a.n, kTile) * ceil_div<int64_t>(a.d, kTile);
+    a.steps = (int32_t)imin<int64_t>(kSteps, imax<int64_t>(1, tiles / (num_sms() * 6)));
+    const int64_t blocks = ceil_div<int64_t>(a.n, kTile) * ceil_div<int64_t>(a.d, kTile * a.steps);
     CSRT_ARG(blocks <= INT32_MAX, "x is too large");
     launch_pdl(embed_fwd_kernel<TT, TX>, dim3((unsigned)blocks), dim3(256), 0, s, a);
     count_launch();

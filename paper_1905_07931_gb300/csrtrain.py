@@ -11,6 +11,8 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
+import threading
 from ctypes import POINTER, c_float, c_int8, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
@@ -588,8 +590,36 @@ def _gate(act):
     return _GATES[act]
 
 
-def _opt(t, name):
-    return None if t is None else _mat(t, name)
+class _Slots(threading.local):
+    """A thread's csrt_mat structures for one call: filled by packing, a third of the time of making new ones (a call of
+    eight matrices is bound by the host up to 15 us)."""
+
+    def __init__(self):
+        self.buf = bytearray(12 * ctypes.sizeof(csrt_mat))
+        self.mats = [csrt_mat.from_buffer(self.buf, k * ctypes.sizeof(csrt_mat)) for k in range(12)]
+
+
+_slots = _Slots()
+_pack_mat = struct.Struct("=Qiiqi4x").pack_into
+assert ctypes.sizeof(csrt_mat) == 32
+
+
+def _put(k, t, name):
+    """_mat in slot k of this thread; None stays None."""
+    if t is None:
+        return None
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-D CUDA tensor")
+    rows, cols = shape
+    ld, inner = t.stride()
+    dtype = _DTYPES.get(t.dtype)
+    slots = _slots
+    if inner != 1 or ld < cols or dtype is None:   # what is left of the checks, and single rows and columns
+        m = _mat(t, name)
+        ld, dtype = m.ld, m.dtype
+    _pack_mat(slots.buf, 32 * k, t.data_ptr(), rows, cols, ld, dtype)
+    return slots.mats[k]
 
 
 def _int32(t, name):
@@ -603,30 +633,31 @@ def block_norm_fwd(y, r, h, v, post: Norm | None = None, pre: Norm | None = None
     """t = post(y), h = r_scale r + a(gate) t, v = pre(h): what lies between two
     blocks of a residual network. None leaves out any of y, r, h, post, gate,
     and pre with v."""
-    shape = next((t.shape for t in (y, r) if t is not None), (0, 0))
-    _check(lib().csrt_block_norm_fwd(_opt(y, "y"), None if post is None else post.struct(*shape), _opt(gate, "gate"),
-                                     _gate(gate_act), _opt(r, "r"), float(r_scale),
-                                     None if pre is None else pre.struct(*shape), _opt(h, "h"), _opt(v, "v"),
-                                     _stream(stream)), "csrt_block_norm_fwd")
+    first = y if y is not None else r
+    d, n = first.shape if first is not None else (0, 0)
+    _check(lib().csrt_block_norm_fwd(_put(0, y, "y"), None if post is None else post.struct(d, n), _put(1, gate, "gate"),
+                                     _gate(gate_act), _put(2, r, "r"), float(r_scale), None if pre is None else pre.struct(d, n),
+                                     _put(3, h, "h"), _put(4, v, "v"), _stream(stream)), "csrt_block_norm_fwd")
 
 
 def block_norm_bwd(dv, dh, h, y, dr, dy, ws: Workspace, post: Norm | None = None, pre: Norm | None = None, gate=None,
                    gate_act: str = "none", dgate=None, r_scale: float = 1.0, accumulate: bool = False, stream=None):
     """The gradients dr, dy and dgate (None: not wanted) from dv and dh (either
     may be None), and the norms' dweight and dbias (added to with accumulate)."""
-    shape = next((t.shape for t in (dv, dh) if t is not None), (0, 0))
-    _check(lib().csrt_block_norm_bwd(_opt(dv, "dv"), _opt(dh, "dh"), _opt(h, "h"),
-                                     None if pre is None else pre.struct(*shape), _opt(y, "y"),
-                                     None if post is None else post.struct(*shape), _opt(gate, "gate"), _gate(gate_act),
-                                     float(r_scale), 1 if accumulate else 0, _opt(dr, "dr"), _opt(dy, "dy"),
-                                     _opt(dgate, "dgate"), ws.ptr, ws.nbytes, _stream(stream)), "csrt_block_norm_bwd")
+    first = dv if dv is not None else dh
+    d, n = first.shape if first is not None else (0, 0)
+    _check(lib().csrt_block_norm_bwd(_put(0, dv, "dv"), _put(1, dh, "dh"), _put(2, h, "h"),
+                                     None if pre is None else pre.struct(d, n), _put(3, y, "y"),
+                                     None if post is None else post.struct(d, n), _put(4, gate, "gate"), _gate(gate_act),
+                                     float(r_scale), 1 if accumulate else 0, _put(5, dr, "dr"), _put(6, dy, "dy"),
+                                     _put(7, dgate, "dgate"), ws.ptr, ws.nbytes, _stream(stream)), "csrt_block_norm_bwd")
 
 
 def embed_fwd(table, tokens, x, ws: Workspace, scale: float = 1.0, stream=None):
     """x[:, c] = scale * table[tokens[c]]; a negative token gives a column of zeros."""
     if _int32(tokens, "tokens").numel() < x.shape[-1]:
         raise ValueError(f"tokens has {tokens.numel()} elements, needs {x.shape[-1]}")
-    _check(lib().csrt_embed_fwd(_mat(table, "table"), _ptr(tokens), float(scale), _mat(x, "x"), ws.ptr, ws.nbytes,
+    _check(lib().csrt_embed_fwd(_put(0, table, "table"), tokens.data_ptr(), float(scale), _put(1, x, "x"), ws.ptr, ws.nbytes,
                                 _stream(stream)), "csrt_embed_fwd")
 
 
@@ -635,8 +666,8 @@ def embed_bwd(dx, tokens, dtable, ws: Workspace, scale: float = 1.0, accumulate:
     accumulate: added to it, rows without tokens left as they are)."""
     if _int32(tokens, "tokens").numel() < dx.shape[-1]:
         raise ValueError(f"tokens has {tokens.numel()} elements, needs {dx.shape[-1]}")
-    _check(lib().csrt_embed_bwd(_mat(dx, "dx"), _ptr(tokens), float(scale), 1 if accumulate else 0,
-                                _mat(dtable, "dtable"), ws.ptr, ws.nbytes, _stream(stream)), "csrt_embed_bwd")
+    _check(lib().csrt_embed_bwd(_put(0, dx, "dx"), tokens.data_ptr(), float(scale), 1 if accumulate else 0,
+                                _put(1, dtable, "dtable"), ws.ptr, ws.nbytes, _stream(stream)), "csrt_embed_bwd")
 
 
 class TensorList:
@@ -682,7 +713,7 @@ def grad_clip(grads, max_norm: float, norm, ws: Workspace, out=None, stream=None
     if out is not None and len(out) != len(grads):
         raise ValueError("out must have one tensor for each of grads")
     _f32(norm, "norm", 2)
-    _check(lib().csrt_grad_clip(grads._s, len(grads), float(max_norm), None if out is None else out._s, _ptr(norm),
+    _check(lib().csrt_grad_clip(grads._s, len(grads), float(max_norm), None if out is None else out._s, norm.data_ptr(),
                                 ws.ptr, ws.nbytes, _stream(stream)), "csrt_grad_clip")
 
 
