@@ -456,7 +456,12 @@ typedef struct csrt_norm {
  * that is not yet rounded. Squares are summed in float32, so entries beyond
  * 1e18 of a normed matrix overflow its statistics. A token that holds an
  * infinity or a NaN does not reach the others. h may be r itself; apart from
- * that no output overlaps anything else. Any d and n, 0 and 1 among them. */
+ * that no output overlaps anything else. Any d and n, 0 and 1 among them; rows
+ * that are 16-byte aligned (data and ld) are fetched by TMA and are faster. Of
+ * other rows, what shares an aligned 16-byte word with an element in front of
+ * it is read too. Up to 16384 features the blocks of a cluster wait for one
+ * another (bounded; there is no workspace to flag one that ran out in: its
+ * results are NaN). */
 int csrt_block_norm_fwd(const csrt_mat *y, const csrt_norm *post, const csrt_mat *gate, int32_t gate_act,
                         const csrt_mat *r, float r_scale, const csrt_norm *pre, csrt_mat *h, csrt_mat *v, void *stream);
 
@@ -472,13 +477,15 @@ int csrt_block_norm_workspace_bytes(int32_t d, int32_t max_n, size_t *bytes);
  * statistics. h may be NULL without pre, y with a post of NULL and no dgate.
  * dr, dy and dgate may be NULL; dy's presence says whether there is a y. dr may
  * be dh itself; apart from that no output overlaps anything else. dv, gate, y,
- * dy and dgate have one type; dh, h and dr that type or float32. */
+ * dy and dgate have one type; dh, h and dr that type or float32. A wait that
+ * ran out sets CSRT_DEV_TIMEOUT. */
 int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *h, const csrt_norm *pre,
                         const csrt_mat *y, const csrt_norm *post, const csrt_mat *gate, int32_t gate_act, float r_scale,
                         int32_t accumulate, csrt_mat *dr, csrt_mat *dy, csrt_mat *dgate, void *ws, size_t ws_bytes,
                         void *stream);
 
-/* Workspace of the embedding calls. */
+/* Workspace of the embedding calls (the gradient keeps dx in rows there, and
+ * the sorted tokens). */
 int csrt_embed_workspace_bytes(int32_t vocab, int32_t d, int32_t max_n, size_t *bytes);
 
 /* csrt_embed_fwd -- x[:, c] = scale * table[tokens[c], :]. table is vocab x d
@@ -513,7 +520,9 @@ int csrt_grad_norm(const csrt_mat *g, int32_t count, float *norm, void *ws, size
  * but, where it is g[i] itself, g[i]; NULL: g itself. Where the factor is 1
  * matrices in place are left as they are. A norm that is infinite or NaN
  * leaves the factor at 1. max_norm > 0 and finite. No matrix of out may
- * overlap another. */
+ * overlap another, or a g of another index (not checked). The blocks of small
+ * calls wait for one another (cooperative launch, bounded): a wait that ran
+ * out sets CSRT_DEV_TIMEOUT and leaves out as it was. */
 int csrt_grad_clip(const csrt_mat *g, int32_t count, float max_norm, const csrt_mat *out, float *norm, void *ws,
                    size_t ws_bytes, void *stream);
 

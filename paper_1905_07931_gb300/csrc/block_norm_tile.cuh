@@ -331,20 +331,20 @@ __device__ __forceinline__ void merge(float &a, float &b, float na, float a2, fl
     b = b + b2 + delta * delta * (na * share);
 }
 
-// Bounded wait for a phase of an mbarrier (try_wait suspends the thread for a while at a time). It never runs out while the
-// cluster lives: results of a wait that did are NaN.
+// Bounded wait for a phase of an mbarrier: about a second, as try_wait suspends the thread for a microsecond at most. It never
+// runs out while the cluster lives: results of a wait that did are NaN.
+constexpr unsigned kNormWaits = 1u << 20;
 __device__ __forceinline__ bool norm_wait(uint64_t *bar, uint32_t parity, WsHeader *hdr) {
     const uint32_t addr = smem_u32(bar);
-    for (unsigned i = 0; i < kSpinLimit; ++i) {
+    for (unsigned i = 0; i < kNormWaits; ++i) {
         uint32_t done;
         asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
             " selp.u32 %0, 1, 0, p;\n}\n"
             : "=r"(done)
-            : "r"(addr), "r"(parity)
+            : "r"(addr), "r"(parity), "r"(1000u)
             : "memory");
         if (done) return true;
-        if (i > 64) __nanosleep(32);
     }
     if (hdr != nullptr) dev_flag(hdr, CSRT_DEV_TIMEOUT);
     return false;

@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "block_norm.cuh"
+#include "gemm16_host.cuh"
 #include "mat.cuh"
 
 namespace csrt {
@@ -28,7 +29,7 @@ struct EmbedArgs {
     float *partial;            // [chunk][2][pitch]: sums of tokens that go on from the chunk before, into the chunk after
     int32_t chunk, chunks;     // tokens of a chunk
     int32_t sort_blocks;       // of the first launch, in front of those that turn
-    int32_t lanes;             // threads along a row
+    int32_t lanes;             // threads along a row; few tokens: elements between two features in shared memory
     int64_t sum_blocks;
 };
 
@@ -547,6 +548,18 @@ __device__ __forceinline__ void embed_chunk(const EmbedArgs &a, int64_t chunk, F
     }
 }
 
+// A row of zeros by `threads` threads (eight at least): 16-byte words, and the elements in front of the first and behind the
+// last.
+template <typename T>
+__device__ __forceinline__ void zero_row(T *row, int64_t d, int thread, int threads) {
+    constexpr int each = 16 / (int)sizeof(T);
+    const int64_t front = imin<int64_t>(d, (int64_t)(-reinterpret_cast<uintptr_t>(row) & 15) / (int64_t)sizeof(T));
+    const int64_t words = (d - front) / each, back = front + words * each;
+    for (int64_t j = thread; j < words; j += threads) reinterpret_cast<uint4 *>(row + front)[j] = make_uint4(0, 0, 0, 0);
+    if (thread < front) row[thread] = from_f<T>(0.f);
+    if (thread < d - back) row[back + thread] = from_f<T>(0.f);
+}
+
 // The group of features and the chunk that a thread of the second and third launch works on.
 template <bool VEC>
 __device__ __forceinline__ bool embed_place(const EmbedArgs &a, Features &f, int64_t &chunk) {
@@ -581,13 +594,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a) {
     TT *out = reinterpret_cast<TT *>(a.out) + v0 * a.ldo;
     for (int r = 0; r < rows; ++r, out += a.ldo) {
         if (used[r]) continue;
-        // 16-byte words, and the elements in front of the first and behind the last
-        constexpr int each = 16 / (int)sizeof(TT);
-        const int64_t front = imin<int64_t>(a.d, (int64_t)(-reinterpret_cast<uintptr_t>(out) & 15) / (int64_t)sizeof(TT));
-        const int64_t words = (a.d - front) / each, back = front + words * each;
-        for (int64_t j = threadIdx.x; j < words; j += kSumThreads) reinterpret_cast<uint4 *>(out + front)[j] = make_uint4(0, 0, 0, 0);
-        if (threadIdx.x < front) out[threadIdx.x] = from_f<TT>(0.f);
-        if (threadIdx.x < a.d - back) out[back + threadIdx.x] = from_f<TT>(0.f);
+        zero_row(out, a.d, threadIdx.x, kSumThreads);
     }
 }
 
@@ -629,6 +636,109 @@ __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(EmbedArgs a) {
     }
     if (a.accumulate) put_row<TT, VEC, true>(a, v, f, s, old);
     else put_row<TT, VEC, false>(a, v, f, s, old);
+}
+
+// ---------------------------------------------------------------------------
+// Gradient of few tokens, one launch: a block takes 32 features, keeps them for all tokens in shared memory and sorts the
+// tokens itself; a warp adds the runs that begin in its share of the sorted tokens, a feature a lane, and writes 32 features
+// of their rows. Other blocks write the zeros. 64 tokens of 4096 features added to a table: 6.4 us, in three launches 8.0; 200 of
+// 300 into 5000 rows 10.4 and 13.9; 300 of 64 features 14.8 and 10.6, as every block sorts for itself.
+// ---------------------------------------------------------------------------
+constexpr int kSmallTokens = 256, kSmallFeatures = 32, kSmallThreads = 1024;
+static_assert(kSmallThreads == 32 * kSmallFeatures, "a warp fetches a feature");
+
+// Ascending over `size` (a power of two, at most kSmallThreads) threads' keys: a bitonic network, exchanges over fewer than
+// 32 threads by shuffles. `buf` holds a key a thread.
+__device__ __forceinline__ uint64_t bitonic_sort(uint64_t key, int size, uint64_t *buf) {
+    const int t = threadIdx.x;
+    for (int k = 2; k <= size; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            uint64_t other;
+            if (j < 32) {
+                other = __shfl_xor_sync(0xffffffffu, key, j);
+            } else {
+                __syncthreads();
+                buf[t] = key;
+                __syncthreads();
+                other = buf[t ^ j];
+            }
+            const bool low = ((t & j) == 0) == ((t & k) == 0);   // this thread keeps the smaller one
+            if (low ? other < key : other > key) key = other;
+        }
+    return key;
+}
+
+template <typename TX>
+constexpr int small_pitch(int n) {   // elements: rows of an odd number of 4-byte words, a lane each without bank conflicts
+    return sizeof(TX) == 4 ? n | 1 : ((n + 1) / 2 | 1) * 2;
+}
+
+template <typename TX, typename TT>
+__global__ void __launch_bounds__(kSmallThreads) embed_bwd_small_kernel(EmbedArgs a) {
+    pdl_enter();
+    constexpr int kAhead = 8;   // runs whose rows are fetched together
+    extern __shared__ __align__(16) char space[];
+    __shared__ uint64_t buf[kSmallThreads];
+    __shared__ int32_t used[kZeroRows];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t groups = ceil_div<int64_t>(a.d, kSmallFeatures);
+    TT *out = reinterpret_cast<TT *>(a.out);
+    const int t = threadIdx.x;
+    int32_t token = t < a.n ? a.tokens[t] : -1;
+    if (token >= a.vocab) {
+        if (blockIdx.x == 0) dev_flag(a.hdr, CSRT_DEV_INVALID);
+        token = -1;
+    }
+    if (blockIdx.x >= groups) {
+        const int64_t v0 = ((int64_t)blockIdx.x - groups) * kZeroRows;
+        const int rows = (int)imin<int64_t>(kZeroRows, a.vocab - v0);
+        if (t < kZeroRows) used[t] = 0;
+        __syncthreads();
+        if (token >= v0 && token < v0 + rows) used[token - v0] = 1;
+        __syncthreads();
+        for (int r = warp; r < rows; r += kSmallThreads / 32)
+            if (!used[r]) zero_row(out + (v0 + r) * a.ldo, a.d, lane, 32);
+        return;
+    }
+    const int64_t i0 = (int64_t)blockIdx.x * kSmallFeatures;
+    const int features = (int)imin<int64_t>(kSmallFeatures, a.d - i0), pitch = a.lanes;
+    TX *tile = reinterpret_cast<TX *>(space);
+    const TX *dx = reinterpret_cast<const TX *>(a.table) + i0 * a.ld;
+    if (warp < features)
+#pragma unroll 16
+        for (int c = lane; c < a.n; c += 32) tile[warp * pitch + c] = dx[warp * a.ld + c];
+    int size = 32;
+    while (size < a.n) size <<= 1;
+    // padding behind all tokens; columns in ascending order within a token
+    uint64_t key = (uint64_t)(token < 0 ? 0xffffffffu : (uint32_t)token) << 32 | (uint32_t)t;
+    key = bitonic_sort(key, size, buf);
+    __syncthreads();
+    buf[t] = key;
+    __syncthreads();
+    const int per = (a.n + 31) / 32, p0 = imin(a.n, warp * per), p1 = imin(a.n, p0 + per);
+    const bool in = lane < features;
+    auto token_at = [&](int p) { return p < a.n ? (uint32_t)(buf[p] >> 32) : 0xffffffffu; };
+    for (int p = p0; p < p1; p += kAhead) {
+        TT old[kAhead];
+        uint32_t v[kAhead];
+        bool first[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            v[u] = p + u < p1 ? token_at(p + u) : 0xffffffffu;
+            first[u] = v[u] != 0xffffffffu && (p + u == 0 || token_at(p + u - 1) != v[u]);
+            old[u] = from_f<TT>(0.f);
+            if (first[u] && a.accumulate && in) old[u] = out[v[u] * a.ldo + i0 + lane];
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (!first[u]) continue;
+            float s = 0.f;
+            for (int q = p + u; token_at(q) == v[u]; ++q)
+                if (in) s += to_f<TX>(tile[lane * pitch + (int)(uint32_t)buf[q]]);
+            if (in)
+                out[v[u] * a.ldo + i0 + lane] = from_f<TT>(a.accumulate ? fmaf(s, a.scale, to_f<TT>(old[u])) : s * a.scale);
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -711,7 +821,21 @@ static int launch_embed_sums(const EmbedArgs &a, cudaStream_t s) {
 }
 
 template <typename TX, typename TT>
+static int launch_embed_small(EmbedArgs a, cudaStream_t s) {
+    a.lanes = small_pitch<TX>(a.n);
+    const int smem = kSmallFeatures * a.lanes * (int)sizeof(TX);
+    constexpr auto kernel = embed_bwd_small_kernel<TX, TT>;
+    CSRT_TRY(allow_smem<kernel>(kSmallFeatures * small_pitch<TX>(kSmallTokens) * (int)sizeof(TX)));
+    const int64_t blocks = ceil_div<int64_t>(a.d, kSmallFeatures) + (a.accumulate ? 0 : ceil_div<int64_t>(a.vocab, kZeroRows));
+    CSRT_ARG(blocks < INT32_MAX, "dtable is too large");
+    launch_pdl(kernel, dim3((unsigned)blocks), dim3(kSmallThreads), (size_t)smem, s, a);
+    count_launch();
+    return check_launch("embed_bwd_small_kernel");
+}
+
+template <typename TX, typename TT>
 static int launch_embed_bwd(EmbedArgs a, cudaStream_t s) {
+    if (a.n <= kSmallTokens) return launch_embed_small<TX, TT>(a, s);
     const bool rank = a.n <= kRankTokens;
     const int64_t tiles = ceil_div<int64_t>(a.n, kTurnTokens) * ceil_div<int64_t>(a.d, kTurnFeatures);
     a.sort_blocks = rank ? imax(1, ceil_div(a.n, kRankColumns)) : 1;

@@ -673,7 +673,8 @@ def embed_bwd(dx, tokens, dtable, ws: Workspace, scale: float = 1.0, accumulate:
 class TensorList:
     """Tensors that grad_norm and grad_clip take together, described once: 2-D
     ones with contiguous rows, or contiguous ones of any shape. The tensors are
-    kept; their storage must stay where it is."""
+    kept; their storage must stay where it is. Lists that grad_clip writes to
+    hold no two tensors of one memory (columns of one buffer count as such)."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -690,6 +691,10 @@ class TensorList:
             if t.dim() != 2 or max(t.shape) >= 2 ** 31:
                 raise ValueError(f"{name} has a side of 2^31 or more")
             self._s[k] = _mat(t, name)
+        # two tensors of one memory: fine to read, not to write
+        extents = sorted((m.data or 0, (m.data or 0) + ((m.rows - 1) * m.ld + m.cols) * (4 if m.dtype == CSRT_DT_F32 else 2),
+                          k) for k, m in enumerate(self._s[:len(self.tensors)]) if m.rows and m.cols)
+        self.overlap = next(((a[2], b[2]) for a, b in zip(extents, extents[1:]) if b[0] < a[1]), None)
 
     def __len__(self):
         return len(self.tensors)
@@ -713,6 +718,9 @@ def grad_clip(grads, max_norm: float, norm, ws: Workspace, out=None, stream=None
     if out is not None and len(out) != len(grads):
         raise ValueError("out must have one tensor for each of grads")
     _f32(norm, "norm", 2)
+    overlap = (grads if out is None else out).overlap
+    if overlap is not None:
+        raise ValueError("tensors %d and %d of %s overlap" % (*sorted(overlap), "grads" if out is None else "out"))
     _check(lib().csrt_grad_clip(grads._s, len(grads), float(max_norm), None if out is None else out._s, norm.data_ptr(),
                                 ws.ptr, ws.nbytes, _stream(stream)), "csrt_grad_clip")
 

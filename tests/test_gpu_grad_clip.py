@@ -168,3 +168,54 @@ def test_captured_on_another_stream(C):
             assert all(torch.equal(a, b) for a, b in zip(want, into + [norm]))
     torch.cuda.current_stream().wait_stream(side)
     assert ws.status()[0] == 0
+
+
+def test_one_memory_twice_is_not_written(C):
+    """A tensor that is listed twice counts twice in a norm, and is refused where it would be scaled twice."""
+    t = torch.full((40, 30), 2.0, device="cuda")
+    ws, norm = C.GradWorkspace(), torch.zeros(2, device="cuda")
+    C.grad_norm([t, t], norm, ws)
+    assert abs(float(norm[0]) - math.sqrt(2 * 1200 * 4)) < 1e-3
+    for pair in ([t, t], [t, t[3:7]], [t.view(-1)[:100], t.view(-1)[99:200]]):
+        with pytest.raises(ValueError, match="overlap"):
+            C.grad_clip(pair, 1.0, norm, ws)
+    assert (t == 2).all()
+    out = [torch.empty_like(t), torch.empty_like(t)]
+    C.grad_clip([t, t], 1.0, norm, ws, out=out)
+    assert torch.equal(out[0], out[1]) and float(out[0][0, 0]) < 1
+    C.grad_clip([t.view(-1)[:100], t.view(-1)[100:200]], 1.0, norm, ws)   # side by side
+
+
+def test_first_call_is_captured(C):
+    """Nothing has to run eagerly first (in a process of its own)."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_1905_07931_gb300 import csrtrain as C
+g = [torch.ones(300, 300, device="cuda"), torch.ones(70000, 200, device="cuda")]
+ws, norm = C.GradWorkspace(), torch.zeros(2, device="cuda")
+y = torch.randn(520, 96, device="cuda").bfloat16(); h, v = torch.empty_like(y), torch.empty_like(y)
+rstd = torch.empty(96, device="cuda")
+wsn = C.BlockNormWorkspace(520, 96)
+dr, dw = torch.empty_like(y), torch.empty(520, device="cuda")
+N = C.Norm("rms", rstd=rstd, dweight=dw)
+table, tok = torch.randn(50, 520, device="cuda"), torch.randint(0, 50, (96,), device="cuda").int()
+wse = C.EmbedWorkspace(50, 520, 96)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    C.embed_fwd(table, tok, y, wse)
+    C.block_norm_fwd(y, None, h, v, pre=N)
+    C.block_norm_bwd(v, None, h, None, dr, None, wsn, pre=N)
+    C.embed_bwd(dr, tok, table, wse, accumulate=True)
+    C.grad_clip(g[:1], 1.0, norm, ws)
+    C.grad_clip(g, 1.0, norm, ws)
+graph.replay()
+torch.cuda.synchronize()
+assert all(w.status()[0] == 0 for w in (ws, wsn, wse))
+assert abs(float((g[0].double() ** 2).sum() + (g[1].double() ** 2).sum()) - 1) < 1e-3
+print("captured")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=110)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr
