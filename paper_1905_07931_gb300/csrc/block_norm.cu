@@ -361,6 +361,8 @@ static NormTile norm_bwd_choice(const NormArgs &a, bool in, bool wide, bool f32_
     if (a.n <= 2) return kTile1x4;
     if (d <= 2048 && (!in || tiles * ceil_div<int64_t>(d, 128) <= 2 * num_sms())) return kTile32x2;
     if (!in) return d <= 4096 ? kTile16x2 : d <= 8192 ? kTile8x2 : kTile8x4;
+    // few tokens: one cluster, which writes the sums over them itself (4096 x 24 on two: 10.5)
+    if (d <= 4096 && tiles * ceil_div<int64_t>(d, 256) <= num_sms()) return kTile32x4;
     // 4096 x 8192 with a float32 stream: 224, on 4 x 32, which leaves one block an SM, 238; 2048 x 8192: 96 and 122
     if (f32_stream && d <= 4096) return kTile16x2;
     // 2048 x 8192: 67 on 4 x 32, 70 on 4 x 16; 4096 x 8192: 148 and 130
@@ -546,6 +548,7 @@ int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *
     const NormTile t = norm_bwd_choice(a, in, tb == CSRT_DT_F32, ts == CSRT_DT_F32);
     CSRT_TRY(t == kTileColumns ? CSRT_NORM_DISPATCH(launch_bwd, tb, ts, a, s) : CSRT_NORM_TILES(norm_bwd, tb, ts)(a, t, in, out, s));
     if (po->dweight == nullptr && po->dbias == nullptr && pr->dweight == nullptr && pr->dbias == nullptr) return CSRT_OK;
+    if (t != kTileColumns && a.groups == 1) return CSRT_OK;   // the only group has written them
     launch_pdl(norm_sums_kernel, dim3((unsigned)ceil_div<int64_t>(d, 32), 4), dim3(256), 0, s, a);
     count_launch();
     return check_launch("norm_sums_kernel");

@@ -21,18 +21,23 @@ struct TokenSums {
             for (int f = 0; f < F; ++f) v[k][f] = 0.f;
     }
     __device__ __forceinline__ void add(int k, int f, float x) { v[k][f] += x; }
-    // partial: [4][d], this group's; i0: the thread's first feature
-    __device__ __forceinline__ void store(float *partial, int64_t d, int64_t i0, int row0, int rows) {
+    // To the group's part of a.partial, or, by the only group, to where they belong; i0: the thread's first feature.
+    __device__ __forceinline__ void store(const NormArgs &a, int64_t group, int64_t i0, int row0, int rows) {
         const int lane = threadIdx.x & 31;
+        float *const out[4] = {a.post.dw, a.post.db, a.pre.dw, a.pre.db};
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k) {
+            if (out[k] == nullptr) continue;
+            float *p = a.groups == 1 ? out[k] : a.partial + (group * 4 + k) * a.d;
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 float s = v[k][f];
 #pragma unroll
                 for (int o = 1; o < kLanes; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (lane % kLanes == 0 && row0 + f * Place<TT, V>::kStep < rows) partial[k * d + i0 + f * Place<TT, V>::kStep] = s;
+                const int64_t i = i0 + f * Place<TT, V>::kStep;
+                if (lane % kLanes == 0 && row0 + f * Place<TT, V>::kStep < rows) p[i] = a.groups == 1 && a.accumulate ? p[i] + s : s;
             }
+        }
     }
 };
 
@@ -335,8 +340,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
             next();
         }
     }
-    if (sums_post || sums_pre)
-        sums.store(a.partial + (int64_t)(blockIdx.x / size) * 4 * a.d, a.d, i0, at.row0, rows);
+    if (sums_post || sums_pre) sums.store(a, blockIdx.x / size, i0, at.row0, rows);
     ex.leave();
 }
 

@@ -633,7 +633,7 @@ int launch_clusters(NormArgs &a, const NormMaps &maps, int size, int64_t tiles, 
     {
         std::lock_guard<std::mutex> hold(lock);
         if (fit[dev][size] == 0) {
-            CSRT_CHECK_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+            CSRT_CHECK_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024));
             CSRT_CHECK_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
             cfg.numAttrs = 1;
             int n = 0;
