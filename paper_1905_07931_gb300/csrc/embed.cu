@@ -138,8 +138,8 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
 // gradient would fetch 32 bytes for every two).
 //
 // Up to kRankTokens tokens are sorted by counting: a token's place is the number of tokens that come before it. That is n^2
-// comparisons, 4 us of the GPU's time for 8192 tokens, spread over all of it, while the radix sort below takes 25 us of one
-// block's; from there on the turn of dx hides the radix sort (features by hundreds) or is the smaller part.
+// comparisons, spread over all SMs (8192 tokens 12 us beside the turn, 777 two), while the radix sort below takes 16 us a
+// digit of 8192 tokens; from there on the turn of dx hides the radix sort (features by hundreds).
 //
 // The radix sort is stable, 8 bits a pass, by one block. Each warp owns a contiguous run of tokens; counts are kept per digit
 // and warp, so that a scan of them in that order gives every warp its places.
@@ -268,7 +268,7 @@ constexpr int kRankColumns = 64, kRankKeys = 4096;
 
 __device__ __forceinline__ void embed_rank(const EmbedArgs &a, int32_t block, int32_t *keys) {
     __shared__ int32_t part[kTurnThreads / kRankColumns][kRankColumns];
-    constexpr int kSlice = kRankKeys / (kTurnThreads / kRankColumns);
+    constexpr int kSlices = kTurnThreads / kRankColumns;
     const int slice = threadIdx.x / kRankColumns, column = threadIdx.x % kRankColumns;
     const int32_t c0 = block * kRankColumns, c = c0 + column;
     auto token = [&](int32_t k) {
@@ -286,19 +286,25 @@ __device__ __forceinline__ void embed_rank(const EmbedArgs &a, int32_t block, in
             keys[k * kTurnThreads + threadIdx.x] = at < a.n ? token(at) : INT32_MAX;
         }
         __syncthreads();
-        const int32_t first = base + slice * kSlice;
-        const int4 *p = reinterpret_cast<const int4 *>(keys + slice * kSlice);
-        if (first + kSlice <= c0 || first >= c0 + kRankColumns) {
+        // each slice's keys, a multiple of four; behind the last are INT32_MAX
+        const int length = (imin(kRankKeys, a.n - base) + 4 * kSlices - 1) / (4 * kSlices) * 4;
+        const int32_t first = base + slice * length;
+        const int4 *p = reinterpret_cast<const int4 *>(keys + slice * length);
+        if (first + length <= c0 || first >= c0 + kRankColumns) {
             // equal tokens count where they lie in front
             const int32_t below = first < c0 ? mine + 1 : mine;
-            const int some = imin(kSlice, imax(0, a.n - first));
 #pragma unroll 8
-            for (int k = 0; k < (some + 3) / 4; ++k) {
+            for (int k = 0; k < length / 4; ++k) {
                 const int4 v = p[k];
                 before += (v.x < below) + (v.y < below) + (v.z < below) + (v.w < below);
             }
         } else {
-            for (int k = 0; k < imin(kSlice, a.n - first); ++k) before += keys[slice * kSlice + k] < mine + (first + k < c);
+#pragma unroll 2
+            for (int k = 0; k < length / 4; ++k) {
+                const int4 v = p[k];
+                const int32_t at = first + 4 * k;
+                before += (v.x < mine + (at < c)) + (v.y < mine + (at + 1 < c)) + (v.z < mine + (at + 2 < c)) + (v.w < mine + (at + 3 < c));
+            }
         }
     }
     part[slice][column] = before;
@@ -306,7 +312,7 @@ __device__ __forceinline__ void embed_rank(const EmbedArgs &a, int32_t block, in
     if (slice != 0 || c >= a.n) return;
     int32_t place = 0;
 #pragma unroll
-    for (int s = 0; s < kTurnThreads / kRankColumns; ++s) place += part[s][column];
+    for (int s = 0; s < kSlices; ++s) place += part[s][column];
     a.key[0][place] = mine;
     a.idx[0][place] = c;
 }
@@ -641,32 +647,11 @@ __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(EmbedArgs a) {
 // ---------------------------------------------------------------------------
 // Gradient of few tokens, one launch: a block takes 32 features, keeps them for all tokens in shared memory and sorts the
 // tokens itself; a warp adds the runs that begin in its share of the sorted tokens, a feature a lane, and writes 32 features
-// of their rows. Other blocks write the zeros. 64 tokens of 4096 features added to a table: 6.4 us, in three launches 8.0; 200 of
-// 300 into 5000 rows 10.4 and 13.9; 300 of 64 features 14.8 and 10.6, as every block sorts for itself.
+// of their rows. Other blocks write the zeros. 64 tokens of 4096 features added to a table: 4.5 us, in three launches 8.1; 200
+// of 300 into 5000 rows 8.0 and 12.5; 512 of 4096 17.7 and 9.4, as every block sorts for itself and holds all tokens.
 // ---------------------------------------------------------------------------
 constexpr int kSmallTokens = 256, kSmallFeatures = 32, kSmallThreads = 1024;
 static_assert(kSmallThreads == 32 * kSmallFeatures, "a warp fetches a feature");
-
-// Ascending over `size` (a power of two, at most kSmallThreads) threads' keys: a bitonic network, exchanges over fewer than
-// 32 threads by shuffles. `buf` holds a key a thread.
-__device__ __forceinline__ uint64_t bitonic_sort(uint64_t key, int size, uint64_t *buf) {
-    const int t = threadIdx.x;
-    for (int k = 2; k <= size; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            uint64_t other;
-            if (j < 32) {
-                other = __shfl_xor_sync(0xffffffffu, key, j);
-            } else {
-                __syncthreads();
-                buf[t] = key;
-                __syncthreads();
-                other = buf[t ^ j];
-            }
-            const bool low = ((t & j) == 0) == ((t & k) == 0);   // this thread keeps the smaller one
-            if (low ? other < key : other > key) key = other;
-        }
-    return key;
-}
 
 template <typename TX>
 constexpr int small_pitch(int n) {   // elements: rows of an odd number of 4-byte words, a lane each without bank conflicts
@@ -678,7 +663,9 @@ __global__ void __launch_bounds__(kSmallThreads) embed_bwd_small_kernel(EmbedArg
     pdl_enter();
     constexpr int kAhead = 8;   // runs whose rows are fetched together
     extern __shared__ __align__(16) char space[];
-    __shared__ uint64_t buf[kSmallThreads];
+    constexpr int32_t kPad = INT32_MAX - 1;                 // above every token, below what lies behind the last one
+    __shared__ __align__(16) int32_t keys[kSmallThreads];   // tokens, kPad, INT32_MAX
+    __shared__ int32_t place[kSmallThreads], sorted[kSmallThreads], column[kSmallThreads];
     __shared__ int32_t used[kZeroRows];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t groups = ceil_div<int64_t>(a.d, kSmallFeatures);
@@ -707,36 +694,52 @@ __global__ void __launch_bounds__(kSmallThreads) embed_bwd_small_kernel(EmbedArg
     if (warp < features)
 #pragma unroll 16
         for (int c = lane; c < a.n; c += 32) tile[warp * pitch + c] = dx[warp * a.ld + c];
+    // a token's place: the tokens that come before it, counted by size columns x slices of threads
+    keys[t] = t >= a.n ? INT32_MAX : token < 0 ? kPad : token;
+    place[t] = 0;
     int size = 32;
     while (size < a.n) size <<= 1;
-    // padding behind all tokens; columns in ascending order within a token
-    uint64_t key = (uint64_t)(token < 0 ? 0xffffffffu : (uint32_t)token) << 32 | (uint32_t)t;
-    key = bitonic_sort(key, size, buf);
+    const int slices = kSmallThreads / size, c = t % size, length = (a.n + 4 * slices - 1) / (4 * slices) * 4;
     __syncthreads();
-    buf[t] = key;
+    if (c < a.n) {
+        const int32_t mine = keys[c];
+        const int from = t / size * length;
+        int before = 0;
+#pragma unroll 4
+        for (int k = from; k < imin(from + length, a.n); k += 4) {   // equal ones count where they lie in front
+            const int4 v = *reinterpret_cast<const int4 *>(keys + k);
+            before += (v.x < mine + (k < c)) + (v.y < mine + (k + 1 < c)) + (v.z < mine + (k + 2 < c)) + (v.w < mine + (k + 3 < c));
+        }
+        atomicAdd(place + c, before);
+    }
+    __syncthreads();
+    if (t < a.n) {
+        sorted[place[t]] = keys[t];
+        column[place[t]] = t;
+    }
     __syncthreads();
     const int per = (a.n + 31) / 32, p0 = imin(a.n, warp * per), p1 = imin(a.n, p0 + per);
     const bool in = lane < features;
-    auto token_at = [&](int p) { return p < a.n ? (uint32_t)(buf[p] >> 32) : 0xffffffffu; };
+    auto token_at = [&](int p) { return p < a.n ? sorted[p] : kPad; };
     for (int p = p0; p < p1; p += kAhead) {
         TT old[kAhead];
-        uint32_t v[kAhead];
+        int32_t v[kAhead];
         bool first[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            v[u] = p + u < p1 ? token_at(p + u) : 0xffffffffu;
-            first[u] = v[u] != 0xffffffffu && (p + u == 0 || token_at(p + u - 1) != v[u]);
+            v[u] = p + u < p1 ? token_at(p + u) : kPad;
+            first[u] = v[u] != kPad && (p + u == 0 || token_at(p + u - 1) != v[u]);
             old[u] = from_f<TT>(0.f);
-            if (first[u] && a.accumulate && in) old[u] = out[v[u] * a.ldo + i0 + lane];
+            if (first[u] && a.accumulate && in) old[u] = out[(int64_t)v[u] * a.ldo + i0 + lane];
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (!first[u]) continue;
             float s = 0.f;
             for (int q = p + u; token_at(q) == v[u]; ++q)
-                if (in) s += to_f<TX>(tile[lane * pitch + (int)(uint32_t)buf[q]]);
+                if (in) s += to_f<TX>(tile[lane * pitch + column[q]]);
             if (in)
-                out[v[u] * a.ldo + i0 + lane] = from_f<TT>(a.accumulate ? fmaf(s, a.scale, to_f<TT>(old[u])) : s * a.scale);
+                out[(int64_t)v[u] * a.ldo + i0 + lane] = from_f<TT>(a.accumulate ? fmaf(s, a.scale, to_f<TT>(old[u])) : s * a.scale);
         }
     }
 }
