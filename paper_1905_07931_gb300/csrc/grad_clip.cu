@@ -278,14 +278,15 @@ __global__ void __launch_bounds__(kGradThreads, 4) grad_scale_kernel(const __gri
     }
 }
 
-// Norm and scaling in one launch, for no more units than four blocks an SM: each block keeps its unit in shared memory, waits
+// Norm and scaling in one launch, for no more units than two blocks an SM: each block keeps its unit in shared memory, waits
 // for the others' sums (cooperative launch: all run at the same time), adds them all by itself in one order and scales.
-// 4.8M float32 gradients in 18 tensors: 15.3 us in two launches. With more units a block the second launch's full occupancy
-// reads and writes at the copy rate, and this did not (58.7M: 111 us, two launches 110).
+// 60 tensors of 1 to 100000: 7.1 us, in two launches 9.2. With four blocks an SM it is no faster (4.8M float32 in 18 tensors
+// 16.4 in a stream, two launches 15.0), nor with several units a block (58.7M: 111 us, two launches 110): the second launch
+// reads and writes at the copy rate.
 constexpr int kHoldBytes = kGradUnit * (int)sizeof(float);
 
 template <int N>
-__global__ void __launch_bounds__(kGradThreads, 4) grad_clip_kernel(const __grid_constant__ GradArgs<N> a) {
+__global__ void __launch_bounds__(kGradThreads, 2) grad_clip_kernel(const __grid_constant__ GradArgs<N> a) {
     pdl_enter();
     extern __shared__ __align__(16) char hold[];
     __shared__ double part[kGradThreads / 32];
@@ -384,7 +385,7 @@ static int grad_launch(const csrt_mat *g, int32_t count, float max_norm, const c
         all += ceil_div<int64_t>(c, kGradUnit);
     }
     const unsigned blocks = (unsigned)imax<int64_t>(1, imin<int64_t>(all, kGradBlocks));
-    const bool once = max_norm > 0.f && full <= N && full > 0 && all <= imin<int64_t>(4 * num_sms(), kGradBlocks);
+    const bool once = max_norm > 0.f && full <= N && full > 0 && all <= 2 * num_sms();
     for (int pass = 0; pass < (max_norm > 0.f ? 2 : 1); ++pass) {
         int32_t done = 0, k = 0;
         do {

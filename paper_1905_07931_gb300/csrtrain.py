@@ -604,22 +604,27 @@ _pack_mat = struct.Struct("=Qiiqi4x").pack_into
 assert ctypes.sizeof(csrt_mat) == 32
 
 
-def _put(k, t, name):
-    """_mat in slot k of this thread; None stays None."""
-    if t is None:
-        return None
-    shape = t.shape
-    if len(shape) != 2 or not t.is_cuda:
-        raise ValueError(f"{name} must be a 2-D CUDA tensor")
-    rows, cols = shape
-    ld, inner = t.stride()
-    dtype = _DTYPES.get(t.dtype)
+def _puts(tensors, names):
+    """_mat of each of up to 12 tensors, in this thread's slots; None stays None."""
     slots = _slots
-    if inner != 1 or ld < cols or dtype is None:   # what is left of the checks, and single rows and columns
-        m = _mat(t, name)
-        ld, dtype = m.ld, m.dtype
-    _pack_mat(slots.buf, 32 * k, t.data_ptr(), rows, cols, ld, dtype)
-    return slots.mats[k]
+    buf, mats, types, pack = slots.buf, slots.mats, _DTYPES, _pack_mat
+    out = []
+    for k, t in enumerate(tensors):
+        if t is None:
+            out.append(None)
+            continue
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 2 or not t.is_cuda:
+            raise ValueError(f"{names[k]} must be a 2-D CUDA tensor")
+        rows, cols = shape
+        ld, inner = stride
+        dtype = types.get(t.dtype)
+        if inner != 1 or ld < cols or dtype is None:   # what is left of the checks, and single rows and columns
+            m = _mat(t, names[k])
+            ld, dtype = m.ld, m.dtype
+        pack(buf, 32 * k, t.data_ptr(), rows, cols, ld, dtype)
+        out.append(mats[k])
+    return out
 
 
 def _int32(t, name):
@@ -635,9 +640,10 @@ def block_norm_fwd(y, r, h, v, post: Norm | None = None, pre: Norm | None = None
     and pre with v."""
     first = y if y is not None else r
     d, n = first.shape if first is not None else (0, 0)
-    _check(lib().csrt_block_norm_fwd(_put(0, y, "y"), None if post is None else post.struct(d, n), _put(1, gate, "gate"),
-                                     _gate(gate_act), _put(2, r, "r"), float(r_scale), None if pre is None else pre.struct(d, n),
-                                     _put(3, h, "h"), _put(4, v, "v"), _stream(stream)), "csrt_block_norm_fwd")
+    y, gate, r, h, v = _puts((y, gate, r, h, v), ("y", "gate", "r", "h", "v"))
+    _check(lib().csrt_block_norm_fwd(y, None if post is None else post.struct(d, n), gate, _gate(gate_act), r, float(r_scale),
+                                     None if pre is None else pre.struct(d, n), h, v, _stream(stream)),
+           "csrt_block_norm_fwd")
 
 
 def block_norm_bwd(dv, dh, h, y, dr, dy, ws: Workspace, post: Norm | None = None, pre: Norm | None = None, gate=None,
@@ -646,19 +652,21 @@ def block_norm_bwd(dv, dh, h, y, dr, dy, ws: Workspace, post: Norm | None = None
     may be None), and the norms' dweight and dbias (added to with accumulate)."""
     first = dv if dv is not None else dh
     d, n = first.shape if first is not None else (0, 0)
-    _check(lib().csrt_block_norm_bwd(_put(0, dv, "dv"), _put(1, dh, "dh"), _put(2, h, "h"),
-                                     None if pre is None else pre.struct(d, n), _put(3, y, "y"),
-                                     None if post is None else post.struct(d, n), _put(4, gate, "gate"), _gate(gate_act),
-                                     float(r_scale), 1 if accumulate else 0, _put(5, dr, "dr"), _put(6, dy, "dy"),
-                                     _put(7, dgate, "dgate"), ws.ptr, ws.nbytes, _stream(stream)), "csrt_block_norm_bwd")
+    dv, dh, h, y, gate, dr, dy, dgate = _puts((dv, dh, h, y, gate, dr, dy, dgate),
+                                              ("dv", "dh", "h", "y", "gate", "dr", "dy", "dgate"))
+    _check(lib().csrt_block_norm_bwd(dv, dh, h, None if pre is None else pre.struct(d, n), y,
+                                     None if post is None else post.struct(d, n), gate, _gate(gate_act), float(r_scale),
+                                     1 if accumulate else 0, dr, dy, dgate, ws.ptr, ws.nbytes, _stream(stream)),
+           "csrt_block_norm_bwd")
 
 
 def embed_fwd(table, tokens, x, ws: Workspace, scale: float = 1.0, stream=None):
     """x[:, c] = scale * table[tokens[c]]; a negative token gives a column of zeros."""
     if _int32(tokens, "tokens").numel() < x.shape[-1]:
         raise ValueError(f"tokens has {tokens.numel()} elements, needs {x.shape[-1]}")
-    _check(lib().csrt_embed_fwd(_put(0, table, "table"), tokens.data_ptr(), float(scale), _put(1, x, "x"), ws.ptr, ws.nbytes,
-                                _stream(stream)), "csrt_embed_fwd")
+    mtable, mx = _puts((table, x), ("table", "x"))
+    _check(lib().csrt_embed_fwd(mtable, tokens.data_ptr(), float(scale), mx, ws.ptr, ws.nbytes, _stream(stream)),
+           "csrt_embed_fwd")
 
 
 def embed_bwd(dx, tokens, dtable, ws: Workspace, scale: float = 1.0, accumulate: bool = False, stream=None):
@@ -666,8 +674,9 @@ def embed_bwd(dx, tokens, dtable, ws: Workspace, scale: float = 1.0, accumulate:
     accumulate: added to it, rows without tokens left as they are)."""
     if _int32(tokens, "tokens").numel() < dx.shape[-1]:
         raise ValueError(f"tokens has {tokens.numel()} elements, needs {dx.shape[-1]}")
-    _check(lib().csrt_embed_bwd(_put(0, dx, "dx"), tokens.data_ptr(), float(scale), 1 if accumulate else 0,
-                                _put(1, dtable, "dtable"), ws.ptr, ws.nbytes, _stream(stream)), "csrt_embed_bwd")
+    mdx, mtable = _puts((dx, dtable), ("dx", "dtable"))
+    _check(lib().csrt_embed_bwd(mdx, tokens.data_ptr(), float(scale), 1 if accumulate else 0, mtable, ws.ptr, ws.nbytes,
+                                _stream(stream)), "csrt_embed_bwd")
 
 
 class TensorList:

@@ -111,7 +111,8 @@ def _norm(x, ex, kind, w, b):
 
 
 SHAPES = [(1, 1), (3, 5), (64, 33), (100, 1), (4096, 1), (784, 256), (1000, 777), (513, 32), (130, 2), (4096, 24),
-          (9216, 40), (5000, 7), (2048, 300), (7, 2000), (264, 1024), (1056, 64), (12000, 9)]
+          (9216, 40), (5000, 7), (2048, 300), (7, 2000), (264, 1024), (1056, 64), (12000, 9), (12000, 16), (20000, 5), (20000, 2),
+          (70000, 1)]
 # block type, stream type, post, pre, gate activation (None: no gate), biases, layout
 FORMS = [("bf16", "bf16", "rms", "rms", "sigmoid", False, "tight"),
          ("f16", "f16", "layer", "layer", "silu", True, "odd"),
