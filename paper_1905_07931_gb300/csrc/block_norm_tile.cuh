@@ -14,8 +14,8 @@
 // a row (or fewer of several) a store.
 #pragma once
 
+#include <atomic>
 #include <cmath>
-#include <mutex>
 #include <type_traits>
 
 #include "block_norm.cuh"
@@ -611,8 +611,11 @@ __device__ __forceinline__ void clear_rows(char *tile, int chunk) {
 // Launches `kernel` on clusters of `size` blocks, as many as fit or as there are tiles (a.groups).
 template <auto kernel>
 int launch_clusters(NormArgs &a, const NormMaps &maps, int size, int64_t tiles, int smem, cudaStream_t s) {
-    static std::mutex lock;
-    static int fit[64][kNormClusterMax + 1] = {{0}};
+    // by what a block holds, so that a call gives the same clusters (and sums over tokens the same order) whatever came before;
+    // threads that come first at the same time find the same
+    static std::atomic<uint16_t> fit[64][kNormClusterMax + 1][32];
+    const int holds = (a.y.p != nullptr) | (a.g.p != nullptr) << 1 | (a.r.p != nullptr) << 2 | (a.h.p != nullptr) << 3 |
+                      (a.dv.p != nullptr) << 4;
     int dev = 0;
     CSRT_ARG(size > 0, "a cluster cannot hold %d features", a.d);
     CSRT_CHECK_CUDA(cudaGetDevice(&dev));
@@ -629,18 +632,15 @@ int launch_clusters(NormArgs &a, const NormMaps &maps, int size, int64_t tiles, 
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = s;
     cfg.attrs = attr;
-    int resident;
-    {
-        std::lock_guard<std::mutex> hold(lock);
-        if (fit[dev][size] == 0) {
-            CSRT_CHECK_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024));
-            CSRT_CHECK_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-            cfg.numAttrs = 1;
-            int n = 0;
-            CSRT_CHECK_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
-            fit[dev][size] = imax(1, n);
-        }
-        resident = fit[dev][size];
+    int resident = fit[dev][size][holds].load(std::memory_order_relaxed);
+    if (resident == 0) {
+        CSRT_CHECK_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024));
+        CSRT_CHECK_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        cfg.numAttrs = 1;
+        int n = 0;
+        CSRT_CHECK_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
+        resident = imin(imax(1, n), 65535);
+        fit[dev][size][holds].store((uint16_t)resident, std::memory_order_relaxed);
     }
     a.cluster = size;
     a.groups = (int32_t)imin<int64_t>(imin<int64_t>(tiles, resident), kNormGroups);

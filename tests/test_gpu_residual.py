@@ -136,3 +136,56 @@ def test_command_runs(R, capsys):
     R.main(["--features", "96", "--hidden", "64", "--blocks", "2", "--batch", "40", "--steps", "2", "--norm", "rms", "--gate", "silu",
             "--vocab", "50", "--clip", "1"])
     assert '"grad_norm"' in capsys.readouterr().out
+
+
+def test_two_streams_at_once(R):
+    """Every call on two streams with a workspace each, many times over: the results are those of the calls one by one."""
+    C = R.C
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(11)
+
+    def work(k):
+        d, n, vocab = 1040 + 8 * k, 1500 + 5 * k, 700
+        s = {"y": torch.randn(d, n, generator=gen, device="cuda").bfloat16(), "r": torch.randn(d, n, generator=gen, device="cuda"),
+             "g": torch.randn(d, n, generator=gen, device="cuda").bfloat16(),
+             "tok": torch.randint(-1, vocab, (n,), generator=gen, device="cuda").int(),
+             "table": torch.randn(vocab, d, generator=gen, device="cuda")}
+        s["h"], s["v"], s["x"] = torch.empty_like(s["r"]), torch.empty_like(s["y"]), torch.empty_like(s["y"])
+        s["dr"], s["dy"], s["dg"], s["dt"] = (torch.empty_like(s[q]) for q in ("r", "y", "g", "table"))
+        stat = [torch.empty(n, device="cuda") for _ in range(4)]
+        s["dw"] = [torch.empty(d, device="cuda") for _ in range(4)]
+        P = C.Norm("layer", mean=stat[0], rstd=stat[1], dweight=s["dw"][0], dbias=s["dw"][1])
+        Q = C.Norm("rms", rstd=stat[2], dweight=s["dw"][2], dbias=s["dw"][3])
+        wsn, wse, wsk = C.BlockNormWorkspace(d, n), C.EmbedWorkspace(vocab, d, n), C.GradWorkspace()
+        small, out = [s["dw"][0], s["dw"][2]], [torch.empty(d, device="cuda") for _ in range(2)]
+        s["out"], s["norm"] = out, torch.zeros(2, device="cuda")
+
+        def run():
+            C.embed_fwd(s["table"], s["tok"], s["x"], wse, scale=0.5)
+            C.block_norm_fwd(s["y"], s["r"], s["h"], s["v"], post=P, pre=Q, gate=s["g"], gate_act="silu")
+            C.block_norm_bwd(s["v"], s["r"], s["h"], s["y"], s["dr"], s["dy"], wsn, post=P, pre=Q, gate=s["g"], gate_act="silu",
+                             dgate=s["dg"])
+            C.embed_bwd(s["dy"], s["tok"], s["dt"], wse)
+            C.grad_clip(small, 1e-3, s["norm"], wsk, out=out)
+
+        return s, run, (wsn, wse, wsk)
+
+    works = [work(k) for k in range(2)]
+    names = ("h", "v", "x", "dr", "dy", "dg", "dt", "norm")
+    want = []
+    for s, run, _ in works:
+        run()
+        torch.cuda.synchronize()
+        want.append([s[q].clone() for q in names] + [t.clone() for t in s["dw"] + s["out"]])
+    streams = [torch.cuda.Stream() for _ in works]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        for stream, (s, run, _) in zip(streams, works):
+            with torch.cuda.stream(stream):
+                run()
+    torch.cuda.synchronize()
+    for (s, _, workspaces), w in zip(works, want):
+        got = [s[q] for q in names] + s["dw"] + s["out"]
+        assert all(torch.equal(a, b) for a, b in zip(got, w))
+        assert all(ws.status()[0] == 0 for ws in workspaces)
