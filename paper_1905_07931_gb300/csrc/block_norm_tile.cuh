@@ -314,7 +314,7 @@ struct Result {
 // Chan, Golub and LeVeque: no cancellation, and one exchange instead of two.
 //
 // Blocks write their totals into each other's shared memory by st.async, which counts on the receiver's mbarrier: a cluster
-// barrier in its place waits for the stores of results in flight too (a fifth of the forward kernel's stalls).
+// barrier in its place waits for the stores of results in flight too (a tenth of the forward kernel's stalls).
 // ---------------------------------------------------------------------------
 enum { kOneSum, kTwoSums, kMoments };
 
