@@ -365,7 +365,7 @@ static NormTile norm_bwd_choice(const NormArgs &a, bool in, bool wide, bool f32_
     if (d <= 4096 && tiles * ceil_div<int64_t>(d, 256) <= num_sms()) return kTile32x4;
     // 4096 x 8192 with a float32 stream: 224, on 4 x 32, which leaves one block an SM, 238; 2048 x 8192: 96 and 122
     if (f32_stream && d <= 4096) return kTile16x2;
-    // 2048 x 8192: 67 on 4 x 32, 70 on 4 x 16; 4096 x 8192: 148 and 130
+    // 2048 x 8192: 67 on 4 x 32, 70 on 4 x 16; 4096 x 8192: 148 and 130 (1 to 2 more since 1 - sigmoid keeps its digits)
     return d <= 2048 ? kTile32x4 : d <= 8192 ? kTile16x4 : kTile8x4;
 }
 

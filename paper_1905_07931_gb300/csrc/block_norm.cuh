@@ -57,23 +57,21 @@ __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat
 // a(g) and a'(g). FAST takes the fast exponential and quotient: the sigmoid is off by (4 + 1.2 |g|) 2^-23 of itself, 2^-18 where
 // it is above 2^-24, far below a 16-bit rounding. float32 matrices take the others.
 template <bool FAST>
-__device__ __forceinline__ float sigmoid_of(float g) {
-    return FAST ? __fdividef(1.f, 1.f + __expf(-g)) : 1.f / (1.f + expf(-g));
-}
-template <bool FAST>
-__device__ __forceinline__ float gate_value(float g, int act) {
-    if (act == CSRT_GATE_NONE) return g;
-    const float p = sigmoid_of<FAST>(g);
-    return act == CSRT_GATE_SIGMOID ? p : g * p;
-}
-template <bool FAST>
 __device__ __forceinline__ void gate_both(float g, int act, float &value, float &slope) {
     value = g;
     slope = 1.f;
     if (act == CSRT_GATE_NONE) return;
-    const float p = sigmoid_of<FAST>(g);
+    const float e = FAST ? __expf(-g) : expf(-g);
+    const float p = FAST ? __fdividef(1.f, 1.f + e) : 1.f / (1.f + e);
+    const float q = fminf(e * p, 1.f);   // 1 - p, with all digits where p is near 1; 1 where e is infinite (and the product NaN)
     value = act == CSRT_GATE_SIGMOID ? p : g * p;
-    slope = act == CSRT_GATE_SIGMOID ? p * (1.f - p) : p * (1.f + g * (1.f - p));
+    slope = act == CSRT_GATE_SIGMOID ? p * q : p * (1.f + g * q);
+}
+template <bool FAST>
+__device__ __forceinline__ float gate_value(float g, int act) {
+    float value, slope;
+    gate_both<FAST>(g, act, value, slope);
+    return value;
 }
 
 // Tiles of the kernels that read every matrix once: tokens wide, features a thread.

@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
 #pragma unroll
                         for (int k = 0; k < T::N; ++k) {
                             P value, slope;
-                            gate_of<kGate, kFast>(g[k], T::all(1.f), T::all(-1.f), value, slope);
+                            gate_of<kGate, kFast>(g[k], T::all(1.f), value, slope);
                             o[k] = mul2(mul2(x[f][k], fma2(hat[k], T::all(w.x), T::all(w.y))), slope);
                             x[f][k] = mul2(x[f][k], value);
                         }

@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(con
 #pragma unroll
                         for (int k = 0; k < T::N; ++k) {
                             P value, slope;
-                            gate_of<kGate, kFast>(g[k], T::all(1.f), T::all(-1.f), value, slope);
+                            gate_of<kGate, kFast>(g[k], T::all(1.f), value, slope);
                             x[f][k] = mul2(x[f][k], value);
                         }
                     }

@@ -518,34 +518,45 @@ __device__ __forceinline__ float rcp_fast(float v) {
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(v));
     return v;
 }
+// p = sigmoid(g) and q = 1 - p = e^-g p, which keeps its digits where p is near 1 (the product is NaN where e^-g is infinite
+// and p is 0: the minimum takes 1).
 template <bool FAST>
-__device__ __forceinline__ f32x2 sigmoid2(f32x2 g) {
-    float a, b;
+__device__ __forceinline__ void sigmoid2(f32x2 g, f32x2 &p, f32x2 &q) {
+    float a, b, c, d;
+    f32x2 e;
     if (FAST) {
         unpack2(mul2(g, pack2(-1.44269504f, -1.44269504f)), a, b);
-        f32x2 e = add2(pack2(exp2_fast(a), exp2_fast(b)), pack2(1.f, 1.f));
-        unpack2(e, a, b);
-        return pack2(rcp_fast(a), rcp_fast(b));
+        e = pack2(exp2_fast(a), exp2_fast(b));
+        unpack2(add2(e, pack2(1.f, 1.f)), a, b);
+        p = pack2(rcp_fast(a), rcp_fast(b));
+    } else {
+        unpack2(g, a, b);
+        a = expf(-a);
+        b = expf(-b);
+        e = pack2(a, b);
+        p = pack2(1.f / (1.f + a), 1.f / (1.f + b));
     }
-    unpack2(g, a, b);
-    return pack2(sigmoid_of<false>(a), sigmoid_of<false>(b));
+    unpack2(mul2(e, p), c, d);
+    q = pack2(fminf(c, 1.f), fminf(d, 1.f));
 }
 template <bool FAST>
-__device__ __forceinline__ float sigmoid2(float g) {
-    return FAST ? rcp_fast(1.f + exp2_fast(g * -1.44269504f)) : sigmoid_of<false>(g);
+__device__ __forceinline__ void sigmoid2(float g, float &p, float &q) {
+    const float e = FAST ? exp2_fast(g * -1.44269504f) : expf(-g);
+    p = FAST ? rcp_fast(1.f + e) : 1.f / (1.f + e);
+    q = fminf(e * p, 1.f);
 }
 
 // a(g) and a'(g) of V tokens. GATE: CSRT_GATE_*, known to the compiler, so that the features of a thread's loop are not
 // separated by branches and their latencies overlap.
 template <int GATE, bool FAST, typename P>
-__device__ __forceinline__ void gate_of(P g, P one, P minus_one, P &value, P &slope) {
+__device__ __forceinline__ void gate_of(P g, P one, P &value, P &slope) {
     value = g;
     slope = one;
     if (GATE == CSRT_GATE_NONE) return;
-    const P p = sigmoid2<FAST>(g);
-    const P left = fma2(p, minus_one, one);   // 1 - p
+    P p, q;
+    sigmoid2<FAST>(g, p, q);
     value = GATE == CSRT_GATE_SILU ? mul2(p, g) : p;
-    slope = GATE == CSRT_GATE_SILU ? mul2(p, fma2(g, left, one)) : mul2(p, left);
+    slope = GATE == CSRT_GATE_SILU ? mul2(p, fma2(g, q, one)) : mul2(p, q);
 }
 template <typename F>
 __device__ __forceinline__ void with_gate(int act, F body) {

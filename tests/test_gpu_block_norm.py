@@ -515,3 +515,34 @@ def test_formula_against_differences(post, pre, act):
             e = e.view_as(t[name])
             num = (loss(dict(t, **{name: t[name] + e}))[0] - loss(dict(t, **{name: t[name] - e}))[0]) / (2 * step)
             assert math.isclose(float(num), float(grad.reshape(-1)[at]), rel_tol=1e-6, abs_tol=1e-7), (name, at)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,n,layout", [(64, 256, "tight"), (1000, 24, "wide"), (513, 33, "odd"), (70000, 1, "tight")])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("act", ["sigmoid", "silu"])
+def test_gradient_of_open_and_shut_gates(C, d, n, layout, dtype, act):
+    """With dh = 1, dv = 0 and t = 1 the gate's gradient is the gate's slope: p q and p (1 + g q), q = 1 - p. Where p is
+    near 1 its digits are those of e^-g. Off by, in steps of 2^-23: the exponential 2 + 1.173 |g|, two roundings of
+    1 + e^-g (half a step, entering p and q), two of the reciprocal (one step each), two products (half a step each)."""
+    gen, dt = _gen(d + n), DT[dtype]
+    g = _mat(gen, d, n, dt, layout)
+    g.copy_(torch.linspace(-80, 80, d * n, device="cuda")[torch.randperm(d * n, generator=gen, device="cuda")].view(d, n))
+    y, dh, dv, h = (_mat(gen, d, n, dt, layout) for _ in range(4))
+    y.fill_(1)
+    dh.fill_(1)
+    dv.zero_()
+    dr, dy, dg = (_mat(gen, d, n, dt, layout) for _ in range(3))
+    Q = C.Norm("rms", eps=EPS, rstd=_statistics(h, "rms")[1])
+    ws = C.BlockNormWorkspace(d, n)
+    C.block_norm_bwd(dv, dh, h, y, dr, dy, ws, post=C.Norm("scale"), pre=Q, gate=g, gate_act=act, dgate=dg)
+    x = g.double()
+    e = torch.exp(-x.abs())
+    big, small = 1 / (1 + e), e / (1 + e)
+    p, q = torch.where(x > 0, big, small), torch.where(x > 0, small, big)
+    err = (6 + 1.173 * x.abs()) * 2.0 ** -23
+    if act == "sigmoid":
+        _check(dg, p * q, err * p * q, "slope")
+    else:
+        slope = p * (1 + x * q)
+        _check(dg, slope, err * slope.abs() + p * (err * x.abs() * q + 2 * U * (1 + x.abs() * q)), "slope")
