@@ -546,3 +546,27 @@ def test_gradient_of_open_and_shut_gates(C, d, n, layout, dtype, act):
     else:
         slope = p * (1 + x * q)
         _check(dg, slope, err * slope.abs() + p * (err * x.abs() * q + 2 * U * (1 + x.abs() * q)), "slope")
+
+
+# A cluster walks over several tiles of tokens (a GB300 holds 14 to 150 of them, three tiles each at least): whole vectors,
+# results that end inside one, rows off the 16-byte grid, every width of the choice of tiles
+LONG = [(784, 15008), (2048, 6001), (4096, 3608), (4096, 3605), (4096, 1201), (6000, 1504), (9216, 800), (12000, 401)]
+LONG_FORMS = [("bf16", "bf16", "rms", "rms", "sigmoid", False, "tight"),
+              ("bf16", "f32", "layer", "rms", "silu", True, "wide"),
+              ("f16", "f16", "layer", "layer", "none", True, "odd"),
+              ("f16", "f32", "rms", "layer", None, False, "tight"),
+              ("f32", "f32", "scale", "layer", "silu", True, "tight")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,n", LONG)
+@pytest.mark.parametrize("form", LONG_FORMS, ids=lambda f: "-".join(str(x) for x in f))
+def test_forward_over_several_tiles(C, d, n, form):
+    test_forward(C, d, n, form)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,n", LONG)
+@pytest.mark.parametrize("form", LONG_FORMS, ids=lambda f: "-".join(str(x) for x in f))
+def test_backward_over_several_tiles(C, d, n, form):
+    test_backward(C, d, n, form)

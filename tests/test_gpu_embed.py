@@ -212,3 +212,32 @@ def test_captured_on_another_stream(C):
             graph.replay()
             assert torch.equal(a, x) and torch.equal(b, dw)
     torch.cuda.current_stream().wait_stream(side)
+
+
+# More tokens than are sorted by counting: one, two, three and four digits of the radix sort, and the last warp's share short
+@pytest.mark.parametrize("vocab,d,n", [(255, 24, 16385), (300, 40, 20001), (70000, 16, 16385), (2 ** 24 + 5, 3, 16400)])
+@pytest.mark.parametrize("table,dtype,layout", [("f32", "bf16", "tight"), ("bf16", "f32", "odd")])
+def test_backward_sorted_by_digits(C, vocab, d, n, table, dtype, layout):
+    test_backward(C, vocab, d, n, table, dtype, layout)
+
+
+@pytest.mark.parametrize("vocab,n", [(50, 130), (50, 777), (300, 16385), (70000, 20000)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_tokens_beyond_the_table_in_every_sort(C, vocab, n, accumulate):
+    """Sorted in one launch, by counting and by digits: a token of vocab or more is padding, and reported."""
+    gen = _gen(n)
+    d = 24
+    dx = _mat(gen, d, n, torch.bfloat16)
+    tok = _tokens(gen, vocab, n, "pad")
+    good = tok.clone()
+    for at, bad in ((0, vocab), (n // 3, 2 ** 31 - 1), (n - 1, vocab + 5), (n // 2, -2 ** 31)):
+        tok[at] = bad
+        good[at] = -1
+    a = _mat(gen, vocab, d, torch.float32)
+    b = a.clone()
+    ws = C.EmbedWorkspace(vocab, d, n)
+    C.embed_bwd(dx, good, b, ws, accumulate=accumulate)
+    assert ws.status()[0] == 0
+    C.embed_bwd(dx, tok, a, ws, accumulate=accumulate)
+    assert ws.status()[0] == C.CSRT_DEV_INVALID
+    assert torch.equal(a, b)
