@@ -455,7 +455,8 @@ typedef struct csrt_norm {
  * Everything is computed in float32 and rounded once: v is the norm of the h
  * that is not yet rounded. Squares are summed in float32, so entries beyond
  * 1e18 of a normed matrix overflow its statistics. A token that holds an
- * infinity or a NaN does not reach the others. h may be r itself; apart from
+ * infinity or a NaN does not reach the others; an infinite gate has its limits
+ * (sigmoid 0 and 1, silu 0 and infinity, slopes 0 or 1). h may be r itself; apart from
  * that no output overlaps anything else. Any d and n, 0 and 1 among them; rows
  * that are 16-byte aligned (data and ld) are fetched by TMA and are faster. Of
  * other rows, what shares an aligned 16-byte word with an element in front of

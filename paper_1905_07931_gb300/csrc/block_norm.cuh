@@ -54,6 +54,17 @@ __device__ __forceinline__ __half from_f(float v) { return __float2half_rn(v); }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
 
+// silu and its slope are products with sigmoid's tails, which are 0 to float32 from |g| = 104 on: with the factor g held to 128
+// an infinite gate has its limits there (-0, and a slope of 0 or 1) instead of 0 times infinity. A NaN stays.
+__device__ __forceinline__ float above_m128(float g) {
+    asm("max.NaN.f32 %0, %0, 0fC3000000;" : "+f"(g));
+    return g;
+}
+__device__ __forceinline__ float within_128(float g) {
+    asm("min.NaN.xorsign.abs.f32 %0, %0, 0f43000000;" : "+f"(g));   // min(|g|, 128) with g's sign
+    return g;
+}
+
 // a(g) and a'(g). FAST takes the fast exponential and quotient: the sigmoid is off by (4 + 1.2 |g|) 2^-23 of itself, 2^-18 where
 // it is above 2^-24, far below a 16-bit rounding. float32 matrices take the others.
 template <bool FAST>
@@ -64,8 +75,8 @@ __device__ __forceinline__ void gate_both(float g, int act, float &value, float 
     const float e = FAST ? __expf(-g) : expf(-g);
     const float p = FAST ? __fdividef(1.f, 1.f + e) : 1.f / (1.f + e);
     const float q = fminf(e * p, 1.f);   // 1 - p, with all digits where p is near 1; 1 where e is infinite (and the product NaN)
-    value = act == CSRT_GATE_SIGMOID ? p : g * p;
-    slope = act == CSRT_GATE_SIGMOID ? p * q : p * (1.f + g * q);
+    value = act == CSRT_GATE_SIGMOID ? p : above_m128(g) * p;
+    slope = act == CSRT_GATE_SIGMOID ? p * q : p * (1.f + within_128(g) * q);
 }
 template <bool FAST>
 __device__ __forceinline__ float gate_value(float g, int act) {

@@ -89,20 +89,20 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(con
     char *stage = reinterpret_cast<char *>(wpre + kFeatures) + (threadIdx.x >> 5) * RS::kStageBytes;   // this warp's
     Exchange<TT> ex(reinterpret_cast<char *>(wpre + kFeatures) + kNormWarps * RS::kStageBytes, size, rank, chunk, a.d, a.hdr);
     const int64_t first = (int64_t)rank * chunk + (threadIdx.x >> 5) * at.kRowsWarp;   // the warp's first feature
-    const int64_t tiles = ((int64_t)a.n + TT - 1) / TT;
-    int64_t tile = blockIdx.x / size;
+    const int tiles = (int)(((int64_t)a.n + TT - 1) / TT);   // n <= 2 where TT is 1
+    int tile = (int)(blockIdx.x / size);
 
-    auto column = [&](int64_t t) { return t * TT + at.q; };
-    auto exist = [&](int64_t t) { return (int)imax<int64_t>(0, imin<int64_t>(V, a.n - column(t))); };
-    auto fetch = [&](int64_t t) {
+    auto column = [&](int t) { return (int64_t)t * TT + at.q; };
+    auto exist = [&](int t) { return (int)imax<int64_t>(0, imin<int64_t>(V, a.n - column(t))); };
+    auto fetch = [&](int t) {
         if constexpr (TMA) {
             if (threadIdx.x != kLoader) return;
             uint64_t *bar = ex.bar + 2;
             const int tokens = a.box * a.boxes * TT;
             mbar_expect_tx(bar, tokens * ((a.y.p ? HB::kSize : 0) + (a.g.p ? HB::kSize : 0) + (a.r.p ? HS::kSize : 0)));
-            if (a.y.p) load_tile(sy, maps.m, a, rank, t * TT, HB::kRow, bar);
-            if (a.g.p) load_tile(sg, maps.m + 1, a, rank, t * TT, HB::kRow, bar);
-            if (a.r.p) load_tile(sr, maps.m + 2, a, rank, t * TT, HS::kRow, bar);
+            if (a.y.p) load_tile(sy, maps.m, a, rank, (int64_t)t * TT, HB::kRow, bar);
+            if (a.g.p) load_tile(sg, maps.m + 1, a, rank, (int64_t)t * TT, HB::kRow, bar);
+            if (a.r.p) load_tile(sr, maps.m + 2, a, rank, (int64_t)t * TT, HS::kRow, bar);
         } else {
             const int nv = exist(t);
             const int64_t c = nv > 0 ? column(t) : 0;
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(con
     for (int turn = 0; tile < tiles; tile += a.groups, ++turn) {
         const int64_t c = column(tile);
         P x[F][T::N], m[T::N], r[T::N];
-        RS out_h(a.h, first, tile * TT, a.n);
+        RS out_h(a.h, first, (int64_t)tile * TT, a.n);
         bool ok = true;
         if constexpr (TMA) ok = norm_wait(ex.bar + 2, turn & 1, ex.hdr);
         else cp_async_wait();
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(con
                 m[k] = T::all(0.f);
                 r[k] = T::all(1.f);
             }
-            if (a.post.kind > CSRT_NORM_SCALE) tile_stats<TT, V, F>(ex, a.post, at, rows, tile * TT, a.n, [] {}, x, m, r);
+            if (a.post.kind > CSRT_NORM_SCALE) tile_stats<TT, V, F>(ex, a.post, at, rows, (int64_t)tile * TT, a.n, [] {}, x, m, r);
             // GATE: CSRT_GATE_*, or -1 for no gate. Stores are spread over the features: in a loop of their own they held up
             // the loads behind them (float32 stream 127 -> 150 us).
             auto pass = [&](auto gate) {
@@ -209,11 +209,11 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(con
             r[k] = T::all(1.f);
         }
         if (stats)
-            tile_stats<TT, V, F>(ex, a.pre, at, rows, tile * TT, a.n, [&] { if (TMA) next(); }, x, m, r);
+            tile_stats<TT, V, F>(ex, a.pre, at, rows, (int64_t)tile * TT, a.n, [&] { if (TMA) next(); }, x, m, r);
         if (!ok)
 #pragma unroll
             for (int k = 0; k < T::N; ++k) r[k] = T::all(NAN);
-        RB out_v(a.v, first, tile * TT, a.n);
+        RB out_v(a.v, first, (int64_t)tile * TT, a.n);
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             const float2 w = wpre[at.row0 + f * at.kStep];

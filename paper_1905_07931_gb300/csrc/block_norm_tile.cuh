@@ -546,6 +546,17 @@ __device__ __forceinline__ void sigmoid2(float g, float &p, float &q) {
     q = fminf(e * p, 1.f);
 }
 
+__device__ __forceinline__ f32x2 above_m128(f32x2 g) {
+    float a, b;
+    unpack2(g, a, b);
+    return pack2(above_m128(a), above_m128(b));
+}
+__device__ __forceinline__ f32x2 within_128(f32x2 g) {
+    float a, b;
+    unpack2(g, a, b);
+    return pack2(within_128(a), within_128(b));
+}
+
 // a(g) and a'(g) of V tokens. GATE: CSRT_GATE_*, known to the compiler, so that the features of a thread's loop are not
 // separated by branches and their latencies overlap.
 template <int GATE, bool FAST, typename P>
@@ -553,10 +564,11 @@ __device__ __forceinline__ void gate_of(P g, P one, P &value, P &slope) {
     value = g;
     slope = one;
     if (GATE == CSRT_GATE_NONE) return;
+    if (GATE == CSRT_GATE_SILU) g = above_m128(g);   // before the sigmoid, which is the same: no second copy of g lives
     P p, q;
     sigmoid2<FAST>(g, p, q);
     value = GATE == CSRT_GATE_SILU ? mul2(p, g) : p;
-    slope = GATE == CSRT_GATE_SILU ? mul2(p, fma2(g, q, one)) : mul2(p, q);
+    slope = GATE == CSRT_GATE_SILU ? mul2(p, fma2(within_128(g), q, one)) : mul2(p, q);
 }
 template <typename F>
 __device__ __forceinline__ void with_gate(int act, F body) {

@@ -570,3 +570,37 @@ def test_forward_over_several_tiles(C, d, n, form):
 @pytest.mark.parametrize("form", LONG_FORMS, ids=lambda f: "-".join(str(x) for x in f))
 def test_backward_over_several_tiles(C, d, n, form):
     test_backward(C, d, n, form)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,n,layout", [(64, 256, "tight"), (1000, 24, "wide"), (513, 33, "odd"), (4096, 1, "tight"), (70000, 1, "tight")])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("act", ["sigmoid", "silu"])
+def test_infinite_gates(C, d, n, layout, dtype, act):
+    """A gate that is infinite has its limits: sigmoid 0 and 1 with slopes 0, silu 0 and infinity with slopes 0 and 1. A NaN
+    stays one, and the gates beside them are as if they were not there. With y = dh = 1 and no norms h is the gate's value,
+    dy too, and dgate its slope."""
+    gen, dt, inf = _gen(d + n), DT[dtype], float("inf")
+    g = _mat(gen, d, n, dt, layout, 2.0)
+    y, dh, h, dr, dy, dg = (_mat(gen, d, n, dt, layout) for _ in range(6))
+    y.fill_(1)
+    dh.fill_(1)
+    kind = torch.randint(0, 8, (d, n), generator=gen, device="cuda")   # 0: -inf, 1: inf, 2: NaN, 3, 4: the largest finite
+    top = torch.finfo(dt).max
+    for k, x in enumerate((-inf, inf, float("nan"), -top, top)):
+        g[kind == k] = x
+    C.block_norm_fwd(y, None, h, None, post=C.Norm("scale"), gate=g, gate_act=act)
+    ws = C.BlockNormWorkspace(d, n)
+    C.block_norm_bwd(None, dh, None, y, dr, dy, ws, post=C.Norm("scale"), gate=g, gate_act=act, dgate=dg)
+    up = (kind == 1) | (kind == 4)
+    value = torch.where(up, torch.where(kind == 1, inf, top) if act == "silu" else 1.0, 0.0).to(dt)
+    slope = (up if act == "silu" else up & False).to(dt)
+    edge = (kind < 5) & (kind != 2)
+    for got, want in ((h, value), (dy, value), (dg, slope)):
+        assert (got[kind == 2].isnan()).all()
+        assert (got[edge] == want[edge]).all()
+    p, s, ep, es = _gate(g.double().nan_to_num(0, 0, 0), act)
+    keep = kind >= 5
+    for name, got, (want, err) in (("h", h, (p, ep)), ("dy", dy, (p, ep)), ("dg", dg, (s, es))):
+        _check(got[keep], want[keep], err[keep] + U * want[keep].abs(), name)
+    assert (dr == dh).all() and ws.status()[0] == 0
