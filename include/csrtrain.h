@@ -523,7 +523,8 @@ int csrt_grad_norm(const csrt_mat *g, int32_t count, float *norm, void *ws, size
  * leaves the factor at 1. max_norm > 0 and finite. No matrix of out may
  * overlap another, or a g of another index (not checked). The blocks of small
  * calls wait for one another (cooperative launch, bounded): a wait that ran
- * out sets CSRT_DEV_TIMEOUT and leaves out as it was. */
+ * out sets CSRT_DEV_TIMEOUT, makes norm[0] and norm[1] NaN and leaves out as it
+ * was; the workspace can be used again. */
 int csrt_grad_clip(const csrt_mat *g, int32_t count, float max_norm, const csrt_mat *out, float *norm, void *ws,
                    size_t ws_bytes, void *stream);
 

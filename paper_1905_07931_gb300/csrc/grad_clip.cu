@@ -284,6 +284,7 @@ __global__ void __launch_bounds__(kGradThreads, 4) grad_scale_kernel(const __gri
 // 16.4 in a stream, two launches 15.0), nor with several units a block (58.7M: 111 us, two launches 110): the second launch
 // reads and writes at the copy rate.
 constexpr int kHoldBytes = kGradUnit * (int)sizeof(float);
+constexpr int kGaveUp = 1 << 30;   // in the count of sums that have come: a wait for them ran out
 
 template <int N>
 __global__ void __launch_bounds__(kGradThreads, 2) grad_clip_kernel(const __grid_constant__ GradArgs<N> a) {
@@ -296,32 +297,42 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_clip_kernel(const __grid
     double s = squares_of(e, base, reinterpret_cast<uint4 *>(hold));
     s = block_sum(s, part);
     if (threadIdx.x == 0) {
+        const int all = (int)gridDim.x;
         a.partial[blockIdx.x] = s;
         __threadfence();
         atomicAdd(a.ticket, 1);
         int seen = 0;
         for (unsigned spin = 0; spin < kSpinLimit; ++spin) {
             asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(a.ticket) : "memory");
-            if (seen == (int)gridDim.x) break;
+            if (seen == all || (seen & kGaveUp) != 0) break;
             if (spin > 16) __nanosleep(20);
         }
-        if (seen != (int)gridDim.x) dev_flag(a.hdr, CSRT_DEV_TIMEOUT);
-        scale = seen == (int)gridDim.x ? 1.f : -1.f;
+        // one outcome for all blocks: the count is complete and stays so, or it is marked before that (each try that fails
+        // met another block's arrival)
+        while (seen != all && (seen & kGaveUp) == 0) {
+            const int old = atomicCAS(a.ticket, seen, seen | kGaveUp);
+            seen = old == seen ? seen | kGaveUp : old;
+            __threadfence();
+        }
+        if (seen != all) dev_flag(a.hdr, CSRT_DEV_TIMEOUT);
+        scale = seen == all ? 1.f : -1.f;
     }
     __syncthreads();
-    if (scale < 0.f) return;   // the others' sums never came: nothing is written
+    const bool come = scale > 0.f;   // else the others' sums never came: nothing is written
     s = 0.;
-    for (int b = threadIdx.x; b < gridDim.x; b += kGradThreads) s += __ldcg(a.partial + b);
+    for (int b = threadIdx.x; come && b < gridDim.x; b += kGradThreads) s += __ldcg(a.partial + b);
     s = block_sum(s, part);
     if (threadIdx.x == 0) {
-        scale = clip_factor(a.max_norm, s, blockIdx.x == 0 ? a.norm : nullptr, a.hdr);
-        // the last block to have seen all of the sums leaves the counters as they were
+        if (come) scale = clip_factor(a.max_norm, s, blockIdx.x == 0 ? a.norm : nullptr, a.hdr);
+        else if (blockIdx.x == 0) a.norm[0] = a.norm[1] = NAN;
+        // the last block to have read the first counter leaves both as they were
         if (atomicAdd(a.ticket + 1, 1) == (int)gridDim.x - 1) {
             a.ticket[1] = 0;
             a.ticket[0] = 0;
         }
     }
     __syncthreads();
+    if (!come) return;
     scale_of(e, base, scale, hold);
 }
 

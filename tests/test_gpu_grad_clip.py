@@ -219,3 +219,26 @@ print("captured")
 """
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=110)
     assert r.returncode == 0 and "captured" in r.stdout, r.stderr
+
+
+def test_wait_that_runs_out(C):
+    """A count of arrived sums that cannot become complete (the test begins it far too high): the call of one launch gives
+    up and says so, out stays as it was, and the workspace serves the next calls, in one launch and in two."""
+    gen = _gen(12)
+    small, large = _tensors(gen, [(300, 100), (7,)], torch.float32), _tensors(gen, [(3000, 1000), (5,)], torch.float32)
+    ws, norm = C.GradWorkspace(), torch.zeros(2, device="cuda")
+    counters = ws.buf[256:264].view(torch.int32)   # behind the status words
+    C.grad_clip(small, 1e6, norm, ws)
+    assert counters.tolist() == [0, 0]
+    counters[0] = 1000
+    before = [t.clone() for t in small]
+    C.grad_clip(small, 1.0, norm, ws)
+    assert ws.status()[0] == C.CSRT_DEV_TIMEOUT
+    assert norm.isnan().all() and all(torch.equal(a, b) for a, b in zip(small, before))
+    assert counters.tolist() == [0, 0]
+    ws.clear_status()
+    for g in (large, small, large):
+        want = _norm(g)
+        C.grad_clip(g, 0.5 * want, norm, ws)
+        assert abs(float(norm[0]) - want) <= 66 * U * want and abs(_norm(g) - 0.5 * want) <= 140 * U * want
+    assert ws.status()[0] == 0
