@@ -108,6 +108,8 @@ class ResidualNet:
             self.extra_ws.append(self.wse)
             self.grads.append(self.dtable)
         if clip is not None:
+            self.dbc = torch.zeros(classes, **f32)   # else its update takes the sums as they are made
+            self.grads.append(self.dbc)
             self.grad_norm = torch.zeros(2, **f32)
             self.wsk = C.GradWorkspace(device=device, stream=stream)
             self.extra_ws.append(self.wsk)
@@ -176,6 +178,8 @@ class ResidualNet:
         """Gradients of everything from ``dlogits`` (the classifier's bias is updated by the step)."""
         s = self.stream
         C.weight_grad_dense(self.dlogits, self.xf, self.gc, self.ws, C.CSRT_PREC_TF32, s)
+        if self.clip is not None:
+            C.bias_grad_sgd(self.dlogits, None, 0.0, self.dbc, s)
         C.spmm_bwd_t(self.wc[self.cur], self.dlogits, self.dxf, self.ws, s)
         if self.norm is not None:
             C.dense_act_bwd(self.dxf, None, "none", self.dv[self.L], stream=s)   # to bfloat16
@@ -199,7 +203,7 @@ class ResidualNet:
         self.forward()
         C.softmax_xent(self.logits, self.labels, self.dlogits, self.loss, s)
         self.backward()
-        if self.clip is not None:   # the classifier's bias is not among them: its gradient is never written
+        if self.clip is not None:
             C.grad_clip(self.grad_list, self.clip, self.grad_norm, self.wsk, stream=s)
         scale = 0.2 * math.sqrt(max(d, h))
         C.orthogonalize(self.g1, self.o1, self.ws1, momentum=self.m1, beta=beta, scale=scale, stream=s)
@@ -219,7 +223,10 @@ class ResidualNet:
         # the classifier: the prox step along the orthogonalised direction, into the other CSR buffer
         C.orthogonalize(self.gc, self.oc, self.wsc, momentum=self.mc, beta=beta,
                         scale=0.2 * math.sqrt(max(self.classes, d)), stream=s)
-        C.bias_grad_sgd(self.dlogits, self.bc, eta, None, s)
+        if self.clip is not None:
+            C.dense_update(self.bc.view(1, -1), self.dbc.view(1, -1), eta, stream=s)
+        else:
+            C.bias_grad_sgd(self.dlogits, self.bc, eta, None, s)
         C.prox_update_compact(self.wc[self.cur], self.oc, eta, lam, self.wc[1 - self.cur], self.ws, s)
         self.cur = 1 - self.cur
         return self.loss

@@ -189,3 +189,29 @@ def test_two_streams_at_once(R):
         got = [s[q] for q in names] + s["dw"] + s["out"]
         assert all(torch.equal(a, b) for a, b in zip(got, w))
         assert all(ws.status()[0] == 0 for ws in workspaces)
+
+
+def test_clipping_takes_the_classifiers_bias(R):
+    """With small inputs most of the gradient is the classifier's bias's: the norm holds it, and its update is scaled with
+    the others'."""
+    net = _net(R, clip=0.01)
+    net.x[0].mul_(1e-3)
+    net.b1.zero_()
+    net.b2.zero_()
+    net.bc.copy_(torch.linspace(-2, 2, net.classes))
+    before = net.bc.clone()
+    net.bc.requires_grad_()
+    _, want = _reference(net)
+    bias = net.bc.grad.double()
+    net.bc.requires_grad_(False)
+    total = math.sqrt(sum(float(w.square().sum()) for w in want.values()) + float(bias.square().sum()))
+    # without it the norm would be 1 - sqrt(1 - 0.5^2) = 13% smaller, or more: far outside tol, which is 4%
+    assert float(bias.norm()) > 0.5 * total and total > 9 * net.clip
+    tol = 2 * math.sqrt(12 * net.L + 2) * 2.0 ** -8
+    net.step(0.003, 0.1)
+    norm, factor = net.grad_norm.tolist()
+    assert abs(norm - total) <= tol * total and abs(factor - net.clip / norm) <= 1e-6 * factor
+    step = 0.003 * factor * bias
+    assert ((net.bc.double() - (before.double() - step)).norm() <= 2 * tol * step.norm() + 2.0 ** -23 * before.double().norm())
+    assert abs(math.sqrt(sum(float(g.double().square().sum()) for g in net.grads)) - net.clip) <= 1e-5 * net.clip
+    assert net.status() == 0
