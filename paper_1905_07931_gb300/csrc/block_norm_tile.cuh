@@ -503,10 +503,10 @@ __device__ __forceinline__ void exchange(Exchange<TT> &e, float (&a)[V], float (
     load_tokens<V>(out + TT + q, y);
 }
 
-// 1 / sqrt(v): the approximation and a Newton step
+// 1 / sqrt(v): the approximation and a Newton step (r first: half of a subnormal v would not be exact)
 __device__ __forceinline__ float rsqrt_near(float v) {
     const float r = rsqrtf(v);
-    return v <= 3.4028235e38f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
+    return v <= 3.4028235e38f ? r * fmaf(-0.5f * r * v, r, 1.5f) : r;
 }
 
 // exp and quotient of the fast sigmoid: 2^-22 and 2^-23 of the result, 2^-24 |g| from the rounded argument

@@ -604,3 +604,19 @@ def test_infinite_gates(C, d, n, layout, dtype, act):
     for name, got, (want, err) in (("h", h, (p, ep)), ("dy", dy, (p, ep)), ("dg", dg, (s, es))):
         _check(got[keep], want[keep], err[keep] + U * want[keep].abs(), name)
     assert (dr == dh).all() and ws.status()[0] == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("eps", [1e-44, 1e-40, 3e-38, 1e-30, 1.0, 1e30])
+@pytest.mark.parametrize("d,n", [(64, 40), (300, 1), (513, 33), (70000, 1)])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_deviation_of_equal_features(C, d, n, kind, eps):
+    """Tokens of zeros: rstd is 1 / sqrt(eps) for every eps that float32 holds (two steps of the root, two of the rest), and
+    the result is the bias."""
+    x = torch.zeros(d, n, device="cuda")
+    rstd, v = torch.empty(n, device="cuda"), torch.full_like(x, float("nan"))
+    b = torch.randn(d, generator=_gen(d), device="cuda")
+    C.block_norm_fwd(None, x, None, v, pre=C.Norm(kind, None, b, eps, torch.empty(n, device="cuda"), rstd))
+    want = float(torch.tensor(eps, dtype=torch.float32)) ** -0.5
+    assert ((rstd.double() - want).abs() <= 4 * U * 2 * want).all()
+    assert torch.equal(v, b[:, None].expand(d, n))
