@@ -235,7 +235,7 @@ __device__ void embed_sort(const EmbedArgs &a, int32_t (*count)[kSortPitch]) {
         __syncthreads();
         for (int64_t k = k0; k < k1; k += 32 * kAhead) {
             int32_t col[kAhead];
-            if (k1 - k0 > 32 * kAhead) fetch(k);   // else they are still there
+            fetch(k);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int64_t at = k + 32 * u + lane;
