@@ -485,8 +485,9 @@ int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *
                         int32_t accumulate, csrt_mat *dr, csrt_mat *dy, csrt_mat *dgate, void *ws, size_t ws_bytes,
                         void *stream);
 
-/* Workspace of the embedding calls (the gradient keeps dx in rows there, and
- * the sorted tokens). */
+/* Workspace of the embedding calls. The gradient keeps dx in rows there, and
+ * the sorted tokens; the lookup needs its status words alone, so that a
+ * workspace for max_n = 0 serves lookups of any size. */
 int csrt_embed_workspace_bytes(int32_t vocab, int32_t d, int32_t max_n, size_t *bytes);
 
 /* csrt_embed_fwd -- x[:, c] = scale * table[tokens[c], :]. table is vocab x d

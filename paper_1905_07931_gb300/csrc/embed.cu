@@ -757,8 +757,8 @@ static size_t embed_bytes(int64_t d, int64_t n) {
     return kWsReservedBytes + 4 * embed_list_bytes(n) + align_up((size_t)n * row, 256) + align_up(chunks * 2 * row, 256);
 }
 
-static int check_embed(const int32_t *tokens, float scale, int32_t vocab, int32_t d, int32_t n, const csrt_mat *out,
-                       const char *out_name, void *ws, size_t ws_bytes) {
+static int check_embed(const int32_t *tokens, float scale, int32_t vocab, int32_t n, const csrt_mat *out,
+                       const char *out_name, void *ws, size_t ws_bytes, size_t need) {
     CSRT_ARG(n == 0 || tokens != nullptr, "tokens is NULL");
     CSRT_TRY(check_vector(reinterpret_cast<const float *>(tokens), "tokens"));
     CSRT_ARG(!vector_meets(reinterpret_cast<const float *>(tokens), n, out), "tokens overlap %s", out_name);
@@ -766,8 +766,7 @@ static int check_embed(const int32_t *tokens, float scale, int32_t vocab, int32_
     CSRT_ARG(vocab < INT32_MAX, "the table has too many rows");
     CSRT_ARG(ws != nullptr, "workspace is NULL");
     CSRT_ARG((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
-    if (ws_bytes < embed_bytes(d, n))
-        return fail(CSRT_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, embed_bytes(d, n));
+    if (ws_bytes < need) return fail(CSRT_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, need);
     return CSRT_OK;
 }
 
@@ -883,7 +882,7 @@ int csrt_embed_fwd(const csrt_mat *table, const int32_t *tokens, float scale, cs
     const int32_t vocab = table->rows, d = table->cols, n = x->cols;
     CSRT_TRY(check_shape(x, "x", d, n));
     CSRT_ARG(!clash(x, table), "x overlaps table");
-    CSRT_TRY(check_embed(tokens, scale, vocab, d, n, x, "x", ws, ws_bytes));
+    CSRT_TRY(check_embed(tokens, scale, vocab, n, x, "x", ws, ws_bytes, kWsReservedBytes));
     if (d == 0 || n == 0) return CSRT_OK;
     EmbedArgs a = embed_args(table, x, tokens, vocab, d, n, scale, ws);
     a.out_vec = tma_rows_ok(x->data, x->ld, dt_size(x->dtype));
@@ -897,7 +896,7 @@ int csrt_embed_bwd(const csrt_mat *dx, const int32_t *tokens, float scale, int32
     const int32_t vocab = dtable->rows, d = dx->rows, n = dx->cols;
     CSRT_TRY(check_shape(dtable, "dtable", vocab, d));
     CSRT_ARG(!clash(dtable, dx), "dtable overlaps dx");
-    CSRT_TRY(check_embed(tokens, scale, vocab, d, n, dtable, "dtable", ws, ws_bytes));
+    CSRT_TRY(check_embed(tokens, scale, vocab, n, dtable, "dtable", ws, ws_bytes, embed_bytes(d, n)));
     if (d == 0 || vocab == 0) return CSRT_OK;
     EmbedArgs a = embed_args(dx, dtable, tokens, vocab, d, n, scale, ws);
     a.accumulate = accumulate != 0;

@@ -535,7 +535,8 @@ class BlockNormWorkspace(Workspace):
 
 
 class EmbedWorkspace(Workspace):
-    """Workspace of the embedding calls for a table of vocab rows of d features and at most max_n tokens."""
+    """Workspace of the embedding calls for a table of vocab rows of d features and at most max_n tokens (lookups alone: 0
+    serves any number)."""
 
     def __init__(self, vocab: int, d: int, max_n: int, device="cuda", stream=None):
         nbytes = c_size_t(0)

@@ -190,3 +190,15 @@ def test_python_side_refuses(C):
         C.embed_fwd(None, torch.zeros(4, dtype=torch.int32), torch.zeros(4, 4), None)
     with pytest.raises(ValueError, match="tensor 0 must be"):
         C.TensorList([torch.zeros(4, 4, 4).transpose(0, 1)])
+
+
+def test_lookups_need_the_status_words_alone(C):
+    """Whatever the number of tokens and features; the gradient asks for more."""
+    L, n = C.lib(), ctypes.c_size_t(0)
+    assert L.csrt_embed_workspace_bytes(100, 4096, 0, ctypes.byref(n)) == 0
+    few = n.value
+    assert L.csrt_embed_workspace_bytes(7, 2 ** 31 - 1, 0, ctypes.byref(n)) == 0 and n.value == few
+    table, x, tok = _m(C, 1, 100, 16, dtype=0), _m(C, 2, 16, 24), ctypes.c_void_p(A * 3)
+    _expect(C, L.csrt_embed_fwd(table, tok, F(1), x, WS, ctypes.c_size_t(few - 1), None), f"needs {few}", C.CSRT_ERR_WORKSPACE)
+    _expect(C, L.csrt_embed_bwd(x, tok, F(1), 0, table, WS, ctypes.c_size_t(few), None), f"workspace has {few} bytes",
+            C.CSRT_ERR_WORKSPACE)

@@ -241,3 +241,20 @@ def test_tokens_beyond_the_table_in_every_sort(C, vocab, n, accumulate):
     C.embed_bwd(dx, tok, a, ws, accumulate=accumulate)
     assert ws.status()[0] == C.CSRT_DEV_INVALID
     assert torch.equal(a, b)
+
+
+def test_lookup_needs_no_workspace_for_its_tokens(C):
+    """A program that only looks tokens up keeps the status words alone; the gradient asks for more."""
+    gen = _gen(6)
+    vocab, d, n = 90, 40, 3000
+    w, tok = _mat(gen, vocab, d, torch.float32), _tokens(gen, vocab, n, "pad")
+    ws = C.EmbedWorkspace(vocab, d, 0)
+    assert ws.nbytes < 1 << 17
+    x = torch.full((d, n), float("nan"), device="cuda")
+    C.embed_fwd(w, tok, x, ws)
+    assert torch.equal(x, torch.where(tok[:, None] >= 0, w[tok.long().clamp_min(0)], 0.0).t())
+    tok[7] = vocab
+    C.embed_fwd(w, tok, x, ws)
+    assert ws.status()[0] == C.CSRT_DEV_INVALID
+    with pytest.raises(C.CsrtError, match="workspace"):
+        C.embed_bwd(x, tok, w, ws)
