@@ -871,6 +871,7 @@ extern "C" {
 int csrt_embed_workspace_bytes(int32_t vocab, int32_t d, int32_t max_n, size_t *bytes) {
     CSRT_ARG(bytes != nullptr, "bytes is NULL");
     CSRT_ARG(vocab >= 0 && d >= 0 && max_n >= 0, "negative size");
+    CSRT_ARG((int64_t)d * max_n <= kMaxElems, "%d x %d activations are too large", d, max_n);   // no call takes them
     *bytes = embed_bytes(d, max_n);
     return CSRT_OK;
 }

@@ -202,3 +202,11 @@ def test_lookups_need_the_status_words_alone(C):
     _expect(C, L.csrt_embed_fwd(table, tok, F(1), x, WS, ctypes.c_size_t(few - 1), None), f"needs {few}", C.CSRT_ERR_WORKSPACE)
     _expect(C, L.csrt_embed_bwd(x, tok, F(1), 0, table, WS, ctypes.c_size_t(few), None), f"workspace has {few} bytes",
             C.CSRT_ERR_WORKSPACE)
+
+
+def test_embed_workspace_sizes_do_not_wrap(C):
+    """Sizes that no call takes are refused."""
+    L, n = C.lib(), ctypes.c_size_t(0)
+    assert L.csrt_embed_workspace_bytes(9, 2 ** 20, 2 ** 20, ctypes.byref(n)) == 0 and n.value > 2 ** 42
+    for d, max_n in ((2 ** 31 - 1, 2 ** 31 - 1), (2 ** 20 + 1, 2 ** 20), (2 ** 31 - 1, 2 ** 30)):
+        _expect(C, L.csrt_embed_workspace_bytes(9, d, max_n, ctypes.byref(n)), "too large")
