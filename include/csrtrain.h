@@ -479,7 +479,7 @@ int csrt_block_norm_workspace_bytes(int32_t d, int32_t max_n, size_t *bytes);
  * dr, dy and dgate may be NULL; dy's presence says whether there is a y. dr may
  * be dh itself; apart from that no output overlaps anything else. dv, gate, y,
  * dy and dgate have one type; dh, h and dr that type or float32. A wait that
- * ran out sets CSRT_DEV_TIMEOUT. */
+ * ran out sets CSRT_DEV_TIMEOUT and gives NaN. */
 int csrt_block_norm_bwd(const csrt_mat *dv, const csrt_mat *dh, const csrt_mat *h, const csrt_norm *pre,
                         const csrt_mat *y, const csrt_norm *post, const csrt_mat *gate, int32_t gate_act, float r_scale,
                         int32_t accumulate, csrt_mat *dr, csrt_mat *dy, csrt_mat *dgate, void *ws, size_t ws_bytes,

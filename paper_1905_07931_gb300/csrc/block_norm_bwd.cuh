@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
         if (a.pre.kind > CSRT_NORM_SCALE) {
             P sa[T::N], sb[T::N];
 #pragma unroll
-            for (int k = 0; k < T::N; ++k) sa[k] = sb[k] = T::all(0.f);
+            for (int k = 0; k < T::N; ++k) sa[k] = sb[k] = T::all(ok ? 0.f : NAN);
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 const float w = weights[at.row0 + f * at.kStep].z;
@@ -239,6 +239,11 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
                 sums.add(kSumPreW, f, T::sum(tw));
                 sums.add(kSumPreB, f, T::sum(tb));
             }
+        if (!ok)
+#pragma unroll
+            for (int f = 0; f < F; ++f)
+#pragma unroll
+                for (int k = 0; k < T::N; ++k) x[f][k] = T::all(NAN);
         if (a.dr.p) {
             RS out_dr(a.dr, first, tile * TT, a.n);
 #pragma unroll
@@ -257,15 +262,13 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_bwd_tile_kernel(con
                 stat = statistics(tile + a.groups);
             }
         };
-        if (!ok)
-#pragma unroll
-            for (int f = 0; f < F; ++f)
-#pragma unroll
-                for (int k = 0; k < T::N; ++k) x[f][k] = T::all(NAN);
         if (a.dy.p) {
             if constexpr (TMA)
                 if (a.y.p) ok = norm_wait(ex.bar + 3, turn & 1, ex.hdr) && ok;
             own_stats(1);
+            if (!ok)
+#pragma unroll
+                for (int k = 0; k < T::N; ++k) r[k] = T::all(NAN);
 #pragma unroll
             for (int k = 0; k < T::N; ++k) sa[k] = sb[k] = T::all(0.f);
             RB out_dg(a.dg, first, tile * TT, a.n);

@@ -6,10 +6,10 @@
 namespace csrt {
 
 // Mean (negated) and reciprocal deviation of this thread's V tokens, over all features; `rows` of the block's features
-// exist, x is zero beyond them. Written out by the cluster's first block.
+// exist, x is zero beyond them. Written out by the cluster's first block. zero: 0, or NaN where a wait for x ran out.
 template <int TT, int V, int F, typename FREED>
 __device__ __forceinline__ void tile_stats(Exchange<TT> &ex, const NormSide &s, const Place<TT, V> &at, int rows, int64_t c0,
-                                           int32_t n, FREED freed, const typename Tok<V>::P (&x)[F][Tok<V>::N],
+                                           int32_t n, float zero, FREED freed, const typename Tok<V>::P (&x)[F][Tok<V>::N],
                                            typename Tok<V>::P (&m)[Tok<V>::N], typename Tok<V>::P (&r)[Tok<V>::N]) {
     typedef Tok<V> T;
     float a[V], b[V];
@@ -25,12 +25,12 @@ __device__ __forceinline__ void tile_stats(Exchange<TT> &ex, const NormSide &s, 
     };
     typename T::P sq[T::N];
 #pragma unroll
-    for (int k = 0; k < T::N; ++k) sq[k] = T::all(0.f);
+    for (int k = 0; k < T::N; ++k) sq[k] = T::all(zero);
     if (s.kind == CSRT_NORM_LAYER) {
         float cnt = 0.f;
         typename T::P sum[T::N];
 #pragma unroll
-        for (int k = 0; k < T::N; ++k) sum[k] = T::all(0.f);
+        for (int k = 0; k < T::N; ++k) sum[k] = T::all(zero);
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             cnt += at.row0 + f * at.kStep < rows ? 1.f : 0.f;
@@ -140,8 +140,8 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(con
         const int64_t c = column(tile);
         P x[F][T::N], m[T::N], r[T::N];
         RS out_h(a.h, first, (int64_t)tile * TT, a.n);
-        bool ok = true;
-        if constexpr (TMA) ok = norm_wait(ex.bar + 2, turn & 1, ex.hdr);
+        float one = 1.f;   // NaN where the wait ran out: all that follows from the inputs is
+        if constexpr (TMA) one = norm_wait(ex.bar + 2, turn & 1, ex.hdr) ? 1.f : NAN;
         else cp_async_wait();
         const int off_r = offset(HS(), a.r, c);
         if (a.y.p) {
@@ -151,9 +151,9 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(con
 #pragma unroll
             for (int k = 0; k < T::N; ++k) {
                 m[k] = T::all(0.f);
-                r[k] = T::all(1.f);
+                r[k] = T::all(one);
             }
-            if (a.post.kind > CSRT_NORM_SCALE) tile_stats<TT, V, F>(ex, a.post, at, rows, (int64_t)tile * TT, a.n, [] {}, x, m, r);
+            if (a.post.kind > CSRT_NORM_SCALE) tile_stats<TT, V, F>(ex, a.post, at, rows, (int64_t)tile * TT, a.n, one - 1.f, [] {}, x, m, r);
             // GATE: CSRT_GATE_*, or -1 for no gate. Stores are spread over the features: in a loop of their own they held up
             // the loads behind them (float32 stream 127 -> 150 us).
             auto pass = [&](auto gate) {
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(con
             for (int f = 0; f < F; ++f) {
                 HS::read(sr, f, off_r, x[f]);
 #pragma unroll
-                for (int k = 0; k < T::N; ++k) x[f][k] = mul2(x[f][k], T::all(a.r_scale));
+                for (int k = 0; k < T::N; ++k) x[f][k] = mul2(x[f][k], T::all(a.r_scale * one));
                 if (a.h.p) out_h.put(stage, f, at.row0, rows, x[f]);
             }
         }
@@ -209,10 +209,7 @@ __global__ void __launch_bounds__(kNormThreads, BLOCKS) norm_fwd_tile_kernel(con
             r[k] = T::all(1.f);
         }
         if (stats)
-            tile_stats<TT, V, F>(ex, a.pre, at, rows, (int64_t)tile * TT, a.n, [&] { if (TMA) next(); }, x, m, r);
-        if (!ok)
-#pragma unroll
-            for (int k = 0; k < T::N; ++k) r[k] = T::all(NAN);
+            tile_stats<TT, V, F>(ex, a.pre, at, rows, (int64_t)tile * TT, a.n, 0.f, [&] { if (TMA) next(); }, x, m, r);
         RB out_v(a.v, first, (int64_t)tile * TT, a.n);
 #pragma unroll
         for (int f = 0; f < F; ++f) {

@@ -620,3 +620,84 @@ def test_deviation_of_equal_features(C, d, n, kind, eps):
     want = float(torch.tensor(eps, dtype=torch.float32)) ** -0.5
     assert ((rstd.double() - want).abs() <= 4 * U * 2 * want).all()
     assert torch.equal(v, b[:, None].expand(d, n))
+
+
+@pytest.fixture(scope="module")
+def late(C, tmp_path_factory):
+    """The binding over a build whose waits count as run out (late_waits.cu); everything else is the library's."""
+    import ctypes
+    import os
+    import subprocess
+    from paper_1905_07931_gb300 import build
+    here = os.path.dirname(os.path.abspath(__file__))
+    so = str(tmp_path_factory.mktemp("late") / "late_waits.so")
+    r = subprocess.run([build.nvcc(), *build.ARCH, *build.NVCC_FLAGS, "-shared", "-o", so, os.path.join(here, "late_waits.cu"),
+                        "-Xlinker", build.LIB, "-Xlinker", "-Bsymbolic", "-Xlinker", "-rpath=" + build.LIBDIR],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    real, over = C.lib(), ctypes.CDLL(so)
+    names = ("csrt_block_norm_fwd", "csrt_block_norm_bwd")
+    for name in names:
+        getattr(over, name).argtypes = C._SIGS[name]
+
+    class Lib:
+        def __getattr__(self, name):
+            return getattr(over if name in names else real, name)
+
+    return Lib()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,n", [(300, 8000), (300, 8001), (100, 8000), (1500, 40)])
+def test_results_of_waits_that_run_out(C, late, monkeypatch, d, n):
+    """Waits for copies (whole vectors) and for the other blocks of a cluster (more than 128 features): what they guard is
+    NaN, h and the statistics as well as v, dr as well as dy; the backward call is flagged; the next call is right."""
+    form = ("bf16", "bf16", "layer", "rms", "silu", True, "tight")
+    gen, s = _inputs(d, n, form)
+    P = C.Norm("layer", s["wpost"], s["bpost"], EPS, *(torch.zeros(n, device="cuda") for _ in range(2)),
+               *(torch.zeros(d, device="cuda") for _ in range(2)))
+    Q = C.Norm("rms", s["wpre"], s["bpre"], EPS, None, torch.zeros(n, device="cuda"), *(torch.zeros(d, device="cuda") for _ in range(2)))
+    h, v, dr, dy, dg = (torch.zeros_like(s["y"]) for _ in range(5))
+    ws = C.BlockNormWorkspace(d, n)
+
+    def fwd(y=s["y"], r=s["r"], v=v, post=P, pre=Q, gate=s["g"]):
+        for t in (h, v, P.mean, P.rstd, Q.rstd):
+            if t is not None:
+                t.zero_()
+        C.block_norm_fwd(y, r, h, v, post=post, pre=pre, gate=gate, gate_act="silu")
+
+    def bwd(dv=s["y"], dh=s["r"], post=P, pre=Q):
+        for t in (dr, dy, dg, P.dweight, P.dbias, Q.dweight, Q.dbias):
+            t.zero_()
+        ws.clear_status()
+        C.block_norm_bwd(dv, dh, h, s["y"], dr, dy, ws, post=post, pre=pre, gate=s["g"], gate_act="silu", dgate=dg)
+
+    def nan(*tensors):
+        return all(bool(t.isnan().all()) for t in tensors)
+
+    with monkeypatch.context() as m:
+        m.setattr(C, "lib", lambda: late)
+        fwd()
+        assert nan(h, v, P.rstd, Q.rstd, P.mean)
+        fwd(v=None, pre=None)
+        assert nan(h, P.rstd)
+        if n % 8 == 0:   # copies
+            fwd(y=None, post=None, gate=None)
+            assert nan(h, v, Q.rstd)
+            fwd(v=None, pre=None, post=None)
+            assert nan(h)
+        h.copy_(s["r"])
+        for t in (P.rstd, Q.rstd):
+            t.fill_(1)
+        P.mean.zero_()
+        bwd()
+        assert nan(dr, dy, dg, P.dweight, P.dbias) and ws.status()[0] == C.CSRT_DEV_TIMEOUT
+        if n % 8 == 0:
+            bwd(dv=None, pre=None)
+            assert nan(dr, dy, dg) and ws.status()[0] == C.CSRT_DEV_TIMEOUT
+    fwd()
+    (hh, eh), (vv, ev), *_ = _forward(s, "layer", "rms", "silu", 1.0)
+    _check(h, hh, eh, "h")
+    _check(v, vv, ev, "v")
+    bwd()
+    assert dr.isfinite().all() and dy.isfinite().all() and ws.status()[0] == 0
