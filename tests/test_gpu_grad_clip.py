@@ -242,3 +242,33 @@ def test_wait_that_runs_out(C):
         C.grad_clip(g, 0.5 * want, norm, ws)
         assert abs(float(norm[0]) - want) <= 66 * U * want and abs(_norm(g) - 0.5 * want) <= 140 * U * want
     assert ws.status()[0] == 0
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("numel,offset,steps", [(3 * 8192 * 304, 0, 6.5), (8192 * 4096 + 3, 0, 6.5), (8192 * 512 + 1000, 1, 17)])
+def test_norms_of_long_sums(C, dt, numel, offset, steps):
+    """The squares of 32 entries are summed in float32, all else in float64. Whole vectors: eight products on each of four sums
+    (a rounding each), two additions, one more for an entry behind the last vector: 11 x 2^-24 of the sum, half of it of the
+    root, which is rounded once. Off the 16-byte grid: 32 roundings one after the other, and the root's."""
+    gen = _gen(numel % 1000)
+    t = torch.rand(numel + offset, generator=gen, device="cuda").to(DT[dt])[offset:]
+    want = float(t.double().square().sum()) ** 0.5
+    ws, norm = C.GradWorkspace(), torch.zeros(2, device="cuda")
+    C.grad_norm([t], norm, ws)
+    assert abs(float(norm[0]) - want) <= steps * U * 1.0001 * want
+    C.grad_clip([t], 0.5 * want, norm, ws, out=[torch.empty(numel, device="cuda")])
+    assert abs(float(norm[0]) - want) <= steps * U * 1.0001 * want
+
+
+def test_norm_beyond_float32(C):
+    """Finite entries whose norm float32 does not hold: it is returned as infinite, and they are clipped as any others."""
+    g = [torch.full((1000,), 3e38, device="cuda"), torch.full((40, 50), -2e38, device="cuda")]
+    want = _norm(g)
+    ws, norm = C.GradWorkspace(), torch.zeros(2, device="cuda")
+    out = [torch.empty_like(t) for t in g]
+    C.grad_clip(g, 1e38, norm, ws, out=out)
+    assert float(norm[0]) == math.inf and abs(float(norm[1]) - 1e38 / want) <= 66 * U * 1e38 / want
+    for a, b in zip(g, out):
+        exact = a.double() * 1e38 / want
+        assert ((b.double() - exact).abs() <= 70 * U * exact.abs()).all()
+    assert ws.status()[0] == 0
