@@ -327,7 +327,7 @@ static NormTile norm_fwd_choice(const NormArgs &a, bool in, bool out, bool wide)
     if (!in) return d <= 2048 ? kTile32x4 : kTile16x4;
     // unaligned results stage through more of it (4096 x 8191: 111, on 8 x 32 142)
     if (d <= 4096 && (!out || tiles * ceil_div<int64_t>(d, 256) <= 2 * num_sms())) return kTile32x4;
-    // 32 tokens of 512 features of a float32 stream leave one block an SM (4096 x 8192: 129, on 4 x 16 111)
+    // 32 tokens of 512 features of a float32 stream leave one block an SM (4096 x 8192: 129, on 4 x 16 111, 109 with tiles counted in 32 bits)
     return wide && d > 2048 ? kTile16x4 : kTile32x8;
 }
 
@@ -363,9 +363,9 @@ static NormTile norm_bwd_choice(const NormArgs &a, bool in, bool wide, bool f32_
     if (!in) return d <= 4096 ? kTile16x2 : d <= 8192 ? kTile8x2 : kTile8x4;
     // few tokens: one cluster, which writes the sums over them itself (4096 x 24 on two: 10.5)
     if (d <= 4096 && tiles * ceil_div<int64_t>(d, 256) <= num_sms()) return kTile32x4;
-    // 4096 x 8192 with a float32 stream: 224, on 4 x 32, which leaves one block an SM, 238; 2048 x 8192: 96 and 122
+    // 4096 x 8192 with a float32 stream: 226, on 4 x 32, which leaves one block an SM, 238; 2048 x 8192: 96 and 122
     if (f32_stream && d <= 4096) return kTile16x2;
-    // 2048 x 8192: 67 on 4 x 32, 70 on 4 x 16; 4096 x 8192: 148 and 130 (1 to 2 more since 1 - sigmoid keeps its digits)
+    // 2048 x 8192: 67 on 4 x 32, 70 on 4 x 16; 4096 x 8192: 148 and 130 (since 1 - sigmoid keeps its digits 68 and 131)
     return d <= 2048 ? kTile32x4 : d <= 8192 ? kTile16x4 : kTile8x4;
 }
 

@@ -65,8 +65,9 @@ __device__ __forceinline__ float within_128(float g) {
     return g;
 }
 
-// a(g) and a'(g). FAST takes the fast exponential and quotient: the sigmoid is off by (4 + 1.2 |g|) 2^-23 of itself, 2^-18 where
-// it is above 2^-24, far below a 16-bit rounding. float32 matrices take the others.
+// a(g) and a'(g). FAST, by the type of g, takes the fast exponential and quotient: the sigmoid is off by (4 + 1.2 |g|) 2^-23 of
+// itself, in a float32 h and the norms' float32 gradients too. g is then a value of 16 bits, whose own half step moves the sigmoid
+// by (1 - p) |g| 2^-9 (bfloat16) or 2^-12. float32 gates take the others.
 template <bool FAST>
 __device__ __forceinline__ void gate_both(float g, int act, float &value, float &slope) {
     value = g;

@@ -138,9 +138,10 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
 // gradient would fetch 32 bytes for every two).
 //
 // Up to kRankTokens tokens are sorted by counting: a token's place is the number of tokens that come before it. That is n^2
-// comparisons, spread over all SMs (the launch takes 6 us for 777 tokens of 1000 features and 26 for 8000 of 200, 43 for 8192
-// of 4096, where the turn is longer), while the radix sort below takes 16 us a digit of 8192 tokens; from there on the turn of
-// dx hides the radix sort (features by hundreds).
+// comparisons, spread over all SMs: the launch takes 5 us for 777 tokens of 1000 features, 24 for 8000 of 200 and 28 for 8192 of
+// 4096, where the turn is longer. The radix sort below takes 28 us a digit of 16385 tokens and 44 of 32768, in one block. Around
+// the limit, two digits: 16384 tokens of 4096 features take 71 us by counting and 79 by digits, of 512 features 63 and 50. The
+// turn of dx hides neither.
 //
 // The radix sort is stable, 8 bits a pass, by one block. Each warp owns a contiguous run of tokens; counts are kept per digit
 // and warp, so that a scan of them in that order gives every warp its places.
@@ -158,8 +159,8 @@ __device__ __forceinline__ int embed_passes(int32_t vocab) {   // digits of the 
     return p;
 }
 
-// The lanes of this warp with the same digit (eight ballots are far shorter than a match of 32 different values:
-// 17 us a pass over 8192 tokens with it).
+// The lanes of this warp with the same digit, by eight ballots (with a match in their place the launch takes 42 for 50 us, two
+// digits of 16385 tokens as frequent as in text).
 __device__ __forceinline__ unsigned same_digit(int digit, bool in) {
     unsigned m = __ballot_sync(0xffffffffu, in);
     if (!in) m = ~m;

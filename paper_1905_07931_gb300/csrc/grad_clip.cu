@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kGradThreads, 4) grad_scale_kernel(const __gri
 
 // Norm and scaling in one launch, for no more units than two blocks an SM: each block keeps its unit in shared memory, waits
 // for the others' sums (cooperative launch: all run at the same time), adds them all by itself in one order and scales.
-// 60 tensors of 1 to 100000: 7.1 us, in two launches 9.2. With four blocks an SM it is no faster (4.8M float32 in 18 tensors
+// 60 tensors of 1 to 100000: 7.2 us, in two launches 9.2. With four blocks an SM it is no faster (4.8M float32 in 18 tensors
 // 16.4 in a stream, two launches 15.0), nor with several units a block (58.7M: 111 us, two launches 110): the second launch
 // reads and writes at the copy rate.
 constexpr int kHoldBytes = kGradUnit * (int)sizeof(float);
