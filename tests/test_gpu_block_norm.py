@@ -548,7 +548,7 @@ def test_gradient_of_open_and_shut_gates(C, d, n, layout, dtype, act):
         _check(dg, slope, err * slope.abs() + p * (err * x.abs() * q + 2 * U * (1 + x.abs() * q)), "slope")
 
 
-# A cluster walks over several tiles of tokens (a GB300 holds 14 to 150 of them, three tiles each at least): whole vectors,
+# A cluster walks over several tiles of tokens (a GB300 holds about 14 to 150 of them: two tiles each or more): whole vectors,
 # results that end inside one, rows off the 16-byte grid, every width of the choice of tiles
 LONG = [(784, 15008), (2048, 6001), (4096, 3608), (4096, 3605), (4096, 1201), (6000, 1504), (9216, 800), (12000, 401)]
 LONG_FORMS = [("bf16", "bf16", "rms", "rms", "sigmoid", False, "tight"),
